@@ -461,6 +461,120 @@ gp_status gp_forest_tree(const gp_forest *forest, int32_t tree, int32_t capacity
 
 void gp_forest_free(gp_forest *forest);
 
+/* ---------------------------------------------------------------- sequence surrogates */
+
+/* Operators of a surrogate that reads the tuning history as a sequence (beside the GP
+ * value model of Sec. 3.2 and the forest of Sec. 4.2): attention over histories packed in
+ * one batch, with its gradient, and the log probabilities of an output row with theirs.
+ * Definitions:
+ *
+ * Document d (one tuning run) has the query rows [q_begin[d], q_end[d]) and the key rows
+ * [k_begin[d], k_end[d]); Lq, Lk their numbers. Query i (from 0) stands at position
+ * pos(i) = i + Lk - Lq and key j at j, so the last query stands on the last key. Query i
+ * sees the keys of its own document that
+ *   - causal == 0: all of them (candidates that read the observations of a run);
+ *   - causal != 0: j <= pos(i), and, with prefix, also j < prefix[d] (observations that
+ *     every row of the run reads).
+ * Score of a visible pair, z = scale q_i . k_j:
+ *   s = (cap > 0 ? cap tanh(z / cap) : z) + b(j - pos(i)),
+ * b = 0, or -slopes[h] |delta|, or table[h][bucket(delta)]. Buckets: per_side distance
+ * classes, class c holding bucket_start[c] <= a < bucket_start[c + 1] (the last one every
+ * a from its start on). One side: a = max(-delta, 0). Two sides: a = |delta|, and keys
+ * ahead (delta > 0) have the classes per_side.. of their own.
+ *   out_i = sum_j softmax_j(s_ij) v_j,  lse_i = log sum_j e^s_ij.
+ * A query that sees no key, or whose scores are all -inf, has out = 0, lse = -inf and no
+ * gradient. Values of keys that a query does not see never reach its result, whatever they
+ * hold (NaN included). The gradient takes finite q, k, v and dout within a document; rows
+ * outside every document may hold anything there too.
+ *
+ * Query rows h of key head h / (heads / kv_heads) share keys and values; gradients of a
+ * key head are the sums over its query heads. Products take the 16-bit inputs exactly and
+ * add in fp32; probabilities and score gradients are rounded to the inputs' type where they
+ * enter the second products (fp16: at a power-of-two factor that keeps them normal); score
+ * arithmetic, sums, lse and the table's gradient are fp32 until the results are rounded. */
+typedef enum { GP_BF16 = 0, GP_FP16 = 1, GP_FP32 = 2 } gp_dtype;
+
+/* Rows x heads x dim values in device memory: element (r, h, c) at data + r row + h head
+ * + c (strides in elements, multiples of 8; data 16-byte aligned; row <= 2^23). */
+typedef struct {
+  void *data;
+  int64_t row;
+  int64_t head;
+} gp_heads;
+
+typedef struct {
+  int32_t dtype;             /* GP_BF16 or GP_FP16: q, k, v, out, table and gradients */
+  int32_t heads, kv_heads;   /* heads a multiple of kv_heads */
+  int32_t dim;               /* head size: a multiple of 8, 8..128 */
+  int32_t n_docs;            /* >= 0 */
+  int32_t q_rows, k_rows;    /* rows of q (out, dout, dq) and of k, v (dk, dv) */
+  int32_t max_q, max_k;      /* no document is longer than these */
+  /* device int32[n_docs]; documents' query rows must not overlap; ranges are clipped to
+   * 0..q_rows and 0..k_rows */
+  const int32_t *q_begin, *q_end, *k_begin, *k_end;
+  const int32_t *prefix;     /* device int32[n_docs] or NULL; causal only */
+  int32_t causal;
+  float scale;               /* finite, > 0 */
+  float cap;                 /* 0: none; else finite, > 0 */
+  const float *slopes;       /* device float[heads] or NULL */
+  int32_t per_side;          /* 0: no table; else 1..64 */
+  int32_t two_sided;
+  const int32_t *bucket_start; /* host int32[per_side]: 0, then ascending, last <= 1024 */
+} gp_attention;
+
+/* Device workspace of gp_attend (with_grad = 0) or gp_attend_grad (1): 0 if none is needed;
+ * SIZE_MAX if the description is invalid (gp_last_error says why). */
+size_t gp_attend_workspace_bytes(const gp_attention *att, int32_t with_grad);
+
+/* out and lse (device float[heads][q_rows]) of every query row that a document has; other
+ * rows are not written. table: device [heads][buckets] of dtype, given exactly when
+ * per_side > 0 (buckets = per_side, or 2 per_side with two_sided); not with slopes. The
+ * workspace may be NULL if none is needed. Asynchronous on `stream`; the work is not
+ * synchronised with other streams. Deterministic. */
+gp_status gp_attend(const gp_attention *att, const gp_heads *q, const gp_heads *k,
+                    const gp_heads *v, const void *table, const gp_heads *out, float *lse,
+                    void *workspace, size_t ws_bytes, void *stream);
+
+/* Gradients of a loss with dout = dloss/dout: dq, dk, dv, and dtable (device
+ * [heads][buckets] of dtype, overwritten) when there is a table. out and lse are those of
+ * gp_attend with the same arguments. dk and dv of key rows that no document has, and dq of
+ * query rows that none has, are not written; documents' key rows must not overlap here.
+ * Asynchronous; deterministic (sums have a fixed order). */
+gp_status gp_attend_grad(const gp_attention *att, const gp_heads *q, const gp_heads *k,
+                         const gp_heads *v, const void *table, const gp_heads *out,
+                         const float *lse, const gp_heads *dout, const gp_heads *dq,
+                         const gp_heads *dk, const gp_heads *dv, void *dtable, void *workspace,
+                         size_t ws_bytes, void *stream);
+
+/* Log probabilities of rows of logits x (device, dtype GP_BF16 / GP_FP16 / GP_FP32, row
+ * stride `stride` elements, `width` entries): with p = softmax(scale x),
+ *   lse = log sum e^(scale x), logp = log p[target], entropy = -sum p log p,
+ *   top_logp / top_id: the `top` largest log p and their entries, larger first, the lower
+ *   entry first among equal logits.
+ *  target   device int64[rows] or NULL; a row whose target is outside 0..width-1 has none:
+ *           logp = 0
+ *  top      0..min(width, 128)
+ *  logp, entropy, lse: device float[rows], each may be NULL; top_logp, top_id: device
+ *           float[rows][top], int64[rows][top], required with top > 0
+ * -inf marks an entry as ruled out (p = 0, no part in the entropy); a row of nothing else
+ * has lse = logp = -inf and entropy 0. A row with a NaN or +inf gives NaN; a NaN is never
+ * an alternative (top_id = -1 if no entry is left).
+ * Workspace: gp_logprob_workspace_bytes (0: may be NULL). Asynchronous; deterministic. */
+size_t gp_logprob_workspace_bytes(int32_t rows, int32_t width, int32_t top);
+gp_status gp_logprob(int32_t dtype, const void *x, int64_t stride, int32_t rows, int32_t width,
+                     float scale, const int64_t *target, int32_t top, float *logp,
+                     float *entropy, float *lse, float *top_logp, int64_t *top_id,
+                     void *workspace, size_t ws_bytes, void *stream);
+
+/* dx = scale (g_logp (1[target] - p) - g_entropy p (log p + entropy)), of x's type, row
+ * stride dx_stride. lse and entropy are gp_logprob's; g_logp (with target) and g_entropy
+ * (with entropy) device float[rows] or NULL. A row without a target takes nothing from
+ * g_logp, a row of ruled out entries has gradient 0. dx may be x. Asynchronous. */
+gp_status gp_logprob_grad(int32_t dtype, const void *x, int64_t stride, int32_t rows,
+                          int32_t width, float scale, const int64_t *target, const float *lse,
+                          const float *entropy, const float *g_logp, const float *g_entropy,
+                          void *dx, int64_t dx_stride, void *stream);
+
 /* ---------------------------------------------------------------- inspection */
 
 /* Bytes of workspace needed by the debug calls below for `count` configurations. */

@@ -10,6 +10,7 @@
 #include <vector>
 
 #include "common.h"
+#include "seq.h"
 
 using namespace bgp;
 
@@ -848,6 +849,14 @@ int stream_cus(hipStream_t s) {
   }
   return ncu;
 }
+
+}  // namespace
+// For the entry points of seq_abi.hip.
+namespace bgp {
+gp_status seq_fail(gp_status st, const std::string &msg) { return fail(st, msg); }
+int seq_cus(hipStream_t s) { return stream_cus(s); }
+}  // namespace bgp
+namespace {
 
 // Scoring fused with a fit: the candidates, the gp_score outputs and the workspace
 // region that the scoring buffers take.

@@ -1,0 +1,246 @@
+// Attention over packed histories, general form: out_i = sum_j softmax_j(s_ij) v_j over the
+// keys j < lim(i) of query i's document, s_ij = cap tanh(scale q_i.k_j / cap) + bias.
+//
+// One pass over the keys with a running maximum and sum. A block of 4 wavefronts takes 128
+// queries of one head, a wavefront 32 of them; a wavefront's scores are the transposed
+// product K Q^T (32 keys x 32 queries at a time), whose registers are the operand of the
+// second product V^T P^T, so that only K and V go through LDS, and each once per block.
+// lim(i) = min(Lk, max(position + 1, prefix)) covers the causal, prefix and document masks
+// with one comparison per score, made only in tiles where some row's limit falls.
+#include <type_traits>
+
+#include "seq_dev.h"
+
+namespace bgp {
+namespace {
+
+constexpr int kBM = 128;   // queries of a block
+constexpr int kBN = 64;    // keys of a tile
+constexpr int kThreads = 256;
+// The running maximum is raised, and the sums rescaled, only when a row's scores pass it by
+// more than 2^8: the sums then hold values up to 2^8, far from fp32's (and, for the rounded
+// probabilities, fp16's) range, and the rescaling of the output is skipped almost always.
+constexpr float kSlack = 8.f;
+
+template <class T, int DP, bool CAP, int BIAS>
+__global__ __launch_bounds__(kThreads, 2) void attend_kernel(const AttnArgs a) {
+  constexpr int KS = DP / 16;   // k-steps of the score product
+  constexpr int DT = DP / 32;   // column blocks of V
+  constexpr int kTile = kBN * DP * 2;
+  extern __shared__ __align__(1024) char lds[];
+  char *kt = lds, *vt = lds + 2 * kTile;
+  float *lut = reinterpret_cast<float *>(lds + 4 * kTile);
+
+  // kv heads fastest: the blocks of one XCD (every 8th) then share few heads' keys; the
+  // last tiles of a document, which see the most keys under a causal mask, come first
+  int id = blockIdx.x;
+  const int kvh = id % a.kv_heads;
+  id /= a.kv_heads;
+  const int head = kvh * a.group + id % a.group;
+  const DocTile t = find_tile<kBM>(a.qb, a.qe, a.docs, a.q_rows, id / a.group);
+  if (t.doc < 0) return;
+  const int lq = t.b1 - t.b0;
+  const int k0 = max(a.kb[t.doc], 0);
+  const int lk = max(min(a.ke[t.doc], a.k_rows) - k0, 0);
+  const int prefix = (a.causal && a.prefix) ? a.prefix[t.doc] : 0;
+  const int tiles = (lq + kBM - 1) / kBM;
+  const int i0 = (tiles - 1 - t.tile) * kBM;
+
+  const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6), h = lane >> 5;
+  const int row_lo = i0 + 32 * wave;             // first query of the wavefront
+  const int row = row_lo + (lane & 31);
+  const int shift = lk - lq;                     // position of query 0
+  auto limit = [&](int i) { return a.causal ? min(lk, max(i + shift + 1, prefix)) : lk; };
+  const int lim = limit(row);
+  const int lim_lo = limit(row_lo);                             // keys all rows see
+  const int lim_hi = row_lo < lq ? limit(min(row_lo + 31, lq - 1)) : 0;  // keys any row sees
+  const int lim_block = max(limit(min(i0 + kBM, lq) - 1), 0);
+  const int n_tiles = (lim_block + kBN - 1) / kBN;
+
+  const char *kbase = a.k + (int64_t)k0 * a.k_row + kvh * a.k_head;
+  const char *vbase = a.v + (int64_t)k0 * a.v_row + kvh * a.v_head;
+  TileCopy<DP, kBN, 4> kc, vc;
+  kc.init(wave, lane, (int)a.k_row, a.bytes);
+  vc.init(wave, lane, (int)a.v_row, a.bytes);
+  auto start = [&](int tile, int buf) {
+    const int n = min(lk - tile * kBN, kBN);
+    kc.start(row_buffer(kbase, (int64_t)tile * kBN, n, a.k_row, a.bytes),
+             lds_address(kt) + buf * kTile);
+    vc.start(row_buffer(vbase, (int64_t)tile * kBN, n, a.v_row, a.bytes),
+             lds_address(vt) + buf * kTile);
+  };
+  if (n_tiles > 0) start(0, 0);
+
+  u32x4 qf[KS];
+  load_operand<DP>(a.q + (int64_t)t.b0 * a.q_row + head * a.q_head, a.q_row, row, lq, a.bytes, lane,
+                   qf);
+  int reach = 0;
+  float slope2 = 0.f;
+  if (BIAS == kBiasTable) {
+    reach = a.buckets.start[a.buckets.per_side - 1];
+    fill_lut<T>(lut, a.buckets, a.table, head, kThreads);
+  }
+  if (BIAS == kBiasSlope) slope2 = a.slopes[head] * kLog2e;
+  ScoreScale sc;
+  sc.cap2 = a.cap * kLog2e;
+  sc.c = CAP ? 2.f * kLog2e * a.scale / a.cap : a.scale * kLog2e;
+
+  f32x16 acc[DT];
+#pragma unroll
+  for (int c = 0; c < DT; ++c) acc[c] = f32x16{};
+  float m = -__builtin_inff(), l = 0.f;   // l: this lane's half of the row's sum
+  bool dirty = false;
+
+  // one tile; `masked`: some row's limit may fall into it
+  auto step = [&](int tile, auto masked_tile) {
+    constexpr bool masked = decltype(masked_tile)::value;
+    const int buf = tile & 1, key0 = tile * kBN;
+    if (tile + 1 < n_tiles) start(tile + 1, buf ^ 1);
+    if (key0 < lim_hi) {
+      const char *kb = kt + buf * kTile, *vb = vt + buf * kTile;
+      f32x16 s[2] = {f32x16{}, f32x16{}};
+#pragma unroll
+      for (int i = 0; i < KS; ++i) {
+        s[0] = T::mfma(row_operand<DP>(kb, 0, i, lane), qf[i], s[0]);
+        s[1] = T::mfma(row_operand<DP>(kb, 32, i, lane), qf[i], s[1]);
+      }
+      // scores; without cap and bias the scale goes into the exponent's fma below
+      const bool raw = !CAP && BIAS == kBiasNone;
+      if (!raw) {
+#pragma unroll
+        for (int b = 0; b < 2; ++b) {
+#pragma unroll
+          for (int e = 0; e < 16; ++e) s[b][e] = scaled<CAP>(s[b][e], sc);
+          add_bias<BIAS>(s[b], key0 + 32 * b, row + shift, row_lo + shift, h, slope2, lut, reach);
+        }
+      }
+      if (masked) {
+        const int mine = lim - key0 - 4 * h;
+#pragma unroll
+        for (int b = 0; b < 2; ++b)
+#pragma unroll
+          for (int e = 0; e < 16; ++e)
+            if (32 * b + 8 * (e >> 2) + (e & 3) >= mine) s[b][e] = -__builtin_inff();
+      }
+      float top = s[0][0];
+#pragma unroll
+      for (int b = 0; b < 2; ++b)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) top = fmaxf(top, s[b][e]);
+      if (raw) top *= sc.c;
+      top = fmaxf(top, other_half(top));
+      if (__any(top > m + kSlack)) {
+        const float mn = top > m + kSlack ? top : m;
+        const float f = mn == -__builtin_inff() ? 1.f : fast_exp2(m - mn);
+        m = mn;
+        l *= f;
+#pragma unroll
+        for (int c = 0; c < DT; ++c)
+#pragma unroll
+          for (int e = 0; e < 16; ++e) acc[c][e] *= f;
+      }
+      const float ms = m == -__builtin_inff() ? 0.f : m;
+      u32x4 p[kBN / 16];
+#pragma unroll
+      for (int b = 0; b < 2; ++b) {
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+          s[b][e] = fast_exp2(raw ? __builtin_fmaf(s[b][e], sc.c, -ms) : s[b][e] - ms);
+          l += s[b][e];
+        }
+        // the probabilities are rounded to the operands' type for the second product; the
+        // sum above is of the unrounded ones
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+#pragma unroll
+          for (int w = 0; w < 4; ++w)
+            p[2 * b + i][w] = T::pack(s[b][8 * i + 2 * w], s[b][8 * i + 2 * w + 1]);
+      }
+      // masked places may hold anything: 0 times an infinity or NaN would spoil the sums, so
+      // in a tile with such values they are taken as 0 and added for who sees them at the end
+      bool clean = true;
+      if (masked && lim_lo < lk) {
+        uint32_t bad = 0;
+#pragma unroll 1   // (rolled and with the reads below kept apart: it must not cost registers)
+        for (int i = 0; i < kBN / 16; ++i)
+#pragma unroll
+          for (int c = 0; c < DT; ++c)
+            bad |= nonfinite<T>(col_operand<DP>(vb, 16 * i, c, lane));
+        clean = !__any(bad != 0);
+        dirty |= !clean;
+      }
+#pragma unroll
+      for (int i = 0; i < kBN / 16; ++i)
+#pragma unroll
+        for (int c = 0; c < DT; ++c) {
+          u32x4 v = col_operand<DP>(vb, 16 * i, c, lane);
+          if (masked && !clean) v = finite_part<T>(v);
+          acc[c] = T::mfma(v, p[i], acc[c]);
+        }
+    }
+    copies_barrier();
+  };
+
+  copies_barrier();
+  const int whole = min(max(lim_lo, 0) / kBN, n_tiles);   // tiles that every row sees
+  for (int tile = 0; tile < whole; ++tile) step(tile, std::false_type{});
+  for (int tile = whole; tile < n_tiles; ++tile) step(tile, std::true_type{});
+
+  l += other_half(l);
+  const bool ok = row < lq;
+  const float inv = l > 0.f ? 1.f / l : (l == 0.f ? 0.f : l);   // a NaN sum stays one
+  store_row<T, DT>(a.o + (int64_t)(t.b0 + row) * a.o_row + head * a.o_head, ok, a.bytes, acc, inv,
+                   lane);
+  if (ok && h == 0)
+    a.lse[(int64_t)head * a.q_rows + t.b0 + row] =
+        l == 0.f ? -__builtin_inff() : (m + __builtin_amdgcn_logf(l)) * kLn2;
+  if (dirty) {
+    __threadfence_block();
+    const int first = max(lim_lo, 0) / kBN * kBN;   // of the first tile with a masked place
+    for (int r = row_lo; r < min(row_lo + 32, lq); ++r)
+      for (int d = lane; 2 * d < a.bytes; d += 64) {
+        const float x = nonfinite_sum<T>(vbase, a.v_row, first, limit(r), d);
+        char *o = a.o + (int64_t)(t.b0 + r) * a.o_row + head * a.o_head;
+        if (x != 0.f) T::store(o, d, T::load(o, d) + x);
+      }
+  }
+}
+
+template <class T, int DP, bool CAP, int BIAS>
+hipError_t launch(const AttnArgs &a, hipStream_t s) {
+  static LdsLimit limit;
+  int lds = 4 * kBN * DP * 2;
+  if (BIAS == kBiasTable) lds += lut_size(a.buckets.start[a.buckets.per_side - 1]) * 4;
+  hipError_t e = limit.set(reinterpret_cast<const void *>(&attend_kernel<T, DP, CAP, BIAS>),
+                           4 * kBN * DP * 2 + lut_size(kMaxReach) * 4);
+  if (e != hipSuccess) return e;
+  // an upper bound of the documents' tiles; the blocks past the last one end at once
+  const int64_t tiles = (int64_t)a.q_rows / kBM + a.docs;
+  const int64_t by_max = (int64_t)a.docs * ((a.max_q + kBM - 1) / kBM);
+  const int64_t blocks = (tiles < by_max ? tiles : by_max) * a.heads;
+  if (blocks == 0) return hipSuccess;
+  attend_kernel<T, DP, CAP, BIAS><<<dim3((uint32_t)blocks), kThreads, lds, s>>>(a);
+  return hipGetLastError();
+}
+
+template <class T, int DP>
+hipError_t by_bias(const AttnArgs &a, hipStream_t s) {
+  const int bias = a.table ? kBiasTable : (a.slopes ? kBiasSlope : kBiasNone);
+  if (a.cap > 0.f) {
+    if (bias == kBiasTable) return launch<T, DP, true, kBiasTable>(a, s);
+    if (bias == kBiasSlope) return launch<T, DP, true, kBiasSlope>(a, s);
+    return launch<T, DP, true, kBiasNone>(a, s);
+  }
+  if (bias == kBiasTable) return launch<T, DP, false, kBiasTable>(a, s);
+  if (bias == kBiasSlope) return launch<T, DP, false, kBiasSlope>(a, s);
+  return launch<T, DP, false, kBiasNone>(a, s);
+}
+
+}  // namespace
+
+hipError_t launch_attend(const AttnArgs &a, hipStream_t s) {
+  if (a.bytes <= 128) return a.fp16 ? by_bias<Fp16, 64>(a, s) : by_bias<Bf16, 64>(a, s);
+  return a.fp16 ? by_bias<Fp16, 128>(a, s) : by_bias<Bf16, 128>(a, s);
+}
+
+}  // namespace bgp

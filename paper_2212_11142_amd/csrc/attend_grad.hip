@@ -1,0 +1,585 @@
+// Gradients of the attention in attend.hip. With P = softmax(S), dP = dO V^T and
+// D_i = dO_i . O_i:
+//   dS = P (dP - D),  dbias = dS,  dZ = dS (1 - (z' / cap)^2)  (z' the capped product)
+//   dQ = scale dZ K,  dK = scale dZ^T Q,  dV = P^T dO
+// P is recomputed from the scores and the forward pass's log-sums. Two kernels, so that
+// every sum has one owner and one order (no atomics): one goes over the queries for 128 keys
+// of a key head (all query heads of its group, in turn) and keeps dK and dV, the other goes
+// over the keys for 128 queries of a head and keeps dQ and the head's table gradient. That
+// costs 7 products of the pairs where one kernel with atomic sums of dQ would take 5.
+//
+// fp16: P is kept times 2^12 and dS times a power of two from a bound of |dS|,
+// 2 max|dO_i| max|v_j|, so that neither leaves fp16's normal range; exact to undo.
+#include <type_traits>
+
+#include "seq_dev.h"
+
+namespace bgp {
+namespace {
+
+constexpr int kThreads = 256;
+constexpr int kRowBlocks = 512;    // blocks of the row pass, at most
+constexpr float kP16 = 12.f;       // fp16: log2 of the factor of P
+
+// ------------------------------------------------------------------ rows
+// delta[head][row] = dO . O; for fp16 also block maxima of |dO_i|^2 (bound[0..]) and of
+// |v_j|^2 (bound[kRowBlocks..]). 16 lanes per row.
+template <class T>
+__device__ inline float dot8(u32x4 a, u32x4 b) {
+  float x = 0.f;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    x = __builtin_fmaf(T::lo(a[i]), T::lo(b[i]), x);
+    x = __builtin_fmaf(T::hi(a[i]), T::hi(b[i]), x);
+  }
+  return x;
+}
+
+template <class T>
+__global__ __launch_bounds__(kThreads) void grad_rows(const AttnGradArgs a) {
+  __shared__ float red[2][4];
+  const int l16 = threadIdx.x & 15;
+  const int64_t step = (int64_t)gridDim.x * (kThreads / 16);
+  const bool in = l16 * 16 < a.f.bytes;
+  float top = 0.f, vtop = 0.f;
+  const int64_t n = (int64_t)a.f.q_rows * a.f.heads;
+  for (int64_t r = blockIdx.x * (kThreads / 16) + threadIdx.x / 16; r < n; r += step) {
+    const int64_t row = r / a.f.heads;
+    const int head = (int)(r % a.f.heads);
+    float d = 0.f, nrm = 0.f;
+    if (in) {
+      const u32x4 g = *reinterpret_cast<const u32x4 *>(a.dout + row * a.do_row + head * a.do_head + l16 * 16);
+      const u32x4 o = *reinterpret_cast<const u32x4 *>(a.f.o + row * a.f.o_row + head * a.f.o_head + l16 * 16);
+      d = dot8<T>(g, o);
+      if (a.f.fp16) nrm = dot8<T>(g, g);
+    }
+#pragma unroll
+    for (int o = 8; o; o >>= 1) {
+      d += __shfl_xor(d, o);
+      if (a.f.fp16) nrm += __shfl_xor(nrm, o);
+    }
+    if (l16 == 0) a.delta[(int64_t)head * a.f.q_rows + row] = d;
+    top = fmaxf(top, nrm);
+  }
+  if (!a.f.fp16) return;
+  const int64_t nv = (int64_t)a.f.k_rows * a.f.kv_heads;
+  for (int64_t r = blockIdx.x * (kThreads / 16) + threadIdx.x / 16; r < nv; r += step) {
+    float nrm = 0.f;
+    if (in) {
+      const u32x4 v = *reinterpret_cast<const u32x4 *>(a.f.v + (r / a.f.kv_heads) * a.f.v_row +
+                                                       (r % a.f.kv_heads) * a.f.v_head + l16 * 16);
+      nrm = dot8<T>(v, v);
+    }
+#pragma unroll
+    for (int o = 8; o; o >>= 1) nrm += __shfl_xor(nrm, o);
+    vtop = fmaxf(vtop, nrm);   // (NaN is passed over)
+  }
+#pragma unroll
+  for (int o = 32; o; o >>= 1) {
+    top = fmaxf(top, __shfl_xor(top, o));
+    vtop = fmaxf(vtop, __shfl_xor(vtop, o));
+  }
+  if ((threadIdx.x & 63) == 0) {
+    red[0][threadIdx.x >> 6] = top;
+    red[1][threadIdx.x >> 6] = vtop;
+  }
+  __syncthreads();
+  if (threadIdx.x < 2) {
+    const float *x = red[threadIdx.x];
+    a.bound[threadIdx.x * kRowBlocks + blockIdx.x] = fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3]));
+  }
+}
+
+// Exponent e of the factor 2^e that dS is kept at: |dS| <= 2 max|dO_i| max|v_j| < 2^15 / 2^e.
+__device__ inline int ds_exponent(const float *bound, int blocks, float *red) {
+  float x = 0.f, y = 0.f;
+  for (int i = threadIdx.x; i < blocks; i += kThreads) {
+    x = fmaxf(x, bound[i]);
+    y = fmaxf(y, bound[kRowBlocks + i]);
+  }
+#pragma unroll
+  for (int o = 32; o; o >>= 1) {
+    x = fmaxf(x, __shfl_xor(x, o));
+    y = fmaxf(y, __shfl_xor(y, o));
+  }
+  if ((threadIdx.x & 63) == 0) {
+    red[threadIdx.x >> 6] = x;
+    red[4 + (threadIdx.x >> 6)] = y;
+  }
+  __syncthreads();
+  x = fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3]));
+  y = fmaxf(fmaxf(red[4], red[5]), fmaxf(red[6], red[7]));
+  __syncthreads();
+  const float b = 2.f * sqrtf(x) * sqrtf(y);
+  if (!(b > 0.f) || !(b < __builtin_inff())) return 0;
+  int e;
+  frexpf(b, &e);            // b < 2^e
+  return uniform(min(max(15 - e, -60), 60));
+}
+
+// log-sums in units of log 2, +inf for a row that saw nothing (its P is then 0)
+__device__ inline float row_lse(float lse) {
+  return lse == -__builtin_inff() ? __builtin_inff() : lse * kLog2e;
+}
+
+// P and dZ of 16 pairs of a lane: s raw products in, P (times 2^p0) out; dp in, dZ times
+// 2^ds0 out; `bias`: dS without the cap's derivative (what the table's gradient sums).
+// lse and delta per element; `seen`: whether the pair is visible.
+template <bool CAP>
+struct PairGrad {
+  ScoreScale sc;
+  float inv_cap2;    // 1 / (cap log2(e))
+};
+
+// ------------------------------------------------------------------ dK, dV
+// A lane's key is fixed, its elements are the queries 8 g + 4 h + r of 32: products are
+// Q K^T (queries x keys), their results the operands of dV^T = dO^T P and dK^T = Q^T dZ.
+template <class T, int DP, bool CAP, int BIAS>
+__global__ __launch_bounds__(kThreads, 2) void grad_kv(const AttnGradArgs ga, int row_blocks) {
+  constexpr int KS = DP / 16, DT = DP / 32;
+  constexpr int kBQ = 32;                      // queries of a step
+  constexpr int kTile = kBQ * DP * 2;
+  constexpr int kBK = 128;                     // keys of a block
+  const AttnArgs &a = ga.f;
+  extern __shared__ __align__(1024) char lds[];                // [2][Q, dO], [2][lse, delta], table
+  float *rows_lds = reinterpret_cast<float *>(lds + 4 * kTile);
+  float *lut = rows_lds + 2 * 128;
+  __shared__ float red[8];
+
+  int id = blockIdx.x;
+  const int kvh = id % a.kv_heads;
+  const DocTile t = find_tile<kBK>(a.kb, a.ke, a.docs, a.k_rows, id / a.kv_heads);
+  if (t.doc < 0) return;
+  const int lk = t.b1 - t.b0;
+  const int q0 = max(a.qb[t.doc], 0);
+  const int lq = max(min(a.qe[t.doc], a.q_rows) - q0, 0);
+  const int prefix = (a.causal && a.prefix) ? a.prefix[t.doc] : 0;
+  const int shift = lk - lq;
+  const int j0 = t.tile * kBK;
+
+  const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6), h = lane >> 5;
+  const int key_lo = j0 + 32 * wave, key = key_lo + (lane & 31);
+  // queries that see key j: those from first(j) on
+  auto first = [&](int j) { return (a.causal && j >= prefix) ? max(j - shift, 0) : 0; };
+  const int i_start = first(j0) / kBQ * kBQ;
+  const int i_wave = key_lo < lk ? first(key_lo) : lq;                 // any key of the wavefront
+  const int i_whole = key_lo + 31 < lk ? first(key_lo + 31) : lq;      // all of its keys
+  const int mine = key < lk ? first(key) : lq;
+  const int steps = max((lq - i_start + kBQ - 1) / kBQ, 0);
+  const int total = steps * a.group;
+
+  TileCopy<DP, kBQ, 4> qc, dc;
+  qc.init(wave, lane, (int)a.q_row, a.bytes);
+  dc.init(wave, lane, (int)ga.do_row, a.bytes);
+  auto start = [&](int n, int buf) {
+    const int head = kvh * a.group + n / steps, i = i_start + n % steps * kBQ;
+    const int rows = min(lq - i, kBQ);
+    qc.start(row_buffer(a.q + (int64_t)q0 * a.q_row + head * a.q_head, i, rows, a.q_row, a.bytes),
+             lds_address(lds) + buf * 2 * kTile);
+    dc.start(row_buffer(ga.dout + (int64_t)q0 * ga.do_row + head * ga.do_head, i, rows, ga.do_row,
+                        a.bytes),
+             lds_address(lds) + (buf * 2 + 1) * kTile);
+    if (threadIdx.x < 2 * kBQ) {               // (wavefront 0)
+      const int r = i + (lane & 31);
+      const int64_t at = (int64_t)head * a.q_rows + q0 + r;
+      const float x = r < lq ? (h ? ga.delta[at] : row_lse(a.lse[at])) : 0.f;
+      rows_lds[buf * 128 + lane] = x;
+    }
+  };
+
+  // operands that stay: this wavefront's 32 keys of K and V
+  u32x4 kf[KS], vf[KS];
+  load_operand<DP>(a.k + (int64_t)t.b0 * a.k_row + kvh * a.k_head, a.k_row, key, lk, a.bytes, lane, kf);
+  load_operand<DP>(a.v + (int64_t)t.b0 * a.v_row + kvh * a.v_head, a.v_row, key, lk, a.bytes, lane, vf);
+  const bool half = std::is_same<T, Fp16>::value;
+  const int ds0 = half ? ds_exponent(ga.bound, row_blocks, red) : 0;
+  const float ds_scale = ldexpf(1.f, half ? ds0 - (int)kP16 : 0);
+  const int reach = BIAS == kBiasTable ? a.buckets.start[a.buckets.per_side - 1] : 0;
+  ScoreScale sc;
+  sc.cap2 = a.cap * kLog2e;
+  sc.c = CAP ? 2.f * kLog2e * a.scale / a.cap : a.scale * kLog2e;
+  const float inv_cap2 = CAP ? 1.f / sc.cap2 : 0.f;
+
+  f32x16 dk[DT], dv[DT];
+#pragma unroll
+  for (int c = 0; c < DT; ++c) dk[c] = dv[c] = f32x16{};
+  float slope2 = 0.f;
+
+  if (total > 0) start(0, 0);
+  copies_barrier();
+  for (int n = 0; n < total; ++n) {
+    const int buf = n & 1, head = kvh * a.group + n / steps, i0 = i_start + n % steps * kBQ;
+    if (BIAS != kBiasNone && n % steps == 0) {   // the next head
+      if (BIAS == kBiasSlope) slope2 = a.slopes[head] * kLog2e;
+      if (BIAS == kBiasTable) {
+        fill_lut<T>(lut, a.buckets, a.table, head, kThreads);
+        __syncthreads();
+      }
+    }
+    if (n + 1 < total) start(n + 1, buf ^ 1);
+    if (i0 + kBQ > i_wave) {
+      const char *qt = lds + buf * 2 * kTile, *dt = qt + kTile;
+      const float *lse = rows_lds + buf * 128 + 4 * h, *delta = lse + 32;
+      f32x16 s = {}, dp = {};
+#pragma unroll
+      for (int k = 0; k < KS; ++k) s = T::mfma(row_operand<DP>(qt, 0, k, lane), kf[k], s);
+#pragma unroll
+      for (int k = 0; k < KS; ++k) dp = T::mfma(row_operand<DP>(dt, 0, k, lane), vf[k], dp);
+      const bool masked = i0 < i_whole || i0 + kBQ > lq;
+      f32x16 z;   // capped products in units of log 2
+#pragma unroll
+      for (int e = 0; e < 16; ++e) z[e] = scaled<CAP>(s[e], sc);
+      s = z;
+      // the distance falls with the query: add_bias's elements in the other direction
+      if (BIAS == kBiasSlope) {
+        const float d0 = (float)(key - shift - i0 - 4 * h);
+#pragma unroll
+        for (int e = 0; e < 16; ++e)
+          s[e] = __builtin_fmaf(-slope2, __builtin_fabsf(d0 - (float)(8 * (e >> 2) + (e & 3))), s[e]);
+      }
+      if (BIAS == kBiasTable) {
+        const int far_hi = key_lo + 31 - (i0 + shift), far_lo = key_lo - (i0 + 31 + shift);
+        if (far_hi <= -reach || far_lo >= reach) {
+          const float b = far_hi <= -reach ? lut[0] : lut[lut_size(reach) - 1];
+#pragma unroll
+          for (int e = 0; e < 16; ++e) s[e] += b;
+        } else {
+          const float *p = lut + (key - shift - i0 - 4 * h + reach + kLutPad);
+#pragma unroll
+          for (int e = 0; e < 16; ++e) s[e] += p[-(8 * (e >> 2) + (e & 3))];
+        }
+      }
+      u32x4 pr[2], dr[2];
+#pragma unroll
+      for (int g = 0; g < 4; ++g) {
+        const f32x4 ls = *reinterpret_cast<const f32x4 *>(lse + 8 * g);
+        const f32x4 dl = *reinterpret_cast<const f32x4 *>(delta + 8 * g);
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          const int e = 4 * g + r;
+          const bool seen = !masked || (i0 + 4 * h + 8 * g + r >= mine && i0 + 4 * h + 8 * g + r < lq);
+          float p = fast_exp2(half ? s[e] - ls[r] + kP16 : s[e] - ls[r]);
+          p = seen ? p : 0.f;
+          float d = p * (dp[e] - dl[r]);
+          if (half) d *= ds_scale;
+          if (CAP) {
+            const float y = z[e] * inv_cap2;
+            d *= __builtin_fmaf(-y, y, 1.f);
+          }
+          s[e] = p;
+          dp[e] = seen ? d : 0.f;
+        }
+      }
+#pragma unroll
+      for (int k = 0; k < 2; ++k)
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+          pr[k][w] = T::pack(s[8 * k + 2 * w], s[8 * k + 2 * w + 1]);
+          dr[k][w] = T::pack(dp[8 * k + 2 * w], dp[8 * k + 2 * w + 1]);
+        }
+#pragma unroll
+      for (int k = 0; k < 2; ++k)
+#pragma unroll
+        for (int c = 0; c < DT; ++c) {
+          dv[c] = T::mfma(col_operand<DP>(dt, 16 * k, c, lane), pr[k], dv[c]);
+          dk[c] = T::mfma(col_operand<DP>(qt, 16 * k, c, lane), dr[k], dk[c]);
+        }
+    }
+    copies_barrier();
+  }
+  const bool ok = key < lk;
+  store_row<T, DT>(ga.dv + (int64_t)(t.b0 + key) * ga.dv_row + kvh * ga.dv_head, ok, a.bytes, dv,
+                   half ? ldexpf(1.f, -(int)kP16) : 1.f, lane);
+  store_row<T, DT>(ga.dk + (int64_t)(t.b0 + key) * ga.dk_row + kvh * ga.dk_head, ok, a.bytes, dk,
+                   a.scale * ldexpf(1.f, -ds0), lane);
+}
+
+// ------------------------------------------------------------------ dQ, table
+// A lane's query is fixed, its elements are the keys, as in the forward kernel.
+template <class T, int DP, bool CAP, int BIAS>
+__global__ __launch_bounds__(kThreads, 2) void grad_q(const AttnGradArgs ga, int row_blocks) {
+  constexpr int KS = DP / 16, DT = DP / 32;
+  constexpr int kBN = 32;                      // keys of a step
+  constexpr int kTile = kBN * DP * 2;
+  constexpr int kBM = 128;
+  const AttnArgs &a = ga.f;
+  extern __shared__ __align__(1024) char lds[];                // [2][K, V], biases, [4] sums by distance
+  float *lut = reinterpret_cast<float *>(lds + 4 * kTile);
+  __shared__ float red[8];
+  __shared__ float far_sum[4][2];
+
+  int id = blockIdx.x;
+  const int kvh = id % a.kv_heads;
+  id /= a.kv_heads;
+  const int head = kvh * a.group + id % a.group, unit = id / a.group;
+  const int nb = a.buckets.two_sided ? 2 * a.buckets.per_side : a.buckets.per_side;
+  const DocTile t = find_tile<kBM>(a.qb, a.qe, a.docs, a.q_rows, unit);
+  float *tout = nullptr;
+  if (BIAS == kBiasTable) tout = ga.tpart + ((int64_t)unit * a.heads + head) * nb;
+  if (t.doc < 0) {
+    if (BIAS == kBiasTable)
+      for (int b = threadIdx.x; b < nb; b += kThreads) tout[b] = 0.f;
+    return;
+  }
+  const int lq = t.b1 - t.b0;
+  const int k0 = max(a.kb[t.doc], 0);
+  const int lk = max(min(a.ke[t.doc], a.k_rows) - k0, 0);
+  const int prefix = (a.causal && a.prefix) ? a.prefix[t.doc] : 0;
+  const int tiles = (lq + kBM - 1) / kBM;
+  const int i0 = (tiles - 1 - t.tile) * kBM;
+
+  const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6), h = lane >> 5;
+  const int row_lo = i0 + 32 * wave, row = row_lo + (lane & 31);
+  const int shift = lk - lq;
+  auto limit = [&](int i) { return a.causal ? min(lk, max(i + shift + 1, prefix)) : lk; };
+  const bool ok = row < lq;
+  const int lim = ok ? limit(row) : 0;
+  const int lim_lo = row_lo + 31 < lq ? limit(row_lo) : 0;
+  const int lim_hi = row_lo < lq ? limit(min(row_lo + 31, lq - 1)) : 0;
+  const int n_tiles = (max(limit(min(i0 + kBM, lq) - 1), 0) + kBN - 1) / kBN;
+
+  const char *kbase = a.k + (int64_t)k0 * a.k_row + kvh * a.k_head;
+  const char *vbase = a.v + (int64_t)k0 * a.v_row + kvh * a.v_head;
+  TileCopy<DP, kBN, 4> kc, vc;
+  kc.init(wave, lane, (int)a.k_row, a.bytes);
+  vc.init(wave, lane, (int)a.v_row, a.bytes);
+  auto start = [&](int tile, int buf) {
+    const int n = min(lk - tile * kBN, kBN);
+    kc.start(row_buffer(kbase, (int64_t)tile * kBN, n, a.k_row, a.bytes),
+             lds_address(lds) + buf * 2 * kTile);
+    vc.start(row_buffer(vbase, (int64_t)tile * kBN, n, a.v_row, a.bytes),
+             lds_address(lds) + (buf * 2 + 1) * kTile);
+  };
+  if (n_tiles > 0) start(0, 0);
+
+  u32x4 qf[KS], df[KS];
+  load_operand<DP>(a.q + (int64_t)t.b0 * a.q_row + head * a.q_head, a.q_row, row, lq, a.bytes, lane, qf);
+  load_operand<DP>(ga.dout + (int64_t)t.b0 * ga.do_row + head * ga.do_head, ga.do_row, row, lq,
+                   a.bytes, lane, df);
+  const int64_t at = (int64_t)head * a.q_rows + t.b0 + row;
+  const float lse = ok ? row_lse(a.lse[at]) : 0.f, delta = ok ? ga.delta[at] : 0.f;
+  const bool half = std::is_same<T, Fp16>::value;
+  const int ds0 = half ? ds_exponent(ga.bound, row_blocks, red) : 0;
+  const float ds_scale = half ? ldexpf(1.f, ds0) : 1.f;
+  int reach = 0;
+  float slope2 = 0.f;
+  float *hist = nullptr;                       // this wavefront's sums of dS by distance
+  float far_l = 0.f, far_r = 0.f;              // behind and ahead of the table's reach
+  if (BIAS == kBiasTable) {
+    reach = a.buckets.start[a.buckets.per_side - 1];
+    const int n = lut_size(reach);
+    fill_lut<T>(lut, a.buckets, a.table, head, kThreads);
+    hist = lut + n * (1 + wave);
+    for (int i = lane; i < n; i += 64) hist[i] = 0.f;
+  }
+  if (BIAS == kBiasSlope) slope2 = a.slopes[head] * kLog2e;
+  ScoreScale sc;
+  sc.cap2 = a.cap * kLog2e;
+  sc.c = CAP ? 2.f * kLog2e * a.scale / a.cap : a.scale * kLog2e;
+  const float inv_cap2 = CAP ? 1.f / sc.cap2 : 0.f;
+
+  f32x16 acc[DT];
+#pragma unroll
+  for (int c = 0; c < DT; ++c) acc[c] = f32x16{};
+
+  copies_barrier();
+  for (int tile = 0; tile < n_tiles; ++tile) {
+    const int buf = tile & 1, key0 = tile * kBN;
+    if (tile + 1 < n_tiles) start(tile + 1, buf ^ 1);
+    if (key0 < lim_hi) {
+      const char *kb = lds + buf * 2 * kTile, *vb = kb + kTile;
+      f32x16 s = {}, dp = {};
+#pragma unroll
+      for (int k = 0; k < KS; ++k) s = T::mfma(row_operand<DP>(kb, 0, k, lane), qf[k], s);
+#pragma unroll
+      for (int k = 0; k < KS; ++k) dp = T::mfma(row_operand<DP>(vb, 0, k, lane), df[k], dp);
+      f32x16 z;
+#pragma unroll
+      for (int e = 0; e < 16; ++e) z[e] = scaled<CAP>(s[e], sc);
+      s = z;
+      add_bias<BIAS>(s, key0, row + shift, row_lo + shift, h, slope2, lut, reach);
+      const bool masked = key0 + kBN > lim_lo;
+      const int mine = lim - key0 - 4 * h;
+      float sum = 0.f;
+#pragma unroll
+      for (int e = 0; e < 16; ++e) {
+        const bool seen = !masked || 8 * (e >> 2) + (e & 3) < mine;
+        const float p = fast_exp2(s[e] - lse);
+        float d = p * (dp[e] - delta);
+        d = seen ? d : 0.f;
+        dp[e] = d;
+        sum += d;
+      }
+      if (BIAS == kBiasTable) {
+        const int d_hi = key0 + 31 - (row_lo + shift), d_lo = key0 - (row_lo + 31 + shift);
+        if (d_hi <= -reach) {
+          far_l += sum;
+        } else if (d_lo >= reach) {
+          far_r += sum;
+        } else {
+          // the halves of the wavefront in turn: within each, every lane has a distance of
+          // its own, so that the order of the sums does not depend on the hardware's
+          float *p = hist + (key0 + 4 * h - (row + shift) + reach + kLutPad);
+#pragma unroll
+          for (int g = 0; g < 2; ++g) {
+            if (h == g) {
+#pragma unroll
+              for (int e = 0; e < 16; ++e)
+                __hip_atomic_fetch_add(p + 8 * (e >> 2) + (e & 3), dp[e], __ATOMIC_RELAXED,
+                                       __HIP_MEMORY_SCOPE_WORKGROUP);
+            }
+          }
+        }
+      }
+      u32x4 dr[2];
+#pragma unroll
+      for (int e = 0; e < 16; ++e) {
+        if (CAP) {
+          const float y = z[e] * inv_cap2;
+          dp[e] *= __builtin_fmaf(-y, y, 1.f);
+        }
+        if (half) dp[e] *= ds_scale;
+      }
+#pragma unroll
+      for (int k = 0; k < 2; ++k)
+#pragma unroll
+        for (int w = 0; w < 4; ++w)
+          dr[k][w] = T::pack(dp[8 * k + 2 * w], dp[8 * k + 2 * w + 1]);
+#pragma unroll
+      for (int k = 0; k < 2; ++k)
+#pragma unroll
+        for (int c = 0; c < DT; ++c)
+          acc[c] = T::mfma(col_operand<DP>(kb, 16 * k, c, lane), dr[k], acc[c]);
+    }
+    copies_barrier();
+  }
+  store_row<T, DT>(ga.dq + (int64_t)(t.b0 + row) * ga.dq_row + head * ga.dq_head, ok, a.bytes, acc,
+                   a.scale * ldexpf(1.f, -ds0), lane);
+
+  if (BIAS == kBiasTable) {
+#pragma unroll
+    for (int o = 32; o; o >>= 1) {
+      far_l += __shfl_xor(far_l, o);
+      far_r += __shfl_xor(far_r, o);
+    }
+    if (lane == 0) {
+      far_sum[wave][0] = far_l;
+      far_sum[wave][1] = far_r;
+    }
+    __syncthreads();
+    const int n = lut_size(reach), mid = reach + kLutPad, ps = a.buckets.per_side;
+    for (int b = threadIdx.x; b < nb; b += kThreads) {
+      const int k = b % ps;
+      const bool ahead = b >= ps;              // the second half of a two-sided table
+      const int from = a.buckets.start[k];
+      const int to = k + 1 < ps ? a.buckets.start[k + 1] : mid + 1;   // distances [from, to)
+      float x = 0.f;
+      for (int w = 0; w < 4; ++w) {
+        const float *hw = lut + n * (1 + w) + mid;
+        for (int d = max(from, ahead ? 1 : 0); d < to; ++d) x += hw[ahead ? d : -d];
+        if (k + 1 == ps) x += far_sum[w][ahead];
+        if (!a.buckets.two_sided && k == 0) {  // keys ahead count as distance 0
+          for (int d = 1; d <= mid; ++d) x += hw[d];
+          x += far_sum[w][1];
+        }
+      }
+      tout[b] = x;
+    }
+  }
+}
+
+// dtable[head][b]: the tiles' partial sums; 64 of them per lane group in turn, then joined.
+template <class T>
+__global__ __launch_bounds__(256) void grad_table(const AttnGradArgs a, int units, int nb) {
+  __shared__ float red[256];
+  const int head = blockIdx.x / nb, b = blockIdx.x % nb;
+  float x = 0.f;
+  for (int u = threadIdx.x; u < units; u += 256)
+    x += a.tpart[((int64_t)u * a.f.heads + head) * nb + b];
+  red[threadIdx.x] = x;
+  __syncthreads();
+  for (int o = 128; o; o >>= 1) {
+    if ((int)threadIdx.x < o) red[threadIdx.x] += red[threadIdx.x + o];
+    __syncthreads();
+  }
+  if (threadIdx.x == 0) T::store(a.dtable, (int64_t)head * nb + b, red[0]);
+}
+
+int64_t tile_bound(int64_t rows, int64_t docs, int64_t longest, int tile) {
+  const int64_t x = rows / tile + docs, y = docs * ((longest + tile - 1) / tile);
+  return x < y ? x : y;
+}
+
+template <class T, int DP, bool CAP, int BIAS>
+hipError_t launch(const AttnGradArgs &a, int row_blocks, hipStream_t s) {
+  static LdsLimit lim_kv, lim_q;
+  const int lut = BIAS == kBiasTable ? lut_size(a.f.buckets.start[a.f.buckets.per_side - 1]) * 4 : 0;
+  const int most = lut_size(kMaxReach) * 4;
+  const int base = 4 * 32 * DP * 2;
+  hipError_t e = lim_kv.set(reinterpret_cast<const void *>(&grad_kv<T, DP, CAP, BIAS>),
+                            base + 1024 + most);
+  if (e != hipSuccess) return e;
+  e = lim_q.set(reinterpret_cast<const void *>(&grad_q<T, DP, CAP, BIAS>), base + 5 * most);
+  if (e != hipSuccess) return e;
+  const int64_t kb = tile_bound(a.f.k_rows, a.f.docs, a.f.max_k, 128) * a.f.kv_heads;
+  const int64_t units = tile_bound(a.f.q_rows, a.f.docs, a.f.max_q, 128);
+  if (kb > 0)
+    grad_kv<T, DP, CAP, BIAS><<<dim3((uint32_t)kb), kThreads, base + 1024 + lut, s>>>(a, row_blocks);
+  if (units > 0)
+    grad_q<T, DP, CAP, BIAS>
+        <<<dim3((uint32_t)(units * a.f.heads)), kThreads, base + 5 * lut, s>>>(a, row_blocks);
+  if (BIAS == kBiasTable) {
+    const int nb = (a.f.buckets.two_sided ? 2 : 1) * a.f.buckets.per_side;
+    grad_table<T><<<dim3((uint32_t)(a.f.heads * nb)), 256, 0, s>>>(a, (int)units, nb);
+  }
+  return hipGetLastError();
+}
+
+template <class T, int DP>
+hipError_t by_bias(const AttnGradArgs &a, int row_blocks, hipStream_t s) {
+  const int bias = a.f.table ? kBiasTable : (a.f.slopes ? kBiasSlope : kBiasNone);
+  if (a.f.cap > 0.f) {
+    if (bias == kBiasTable) return launch<T, DP, true, kBiasTable>(a, row_blocks, s);
+    if (bias == kBiasSlope) return launch<T, DP, true, kBiasSlope>(a, row_blocks, s);
+    return launch<T, DP, true, kBiasNone>(a, row_blocks, s);
+  }
+  if (bias == kBiasTable) return launch<T, DP, false, kBiasTable>(a, row_blocks, s);
+  if (bias == kBiasSlope) return launch<T, DP, false, kBiasSlope>(a, row_blocks, s);
+  return launch<T, DP, false, kBiasNone>(a, row_blocks, s);
+}
+
+}  // namespace
+
+size_t attend_grad_bytes(int32_t q_rows, int32_t docs, int32_t heads, int32_t buckets, bool fp16) {
+  auto up = [](int64_t n) { return (n + 63) / 64 * 64; };
+  int64_t n = up((int64_t)q_rows * heads);
+  if (fp16) n += 2 * kRowBlocks;
+  if (buckets) n += up(((int64_t)q_rows / 128 + docs) * heads * buckets);
+  return (size_t)n * 4;
+}
+
+hipError_t launch_attend_grad(const AttnGradArgs &args, void *ws, hipStream_t s) {
+  AttnGradArgs a = args;
+  auto up = [](int64_t n) { return (n + 63) / 64 * 64; };
+  a.delta = static_cast<float *>(ws);
+  a.bound = a.delta + up((int64_t)a.f.q_rows * a.f.heads);
+  a.tpart = a.bound + (a.f.fp16 ? 2 * kRowBlocks : 0);
+  int64_t need = (int64_t)a.f.q_rows * a.f.heads;
+  if (a.f.fp16 && (int64_t)a.f.k_rows * a.f.kv_heads > need) need = (int64_t)a.f.k_rows * a.f.kv_heads;
+  int64_t blocks = (need + kThreads / 16 - 1) / (kThreads / 16);
+  if (!a.f.fp16) {
+    if (blocks > 8192) blocks = 8192;
+  } else if (blocks > kRowBlocks) {
+    blocks = kRowBlocks;
+  }
+  if (blocks < 1) blocks = 1;
+  if (a.f.fp16) grad_rows<Fp16><<<dim3((uint32_t)blocks), kThreads, 0, s>>>(a);
+  else grad_rows<Bf16><<<dim3((uint32_t)blocks), kThreads, 0, s>>>(a);
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  const int rb = (int)blocks;
+  if (a.f.bytes <= 128) return a.f.fp16 ? by_bias<Fp16, 64>(a, rb, s) : by_bias<Bf16, 64>(a, rb, s);
+  return a.f.fp16 ? by_bias<Fp16, 128>(a, rb, s) : by_bias<Bf16, 128>(a, rb, s);
+}
+
+}  // namespace bgp

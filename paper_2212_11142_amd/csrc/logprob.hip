@@ -1,0 +1,592 @@
+// Log probability of a given entry, entropy and best alternatives of rows of logits, and the
+// gradient of the first two. With m = max x, d_v = c (x_v - m) (c the scale), A = sum e^d,
+// B = sum e^d d:  lse = c m + log A,  logp = d_t - log A,  H = log A - B / A (a sum of terms
+// of one sign, so that a peaked row's entropy keeps its digits).
+//
+// Bound by reading the logits once: a wavefront keeps a short row in registers, a block goes
+// once over a long one with a running maximum, and where rows are few several blocks share
+// one. The alternatives come from the same pass: every thread remembers its largest entry;
+// the k-th largest of 64 (or 256) groups' entries bounds the k-th best from below, so that
+// only the few threads above it look at their entries again. Order: larger value, then lower
+// index; a NaN is no alternative.
+#include <type_traits>
+
+#include "seq_dev.h"
+
+namespace bgp {
+namespace {
+
+constexpr int kThreads = 256;
+constexpr int kList = 2048;        // candidates for the alternatives
+constexpr int kWaveWidth = 1024;   // widest row of the one-wavefront form
+constexpr float kLowest = -3.4028234663852886e38f;
+
+enum { kBf16 = GP_BF16, kFp16 = GP_FP16, kFp32 = GP_FP32 };
+
+template <int DT>
+struct Elem {
+  static constexpr int kVec = 8, kSize = 2;
+};
+template <>
+struct Elem<kFp32> {
+  static constexpr int kVec = 4, kSize = 4;
+};
+
+template <int DT>
+__device__ inline float load_one(const char *p, int64_t i) {
+  if (DT == kBf16) return Bf16::load(p, i);
+  if (DT == kFp16) return Fp16::load(p, i);
+  return reinterpret_cast<const float *>(p)[i];
+}
+
+// 16 bytes of entries at any alignment of an entry
+template <int DT>
+__device__ inline void load_vec(const char *p, float *x) {
+  u32x4 v;
+  if (DT == kFp32) {
+    typedef float f4u __attribute__((ext_vector_type(4), aligned(4)));
+    const f4u f = *reinterpret_cast<const f4u *>(p);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) x[i] = f[i];
+    return;
+  }
+  typedef uint32_t u4u __attribute__((ext_vector_type(4), aligned(2)));
+  const u4u w = *reinterpret_cast<const u4u *>(p);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    v[i] = w[i];
+    x[2 * i] = DT == kBf16 ? Bf16::lo(v[i]) : Fp16::lo(v[i]);
+    x[2 * i + 1] = DT == kBf16 ? Bf16::hi(v[i]) : Fp16::hi(v[i]);
+  }
+}
+
+// entries v * kVec.. of a range [0, n) (past it: `fill`)
+template <int DT>
+__device__ inline void load_some(const char *p, int64_t v, int64_t n, float fill, float *x) {
+  constexpr int kVec = Elem<DT>::kVec;
+  if ((v + 1) * kVec <= n) {
+    load_vec<DT>(p + v * 16, x);
+  } else {
+#pragma unroll
+    for (int i = 0; i < kVec; ++i) x[i] = v * kVec + i < n ? load_one<DT>(p, v * kVec + i) : fill;
+  }
+}
+
+// Sort key of an entry: larger for a larger value, then for a lower index; 0 for a NaN.
+__device__ inline uint64_t key_of(float x, int64_t index) {
+  if (x != x) return 0;
+  const uint32_t b = __builtin_bit_cast(uint32_t, x + 0.f);
+  const uint32_t o = (b & 0x80000000u) ? ~b : b | 0x80000000u;
+  return (uint64_t)o << 32 | (0xffffffffu - (uint32_t)index);
+}
+__device__ inline float key_value(uint64_t k) {
+  const uint32_t o = (uint32_t)(k >> 32);
+  return __builtin_bit_cast(float, (o & 0x80000000u) ? o & 0x7fffffffu : ~o);
+}
+__device__ inline int64_t key_index(uint64_t k) { return 0xffffffffu - (uint32_t)k; }
+
+// Running sums at the maximum m (raw units; kLowest before the first entry).
+struct Sums {
+  float m, a, b;
+};
+__device__ inline void raise(Sums &s, float m, float c2) {
+  const float d = fmaxf((s.m - m) * c2, -1e4f);   // (finite: the sums may be 0)
+  const float f = fast_exp2(d);
+  s.b = (s.b + s.a * d) * f;
+  s.a *= f;
+  s.m = m;
+}
+__device__ inline void add(Sums &s, float x, float c2) {
+  const float d = (x - s.m) * c2;
+  const float e = fast_exp2(d);
+  s.a += e;
+  s.b = __builtin_fmaf(e, fmaxf(d, -200.f), s.b);   // (a ruled out entry: 0 times -200)
+}
+__device__ inline Sums joined(Sums x, Sums y, float c2) {
+  const float m = fmaxf(x.m, y.m);
+  raise(x, m, c2);
+  raise(y, m, c2);
+  return Sums{m, x.a + y.a, x.b + y.b};
+}
+
+__device__ inline uint64_t shfl_xor64(uint64_t v, int o) {
+  return (uint64_t)__shfl_xor((uint32_t)(v >> 32), o) << 32 | __shfl_xor((uint32_t)v, o);
+}
+__device__ inline uint64_t max64(uint64_t a, uint64_t b) { return a > b ? a : b; }
+
+struct RowOut {
+  float lse, logp, entropy;
+};
+// x_t: the given entry (only read if there is one)
+__device__ inline RowOut finish(const Sums &s, float scale, bool has, float xt) {
+  RowOut r;
+  if (s.a == 0.f) {      // nothing but ruled out entries
+    const float inf = __builtin_inff();
+    return RowOut{-inf, has ? -inf : 0.f, 0.f};
+  }
+  const float la = logf(s.a);
+  r.lse = __builtin_fmaf(scale, s.m, la);
+  r.logp = has ? __builtin_fmaf(scale, xt - s.m, -la) : 0.f;
+  r.entropy = la - kLn2 * (s.b / s.a);
+  return r;
+}
+__device__ inline float alt_logp(const Sums &s, float scale, uint64_t key) {
+  if (key == 0) return __builtin_nanf("");
+  if (s.a == 0.f) return -__builtin_inff();
+  return __builtin_fmaf(scale, key_value(key) - s.m, -logf(s.a));
+}
+
+// ------------------------------------------------------------------ short rows
+// One wavefront per row, the row in registers (VL vectors a lane).
+template <int DT, int VL>
+__global__ __launch_bounds__(kThreads) void logprob_wave(const LogprobArgs a) {
+  constexpr int kVec = Elem<DT>::kVec;
+  const int lane = threadIdx.x & 63;
+  const int64_t row = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+  if (row >= a.rows) return;
+  const char *p = static_cast<const char *>(a.x) + row * a.row * Elem<DT>::kSize;
+  const float c2 = a.scale * kLog2e;
+  float x[VL][kVec];
+  float m = kLowest;
+#pragma unroll
+  for (int v = 0; v < VL; ++v) {
+    load_some<DT>(p, v * 64 + lane, a.width, -__builtin_inff(), x[v]);
+#pragma unroll
+    for (int i = 0; i < kVec; ++i) m = fmaxf(m, x[v][i]);
+  }
+#pragma unroll
+  for (int o = 32; o; o >>= 1) m = fmaxf(m, __shfl_xor(m, o));
+  Sums s{m, 0.f, 0.f};
+#pragma unroll
+  for (int v = 0; v < VL; ++v)
+#pragma unroll
+    for (int i = 0; i < kVec; ++i) add(s, x[v][i], c2);
+#pragma unroll
+  for (int o = 32; o; o >>= 1) {
+    s.a += __shfl_xor(s.a, o);
+    s.b += __shfl_xor(s.b, o);
+  }
+  const int64_t t = a.target ? a.target[row] : -1;
+  const bool has = t >= 0 && t < a.width;
+  if (lane == 0) {
+    const RowOut r = finish(s, a.scale, has, has ? load_one<DT>(p, t) : 0.f);
+    if (a.logp) a.logp[row] = r.logp;
+    if (a.entropy) a.entropy[row] = r.entropy;
+    if (a.lse) a.lse[row] = r.lse;
+  }
+  uint64_t last = ~0ull;
+  for (int k = 0; k < a.top; ++k) {     // the best entry below the last one
+    uint64_t best = 0;
+#pragma unroll
+    for (int v = 0; v < VL; ++v)
+#pragma unroll
+      for (int i = 0; i < kVec; ++i) {
+        const int64_t at = ((int64_t)v * 64 + lane) * kVec + i;
+        const uint64_t key = at < a.width ? key_of(x[v][i], at) : 0;
+        if (key < last) best = max64(best, key);
+      }
+#pragma unroll
+    for (int o = 32; o; o >>= 1) best = max64(best, shfl_xor64(best, o));
+    if (lane == 0) {
+      a.top_logp[row * a.top + k] = alt_logp(s, a.scale, best);
+      a.top_id[row * a.top + k] = best ? key_index(best) : -1;
+    }
+    last = best;
+  }
+}
+
+// ------------------------------------------------------------------ alternatives of a block
+struct TopShared {
+  uint64_t group[kThreads];
+  uint64_t list[kList];
+  uint64_t best[4];
+  int owners[kThreads];
+  int n_owners, n_list;
+};
+
+// The k-th largest of the block's keys of groups of 256 / G threads (0 if fewer than k).
+__device__ inline uint64_t bound_from_below(TopShared &sh, uint64_t mine, int k) {
+  uint64_t g = mine;
+  const int groups = k <= 32 ? 64 : 256;
+  if (groups == 64) {
+    g = max64(g, shfl_xor64(g, 1));
+    g = max64(g, shfl_xor64(g, 2));
+  }
+  const int per = kThreads / groups;
+  if (threadIdx.x % per == 0) sh.group[threadIdx.x / per] = g;
+  if (threadIdx.x == 0) {
+    sh.n_owners = sh.n_list = 0;
+    sh.best[0] = 0;
+  }
+  __syncthreads();
+  if ((int)threadIdx.x < groups) {
+    const uint64_t own = sh.group[threadIdx.x];
+    int rank = 0;
+    for (int i = 0; i < groups; ++i) rank += sh.group[i] > own ? 1 : 0;
+    // (nonzero keys are distinct)
+    if (own && rank == k - 1) sh.best[0] = own;
+  }
+  __syncthreads();
+  return sh.best[0];
+}
+
+__device__ inline void offer(TopShared &sh, uint64_t key, uint64_t bound) {
+  if (key && key >= bound) {
+    const int at = atomicAdd(&sh.n_list, 1);
+    if (at < kList) sh.list[at] = key;
+  }
+}
+
+// Calls out(k, key) for the k best of the listed keys, in order.
+template <class Out>
+__device__ inline void rank_list(TopShared &sh, int n, int k, Out out) {
+  for (int i = threadIdx.x; i < n; i += kThreads) {
+    const uint64_t own = sh.list[i];
+    int rank = 0;
+    for (int j = 0; j < n; ++j) rank += sh.list[j] > own ? 1 : 0;
+    if (rank < k) out(rank, own);
+  }
+  for (int r = n + threadIdx.x; r < k; r += kThreads) out(r, (uint64_t)0);
+}
+
+// ------------------------------------------------------------------ long rows
+// A block's range [lo, hi) of a row: sums and the k best keys.
+template <int DT, class Out>
+__device__ inline Sums range_pass(TopShared &sh, const char *row, int64_t lo, int64_t hi, float c2,
+                                  int k, Out out) {
+  constexpr int kVec = Elem<DT>::kVec, kUnroll = 4;
+  const char *p = row + lo * Elem<DT>::kSize;
+  const int64_t n = hi - lo, nv = (n + kVec - 1) / kVec;
+  const float inf = __builtin_inff();
+  Sums s{kLowest, 0.f, 0.f};
+  float best = -inf;                    // largest entry of this thread,
+  int64_t best_v = threadIdx.x;         // and the first of its vectors that holds it
+  auto batch = [&](int64_t v0, auto whole) {
+    constexpr bool kWhole = decltype(whole)::value;
+    float x[kUnroll][kVec], top[kUnroll];
+#pragma unroll
+    for (int u = 0; u < kUnroll; ++u) {
+      const int64_t v = v0 + u * kThreads;
+      if (kWhole) load_vec<DT>(p + v * 16, x[u]);
+      else load_some<DT>(p, v, n, -inf, x[u]);
+    }
+#pragma unroll
+    for (int u = 0; u < kUnroll; ++u) {
+      top[u] = x[u][0];
+#pragma unroll
+      for (int i = 1; i < kVec; ++i) top[u] = fmaxf(top[u], x[u][i]);
+      if (top[u] > best) {
+        best = top[u];
+        best_v = v0 + u * kThreads;
+      }
+    }
+    raise(s, fmaxf(s.m, best), c2);
+#pragma unroll
+    for (int u = 0; u < kUnroll; ++u)
+#pragma unroll
+      for (int i = 0; i < kVec; ++i) add(s, x[u][i], c2);
+  };
+  int64_t v = threadIdx.x;
+  for (; (v + (kUnroll - 1) * kThreads + 1) * kVec <= n; v += kUnroll * kThreads)
+    batch(v, std::true_type{});
+  for (; v < nv; v += kUnroll * kThreads) batch(v, std::false_type{});
+
+  if (k > 0) {
+    uint64_t mine = 0;
+    if (best_v < nv) {
+      float x[kVec];
+      load_some<DT>(p, best_v, n, __builtin_nanf(""), x);
+#pragma unroll
+      for (int i = 0; i < kVec; ++i) mine = max64(mine, key_of(x[i], lo + best_v * kVec + i));
+    }
+    const uint64_t bound = bound_from_below(sh, mine, k);
+    if (mine && mine >= bound) sh.owners[atomicAdd(&sh.n_owners, 1)] = threadIdx.x;
+    __syncthreads();
+    // a wavefront looks through one such thread's vectors at a time
+    const int lane = threadIdx.x & 63;
+    for (int o = threadIdx.x >> 6; o < sh.n_owners; o += 4)
+      for (int64_t w = sh.owners[o] + (int64_t)lane * kThreads; w < nv; w += 64 * kThreads) {
+        float x[kVec];
+        load_some<DT>(p, w, n, __builtin_nanf(""), x);
+#pragma unroll
+        for (int i = 0; i < kVec; ++i) offer(sh, key_of(x[i], lo + w * kVec + i), bound);
+      }
+    __syncthreads();
+    const int listed = sh.n_list;
+    if (listed <= kList) {
+      rank_list(sh, listed, k, out);
+    } else {
+      // more entries above the bound than the list holds (possible where equal entries
+      // fall on few threads): one pass over the range per alternative
+      uint64_t last = ~0ull;
+      for (int r = 0; r < k; ++r) {
+        uint64_t b = 0;
+        for (int64_t w = threadIdx.x; w < nv; w += kThreads) {
+          float x[kVec];
+          load_some<DT>(p, w, n, __builtin_nanf(""), x);
+#pragma unroll
+          for (int i = 0; i < kVec; ++i) {
+            const uint64_t key = key_of(x[i], lo + w * kVec + i);
+            if (key < last) b = max64(b, key);
+          }
+        }
+#pragma unroll
+        for (int o = 32; o; o >>= 1) b = max64(b, shfl_xor64(b, o));
+        if (lane == 0) sh.best[threadIdx.x >> 6] = b;
+        __syncthreads();
+        last = max64(max64(sh.best[0], sh.best[1]), max64(sh.best[2], sh.best[3]));
+        __syncthreads();
+        if (threadIdx.x == 0) out(r, last);
+      }
+    }
+  }
+  return s;
+}
+
+// The block's sums, the same on every thread.
+__device__ inline Sums block_sums(Sums s, float c2, float (*red)[3]) {
+#pragma unroll
+  for (int o = 32; o; o >>= 1) {
+    Sums y{__shfl_xor(s.m, o), __shfl_xor(s.a, o), __shfl_xor(s.b, o)};
+    s = joined(s, y, c2);
+  }
+  const int wave = threadIdx.x >> 6;
+  if ((threadIdx.x & 63) == 0) {
+    red[wave][0] = s.m;
+    red[wave][1] = s.a;
+    red[wave][2] = s.b;
+  }
+  __syncthreads();
+  s = Sums{red[0][0], red[0][1], red[0][2]};
+#pragma unroll
+  for (int w = 1; w < 4; ++w) s = joined(s, Sums{red[w][0], red[w][1], red[w][2]}, c2);
+  return s;
+}
+
+template <int DT>
+__device__ inline void write_row(const LogprobArgs &a, int64_t row, const Sums &s, const char *p) {
+  const int64_t t = a.target ? a.target[row] : -1;
+  const bool has = t >= 0 && t < a.width;
+  const RowOut r = finish(s, a.scale, has, has ? load_one<DT>(p, t) : 0.f);
+  if (a.logp) a.logp[row] = r.logp;
+  if (a.entropy) a.entropy[row] = r.entropy;
+  if (a.lse) a.lse[row] = r.lse;
+}
+
+template <int DT>
+__global__ __launch_bounds__(kThreads) void logprob_row(const LogprobArgs a) {
+  __shared__ TopShared sh;
+  __shared__ uint64_t keys[kMaxTop];
+  __shared__ float red[4][3];
+  const int64_t row = blockIdx.x;
+  const char *p = static_cast<const char *>(a.x) + row * a.row * Elem<DT>::kSize;
+  const float c2 = a.scale * kLog2e;
+  Sums s = range_pass<DT>(sh, p, 0, a.width, c2, a.top, [&](int r, uint64_t k) { keys[r] = k; });
+  s = block_sums(s, c2, red);   // (its barrier also covers keys)
+  if (threadIdx.x == 0) write_row<DT>(a, row, s, p);
+  for (int r = threadIdx.x; r < a.top; r += kThreads) {
+    a.top_logp[row * a.top + r] = alt_logp(s, a.scale, keys[r]);
+    a.top_id[row * a.top + r] = keys[r] ? key_index(keys[r]) : -1;
+  }
+}
+
+// ------------------------------------------------------------------ rows shared by blocks
+struct SplitPlan {
+  int parts;       // blocks of a row
+  int64_t chunk;   // entries of a block
+};
+SplitPlan split_plan(int32_t rows, int32_t width, int32_t top, int cus) {
+  SplitPlan p{1, width};
+  // one block per row where that fills the device, or the rows are short
+  if (rows >= 2 * cus || width <= 8192) return p;
+  int64_t parts = (4 * (int64_t)cus + rows - 1) / rows;
+  const int64_t most = width / 2048;            // (a vector or two per thread)
+  if (parts > most) parts = most;
+  if (top > 0 && parts > kList / top) parts = kList / top;
+  if (parts < 2) return p;
+  p.chunk = ((width + parts - 1) / parts + 63) / 64 * 64;
+  p.parts = (int)((width + p.chunk - 1) / p.chunk);
+  return p;
+}
+
+template <int DT>
+__global__ __launch_bounds__(kThreads) void logprob_part(const LogprobArgs a, SplitPlan sp,
+                                                         float *sums, uint64_t *keys) {
+  __shared__ TopShared sh;
+  __shared__ float red[4][3];
+  const int64_t row = blockIdx.x / sp.parts;
+  const int part = blockIdx.x % sp.parts;
+  const char *p = static_cast<const char *>(a.x) + row * a.row * Elem<DT>::kSize;
+  const float c2 = a.scale * kLog2e;
+  const int64_t lo = part * sp.chunk, hi = lo + sp.chunk < a.width ? lo + sp.chunk : a.width;
+  uint64_t *out = keys + (int64_t)blockIdx.x * a.top;
+  Sums s = range_pass<DT>(sh, p, lo, hi, c2, a.top, [&](int r, uint64_t k) { out[r] = k; });
+  s = block_sums(s, c2, red);
+  if (threadIdx.x == 0) {
+    sums[3 * (int64_t)blockIdx.x] = s.m;
+    sums[3 * (int64_t)blockIdx.x + 1] = s.a;
+    sums[3 * (int64_t)blockIdx.x + 2] = s.b;
+  }
+}
+
+template <int DT>
+__global__ __launch_bounds__(kThreads) void logprob_join(const LogprobArgs a, SplitPlan sp,
+                                                         const float *sums, const uint64_t *keys) {
+  __shared__ TopShared sh;
+  __shared__ float red[4][3];
+  const int64_t row = blockIdx.x;
+  const char *p = static_cast<const char *>(a.x) + row * a.row * Elem<DT>::kSize;
+  const float c2 = a.scale * kLog2e;
+  Sums s{kLowest, 0.f, 0.f};
+  for (int i = threadIdx.x; i < sp.parts; i += kThreads) {
+    const float *q = sums + 3 * (row * sp.parts + i);
+    s = joined(s, Sums{q[0], q[1], q[2]}, c2);
+  }
+  s = block_sums(s, c2, red);
+  if (threadIdx.x == 0) write_row<DT>(a, row, s, p);
+  if (a.top == 0) return;
+  const uint64_t *kr = keys + row * sp.parts * a.top;
+  const int n = sp.parts * a.top;       // at most kList
+  uint64_t mine = 0;
+  for (int i = threadIdx.x; i < n; i += kThreads) mine = max64(mine, kr[i]);
+  const uint64_t bound = bound_from_below(sh, mine, a.top);
+  for (int i = threadIdx.x; i < n; i += kThreads) offer(sh, kr[i], bound);
+  __syncthreads();
+  rank_list(sh, sh.n_list, a.top, [&](int r, uint64_t k) {
+    a.top_logp[row * a.top + r] = alt_logp(s, a.scale, k);
+    a.top_id[row * a.top + r] = k ? key_index(k) : -1;
+  });
+}
+
+// ------------------------------------------------------------------ gradient
+// dx_v = c [ g (1[v = t] - p_v) - h p_v (log p_v + H) ]: one pass, each block a range of a
+// row (or, for short rows, each wavefront a row).
+template <int DT>
+__device__ inline void store_vec(char *p, const float *y) {
+  if (DT == kFp32) {
+    typedef float f4u __attribute__((ext_vector_type(4), aligned(4)));
+    *reinterpret_cast<f4u *>(p) = f4u{y[0], y[1], y[2], y[3]};
+    return;
+  }
+  typedef uint32_t u4u __attribute__((ext_vector_type(4), aligned(2)));
+  u4u w;
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+    w[i] = DT == kBf16 ? Bf16::pack(y[2 * i], y[2 * i + 1]) : Fp16::pack(y[2 * i], y[2 * i + 1]);
+  *reinterpret_cast<u4u *>(p) = w;
+}
+template <int DT>
+__device__ inline void store_one(char *p, int64_t i, float y) {
+  if (DT == kBf16) Bf16::store(p, i, y);
+  else if (DT == kFp16) Fp16::store(p, i, y);
+  else reinterpret_cast<float *>(p)[i] = y;
+}
+
+template <int DT>
+__global__ __launch_bounds__(kThreads) void logprob_grad(const LogprobArgs a, int per_row,
+                                                         int threads) {
+  constexpr int kVec = Elem<DT>::kVec;
+  // `threads` of the block's 256 share a row
+  const int64_t unit = (int64_t)blockIdx.x * (kThreads / threads) + threadIdx.x / threads;
+  const int64_t row = unit / per_row;
+  if (row >= a.rows) return;
+  const int64_t first = unit % per_row * threads + threadIdx.x % threads;
+  const int64_t step = (int64_t)per_row * threads;
+  const char *p = static_cast<const char *>(a.x) + row * a.row * Elem<DT>::kSize;
+  char *q = static_cast<char *>(a.dx) + row * a.dx_row * Elem<DT>::kSize;
+  const float lse = a.lse[row];
+  const bool none = lse == -__builtin_inff();
+  const int64_t t = a.target ? a.target[row] : -1;
+  const bool has = !none && t >= 0 && t < a.width && a.g_logp;
+  const float g = has ? a.g_logp[row] * a.scale : 0.f;
+  const float eh = (!none && a.g_entropy) ? a.g_entropy[row] * a.scale : 0.f;
+  const float H = (!none && a.g_entropy) ? a.entropy[row] : 0.f;
+  const float w = __builtin_fmaf(eh, H, g);
+  const int64_t nv = (a.width + kVec - 1) / kVec;
+  for (int64_t v = first; v < nv; v += step) {
+    float x[kVec];
+    load_some<DT>(p, v, a.width, -__builtin_inff(), x);
+#pragma unroll
+    for (int i = 0; i < kVec; ++i) {
+      const float lp = __builtin_fmaf(x[i], a.scale, -lse);
+      const float pr = fast_exp2(lp * kLog2e);
+      // -p (g + h (log p + H)), 0 for a ruled out entry
+      float y = -pr * __builtin_fmaf(eh, fmaxf(lp, -1e30f), w);
+      if (none) y = 0.f;
+      if (v * kVec + i == t) y += g;
+      x[i] = y;
+    }
+    if ((v + 1) * kVec <= a.width) {
+      store_vec<DT>(q + v * 16, x);
+    } else {
+#pragma unroll
+      for (int i = 0; i < kVec; ++i)
+        if (v * kVec + i < a.width) store_one<DT>(q, v * kVec + i, x[i]);
+    }
+  }
+}
+
+template <int DT>
+hipError_t forward(const LogprobArgs &a, void *ws, int cus, hipStream_t s) {
+  constexpr int kVec = Elem<DT>::kVec;
+  if (a.width <= kWaveWidth) {
+    const dim3 grid((uint32_t)((a.rows + 3) / 4));
+    const int vl = (a.width + 64 * kVec - 1) / (64 * kVec);
+    if (vl <= 1) logprob_wave<DT, 1><<<grid, kThreads, 0, s>>>(a);
+    else if (vl <= 2) logprob_wave<DT, 2><<<grid, kThreads, 0, s>>>(a);
+    else logprob_wave<DT, kWaveWidth / (64 * kVec)><<<grid, kThreads, 0, s>>>(a);
+    return hipGetLastError();
+  }
+  const SplitPlan sp = split_plan(a.rows, a.width, a.top, cus);
+  if (sp.parts == 1) {
+    logprob_row<DT><<<dim3((uint32_t)a.rows), kThreads, 0, s>>>(a);
+    return hipGetLastError();
+  }
+  const int64_t n = (int64_t)a.rows * sp.parts;
+  uint64_t *keys = static_cast<uint64_t *>(ws);
+  float *sums = reinterpret_cast<float *>(keys + n * a.top);
+  logprob_part<DT><<<dim3((uint32_t)n), kThreads, 0, s>>>(a, sp, sums, keys);
+  logprob_join<DT><<<dim3((uint32_t)a.rows), kThreads, 0, s>>>(a, sp, sums, keys);
+  return hipGetLastError();
+}
+
+template <int DT>
+hipError_t gradient(const LogprobArgs &a, int cus, hipStream_t s) {
+  constexpr int kVec = Elem<DT>::kVec;
+  const int64_t nv = (a.width + kVec - 1) / kVec;
+  // a wavefront per row up to 512 vectors, a block per row above; more blocks per row (each
+  // thread 4 vectors at least) while the rows do not fill the device
+  const int threads = nv <= 512 ? 64 : kThreads;
+  int64_t per_row = 1;
+  if (threads == kThreads) {
+    const int64_t want = (8 * (int64_t)cus + a.rows - 1) / a.rows, most = nv / (4 * kThreads);
+    per_row = want < most ? want : most;
+    if (per_row < 1) per_row = 1;
+  }
+  const int64_t units = (int64_t)a.rows * per_row, per = kThreads / threads;
+  logprob_grad<DT><<<dim3((uint32_t)((units + per - 1) / per)), kThreads, 0, s>>>(a, (int)per_row,
+                                                                                  threads);
+  return hipGetLastError();
+}
+
+}  // namespace
+
+size_t logprob_bytes(int32_t rows, int32_t width, int32_t top, int cus) {
+  if (width <= kWaveWidth) return 0;
+  const SplitPlan sp = split_plan(rows, width, top, cus);
+  return sp.parts == 1 ? 0 : (size_t)rows * sp.parts * ((size_t)top * 8 + 12);
+}
+
+hipError_t launch_logprob(const LogprobArgs &a, void *ws, int cus, hipStream_t s) {
+  if (a.dtype == kBf16) return forward<kBf16>(a, ws, cus, s);
+  if (a.dtype == kFp16) return forward<kFp16>(a, ws, cus, s);
+  return forward<kFp32>(a, ws, cus, s);
+}
+
+hipError_t launch_logprob_grad(const LogprobArgs &a, int cus, hipStream_t s) {
+  if (a.dtype == kBf16) return gradient<kBf16>(a, cus, s);
+  if (a.dtype == kFp16) return gradient<kFp16>(a, cus, s);
+  return gradient<kFp32>(a, cus, s);
+}
+
+}  // namespace bgp

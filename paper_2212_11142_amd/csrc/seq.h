@@ -1,0 +1,88 @@
+// Internal declarations of the sequence-surrogate operators (attention over packed
+// histories and log probabilities): kernels in attend.hip, attend_few.hip, attend_grad.hip
+// and logprob.hip, their C-ABI in seq_abi.hip.
+#pragma once
+#include <hip/hip_runtime.h>
+#include <cstddef>
+#include <cstdint>
+#include <string>
+
+#include "baco_gp.h"
+#include "lds_limit.h"
+
+namespace bgp {
+
+constexpr int kSeqMaxDim = 128;       // head size
+constexpr int kMaxBuckets = 64;       // buckets of one side
+constexpr int kMaxReach = 1024;       // first distance of the last bucket
+constexpr int kMaxTop = 128;          // alternatives of a row
+
+// First distance of each bucket of a side (start[0] = 0, ascending).
+struct BucketMap {
+  int32_t per_side;
+  int32_t two_sided;
+  int32_t start[kMaxBuckets];
+};
+
+struct AttnArgs {
+  const char *q, *k, *v;
+  char *o;
+  float *lse;                          // [heads][q_rows]
+  // strides in bytes
+  int64_t q_row, q_head, k_row, k_head, v_row, v_head, o_row, o_head;
+  const int32_t *qb, *qe, *kb, *ke, *prefix;
+  int32_t docs, heads, kv_heads, group, bytes;  // bytes: of a head's row, 2 dim
+  int32_t q_rows, k_rows, max_q, max_k;
+  int32_t causal;
+  float scale, cap;
+  const float *slopes;                 // [heads]
+  const void *table;                   // [heads][buckets]
+  BucketMap buckets;
+  int32_t fp16;
+};
+
+// Gradient: q, k, v, o, lse as of the forward call.
+struct AttnGradArgs {
+  AttnArgs f;
+  const char *dout;
+  char *dq, *dk, *dv;
+  void *dtable;                        // [heads][buckets] or null
+  int64_t do_row, do_head, dq_row, dq_head, dk_row, dk_head, dv_row, dv_head;
+  // workspace
+  float *delta;                        // [heads][q_rows] dout . out
+  float *bound;                        // fp16: block maxima and the power of two dS is kept at
+  float *tpart;                        // [tiles][heads][buckets] partial table gradients
+};
+
+hipError_t launch_attend(const AttnArgs &a, hipStream_t s);
+// few query rows: key ranges split over blocks; part: attend_few_bytes() of workspace
+size_t attend_few_bytes(int32_t docs, int32_t kv_heads, int32_t group, int32_t max_q, int32_t max_k,
+                        int32_t dim, int cus);
+bool attend_use_few(int32_t docs, int32_t kv_heads, int32_t group, int32_t max_q, int32_t max_k,
+                    int cus);
+hipError_t launch_attend_few(const AttnArgs &a, float *part, int cus, hipStream_t s);
+
+size_t attend_grad_bytes(int32_t q_rows, int32_t docs, int32_t heads, int32_t buckets, bool fp16);
+hipError_t launch_attend_grad(const AttnGradArgs &a, void *ws, hipStream_t s);
+
+struct LogprobArgs {
+  const void *x;
+  int64_t row;                         // row stride in elements
+  int32_t rows, width, top, dtype;
+  float scale;
+  const int64_t *target;
+  float *logp, *entropy, *lse, *top_logp;
+  int64_t *top_id;
+  const float *g_logp, *g_entropy;     // gradient
+  void *dx;
+  int64_t dx_row;
+};
+size_t logprob_bytes(int32_t rows, int32_t width, int32_t top, int cus);
+hipError_t launch_logprob(const LogprobArgs &a, void *ws, int cus, hipStream_t s);
+hipError_t launch_logprob_grad(const LogprobArgs &a, int cus, hipStream_t s);
+
+// abi.hip: records the calling thread's error message
+gp_status seq_fail(gp_status st, const std::string &msg);
+int seq_cus(hipStream_t s);
+
+}  // namespace bgp

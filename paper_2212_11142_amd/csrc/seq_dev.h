@@ -1,0 +1,362 @@
+// Device building blocks of the sequence-surrogate kernels: matrix-instruction tiles of
+// 16-bit operands, tile loads into LDS, and the masked, capped, biased scores.
+//
+// Tile forms. v_mfma_f32_32x32x16 takes A (row = lane % 32) and B (column = lane % 32) as
+// 8 consecutive k per lane, k = 8 (lane / 32) + j, and gives D with column = lane % 32 and
+// row = 8 g + 4 (lane / 32) + r in element 4 g + r. A product whose result is the B operand
+// of the next one is therefore taken transposed (scores as keys x queries): a lane then
+// holds 4 + 4 consecutive rows of each 16, which is the B operand of the next product up to
+// the order of k, and k's order is free as long as A is read in the same one. So the
+// probabilities never leave their lane's registers, and A (V, dO, Q, K with the summed
+// axis along rows) comes out of LDS through the transposing read, 4 rows at a time.
+#pragma once
+#include "seq.h"
+
+namespace bgp {
+
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
+
+constexpr float kLog2e = 1.4426950408889634f;
+constexpr float kLn2 = 0.6931471805599453f;
+
+// ------------------------------------------------------------------ element types
+struct Bf16 {
+  static constexpr uint32_t kExp = 0x7f807f80u, kExpOne = 0x00800080u;
+  static __device__ f32x16 mfma(u32x4 a, u32x4 b, f32x16 c) {
+    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a),
+                                                   __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+  }
+  // two values rounded to nearest even, the first in the low half
+  static __device__ uint32_t pack(float a, float b) {
+    return __builtin_bit_cast(uint32_t, bf16x2{(__bf16)a, (__bf16)b});
+  }
+  static __device__ float lo(uint32_t x) { return __builtin_bit_cast(float, x << 16); }
+  static __device__ float hi(uint32_t x) { return __builtin_bit_cast(float, x & 0xffff0000u); }
+  static __device__ float load(const void *p, int64_t i) {
+    return __builtin_bit_cast(float, (uint32_t)static_cast<const uint16_t *>(p)[i] << 16);
+  }
+  static __device__ void store(void *p, int64_t i, float v) {
+    static_cast<__bf16 *>(p)[i] = (__bf16)v;
+  }
+};
+struct Fp16 {
+  static constexpr uint32_t kExp = 0x7c007c00u, kExpOne = 0x04000400u;
+  static __device__ f32x16 mfma(u32x4 a, u32x4 b, f32x16 c) {
+    return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, a),
+                                                  __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
+  }
+  static __device__ uint32_t pack(float a, float b) {
+    return __builtin_bit_cast(uint32_t, f16x2{(_Float16)a, (_Float16)b});
+  }
+  static __device__ float lo(uint32_t x) { return (float)__builtin_bit_cast(f16x2, x)[0]; }
+  static __device__ float hi(uint32_t x) { return (float)__builtin_bit_cast(f16x2, x)[1]; }
+  static __device__ float load(const void *p, int64_t i) {
+    return (float)static_cast<const _Float16 *>(p)[i];
+  }
+  static __device__ void store(void *p, int64_t i, float v) {
+    static_cast<_Float16 *>(p)[i] = (_Float16)v;
+  }
+};
+
+__device__ inline float fast_exp2(float x) { return __builtin_amdgcn_exp2f(x); }
+__device__ inline int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
+
+// value of the lane 32 away
+__device__ inline float other_half(float x) {
+  const u32x2 r = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(uint32_t, x),
+                                                   __builtin_bit_cast(uint32_t, x), false, false);
+  return __builtin_bit_cast(float, (threadIdx.x & 32) ? r[0] : r[1]);
+}
+
+// ------------------------------------------------------------------ LDS tiles
+// A tile is rows of DP 16-bit values without padding. The 16-byte pieces of a row are
+// stored in the order piece ^ swizzle(row): then both the row reads (32 rows, one piece
+// each half wavefront) and the transposing reads (4 rows x 4 pieces per half wavefront)
+// touch all of LDS's 64 banks evenly.
+template <int DP>
+__device__ inline int swizzle(int row) {
+  if (DP == 128) return ((row & 3) << 2) | ((row >> 2) & 3);
+  return (((row >> 1) & 1) << 2) | ((row >> 2) & 3);
+}
+
+// Rows r0.. of a matrix with `rows` rows from base (row stride `stride` bytes, `bytes` of
+// each row used) as a buffer: reads past it, and of pieces past `bytes`, give zeros.
+__device__ inline u32x4 row_buffer(const char *base, int64_t r0, int rows, int64_t stride,
+                                   int bytes) {
+  const uint64_t a = (uint64_t)base + (uint64_t)(r0 * stride);
+  u32x4 d;
+  d[0] = uniform((int)(uint32_t)a);
+  d[1] = uniform((int)((uint32_t)(a >> 32) & 0xffffu));
+  d[2] = uniform(rows > 0 ? (int)((rows - 1) * stride) + bytes : 0);
+  d[3] = 0x00020000u;
+  return d;
+}
+
+// Starts the copy of ROWS rows of a buffer into an LDS tile by WAVES wavefronts (`wave`
+// is this one's number): each instruction moves 64 pieces of 16 bytes, and what is out of
+// range arrives as zeros. Completion: wait_copies().
+template <int DP, int ROWS, int WAVES>
+struct TileCopy {
+  static constexpr int kPieces = DP / 8;               // pieces of a row
+  static constexpr int kRowsPer = 64 / kPieces;        // rows an instruction moves
+  static constexpr int kCount = ROWS / kRowsPer / WAVES;
+  int voff[kCount];
+  int lds0;
+
+  __device__ void init(int wave, int lane, int stride, int bytes) {
+#pragma unroll
+    for (int i = 0; i < kCount; ++i) {
+      const int row = (i * WAVES + wave) * kRowsPer + lane / kPieces;
+      const int piece = (lane % kPieces) ^ swizzle<DP>(row);
+      voff[i] = piece * 16 < bytes ? row * stride + piece * 16 : 0x7ffffff0;
+    }
+    lds0 = wave * 1024;
+  }
+  __device__ void start(u32x4 buf, uint32_t lds) const {
+#pragma unroll
+    for (int i = 0; i < kCount; ++i) {
+      const uint32_t m = uniform((int)(lds + lds0 + i * WAVES * 1024));
+      asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds"
+                   ::"s"(m), "v"(voff[i]), "s"(buf)
+                   : "memory");
+    }
+  }
+};
+
+// Until the copies that this wavefront started are in LDS, but for the last `left` of them.
+template <int LEFT>
+__device__ inline void wait_copies() {
+  asm volatile("s_waitcnt vmcnt(%0)" ::"n"(LEFT) : "memory");
+}
+// Joins the block: copies started by all wavefronts are in LDS, reads of LDS are done.
+__device__ inline void copies_barrier() {
+  asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+}
+
+__device__ inline uint32_t lds_address(const void *p) {
+  return (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const void *)p;
+}
+
+// A operand (32 rows from row0, k = 16 s + ..) of a tile whose rows run along k.
+template <int DP>
+__device__ inline u32x4 row_operand(const char *tile, int row0, int s, int lane) {
+  const int row = row0 + (lane & 31);
+  const int piece = (2 * s + (lane >> 5)) ^ swizzle<DP>(row);
+  return *reinterpret_cast<const u32x4 *>(tile + row * (DP * 2) + piece * 16);
+}
+
+// A operand of the transposed tile: rows of the operand are the columns 32 c.. of the tile,
+// its k the tile's rows row0 + 16.. in the order of a D result's registers: lane half h has
+// the rows row0 + 4 h + {0..3} and row0 + 8 + 4 h + {0..3}.
+template <int DP>
+__device__ inline u32x4 col_operand(const char *tile, int row0, int c, int lane) {
+  typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
+  const int row = row0 + 4 * (lane >> 5) + ((lane & 15) >> 2);
+  const int piece = 4 * c + 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1);
+  const int half = (lane & 1) * 8;
+  const char *p0 = tile + row * (DP * 2) + ((piece ^ swizzle<DP>(row)) * 16) + half;
+  const char *p1 = tile + (row + 8) * (DP * 2) + ((piece ^ swizzle<DP>(row + 8)) * 16) + half;
+  const s16x4 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)p0);
+  const s16x4 b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)p1);
+  const u32x2 ua = __builtin_bit_cast(u32x2, a), ub = __builtin_bit_cast(u32x2, b);
+  return u32x4{ua[0], ua[1], ub[0], ub[1]};
+}
+
+// B operand of 32 rows of a matrix in memory (column = row, k = 16 s + ..): one lane's
+// pieces for all s; rows from `rows` on and values from `bytes` on are zero.
+template <int DP>
+__device__ inline void load_operand(const char *base, int64_t stride, int row, int rows, int bytes,
+                                    int lane, u32x4 *out) {
+#pragma unroll
+  for (int s = 0; s < DP / 16; ++s) {
+    const int off = (2 * s + (lane >> 5)) * 16;
+    u32x4 v = {0, 0, 0, 0};
+    if (row < rows && off < bytes)
+      v = *reinterpret_cast<const u32x4 *>(base + (int64_t)row * stride + off);
+    out[s] = v;
+  }
+}
+
+// Writes a transposed result (D^T: element d = 32 c + 8 g + 4 (lane / 32) + r of the row at
+// p, both lane halves of a row) as 16-byte pieces, times f.
+template <class T, int DT>
+__device__ inline void store_row(char *p, bool ok, int bytes, const f32x16 *acc, float f, int lane) {
+  const int h = lane >> 5;
+#pragma unroll
+  for (int c = 0; c < DT; ++c)
+#pragma unroll
+    for (int g = 0; g < 4; g += 2) {
+      uint32_t w[4];
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const int e = 4 * (g + i);
+        w[2 * i] = T::pack(acc[c][e] * f, acc[c][e + 1] * f);
+        w[2 * i + 1] = T::pack(acc[c][e + 2] * f, acc[c][e + 3] * f);
+      }
+      // lower half: all of piece g, upper half: all of piece g + 1
+      const u32x2 x = __builtin_amdgcn_permlane32_swap(w[0], w[2], false, false);
+      const u32x2 y = __builtin_amdgcn_permlane32_swap(w[1], w[3], false, false);
+      const u32x4 v = {x[0], y[0], x[1], y[1]};
+      const int off = (32 * c + 8 * (g + h)) * 2;
+      if (ok && off < bytes) *reinterpret_cast<u32x4 *>(p + off) = v;
+    }
+}
+
+// ------------------------------------------------------------------ values in masked places
+// Nonzero if one of the 8 values is infinite or NaN (its exponent's carry goes into the
+// place of the sign).
+template <class T>
+__device__ inline uint32_t nonfinite(u32x4 v) {
+  uint32_t r = 0;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) r |= (v[i] & T::kExp) + T::kExpOne;
+  return r & 0x80008000u;
+}
+// The values with 0 in place of infinities and NaN.
+template <class T>
+__device__ inline u32x4 finite_part(u32x4 v) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const uint32_t t = (v[i] & T::kExp) + T::kExpOne;
+    if (t & 0x8000u) v[i] &= 0xffff0000u;
+    if (t & 0x80000000u) v[i] &= 0x0000ffffu;
+  }
+  return v;
+}
+// Sum of the infinities and NaN in column d of the rows r0..r1 - 1.
+template <class T>
+__device__ inline float nonfinite_sum(const char *base, int64_t stride, int r0, int r1, int d) {
+  float x = 0.f;
+  for (int r = r0; r < r1; ++r) {
+    const float v = T::load(base + r * stride, d);
+    if (!(__builtin_fabsf(v) < __builtin_inff())) x += v;
+  }
+  return x;
+}
+
+// ------------------------------------------------------------------ documents
+struct DocTile {
+  int doc, tile;  // doc < 0: past the last tile
+  int b0, b1;     // the document's rows on the tiled side
+};
+
+// The tile-th tile of TILE rows of the documents with rows [b[d], e[d]) within 0..limit, in
+// order. Every lane gets the same answer.
+template <int TILE>
+__device__ inline DocTile find_tile(const int32_t *b, const int32_t *e, int docs, int limit,
+                                    int tile) {
+  const int lane = threadIdx.x & 63;
+  for (int d0 = 0; d0 < docs; d0 += 64) {
+    int lo = 0, hi = 0;
+    if (d0 + lane < docs) {
+      lo = max(b[d0 + lane], 0);
+      hi = max(min(e[d0 + lane], limit), lo);
+    }
+    const int n = (hi - lo + TILE - 1) / TILE;
+    int inc = n;  // inclusive sum over the lanes
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+      const int v = __shfl_up(inc, o);
+      if (lane >= o) inc += v;
+    }
+    const unsigned long long past = __ballot(inc > tile);
+    if (past) {
+      const int l = __ffsll(past) - 1;
+      DocTile r;
+      r.doc = d0 + l;
+      r.b0 = uniform(__shfl(lo, l));
+      r.b1 = uniform(__shfl(hi, l));
+      r.tile = uniform(tile - __shfl(inc - n, l));
+      return r;
+    }
+    tile -= uniform(__shfl(inc, 63));
+  }
+  return DocTile{-1, 0, 0, 0};
+}
+
+// ------------------------------------------------------------------ scores
+// Score of a pair in units of log 2: capped product plus bias.
+struct ScoreScale {
+  float c;      // no cap: scale * log2(e); cap: 2 log2(e) scale / cap
+  float cap2;   // cap * log2(e)
+};
+
+// cap tanh(z / cap) = cap - 2 cap / (1 + e^(2 z / cap)), exact at both ends: the
+// exponential is 0 or infinite there.
+template <bool CAP>
+__device__ inline float scaled(float s, const ScoreScale &k) {
+  if (!CAP) return s * k.c;
+  const float r = __builtin_amdgcn_rcpf(1.f + fast_exp2(s * k.c));
+  return __builtin_fmaf(-2.f * k.cap2, r, k.cap2);
+}
+
+enum BiasKind { kBiasNone = 0, kBiasSlope = 1, kBiasTable = 2 };
+
+// Room on both sides of the table's distances -reach..reach, so that a block of 32 keys and
+// 32 queries of which any pair is nearer than reach reads the table without clamping.
+constexpr int kLutPad = 64;
+__host__ __device__ inline int lut_size(int reach) { return 2 * (reach + kLutPad) + 1; }
+
+// Bucket of the distance delta = key - query position.
+__device__ inline int bucket_of(const BucketMap &m, int delta) {
+  const int a = m.two_sided ? (delta < 0 ? -delta : delta) : (delta < 0 ? -delta : 0);
+  int b = 0;
+  for (int t = 1; t < m.per_side; ++t) b += a >= m.start[t] ? 1 : 0;
+  return b + ((m.two_sided && delta > 0) ? m.per_side : 0);
+}
+
+// Fills the LDS table of the head's biases (log 2 units) by distance.
+template <class T>
+__device__ inline void fill_lut(float *lut, const BucketMap &m, const void *table, int head,
+                                int threads) {
+  const int nb = m.two_sided ? 2 * m.per_side : m.per_side;
+  const int reach = m.start[m.per_side - 1], n = lut_size(reach);
+  for (int i = threadIdx.x; i < n; i += threads)
+    lut[i] = T::load(table, (int64_t)head * nb + bucket_of(m, i - (reach + kLutPad))) * kLog2e;
+}
+
+// Adds the bias of 32 keys (from key0) to the 16 scores of a lane whose query stands at
+// pos; the block's positions are pos_lo..pos_lo + 31. `lut` is the head's table, `slope2`
+// its slope, both in log 2 units.
+template <int BIAS>
+__device__ inline void add_bias(f32x16 &s, int key0, int pos, int pos_lo, int h, float slope2,
+                                const float *lut, int reach) {
+  if (BIAS == kBiasSlope) {
+    const float d0 = (float)(key0 + 4 * h - pos);
+    if (key0 + 31 <= pos_lo) {  // no key ahead of a query: the bias is linear
+      const float b0 = slope2 * d0;
+#pragma unroll
+      for (int e = 0; e < 16; ++e)
+        s[e] += __builtin_fmaf(slope2, (float)(8 * (e >> 2) + (e & 3)), b0);
+    } else {
+#pragma unroll
+      for (int e = 0; e < 16; ++e)
+        s[e] = __builtin_fmaf(-slope2, __builtin_fabsf(d0 + (float)(8 * (e >> 2) + (e & 3))), s[e]);
+    }
+  }
+  if (BIAS == kBiasTable) {
+    if (key0 + 31 - pos_lo <= -reach) {
+      const float b = lut[0];
+#pragma unroll
+      for (int e = 0; e < 16; ++e) s[e] += b;
+    } else if (key0 - (pos_lo + 31) >= reach) {
+      const float b = lut[lut_size(reach) - 1];
+#pragma unroll
+      for (int e = 0; e < 16; ++e) s[e] += b;
+    } else {
+      const float *p = lut + (key0 + 4 * h - pos + reach + kLutPad);
+#pragma unroll
+      for (int e = 0; e < 16; ++e) s[e] += p[8 * (e >> 2) + (e & 3)];
+    }
+  }
+}
+
+}  // namespace bgp

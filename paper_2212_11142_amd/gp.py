@@ -56,6 +56,19 @@ class _Info(C.Structure):
                 ("noise_var", C.c_double), ("cls_signal_var", C.c_double)]
 
 
+class _Heads(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("row", C.c_int64), ("head", C.c_int64)]
+
+
+class _Attention(C.Structure):
+    _fields_ = ([(k, C.c_int32) for k in ("dtype", "heads", "kv_heads", "dim", "n_docs", "q_rows",
+                                          "k_rows", "max_q", "max_k")]
+                + [(k, C.c_void_p) for k in ("q_begin", "q_end", "k_begin", "k_end", "prefix")]
+                + [("causal", C.c_int32), ("scale", C.c_float), ("cap", C.c_float),
+                   ("slopes", C.c_void_p), ("per_side", C.c_int32), ("two_sided", C.c_int32),
+                   ("bucket_start", C.POINTER(C.c_int32))])
+
+
 _lib = None
 
 # (name, restype, argtypes) for every entry point of include/baco_gp.h
@@ -108,6 +121,16 @@ _SIGS = [
     ("gp_forest_tree", C.c_int, [_VP, C.c_int32, C.c_int32, C.POINTER(C.c_int32), _VP, _VP, _VP,
                                  _VP]),
     ("gp_forest_free", None, [_VP]),
+    ("gp_attend_workspace_bytes", C.c_size_t, [C.POINTER(_Attention), C.c_int32]),
+    ("gp_attend", C.c_int, [C.POINTER(_Attention)] + [C.POINTER(_Heads)] * 3
+     + [_VP, C.POINTER(_Heads), _VP, _VP, C.c_size_t, _VP]),
+    ("gp_attend_grad", C.c_int, [C.POINTER(_Attention)] + [C.POINTER(_Heads)] * 3
+     + [_VP, C.POINTER(_Heads), _VP] + [C.POINTER(_Heads)] * 4 + [_VP, _VP, C.c_size_t, _VP]),
+    ("gp_logprob_workspace_bytes", C.c_size_t, [C.c_int32, C.c_int32, C.c_int32]),
+    ("gp_logprob", C.c_int, [C.c_int32, _VP, C.c_int64, C.c_int32, C.c_int32, C.c_float, _VP,
+                             C.c_int32, _VP, _VP, _VP, _VP, _VP, _VP, C.c_size_t, _VP]),
+    ("gp_logprob_grad", C.c_int, [C.c_int32, _VP, C.c_int64, C.c_int32, C.c_int32, C.c_float,
+                                  _VP, _VP, _VP, _VP, _VP, _VP, C.c_int64, _VP]),
     ("gp_debug_workspace_bytes", C.c_size_t, [C.POINTER(_Space), _VP, C.c_int64]),
     ("gp_debug_encode", C.c_int, [C.POINTER(_Space), C.POINTER(_VP), C.c_int64, _VP, _VP, _VP,
                                   C.c_size_t, _VP]),

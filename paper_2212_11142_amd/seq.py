@@ -1,0 +1,350 @@
+"""Operators of a sequence surrogate on CUDA tensors (gp_attend*, gp_logprob* of
+include/baco_gp.h): attention over tuning histories packed in one batch, with its gradient,
+and the log probabilities of an output row with theirs.
+
+As in ``gp``, this module only marshals arguments. A layout of documents and an `Attention`
+description are made once per batch shape, buffers once per use; the `*_into` calls are
+asynchronous on the current stream, and the plain calls allocate their outputs. A
+description's tensors and a call's buffers belong to one stream at a time.
+"""
+from __future__ import annotations
+
+import ctypes as C
+import math
+from typing import Optional, Sequence
+
+from . import gp
+from .gp import GPError, _check, _ptr, _stream, _torch
+
+MAX_REACH = 1024     # the last bucket starts at this distance at most
+_INVALID = (1 << (8 * C.sizeof(C.c_size_t))) - 1
+
+
+def _dtype_code(dtype):
+    torch = _torch()
+    code = {torch.bfloat16: 0, torch.float16: 1, torch.float32: 2}.get(dtype)
+    if code is None:
+        raise TypeError(f"unsupported dtype {dtype}")
+    return code
+
+
+# ------------------------------------------------------------------ layouts
+class Documents:
+    """The documents (tuning runs) of a packed batch.
+
+    q_len, k_len: rows of each document (k_len None: as q_len). The query rows follow one
+    another; the key rows too, unless k_begin gives each document's first key row (a cache
+    with a slot per run; slots may be longer than k_len, and with gradients must not
+    overlap). prefix: keys of each document that every row of it sees under a causal mask.
+    q_rows, k_rows: rows of the tensors, if more than the documents take."""
+
+    def __init__(self, q_len: Sequence[int], k_len: Optional[Sequence[int]] = None, prefix=None,
+                 k_begin=None, q_rows=None, k_rows=None):
+        torch = _torch()
+        q_len = [int(x) for x in q_len]
+        k_len = q_len if k_len is None else [int(x) for x in k_len]
+        n = len(q_len)
+        if len(k_len) != n or (prefix is not None and len(prefix) != n) or \
+                (k_begin is not None and len(k_begin) != n):
+            raise ValueError("one q_len, k_len, prefix and k_begin per document")
+        if any(x < 0 for x in q_len) or any(x < 0 for x in k_len):
+            raise ValueError("negative length")
+        qb, at = [], 0
+        for x in q_len:
+            qb.append(at)
+            at += x
+        self.q_rows = at if q_rows is None else int(q_rows)
+        if self.q_rows < at:
+            raise ValueError(f"the documents have {at} query rows, q_rows is {self.q_rows}")
+        self.q_full = self.q_rows == at      # every query row is some document's
+        if k_begin is None:
+            kb, at = [], 0
+            for x in k_len:
+                kb.append(at)
+                at += x
+        else:
+            kb = [int(x) for x in k_begin]
+            if any(x < 0 for x in kb):
+                raise ValueError("negative k_begin")
+            at = max([b + x for b, x in zip(kb, k_len)], default=0)
+        self.k_rows = at if k_rows is None else int(k_rows)
+        if self.k_rows < at:
+            raise ValueError(f"the documents reach key row {at}, k_rows is {self.k_rows}")
+        spans = sorted((b, b + x) for b, x in zip(kb, k_len) if x > 0)
+        self.k_disjoint = all(a[1] <= b[0] for a, b in zip(spans, spans[1:]))
+        self.k_full = self.k_disjoint and sum(k_len) == self.k_rows
+        self.n = n
+        self.max_q, self.max_k = max(q_len, default=0), max(k_len, default=0)
+        rows = [qb, [a + b for a, b in zip(qb, q_len)], kb, [a + b for a, b in zip(kb, k_len)]]
+        if prefix is not None:
+            rows.append([int(x) for x in prefix])
+        self._dev = torch.tensor(rows, dtype=torch.int32).reshape(len(rows), n).cuda()
+        self.q_begin, self.q_end, self.k_begin, self.k_end = self._dev[:4]
+        self.prefix = self._dev[4] if prefix is not None else None
+
+    @classmethod
+    def on_device(cls, q_begin, q_end, k_begin, k_end, q_rows, k_rows, max_q, max_k, prefix=None):
+        """From int32 CUDA tensors that already hold the ranges (a cache whose lengths grow
+        on the device, e.g. within a captured graph). max_q and max_k bound the lengths.
+        Nothing is read back, so gradients of rows outside the documents are zeroed by the
+        buffers, and disjoint key ranges are the caller's promise."""
+        torch = _torch()
+        self = cls.__new__(cls)
+        ts = [q_begin, q_end, k_begin, k_end] + ([prefix] if prefix is not None else [])
+        for t in ts:
+            if t.dtype != torch.int32 or not t.is_cuda or not t.is_contiguous() or \
+                    t.dim() != 1 or t.shape[0] != q_begin.shape[0]:
+                raise ValueError("ranges must be contiguous int32 CUDA vectors of one length")
+        self.q_begin, self.q_end, self.k_begin, self.k_end = ts[:4]
+        self.prefix = prefix
+        self.n = int(q_begin.shape[0])
+        self.q_rows, self.k_rows = int(q_rows), int(k_rows)
+        self.max_q, self.max_k = int(max_q), int(max_k)
+        self.q_full = self.k_full = False
+        self.k_disjoint = True
+        return self
+
+
+class Buckets:
+    """Distance classes of a learned bias: class c of a side holds the distances from
+    start[c] up to start[c + 1]; two_sided gives keys ahead of the query classes of their
+    own (else they count as distance 0)."""
+
+    def __init__(self, start: Sequence[int], two_sided: bool = False):
+        self.start = [int(x) for x in start]
+        self.two_sided = bool(two_sided)
+
+    @property
+    def count(self):
+        return len(self.start) * (2 if self.two_sided else 1)
+
+
+def log_buckets(per_side: int, max_distance: int, two_sided: bool = False) -> Buckets:
+    """per_side classes a side: the first half one distance each, then steps of equal ratio
+    up to max_distance; the last class takes all that is farther. The t-th class past the
+    exact ones starts at the smallest a with (a / exact)^n >= (max_distance / exact)^t
+    (n of them), compared in integers."""
+    exact = max(per_side // 2, 1)
+    n = per_side - exact
+    if per_side < 1 or (n > 0 and max_distance <= exact):
+        raise ValueError("need per_side >= 1 and max_distance above the exact classes")
+    start = list(range(exact + (1 if n > 0 else 0)))
+    for t in range(1, n):
+        a = start[-1] + 1
+        while a ** n < exact ** (n - t) * max_distance ** t:
+            a += 1
+        start.append(a)
+    return Buckets(start, two_sided)
+
+
+# ------------------------------------------------------------------ attention
+class Attention:
+    """What is attended to and how: documents, heads (a multiple of kv_heads), head size,
+    dtype (torch.bfloat16 or torch.float16), causal or full mask (a prefix is the
+    documents'), scale (1 / sqrt(dim) if None), cap of the scores by a tanh (0: none), and a
+    bias by distance: slopes (float32 CUDA [heads], -slope |distance|) or Buckets (the table
+    [heads, buckets.count] of dtype goes with each call)."""
+
+    def __init__(self, docs: Documents, heads: int, kv_heads: int, dim: int, dtype,
+                 causal: bool = True, scale: Optional[float] = None, cap: float = 0.0,
+                 slopes=None, buckets: Optional[Buckets] = None):
+        torch = _torch()
+        self.docs, self.heads, self.kv_heads, self.dim = docs, int(heads), int(kv_heads), int(dim)
+        self.dtype, self.buckets, self.slopes = dtype, buckets, slopes
+        if slopes is not None and (slopes.dtype != torch.float32 or not slopes.is_cuda or
+                                   not slopes.is_contiguous() or tuple(slopes.shape) != (heads,)):
+            raise ValueError("slopes must be a contiguous float32 CUDA vector of `heads`")
+        s = gp._Attention()
+        s.dtype, s.heads, s.kv_heads, s.dim = _dtype_code(dtype), heads, kv_heads, dim
+        s.n_docs, s.q_rows, s.k_rows = docs.n, docs.q_rows, docs.k_rows
+        s.max_q, s.max_k = min(docs.max_q, docs.q_rows), min(docs.max_k, docs.k_rows)
+        s.q_begin, s.q_end = docs.q_begin.data_ptr(), docs.q_end.data_ptr()
+        s.k_begin, s.k_end = docs.k_begin.data_ptr(), docs.k_end.data_ptr()
+        s.prefix = docs.prefix.data_ptr() if docs.prefix is not None else None
+        s.causal = 1 if causal else 0
+        s.scale = 1.0 / math.sqrt(dim) if scale is None else float(scale)
+        s.cap = float(cap)
+        s.slopes = slopes.data_ptr() if slopes is not None else None
+        if buckets is not None:
+            self._start = (C.c_int32 * len(buckets.start))(*buckets.start)
+            s.per_side, s.two_sided = len(buckets.start), int(buckets.two_sided)
+            s.bucket_start = self._start
+        self.struct = s
+        self.ref = C.byref(s)
+        self.workspace_bytes(False)          # raises if the description is invalid
+
+    def workspace_bytes(self, with_grad: bool) -> int:
+        lib = gp.load()
+        n = lib.gp_attend_workspace_bytes(self.ref, int(with_grad))
+        if n == _INVALID:
+            msg = lib.gp_last_error().decode()
+            raise GPError(4 if "must be a multiple of 8 in" in msg or "at most" in msg else 1, msg)
+        return n
+
+
+class AttendBuffers:
+    """Outputs and workspaces of attention calls with a description: out, lse
+    [heads, q_rows], and with grad dq, dk, dv and (with buckets) dtable. Rows outside every
+    document are 0."""
+
+    def __init__(self, att: Attention, grad: bool = False):
+        torch = _torch()
+        d = att.docs
+        f16 = dict(dtype=att.dtype, device="cuda")
+
+        def rows(full, n, heads):
+            make = torch.empty if full else torch.zeros
+            return make((n, heads, att.dim), **f16)
+
+        self.out = rows(d.q_full, d.q_rows, att.heads)
+        self.lse = torch.full((att.heads, d.q_rows), -math.inf, dtype=torch.float32, device="cuda")
+        n = att.workspace_bytes(False)
+        self.workspace = gp._workspace(n) if n else None
+        self.dq = self.dk = self.dv = self.dtable = self.grad_workspace = None
+        if grad:
+            if not d.k_disjoint:
+                raise ValueError("gradients need documents whose key rows do not overlap")
+            self.dq = rows(d.q_full, d.q_rows, att.heads)
+            self.dk = rows(d.k_full, d.k_rows, att.kv_heads)
+            self.dv = rows(d.k_full, d.k_rows, att.kv_heads)
+            if att.buckets is not None:
+                self.dtable = torch.empty((att.heads, att.buckets.count), **f16)
+            self.grad_workspace = gp._workspace(att.workspace_bytes(True))
+
+
+def _heads(x, att: Attention, rows: int, heads: int, name: str):
+    if x.dtype != att.dtype or not x.is_cuda:
+        raise ValueError(f"{name} must be a {att.dtype} CUDA tensor")
+    if tuple(x.shape) != (rows, heads, att.dim):
+        raise ValueError(f"{name} has shape {tuple(x.shape)}, need {(rows, heads, att.dim)}")
+    row, head, one = x.stride()
+    if one != 1 and att.dim > 1:
+        raise ValueError(f"{name}'s last axis must be contiguous")
+    return C.byref(gp._Heads(x.data_ptr(), row, head))
+
+
+def _table(table, att: Attention):
+    if (table is None) != (att.buckets is None):
+        raise ValueError("a table goes with a description that has buckets")
+    if table is None:
+        return None
+    if table.dtype != att.dtype or not table.is_cuda or not table.is_contiguous() or \
+            tuple(table.shape) != (att.heads, att.buckets.count):
+        raise ValueError(f"table must be a contiguous {att.dtype} CUDA tensor "
+                         f"{(att.heads, att.buckets.count)}")
+    return table.data_ptr()
+
+
+def attend_into(att: Attention, q, k, v, bufs: AttendBuffers, table=None):
+    """gp_attend into bufs.out and bufs.lse (asynchronous on the current stream). q
+    [q_rows, heads, dim], k and v [k_rows, kv_heads, dim]; strides of rows and heads are
+    free (multiples of 8)."""
+    d = att.docs
+    ws = bufs.workspace
+    _check(gp.load().gp_attend(
+        att.ref, _heads(q, att, d.q_rows, att.heads, "q"),
+        _heads(k, att, d.k_rows, att.kv_heads, "k"), _heads(v, att, d.k_rows, att.kv_heads, "v"),
+        _table(table, att), _heads(bufs.out, att, d.q_rows, att.heads, "out"),
+        bufs.lse.data_ptr(), _ptr(ws), 0 if ws is None else ws.numel(), _stream()))
+
+
+def attend(att: Attention, q, k, v, table=None) -> dict:
+    bufs = AttendBuffers(att)
+    attend_into(att, q, k, v, bufs, table)
+    return {"out": bufs.out, "lse": bufs.lse, "_buffers": bufs}
+
+
+def attend_grad_into(att: Attention, q, k, v, dout, bufs: AttendBuffers, table=None):
+    """gp_attend_grad into bufs.dq, dk, dv and dtable, from dout [q_rows, heads, dim] and
+    the out and lse that attend_into left in bufs for the same inputs."""
+    if bufs.dq is None:
+        raise ValueError("the buffers were made without grad")
+    d = att.docs
+    H, K = att.heads, att.kv_heads
+    ws = bufs.grad_workspace
+    _check(gp.load().gp_attend_grad(
+        att.ref, _heads(q, att, d.q_rows, H, "q"), _heads(k, att, d.k_rows, K, "k"),
+        _heads(v, att, d.k_rows, K, "v"), _table(table, att),
+        _heads(bufs.out, att, d.q_rows, H, "out"), bufs.lse.data_ptr(),
+        _heads(dout, att, d.q_rows, H, "dout"), _heads(bufs.dq, att, d.q_rows, H, "dq"),
+        _heads(bufs.dk, att, d.k_rows, K, "dk"), _heads(bufs.dv, att, d.k_rows, K, "dv"),
+        _ptr(bufs.dtable), _ptr(ws), ws.numel(), _stream()))
+
+
+# ------------------------------------------------------------------ log probabilities
+class LogprobBuffers:
+    """Outputs and workspace of logprob calls on [rows, width] logits: logp, entropy, lse
+    [rows], with top the best alternatives top_logp and top_id [rows, top], and with grad
+    dlogits."""
+
+    def __init__(self, rows: int, width: int, dtype, top: int = 0, grad: bool = False):
+        torch = _torch()
+        self.rows, self.width, self.top, self.dtype = int(rows), int(width), int(top), dtype
+        _dtype_code(dtype)
+        f32 = dict(dtype=torch.float32, device="cuda")
+        self.logp, self.entropy, self.lse = (torch.empty(self.rows, **f32) for _ in range(3))
+        self.top_logp = torch.empty((self.rows, self.top), **f32) if top else None
+        self.top_id = (torch.empty((self.rows, self.top), dtype=torch.int64, device="cuda")
+                       if top else None)
+        self.dlogits = (torch.empty((self.rows, self.width), dtype=dtype, device="cuda")
+                        if grad else None)
+        n = gp.load().gp_logprob_workspace_bytes(self.rows, self.width, self.top)
+        self.workspace = gp._workspace(n) if n else None
+
+
+def _logits(x, bufs, name="logits"):
+    if x.dtype != bufs.dtype or not x.is_cuda or tuple(x.shape) != (bufs.rows, bufs.width):
+        raise ValueError(f"{name} must be a {bufs.dtype} CUDA tensor {(bufs.rows, bufs.width)}")
+    if x.stride(1) != 1 and bufs.width > 1:
+        raise ValueError(f"{name}'s rows must be contiguous")
+    return x.data_ptr(), x.stride(0)
+
+
+def _row_vector(x, bufs, dtype, name):
+    if x is None:
+        return None
+    if x.dtype != dtype or not x.is_cuda or not x.is_contiguous() or tuple(x.shape) != (bufs.rows,):
+        raise ValueError(f"{name} must be a contiguous {dtype} CUDA vector of {bufs.rows}")
+    return x.data_ptr()
+
+
+def logprob_into(logits, targets, bufs: LogprobBuffers, scale: float = 1.0):
+    """gp_logprob of logits [rows, width] (the rows' stride is free): log p(targets)
+    (int64 [rows]; outside 0..width-1: no target, 0), entropy and lse of
+    softmax(scale * logits), and the bufs.top best entries, into bufs."""
+    torch = _torch()
+    x, stride = _logits(logits, bufs)
+    t = _row_vector(targets, bufs, torch.int64, "targets")
+    ws = bufs.workspace
+    if bufs.logp is not None and t is None:
+        raise ValueError("targets are required")
+    _check(gp.load().gp_logprob(
+        _dtype_code(bufs.dtype), x, stride, bufs.rows, bufs.width, float(scale), t, bufs.top,
+        bufs.logp.data_ptr(), bufs.entropy.data_ptr(), bufs.lse.data_ptr(), _ptr(bufs.top_logp),
+        _ptr(bufs.top_id), _ptr(ws), 0 if ws is None else ws.numel(), _stream()))
+
+
+def logprob(logits, targets, top: int = 0, scale: float = 1.0) -> dict:
+    bufs = LogprobBuffers(logits.shape[0], logits.shape[1], logits.dtype, top)
+    logprob_into(logits, targets, bufs, scale)
+    out = {"logp": bufs.logp, "entropy": bufs.entropy, "lse": bufs.lse}
+    if top:
+        out["top_logp"], out["top_id"] = bufs.top_logp, bufs.top_id
+    out["_buffers"] = bufs
+    return out
+
+
+def logprob_grad_into(logits, targets, g_logp, g_entropy, bufs: LogprobBuffers,
+                      scale: float = 1.0):
+    """gp_logprob_grad into bufs.dlogits, from the gradients (float32 [rows], or None) of
+    logp and entropy and what logprob_into left in bufs for the same inputs."""
+    torch = _torch()
+    if bufs.dlogits is None:
+        raise ValueError("the buffers were made without grad")
+    x, stride = _logits(logits, bufs)
+    dx, dstride = _logits(bufs.dlogits, bufs, "dlogits")
+    _check(gp.load().gp_logprob_grad(
+        _dtype_code(bufs.dtype), x, stride, bufs.rows, bufs.width, float(scale),
+        _row_vector(targets, bufs, torch.int64, "targets"), bufs.lse.data_ptr(),
+        bufs.entropy.data_ptr(), _row_vector(g_logp, bufs, torch.float32, "g_logp"),
+        _row_vector(g_entropy, bufs, torch.float32, "g_entropy"), dx, dstride, _stream()))
