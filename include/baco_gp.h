@@ -527,24 +527,27 @@ typedef struct {
 size_t gp_attend_workspace_bytes(const gp_attention *att, int32_t with_grad);
 
 /* out and lse (device float[heads][q_rows]) of every query row that a document has; other
- * rows are not written. table: device [heads][buckets] of dtype, given exactly when
+ * rows are not written. rest (NULL unless gradients follow): receives what the rounding to
+ * dtype took from out; probabilities then enter the second product at twice the precision
+ * (the gradient takes differences with out that the rounding alone would spoil). table: device [heads][buckets] of dtype, given exactly when
  * per_side > 0 (buckets = per_side, or 2 per_side with two_sided); not with slopes. The
  * workspace may be NULL if none is needed. Asynchronous on `stream`; the work is not
  * synchronised with other streams. Deterministic. */
 gp_status gp_attend(const gp_attention *att, const gp_heads *q, const gp_heads *k,
-                    const gp_heads *v, const void *table, const gp_heads *out, float *lse,
-                    void *workspace, size_t ws_bytes, void *stream);
+                    const gp_heads *v, const void *table, const gp_heads *out,
+                    const gp_heads *rest, float *lse, void *workspace, size_t ws_bytes,
+                    void *stream);
 
 /* Gradients of a loss with dout = dloss/dout: dq, dk, dv, and dtable (device
- * [heads][buckets] of dtype, overwritten) when there is a table. out and lse are those of
- * gp_attend with the same arguments. dk and dv of key rows that no document has, and dq of
+ * [heads][buckets] of dtype, overwritten) when there is a table. out, rest and lse are those
+ * of gp_attend with the same arguments. dk and dv of key rows that no document has, and dq of
  * query rows that none has, are not written; documents' key rows must not overlap here.
  * Asynchronous; deterministic (sums have a fixed order). */
 gp_status gp_attend_grad(const gp_attention *att, const gp_heads *q, const gp_heads *k,
                          const gp_heads *v, const void *table, const gp_heads *out,
-                         const float *lse, const gp_heads *dout, const gp_heads *dq,
-                         const gp_heads *dk, const gp_heads *dv, void *dtable, void *workspace,
-                         size_t ws_bytes, void *stream);
+                         const gp_heads *rest, const float *lse, const gp_heads *dout,
+                         const gp_heads *dq, const gp_heads *dk, const gp_heads *dv,
+                         void *dtable, void *workspace, size_t ws_bytes, void *stream);
 
 /* Log probabilities of rows of logits x (device, dtype GP_BF16 / GP_FP16 / GP_FP32, row
  * stride `stride` elements, `width` entries): with p = softmax(scale x),

@@ -22,7 +22,7 @@ constexpr int kThreads = 256;
 // probabilities, fp16's) range, and the rescaling of the output is skipped almost always.
 constexpr float kSlack = 8.f;
 
-template <class T, int DP, bool CAP, int BIAS>
+template <class T, int DP, bool CAP, int BIAS, bool REST>
 __global__ __launch_bounds__(kThreads, 2) void attend_kernel(const AttnArgs a) {
   constexpr int KS = DP / 16;   // k-steps of the score product
   constexpr int DT = DP / 32;   // column blocks of V
@@ -59,6 +59,8 @@ __global__ __launch_bounds__(kThreads, 2) void attend_kernel(const AttnArgs a) {
 
   const char *kbase = a.k + (int64_t)k0 * a.k_row + kvh * a.k_head;
   const char *vbase = a.v + (int64_t)k0 * a.v_row + kvh * a.v_head;
+  TileReader<DP> rd;
+  rd.init(lane);
   TileCopy<DP, kBN, 4> kc, vc;
   kc.init(wave, lane, (int)a.k_row, a.bytes);
   vc.init(wave, lane, (int)a.v_row, a.bytes);
@@ -97,12 +99,13 @@ __global__ __launch_bounds__(kThreads, 2) void attend_kernel(const AttnArgs a) {
     const int buf = tile & 1, key0 = tile * kBN;
     if (tile + 1 < n_tiles) start(tile + 1, buf ^ 1);
     if (key0 < lim_hi) {
-      const char *kb = kt + buf * kTile, *vb = vt + buf * kTile;
+      const uint32_t kb = rd.at(lds_address(kt) + buf * kTile, rd.row);
+      const uint32_t vb = rd.at(lds_address(vt) + buf * kTile, rd.col);
       f32x16 s[2] = {f32x16{}, f32x16{}};
 #pragma unroll
       for (int i = 0; i < KS; ++i) {
-        s[0] = T::mfma(row_operand<DP>(kb, 0, i, lane), qf[i], s[0]);
-        s[1] = T::mfma(row_operand<DP>(kb, 32, i, lane), qf[i], s[1]);
+        s[0] = T::mfma(row_operand<DP>(kb, 0, i), qf[i], s[0]);
+        s[1] = T::mfma(row_operand<DP>(kb, 32, i), qf[i], s[1]);
       }
       // scores; without cap and bias the scale goes into the exponent's fma below
       const bool raw = !CAP && BIAS == kBiasNone;
@@ -128,7 +131,7 @@ __global__ __launch_bounds__(kThreads, 2) void attend_kernel(const AttnArgs a) {
 #pragma unroll
         for (int e = 0; e < 16; ++e) top = fmaxf(top, s[b][e]);
       if (raw) top *= sc.c;
-      top = fmaxf(top, other_half(top));
+      top = max_halves(top);
       if (__any(top > m + kSlack)) {
         const float mn = top > m + kSlack ? top : m;
         const float f = mn == -__builtin_inff() ? 1.f : fast_exp2(m - mn);
@@ -148,8 +151,8 @@ __global__ __launch_bounds__(kThreads, 2) void attend_kernel(const AttnArgs a) {
           s[b][e] = fast_exp2(raw ? __builtin_fmaf(s[b][e], sc.c, -ms) : s[b][e] - ms);
           l += s[b][e];
         }
-        // the probabilities are rounded to the operands' type for the second product; the
-        // sum above is of the unrounded ones
+        // the probabilities are rounded to the operands' type for the second product (with
+        // REST, a second term holds what that loses); the sum above is of the unrounded ones
 #pragma unroll
         for (int i = 0; i < 2; ++i)
 #pragma unroll
@@ -165,18 +168,28 @@ __global__ __launch_bounds__(kThreads, 2) void attend_kernel(const AttnArgs a) {
         for (int i = 0; i < kBN / 16; ++i)
 #pragma unroll
           for (int c = 0; c < DT; ++c)
-            bad |= nonfinite<T>(col_operand<DP>(vb, 16 * i, c, lane));
+            bad |= nonfinite<T>(col_operand<DP>(vb, 16 * i, c));
         clean = !__any(bad != 0);
         dirty |= !clean;
       }
 #pragma unroll
-      for (int i = 0; i < kBN / 16; ++i)
+      for (int i = 0; i < kBN / 16; ++i) {
+        u32x4 rest;
+        if (REST) {
+#pragma unroll
+          for (int w = 0; w < 4; ++w) {
+            const int e = 8 * (i & 1) + 2 * w;
+            rest[w] = T::pack(s[i >> 1][e] - T::lo(p[i][w]), s[i >> 1][e + 1] - T::hi(p[i][w]));
+          }
+        }
 #pragma unroll
         for (int c = 0; c < DT; ++c) {
-          u32x4 v = col_operand<DP>(vb, 16 * i, c, lane);
+          u32x4 v = col_operand<DP>(vb, 16 * i, c);
           if (masked && !clean) v = finite_part<T>(v);
           acc[c] = T::mfma(v, p[i], acc[c]);
+          if (REST) acc[c] = T::mfma(v, rest, acc[c]);
         }
+      }
     }
     copies_barrier();
   };
@@ -186,11 +199,14 @@ __global__ __launch_bounds__(kThreads, 2) void attend_kernel(const AttnArgs a) {
   for (int tile = 0; tile < whole; ++tile) step(tile, std::false_type{});
   for (int tile = whole; tile < n_tiles; ++tile) step(tile, std::true_type{});
 
-  l += other_half(l);
+  l = sum_halves(l);
   const bool ok = row < lq;
   const float inv = l > 0.f ? 1.f / l : (l == 0.f ? 0.f : l);   // a NaN sum stays one
   store_row<T, DT>(a.o + (int64_t)(t.b0 + row) * a.o_row + head * a.o_head, ok, a.bytes, acc, inv,
                    lane);
+  if (REST)
+    store_row<T, DT, true>(a.rest + (int64_t)(t.b0 + row) * a.rest_row + head * a.rest_head, ok,
+                           a.bytes, acc, inv, lane);
   if (ok && h == 0)
     a.lse[(int64_t)head * a.q_rows + t.b0 + row] =
         l == 0.f ? -__builtin_inff() : (m + __builtin_amdgcn_logf(l)) * kLn2;
@@ -206,12 +222,12 @@ __global__ __launch_bounds__(kThreads, 2) void attend_kernel(const AttnArgs a) {
   }
 }
 
-template <class T, int DP, bool CAP, int BIAS>
-hipError_t launch(const AttnArgs &a, hipStream_t s) {
+template <class T, int DP, bool CAP, int BIAS, bool REST>
+hipError_t launch_form(const AttnArgs &a, hipStream_t s) {
   static LdsLimit limit;
   int lds = 4 * kBN * DP * 2;
   if (BIAS == kBiasTable) lds += lut_size(a.buckets.start[a.buckets.per_side - 1]) * 4;
-  hipError_t e = limit.set(reinterpret_cast<const void *>(&attend_kernel<T, DP, CAP, BIAS>),
+  hipError_t e = limit.set(reinterpret_cast<const void *>(&attend_kernel<T, DP, CAP, BIAS, REST>),
                            4 * kBN * DP * 2 + lut_size(kMaxReach) * 4);
   if (e != hipSuccess) return e;
   // an upper bound of the documents' tiles; the blocks past the last one end at once
@@ -219,8 +235,14 @@ hipError_t launch(const AttnArgs &a, hipStream_t s) {
   const int64_t by_max = (int64_t)a.docs * ((a.max_q + kBM - 1) / kBM);
   const int64_t blocks = (tiles < by_max ? tiles : by_max) * a.heads;
   if (blocks == 0) return hipSuccess;
-  attend_kernel<T, DP, CAP, BIAS><<<dim3((uint32_t)blocks), kThreads, lds, s>>>(a);
+  attend_kernel<T, DP, CAP, BIAS, REST><<<dim3((uint32_t)blocks), kThreads, lds, s>>>(a);
   return hipGetLastError();
+}
+
+template <class T, int DP, bool CAP, int BIAS>
+hipError_t launch(const AttnArgs &a, hipStream_t s) {
+  if (a.rest) return launch_form<T, DP, CAP, BIAS, true>(a, s);
+  return launch_form<T, DP, CAP, BIAS, false>(a, s);
 }
 
 template <class T, int DP>

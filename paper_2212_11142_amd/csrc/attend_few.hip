@@ -86,6 +86,8 @@ __global__ __launch_bounds__(kThreads, 1) void few_kernel(const AttnArgs a, cons
 
   const char *kbase = a.k + (int64_t)k0 * a.k_row + kvh * a.k_head;
   const char *vbase = a.v + (int64_t)k0 * a.v_row + kvh * a.v_head;
+  TileReader<DP> rd;
+  rd.init(lane);
   TileCopy<DP, kKeys, 1> kc, vc;
   kc.init(0, lane, (int)a.k_row, a.bytes);
   vc.init(0, lane, (int)a.v_row, a.bytes);
@@ -134,10 +136,11 @@ __global__ __launch_bounds__(kThreads, 1) void few_kernel(const AttnArgs a, cons
     } else {
       wait_copies<0>();
     }
-    const char *kb = mine + buf * 2 * kTile, *vb = kb + kTile;
+    const uint32_t kb = rd.at(lds_address(mine) + buf * 2 * kTile, rd.row);
+    const uint32_t vb = rd.at(lds_address(mine) + (buf * 2 + 1) * kTile, rd.col);
     f32x16 s = {};
 #pragma unroll
-    for (int k = 0; k < KS; ++k) s = T::mfma(row_operand<DP>(kb, 0, k, lane), qf[k], s);
+    for (int k = 0; k < KS; ++k) s = T::mfma(row_operand<DP>(kb, 0, k), qf[k], s);
 #pragma unroll
     for (int e = 0; e < 16; ++e) s[e] = scaled<CAP>(s[e], sc);
     if (BIAS == kBiasSlope) {
@@ -168,7 +171,7 @@ __global__ __launch_bounds__(kThreads, 1) void few_kernel(const AttnArgs a, cons
     float top = s[0];
 #pragma unroll
     for (int e = 1; e < 16; ++e) top = fmaxf(top, s[e]);
-    top = fmaxf(top, other_half(top));
+    top = max_halves(top);
     if (__any(top > m + kSlack)) {
       const float mn = top > m + kSlack ? top : m;
       const float f = mn == -__builtin_inff() ? 1.f : fast_exp2(m - mn);
@@ -196,7 +199,7 @@ __global__ __launch_bounds__(kThreads, 1) void few_kernel(const AttnArgs a, cons
 #pragma unroll
       for (int k = 0; k < 2; ++k)
 #pragma unroll
-        for (int c = 0; c < DT; ++c) bad |= nonfinite<T>(col_operand<DP>(vb, 16 * k, c, lane));
+        for (int c = 0; c < DT; ++c) bad |= nonfinite<T>(col_operand<DP>(vb, 16 * k, c));
       clean = !__any(bad != 0);
       dirty |= !clean;
     }
@@ -204,12 +207,12 @@ __global__ __launch_bounds__(kThreads, 1) void few_kernel(const AttnArgs a, cons
     for (int k = 0; k < 2; ++k)
 #pragma unroll
       for (int c = 0; c < DT; ++c) {
-        u32x4 v = col_operand<DP>(vb, 16 * k, c, lane);
+        u32x4 v = col_operand<DP>(vb, 16 * k, c);
         if (!clean) v = finite_part<T>(v);
         acc[c] = T::mfma(v, pr[k], acc[c]);
       }
   }
-  l += other_half(l);
+  l = sum_halves(l);
 
   // join the four wavefronts
   copies_barrier();

@@ -2,11 +2,11 @@
 // D_i = dO_i . O_i:
 //   dS = P (dP - D),  dbias = dS,  dZ = dS (1 - (z' / cap)^2)  (z' the capped product)
 //   dQ = scale dZ K,  dK = scale dZ^T Q,  dV = P^T dO
-// P is recomputed from the scores and the forward pass's log-sums. Two kernels, so that
-// every sum has one owner and one order (no atomics): one goes over the queries for 128 keys
-// of a key head (all query heads of its group, in turn) and keeps dK and dV, the other goes
-// over the keys for 128 queries of a head and keeps dQ and the head's table gradient. That
-// costs 7 products of the pairs where one kernel with atomic sums of dQ would take 5.
+// P is recomputed from the scores and the forward pass's log-sums. Two kinds of blocks, so
+// that every sum has one owner and one order (no atomics): one goes over the queries for 128
+// keys of a key head (all query heads of its group, in turn) and keeps dK and dV, the other
+// goes over the keys for 128 queries of a head and keeps dQ and the head's table gradient.
+// That costs 7 products of the pairs where one kind with atomic sums of dQ would take 5.
 //
 // fp16: P is kept times 2^12 and dS times a power of two from a bound of |dS|,
 // 2 max|dO_i| max|v_j|, so that neither leaves fp16's normal range; exact to undo.
@@ -20,10 +20,34 @@ namespace {
 constexpr int kThreads = 256;
 constexpr int kRowBlocks = 512;    // blocks of the row pass, at most
 constexpr float kP16 = 12.f;       // fp16: log2 of the factor of P
+constexpr int kSkew = 32 * 64 + 64;  // floats of a wavefront's skewed values
+
+// Rows of a step (the tiles that go through LDS while a block's own stay).
+template <int DP>
+struct GradTiles {
+  static constexpr int kStep = DP == 128 ? 32 : 64;
+};
+
+// Starts the copy of one word per lane into LDS.
+__device__ inline void copy_words(u32x4 buf, int voff, uint32_t lds) {
+  const uint32_t m = uniform((int)lds);
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dword %1, %2, 0 offen lds"
+               ::"s"(m), "v"(voff), "s"(buf)
+               : "memory");
+}
+
+// Sum over the wavefront's four rows of 16 lanes, on all of them.
+__device__ inline float sum_rows(float x) {
+  const uint32_t u = __builtin_bit_cast(uint32_t, x);
+  const u32x2 a = __builtin_amdgcn_permlane16_swap(u, u, false, false);
+  return sum_halves(word_float(a[0]) + word_float(a[1]));
+}
 
 // ------------------------------------------------------------------ rows
-// delta[head][row] = dO . O; for fp16 also block maxima of |dO_i|^2 (bound[0..]) and of
-// |v_j|^2 (bound[kRowBlocks..]). 16 lanes per row.
+// rows[head][row] = {log-sum in units of log 2, D = dO . (O + what its rounding took)}; for
+// fp16 also block maxima of |dO_i|^2 (bound[0..]) and of |v_j|^2 (bound[kRowBlocks..]). 16
+// lanes per row. D is a difference's other half in dS, so it takes O at full precision: the
+// rounding of O alone would double the error of dQ and dK.
 template <class T>
 __device__ inline float dot8(u32x4 a, u32x4 b) {
   float x = 0.f;
@@ -50,7 +74,8 @@ __global__ __launch_bounds__(kThreads) void grad_rows(const AttnGradArgs a) {
     if (in) {
       const u32x4 g = *reinterpret_cast<const u32x4 *>(a.dout + row * a.do_row + head * a.do_head + l16 * 16);
       const u32x4 o = *reinterpret_cast<const u32x4 *>(a.f.o + row * a.f.o_row + head * a.f.o_head + l16 * 16);
-      d = dot8<T>(g, o);
+      const u32x4 e = *reinterpret_cast<const u32x4 *>(a.f.rest + row * a.f.rest_row + head * a.f.rest_head + l16 * 16);
+      d = dot8<T>(g, o) + dot8<T>(g, e);
       if (a.f.fp16) nrm = dot8<T>(g, g);
     }
 #pragma unroll
@@ -58,7 +83,13 @@ __global__ __launch_bounds__(kThreads) void grad_rows(const AttnGradArgs a) {
       d += __shfl_xor(d, o);
       if (a.f.fp16) nrm += __shfl_xor(nrm, o);
     }
-    if (l16 == 0) a.delta[(int64_t)head * a.f.q_rows + row] = d;
+    if (l16 == 0) {
+      const int64_t at = (int64_t)head * a.f.q_rows + row;
+      const float lse = a.f.lse[at];
+      // (a row that saw nothing: +inf, so that its P is 0)
+      a.rows[2 * at] = lse == -__builtin_inff() ? __builtin_inff() : lse * kLog2e;
+      a.rows[2 * at + 1] = d;
+    }
     top = fmaxf(top, nrm);
   }
   if (!a.f.fp16) return;
@@ -117,36 +148,45 @@ __device__ inline int ds_exponent(const float *bound, int blocks, float *red) {
   return uniform(min(max(15 - e, -60), 60));
 }
 
-// log-sums in units of log 2, +inf for a row that saw nothing (its P is then 0)
-__device__ inline float row_lse(float lse) {
-  return lse == -__builtin_inff() ? __builtin_inff() : lse * kLog2e;
-}
-
-// P and dZ of 16 pairs of a lane: s raw products in, P (times 2^p0) out; dp in, dZ times
-// 2^ds0 out; `bias`: dS without the cap's derivative (what the table's gradient sums).
-// lse and delta per element; `seen`: whether the pair is visible.
-template <bool CAP>
-struct PairGrad {
+// Products of a block: the same for both halves of the kernel below.
+template <class T, bool CAP>
+struct PairScale {
+  static constexpr bool kHalf = std::is_same<T, Fp16>::value;
   ScoreScale sc;
-  float inv_cap2;    // 1 / (cap log2(e))
+  float inv_cap2, ds_scale;
+  int ds0;
+
+  __device__ void init(const AttnGradArgs &g, int row_blocks, float *red) {
+    sc.cap2 = g.f.cap * kLog2e;
+    sc.c = CAP ? 2.f * kLog2e * g.f.scale / g.f.cap : g.f.scale * kLog2e;
+    inv_cap2 = CAP ? 1.f / sc.cap2 : 0.f;
+    ds0 = kHalf ? ds_exponent(g.bound, row_blocks, red) : 0;
+    ds_scale = kHalf ? ldexpf(1.f, ds0) : 1.f;
+  }
+  // derivative of the capped product z (log 2 units)
+  __device__ float slope(float z) const {
+    const float y = z * inv_cap2;
+    return __builtin_fmaf(-y, y, 1.f);
+  }
 };
 
 // ------------------------------------------------------------------ dK, dV
 // A lane's key is fixed, its elements are the queries 8 g + 4 h + r of 32: products are
 // Q K^T (queries x keys), their results the operands of dV^T = dO^T P and dK^T = Q^T dZ.
+// K stays in registers and V in LDS: with V in registers too the accumulators would spill.
 template <class T, int DP, bool CAP, int BIAS>
-__global__ __launch_bounds__(kThreads, 2) void grad_kv(const AttnGradArgs ga, int row_blocks) {
+__device__ __forceinline__ void grad_kv(const AttnGradArgs &ga, int row_blocks, int id, char *lds,
+                                        float *red) {
   constexpr int KS = DP / 16, DT = DP / 32;
-  constexpr int kBQ = 32;                      // queries of a step
+  constexpr int kBQ = GradTiles<DP>::kStep;    // queries of a step
   constexpr int kTile = kBQ * DP * 2;
   constexpr int kBK = 128;                     // keys of a block
   const AttnArgs &a = ga.f;
-  extern __shared__ __align__(1024) char lds[];                // [2][Q, dO], [2][lse, delta], table
-  float *rows_lds = reinterpret_cast<float *>(lds + 4 * kTile);
-  float *lut = rows_lds + 2 * 128;
-  __shared__ float red[8];
+  // [2][Q, dO], V, [2][rows of log-sum and D], table
+  char *vt = lds + 4 * kTile;
+  char *rows_lds = vt + kBK * DP * 2;
+  float *lut = reinterpret_cast<float *>(rows_lds + 2 * kBQ * 8);
 
-  int id = blockIdx.x;
   const int kvh = id % a.kv_heads;
   const DocTile t = find_tile<kBK>(a.kb, a.ke, a.docs, a.k_rows, id / a.kv_heads);
   if (t.doc < 0) return;
@@ -168,6 +208,8 @@ __global__ __launch_bounds__(kThreads, 2) void grad_kv(const AttnGradArgs ga, in
   const int steps = max((lq - i_start + kBQ - 1) / kBQ, 0);
   const int total = steps * a.group;
 
+  TileReader<DP> rd;
+  rd.init(lane);
   TileCopy<DP, kBQ, 4> qc, dc;
   qc.init(wave, lane, (int)a.q_row, a.bytes);
   dc.init(wave, lane, (int)ga.do_row, a.bytes);
@@ -179,37 +221,37 @@ __global__ __launch_bounds__(kThreads, 2) void grad_kv(const AttnGradArgs ga, in
     dc.start(row_buffer(ga.dout + (int64_t)q0 * ga.do_row + head * ga.do_head, i, rows, ga.do_row,
                         a.bytes),
              lds_address(lds) + (buf * 2 + 1) * kTile);
-    if (threadIdx.x < 2 * kBQ) {               // (wavefront 0)
-      const int r = i + (lane & 31);
-      const int64_t at = (int64_t)head * a.q_rows + q0 + r;
-      const float x = r < lq ? (h ? ga.delta[at] : row_lse(a.lse[at])) : 0.f;
-      rows_lds[buf * 128 + lane] = x;
-    }
+    if (wave < kBQ / 32)
+      copy_words(row_buffer(reinterpret_cast<const char *>(ga.rows) +
+                                ((int64_t)head * a.q_rows + q0) * 8, i, rows, 8, 8),
+                 (wave * 64 + lane) * 4, lds_address(rows_lds) + buf * kBQ * 8 + wave * 256);
   };
+  {
+    TileCopy<DP, kBK, 4> vc;
+    vc.init(wave, lane, (int)a.v_row, a.bytes);
+    vc.start(row_buffer(a.v + (int64_t)t.b0 * a.v_row + kvh * a.v_head, j0, min(lk - j0, kBK),
+                        a.v_row, a.bytes),
+             lds_address(vt));
+  }
+  if (total > 0) start(0, 0);
 
-  // operands that stay: this wavefront's 32 keys of K and V
-  u32x4 kf[KS], vf[KS];
+  u32x4 kf[KS];
   load_operand<DP>(a.k + (int64_t)t.b0 * a.k_row + kvh * a.k_head, a.k_row, key, lk, a.bytes, lane, kf);
-  load_operand<DP>(a.v + (int64_t)t.b0 * a.v_row + kvh * a.v_head, a.v_row, key, lk, a.bytes, lane, vf);
-  const bool half = std::is_same<T, Fp16>::value;
-  const int ds0 = half ? ds_exponent(ga.bound, row_blocks, red) : 0;
-  const float ds_scale = ldexpf(1.f, half ? ds0 - (int)kP16 : 0);
+  PairScale<T, CAP> ps;
+  ps.init(ga, row_blocks, red);
+  const float p0 = ps.kHalf ? kP16 : 0.f, ds_scale = ps.ds_scale * exp2f(-p0);
   const int reach = BIAS == kBiasTable ? a.buckets.start[a.buckets.per_side - 1] : 0;
-  ScoreScale sc;
-  sc.cap2 = a.cap * kLog2e;
-  sc.c = CAP ? 2.f * kLog2e * a.scale / a.cap : a.scale * kLog2e;
-  const float inv_cap2 = CAP ? 1.f / sc.cap2 : 0.f;
 
   f32x16 dk[DT], dv[DT];
 #pragma unroll
   for (int c = 0; c < DT; ++c) dk[c] = dv[c] = f32x16{};
   float slope2 = 0.f;
 
-  if (total > 0) start(0, 0);
   copies_barrier();
   for (int n = 0; n < total; ++n) {
-    const int buf = n & 1, head = kvh * a.group + n / steps, i0 = i_start + n % steps * kBQ;
+    const int buf = n & 1;
     if (BIAS != kBiasNone && n % steps == 0) {   // the next head
+      const int head = kvh * a.group + n / steps;
       if (BIAS == kBiasSlope) slope2 = a.slopes[head] * kLog2e;
       if (BIAS == kBiasTable) {
         fill_lut<T>(lut, a.buckets, a.table, head, kThreads);
@@ -217,19 +259,33 @@ __global__ __launch_bounds__(kThreads, 2) void grad_kv(const AttnGradArgs ga, in
       }
     }
     if (n + 1 < total) start(n + 1, buf ^ 1);
-    if (i0 + kBQ > i_wave) {
-      const char *qt = lds + buf * 2 * kTile, *dt = qt + kTile;
-      const float *lse = rows_lds + buf * 128 + 4 * h, *delta = lse + 32;
+#pragma unroll 1
+    for (int sub = 0; sub < kBQ; sub += 32) {
+      const int i0 = i_start + n % steps * kBQ + sub;
+      if (i0 + 32 <= i_wave || i0 >= lq) continue;
+      const uint32_t tile = lds_address(lds) + buf * 2 * kTile;
+      const uint32_t qr = rd.at(tile, rd.row), qc0 = rd.at(tile, rd.col);
+      const uint32_t vr = rd.at(lds_address(vt), rd.row);
+      const char *rows = rows_lds + (buf * kBQ + sub + 4 * h) * 8;
       f32x16 s = {}, dp = {};
 #pragma unroll
-      for (int k = 0; k < KS; ++k) s = T::mfma(row_operand<DP>(qt, 0, k, lane), kf[k], s);
+      for (int k = 0; k < KS; ++k) s = T::mfma(row_operand<DP>(qr, sub, k), kf[k], s);
 #pragma unroll
-      for (int k = 0; k < KS; ++k) dp = T::mfma(row_operand<DP>(dt, 0, k, lane), vf[k], dp);
-      const bool masked = i0 < i_whole || i0 + kBQ > lq;
-      f32x16 z;   // capped products in units of log 2
+      for (int k = 0; k < KS; ++k)
+        dp = T::mfma(row_operand<DP>(qr + kTile, sub, k), row_operand<DP>(vr + 32 * wave * DP * 2, 0, k), dp);
+      const bool masked = i0 < i_whole || i0 + 32 > lq;
 #pragma unroll
-      for (int e = 0; e < 16; ++e) z[e] = scaled<CAP>(s[e], sc);
-      s = z;
+      for (int g = 0; g < 4; ++g) {   // (dP - D) dZ/dS first: the capped products then are done
+        const f32x4 x0 = *reinterpret_cast<const f32x4 *>(rows + 64 * g);
+        const f32x4 x1 = *reinterpret_cast<const f32x4 *>(rows + 64 * g + 16);
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          const int e = 4 * g + r;
+          s[e] = scaled<CAP>(s[e], ps.sc);
+          dp[e] -= r < 2 ? x0[2 * r + 1] : x1[2 * r - 3];
+          if (CAP) dp[e] *= ps.slope(s[e]);
+        }
+      }
       // the distance falls with the query: add_bias's elements in the other direction
       if (BIAS == kBiasSlope) {
         const float d0 = (float)(key - shift - i0 - 4 * h);
@@ -249,27 +305,27 @@ __global__ __launch_bounds__(kThreads, 2) void grad_kv(const AttnGradArgs ga, in
           for (int e = 0; e < 16; ++e) s[e] += p[-(8 * (e >> 2) + (e & 3))];
         }
       }
-      u32x4 pr[2], dr[2];
+      if (masked) {   // exp2(-inf) below
+        const int lo = mine - i0 - 4 * h, hi = lq - i0 - 4 * h;
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+          const int r = 8 * (e >> 2) + (e & 3);
+          if (r < lo || r >= hi) s[e] = -__builtin_inff();
+        }
+      }
+      asm volatile("" ::: "memory");   // reads the rows again rather than keep 32 registers
 #pragma unroll
       for (int g = 0; g < 4; ++g) {
-        const f32x4 ls = *reinterpret_cast<const f32x4 *>(lse + 8 * g);
-        const f32x4 dl = *reinterpret_cast<const f32x4 *>(delta + 8 * g);
+        const f32x4 x0 = *reinterpret_cast<const f32x4 *>(rows + 64 * g);
+        const f32x4 x1 = *reinterpret_cast<const f32x4 *>(rows + 64 * g + 16);
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
           const int e = 4 * g + r;
-          const bool seen = !masked || (i0 + 4 * h + 8 * g + r >= mine && i0 + 4 * h + 8 * g + r < lq);
-          float p = fast_exp2(half ? s[e] - ls[r] + kP16 : s[e] - ls[r]);
-          p = seen ? p : 0.f;
-          float d = p * (dp[e] - dl[r]);
-          if (half) d *= ds_scale;
-          if (CAP) {
-            const float y = z[e] * inv_cap2;
-            d *= __builtin_fmaf(-y, y, 1.f);
-          }
-          s[e] = p;
-          dp[e] = seen ? d : 0.f;
+          s[e] = fast_exp2(s[e] - ((r < 2 ? x0[2 * r] : x1[2 * r - 4]) - p0));
+          dp[e] *= ps.kHalf ? s[e] * ds_scale : s[e];
         }
       }
+      u32x4 pr[2], dr[2];
 #pragma unroll
       for (int k = 0; k < 2; ++k)
 #pragma unroll
@@ -281,34 +337,37 @@ __global__ __launch_bounds__(kThreads, 2) void grad_kv(const AttnGradArgs ga, in
       for (int k = 0; k < 2; ++k)
 #pragma unroll
         for (int c = 0; c < DT; ++c) {
-          dv[c] = T::mfma(col_operand<DP>(dt, 16 * k, c, lane), pr[k], dv[c]);
-          dk[c] = T::mfma(col_operand<DP>(qt, 16 * k, c, lane), dr[k], dk[c]);
+          dv[c] = T::mfma(col_operand<DP>(qc0 + kTile, sub + 16 * k, c), pr[k], dv[c]);
+          dk[c] = T::mfma(col_operand<DP>(qc0, sub + 16 * k, c), dr[k], dk[c]);
         }
     }
     copies_barrier();
   }
   const bool ok = key < lk;
   store_row<T, DT>(ga.dv + (int64_t)(t.b0 + key) * ga.dv_row + kvh * ga.dv_head, ok, a.bytes, dv,
-                   half ? ldexpf(1.f, -(int)kP16) : 1.f, lane);
+                   exp2f(-p0), lane);
   store_row<T, DT>(ga.dk + (int64_t)(t.b0 + key) * ga.dk_row + kvh * ga.dk_head, ok, a.bytes, dk,
-                   a.scale * ldexpf(1.f, -ds0), lane);
+                   a.scale * ldexpf(1.f, -ps.ds0), lane);
 }
 
 // ------------------------------------------------------------------ dQ, table
 // A lane's query is fixed, its elements are the keys, as in the forward kernel.
+//
+// Table gradient: the sums of dS by distance. Beyond the table's reach that is one sum per
+// lane; within, a wavefront writes its 32 x 32 values of dS into LDS skewed, so that a
+// distance is a column, adds up the 63 columns and adds those to its sums by distance.
 template <class T, int DP, bool CAP, int BIAS>
-__global__ __launch_bounds__(kThreads, 2) void grad_q(const AttnGradArgs ga, int row_blocks) {
+__device__ __forceinline__ void grad_q(const AttnGradArgs &ga, int row_blocks, int id, char *lds,
+                                       float *red) {
   constexpr int KS = DP / 16, DT = DP / 32;
-  constexpr int kBN = 32;                      // keys of a step
+  constexpr int kBN = GradTiles<DP>::kStep;    // keys of a step
   constexpr int kTile = kBN * DP * 2;
   constexpr int kBM = 128;
   const AttnArgs &a = ga.f;
-  extern __shared__ __align__(1024) char lds[];                // [2][K, V], biases, [4] sums by distance
-  float *lut = reinterpret_cast<float *>(lds + 4 * kTile);
-  __shared__ float red[8];
-  __shared__ float far_sum[4][2];
+  // [2][K, V], [4] skewed values, biases, [4] sums by distance
+  float *skewed = reinterpret_cast<float *>(lds + 4 * kTile);
+  float *lut = skewed + 4 * kSkew;
 
-  int id = blockIdx.x;
   const int kvh = id % a.kv_heads;
   id /= a.kv_heads;
   const int head = kvh * a.group + id % a.group, unit = id / a.group;
@@ -340,6 +399,8 @@ __global__ __launch_bounds__(kThreads, 2) void grad_q(const AttnGradArgs ga, int
 
   const char *kbase = a.k + (int64_t)k0 * a.k_row + kvh * a.k_head;
   const char *vbase = a.v + (int64_t)k0 * a.v_row + kvh * a.v_head;
+  TileReader<DP> rd;
+  rd.init(lane);
   TileCopy<DP, kBN, 4> kc, vc;
   kc.init(wave, lane, (int)a.k_row, a.bytes);
   vc.init(wave, lane, (int)a.v_row, a.bytes);
@@ -357,13 +418,12 @@ __global__ __launch_bounds__(kThreads, 2) void grad_q(const AttnGradArgs ga, int
   load_operand<DP>(ga.dout + (int64_t)t.b0 * ga.do_row + head * ga.do_head, ga.do_row, row, lq,
                    a.bytes, lane, df);
   const int64_t at = (int64_t)head * a.q_rows + t.b0 + row;
-  const float lse = ok ? row_lse(a.lse[at]) : 0.f, delta = ok ? ga.delta[at] : 0.f;
-  const bool half = std::is_same<T, Fp16>::value;
-  const int ds0 = half ? ds_exponent(ga.bound, row_blocks, red) : 0;
-  const float ds_scale = half ? ldexpf(1.f, ds0) : 1.f;
+  const float lse = ok ? ga.rows[2 * at] : 0.f, delta = ok ? ga.rows[2 * at + 1] : 0.f;
+  PairScale<T, CAP> ps;
+  ps.init(ga, row_blocks, red);
   int reach = 0;
   float slope2 = 0.f;
-  float *hist = nullptr;                       // this wavefront's sums of dS by distance
+  float *hist = nullptr, *skew = skewed + wave * kSkew;
   float far_l = 0.f, far_r = 0.f;              // behind and ahead of the table's reach
   if (BIAS == kBiasTable) {
     reach = a.buckets.start[a.buckets.per_side - 1];
@@ -371,12 +431,9 @@ __global__ __launch_bounds__(kThreads, 2) void grad_q(const AttnGradArgs ga, int
     fill_lut<T>(lut, a.buckets, a.table, head, kThreads);
     hist = lut + n * (1 + wave);
     for (int i = lane; i < n; i += 64) hist[i] = 0.f;
+    for (int i = lane; i < kSkew; i += 64) skew[i] = 0.f;
   }
   if (BIAS == kBiasSlope) slope2 = a.slopes[head] * kLog2e;
-  ScoreScale sc;
-  sc.cap2 = a.cap * kLog2e;
-  sc.c = CAP ? 2.f * kLog2e * a.scale / a.cap : a.scale * kLog2e;
-  const float inv_cap2 = CAP ? 1.f / sc.cap2 : 0.f;
 
   f32x16 acc[DT];
 #pragma unroll
@@ -384,31 +441,35 @@ __global__ __launch_bounds__(kThreads, 2) void grad_q(const AttnGradArgs ga, int
 
   copies_barrier();
   for (int tile = 0; tile < n_tiles; ++tile) {
-    const int buf = tile & 1, key0 = tile * kBN;
+    const int buf = tile & 1;
     if (tile + 1 < n_tiles) start(tile + 1, buf ^ 1);
-    if (key0 < lim_hi) {
-      const char *kb = lds + buf * 2 * kTile, *vb = kb + kTile;
+#pragma unroll 1
+    for (int sub = 0; sub < kBN; sub += 32) {
+      const int key0 = tile * kBN + sub;
+      if (key0 >= lim_hi) break;
+      const uint32_t tile_at = lds_address(lds) + buf * 2 * kTile;
+      const uint32_t kr = rd.at(tile_at, rd.row), kcol = rd.at(tile_at, rd.col);
       f32x16 s = {}, dp = {};
 #pragma unroll
-      for (int k = 0; k < KS; ++k) s = T::mfma(row_operand<DP>(kb, 0, k, lane), qf[k], s);
+      for (int k = 0; k < KS; ++k) s = T::mfma(row_operand<DP>(kr, sub, k), qf[k], s);
 #pragma unroll
-      for (int k = 0; k < KS; ++k) dp = T::mfma(row_operand<DP>(vb, 0, k, lane), df[k], dp);
+      for (int k = 0; k < KS; ++k) dp = T::mfma(row_operand<DP>(kr + kTile, sub, k), df[k], dp);
       f32x16 z;
 #pragma unroll
-      for (int e = 0; e < 16; ++e) z[e] = scaled<CAP>(s[e], sc);
+      for (int e = 0; e < 16; ++e) z[e] = scaled<CAP>(s[e], ps.sc);
       s = z;
       add_bias<BIAS>(s, key0, row + shift, row_lo + shift, h, slope2, lut, reach);
-      const bool masked = key0 + kBN > lim_lo;
-      const int mine = lim - key0 - 4 * h;
+      if (key0 + 32 > lim_lo) {
+        const int mine = lim - key0 - 4 * h;
+#pragma unroll
+        for (int e = 0; e < 16; ++e)
+          if (8 * (e >> 2) + (e & 3) >= mine) s[e] = -__builtin_inff();
+      }
       float sum = 0.f;
 #pragma unroll
       for (int e = 0; e < 16; ++e) {
-        const bool seen = !masked || 8 * (e >> 2) + (e & 3) < mine;
-        const float p = fast_exp2(s[e] - lse);
-        float d = p * (dp[e] - delta);
-        d = seen ? d : 0.f;
-        dp[e] = d;
-        sum += d;
+        dp[e] = fast_exp2(s[e] - lse) * (dp[e] - delta);
+        if (BIAS == kBiasTable) sum += dp[e];
       }
       if (BIAS == kBiasTable) {
         const int d_hi = key0 + 31 - (row_lo + shift), d_lo = key0 - (row_lo + 31 + shift);
@@ -417,29 +478,27 @@ __global__ __launch_bounds__(kThreads, 2) void grad_q(const AttnGradArgs ga, int
         } else if (d_lo >= reach) {
           far_r += sum;
         } else {
-          // the halves of the wavefront in turn: within each, every lane has a distance of
-          // its own, so that the order of the sums does not depend on the hardware's
-          float *p = hist + (key0 + 4 * h - (row + shift) + reach + kLutPad);
+          // value (key k, query q) at [k][k - q + 31]; what lies outside stays 0
+          float *w = skew + 4 * h * 65 + 31 - (lane & 31);
 #pragma unroll
-          for (int g = 0; g < 2; ++g) {
-            if (h == g) {
+          for (int e = 0; e < 16; ++e) w[(8 * (e >> 2) + (e & 3)) * 65] = dp[e];
+          const float *r = skew + (lane >> 4) * 8 * 64 + (lane & 15) * 4;
+          f32x4 v = {};
 #pragma unroll
-              for (int e = 0; e < 16; ++e)
-                __hip_atomic_fetch_add(p + 8 * (e >> 2) + (e & 3), dp[e], __ATOMIC_RELAXED,
-                                       __HIP_MEMORY_SCOPE_WORKGROUP);
-            }
-          }
+          for (int k = 0; k < 8; ++k) v += *reinterpret_cast<const f32x4 *>(r + k * 64);
+#pragma unroll
+          for (int k = 0; k < 4; ++k) v[k] = sum_rows(v[k]);
+          const int g = lane >> 4, d = (lane & 15) * 4 + g;   // this lane's column
+          const float x = g == 0 ? v[0] : (g == 1 ? v[1] : (g == 2 ? v[2] : v[3]));
+          if (d < 63) hist[d_lo + d + reach + kLutPad] += x;
         }
       }
-      u32x4 dr[2];
 #pragma unroll
       for (int e = 0; e < 16; ++e) {
-        if (CAP) {
-          const float y = z[e] * inv_cap2;
-          dp[e] *= __builtin_fmaf(-y, y, 1.f);
-        }
-        if (half) dp[e] *= ds_scale;
+        if (CAP) dp[e] *= ps.slope(z[e]);
+        if (ps.kHalf) dp[e] *= ps.ds_scale;
       }
+      u32x4 dr[2];
 #pragma unroll
       for (int k = 0; k < 2; ++k)
 #pragma unroll
@@ -449,12 +508,12 @@ __global__ __launch_bounds__(kThreads, 2) void grad_q(const AttnGradArgs ga, int
       for (int k = 0; k < 2; ++k)
 #pragma unroll
         for (int c = 0; c < DT; ++c)
-          acc[c] = T::mfma(col_operand<DP>(kb, 16 * k, c, lane), dr[k], acc[c]);
+          acc[c] = T::mfma(col_operand<DP>(kcol, sub + 16 * k, c), dr[k], acc[c]);
     }
     copies_barrier();
   }
   store_row<T, DT>(ga.dq + (int64_t)(t.b0 + row) * ga.dq_row + head * ga.dq_head, ok, a.bytes, acc,
-                   a.scale * ldexpf(1.f, -ds0), lane);
+                   a.scale * ldexpf(1.f, -ps.ds0), lane);
 
   if (BIAS == kBiasTable) {
 #pragma unroll
@@ -463,29 +522,46 @@ __global__ __launch_bounds__(kThreads, 2) void grad_q(const AttnGradArgs ga, int
       far_r += __shfl_xor(far_r, o);
     }
     if (lane == 0) {
-      far_sum[wave][0] = far_l;
-      far_sum[wave][1] = far_r;
+      red[2 * wave] = far_l;
+      red[2 * wave + 1] = far_r;
     }
     __syncthreads();
-    const int n = lut_size(reach), mid = reach + kLutPad, ps = a.buckets.per_side;
-    for (int b = threadIdx.x; b < nb; b += kThreads) {
-      const int k = b % ps;
-      const bool ahead = b >= ps;              // the second half of a two-sided table
-      const int from = a.buckets.start[k];
-      const int to = k + 1 < ps ? a.buckets.start[k + 1] : mid + 1;   // distances [from, to)
+    // the four wavefronts' sums by distance in the place of the first's
+    const int n = lut_size(reach), mid = reach + kLutPad, per = a.buckets.per_side;
+    float *all = lut + n;
+    for (int i = threadIdx.x; i < n; i += kThreads)
+      all[i] = (all[i] + all[n + i]) + (all[2 * n + i] + all[3 * n + i]);
+    __syncthreads();
+    // a wavefront per bucket in turn
+    const float fl = (red[0] + red[2]) + (red[4] + red[6]), fr = (red[1] + red[3]) + (red[5] + red[7]);
+    for (int b = wave; b < nb; b += 4) {
+      const int k = b % per;
+      const bool ahead = b >= per;             // the second half of a two-sided table
+      const int to = k + 1 < per ? a.buckets.start[k + 1] : mid + 1;   // distances [from, to)
       float x = 0.f;
-      for (int w = 0; w < 4; ++w) {
-        const float *hw = lut + n * (1 + w) + mid;
-        for (int d = max(from, ahead ? 1 : 0); d < to; ++d) x += hw[ahead ? d : -d];
-        if (k + 1 == ps) x += far_sum[w][ahead];
-        if (!a.buckets.two_sided && k == 0) {  // keys ahead count as distance 0
-          for (int d = 1; d <= mid; ++d) x += hw[d];
-          x += far_sum[w][1];
-        }
-      }
-      tout[b] = x;
+      for (int d = max(a.buckets.start[k], ahead ? 1 : 0) + lane; d < to; d += 64)
+        x += all[mid + (ahead ? d : -d)];
+      if (!a.buckets.two_sided && k == 0)      // keys ahead count as distance 0
+        for (int d = 1 + lane; d <= mid; d += 64) x += all[mid + d];
+#pragma unroll
+      for (int o = 32; o; o >>= 1) x += __shfl_xor(x, o);
+      if (k + 1 == per) x += ahead ? fr : fl;
+      if (!a.buckets.two_sided && k == 0) x += fr;
+      if (lane == 0) tout[b] = x;
     }
   }
+}
+
+// Both in one launch, the longer-running blocks of dK and dV first.
+template <class T, int DP, bool CAP, int BIAS>
+__global__ __launch_bounds__(kThreads, 2) void grad_pairs(const AttnGradArgs ga, int row_blocks,
+                                                          int kv_blocks) {
+  extern __shared__ __align__(1024) char lds[];
+  __shared__ float red[8];
+  if ((int)blockIdx.x < kv_blocks)
+    grad_kv<T, DP, CAP, BIAS>(ga, row_blocks, blockIdx.x, lds, red);
+  else
+    grad_q<T, DP, CAP, BIAS>(ga, row_blocks, blockIdx.x - kv_blocks, lds, red);
 }
 
 // dtable[head][b]: the tiles' partial sums; 64 of them per lane group in turn, then joined.
@@ -512,22 +588,24 @@ int64_t tile_bound(int64_t rows, int64_t docs, int64_t longest, int tile) {
 
 template <class T, int DP, bool CAP, int BIAS>
 hipError_t launch(const AttnGradArgs &a, int row_blocks, hipStream_t s) {
-  static LdsLimit lim_kv, lim_q;
+  static LdsLimit limit;
+  constexpr int kTiles = 4 * GradTiles<DP>::kStep * DP * 2;
+  constexpr int kKv = kTiles + 128 * DP * 2 + 2 * GradTiles<DP>::kStep * 8;
+  constexpr int kQ = kTiles + (BIAS == kBiasTable ? 4 * kSkew * 4 : 0);
+  auto bytes = [](int lut) {
+    const int x = kKv + lut, y = kQ + 5 * lut;
+    return x > y ? x : y;
+  };
   const int lut = BIAS == kBiasTable ? lut_size(a.f.buckets.start[a.f.buckets.per_side - 1]) * 4 : 0;
-  const int most = lut_size(kMaxReach) * 4;
-  const int base = 4 * 32 * DP * 2;
-  hipError_t e = lim_kv.set(reinterpret_cast<const void *>(&grad_kv<T, DP, CAP, BIAS>),
-                            base + 1024 + most);
-  if (e != hipSuccess) return e;
-  e = lim_q.set(reinterpret_cast<const void *>(&grad_q<T, DP, CAP, BIAS>), base + 5 * most);
+  hipError_t e = limit.set(reinterpret_cast<const void *>(&grad_pairs<T, DP, CAP, BIAS>),
+                           bytes(BIAS == kBiasTable ? lut_size(kMaxReach) * 4 : 0));
   if (e != hipSuccess) return e;
   const int64_t kb = tile_bound(a.f.k_rows, a.f.docs, a.f.max_k, 128) * a.f.kv_heads;
   const int64_t units = tile_bound(a.f.q_rows, a.f.docs, a.f.max_q, 128);
-  if (kb > 0)
-    grad_kv<T, DP, CAP, BIAS><<<dim3((uint32_t)kb), kThreads, base + 1024 + lut, s>>>(a, row_blocks);
-  if (units > 0)
-    grad_q<T, DP, CAP, BIAS>
-        <<<dim3((uint32_t)(units * a.f.heads)), kThreads, base + 5 * lut, s>>>(a, row_blocks);
+  const int64_t blocks = kb + units * a.f.heads;
+  if (blocks > 0)
+    grad_pairs<T, DP, CAP, BIAS>
+        <<<dim3((uint32_t)blocks), kThreads, bytes(lut), s>>>(a, row_blocks, (int)kb);
   if (BIAS == kBiasTable) {
     const int nb = (a.f.buckets.two_sided ? 2 : 1) * a.f.buckets.per_side;
     grad_table<T><<<dim3((uint32_t)(a.f.heads * nb)), 256, 0, s>>>(a, (int)units, nb);
@@ -552,7 +630,7 @@ hipError_t by_bias(const AttnGradArgs &a, int row_blocks, hipStream_t s) {
 
 size_t attend_grad_bytes(int32_t q_rows, int32_t docs, int32_t heads, int32_t buckets, bool fp16) {
   auto up = [](int64_t n) { return (n + 63) / 64 * 64; };
-  int64_t n = up((int64_t)q_rows * heads);
+  int64_t n = up(2 * (int64_t)q_rows * heads);
   if (fp16) n += 2 * kRowBlocks;
   if (buckets) n += up(((int64_t)q_rows / 128 + docs) * heads * buckets);
   return (size_t)n * 4;
@@ -561,8 +639,8 @@ size_t attend_grad_bytes(int32_t q_rows, int32_t docs, int32_t heads, int32_t bu
 hipError_t launch_attend_grad(const AttnGradArgs &args, void *ws, hipStream_t s) {
   AttnGradArgs a = args;
   auto up = [](int64_t n) { return (n + 63) / 64 * 64; };
-  a.delta = static_cast<float *>(ws);
-  a.bound = a.delta + up((int64_t)a.f.q_rows * a.f.heads);
+  a.rows = static_cast<float *>(ws);
+  a.bound = a.rows + up(2 * (int64_t)a.f.q_rows * a.f.heads);
   a.tpart = a.bound + (a.f.fp16 ? 2 * kRowBlocks : 0);
   int64_t need = (int64_t)a.f.q_rows * a.f.heads;
   if (a.f.fp16 && (int64_t)a.f.k_rows * a.f.kv_heads > need) need = (int64_t)a.f.k_rows * a.f.kv_heads;

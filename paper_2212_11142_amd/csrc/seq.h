@@ -27,9 +27,10 @@ struct BucketMap {
 struct AttnArgs {
   const char *q, *k, *v;
   char *o;
+  char *rest;                          // what rounding took from o (null: not kept)
   float *lse;                          // [heads][q_rows]
   // strides in bytes
-  int64_t q_row, q_head, k_row, k_head, v_row, v_head, o_row, o_head;
+  int64_t q_row, q_head, k_row, k_head, v_row, v_head, o_row, o_head, rest_row, rest_head;
   const int32_t *qb, *qe, *kb, *ke, *prefix;
   int32_t docs, heads, kv_heads, group, bytes;  // bytes: of a head's row, 2 dim
   int32_t q_rows, k_rows, max_q, max_k;
@@ -41,7 +42,7 @@ struct AttnArgs {
   int32_t fp16;
 };
 
-// Gradient: q, k, v, o, lse as of the forward call.
+// Gradient: q, k, v, o, rest, lse as of the forward call.
 struct AttnGradArgs {
   AttnArgs f;
   const char *dout;
@@ -49,7 +50,7 @@ struct AttnGradArgs {
   void *dtable;                        // [heads][buckets] or null
   int64_t do_row, do_head, dq_row, dq_head, dk_row, dk_head, dv_row, dv_head;
   // workspace
-  float *delta;                        // [heads][q_rows] dout . out
+  float *rows;                         // [heads][q_rows][2] log-sum, dout . out
   float *bound;                        // fp16: block maxima and the power of two dS is kept at
   float *tpart;                        // [tiles][heads][buckets] partial table gradients
 };

@@ -69,18 +69,20 @@ gp_status check_heads(const gp_heads *x, const char *name, int32_t rows) {
 }
 
 AttnArgs make_args(const gp_attention *t, const gp_heads *q, const gp_heads *k, const gp_heads *v,
-                   const gp_heads *o, const void *table, float *lse) {
+                   const gp_heads *o, const gp_heads *rest, const void *table, float *lse) {
   AttnArgs a;
   std::memset(&a, 0, sizeof a);
-  if (q) {
-    a.q = static_cast<const char *>(q->data);
-    a.k = static_cast<const char *>(k->data);
-    a.v = static_cast<const char *>(v->data);
-    a.o = static_cast<char *>(o->data);
-    a.q_row = 2 * q->row, a.q_head = 2 * q->head;
-    a.k_row = 2 * k->row, a.k_head = 2 * k->head;
-    a.v_row = 2 * v->row, a.v_head = 2 * v->head;
-    a.o_row = 2 * o->row, a.o_head = 2 * o->head;
+  a.q = static_cast<const char *>(q->data);
+  a.k = static_cast<const char *>(k->data);
+  a.v = static_cast<const char *>(v->data);
+  a.o = static_cast<char *>(o->data);
+  a.q_row = 2 * q->row, a.q_head = 2 * q->head;
+  a.k_row = 2 * k->row, a.k_head = 2 * k->head;
+  a.v_row = 2 * v->row, a.v_head = 2 * v->head;
+  a.o_row = 2 * o->row, a.o_head = 2 * o->head;
+  if (rest) {
+    a.rest = static_cast<char *>(rest->data);
+    a.rest_row = 2 * rest->row, a.rest_head = 2 * rest->head;
   }
   a.lse = lse;
   a.qb = t->q_begin, a.qe = t->q_end, a.kb = t->k_begin, a.ke = t->k_end, a.prefix = t->prefix;
@@ -167,23 +169,25 @@ size_t gp_attend_workspace_bytes(const gp_attention *t, int32_t with_grad) {
 }
 
 gp_status gp_attend(const gp_attention *t, const gp_heads *q, const gp_heads *k, const gp_heads *v,
-                    const void *table, const gp_heads *out, float *lse, void *workspace,
-                    size_t ws_bytes, void *stream) {
+                    const void *table, const gp_heads *out, const gp_heads *rest, float *lse,
+                    void *workspace, size_t ws_bytes, void *stream) {
   return guarded([&]() -> gp_status {
     gp_status st = check_attention(t);
     if (st == GP_OK) st = check_heads(q, "q", t->q_rows);
     if (st == GP_OK) st = check_heads(k, "k", t->k_rows);
     if (st == GP_OK) st = check_heads(v, "v", t->k_rows);
     if (st == GP_OK) st = check_heads(out, "out", t->q_rows);
+    if (st == GP_OK && rest) st = check_heads(rest, "rest", t->q_rows);
     if (st != GP_OK) return st;
     if ((t->per_side > 0) != (table != nullptr)) return bad("a table goes with per_side > 0");
     if (!lse && t->q_rows > 0) return bad("lse is NULL");
     if (t->n_docs == 0 || t->max_q == 0) return GP_OK;
     const int cus = cus_of(stream);
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    const AttnArgs a = make_args(t, q, k, v, out, rest, table, lse);
+    if (rest) return hip_status(launch_attend(a, s), "attention");
     st = check_workspace(workspace, ws_bytes, attend_bytes(t, cus));
     if (st != GP_OK) return st;
-    const AttnArgs a = make_args(t, q, k, v, out, table, lse);
-    hipStream_t s = static_cast<hipStream_t>(stream);
     if (attend_use_few(a.docs, a.kv_heads, a.group, a.max_q, a.max_k, cus))
       return hip_status(launch_attend_few(a, static_cast<float *>(workspace), cus, s), "attention");
     return hip_status(launch_attend(a, s), "attention");
@@ -192,7 +196,7 @@ gp_status gp_attend(const gp_attention *t, const gp_heads *q, const gp_heads *k,
 
 gp_status gp_attend_grad(const gp_attention *t, const gp_heads *q, const gp_heads *k,
                          const gp_heads *v, const void *table, const gp_heads *out,
-                         const float *lse, const gp_heads *dout, const gp_heads *dq,
+                         const gp_heads *rest, const float *lse, const gp_heads *dout, const gp_heads *dq,
                          const gp_heads *dk, const gp_heads *dv, void *dtable, void *workspace,
                          size_t ws_bytes, void *stream) {
   return guarded([&]() -> gp_status {
@@ -201,6 +205,7 @@ gp_status gp_attend_grad(const gp_attention *t, const gp_heads *q, const gp_head
     if (st == GP_OK) st = check_heads(k, "k", t->k_rows);
     if (st == GP_OK) st = check_heads(v, "v", t->k_rows);
     if (st == GP_OK) st = check_heads(out, "out", t->q_rows);
+    if (st == GP_OK) st = check_heads(rest, "rest", t->q_rows);
     if (st == GP_OK) st = check_heads(dout, "dout", t->q_rows);
     if (st == GP_OK) st = check_heads(dq, "dq", t->q_rows);
     if (st == GP_OK) st = check_heads(dk, "dk", t->k_rows);
@@ -215,7 +220,7 @@ gp_status gp_attend_grad(const gp_attention *t, const gp_heads *q, const gp_head
     if (st != GP_OK) return st;
     AttnGradArgs g;
     std::memset(&g, 0, sizeof g);
-    g.f = make_args(t, q, k, v, out, table, const_cast<float *>(lse));
+    g.f = make_args(t, q, k, v, out, rest, table, const_cast<float *>(lse));
     g.dout = static_cast<const char *>(dout->data);
     g.dq = static_cast<char *>(dq->data);
     g.dk = static_cast<char *>(dk->data);

@@ -69,11 +69,19 @@ struct Fp16 {
 __device__ inline float fast_exp2(float x) { return __builtin_amdgcn_exp2f(x); }
 __device__ inline int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
 
-// value of the lane 32 away
-__device__ inline float other_half(float x) {
-  const u32x2 r = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(uint32_t, x),
-                                                   __builtin_bit_cast(uint32_t, x), false, false);
-  return __builtin_bit_cast(float, (threadIdx.x & 32) ? r[0] : r[1]);
+// (a parameter, not an element of a vector: __builtin_bit_cast takes those from the front)
+__device__ inline float word_float(uint32_t x) { return __builtin_bit_cast(float, x); }
+
+// Sum and maximum over a lane and the one 32 away.
+__device__ inline float sum_halves(float x) {
+  const uint32_t u = __builtin_bit_cast(uint32_t, x);
+  const u32x2 r = __builtin_amdgcn_permlane32_swap(u, u, false, false);
+  return word_float(r[0]) + word_float(r[1]);
+}
+__device__ inline float max_halves(float x) {
+  const uint32_t u = __builtin_bit_cast(uint32_t, x);
+  const u32x2 r = __builtin_amdgcn_permlane32_swap(u, u, false, false);
+  return fmaxf(word_float(r[0]), word_float(r[1]));
 }
 
 // ------------------------------------------------------------------ LDS tiles
@@ -145,27 +153,47 @@ __device__ inline uint32_t lds_address(const void *p) {
   return (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const void *)p;
 }
 
-// A operand (32 rows from row0, k = 16 s + ..) of a tile whose rows run along k.
+// Operands out of LDS tiles. A lane's addresses differ from its first one by an XOR of the
+// piece (the swizzle is one too) and by whole rows, so that two offsets per lane and one
+// instruction per address do: kept ready for every piece, they would take the accumulators'
+// registers.
 template <int DP>
-__device__ inline u32x4 row_operand(const char *tile, int row0, int s, int lane) {
-  const int row = row0 + (lane & 31);
-  const int piece = (2 * s + (lane >> 5)) ^ swizzle<DP>(row);
-  return *reinterpret_cast<const u32x4 *>(tile + row * (DP * 2) + piece * 16);
+struct TileReader {
+  uint32_t row, col;   // of this lane within a tile
+
+  __device__ void init(int lane) {
+    const int r = lane & 31;
+    row = r * (DP * 2) + ((lane >> 5) ^ swizzle<DP>(r)) * 16;
+    const int q = 4 * (lane >> 5) + ((lane & 15) >> 2);
+    const int piece = 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1);
+    col = q * (DP * 2) + (piece ^ swizzle<DP>(q)) * 16 + (lane & 1) * 8;
+  }
+  // an offset of the tile at LDS address `tile` (a multiple of 1024)
+  static __device__ uint32_t at(uint32_t tile, uint32_t offset) {
+    uint32_t x = tile + offset;
+    asm volatile("" : "+v"(x));   // (not to be precomputed for every piece)
+    return x;
+  }
+};
+
+// A operand (32 rows from row0, k = 16 s + ..) of a tile whose rows run along k; x =
+// at(tile, row).
+template <int DP>
+__device__ inline u32x4 row_operand(uint32_t x, int row0, int s) {
+  typedef __attribute__((address_space(3))) const u32x4 lds_u32x4;
+  return *(lds_u32x4 *)(uintptr_t)((x ^ (s * 32)) + row0 * (DP * 2));
 }
 
 // A operand of the transposed tile: rows of the operand are the columns 32 c.. of the tile,
 // its k the tile's rows row0 + 16.. in the order of a D result's registers: lane half h has
-// the rows row0 + 4 h + {0..3} and row0 + 8 + 4 h + {0..3}.
+// the rows row0 + 4 h + {0..3} and row0 + 8 + 4 h + {0..3}; x = at(tile, col).
 template <int DP>
-__device__ inline u32x4 col_operand(const char *tile, int row0, int c, int lane) {
+__device__ inline u32x4 col_operand(uint32_t x, int row0, int c) {
   typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
-  const int row = row0 + 4 * (lane >> 5) + ((lane & 15) >> 2);
-  const int piece = 4 * c + 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1);
-  const int half = (lane & 1) * 8;
-  const char *p0 = tile + row * (DP * 2) + ((piece ^ swizzle<DP>(row)) * 16) + half;
-  const char *p1 = tile + (row + 8) * (DP * 2) + ((piece ^ swizzle<DP>(row + 8)) * 16) + half;
-  const s16x4 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)p0);
-  const s16x4 b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)p1);
+  const s16x4 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+      (lds_s16x4 *)(uintptr_t)((x ^ (c * 64)) + row0 * (DP * 2)));
+  const s16x4 b = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+      (lds_s16x4 *)(uintptr_t)((x ^ (c * 64 + 32)) + (row0 + 8) * (DP * 2)));
   const u32x2 ua = __builtin_bit_cast(u32x2, a), ub = __builtin_bit_cast(u32x2, b);
   return u32x4{ua[0], ua[1], ub[0], ub[1]};
 }
@@ -186,8 +214,9 @@ __device__ inline void load_operand(const char *base, int64_t stride, int row, i
 }
 
 // Writes a transposed result (D^T: element d = 32 c + 8 g + 4 (lane / 32) + r of the row at
-// p, both lane halves of a row) as 16-byte pieces, times f.
-template <class T, int DT>
+// p, both lane halves of a row) as 16-byte pieces, times f; with REST what the rounding to T
+// took from each value, instead.
+template <class T, int DT, bool REST = false>
 __device__ inline void store_row(char *p, bool ok, int bytes, const f32x16 *acc, float f, int lane) {
   const int h = lane >> 5;
 #pragma unroll
@@ -197,9 +226,13 @@ __device__ inline void store_row(char *p, bool ok, int bytes, const f32x16 *acc,
       uint32_t w[4];
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
-        const int e = 4 * (g + i);
-        w[2 * i] = T::pack(acc[c][e] * f, acc[c][e + 1] * f);
-        w[2 * i + 1] = T::pack(acc[c][e + 2] * f, acc[c][e + 3] * f);
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+          const int e = 4 * (g + i) + 2 * k;
+          const float x = acc[c][e] * f, y = acc[c][e + 1] * f;
+          const uint32_t r = T::pack(x, y);
+          w[2 * i + k] = REST ? T::pack(x - T::lo(r), y - T::hi(r)) : r;
+        }
       }
       // lower half: all of piece g, upper half: all of piece g + 1
       const u32x2 x = __builtin_amdgcn_permlane32_swap(w[0], w[2], false, false);

@@ -123,9 +123,9 @@ _SIGS = [
     ("gp_forest_free", None, [_VP]),
     ("gp_attend_workspace_bytes", C.c_size_t, [C.POINTER(_Attention), C.c_int32]),
     ("gp_attend", C.c_int, [C.POINTER(_Attention)] + [C.POINTER(_Heads)] * 3
-     + [_VP, C.POINTER(_Heads), _VP, _VP, C.c_size_t, _VP]),
+     + [_VP, C.POINTER(_Heads), C.POINTER(_Heads), _VP, _VP, C.c_size_t, _VP]),
     ("gp_attend_grad", C.c_int, [C.POINTER(_Attention)] + [C.POINTER(_Heads)] * 3
-     + [_VP, C.POINTER(_Heads), _VP] + [C.POINTER(_Heads)] * 4 + [_VP, _VP, C.c_size_t, _VP]),
+     + [_VP, C.POINTER(_Heads), C.POINTER(_Heads), _VP] + [C.POINTER(_Heads)] * 4 + [_VP, _VP, C.c_size_t, _VP]),
     ("gp_logprob_workspace_bytes", C.c_size_t, [C.c_int32, C.c_int32, C.c_int32]),
     ("gp_logprob", C.c_int, [C.c_int32, _VP, C.c_int64, C.c_int32, C.c_int32, C.c_float, _VP,
                              C.c_int32, _VP, _VP, _VP, _VP, _VP, _VP, C.c_size_t, _VP]),

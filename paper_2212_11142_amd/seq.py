@@ -184,8 +184,8 @@ class Attention:
 
 class AttendBuffers:
     """Outputs and workspaces of attention calls with a description: out, lse
-    [heads, q_rows], and with grad dq, dk, dv and (with buckets) dtable. Rows outside every
-    document are 0."""
+    [heads, q_rows], and with grad dq, dk, dv and (with buckets) dtable, and rest (what
+    rounding took from out, which the gradient reads). Rows outside every document are 0."""
 
     def __init__(self, att: Attention, grad: bool = False):
         torch = _torch()
@@ -200,10 +200,11 @@ class AttendBuffers:
         self.lse = torch.full((att.heads, d.q_rows), -math.inf, dtype=torch.float32, device="cuda")
         n = att.workspace_bytes(False)
         self.workspace = gp._workspace(n) if n else None
-        self.dq = self.dk = self.dv = self.dtable = self.grad_workspace = None
+        self.dq = self.dk = self.dv = self.dtable = self.rest = self.grad_workspace = None
         if grad:
             if not d.k_disjoint:
                 raise ValueError("gradients need documents whose key rows do not overlap")
+            self.rest = rows(d.q_full, d.q_rows, att.heads)
             self.dq = rows(d.q_full, d.q_rows, att.heads)
             self.dk = rows(d.k_full, d.k_rows, att.kv_heads)
             self.dv = rows(d.k_full, d.k_rows, att.kv_heads)
@@ -245,6 +246,7 @@ def attend_into(att: Attention, q, k, v, bufs: AttendBuffers, table=None):
         att.ref, _heads(q, att, d.q_rows, att.heads, "q"),
         _heads(k, att, d.k_rows, att.kv_heads, "k"), _heads(v, att, d.k_rows, att.kv_heads, "v"),
         _table(table, att), _heads(bufs.out, att, d.q_rows, att.heads, "out"),
+        None if bufs.rest is None else _heads(bufs.rest, att, d.q_rows, att.heads, "rest"),
         bufs.lse.data_ptr(), _ptr(ws), 0 if ws is None else ws.numel(), _stream()))
 
 
@@ -265,7 +267,8 @@ def attend_grad_into(att: Attention, q, k, v, dout, bufs: AttendBuffers, table=N
     _check(gp.load().gp_attend_grad(
         att.ref, _heads(q, att, d.q_rows, H, "q"), _heads(k, att, d.k_rows, K, "k"),
         _heads(v, att, d.k_rows, K, "v"), _table(table, att),
-        _heads(bufs.out, att, d.q_rows, H, "out"), bufs.lse.data_ptr(),
+        _heads(bufs.out, att, d.q_rows, H, "out"), _heads(bufs.rest, att, d.q_rows, H, "rest"),
+        bufs.lse.data_ptr(),
         _heads(dout, att, d.q_rows, H, "dout"), _heads(bufs.dq, att, d.q_rows, H, "dq"),
         _heads(bufs.dk, att, d.k_rows, K, "dk"), _heads(bufs.dv, att, d.k_rows, K, "dv"),
         _ptr(bufs.dtable), _ptr(ws), ws.numel(), _stream()))
