@@ -854,7 +854,6 @@ int stream_cus(hipStream_t s) {
 // For the entry points of seq_abi.hip.
 namespace bgp {
 gp_status seq_fail(gp_status st, const std::string &msg) { return fail(st, msg); }
-int seq_cus(hipStream_t s) { return stream_cus(s); }
 }  // namespace bgp
 namespace {
 

@@ -20,14 +20,14 @@ struct FewPlan {
   int row_tiles, rows, chunk, chunks;  // rows: kept per tile; chunk: keys of a block
 };
 
-FewPlan plan(int docs, int kv_heads, int group, int max_q, int max_k, int cus) {
+FewPlan plan(int docs, int kv_heads, int group, int max_q, int max_k) {
   FewPlan p;
   const int64_t r = (int64_t)group * max_q;
   p.row_tiles = (int)((r + kRows - 1) / kRows);
   p.rows = (int)(r < kRows ? r : kRows);
   const int64_t units = (int64_t)docs * kv_heads * p.row_tiles;
   // about 8 blocks per compute unit if the keys allow it, none under 128 keys
-  int64_t c = ((int64_t)max_k * units / (8 * (int64_t)cus) + 127) / 128 * 128;
+  int64_t c = ((int64_t)max_k * units / (8 * (int64_t)kSeqCus) + 127) / 128 * 128;
   if (c < 128) c = 128;
   if (c > 4096) c = 4096;
   p.chunk = (int)c;
@@ -342,9 +342,9 @@ __global__ __launch_bounds__(256) void few_join(const AttnArgs a, const FewPlan 
 }
 
 template <class T, int DP, bool CAP, int BIAS>
-hipError_t launch(const AttnArgs &a, float *part, int cus, hipStream_t s) {
+hipError_t launch(const AttnArgs &a, float *part, hipStream_t s) {
   static LdsLimit limit;
-  const FewPlan p = plan(a.docs, a.kv_heads, a.group, a.max_q, a.max_k, cus);
+  const FewPlan p = plan(a.docs, a.kv_heads, a.group, a.max_q, a.max_k);
   int lds = 16 * kKeys * DP * 2;
   const int join = 4 * kRows * (DP + 4) * 4;
   if (lds < join) lds = join;
@@ -361,39 +361,38 @@ hipError_t launch(const AttnArgs &a, float *part, int cus, hipStream_t s) {
 }
 
 template <class T, int DP>
-hipError_t by_bias(const AttnArgs &a, float *part, int cus, hipStream_t s) {
+hipError_t by_bias(const AttnArgs &a, float *part, hipStream_t s) {
   const int bias = a.table ? kBiasTable : (a.slopes ? kBiasSlope : kBiasNone);
   if (a.cap > 0.f) {
-    if (bias == kBiasTable) return launch<T, DP, true, kBiasTable>(a, part, cus, s);
-    if (bias == kBiasSlope) return launch<T, DP, true, kBiasSlope>(a, part, cus, s);
-    return launch<T, DP, true, kBiasNone>(a, part, cus, s);
+    if (bias == kBiasTable) return launch<T, DP, true, kBiasTable>(a, part, s);
+    if (bias == kBiasSlope) return launch<T, DP, true, kBiasSlope>(a, part, s);
+    return launch<T, DP, true, kBiasNone>(a, part, s);
   }
-  if (bias == kBiasTable) return launch<T, DP, false, kBiasTable>(a, part, cus, s);
-  if (bias == kBiasSlope) return launch<T, DP, false, kBiasSlope>(a, part, cus, s);
-  return launch<T, DP, false, kBiasNone>(a, part, cus, s);
+  if (bias == kBiasTable) return launch<T, DP, false, kBiasTable>(a, part, s);
+  if (bias == kBiasSlope) return launch<T, DP, false, kBiasSlope>(a, part, s);
+  return launch<T, DP, false, kBiasNone>(a, part, s);
 }
 
 }  // namespace
 
-bool attend_use_few(int32_t docs, int32_t kv_heads, int32_t group, int32_t max_q, int32_t max_k,
-                    int cus) {
-  (void)docs, (void)kv_heads, (void)max_k, (void)cus;
+bool attend_use_few(int32_t docs, int32_t kv_heads, int32_t group, int32_t max_q, int32_t max_k) {
+  (void)docs, (void)kv_heads, (void)max_k;
   return (int64_t)group * max_q <= kRows;
 }
 
 size_t attend_few_bytes(int32_t docs, int32_t kv_heads, int32_t group, int32_t max_q, int32_t max_k,
-                        int32_t dim, int cus) {
-  const FewPlan p = plan(docs, kv_heads, group, max_q, max_k, cus);
+                        int32_t dim) {
+  const FewPlan p = plan(docs, kv_heads, group, max_q, max_k);
   const int64_t units = (int64_t)docs * kv_heads * p.row_tiles;
   if (p.chunks == 1) return 0;
   const int64_t rows = units * p.chunks * p.rows;
   return (size_t)((rows * 2 + 63) / 64 * 64 + rows * (dim <= 64 ? 64 : 128)) * 4;
 }
 
-hipError_t launch_attend_few(const AttnArgs &a, float *part, int cus, hipStream_t s) {
+hipError_t launch_attend_few(const AttnArgs &a, float *part, hipStream_t s) {
   if (a.bytes <= 128)
-    return a.fp16 ? by_bias<Fp16, 64>(a, part, cus, s) : by_bias<Bf16, 64>(a, part, cus, s);
-  return a.fp16 ? by_bias<Fp16, 128>(a, part, cus, s) : by_bias<Bf16, 128>(a, part, cus, s);
+    return a.fp16 ? by_bias<Fp16, 64>(a, part, s) : by_bias<Bf16, 64>(a, part, s);
+  return a.fp16 ? by_bias<Fp16, 128>(a, part, s) : by_bias<Bf16, 128>(a, part, s);
 }
 
 }  // namespace bgp

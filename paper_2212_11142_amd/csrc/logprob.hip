@@ -395,11 +395,11 @@ struct SplitPlan {
   int parts;       // blocks of a row
   int64_t chunk;   // entries of a block
 };
-SplitPlan split_plan(int32_t rows, int32_t width, int32_t top, int cus) {
+SplitPlan split_plan(int32_t rows, int32_t width, int32_t top) {
   SplitPlan p{1, width};
   // one block per row where that fills the device, or the rows are short
-  if (rows >= 2 * cus || width <= 8192) return p;
-  int64_t parts = (4 * (int64_t)cus + rows - 1) / rows;
+  if (rows >= 2 * kSeqCus || width <= 8192) return p;
+  int64_t parts = (4 * (int64_t)kSeqCus + rows - 1) / rows;
   const int64_t most = width / 2048;            // (a vector or two per thread)
   if (parts > most) parts = most;
   if (top > 0 && parts > kList / top) parts = kList / top;
@@ -527,7 +527,7 @@ __global__ __launch_bounds__(kThreads) void logprob_grad(const LogprobArgs a, in
 }
 
 template <int DT>
-hipError_t forward(const LogprobArgs &a, void *ws, int cus, hipStream_t s) {
+hipError_t forward(const LogprobArgs &a, void *ws, hipStream_t s) {
   constexpr int kVec = Elem<DT>::kVec;
   if (a.width <= kWaveWidth) {
     const dim3 grid((uint32_t)((a.rows + 3) / 4));
@@ -537,7 +537,7 @@ hipError_t forward(const LogprobArgs &a, void *ws, int cus, hipStream_t s) {
     else logprob_wave<DT, kWaveWidth / (64 * kVec)><<<grid, kThreads, 0, s>>>(a);
     return hipGetLastError();
   }
-  const SplitPlan sp = split_plan(a.rows, a.width, a.top, cus);
+  const SplitPlan sp = split_plan(a.rows, a.width, a.top);
   if (sp.parts == 1) {
     logprob_row<DT><<<dim3((uint32_t)a.rows), kThreads, 0, s>>>(a);
     return hipGetLastError();
@@ -551,7 +551,7 @@ hipError_t forward(const LogprobArgs &a, void *ws, int cus, hipStream_t s) {
 }
 
 template <int DT>
-hipError_t gradient(const LogprobArgs &a, int cus, hipStream_t s) {
+hipError_t gradient(const LogprobArgs &a, hipStream_t s) {
   constexpr int kVec = Elem<DT>::kVec;
   const int64_t nv = (a.width + kVec - 1) / kVec;
   // a wavefront per row up to 512 vectors, a block per row above; more blocks per row (each
@@ -559,7 +559,7 @@ hipError_t gradient(const LogprobArgs &a, int cus, hipStream_t s) {
   const int threads = nv <= 512 ? 64 : kThreads;
   int64_t per_row = 1;
   if (threads == kThreads) {
-    const int64_t want = (8 * (int64_t)cus + a.rows - 1) / a.rows, most = nv / (4 * kThreads);
+    const int64_t want = (8 * (int64_t)kSeqCus + a.rows - 1) / a.rows, most = nv / (4 * kThreads);
     per_row = want < most ? want : most;
     if (per_row < 1) per_row = 1;
   }
@@ -571,22 +571,22 @@ hipError_t gradient(const LogprobArgs &a, int cus, hipStream_t s) {
 
 }  // namespace
 
-size_t logprob_bytes(int32_t rows, int32_t width, int32_t top, int cus) {
+size_t logprob_bytes(int32_t rows, int32_t width, int32_t top) {
   if (width <= kWaveWidth) return 0;
-  const SplitPlan sp = split_plan(rows, width, top, cus);
+  const SplitPlan sp = split_plan(rows, width, top);
   return sp.parts == 1 ? 0 : (size_t)rows * sp.parts * ((size_t)top * 8 + 12);
 }
 
-hipError_t launch_logprob(const LogprobArgs &a, void *ws, int cus, hipStream_t s) {
-  if (a.dtype == kBf16) return forward<kBf16>(a, ws, cus, s);
-  if (a.dtype == kFp16) return forward<kFp16>(a, ws, cus, s);
-  return forward<kFp32>(a, ws, cus, s);
+hipError_t launch_logprob(const LogprobArgs &a, void *ws, hipStream_t s) {
+  if (a.dtype == kBf16) return forward<kBf16>(a, ws, s);
+  if (a.dtype == kFp16) return forward<kFp16>(a, ws, s);
+  return forward<kFp32>(a, ws, s);
 }
 
-hipError_t launch_logprob_grad(const LogprobArgs &a, int cus, hipStream_t s) {
-  if (a.dtype == kBf16) return gradient<kBf16>(a, cus, s);
-  if (a.dtype == kFp16) return gradient<kFp16>(a, cus, s);
-  return gradient<kFp32>(a, cus, s);
+hipError_t launch_logprob_grad(const LogprobArgs &a, hipStream_t s) {
+  if (a.dtype == kBf16) return gradient<kBf16>(a, s);
+  if (a.dtype == kFp16) return gradient<kFp16>(a, s);
+  return gradient<kFp32>(a, s);
 }
 
 }  // namespace bgp

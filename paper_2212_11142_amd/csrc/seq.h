@@ -13,6 +13,7 @@
 namespace bgp {
 
 constexpr int kSeqMaxDim = 128;       // head size
+constexpr int kSeqCus = 256;          // compute units of an MI355X: what splits are sized for
 constexpr int kMaxBuckets = 64;       // buckets of one side
 constexpr int kMaxReach = 1024;       // first distance of the last bucket
 constexpr int kMaxTop = 128;          // alternatives of a row
@@ -58,10 +59,9 @@ struct AttnGradArgs {
 hipError_t launch_attend(const AttnArgs &a, hipStream_t s);
 // few query rows: key ranges split over blocks; part: attend_few_bytes() of workspace
 size_t attend_few_bytes(int32_t docs, int32_t kv_heads, int32_t group, int32_t max_q, int32_t max_k,
-                        int32_t dim, int cus);
-bool attend_use_few(int32_t docs, int32_t kv_heads, int32_t group, int32_t max_q, int32_t max_k,
-                    int cus);
-hipError_t launch_attend_few(const AttnArgs &a, float *part, int cus, hipStream_t s);
+                        int32_t dim);
+bool attend_use_few(int32_t docs, int32_t kv_heads, int32_t group, int32_t max_q, int32_t max_k);
+hipError_t launch_attend_few(const AttnArgs &a, float *part, hipStream_t s);
 
 size_t attend_grad_bytes(int32_t q_rows, int32_t docs, int32_t heads, int32_t buckets, bool fp16);
 hipError_t launch_attend_grad(const AttnGradArgs &a, void *ws, hipStream_t s);
@@ -78,12 +78,11 @@ struct LogprobArgs {
   void *dx;
   int64_t dx_row;
 };
-size_t logprob_bytes(int32_t rows, int32_t width, int32_t top, int cus);
-hipError_t launch_logprob(const LogprobArgs &a, void *ws, int cus, hipStream_t s);
-hipError_t launch_logprob_grad(const LogprobArgs &a, int cus, hipStream_t s);
+size_t logprob_bytes(int32_t rows, int32_t width, int32_t top);
+hipError_t launch_logprob(const LogprobArgs &a, void *ws, hipStream_t s);
+hipError_t launch_logprob_grad(const LogprobArgs &a, hipStream_t s);
 
 // abi.hip: records the calling thread's error message
 gp_status seq_fail(gp_status st, const std::string &msg);
-int seq_cus(hipStream_t s);
 
 }  // namespace bgp

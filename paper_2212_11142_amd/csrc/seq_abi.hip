@@ -9,14 +9,6 @@ using namespace bgp;
 
 namespace {
 
-// Compute units that workspaces are sized for (an MI355X has 256).
-constexpr int kCus = 256;
-
-int cus_of(void *stream) {
-  const int n = seq_cus(static_cast<hipStream_t>(stream));
-  return n < 1 ? 1 : (n > kCus ? kCus : n);
-}
-
 gp_status bad(const std::string &msg) { return seq_fail(GP_E_INVALID, msg); }
 
 gp_status check_attention(const gp_attention *t) {
@@ -114,11 +106,11 @@ gp_status check_workspace(const void *ws, size_t bytes, size_t need) {
   return GP_OK;
 }
 
-size_t attend_bytes(const gp_attention *t, int cus) {
+size_t attend_bytes(const gp_attention *t) {
   const int group = t->heads / t->kv_heads;
   if (t->n_docs == 0 || t->max_q == 0) return 0;
-  if (!attend_use_few(t->n_docs, t->kv_heads, group, t->max_q, t->max_k, cus)) return 0;
-  return attend_few_bytes(t->n_docs, t->kv_heads, group, t->max_q, t->max_k, t->dim, cus);
+  if (!attend_use_few(t->n_docs, t->kv_heads, group, t->max_q, t->max_k)) return 0;
+  return attend_few_bytes(t->n_docs, t->kv_heads, group, t->max_q, t->max_k, t->dim);
 }
 
 gp_status hip_status(hipError_t e, const char *what) {
@@ -162,7 +154,7 @@ size_t gp_attend_workspace_bytes(const gp_attention *t, int32_t with_grad) {
     if (st != GP_OK) return st;
     n = with_grad ? attend_grad_bytes(t->q_rows, t->n_docs, t->heads, bucket_count(t),
                                       t->dtype == GP_FP16)
-                  : attend_bytes(t, kCus);
+                  : attend_bytes(t);
     return GP_OK;
   });
   return n;
@@ -182,14 +174,13 @@ gp_status gp_attend(const gp_attention *t, const gp_heads *q, const gp_heads *k,
     if ((t->per_side > 0) != (table != nullptr)) return bad("a table goes with per_side > 0");
     if (!lse && t->q_rows > 0) return bad("lse is NULL");
     if (t->n_docs == 0 || t->max_q == 0) return GP_OK;
-    const int cus = cus_of(stream);
     hipStream_t s = static_cast<hipStream_t>(stream);
     const AttnArgs a = make_args(t, q, k, v, out, rest, table, lse);
     if (rest) return hip_status(launch_attend(a, s), "attention");
-    st = check_workspace(workspace, ws_bytes, attend_bytes(t, cus));
+    st = check_workspace(workspace, ws_bytes, attend_bytes(t));
     if (st != GP_OK) return st;
-    if (attend_use_few(a.docs, a.kv_heads, a.group, a.max_q, a.max_k, cus))
-      return hip_status(launch_attend_few(a, static_cast<float *>(workspace), cus, s), "attention");
+    if (attend_use_few(a.docs, a.kv_heads, a.group, a.max_q, a.max_k))
+      return hip_status(launch_attend_few(a, static_cast<float *>(workspace), s), "attention");
     return hip_status(launch_attend(a, s), "attention");
   });
 }
@@ -237,7 +228,7 @@ gp_status gp_attend_grad(const gp_attention *t, const gp_heads *q, const gp_head
 
 size_t gp_logprob_workspace_bytes(int32_t rows, int32_t width, int32_t top) {
   if (rows < 1 || width < 1 || top < 0 || top > kMaxTop) return 0;
-  return logprob_bytes(rows, width, top, kCus);
+  return logprob_bytes(rows, width, top);
 }
 
 gp_status gp_logprob(int32_t dtype, const void *x, int64_t stride, int32_t rows, int32_t width,
@@ -252,15 +243,14 @@ gp_status gp_logprob(int32_t dtype, const void *x, int64_t stride, int32_t rows,
     if (top > 0 && rows > 0 && (!top_logp || !top_id)) return bad("top_logp and top_id are required");
     if (logp && !target && rows > 0) return bad("logp needs target");
     if (rows == 0) return GP_OK;
-    const int cus = cus_of(stream);
-    st = check_workspace(workspace, ws_bytes, logprob_bytes(rows, width, top, cus));
+    st = check_workspace(workspace, ws_bytes, logprob_bytes(rows, width, top));
     if (st != GP_OK) return st;
     LogprobArgs a;
     std::memset(&a, 0, sizeof a);
     a.x = x, a.row = stride, a.rows = rows, a.width = width, a.top = top, a.dtype = dtype;
     a.scale = scale, a.target = target, a.logp = logp, a.entropy = entropy, a.lse = lse;
     a.top_logp = top_logp, a.top_id = top_id;
-    return hip_status(launch_logprob(a, workspace, cus, static_cast<hipStream_t>(stream)),
+    return hip_status(launch_logprob(a, workspace, static_cast<hipStream_t>(stream)),
                       "log probabilities");
   });
 }
@@ -283,7 +273,7 @@ gp_status gp_logprob_grad(int32_t dtype, const void *x, int64_t stride, int32_t 
     a.x = x, a.row = stride, a.rows = rows, a.width = width, a.dtype = dtype, a.scale = scale;
     a.target = target, a.lse = const_cast<float *>(lse), a.entropy = const_cast<float *>(entropy);
     a.g_logp = g_logp, a.g_entropy = g_entropy, a.dx = dx, a.dx_row = dx_stride;
-    return hip_status(launch_logprob_grad(a, cus_of(stream), static_cast<hipStream_t>(stream)),
+    return hip_status(launch_logprob_grad(a, static_cast<hipStream_t>(stream)),
                       "log probability gradient");
   });
 }
