@@ -80,7 +80,9 @@ __global__ __launch_bounds__(kThreads, 2) void attend_kernel(const AttnArgs a) {
   float slope2 = 0.f;
   if (BIAS == kBiasTable) {
     reach = a.buckets.start[a.buckets.per_side - 1];
-    fill_lut<T>(lut, a.buckets, a.table, head, kThreads);
+    uint8_t *map = reinterpret_cast<uint8_t *>(lut + lut_size(reach));
+    fill_map(map, a.buckets, threadIdx.x, kThreads);   // (each thread reads what it wrote)
+    fill_lut<T>(lut, map, a.buckets, a.table, head, threadIdx.x, kThreads);
   }
   if (BIAS == kBiasSlope) slope2 = a.slopes[head] * kLog2e;
   ScoreScale sc;
@@ -226,9 +228,12 @@ template <class T, int DP, bool CAP, int BIAS, bool REST>
 hipError_t launch_form(const AttnArgs &a, hipStream_t s) {
   static LdsLimit limit;
   int lds = 4 * kBN * DP * 2;
-  if (BIAS == kBiasTable) lds += lut_size(a.buckets.start[a.buckets.per_side - 1]) * 4;
+  if (BIAS == kBiasTable) {
+    const int reach = a.buckets.start[a.buckets.per_side - 1];
+    lds += lut_size(reach) * 4 + map_bytes(reach);
+  }
   hipError_t e = limit.set(reinterpret_cast<const void *>(&attend_kernel<T, DP, CAP, BIAS, REST>),
-                           4 * kBN * DP * 2 + lut_size(kMaxReach) * 4);
+                           4 * kBN * DP * 2 + lut_size(kMaxReach) * 4 + map_bytes(kMaxReach));
   if (e != hipSuccess) return e;
   // an upper bound of the documents' tiles; the blocks past the last one end at once
   const int64_t tiles = (int64_t)a.q_rows / kBM + a.docs;

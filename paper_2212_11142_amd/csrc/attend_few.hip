@@ -4,8 +4,10 @@
 // The group x queries rows that share a key head are the columns of one score tile (32 of
 // them, fewer are padding: the matrix instructions have 10 times the rate that memory can
 // feed). A block takes a range of keys, its 4 wavefronts take 32 keys each in turn, every
-// one with LDS buffers and copies of its own and no barrier in the loop; the blocks' sums
-// are joined by a second kernel in the order of the ranges.
+// one with LDS buffers and copies of its own and no barrier in the loop; a second kernel
+// joins the blocks' sums in the order of the ranges. (Joining them in the first kernel's last
+// block costs more than the launch it saves: what blocks hand over must pass the L2 of each
+// XCD, 15.4 against 7.6 + 4.4 us for 4095 keys and 4 key heads of 128.)
 #include "seq_dev.h"
 
 namespace bgp {
@@ -15,6 +17,13 @@ constexpr int kThreads = 256;
 constexpr int kKeys = 32;      // keys of a wavefront's step
 constexpr int kRows = 32;      // rows of a tile
 constexpr float kSlack = 8.f;  // as in the general form
+constexpr int kFewBlocks = 160;
+constexpr int kMaxValues = 4096;   // of the table for a group
+
+constexpr int few_tiles(int dp) {
+  const int tiles = 16 * kKeys * dp * 2, sums = 4 * kRows * (dp + 4) * 4;
+  return tiles > sums ? tiles : sums;
+}
 
 struct FewPlan {
   int row_tiles, rows, chunk, chunks;  // rows: kept per tile; chunk: keys of a block
@@ -26,9 +35,15 @@ FewPlan plan(int docs, int kv_heads, int group, int max_q, int max_k) {
   p.row_tiles = (int)((r + kRows - 1) / kRows);
   p.rows = (int)(r < kRows ? r : kRows);
   const int64_t units = (int64_t)docs * kv_heads * p.row_tiles;
-  // about 8 blocks per compute unit if the keys allow it, none under 128 keys
-  int64_t c = ((int64_t)max_k * units / (8 * (int64_t)kSeqCus) + 127) / 128 * 128;
-  if (c < 128) c = 128;
+  // about 8 blocks per compute unit; where those would have less than 512 keys each, one per
+  // compute unit, of 128 keys at least
+  auto up = [](int64_t x) { return (x + 127) / 128 * 128; };
+  int64_t c = up((int64_t)max_k * units / (8 * kSeqCus));
+  if (c < 512) {
+    c = up((int64_t)max_k * units / kSeqCus);
+    if (c > 512) c = 512;
+    if (c < 128) c = 128;
+  }
   if (c > 4096) c = 4096;
   p.chunk = (int)c;
   p.chunks = (int)((max_k + c - 1) / c);
@@ -41,13 +56,33 @@ FewPlan plan(int docs, int kv_heads, int group, int max_q, int max_k) {
 struct Part {
   float *ml, *o;
 };
-__host__ __device__ inline Part part_of(float *base, const FewPlan &p, int64_t units) {
-  return Part{base, base + ((units * p.chunks * p.rows * 2 + 63) / 64) * 64};
+__host__ __device__ inline Part part_of(void *base, const FewPlan &p, int64_t units) {
+  float *f = static_cast<float *>(base);
+  return Part{f, f + (units * p.chunks * p.rows * 2 + 63) / 64 * 64};
 }
 
-template <class T, int DP, bool CAP, int BIAS>
+// Writes 4 columns of a finished row (sum l at the maximum m, in log 2 units).
+template <class T, bool REST>
+__device__ inline void write_quad(const AttnArgs &a, int row, int head, int d, f32x4 x, float m,
+                                  float l) {
+  const float inv = l > 0.f ? 1.f / l : (l == 0.f ? 0.f : l);   // a NaN sum stays one
+  x *= inv;
+  if (2 * d < a.bytes) {
+    const u32x2 w = {T::pack(x[0], x[1]), T::pack(x[2], x[3])};
+    *reinterpret_cast<u32x2 *>(a.o + (int64_t)row * a.o_row + head * a.o_head + 2 * d) = w;
+    if (REST)
+      *reinterpret_cast<u32x2 *>(a.rest + (int64_t)row * a.rest_row + head * a.rest_head + 2 * d) =
+          u32x2{T::pack(x[0] - T::lo(w[0]), x[1] - T::hi(w[0])),
+                T::pack(x[2] - T::lo(w[1]), x[3] - T::hi(w[1]))};
+  }
+  if (d == 0)
+    a.lse[(int64_t)head * a.q_rows + row] =
+        l == 0.f ? -__builtin_inff() : (m + __builtin_amdgcn_logf(l)) * kLn2;
+}
+
+template <class T, int DP, bool CAP, int BIAS, bool REST>
 __global__ __launch_bounds__(kThreads, 1) void few_kernel(const AttnArgs a, const FewPlan p,
-                                                          float *part) {
+                                                          void *part) {
   constexpr int KS = DP / 16, DT = DP / 32;
   constexpr int kTile = kKeys * DP * 2;
   constexpr int kCopies = 2 * (kTile / 1024);       // copy instructions of a step
@@ -55,7 +90,8 @@ __global__ __launch_bounds__(kThreads, 1) void few_kernel(const AttnArgs a, cons
   extern __shared__ __align__(1024) char lds[];
   __shared__ float ml[4][kRows][2];
   __shared__ int any_dirty;
-  uint8_t *map = reinterpret_cast<uint8_t *>(lds + 16 * kTile);
+  // tiles (then the wavefronts' sums), the group's rows of the table, buckets by distance
+  float *values = reinterpret_cast<float *>(lds + few_tiles(DP));
 
   int id = blockIdx.x;
   const int kvh = id % a.kv_heads;
@@ -104,15 +140,21 @@ __global__ __launch_bounds__(kThreads, 1) void few_kernel(const AttnArgs a, cons
   u32x4 qf[KS];
   load_operand<DP>(a.q + (int64_t)(q0 + i) * a.q_row + head * a.q_head, 0, live ? 0 : 1, 1,
                    a.bytes, lane, qf);
-  int reach = 0, nb = 0;
+  int reach = 0, span = 1, nb = 0;
   float slope2 = 0.f, far = 0.f;
-  if (BIAS == kBiasTable) {   // buckets by distance -reach..reach
+  uint8_t *map = nullptr;
+  if (BIAS == kBiasTable) {   // buckets by distance -span..span
     reach = a.buckets.start[a.buckets.per_side - 1];
-    nb = a.buckets.two_sided ? 2 * a.buckets.per_side : a.buckets.per_side;
+    span = max(reach, 1);     // (the sides differ from distance 1 on)
+    nb = bucket_count(a.buckets);
+    map = reinterpret_cast<uint8_t *>(values + a.group * nb);
     far = T::load(a.table, (int64_t)head * nb + a.buckets.per_side - 1) * kLog2e;
-    if (key_hi + 31 - shift > -reach)
-      for (int d = threadIdx.x; d <= 2 * reach; d += kThreads)
-        map[d] = (uint8_t)bucket_of(a.buckets, d - reach);
+    if (key_hi + 31 - shift > -reach) {
+      for (int d = threadIdx.x; d <= 2 * span; d += kThreads)
+        map[d] = (uint8_t)bucket_of(a.buckets, d - span);
+      for (int d = threadIdx.x; d < a.group * nb; d += kThreads)
+        values[d] = T::load(a.table, (int64_t)kvh * a.group * nb + d) * kLog2e;
+    }
   }
   if (BIAS == kBiasSlope) slope2 = a.slopes[head] * kLog2e;
   ScoreScale sc;
@@ -157,8 +199,7 @@ __global__ __launch_bounds__(kThreads, 1) void few_kernel(const AttnArgs a, cons
 #pragma unroll
         for (int e = 0; e < 16; ++e) {
           const int d = key + 4 * h - pos + 8 * (e >> 2) + (e & 3);
-          const int b = map[min(max(d, -reach), reach) + reach];
-          s[e] += T::load(a.table, (int64_t)head * nb + b) * kLog2e;
+          s[e] += values[g * nb + map[min(max(d, -span), span) + span]];
         }
       }
     }
@@ -204,13 +245,21 @@ __global__ __launch_bounds__(kThreads, 1) void few_kernel(const AttnArgs a, cons
       dirty |= !clean;
     }
 #pragma unroll
-    for (int k = 0; k < 2; ++k)
+    for (int k = 0; k < 2; ++k) {
+      u32x4 rest;   // what the rounding of the probabilities lost
+      if (REST) {
+#pragma unroll
+        for (int w = 0; w < 4; ++w)
+          rest[w] = T::pack(s[8 * k + 2 * w] - T::lo(pr[k][w]), s[8 * k + 2 * w + 1] - T::hi(pr[k][w]));
+      }
 #pragma unroll
       for (int c = 0; c < DT; ++c) {
         u32x4 v = col_operand<DP>(vb, 16 * k, c);
         if (!clean) v = finite_part<T>(v);
         acc[c] = T::mfma(v, pr[k], acc[c]);
+        if (REST) acc[c] = T::mfma(v, rest, acc[c]);
       }
+    }
   }
   l = sum_halves(l);
 
@@ -233,6 +282,8 @@ __global__ __launch_bounds__(kThreads, 1) void few_kernel(const AttnArgs a, cons
   __syncthreads();
   constexpr int kQuads = DP / 4;
   const int d = (threadIdx.x % kQuads) * 4;
+  const int64_t unit = ((int64_t)doc * a.kv_heads + kvh) * p.row_tiles + rt;
+  const Part pt = part_of(part, p, (int64_t)a.docs * a.kv_heads * p.row_tiles);
   for (int q = threadIdx.x / kQuads; q < rows; q += kThreads / kQuads) {
     float mm = ml[0][q][0];
 #pragma unroll
@@ -255,18 +306,9 @@ __global__ __launch_bounds__(kThreads, 1) void few_kernel(const AttnArgs a, cons
           x[e] += nonfinite_sum<T>(vbase, a.v_row, first, min(limit(qi), key_hi), d + e);
     }
     if (n_chunks == 1) {
-      const float inv = ll > 0.f ? 1.f / ll : (ll == 0.f ? 0.f : ll);
-      if (2 * d < a.bytes)
-        *reinterpret_cast<u32x2 *>(a.o + (int64_t)(q0 + qi) * a.o_row + qh * a.o_head + 2 * d) =
-            u32x2{T::pack(x[0] * inv, x[1] * inv), T::pack(x[2] * inv, x[3] * inv)};
-      if (d == 0)
-        a.lse[(int64_t)qh * a.q_rows + q0 + qi] =
-            ll == 0.f ? -__builtin_inff() : (mm + __builtin_amdgcn_logf(ll)) * kLn2;
+      write_quad<T, REST>(a, q0 + qi, qh, d, x, mm, ll);
     } else {
-      const int64_t units = (int64_t)a.docs * a.kv_heads * p.row_tiles;
-      const Part pt = part_of(part, p, units);
-      const int64_t at =
-          ((((int64_t)doc * a.kv_heads + kvh) * p.row_tiles + rt) * p.chunks + chunk) * p.rows + q;
+      const int64_t at = (unit * p.chunks + chunk) * p.rows + q;
       *reinterpret_cast<f32x4 *>(pt.o + at * DP + d) = x;
       if (d == 0) {
         pt.ml[2 * at] = mm;
@@ -276,12 +318,13 @@ __global__ __launch_bounds__(kThreads, 1) void few_kernel(const AttnArgs a, cons
   }
 }
 
-// One block per row: the sums of its ranges, in their order.
-template <class T, int DP>
-__global__ __launch_bounds__(256) void few_join(const AttnArgs a, const FewPlan p, float *part) {
-  constexpr int kQuads = DP / 4, kSlices = 256 / kQuads;
+// One block per row: slices of threads take its ranges in turn, each with a running maximum
+// (so that all loads are under way at once), then join in order.
+template <class T, int DP, bool REST>
+__global__ __launch_bounds__(kThreads) void few_join(const AttnArgs a, const FewPlan p, void *part) {
+  constexpr int kQuads = DP / 4, kSlices = kThreads / kQuads;
   __shared__ f32x4 so[kSlices][kQuads];
-  __shared__ float sm[4];
+  __shared__ float sml[kSlices][2];
   int id = blockIdx.x;
   const int q = id % p.rows;
   id /= p.rows;
@@ -293,75 +336,74 @@ __global__ __launch_bounds__(256) void few_join(const AttnArgs a, const FewPlan 
   const int r = rt * kRows + q;
   if (r >= a.group * lq) return;
   const int lk = max(min(a.ke[doc], a.k_rows) - max(a.kb[doc], 0), 0);
-  const int prefix = (a.causal && a.prefix) ? a.prefix[doc] : 0;
-  const int lim_hi = a.causal ? min(lk, max(lk, prefix)) : lk;
-  const int n = (lim_hi + p.chunk - 1) / p.chunk;
-  if (n <= 1 || n > p.chunks) return;               // written by the first kernel
-  const int i = r % lq, head = kvh * a.group + r / lq;
-  const int64_t units = (int64_t)a.docs * a.kv_heads * p.row_tiles;
-  const Part pt = part_of(part, p, units);
+  const int n = (lk + p.chunk - 1) / p.chunk;   // the last query sees every key
+  if (n <= 1 || n > p.chunks) return;           // written by the first kernel
+  const Part pt = part_of(part, p, (int64_t)a.docs * a.kv_heads * p.row_tiles);
   const int64_t at =
-      ((((int64_t)doc * a.kv_heads + kvh) * p.row_tiles + rt) * p.chunks) * (int64_t)p.rows + q;
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  float mm = -__builtin_inff();
-  for (int c = threadIdx.x; c < n; c += 256) mm = fmaxf(mm, pt.ml[2 * (at + (int64_t)c * p.rows)]);
-#pragma unroll
-  for (int o = 32; o; o >>= 1) mm = fmaxf(mm, __shfl_xor(mm, o));
-  if (lane == 0) sm[wave] = mm;
-  __syncthreads();
-  mm = fmaxf(fmaxf(sm[0], sm[1]), fmaxf(sm[2], sm[3]));
-  const float base = mm == -__builtin_inff() ? 0.f : mm;
+      (((int64_t)doc * a.kv_heads + kvh) * p.row_tiles + rt) * p.chunks * (int64_t)p.rows + q;
   const int quad = threadIdx.x % kQuads, slice = threadIdx.x / kQuads;
+  float mm = -__builtin_inff(), ll = 0.f;
   f32x4 x = {};
-  float ll = 0.f;
+#pragma unroll 4
   for (int c = slice; c < n; c += kSlices) {
     const int64_t k = at + (int64_t)c * p.rows;
-    const float f = fast_exp2(pt.ml[2 * k] - base);
-    ll += f * pt.ml[2 * k + 1];
-    x += f * *reinterpret_cast<const f32x4 *>(pt.o + k * DP + 4 * quad);
+    const float mc = pt.ml[2 * k], lc = pt.ml[2 * k + 1];
+    const f32x4 xc = *reinterpret_cast<const f32x4 *>(pt.o + k * DP + 4 * quad);
+    const float top = fmaxf(mm, mc), base = top == -__builtin_inff() ? 0.f : top;
+    const float f = fast_exp2(mm - base), fc = fast_exp2(mc - base);
+    ll = ll * f + lc * fc;
+    x = x * f + xc * fc;
+    mm = top;
   }
   so[slice][quad] = x;
-  __shared__ float ssum[kSlices];
-  if (quad == 0) ssum[slice] = ll;
+  if (quad == 0) {
+    sml[slice][0] = mm;
+    sml[slice][1] = ll;
+  }
   __syncthreads();
   if (slice) return;
-  ll = 0.f;
-  x = f32x4{};
+  float top = mm;
 #pragma unroll
-  for (int s = 0; s < kSlices; ++s) {
-    ll += ssum[s];
-    x += so[s][quad];
+  for (int s = 1; s < kSlices; ++s) top = fmaxf(top, sml[s][0]);
+  const float base = top == -__builtin_inff() ? 0.f : top;
+  const float f0 = fast_exp2(mm - base);
+  ll *= f0;
+  x *= f0;
+#pragma unroll
+  for (int s = 1; s < kSlices; ++s) {
+    const float f = fast_exp2(sml[s][0] - base);
+    ll += f * sml[s][1];
+    x += f * so[s][quad];
   }
-  const float inv = ll > 0.f ? 1.f / ll : (ll == 0.f ? 0.f : ll);
-  if (8 * quad < a.bytes)
-    *reinterpret_cast<u32x2 *>(a.o + (int64_t)(q0 + i) * a.o_row + head * a.o_head + 8 * quad) =
-        u32x2{T::pack(x[0] * inv, x[1] * inv), T::pack(x[2] * inv, x[3] * inv)};
-  if (quad == 0)
-    a.lse[(int64_t)head * a.q_rows + q0 + i] =
-        ll == 0.f ? -__builtin_inff() : (mm + __builtin_amdgcn_logf(ll)) * kLn2;
+  write_quad<T, REST>(a, q0 + r % lq, kvh * a.group + r / lq, 4 * quad, x, top, ll);
 }
 
-template <class T, int DP, bool CAP, int BIAS>
-hipError_t launch(const AttnArgs &a, float *part, hipStream_t s) {
+template <class T, int DP, bool CAP, int BIAS, bool REST>
+hipError_t launch_form(const AttnArgs &a, void *part, hipStream_t s) {
   static LdsLimit limit;
   const FewPlan p = plan(a.docs, a.kv_heads, a.group, a.max_q, a.max_k);
-  int lds = 16 * kKeys * DP * 2;
-  const int join = 4 * kRows * (DP + 4) * 4;
-  if (lds < join) lds = join;
-  const int most = lds + 2 * kMaxReach + 4;
-  if (BIAS == kBiasTable) lds += 2 * a.buckets.start[a.buckets.per_side - 1] + 4;
-  hipError_t e = limit.set(reinterpret_cast<const void *>(&few_kernel<T, DP, CAP, BIAS>), most);
+  int lds = few_tiles(DP);
+  if (BIAS == kBiasTable)
+    lds += a.group * bucket_count(a.buckets) * 4 + 2 * a.buckets.start[a.buckets.per_side - 1] + 4;
+  hipError_t e = limit.set(reinterpret_cast<const void *>(&few_kernel<T, DP, CAP, BIAS, REST>),
+                           few_tiles(DP) + kMaxValues * 4 + 2 * kMaxReach + 4);
   if (e != hipSuccess) return e;
   const int64_t units = (int64_t)a.docs * a.kv_heads * p.row_tiles;
-  few_kernel<T, DP, CAP, BIAS>
+  few_kernel<T, DP, CAP, BIAS, REST>
       <<<dim3((uint32_t)(units * p.chunks)), kThreads, lds, s>>>(a, p, part);
   if (p.chunks > 1)
-    few_join<T, DP><<<dim3((uint32_t)(units * p.rows)), 256, 0, s>>>(a, p, part);
+    few_join<T, DP, REST><<<dim3((uint32_t)(units * p.rows)), kThreads, 0, s>>>(a, p, part);
   return hipGetLastError();
 }
 
+template <class T, int DP, bool CAP, int BIAS>
+hipError_t launch(const AttnArgs &a, void *part, hipStream_t s) {
+  if (a.rest) return launch_form<T, DP, CAP, BIAS, true>(a, part, s);
+  return launch_form<T, DP, CAP, BIAS, false>(a, part, s);
+}
+
 template <class T, int DP>
-hipError_t by_bias(const AttnArgs &a, float *part, hipStream_t s) {
+hipError_t by_bias(const AttnArgs &a, void *part, hipStream_t s) {
   const int bias = a.table ? kBiasTable : (a.slopes ? kBiasSlope : kBiasNone);
   if (a.cap > 0.f) {
     if (bias == kBiasTable) return launch<T, DP, true, kBiasTable>(a, part, s);
@@ -375,21 +417,24 @@ hipError_t by_bias(const AttnArgs &a, float *part, hipStream_t s) {
 
 }  // namespace
 
-bool attend_use_few(int32_t docs, int32_t kv_heads, int32_t group, int32_t max_q, int32_t max_k) {
-  (void)docs, (void)kv_heads, (void)max_k;
-  return (int64_t)group * max_q <= kRows;
+// Small calls too: while the general form's blocks of 128 queries leave compute units idle,
+// 32 rows per block with the keys split over its wavefronts finish sooner.
+bool attend_use_few(const AttnArgs &a) {
+  if ((int64_t)a.group * bucket_count(a.buckets) > kMaxValues) return false;
+  if ((int64_t)a.group * a.max_q <= kRows) return true;
+  const int64_t x = (int64_t)a.q_rows / 128 + a.docs, y = (int64_t)a.docs * ((a.max_q + 127) / 128);
+  return (x < y ? x : y) * a.heads <= kFewBlocks;
 }
 
-size_t attend_few_bytes(int32_t docs, int32_t kv_heads, int32_t group, int32_t max_q, int32_t max_k,
-                        int32_t dim) {
-  const FewPlan p = plan(docs, kv_heads, group, max_q, max_k);
-  const int64_t units = (int64_t)docs * kv_heads * p.row_tiles;
+size_t attend_few_bytes(const AttnArgs &a) {
+  const FewPlan p = plan(a.docs, a.kv_heads, a.group, a.max_q, a.max_k);
   if (p.chunks == 1) return 0;
-  const int64_t rows = units * p.chunks * p.rows;
-  return (size_t)((rows * 2 + 63) / 64 * 64 + rows * (dim <= 64 ? 64 : 128)) * 4;
+  const int64_t units = (int64_t)a.docs * a.kv_heads * p.row_tiles;
+  const Part pt = part_of(nullptr, p, units);
+  return (size_t)((pt.o - pt.ml) + units * p.chunks * p.rows * (a.bytes <= 128 ? 64 : 128)) * 4;
 }
 
-hipError_t launch_attend_few(const AttnArgs &a, float *part, hipStream_t s) {
+hipError_t launch_attend_few(const AttnArgs &a, void *part, hipStream_t s) {
   if (a.bytes <= 128)
     return a.fp16 ? by_bias<Fp16, 64>(a, part, s) : by_bias<Bf16, 64>(a, part, s);
   return a.fp16 ? by_bias<Fp16, 128>(a, part, s) : by_bias<Bf16, 128>(a, part, s);

@@ -20,7 +20,7 @@ namespace {
 constexpr int kThreads = 256;
 constexpr int kRowBlocks = 512;    // blocks of the row pass, at most
 constexpr float kP16 = 12.f;       // fp16: log2 of the factor of P
-constexpr int kSkew = 32 * 64 + 64;  // floats of a wavefront's skewed values
+constexpr int kSkew = 16 * 64;      // floats of a wavefront's skewed values
 
 // Rows of a step (the tiles that go through LDS while a block's own stay).
 template <int DP>
@@ -41,6 +41,34 @@ __device__ inline float sum_rows(float x) {
   const uint32_t u = __builtin_bit_cast(uint32_t, x);
   const u32x2 a = __builtin_amdgcn_permlane16_swap(u, u, false, false);
   return sum_halves(word_float(a[0]) + word_float(a[1]));
+}
+
+// Adds the four wavefronts' results; true on the one (the first) that has the sum then.
+template <int DT>
+__device__ __forceinline__ bool add_waves(f32x16 *acc, char *lds) {
+  f32x4 *x = reinterpret_cast<f32x4 *>(lds);   // [3][DT][4][64]
+  const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6);
+  __syncthreads();
+  if (wave) {
+#pragma unroll
+    for (int c = 0; c < DT; ++c)
+#pragma unroll
+      for (int g = 0; g < 4; ++g)
+        x[(((wave - 1) * DT + c) * 4 + g) * 64 + lane] =
+            f32x4{acc[c][4 * g], acc[c][4 * g + 1], acc[c][4 * g + 2], acc[c][4 * g + 3]};
+  }
+  __syncthreads();
+  if (wave) return false;
+  for (int w = 0; w < 3; ++w)
+#pragma unroll
+    for (int c = 0; c < DT; ++c)
+#pragma unroll
+      for (int g = 0; g < 4; ++g) {
+        const f32x4 y = x[((w * DT + c) * 4 + g) * 64 + lane];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) acc[c][4 * g + e] += y[e];
+      }
+  return true;
 }
 
 // ------------------------------------------------------------------ rows
@@ -174,18 +202,31 @@ struct PairScale {
 // A lane's key is fixed, its elements are the queries 8 g + 4 h + r of 32: products are
 // Q K^T (queries x keys), their results the operands of dV^T = dO^T P and dK^T = Q^T dZ.
 // K stays in registers and V in LDS: with V in registers too the accumulators would spill.
-template <class T, int DP, bool CAP, int BIAS>
+//
+// NARROW: a block has 32 keys, its wavefronts go over every fourth step of the queries with
+// LDS buffers of their own, and their sums are added at the end.
+template <class T, int DP, bool CAP, int BIAS, bool NARROW>
 __device__ __forceinline__ void grad_kv(const AttnGradArgs &ga, int row_blocks, int id, char *lds,
                                         float *red) {
   constexpr int KS = DP / 16, DT = DP / 32;
-  constexpr int kBQ = GradTiles<DP>::kStep;    // queries of a step
+  constexpr int kBQ = NARROW ? 32 : GradTiles<DP>::kStep;    // queries of a step
   constexpr int kTile = kBQ * DP * 2;
-  constexpr int kBK = 128;                     // keys of a block
+  constexpr int kBK = NARROW ? 32 : 128;       // keys of a block
+  constexpr int kParts = NARROW ? 4 : 1;       // wavefronts (or the block) with own steps
   const AttnArgs &a = ga.f;
-  // [2][Q, dO], V, [2][rows of log-sum and D], table
-  char *vt = lds + 4 * kTile;
-  char *rows_lds = vt + kBK * DP * 2;
-  float *lut = reinterpret_cast<float *>(rows_lds + 2 * kBQ * 8);
+  const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6), h = lane >> 5;
+  const int part = NARROW ? wave : 0;
+  // per part [2][Q, dO]; V; per part [2][rows of log-sum and D]; per part the table
+  char *const tiles = lds + part * 4 * kTile;
+  char *vt = lds + kParts * 4 * kTile;
+  char *rows_lds = vt + kBK * DP * 2 + part * 2 * kBQ * 8;
+  float *lut = reinterpret_cast<float *>(vt + kBK * DP * 2 + kParts * 2 * kBQ * 8);
+  uint8_t *map = nullptr;
+  if (BIAS == kBiasTable) {
+    const int n = lut_size(a.buckets.start[a.buckets.per_side - 1]);
+    map = reinterpret_cast<uint8_t *>(lut + kParts * n);
+    lut += part * n;
+  }
 
   const int kvh = id % a.kv_heads;
   const DocTile t = find_tile<kBK>(a.kb, a.ke, a.docs, a.k_rows, id / a.kv_heads);
@@ -197,8 +238,7 @@ __device__ __forceinline__ void grad_kv(const AttnGradArgs &ga, int row_blocks, 
   const int shift = lk - lq;
   const int j0 = t.tile * kBK;
 
-  const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6), h = lane >> 5;
-  const int key_lo = j0 + 32 * wave, key = key_lo + (lane & 31);
+  const int key_lo = NARROW ? j0 : j0 + 32 * wave, key = key_lo + (lane & 31);
   // queries that see key j: those from first(j) on
   auto first = [&](int j) { return (a.causal && j >= prefix) ? max(j - shift, 0) : 0; };
   const int i_start = first(j0) / kBQ * kBQ;
@@ -210,21 +250,22 @@ __device__ __forceinline__ void grad_kv(const AttnGradArgs &ga, int row_blocks, 
 
   TileReader<DP> rd;
   rd.init(lane);
-  TileCopy<DP, kBQ, 4> qc, dc;
-  qc.init(wave, lane, (int)a.q_row, a.bytes);
-  dc.init(wave, lane, (int)ga.do_row, a.bytes);
+  TileCopy<DP, kBQ, NARROW ? 1 : 4> qc, dc;
+  qc.init(NARROW ? 0 : wave, lane, (int)a.q_row, a.bytes);
+  dc.init(NARROW ? 0 : wave, lane, (int)ga.do_row, a.bytes);
   auto start = [&](int n, int buf) {
     const int head = kvh * a.group + n / steps, i = i_start + n % steps * kBQ;
     const int rows = min(lq - i, kBQ);
     qc.start(row_buffer(a.q + (int64_t)q0 * a.q_row + head * a.q_head, i, rows, a.q_row, a.bytes),
-             lds_address(lds) + buf * 2 * kTile);
+             lds_address(tiles) + buf * 2 * kTile);
     dc.start(row_buffer(ga.dout + (int64_t)q0 * ga.do_row + head * ga.do_head, i, rows, ga.do_row,
                         a.bytes),
-             lds_address(lds) + (buf * 2 + 1) * kTile);
-    if (wave < kBQ / 32)
+             lds_address(tiles) + (buf * 2 + 1) * kTile);
+    const int sixty4 = NARROW ? 0 : wave;
+    if (sixty4 < kBQ / 32)
       copy_words(row_buffer(reinterpret_cast<const char *>(ga.rows) +
                                 ((int64_t)head * a.q_rows + q0) * 8, i, rows, 8, 8),
-                 (wave * 64 + lane) * 4, lds_address(rows_lds) + buf * kBQ * 8 + wave * 256);
+                 (sixty4 * 64 + lane) * 4, lds_address(rows_lds) + buf * kBQ * 8 + sixty4 * 256);
   };
   {
     TileCopy<DP, kBK, 4> vc;
@@ -233,7 +274,7 @@ __device__ __forceinline__ void grad_kv(const AttnGradArgs &ga, int row_blocks, 
                         a.v_row, a.bytes),
              lds_address(vt));
   }
-  if (total > 0) start(0, 0);
+  if (part < total) start(part, 0);
 
   u32x4 kf[KS];
   load_operand<DP>(a.k + (int64_t)t.b0 * a.k_row + kvh * a.k_head, a.k_row, key, lk, a.bytes, lane, kf);
@@ -242,28 +283,42 @@ __device__ __forceinline__ void grad_kv(const AttnGradArgs &ga, int row_blocks, 
   const float p0 = ps.kHalf ? kP16 : 0.f, ds_scale = ps.ds_scale * exp2f(-p0);
   const int reach = BIAS == kBiasTable ? a.buckets.start[a.buckets.per_side - 1] : 0;
 
+  if (BIAS == kBiasTable) fill_map(map, a.buckets, threadIdx.x, kThreads);
+
   f32x16 dk[DT], dv[DT];
 #pragma unroll
   for (int c = 0; c < DT; ++c) dk[c] = dv[c] = f32x16{};
   float slope2 = 0.f;
 
   copies_barrier();
-  for (int n = 0; n < total; ++n) {
-    const int buf = n & 1;
-    if (BIAS != kBiasNone && n % steps == 0) {   // the next head
-      const int head = kvh * a.group + n / steps;
+  int head_now = -1;
+  for (int n = part, buf = 0; n < total; n += kParts, buf ^= 1) {
+    if (BIAS != kBiasNone && n / steps != head_now) {   // the next head
+      head_now = n / steps;
+      const int head = kvh * a.group + head_now;
       if (BIAS == kBiasSlope) slope2 = a.slopes[head] * kLog2e;
       if (BIAS == kBiasTable) {
-        fill_lut<T>(lut, a.buckets, a.table, head, kThreads);
-        __syncthreads();
+        fill_lut<T>(lut, map, a.buckets, a.table, head, NARROW ? lane : threadIdx.x,
+                    NARROW ? 64 : kThreads);
+        if (!NARROW) __syncthreads();
       }
     }
-    if (n + 1 < total) start(n + 1, buf ^ 1);
+    if (NARROW) {   // (the buffer that is filled next was read in the step before)
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+      if (n + kParts < total) {
+        start(n + kParts, buf ^ 1);
+        wait_copies<2 * (kTile / 1024) + 1>();
+      } else {
+        wait_copies<0>();
+      }
+    } else if (n + 1 < total) {
+      start(n + 1, buf ^ 1);
+    }
 #pragma unroll 1
     for (int sub = 0; sub < kBQ; sub += 32) {
       const int i0 = i_start + n % steps * kBQ + sub;
       if (i0 + 32 <= i_wave || i0 >= lq) continue;
-      const uint32_t tile = lds_address(lds) + buf * 2 * kTile;
+      const uint32_t tile = lds_address(tiles) + buf * 2 * kTile;
       const uint32_t qr = rd.at(tile, rd.row), qc0 = rd.at(tile, rd.col);
       const uint32_t vr = rd.at(lds_address(vt), rd.row);
       const char *rows = rows_lds + (buf * kBQ + sub + 4 * h) * 8;
@@ -272,7 +327,7 @@ __device__ __forceinline__ void grad_kv(const AttnGradArgs &ga, int row_blocks, 
       for (int k = 0; k < KS; ++k) s = T::mfma(row_operand<DP>(qr, sub, k), kf[k], s);
 #pragma unroll
       for (int k = 0; k < KS; ++k)
-        dp = T::mfma(row_operand<DP>(qr + kTile, sub, k), row_operand<DP>(vr + 32 * wave * DP * 2, 0, k), dp);
+        dp = T::mfma(row_operand<DP>(qr + kTile, sub, k), row_operand<DP>(vr + (NARROW ? 0 : 32 * wave * DP * 2), 0, k), dp);
       const bool masked = i0 < i_whole || i0 + 32 > lq;
 #pragma unroll
       for (int g = 0; g < 4; ++g) {   // (dP - D) dZ/dS first: the capped products then are done
@@ -341,7 +396,12 @@ __device__ __forceinline__ void grad_kv(const AttnGradArgs &ga, int row_blocks, 
           dk[c] = T::mfma(col_operand<DP>(qc0, sub + 16 * k, c), dr[k], dk[c]);
         }
     }
+    if (!NARROW) copies_barrier();
+  }
+  if (NARROW) {
     copies_barrier();
+    add_waves<DT>(dv, lds);
+    if (!add_waves<DT>(dk, lds)) return;
   }
   const bool ok = key < lk;
   store_row<T, DT>(ga.dv + (int64_t)(t.b0 + key) * ga.dv_row + kvh * ga.dv_head, ok, a.bytes, dv,
@@ -354,24 +414,31 @@ __device__ __forceinline__ void grad_kv(const AttnGradArgs &ga, int row_blocks, 
 // A lane's query is fixed, its elements are the keys, as in the forward kernel.
 //
 // Table gradient: the sums of dS by distance. Beyond the table's reach that is one sum per
-// lane; within, a wavefront writes its 32 x 32 values of dS into LDS skewed, so that a
-// distance is a column, adds up the 63 columns and adds those to its sums by distance.
-template <class T, int DP, bool CAP, int BIAS>
+// lane; within, a wavefront writes its values of dS into LDS skewed, so that a distance is a
+// column, adds up the columns and adds those to its sums by distance (LDS atomics on those
+// took 3.5 times as long).
+//
+// NARROW: a block has 32 queries, its wavefronts go over every fourth step of the keys.
+template <class T, int DP, bool CAP, int BIAS, bool NARROW>
 __device__ __forceinline__ void grad_q(const AttnGradArgs &ga, int row_blocks, int id, char *lds,
                                        float *red) {
   constexpr int KS = DP / 16, DT = DP / 32;
-  constexpr int kBN = GradTiles<DP>::kStep;    // keys of a step
+  constexpr int kBN = NARROW ? 32 : GradTiles<DP>::kStep;    // keys of a step
   constexpr int kTile = kBN * DP * 2;
-  constexpr int kBM = 128;
+  constexpr int kBM = NARROW ? 32 : 128;
+  constexpr int kParts = NARROW ? 4 : 1;
   const AttnArgs &a = ga.f;
-  // [2][K, V], [4] skewed values, biases, [4] sums by distance
-  float *skewed = reinterpret_cast<float *>(lds + 4 * kTile);
+  const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6), h = lane >> 5;
+  const int part = NARROW ? wave : 0;
+  // per part [2][K, V]; [4] skewed values, biases, [4] sums by distance
+  char *const kv_tiles = lds + part * 4 * kTile;
+  float *skewed = reinterpret_cast<float *>(lds + kParts * 4 * kTile);
   float *lut = skewed + 4 * kSkew;
 
   const int kvh = id % a.kv_heads;
   id /= a.kv_heads;
   const int head = kvh * a.group + id % a.group, unit = id / a.group;
-  const int nb = a.buckets.two_sided ? 2 * a.buckets.per_side : a.buckets.per_side;
+  const int nb = bucket_count(a.buckets);
   const DocTile t = find_tile<kBM>(a.qb, a.qe, a.docs, a.q_rows, unit);
   float *tout = nullptr;
   if (BIAS == kBiasTable) tout = ga.tpart + ((int64_t)unit * a.heads + head) * nb;
@@ -387,8 +454,7 @@ __device__ __forceinline__ void grad_q(const AttnGradArgs &ga, int row_blocks, i
   const int tiles = (lq + kBM - 1) / kBM;
   const int i0 = (tiles - 1 - t.tile) * kBM;
 
-  const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6), h = lane >> 5;
-  const int row_lo = i0 + 32 * wave, row = row_lo + (lane & 31);
+  const int row_lo = NARROW ? i0 : i0 + 32 * wave, row = row_lo + (lane & 31);
   const int shift = lk - lq;
   auto limit = [&](int i) { return a.causal ? min(lk, max(i + shift + 1, prefix)) : lk; };
   const bool ok = row < lq;
@@ -401,17 +467,17 @@ __device__ __forceinline__ void grad_q(const AttnGradArgs &ga, int row_blocks, i
   const char *vbase = a.v + (int64_t)k0 * a.v_row + kvh * a.v_head;
   TileReader<DP> rd;
   rd.init(lane);
-  TileCopy<DP, kBN, 4> kc, vc;
-  kc.init(wave, lane, (int)a.k_row, a.bytes);
-  vc.init(wave, lane, (int)a.v_row, a.bytes);
+  TileCopy<DP, kBN, NARROW ? 1 : 4> kc, vc;
+  kc.init(NARROW ? 0 : wave, lane, (int)a.k_row, a.bytes);
+  vc.init(NARROW ? 0 : wave, lane, (int)a.v_row, a.bytes);
   auto start = [&](int tile, int buf) {
     const int n = min(lk - tile * kBN, kBN);
     kc.start(row_buffer(kbase, (int64_t)tile * kBN, n, a.k_row, a.bytes),
-             lds_address(lds) + buf * 2 * kTile);
+             lds_address(kv_tiles) + buf * 2 * kTile);
     vc.start(row_buffer(vbase, (int64_t)tile * kBN, n, a.v_row, a.bytes),
-             lds_address(lds) + (buf * 2 + 1) * kTile);
+             lds_address(kv_tiles) + (buf * 2 + 1) * kTile);
   };
-  if (n_tiles > 0) start(0, 0);
+  if (part < n_tiles) start(part, 0);
 
   u32x4 qf[KS], df[KS];
   load_operand<DP>(a.q + (int64_t)t.b0 * a.q_row + head * a.q_head, a.q_row, row, lq, a.bytes, lane, qf);
@@ -428,7 +494,9 @@ __device__ __forceinline__ void grad_q(const AttnGradArgs &ga, int row_blocks, i
   if (BIAS == kBiasTable) {
     reach = a.buckets.start[a.buckets.per_side - 1];
     const int n = lut_size(reach);
-    fill_lut<T>(lut, a.buckets, a.table, head, kThreads);
+    uint8_t *map = reinterpret_cast<uint8_t *>(lut + 5 * n);
+    fill_map(map, a.buckets, threadIdx.x, kThreads);   // (each thread reads what it wrote)
+    fill_lut<T>(lut, map, a.buckets, a.table, head, threadIdx.x, kThreads);
     hist = lut + n * (1 + wave);
     for (int i = lane; i < n; i += 64) hist[i] = 0.f;
     for (int i = lane; i < kSkew; i += 64) skew[i] = 0.f;
@@ -440,14 +508,23 @@ __device__ __forceinline__ void grad_q(const AttnGradArgs &ga, int row_blocks, i
   for (int c = 0; c < DT; ++c) acc[c] = f32x16{};
 
   copies_barrier();
-  for (int tile = 0; tile < n_tiles; ++tile) {
-    const int buf = tile & 1;
-    if (tile + 1 < n_tiles) start(tile + 1, buf ^ 1);
+  for (int tile = part, buf = 0; tile < n_tiles; tile += kParts, buf ^= 1) {
+    if (NARROW) {   // (as above)
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+      if (tile + kParts < n_tiles) {
+        start(tile + kParts, buf ^ 1);
+        wait_copies<2 * (kTile / 1024)>();
+      } else {
+        wait_copies<0>();
+      }
+    } else if (tile + 1 < n_tiles) {
+      start(tile + 1, buf ^ 1);
+    }
 #pragma unroll 1
     for (int sub = 0; sub < kBN; sub += 32) {
       const int key0 = tile * kBN + sub;
       if (key0 >= lim_hi) break;
-      const uint32_t tile_at = lds_address(lds) + buf * 2 * kTile;
+      const uint32_t tile_at = lds_address(kv_tiles) + buf * 2 * kTile;
       const uint32_t kr = rd.at(tile_at, rd.row), kcol = rd.at(tile_at, rd.col);
       f32x16 s = {}, dp = {};
 #pragma unroll
@@ -478,19 +555,24 @@ __device__ __forceinline__ void grad_q(const AttnGradArgs &ga, int row_blocks, i
         } else if (d_lo >= reach) {
           far_r += sum;
         } else {
-          // value (key k, query q) at [k][k - q + 31]; what lies outside stays 0
+          // 16 keys at a time: value (key k, query q) at [k][k - q + 31]; what lies outside
+          // stays 0
           float *w = skew + 4 * h * 65 + 31 - (lane & 31);
-#pragma unroll
-          for (int e = 0; e < 16; ++e) w[(8 * (e >> 2) + (e & 3)) * 65] = dp[e];
-          const float *r = skew + (lane >> 4) * 8 * 64 + (lane & 15) * 4;
-          f32x4 v = {};
-#pragma unroll
-          for (int k = 0; k < 8; ++k) v += *reinterpret_cast<const f32x4 *>(r + k * 64);
-#pragma unroll
-          for (int k = 0; k < 4; ++k) v[k] = sum_rows(v[k]);
+          const float *r = skew + (lane >> 4) * 4 * 64 + (lane & 15) * 4;
           const int g = lane >> 4, d = (lane & 15) * 4 + g;   // this lane's column
-          const float x = g == 0 ? v[0] : (g == 1 ? v[1] : (g == 2 ? v[2] : v[3]));
-          if (d < 63) hist[d_lo + d + reach + kLutPad] += x;
+          float *to = hist + d_lo + d + reach + kLutPad;
+#pragma unroll
+          for (int k16 = 0; k16 < 2; ++k16) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) w[(8 * (e >> 2) + (e & 3)) * 65] = dp[8 * k16 + e];
+            f32x4 v = {};
+#pragma unroll
+            for (int k = 0; k < 4; ++k) v += *reinterpret_cast<const f32x4 *>(r + k * 64);
+#pragma unroll
+            for (int k = 0; k < 4; ++k) v[k] = sum_rows(v[k]);
+            const float x = g == 0 ? v[0] : (g == 1 ? v[1] : (g == 2 ? v[2] : v[3]));
+            if (d < 47) to[16 * k16] += x;
+          }
         }
       }
 #pragma unroll
@@ -510,10 +592,16 @@ __device__ __forceinline__ void grad_q(const AttnGradArgs &ga, int row_blocks, i
         for (int c = 0; c < DT; ++c)
           acc[c] = T::mfma(col_operand<DP>(kcol, sub + 16 * k, c), dr[k], acc[c]);
     }
-    copies_barrier();
+    if (!NARROW) copies_barrier();
   }
-  store_row<T, DT>(ga.dq + (int64_t)(t.b0 + row) * ga.dq_row + head * ga.dq_head, ok, a.bytes, acc,
-                   a.scale * ldexpf(1.f, -ps.ds0), lane);
+  bool writes = true;
+  if (NARROW) {
+    copies_barrier();
+    writes = add_waves<DT>(acc, lds);
+  }
+  if (writes)
+    store_row<T, DT>(ga.dq + (int64_t)(t.b0 + row) * ga.dq_row + head * ga.dq_head, ok, a.bytes,
+                     acc, a.scale * ldexpf(1.f, -ps.ds0), lane);
 
   if (BIAS == kBiasTable) {
 #pragma unroll
@@ -553,15 +641,15 @@ __device__ __forceinline__ void grad_q(const AttnGradArgs &ga, int row_blocks, i
 }
 
 // Both in one launch, the longer-running blocks of dK and dV first.
-template <class T, int DP, bool CAP, int BIAS>
-__global__ __launch_bounds__(kThreads, 2) void grad_pairs(const AttnGradArgs ga, int row_blocks,
+template <class T, int DP, bool CAP, int BIAS, bool NARROW>
+__global__ __launch_bounds__(kThreads, NARROW && DP == 128 ? 1 : 2) void grad_pairs(const AttnGradArgs ga, int row_blocks,
                                                           int kv_blocks) {
   extern __shared__ __align__(1024) char lds[];
   __shared__ float red[8];
   if ((int)blockIdx.x < kv_blocks)
-    grad_kv<T, DP, CAP, BIAS>(ga, row_blocks, blockIdx.x, lds, red);
+    grad_kv<T, DP, CAP, BIAS, NARROW>(ga, row_blocks, blockIdx.x, lds, red);
   else
-    grad_q<T, DP, CAP, BIAS>(ga, row_blocks, blockIdx.x - kv_blocks, lds, red);
+    grad_q<T, DP, CAP, BIAS, NARROW>(ga, row_blocks, blockIdx.x - kv_blocks, lds, red);
 }
 
 // dtable[head][b]: the tiles' partial sums; 64 of them per lane group in turn, then joined.
@@ -586,31 +674,55 @@ int64_t tile_bound(int64_t rows, int64_t docs, int64_t longest, int tile) {
   return x < y ? x : y;
 }
 
-template <class T, int DP, bool CAP, int BIAS>
-hipError_t launch(const AttnGradArgs &a, int row_blocks, hipStream_t s) {
+// LDS of a block; lut: bytes of a head's table of biases, 0 without, and of the map to it.
+constexpr int pair_bytes(int dp, bool narrow, int lut, int map) {
+  const int step = narrow || dp == 128 ? 32 : 64, parts = narrow ? 4 : 1;
+  const int tiles = parts * 4 * step * dp * 2;
+  const int kv = tiles + (narrow ? 32 : 128) * dp * 2 + parts * (2 * step * 8 + lut) + map;
+  const int q = tiles + (lut ? 4 * kSkew * 4 + 5 * lut + map : 0);
+  return kv > q ? kv : q;
+}
+
+// The narrow form's tiles where the wide one's blocks would leave compute units idle, if
+// the table leaves room in LDS.
+constexpr int kNarrowBlocks = 256;
+int pair_bytes(const AttnArgs &f, bool narrow) {
+  const int dp = f.bytes <= 128 ? 64 : 128;
+  if (f.buckets.per_side == 0) return pair_bytes(dp, narrow, 0, 0);
+  const int reach = f.buckets.start[f.buckets.per_side - 1];
+  return pair_bytes(dp, narrow, lut_size(reach) * 4, map_bytes(reach));
+}
+int tile_rows(const AttnArgs &f) {
+  const int64_t wide = tile_bound(f.k_rows, f.docs, f.max_k, 128) * f.kv_heads +
+                       tile_bound(f.q_rows, f.docs, f.max_q, 128) * f.heads;
+  return wide <= kNarrowBlocks && pair_bytes(f, true) <= kLdsBytes - 1024 ? 32 : 128;
+}
+
+template <class T, int DP, bool CAP, int BIAS, bool NARROW>
+hipError_t launch_form(const AttnGradArgs &a, int row_blocks, hipStream_t s) {
   static LdsLimit limit;
-  constexpr int kTiles = 4 * GradTiles<DP>::kStep * DP * 2;
-  constexpr int kKv = kTiles + 128 * DP * 2 + 2 * GradTiles<DP>::kStep * 8;
-  constexpr int kQ = kTiles + (BIAS == kBiasTable ? 4 * kSkew * 4 : 0);
-  auto bytes = [](int lut) {
-    const int x = kKv + lut, y = kQ + 5 * lut;
-    return x > y ? x : y;
-  };
-  const int lut = BIAS == kBiasTable ? lut_size(a.f.buckets.start[a.f.buckets.per_side - 1]) * 4 : 0;
-  hipError_t e = limit.set(reinterpret_cast<const void *>(&grad_pairs<T, DP, CAP, BIAS>),
-                           bytes(BIAS == kBiasTable ? lut_size(kMaxReach) * 4 : 0));
+  constexpr int kTile = NARROW ? 32 : 128;
+  const int lds = pair_bytes(a.f, NARROW);
+  hipError_t e = limit.set(reinterpret_cast<const void *>(&grad_pairs<T, DP, CAP, BIAS, NARROW>),
+                           kLdsBytes - 1024);   // (the rest for what is static)
   if (e != hipSuccess) return e;
-  const int64_t kb = tile_bound(a.f.k_rows, a.f.docs, a.f.max_k, 128) * a.f.kv_heads;
-  const int64_t units = tile_bound(a.f.q_rows, a.f.docs, a.f.max_q, 128);
+  const int64_t kb = tile_bound(a.f.k_rows, a.f.docs, a.f.max_k, kTile) * a.f.kv_heads;
+  const int64_t units = tile_bound(a.f.q_rows, a.f.docs, a.f.max_q, kTile);
   const int64_t blocks = kb + units * a.f.heads;
   if (blocks > 0)
-    grad_pairs<T, DP, CAP, BIAS>
-        <<<dim3((uint32_t)blocks), kThreads, bytes(lut), s>>>(a, row_blocks, (int)kb);
+    grad_pairs<T, DP, CAP, BIAS, NARROW>
+        <<<dim3((uint32_t)blocks), kThreads, lds, s>>>(a, row_blocks, (int)kb);
   if (BIAS == kBiasTable) {
-    const int nb = (a.f.buckets.two_sided ? 2 : 1) * a.f.buckets.per_side;
+    const int nb = bucket_count(a.f.buckets);
     grad_table<T><<<dim3((uint32_t)(a.f.heads * nb)), 256, 0, s>>>(a, (int)units, nb);
   }
   return hipGetLastError();
+}
+
+template <class T, int DP, bool CAP, int BIAS>
+hipError_t launch(const AttnGradArgs &a, int row_blocks, hipStream_t s) {
+  if (tile_rows(a.f) == 32) return launch_form<T, DP, CAP, BIAS, true>(a, row_blocks, s);
+  return launch_form<T, DP, CAP, BIAS, false>(a, row_blocks, s);
 }
 
 template <class T, int DP>
@@ -628,11 +740,12 @@ hipError_t by_bias(const AttnGradArgs &a, int row_blocks, hipStream_t s) {
 
 }  // namespace
 
-size_t attend_grad_bytes(int32_t q_rows, int32_t docs, int32_t heads, int32_t buckets, bool fp16) {
+size_t attend_grad_bytes(const AttnArgs &f) {
   auto up = [](int64_t n) { return (n + 63) / 64 * 64; };
-  int64_t n = up(2 * (int64_t)q_rows * heads);
-  if (fp16) n += 2 * kRowBlocks;
-  if (buckets) n += up(((int64_t)q_rows / 128 + docs) * heads * buckets);
+  int64_t n = up(2 * (int64_t)f.q_rows * f.heads);
+  if (f.fp16) n += 2 * kRowBlocks;
+  const int nb = bucket_count(f.buckets);
+  n += up(tile_bound(f.q_rows, f.docs, f.max_q, tile_rows(f)) * f.heads * nb);
   return (size_t)n * 4;
 }
 

@@ -18,6 +18,7 @@ namespace {
 
 constexpr int kThreads = 256;
 constexpr int kList = 2048;        // candidates for the alternatives
+constexpr int kOwners = 512;       // groups of entries that may hold candidates
 constexpr int kWaveWidth = 1024;   // widest row of the one-wavefront form
 constexpr float kLowest = -3.4028234663852886e38f;
 
@@ -200,31 +201,41 @@ struct TopShared {
   uint64_t group[kThreads];
   uint64_t list[kList];
   uint64_t best[4];
-  int owners[kThreads];
+  int owners[kOwners];
   int n_owners, n_list;
 };
 
-// The k-th largest of the block's keys of groups of 256 / G threads (0 if fewer than k).
+// The k-th largest of the block's keys of groups of 256 / G threads (0 if fewer than k);
+// nonzero keys are distinct. With 64 groups one wavefront compares them from its registers.
 __device__ inline uint64_t bound_from_below(TopShared &sh, uint64_t mine, int k) {
-  uint64_t g = mine;
-  const int groups = k <= 32 ? 64 : 256;
-  if (groups == 64) {
-    g = max64(g, shfl_xor64(g, 1));
-    g = max64(g, shfl_xor64(g, 2));
-  }
-  const int per = kThreads / groups;
-  if (threadIdx.x % per == 0) sh.group[threadIdx.x / per] = g;
   if (threadIdx.x == 0) {
     sh.n_owners = sh.n_list = 0;
     sh.best[0] = 0;
   }
-  __syncthreads();
-  if ((int)threadIdx.x < groups) {
-    const uint64_t own = sh.group[threadIdx.x];
+  if (k <= 32) {
+    uint64_t g = max64(mine, shfl_xor64(mine, 1));
+    g = max64(g, shfl_xor64(g, 2));
+    if (threadIdx.x % 4 == 0) sh.group[threadIdx.x / 4] = g;
+    __syncthreads();
+    if (threadIdx.x < 64) {
+      const uint64_t own = sh.group[threadIdx.x];
+      const uint32_t lo = (uint32_t)own, hi = (uint32_t)(own >> 32);
+      int rank = 0;
+#pragma unroll
+      for (int i = 0; i < 64; ++i) {
+        const uint64_t other = (uint64_t)__builtin_amdgcn_readlane(hi, i) << 32 |
+                               (uint32_t)__builtin_amdgcn_readlane(lo, i);
+        rank += other > own ? 1 : 0;
+      }
+      if (own && rank == k - 1) sh.best[0] = own;
+    }
+  } else {
+    sh.group[threadIdx.x] = mine;
+    __syncthreads();
     int rank = 0;
-    for (int i = 0; i < groups; ++i) rank += sh.group[i] > own ? 1 : 0;
-    // (nonzero keys are distinct)
-    if (own && rank == k - 1) sh.best[0] = own;
+#pragma unroll 8
+    for (int i = 0; i < kThreads; ++i) rank += sh.group[i] > mine ? 1 : 0;
+    if (mine && rank == k - 1) sh.best[0] = mine;
   }
   __syncthreads();
   return sh.best[0];
@@ -237,26 +248,56 @@ __device__ inline void offer(TopShared &sh, uint64_t key, uint64_t bound) {
   }
 }
 
-// Calls out(k, key) for the k best of the listed keys, in order.
+// Calls out(k, key) for the k best of the listed keys, in order (the list's own order, which
+// depends on the wavefronts' timing, does not matter).
 template <class Out>
 __device__ inline void rank_list(TopShared &sh, int n, int k, Out out) {
   for (int i = threadIdx.x; i < n; i += kThreads) {
     const uint64_t own = sh.list[i];
     int rank = 0;
+#pragma unroll 4
     for (int j = 0; j < n; ++j) rank += sh.list[j] > own ? 1 : 0;
     if (rank < k) out(rank, own);
   }
   for (int r = n + threadIdx.x; r < k; r += kThreads) out(r, (uint64_t)0);
 }
 
-// ------------------------------------------------------------------ long rows
-// A block's range [lo, hi) of a row: sums and the k best keys.
+// More entries above the bound than the list holds (possible where many of the best fall on
+// few threads): one pass over the entries [0, n) at p per alternative.
 template <int DT, class Out>
-__device__ inline Sums range_pass(TopShared &sh, const char *row, int64_t lo, int64_t hi, float c2,
-                                  int k, Out out) {
+__device__ inline void by_passes(TopShared &sh, const char *p, int64_t n, int k, Out out) {
+  constexpr int kVec = Elem<DT>::kVec;
+  const int64_t nv = (n + kVec - 1) / kVec;
+  uint64_t last = ~0ull;
+  for (int r = 0; r < k; ++r) {
+    uint64_t b = 0;
+    for (int64_t w = threadIdx.x; w < nv; w += kThreads) {
+      float x[kVec];
+      load_some<DT>(p, w, n, __builtin_nanf(""), x);
+#pragma unroll
+      for (int i = 0; i < kVec; ++i) {
+        const uint64_t key = key_of(x[i], w * kVec + i);
+        if (key < last) b = max64(b, key);
+      }
+    }
+#pragma unroll
+    for (int o = 32; o; o >>= 1) b = max64(b, shfl_xor64(b, o));
+    if ((threadIdx.x & 63) == 0) sh.best[threadIdx.x >> 6] = b;
+    __syncthreads();
+    last = max64(max64(sh.best[0], sh.best[1]), max64(sh.best[2], sh.best[3]));
+    __syncthreads();
+    if (threadIdx.x == 0) out(r, last);
+  }
+}
+
+// ------------------------------------------------------------------ long rows
+// A thread's share of a block's range [0, n) at p (index `first` of the row on): its sums, and
+// with KEYS the key of its largest entry.
+template <int DT, bool KEYS>
+__device__ inline Sums range_pass(const char *p, int64_t first, int64_t n, float c2,
+                                  uint64_t *key) {
   constexpr int kVec = Elem<DT>::kVec, kUnroll = 4;
-  const char *p = row + lo * Elem<DT>::kSize;
-  const int64_t n = hi - lo, nv = (n + kVec - 1) / kVec;
+  const int64_t nv = (n + kVec - 1) / kVec;
   const float inf = __builtin_inff();
   Sums s{kLowest, 0.f, 0.f};
   float best = -inf;                    // largest entry of this thread,
@@ -277,7 +318,7 @@ __device__ inline Sums range_pass(TopShared &sh, const char *row, int64_t lo, in
       for (int i = 1; i < kVec; ++i) top[u] = fmaxf(top[u], x[u][i]);
       if (top[u] > best) {
         best = top[u];
-        best_v = v0 + u * kThreads;
+        if (KEYS) best_v = v0 + u * kThreads;
       }
     }
     raise(s, fmaxf(s.m, best), c2);
@@ -290,54 +331,13 @@ __device__ inline Sums range_pass(TopShared &sh, const char *row, int64_t lo, in
   for (; (v + (kUnroll - 1) * kThreads + 1) * kVec <= n; v += kUnroll * kThreads)
     batch(v, std::true_type{});
   for (; v < nv; v += kUnroll * kThreads) batch(v, std::false_type{});
-
-  if (k > 0) {
-    uint64_t mine = 0;
+  if (KEYS) {
+    *key = 0;
     if (best_v < nv) {
       float x[kVec];
       load_some<DT>(p, best_v, n, __builtin_nanf(""), x);
 #pragma unroll
-      for (int i = 0; i < kVec; ++i) mine = max64(mine, key_of(x[i], lo + best_v * kVec + i));
-    }
-    const uint64_t bound = bound_from_below(sh, mine, k);
-    if (mine && mine >= bound) sh.owners[atomicAdd(&sh.n_owners, 1)] = threadIdx.x;
-    __syncthreads();
-    // a wavefront looks through one such thread's vectors at a time
-    const int lane = threadIdx.x & 63;
-    for (int o = threadIdx.x >> 6; o < sh.n_owners; o += 4)
-      for (int64_t w = sh.owners[o] + (int64_t)lane * kThreads; w < nv; w += 64 * kThreads) {
-        float x[kVec];
-        load_some<DT>(p, w, n, __builtin_nanf(""), x);
-#pragma unroll
-        for (int i = 0; i < kVec; ++i) offer(sh, key_of(x[i], lo + w * kVec + i), bound);
-      }
-    __syncthreads();
-    const int listed = sh.n_list;
-    if (listed <= kList) {
-      rank_list(sh, listed, k, out);
-    } else {
-      // more entries above the bound than the list holds (possible where equal entries
-      // fall on few threads): one pass over the range per alternative
-      uint64_t last = ~0ull;
-      for (int r = 0; r < k; ++r) {
-        uint64_t b = 0;
-        for (int64_t w = threadIdx.x; w < nv; w += kThreads) {
-          float x[kVec];
-          load_some<DT>(p, w, n, __builtin_nanf(""), x);
-#pragma unroll
-          for (int i = 0; i < kVec; ++i) {
-            const uint64_t key = key_of(x[i], lo + w * kVec + i);
-            if (key < last) b = max64(b, key);
-          }
-        }
-#pragma unroll
-        for (int o = 32; o; o >>= 1) b = max64(b, shfl_xor64(b, o));
-        if (lane == 0) sh.best[threadIdx.x >> 6] = b;
-        __syncthreads();
-        last = max64(max64(sh.best[0], sh.best[1]), max64(sh.best[2], sh.best[3]));
-        __syncthreads();
-        if (threadIdx.x == 0) out(r, last);
-      }
+      for (int i = 0; i < kVec; ++i) *key = max64(*key, key_of(x[i], first + best_v * kVec + i));
     }
   }
   return s;
@@ -373,21 +373,39 @@ __device__ inline void write_row(const LogprobArgs &a, int64_t row, const Sums &
   if (a.lse) a.lse[row] = r.lse;
 }
 
-template <int DT>
+template <int DT, bool KEYS>
 __global__ __launch_bounds__(kThreads) void logprob_row(const LogprobArgs a) {
-  __shared__ TopShared sh;
-  __shared__ uint64_t keys[kMaxTop];
+  constexpr int kVec = Elem<DT>::kVec;
   __shared__ float red[4][3];
   const int64_t row = blockIdx.x;
   const char *p = static_cast<const char *>(a.x) + row * a.row * Elem<DT>::kSize;
   const float c2 = a.scale * kLog2e;
-  Sums s = range_pass<DT>(sh, p, 0, a.width, c2, a.top, [&](int r, uint64_t k) { keys[r] = k; });
-  s = block_sums(s, c2, red);   // (its barrier also covers keys)
+  uint64_t mine = 0;
+  const Sums s = block_sums(range_pass<DT, KEYS>(p, 0, a.width, c2, &mine), c2, red);
   if (threadIdx.x == 0) write_row<DT>(a, row, s, p);
-  for (int r = threadIdx.x; r < a.top; r += kThreads) {
-    a.top_logp[row * a.top + r] = alt_logp(s, a.scale, keys[r]);
-    a.top_id[row * a.top + r] = keys[r] ? key_index(keys[r]) : -1;
-  }
+  if (!KEYS) return;
+  __shared__ TopShared sh;
+  const uint64_t bound = bound_from_below(sh, mine, a.top);
+  if (mine && mine >= bound) sh.owners[atomicAdd(&sh.n_owners, 1)] = threadIdx.x;
+  __syncthreads();
+  // a wavefront looks through one such thread's vectors at a time
+  const int64_t nv = (a.width + kVec - 1) / kVec;
+  for (int o = threadIdx.x >> 6; o < sh.n_owners; o += 4)
+    for (int64_t w = sh.owners[o] + (int64_t)(threadIdx.x & 63) * kThreads; w < nv;
+         w += 64 * kThreads) {
+      float x[kVec];
+      load_some<DT>(p, w, a.width, __builtin_nanf(""), x);
+#pragma unroll
+      for (int i = 0; i < kVec; ++i) offer(sh, key_of(x[i], w * kVec + i), bound);
+    }
+  __syncthreads();
+  auto out = [&](int r, uint64_t k) {
+    a.top_logp[row * a.top + r] = alt_logp(s, a.scale, k);
+    a.top_id[row * a.top + r] = k ? key_index(k) : -1;
+  };
+  const int n = sh.n_list;
+  if (n <= kList) rank_list(sh, n, a.top, out);
+  else by_passes<DT>(sh, p, a.width, a.top, out);
 }
 
 // ------------------------------------------------------------------ rows shared by blocks
@@ -395,67 +413,112 @@ struct SplitPlan {
   int parts;       // blocks of a row
   int64_t chunk;   // entries of a block
 };
-SplitPlan split_plan(int32_t rows, int32_t width, int32_t top) {
+SplitPlan split_plan(int32_t rows, int32_t width) {
   SplitPlan p{1, width};
   // one block per row where that fills the device, or the rows are short
   if (rows >= 2 * kSeqCus || width <= 8192) return p;
   int64_t parts = (4 * (int64_t)kSeqCus + rows - 1) / rows;
   const int64_t most = width / 2048;            // (a vector or two per thread)
   if (parts > most) parts = most;
-  if (top > 0 && parts > kList / top) parts = kList / top;
   if (parts < 2) return p;
   p.chunk = ((width + parts - 1) / parts + 63) / 64 * 64;
   p.parts = (int)((width + p.chunk - 1) / p.chunk);
   return p;
 }
 
-template <int DT>
+// Every block leaves its range's sums and the keys of its 64 groups of 4 threads; a second
+// kernel joins them, one block per row.
+struct PartSpace {
+  uint64_t *keys;    // [rows][parts][64]
+  float *sums;       // [rows][parts][4]
+};
+__host__ __device__ inline PartSpace part_space(void *ws, int64_t rows, int parts, bool keys) {
+  PartSpace s;
+  s.keys = static_cast<uint64_t *>(ws);
+  s.sums = reinterpret_cast<float *>(s.keys + (keys ? rows * parts * 64 : 0));
+  return s;
+}
+
+template <int DT, bool KEYS>
 __global__ __launch_bounds__(kThreads) void logprob_part(const LogprobArgs a, SplitPlan sp,
-                                                         float *sums, uint64_t *keys) {
-  __shared__ TopShared sh;
+                                                         void *ws) {
   __shared__ float red[4][3];
   const int64_t row = blockIdx.x / sp.parts;
   const int part = blockIdx.x % sp.parts;
+  const PartSpace sc = part_space(ws, a.rows, sp.parts, KEYS);
   const char *p = static_cast<const char *>(a.x) + row * a.row * Elem<DT>::kSize;
   const float c2 = a.scale * kLog2e;
   const int64_t lo = part * sp.chunk, hi = lo + sp.chunk < a.width ? lo + sp.chunk : a.width;
-  uint64_t *out = keys + (int64_t)blockIdx.x * a.top;
-  Sums s = range_pass<DT>(sh, p, lo, hi, c2, a.top, [&](int r, uint64_t k) { out[r] = k; });
-  s = block_sums(s, c2, red);
-  if (threadIdx.x == 0) {
-    sums[3 * (int64_t)blockIdx.x] = s.m;
-    sums[3 * (int64_t)blockIdx.x + 1] = s.a;
-    sums[3 * (int64_t)blockIdx.x + 2] = s.b;
+  uint64_t mine = 0;
+  Sums s = range_pass<DT, KEYS>(p + lo * Elem<DT>::kSize, lo, hi - lo, c2, &mine);
+  if (KEYS) {
+    mine = max64(mine, shfl_xor64(mine, 1));
+    mine = max64(mine, shfl_xor64(mine, 2));
+    if (threadIdx.x % 4 == 0) sc.keys[(int64_t)blockIdx.x * 64 + threadIdx.x / 4] = mine;
   }
+  s = block_sums(s, c2, red);
+  if (threadIdx.x == 0)
+    *reinterpret_cast<f32x4 *>(sc.sums + 4 * (int64_t)blockIdx.x) = f32x4{s.m, s.a, s.b, 0.f};
 }
 
-template <int DT>
+template <int DT, bool KEYS>
 __global__ __launch_bounds__(kThreads) void logprob_join(const LogprobArgs a, SplitPlan sp,
-                                                         const float *sums, const uint64_t *keys) {
-  __shared__ TopShared sh;
+                                                         void *ws) {
+  constexpr int kVec = Elem<DT>::kVec;
   __shared__ float red[4][3];
   const int64_t row = blockIdx.x;
+  const PartSpace sc = part_space(ws, a.rows, sp.parts, KEYS);
   const char *p = static_cast<const char *>(a.x) + row * a.row * Elem<DT>::kSize;
   const float c2 = a.scale * kLog2e;
+  uint64_t mine = 0;
+  const uint64_t *kr = sc.keys + row * sp.parts * 64;
+  const int n = sp.parts * 64;
+  if (KEYS) {
+#pragma unroll 4
+    for (int i = threadIdx.x; i < n; i += kThreads) mine = max64(mine, kr[i]);
+  }
   Sums s{kLowest, 0.f, 0.f};
   for (int i = threadIdx.x; i < sp.parts; i += kThreads) {
-    const float *q = sums + 3 * (row * sp.parts + i);
+    const f32x4 q = *reinterpret_cast<const f32x4 *>(sc.sums + 4 * (row * sp.parts + i));
     s = joined(s, Sums{q[0], q[1], q[2]}, c2);
   }
   s = block_sums(s, c2, red);
   if (threadIdx.x == 0) write_row<DT>(a, row, s, p);
-  if (a.top == 0) return;
-  const uint64_t *kr = keys + row * sp.parts * a.top;
-  const int n = sp.parts * a.top;       // at most kList
-  uint64_t mine = 0;
-  for (int i = threadIdx.x; i < n; i += kThreads) mine = max64(mine, kr[i]);
+  if (!KEYS) return;
+  __shared__ TopShared sh;
   const uint64_t bound = bound_from_below(sh, mine, a.top);
-  for (int i = threadIdx.x; i < n; i += kThreads) offer(sh, kr[i], bound);
+  for (int i = threadIdx.x; i < n; i += kThreads) {
+    const uint64_t k = kr[i];
+    if (k && k >= bound) {
+      const int at = atomicAdd(&sh.n_owners, 1);
+      if (at < kOwners) sh.owners[at] = i;
+    }
+  }
   __syncthreads();
-  rank_list(sh, sh.n_list, a.top, [&](int r, uint64_t k) {
+  auto out = [&](int r, uint64_t k) {
     a.top_logp[row * a.top + r] = alt_logp(s, a.scale, k);
     a.top_id[row * a.top + r] = k ? key_index(k) : -1;
-  });
+  };
+  if (sh.n_owners <= kOwners) {
+    // 4 vectors side by side every 256 of the group's block
+    const int turns = (int)((sp.chunk / kVec + kThreads - 1) / kThreads), items = sh.n_owners * turns * 4;
+    for (int i = threadIdx.x; i < items; i += kThreads) {
+      const int g = sh.owners[i / (turns * 4)];
+      const int64_t from = (g / 64) * sp.chunk, v = (int64_t)(i / 4 % turns) * kThreads + g % 64 * 4 + i % 4;
+      const int64_t len = from + sp.chunk < a.width ? sp.chunk : a.width - from;
+      float x[kVec];
+      load_some<DT>(p + from * Elem<DT>::kSize, v, len, __builtin_nanf(""), x);
+#pragma unroll
+      for (int e = 0; e < kVec; ++e) offer(sh, key_of(x[e], from + v * kVec + e), bound);
+    }
+    __syncthreads();
+    if (sh.n_list <= kList) {
+      rank_list(sh, sh.n_list, a.top, out);
+      return;
+    }
+  }
+  __syncthreads();
+  by_passes<DT>(sh, p, a.width, a.top, out);
 }
 
 // ------------------------------------------------------------------ gradient
@@ -537,16 +600,21 @@ hipError_t forward(const LogprobArgs &a, void *ws, hipStream_t s) {
     else logprob_wave<DT, kWaveWidth / (64 * kVec)><<<grid, kThreads, 0, s>>>(a);
     return hipGetLastError();
   }
-  const SplitPlan sp = split_plan(a.rows, a.width, a.top);
+  const SplitPlan sp = split_plan(a.rows, a.width);
+  const dim3 grid((uint32_t)((int64_t)a.rows * sp.parts));
   if (sp.parts == 1) {
-    logprob_row<DT><<<dim3((uint32_t)a.rows), kThreads, 0, s>>>(a);
-    return hipGetLastError();
+    if (a.top) logprob_row<DT, true><<<grid, kThreads, 0, s>>>(a);
+    else logprob_row<DT, false><<<grid, kThreads, 0, s>>>(a);
+  } else {
+    const dim3 rows((uint32_t)a.rows);
+    if (a.top) {
+      logprob_part<DT, true><<<grid, kThreads, 0, s>>>(a, sp, ws);
+      logprob_join<DT, true><<<rows, kThreads, 0, s>>>(a, sp, ws);
+    } else {
+      logprob_part<DT, false><<<grid, kThreads, 0, s>>>(a, sp, ws);
+      logprob_join<DT, false><<<rows, kThreads, 0, s>>>(a, sp, ws);
+    }
   }
-  const int64_t n = (int64_t)a.rows * sp.parts;
-  uint64_t *keys = static_cast<uint64_t *>(ws);
-  float *sums = reinterpret_cast<float *>(keys + n * a.top);
-  logprob_part<DT><<<dim3((uint32_t)n), kThreads, 0, s>>>(a, sp, sums, keys);
-  logprob_join<DT><<<dim3((uint32_t)a.rows), kThreads, 0, s>>>(a, sp, sums, keys);
   return hipGetLastError();
 }
 
@@ -573,8 +641,9 @@ hipError_t gradient(const LogprobArgs &a, hipStream_t s) {
 
 size_t logprob_bytes(int32_t rows, int32_t width, int32_t top) {
   if (width <= kWaveWidth) return 0;
-  const SplitPlan sp = split_plan(rows, width, top);
-  return sp.parts == 1 ? 0 : (size_t)rows * sp.parts * ((size_t)top * 8 + 12);
+  const SplitPlan sp = split_plan(rows, width);
+  if (sp.parts == 1) return 0;
+  return (size_t)rows * sp.parts * ((top > 0 ? 64 * 8 : 0) + 16);
 }
 
 hipError_t launch_logprob(const LogprobArgs &a, void *ws, hipStream_t s) {

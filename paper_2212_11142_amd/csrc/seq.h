@@ -17,8 +17,9 @@ constexpr int kSeqCus = 256;          // compute units of an MI355X: what splits
 constexpr int kMaxBuckets = 64;       // buckets of one side
 constexpr int kMaxReach = 1024;       // first distance of the last bucket
 constexpr int kMaxTop = 128;          // alternatives of a row
+constexpr int kLdsBytes = 160 * 1024; // of a compute unit
 
-// First distance of each bucket of a side (start[0] = 0, ascending).
+// First distance of each bucket of a side (start[0] = 0, ascending; INT32_MAX past the last).
 struct BucketMap {
   int32_t per_side;
   int32_t two_sided;
@@ -58,12 +59,11 @@ struct AttnGradArgs {
 
 hipError_t launch_attend(const AttnArgs &a, hipStream_t s);
 // few query rows: key ranges split over blocks; part: attend_few_bytes() of workspace
-size_t attend_few_bytes(int32_t docs, int32_t kv_heads, int32_t group, int32_t max_q, int32_t max_k,
-                        int32_t dim);
-bool attend_use_few(int32_t docs, int32_t kv_heads, int32_t group, int32_t max_q, int32_t max_k);
-hipError_t launch_attend_few(const AttnArgs &a, float *part, hipStream_t s);
+size_t attend_few_bytes(const AttnArgs &a);
+bool attend_use_few(const AttnArgs &a);
+hipError_t launch_attend_few(const AttnArgs &a, void *part, hipStream_t s);
 
-size_t attend_grad_bytes(int32_t q_rows, int32_t docs, int32_t heads, int32_t buckets, bool fp16);
+size_t attend_grad_bytes(const AttnArgs &f);
 hipError_t launch_attend_grad(const AttnGradArgs &a, void *ws, hipStream_t s);
 
 struct LogprobArgs {

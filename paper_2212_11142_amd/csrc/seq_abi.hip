@@ -60,10 +60,27 @@ gp_status check_heads(const gp_heads *x, const char *name, int32_t rows) {
   return GP_OK;
 }
 
-AttnArgs make_args(const gp_attention *t, const gp_heads *q, const gp_heads *k, const gp_heads *v,
-                   const gp_heads *o, const gp_heads *rest, const void *table, float *lse) {
+AttnArgs make_args(const gp_attention *t) {
   AttnArgs a;
   std::memset(&a, 0, sizeof a);
+  a.qb = t->q_begin, a.qe = t->q_end, a.kb = t->k_begin, a.ke = t->k_end, a.prefix = t->prefix;
+  a.docs = t->n_docs, a.heads = t->heads, a.kv_heads = t->kv_heads;
+  a.group = t->heads / t->kv_heads;
+  a.bytes = 2 * t->dim;
+  a.q_rows = t->q_rows, a.k_rows = t->k_rows, a.max_q = t->max_q, a.max_k = t->max_k;
+  a.causal = t->causal ? 1 : 0;
+  a.scale = t->scale, a.cap = t->cap;
+  a.slopes = t->slopes;
+  a.buckets.per_side = t->per_side;
+  a.buckets.two_sided = t->two_sided ? 1 : 0;
+  for (int i = 0; i < kMaxBuckets; ++i)
+    a.buckets.start[i] = i < t->per_side ? t->bucket_start[i] : INT32_MAX;
+  a.fp16 = t->dtype == GP_FP16;
+  return a;
+}
+
+void set_tensors(AttnArgs &a, const gp_heads *q, const gp_heads *k, const gp_heads *v,
+                 const gp_heads *o, const gp_heads *rest, const void *table, float *lse) {
   a.q = static_cast<const char *>(q->data);
   a.k = static_cast<const char *>(k->data);
   a.v = static_cast<const char *>(v->data);
@@ -76,24 +93,9 @@ AttnArgs make_args(const gp_attention *t, const gp_heads *q, const gp_heads *k, 
     a.rest = static_cast<char *>(rest->data);
     a.rest_row = 2 * rest->row, a.rest_head = 2 * rest->head;
   }
-  a.lse = lse;
-  a.qb = t->q_begin, a.qe = t->q_end, a.kb = t->k_begin, a.ke = t->k_end, a.prefix = t->prefix;
-  a.docs = t->n_docs, a.heads = t->heads, a.kv_heads = t->kv_heads;
-  a.group = t->heads / t->kv_heads;
-  a.bytes = 2 * t->dim;
-  a.q_rows = t->q_rows, a.k_rows = t->k_rows, a.max_q = t->max_q, a.max_k = t->max_k;
-  a.causal = t->causal ? 1 : 0;
-  a.scale = t->scale, a.cap = t->cap;
-  a.slopes = t->slopes;
   a.table = table;
-  a.buckets.per_side = t->per_side;
-  a.buckets.two_sided = t->two_sided ? 1 : 0;
-  for (int i = 0; i < t->per_side; ++i) a.buckets.start[i] = t->bucket_start[i];
-  a.fp16 = t->dtype == GP_FP16;
-  return a;
+  a.lse = lse;
 }
-
-int bucket_count(const gp_attention *t) { return t->per_side * (t->two_sided ? 2 : 1); }
 
 gp_status check_workspace(const void *ws, size_t bytes, size_t need) {
   if (need == 0) return GP_OK;
@@ -106,11 +108,9 @@ gp_status check_workspace(const void *ws, size_t bytes, size_t need) {
   return GP_OK;
 }
 
-size_t attend_bytes(const gp_attention *t) {
-  const int group = t->heads / t->kv_heads;
-  if (t->n_docs == 0 || t->max_q == 0) return 0;
-  if (!attend_use_few(t->n_docs, t->kv_heads, group, t->max_q, t->max_k)) return 0;
-  return attend_few_bytes(t->n_docs, t->kv_heads, group, t->max_q, t->max_k, t->dim);
+size_t attend_bytes(const AttnArgs &a) {
+  if (a.docs == 0 || a.max_q == 0 || !attend_use_few(a)) return 0;
+  return attend_few_bytes(a);
 }
 
 gp_status hip_status(hipError_t e, const char *what) {
@@ -152,9 +152,7 @@ size_t gp_attend_workspace_bytes(const gp_attention *t, int32_t with_grad) {
   guarded([&] {
     const gp_status st = check_attention(t);
     if (st != GP_OK) return st;
-    n = with_grad ? attend_grad_bytes(t->q_rows, t->n_docs, t->heads, bucket_count(t),
-                                      t->dtype == GP_FP16)
-                  : attend_bytes(t);
+    n = with_grad ? attend_grad_bytes(make_args(t)) : attend_bytes(make_args(t));
     return GP_OK;
   });
   return n;
@@ -175,12 +173,12 @@ gp_status gp_attend(const gp_attention *t, const gp_heads *q, const gp_heads *k,
     if (!lse && t->q_rows > 0) return bad("lse is NULL");
     if (t->n_docs == 0 || t->max_q == 0) return GP_OK;
     hipStream_t s = static_cast<hipStream_t>(stream);
-    const AttnArgs a = make_args(t, q, k, v, out, rest, table, lse);
-    if (rest) return hip_status(launch_attend(a, s), "attention");
-    st = check_workspace(workspace, ws_bytes, attend_bytes(t));
+    AttnArgs a = make_args(t);
+    set_tensors(a, q, k, v, out, rest, table, lse);
+    st = check_workspace(workspace, ws_bytes, attend_bytes(a));
     if (st != GP_OK) return st;
-    if (attend_use_few(a.docs, a.kv_heads, a.group, a.max_q, a.max_k))
-      return hip_status(launch_attend_few(a, static_cast<float *>(workspace), s), "attention");
+    if (attend_use_few(a))
+      return hip_status(launch_attend_few(a, workspace, s), "attention");
     return hip_status(launch_attend(a, s), "attention");
   });
 }
@@ -205,13 +203,12 @@ gp_status gp_attend_grad(const gp_attention *t, const gp_heads *q, const gp_head
     if ((t->per_side > 0) != (table != nullptr)) return bad("a table goes with per_side > 0");
     if ((table != nullptr) != (dtable != nullptr)) return bad("dtable goes with a table");
     if (!lse && t->q_rows > 0) return bad("lse is NULL");
-    st = check_workspace(workspace, ws_bytes,
-                         attend_grad_bytes(t->q_rows, t->n_docs, t->heads, bucket_count(t),
-                                           t->dtype == GP_FP16));
-    if (st != GP_OK) return st;
     AttnGradArgs g;
     std::memset(&g, 0, sizeof g);
-    g.f = make_args(t, q, k, v, out, rest, table, const_cast<float *>(lse));
+    g.f = make_args(t);
+    set_tensors(g.f, q, k, v, out, rest, table, const_cast<float *>(lse));
+    st = check_workspace(workspace, ws_bytes, attend_grad_bytes(g.f));
+    if (st != GP_OK) return st;
     g.dout = static_cast<const char *>(dout->data);
     g.dq = static_cast<char *>(dq->data);
     g.dk = static_cast<char *>(dk->data);

@@ -338,23 +338,36 @@ enum BiasKind { kBiasNone = 0, kBiasSlope = 1, kBiasTable = 2 };
 constexpr int kLutPad = 64;
 __host__ __device__ inline int lut_size(int reach) { return 2 * (reach + kLutPad) + 1; }
 
-// Bucket of the distance delta = key - query position.
+// Bucket of the distance delta = key - query position. (The starts past the last one are
+// never reached, so that the comparisons go in eights.)
 __device__ inline int bucket_of(const BucketMap &m, int delta) {
   const int a = m.two_sided ? (delta < 0 ? -delta : delta) : (delta < 0 ? -delta : 0);
   int b = 0;
-  for (int t = 1; t < m.per_side; ++t) b += a >= m.start[t] ? 1 : 0;
-  return b + ((m.two_sided && delta > 0) ? m.per_side : 0);
+  for (int t = 0; t < m.per_side; t += 8)
+#pragma unroll
+    for (int i = 0; i < 8; ++i) b += a >= m.start[t + i] ? 1 : 0;
+  return b - 1 + ((m.two_sided && delta > 0) ? m.per_side : 0);
+}
+__host__ __device__ inline int bucket_count(const BucketMap &m) {
+  return m.two_sided ? 2 * m.per_side : m.per_side;
 }
 
-// Fills the LDS table of the head's biases (log 2 units) by distance.
-template <class T>
-__device__ inline void fill_lut(float *lut, const BucketMap &m, const void *table, int head,
-                                int threads) {
-  const int nb = m.two_sided ? 2 * m.per_side : m.per_side;
+// The buckets of the table's distances in LDS, and a head's biases (log 2 units) from them,
+// each as `thread` of `threads`.
+__device__ inline void fill_map(uint8_t *map, const BucketMap &m, int thread, int threads) {
   const int reach = m.start[m.per_side - 1], n = lut_size(reach);
-  for (int i = threadIdx.x; i < n; i += threads)
-    lut[i] = T::load(table, (int64_t)head * nb + bucket_of(m, i - (reach + kLutPad))) * kLog2e;
+  for (int i = thread; i < n; i += threads) map[i] = (uint8_t)bucket_of(m, i - (reach + kLutPad));
 }
+template <class T>
+__device__ inline void fill_lut(float *lut, const uint8_t *map, const BucketMap &m, const void *table,
+                                int head, int thread, int threads) {
+  const int n = lut_size(m.start[m.per_side - 1]);
+  const int64_t row = (int64_t)head * bucket_count(m);
+#pragma unroll 4
+  for (int i = thread; i < n; i += threads) lut[i] = T::load(table, row + map[i]) * kLog2e;
+}
+// LDS of a map, rounded up
+__host__ __device__ inline int map_bytes(int reach) { return (lut_size(reach) + 15) / 16 * 16; }
 
 // Adds the bias of 32 keys (from key0) to the 16 scores of a lane whose query stands at
 // pos; the block's positions are pos_lo..pos_lo + 31. `lut` is the head's table, `slope2`

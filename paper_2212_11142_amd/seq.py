@@ -28,6 +28,14 @@ def _dtype_code(dtype):
     return code
 
 
+def _workspace(nbytes):
+    """A workspace and its size."""
+    if not nbytes:
+        return None, 0
+    ws = gp._workspace(nbytes)
+    return ws, ws.numel()
+
+
 # ------------------------------------------------------------------ layouts
 class Documents:
     """The documents (tuning runs) of a packed batch.
@@ -171,7 +179,13 @@ class Attention:
             s.bucket_start = self._start
         self.struct = s
         self.ref = C.byref(s)
+        self.lib = gp.load()
         self.workspace_bytes(False)          # raises if the description is invalid
+        self.table_shape = None if buckets is None else (self.heads, buckets.count)
+        self.slots = {n: _Slot(n, docs.q_rows, self.heads, self)
+                      for n in ("q", "out", "rest", "dout", "dq")}
+        self.slots.update({n: _Slot(n, docs.k_rows, self.kv_heads, self)
+                           for n in ("k", "v", "dk", "dv")})
 
     def workspace_bytes(self, with_grad: bool) -> int:
         lib = gp.load()
@@ -198,8 +212,7 @@ class AttendBuffers:
 
         self.out = rows(d.q_full, d.q_rows, att.heads)
         self.lse = torch.full((att.heads, d.q_rows), -math.inf, dtype=torch.float32, device="cuda")
-        n = att.workspace_bytes(False)
-        self.workspace = gp._workspace(n) if n else None
+        self.workspace, self.workspace_bytes = _workspace(att.workspace_bytes(False))
         self.dq = self.dk = self.dv = self.dtable = self.rest = self.grad_workspace = None
         if grad:
             if not d.k_disjoint:
@@ -211,17 +224,30 @@ class AttendBuffers:
             if att.buckets is not None:
                 self.dtable = torch.empty((att.heads, att.buckets.count), **f16)
             self.grad_workspace = gp._workspace(att.workspace_bytes(True))
+            self.grad_workspace_bytes = self.grad_workspace.numel()
 
 
-def _heads(x, att: Attention, rows: int, heads: int, name: str):
-    if x.dtype != att.dtype or not x.is_cuda:
-        raise ValueError(f"{name} must be a {att.dtype} CUDA tensor")
-    if tuple(x.shape) != (rows, heads, att.dim):
-        raise ValueError(f"{name} has shape {tuple(x.shape)}, need {(rows, heads, att.dim)}")
-    row, head, one = x.stride()
-    if one != 1 and att.dim > 1:
-        raise ValueError(f"{name}'s last axis must be contiguous")
-    return C.byref(gp._Heads(x.data_ptr(), row, head))
+class _Slot:
+    """One tensor argument of a description's calls: its shape, and the gp_heads struct that
+    is filled for each call."""
+
+    __slots__ = ("name", "shape", "dtype", "dim", "struct", "ref")
+
+    def __init__(self, name, rows, heads, att):
+        self.name, self.shape, self.dtype = name, (rows, heads, att.dim), att.dtype
+        self.struct = gp._Heads()
+        self.ref = C.byref(self.struct)
+
+    def __call__(self, x):
+        if x.shape != self.shape or x.dtype is not self.dtype or not x.is_cuda:
+            raise ValueError(f"{self.name} must be a {self.dtype} CUDA tensor of shape {self.shape}, "
+                             f"not {x.dtype} {tuple(x.shape)} on {x.device}")
+        s = self.struct
+        s.row, s.head, one = x.stride()
+        if one != 1:
+            raise ValueError(f"{self.name}'s last axis must be contiguous")
+        s.data = x.data_ptr()
+        return self.ref
 
 
 def _table(table, att: Attention):
@@ -229,10 +255,9 @@ def _table(table, att: Attention):
         raise ValueError("a table goes with a description that has buckets")
     if table is None:
         return None
-    if table.dtype != att.dtype or not table.is_cuda or not table.is_contiguous() or \
-            tuple(table.shape) != (att.heads, att.buckets.count):
-        raise ValueError(f"table must be a contiguous {att.dtype} CUDA tensor "
-                         f"{(att.heads, att.buckets.count)}")
+    if table.shape != att.table_shape or table.dtype is not att.dtype or not table.is_cuda or \
+            not table.is_contiguous():
+        raise ValueError(f"table must be a contiguous {att.dtype} CUDA tensor {att.table_shape}")
     return table.data_ptr()
 
 
@@ -240,14 +265,13 @@ def attend_into(att: Attention, q, k, v, bufs: AttendBuffers, table=None):
     """gp_attend into bufs.out and bufs.lse (asynchronous on the current stream). q
     [q_rows, heads, dim], k and v [k_rows, kv_heads, dim]; strides of rows and heads are
     free (multiples of 8)."""
-    d = att.docs
-    ws = bufs.workspace
-    _check(gp.load().gp_attend(
-        att.ref, _heads(q, att, d.q_rows, att.heads, "q"),
-        _heads(k, att, d.k_rows, att.kv_heads, "k"), _heads(v, att, d.k_rows, att.kv_heads, "v"),
-        _table(table, att), _heads(bufs.out, att, d.q_rows, att.heads, "out"),
-        None if bufs.rest is None else _heads(bufs.rest, att, d.q_rows, att.heads, "rest"),
-        bufs.lse.data_ptr(), _ptr(ws), 0 if ws is None else ws.numel(), _stream()))
+    t, ws, rest = att.slots, bufs.workspace, bufs.rest
+    st = att.lib.gp_attend(att.ref, t["q"](q), t["k"](k), t["v"](v), _table(table, att),
+                           t["out"](bufs.out), None if rest is None else t["rest"](rest),
+                           bufs.lse.data_ptr(), None if ws is None else ws.data_ptr(),
+                           bufs.workspace_bytes, _stream())
+    if st:
+        _check(st)
 
 
 def attend(att: Attention, q, k, v, table=None) -> dict:
@@ -261,17 +285,14 @@ def attend_grad_into(att: Attention, q, k, v, dout, bufs: AttendBuffers, table=N
     the out and lse that attend_into left in bufs for the same inputs."""
     if bufs.dq is None:
         raise ValueError("the buffers were made without grad")
-    d = att.docs
-    H, K = att.heads, att.kv_heads
-    ws = bufs.grad_workspace
-    _check(gp.load().gp_attend_grad(
-        att.ref, _heads(q, att, d.q_rows, H, "q"), _heads(k, att, d.k_rows, K, "k"),
-        _heads(v, att, d.k_rows, K, "v"), _table(table, att),
-        _heads(bufs.out, att, d.q_rows, H, "out"), _heads(bufs.rest, att, d.q_rows, H, "rest"),
-        bufs.lse.data_ptr(),
-        _heads(dout, att, d.q_rows, H, "dout"), _heads(bufs.dq, att, d.q_rows, H, "dq"),
-        _heads(bufs.dk, att, d.k_rows, K, "dk"), _heads(bufs.dv, att, d.k_rows, K, "dv"),
-        _ptr(bufs.dtable), _ptr(ws), ws.numel(), _stream()))
+    t = att.slots
+    st = att.lib.gp_attend_grad(
+        att.ref, t["q"](q), t["k"](k), t["v"](v), _table(table, att), t["out"](bufs.out),
+        t["rest"](bufs.rest), bufs.lse.data_ptr(), t["dout"](dout), t["dq"](bufs.dq),
+        t["dk"](bufs.dk), t["dv"](bufs.dv), _ptr(bufs.dtable), bufs.grad_workspace.data_ptr(),
+        bufs.grad_workspace_bytes, _stream())
+    if st:
+        _check(st)
 
 
 # ------------------------------------------------------------------ log probabilities
@@ -283,7 +304,6 @@ class LogprobBuffers:
     def __init__(self, rows: int, width: int, dtype, top: int = 0, grad: bool = False):
         torch = _torch()
         self.rows, self.width, self.top, self.dtype = int(rows), int(width), int(top), dtype
-        _dtype_code(dtype)
         f32 = dict(dtype=torch.float32, device="cuda")
         self.logp, self.entropy, self.lse = (torch.empty(self.rows, **f32) for _ in range(3))
         self.top_logp = torch.empty((self.rows, self.top), **f32) if top else None
@@ -291,22 +311,26 @@ class LogprobBuffers:
                        if top else None)
         self.dlogits = (torch.empty((self.rows, self.width), dtype=dtype, device="cuda")
                         if grad else None)
-        n = gp.load().gp_logprob_workspace_bytes(self.rows, self.width, self.top)
-        self.workspace = gp._workspace(n) if n else None
+        self.code = _dtype_code(dtype)
+        self.shape = (self.rows, self.width)
+        self.lib = gp.load()
+        self.workspace, self.workspace_bytes = _workspace(
+            self.lib.gp_logprob_workspace_bytes(self.rows, self.width, self.top))
 
 
 def _logits(x, bufs, name="logits"):
-    if x.dtype != bufs.dtype or not x.is_cuda or tuple(x.shape) != (bufs.rows, bufs.width):
-        raise ValueError(f"{name} must be a {bufs.dtype} CUDA tensor {(bufs.rows, bufs.width)}")
-    if x.stride(1) != 1 and bufs.width > 1:
+    if x.shape != bufs.shape or x.dtype is not bufs.dtype or not x.is_cuda:
+        raise ValueError(f"{name} must be a {bufs.dtype} CUDA tensor {bufs.shape}")
+    row, one = x.stride()
+    if one != 1 and bufs.width > 1:
         raise ValueError(f"{name}'s rows must be contiguous")
-    return x.data_ptr(), x.stride(0)
+    return x.data_ptr(), row
 
 
 def _row_vector(x, bufs, dtype, name):
     if x is None:
         return None
-    if x.dtype != dtype or not x.is_cuda or not x.is_contiguous() or tuple(x.shape) != (bufs.rows,):
+    if x.shape != (bufs.rows,) or x.dtype is not dtype or not x.is_cuda or not x.is_contiguous():
         raise ValueError(f"{name} must be a contiguous {dtype} CUDA vector of {bufs.rows}")
     return x.data_ptr()
 
@@ -315,16 +339,18 @@ def logprob_into(logits, targets, bufs: LogprobBuffers, scale: float = 1.0):
     """gp_logprob of logits [rows, width] (the rows' stride is free): log p(targets)
     (int64 [rows]; outside 0..width-1: no target, 0), entropy and lse of
     softmax(scale * logits), and the bufs.top best entries, into bufs."""
-    torch = _torch()
     x, stride = _logits(logits, bufs)
-    t = _row_vector(targets, bufs, torch.int64, "targets")
-    ws = bufs.workspace
-    if bufs.logp is not None and t is None:
+    t = _row_vector(targets, bufs, _torch().int64, "targets")
+    if t is None:
         raise ValueError("targets are required")
-    _check(gp.load().gp_logprob(
-        _dtype_code(bufs.dtype), x, stride, bufs.rows, bufs.width, float(scale), t, bufs.top,
-        bufs.logp.data_ptr(), bufs.entropy.data_ptr(), bufs.lse.data_ptr(), _ptr(bufs.top_logp),
-        _ptr(bufs.top_id), _ptr(ws), 0 if ws is None else ws.numel(), _stream()))
+    ws, top = bufs.workspace, bufs.top
+    st = bufs.lib.gp_logprob(
+        bufs.code, x, stride, bufs.rows, bufs.width, scale, t, top, bufs.logp.data_ptr(),
+        bufs.entropy.data_ptr(), bufs.lse.data_ptr(), bufs.top_logp.data_ptr() if top else None,
+        bufs.top_id.data_ptr() if top else None, None if ws is None else ws.data_ptr(),
+        bufs.workspace_bytes, _stream())
+    if st:
+        _check(st)
 
 
 def logprob(logits, targets, top: int = 0, scale: float = 1.0) -> dict:
@@ -346,8 +372,10 @@ def logprob_grad_into(logits, targets, g_logp, g_entropy, bufs: LogprobBuffers,
         raise ValueError("the buffers were made without grad")
     x, stride = _logits(logits, bufs)
     dx, dstride = _logits(bufs.dlogits, bufs, "dlogits")
-    _check(gp.load().gp_logprob_grad(
-        _dtype_code(bufs.dtype), x, stride, bufs.rows, bufs.width, float(scale),
+    st = bufs.lib.gp_logprob_grad(
+        bufs.code, x, stride, bufs.rows, bufs.width, scale,
         _row_vector(targets, bufs, torch.int64, "targets"), bufs.lse.data_ptr(),
         bufs.entropy.data_ptr(), _row_vector(g_logp, bufs, torch.float32, "g_logp"),
-        _row_vector(g_entropy, bufs, torch.float32, "g_entropy"), dx, dstride, _stream()))
+        _row_vector(g_entropy, bufs, torch.float32, "g_entropy"), dx, dstride, _stream())
+    if st:
+        _check(st)
