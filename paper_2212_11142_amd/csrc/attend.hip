@@ -85,9 +85,9 @@ __global__ __launch_bounds__(kThreads, 2) void attend_kernel(const AttnArgs a) {
     fill_lut<T>(lut, map, a.buckets, a.table, head, threadIdx.x, kThreads);
   }
   if (BIAS == kBiasSlope) slope2 = a.slopes[head] * kLog2e;
-  ScoreScale sc;
-  sc.cap2 = a.cap * kLog2e;
-  sc.c = CAP ? 2.f * kLog2e * a.scale / a.cap : a.scale * kLog2e;
+  float steps[16];
+  slope_steps<BIAS>(steps, slope2);
+  const ScoreScale sc = score_scale<CAP>(a.scale, a.cap);
 
   f32x16 acc[DT];
 #pragma unroll
@@ -109,48 +109,47 @@ __global__ __launch_bounds__(kThreads, 2) void attend_kernel(const AttnArgs a) {
         s[0] = T::mfma(row_operand<DP>(kb, 0, i), qf[i], s[0]);
         s[1] = T::mfma(row_operand<DP>(kb, 32, i), qf[i], s[1]);
       }
-      // scores; without cap and bias the scale goes into the exponent's fma below
-      const bool raw = !CAP && BIAS == kBiasNone;
-      if (!raw) {
+      Affine f[2];
+      float top = -__builtin_inff();
 #pragma unroll
-        for (int b = 0; b < 2; ++b) {
+      for (int b = 0; b < 2; ++b) {
+        if (CAP) {
 #pragma unroll
-          for (int e = 0; e < 16; ++e) s[b][e] = scaled<CAP>(s[b][e], sc);
-          add_bias<BIAS>(s[b], key0 + 32 * b, row + shift, row_lo + shift, h, slope2, lut, reach);
+          for (int e = 0; e < 16; ++e) s[b][e] = score_x<CAP>(s[b][e], sc);
         }
-      }
-      if (masked) {
-        const int mine = lim - key0 - 4 * h;
-#pragma unroll
-        for (int b = 0; b < 2; ++b)
+        f[b] = add_bias<BIAS>(s[b], sc, key0 + 32 * b, row + shift, row_lo + shift, h, slope2, steps,
+                              lut, reach);
+        if (masked) {
+          const int mine = lim - key0 - 32 * b - 4 * h;
 #pragma unroll
           for (int e = 0; e < 16; ++e)
-            if (32 * b + 8 * (e >> 2) + (e & 3) >= mine) s[b][e] = -__builtin_inff();
+            if (row_of(e) >= mine) s[b][e] = -__builtin_inff();
+        }
+        float t = max3(s[b][0], s[b][1], s[b][2]);
+#pragma unroll
+        for (int e = 3; e < 15; e += 2) t = max3(t, s[b][e], s[b][e + 1]);
+        t = max3(t, s[b][15], s[b][15]);
+        top = fmaxf(top, __builtin_fmaf(t, f[b].a, f[b].b));
       }
-      float top = s[0][0];
-#pragma unroll
-      for (int b = 0; b < 2; ++b)
-#pragma unroll
-        for (int e = 0; e < 16; ++e) top = fmaxf(top, s[b][e]);
-      if (raw) top *= sc.c;
       top = max_halves(top);
       if (__any(top > m + kSlack)) {
         const float mn = top > m + kSlack ? top : m;
-        const float f = mn == -__builtin_inff() ? 1.f : fast_exp2(m - mn);
+        const float r = mn == -__builtin_inff() ? 1.f : fast_exp2(m - mn);
         m = mn;
-        l *= f;
+        l *= r;
 #pragma unroll
         for (int c = 0; c < DT; ++c)
 #pragma unroll
-          for (int e = 0; e < 16; ++e) acc[c][e] *= f;
+          for (int e = 0; e < 16; ++e) acc[c][e] *= r;
       }
       const float ms = m == -__builtin_inff() ? 0.f : m;
       u32x4 p[kBN / 16];
 #pragma unroll
       for (int b = 0; b < 2; ++b) {
+        const float off = f[b].b - ms;
 #pragma unroll
         for (int e = 0; e < 16; ++e) {
-          s[b][e] = fast_exp2(raw ? __builtin_fmaf(s[b][e], sc.c, -ms) : s[b][e] - ms);
+          s[b][e] = fast_exp2(__builtin_fmaf(s[b][e], f[b].a, off));
           l += s[b][e];
         }
         // the probabilities are rounded to the operands' type for the second product (with

@@ -85,7 +85,7 @@ __global__ __launch_bounds__(kThreads, 1) void few_kernel(const AttnArgs a, cons
                                                           void *part) {
   constexpr int KS = DP / 16, DT = DP / 32;
   constexpr int kTile = kKeys * DP * 2;
-  constexpr int kCopies = 2 * (kTile / 1024);       // copy instructions of a step
+  constexpr int kCopies = kTile / 1024;             // copy instructions of a tile
   constexpr int kLine = DP + 4;                     // floats of a row in the join below
   extern __shared__ __align__(1024) char lds[];
   __shared__ float ml[4][kRows][2];
@@ -128,18 +128,26 @@ __global__ __launch_bounds__(kThreads, 1) void few_kernel(const AttnArgs a, cons
   kc.init(0, lane, (int)a.k_row, a.bytes);
   vc.init(0, lane, (int)a.v_row, a.bytes);
   char *mine = lds + wave * 4 * kTile;              // K, V of two steps
-  auto start = [&](int key, int buf) {
-    const int n = min(lk - key, kKeys);
-    kc.start(row_buffer(kbase, key, n, a.k_row, a.bytes), lds_address(mine) + buf * 2 * kTile);
-    vc.start(row_buffer(vbase, key, n, a.v_row, a.bytes),
+  // (past the last key: nothing but zeros is copied, so that the waits below count evenly)
+  auto start_k = [&](int key, int buf) {
+    kc.start(row_buffer(kbase, key, key < key_hi ? min(lk - key, kKeys) : 0, a.k_row, a.bytes),
+             lds_address(mine) + buf * 2 * kTile);
+  };
+  auto start_v = [&](int key, int buf) {
+    vc.start(row_buffer(vbase, key, key < key_hi ? min(lk - key, kKeys) : 0, a.v_row, a.bytes),
              lds_address(mine) + (buf * 2 + 1) * kTile);
   };
-  int key = key_lo + wave * kKeys;
-  if (key < key_hi) start(key, 0);
-
-  u32x4 qf[KS];
+  u32x4 qf[KS];   // (asked for before the tiles: their arrival is waited for in order)
   load_operand<DP>(a.q + (int64_t)(q0 + i) * a.q_row + head * a.q_head, 0, live ? 0 : 1, 1,
                    a.bytes, lane, qf);
+  int key = key_lo + wave * kKeys;
+  if (key < key_hi) {
+    start_k(key, 0);
+    start_v(key, 0);
+    start_k(key + 4 * kKeys, 1);
+    start_v(key + 4 * kKeys, 1);
+  }
+
   int reach = 0, span = 1, nb = 0;
   float slope2 = 0.f, far = 0.f;
   uint8_t *map = nullptr;
@@ -157,9 +165,7 @@ __global__ __launch_bounds__(kThreads, 1) void few_kernel(const AttnArgs a, cons
     }
   }
   if (BIAS == kBiasSlope) slope2 = a.slopes[head] * kLog2e;
-  ScoreScale sc;
-  sc.cap2 = a.cap * kLog2e;
-  sc.c = CAP ? 2.f * kLog2e * a.scale / a.cap : a.scale * kLog2e;
+  const ScoreScale sc = score_scale<CAP>(a.scale, a.cap);
 
   f32x16 acc[DT];
 #pragma unroll
@@ -170,21 +176,17 @@ __global__ __launch_bounds__(kThreads, 1) void few_kernel(const AttnArgs a, cons
   __syncthreads();
 
   for (int buf = 0; key < key_hi; key += 4 * kKeys, buf ^= 1) {
-    // the buffer that is filled next was read in the step before
-    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-    if (key + 4 * kKeys < key_hi) {
-      start(key + 4 * kKeys, buf ^ 1);
-      wait_copies<kCopies>();
-    } else {
-      wait_copies<0>();
-    }
+    // two steps' tiles are under way; each is asked for again as soon as it has been read
+    wait_copies<3 * kCopies>();
     const uint32_t kb = rd.at(lds_address(mine) + buf * 2 * kTile, rd.row);
     const uint32_t vb = rd.at(lds_address(mine) + (buf * 2 + 1) * kTile, rd.col);
     f32x16 s = {};
 #pragma unroll
     for (int k = 0; k < KS; ++k) s = T::mfma(row_operand<DP>(kb, 0, k), qf[k], s);
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    start_k(key + 8 * kKeys, buf);
 #pragma unroll
-    for (int e = 0; e < 16; ++e) s[e] = scaled<CAP>(s[e], sc);
+    for (int e = 0; e < 16; ++e) s[e] = __builtin_fmaf(score_x<CAP>(s[e], sc), sc.a, sc.b);
     if (BIAS == kBiasSlope) {
       const float d0 = (float)(key + 4 * h - pos);
 #pragma unroll
@@ -234,6 +236,7 @@ __global__ __launch_bounds__(kThreads, 1) void few_kernel(const AttnArgs a, cons
     for (int k = 0; k < 2; ++k)
 #pragma unroll
       for (int w = 0; w < 4; ++w) pr[k][w] = T::pack(s[8 * k + 2 * w], s[8 * k + 2 * w + 1]);
+    wait_copies<3 * kCopies>();
     bool clean = true;
     if (masked && lim_lo < lk) {                    // as in the general form
       uint32_t bad = 0;
@@ -260,6 +263,8 @@ __global__ __launch_bounds__(kThreads, 1) void few_kernel(const AttnArgs a, cons
         if (REST) acc[c] = T::mfma(v, rest, acc[c]);
       }
     }
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    start_v(key + 8 * kKeys, buf);
   }
   l = sum_halves(l);
 

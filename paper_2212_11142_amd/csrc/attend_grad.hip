@@ -176,25 +176,16 @@ __device__ inline int ds_exponent(const float *bound, int blocks, float *red) {
   return uniform(min(max(15 - e, -60), 60));
 }
 
-// Products of a block: the same for both halves of the kernel below.
-template <class T, bool CAP>
-struct PairScale {
+// dS's factor: a block's, the same for both kinds below.
+template <class T>
+struct GradScale {
   static constexpr bool kHalf = std::is_same<T, Fp16>::value;
-  ScoreScale sc;
-  float inv_cap2, ds_scale;
+  float ds_scale;
   int ds0;
 
   __device__ void init(const AttnGradArgs &g, int row_blocks, float *red) {
-    sc.cap2 = g.f.cap * kLog2e;
-    sc.c = CAP ? 2.f * kLog2e * g.f.scale / g.f.cap : g.f.scale * kLog2e;
-    inv_cap2 = CAP ? 1.f / sc.cap2 : 0.f;
     ds0 = kHalf ? ds_exponent(g.bound, row_blocks, red) : 0;
     ds_scale = kHalf ? ldexpf(1.f, ds0) : 1.f;
-  }
-  // derivative of the capped product z (log 2 units)
-  __device__ float slope(float z) const {
-    const float y = z * inv_cap2;
-    return __builtin_fmaf(-y, y, 1.f);
   }
 };
 
@@ -278,8 +269,9 @@ __device__ __forceinline__ void grad_kv(const AttnGradArgs &ga, int row_blocks, 
 
   u32x4 kf[KS];
   load_operand<DP>(a.k + (int64_t)t.b0 * a.k_row + kvh * a.k_head, a.k_row, key, lk, a.bytes, lane, kf);
-  PairScale<T, CAP> ps;
+  GradScale<T> ps;
   ps.init(ga, row_blocks, red);
+  const ScoreScale sc = score_scale<CAP>(a.scale, a.cap);
   const float p0 = ps.kHalf ? kP16 : 0.f, ds_scale = ps.ds_scale * exp2f(-p0);
   const int reach = BIAS == kBiasTable ? a.buckets.start[a.buckets.per_side - 1] : 0;
 
@@ -336,36 +328,37 @@ __device__ __forceinline__ void grad_kv(const AttnGradArgs &ga, int row_blocks, 
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
           const int e = 4 * g + r;
-          s[e] = scaled<CAP>(s[e], ps.sc);
+          s[e] = score_x<CAP>(s[e], sc);
           dp[e] -= r < 2 ? x0[2 * r + 1] : x1[2 * r - 3];
-          if (CAP) dp[e] *= ps.slope(s[e]);
+          if (CAP) dp[e] *= cap_slope(s[e]);
         }
       }
       // the distance falls with the query: add_bias's elements in the other direction
+      Affine f = {sc.a, sc.b};
       if (BIAS == kBiasSlope) {
         const float d0 = (float)(key - shift - i0 - 4 * h);
 #pragma unroll
         for (int e = 0; e < 16; ++e)
-          s[e] = __builtin_fmaf(-slope2, __builtin_fabsf(d0 - (float)(8 * (e >> 2) + (e & 3))), s[e]);
+          s[e] = __builtin_fmaf(s[e], sc.a, -slope2 * __builtin_fabsf(d0 - (float)row_of(e)));
+        f.a = 1.f;
       }
       if (BIAS == kBiasTable) {
         const int far_hi = key_lo + 31 - (i0 + shift), far_lo = key_lo - (i0 + 31 + shift);
         if (far_hi <= -reach || far_lo >= reach) {
-          const float b = far_hi <= -reach ? lut[0] : lut[lut_size(reach) - 1];
-#pragma unroll
-          for (int e = 0; e < 16; ++e) s[e] += b;
+          f.b += far_hi <= -reach ? lut[0] : lut[lut_size(reach) - 1];
         } else {
           const float *p = lut + (key - shift - i0 - 4 * h + reach + kLutPad);
 #pragma unroll
-          for (int e = 0; e < 16; ++e) s[e] += p[-(8 * (e >> 2) + (e & 3))];
+          for (int e = 0; e < 16; ++e) s[e] = __builtin_fmaf(s[e], sc.a, p[-row_of(e)]);
+          f.a = 1.f;
         }
       }
+      const float off = f.b + p0;
       if (masked) {   // exp2(-inf) below
         const int lo = mine - i0 - 4 * h, hi = lq - i0 - 4 * h;
 #pragma unroll
         for (int e = 0; e < 16; ++e) {
-          const int r = 8 * (e >> 2) + (e & 3);
-          if (r < lo || r >= hi) s[e] = -__builtin_inff();
+          if (row_of(e) < lo || row_of(e) >= hi) s[e] = -__builtin_inff();
         }
       }
       asm volatile("" ::: "memory");   // reads the rows again rather than keep 32 registers
@@ -376,7 +369,7 @@ __device__ __forceinline__ void grad_kv(const AttnGradArgs &ga, int row_blocks, 
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
           const int e = 4 * g + r;
-          s[e] = fast_exp2(s[e] - ((r < 2 ? x0[2 * r] : x1[2 * r - 4]) - p0));
+          s[e] = fast_exp2(__builtin_fmaf(s[e], f.a, off - (r < 2 ? x0[2 * r] : x1[2 * r - 4])));
           dp[e] *= ps.kHalf ? s[e] * ds_scale : s[e];
         }
       }
@@ -485,8 +478,9 @@ __device__ __forceinline__ void grad_q(const AttnGradArgs &ga, int row_blocks, i
                    a.bytes, lane, df);
   const int64_t at = (int64_t)head * a.q_rows + t.b0 + row;
   const float lse = ok ? ga.rows[2 * at] : 0.f, delta = ok ? ga.rows[2 * at + 1] : 0.f;
-  PairScale<T, CAP> ps;
+  GradScale<T> ps;
   ps.init(ga, row_blocks, red);
+  const ScoreScale sc = score_scale<CAP>(a.scale, a.cap);
   int reach = 0;
   float slope2 = 0.f;
   float *hist = nullptr, *skew = skewed + wave * kSkew;
@@ -502,6 +496,8 @@ __device__ __forceinline__ void grad_q(const AttnGradArgs &ga, int row_blocks, i
     for (int i = lane; i < kSkew; i += 64) skew[i] = 0.f;
   }
   if (BIAS == kBiasSlope) slope2 = a.slopes[head] * kLog2e;
+  float steps[16];
+  slope_steps<BIAS>(steps, slope2);
 
   f32x16 acc[DT];
 #pragma unroll
@@ -531,21 +527,23 @@ __device__ __forceinline__ void grad_q(const AttnGradArgs &ga, int row_blocks, i
       for (int k = 0; k < KS; ++k) s = T::mfma(row_operand<DP>(kr, sub, k), qf[k], s);
 #pragma unroll
       for (int k = 0; k < KS; ++k) dp = T::mfma(row_operand<DP>(kr + kTile, sub, k), df[k], dp);
-      f32x16 z;
+      f32x16 z;   // x of the capped products
+      if (CAP) {
 #pragma unroll
-      for (int e = 0; e < 16; ++e) z[e] = scaled<CAP>(s[e], ps.sc);
-      s = z;
-      add_bias<BIAS>(s, key0, row + shift, row_lo + shift, h, slope2, lut, reach);
+        for (int e = 0; e < 16; ++e) z[e] = s[e] = score_x<CAP>(s[e], sc);
+      }
+      const Affine f = add_bias<BIAS>(s, sc, key0, row + shift, row_lo + shift, h, slope2, steps, lut, reach);
       if (key0 + 32 > lim_lo) {
         const int mine = lim - key0 - 4 * h;
 #pragma unroll
         for (int e = 0; e < 16; ++e)
-          if (8 * (e >> 2) + (e & 3) >= mine) s[e] = -__builtin_inff();
+          if (row_of(e) >= mine) s[e] = -__builtin_inff();
       }
+      const float off = f.b - lse;
       float sum = 0.f;
 #pragma unroll
       for (int e = 0; e < 16; ++e) {
-        dp[e] = fast_exp2(s[e] - lse) * (dp[e] - delta);
+        dp[e] = fast_exp2(__builtin_fmaf(s[e], f.a, off)) * (dp[e] - delta);
         if (BIAS == kBiasTable) sum += dp[e];
       }
       if (BIAS == kBiasTable) {
@@ -577,7 +575,7 @@ __device__ __forceinline__ void grad_q(const AttnGradArgs &ga, int row_blocks, i
       }
 #pragma unroll
       for (int e = 0; e < 16; ++e) {
-        if (CAP) dp[e] *= ps.slope(z[e]);
+        if (CAP) dp[e] *= cap_slope(z[e]);
         if (ps.kHalf) dp[e] *= ps.ds_scale;
       }
       u32x4 dr[2];

@@ -72,6 +72,14 @@ __device__ inline int uniform(int x) { return __builtin_amdgcn_readfirstlane(x);
 // (a parameter, not an element of a vector: __builtin_bit_cast takes those from the front)
 __device__ inline float word_float(uint32_t x) { return __builtin_bit_cast(float, x); }
 
+// (the compiler would first multiply each operand that comes out of a matrix instruction by
+// 1, against signalling NaN)
+__device__ inline float max3(float a, float b, float c) {
+  float r;
+  asm("v_max3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));
+  return r;
+}
+
 // Sum and maximum over a lane and the one 32 away.
 __device__ inline float sum_halves(float x) {
   const uint32_t u = __builtin_bit_cast(uint32_t, x);
@@ -316,20 +324,29 @@ __device__ inline DocTile find_tile(const int32_t *b, const int32_t *e, int docs
 }
 
 // ------------------------------------------------------------------ scores
-// Score of a pair in units of log 2: capped product plus bias.
+// A score in units of log 2 is a x + b + bias: x the product itself, or for a capped one
+// x = -1 / (1 + e^(2 z / cap)), as cap tanh(z / cap) = cap + 2 cap x (exact at both ends: the
+// exponential is 0 or infinite there).
 struct ScoreScale {
-  float c;      // no cap: scale * log2(e); cap: 2 log2(e) scale / cap
-  float cap2;   // cap * log2(e)
+  float c;   // cap: the product's factor in the exponential
+  float a, b;
+  float inv; // cap: 1 / b
 };
-
-// cap tanh(z / cap) = cap - 2 cap / (1 + e^(2 z / cap)), exact at both ends: the
-// exponential is 0 or infinite there.
 template <bool CAP>
-__device__ inline float scaled(float s, const ScoreScale &k) {
-  if (!CAP) return s * k.c;
-  const float r = __builtin_amdgcn_rcpf(1.f + fast_exp2(s * k.c));
-  return __builtin_fmaf(-2.f * k.cap2, r, k.cap2);
+__device__ inline ScoreScale score_scale(float scale, float cap) {
+  ScoreScale k;
+  k.b = CAP ? cap * kLog2e : 0.f;
+  k.a = CAP ? 2.f * k.b : scale * kLog2e;
+  k.c = CAP ? 2.f * kLog2e * scale / cap : 0.f;
+  k.inv = CAP ? 1.f / k.b : 0.f;
+  return k;
 }
+template <bool CAP>
+__device__ inline float score_x(float s, const ScoreScale &k) {
+  return CAP ? __builtin_amdgcn_rcpf(-(1.f + fast_exp2(s * k.c))) : s;
+}
+// Derivative of the capped product, 1 - tanh^2 = 1 - (1 + 2 x)^2 = -4 x (1 + x).
+__device__ inline float cap_slope(float x) { return -4.f * x * (1.f + x); }
 
 enum BiasKind { kBiasNone = 0, kBiasSlope = 1, kBiasTable = 2 };
 
@@ -369,40 +386,50 @@ __device__ inline void fill_lut(float *lut, const uint8_t *map, const BucketMap 
 // LDS of a map, rounded up
 __host__ __device__ inline int map_bytes(int reach) { return (lut_size(reach) + 15) / 16 * 16; }
 
-// Adds the bias of 32 keys (from key0) to the 16 scores of a lane whose query stands at
-// pos; the block's positions are pos_lo..pos_lo + 31. `lut` is the head's table, `slope2`
-// its slope, both in log 2 units.
+// Offset of element e of a D result along its rows, without the lane half's 4.
+constexpr int row_of(int e) { return 8 * (e >> 2) + (e & 3); }
+
+// Puts the bias of 32 keys (from key0) on the 16 x of a lane whose query stands at pos; the
+// block's positions are pos_lo..pos_lo + 31. Afterwards the scores are a x + b with the
+// returned a (the same on all lanes) and b: what all of a lane's pairs share, or what every
+// pair has, is left to those. `lut` is the head's table, `slope2` its slope, both in log 2
+// units, steps[e] slope2 row_of(e).
+struct Affine {
+  float a, b;
+};
 template <int BIAS>
-__device__ inline void add_bias(f32x16 &s, int key0, int pos, int pos_lo, int h, float slope2,
-                                const float *lut, int reach) {
+__device__ inline Affine add_bias(f32x16 &x, const ScoreScale &k, int key0, int pos, int pos_lo, int h,
+                                  float slope2, const float *steps, const float *lut, int reach) {
   if (BIAS == kBiasSlope) {
     const float d0 = (float)(key0 + 4 * h - pos);
     if (key0 + 31 <= pos_lo) {  // no key ahead of a query: the bias is linear
-      const float b0 = slope2 * d0;
+      float a = k.a;
+      asm volatile("" : "+v"(a));   // (an instruction takes one scalar register: the step's)
 #pragma unroll
-      for (int e = 0; e < 16; ++e)
-        s[e] += __builtin_fmaf(slope2, (float)(8 * (e >> 2) + (e & 3)), b0);
-    } else {
-#pragma unroll
-      for (int e = 0; e < 16; ++e)
-        s[e] = __builtin_fmaf(-slope2, __builtin_fabsf(d0 + (float)(8 * (e >> 2) + (e & 3))), s[e]);
+      for (int e = 0; e < 16; ++e) x[e] = __builtin_fmaf(x[e], a, steps[e]);
+      return Affine{1.f, __builtin_fmaf(slope2, d0, k.b)};
     }
+#pragma unroll
+    for (int e = 0; e < 16; ++e)
+      x[e] = __builtin_fmaf(x[e], k.a, -slope2 * __builtin_fabsf(d0 + (float)row_of(e)));
+    return Affine{1.f, k.b};
   }
   if (BIAS == kBiasTable) {
-    if (key0 + 31 - pos_lo <= -reach) {
-      const float b = lut[0];
+    if (key0 + 31 - pos_lo <= -reach) return Affine{k.a, k.b + lut[0]};
+    if (key0 - (pos_lo + 31) >= reach) return Affine{k.a, k.b + lut[lut_size(reach) - 1]};
+    const float *p = lut + (key0 + 4 * h - pos + reach + kLutPad);
 #pragma unroll
-      for (int e = 0; e < 16; ++e) s[e] += b;
-    } else if (key0 - (pos_lo + 31) >= reach) {
-      const float b = lut[lut_size(reach) - 1];
-#pragma unroll
-      for (int e = 0; e < 16; ++e) s[e] += b;
-    } else {
-      const float *p = lut + (key0 + 4 * h - pos + reach + kLutPad);
-#pragma unroll
-      for (int e = 0; e < 16; ++e) s[e] += p[8 * (e >> 2) + (e & 3)];
-    }
+    for (int e = 0; e < 16; ++e) x[e] = __builtin_fmaf(x[e], k.a, p[row_of(e)]);
+    return Affine{1.f, k.b};
   }
+  return Affine{k.a, k.b};
+}
+template <int BIAS>
+__device__ inline void slope_steps(float *steps, float slope2) {
+  if (BIAS != kBiasSlope) return;
+#pragma unroll
+  for (int e = 0; e < 16; ++e)
+    steps[e] = __builtin_bit_cast(float, uniform(__builtin_bit_cast(int, slope2 * (float)row_of(e))));
 }
 
 }  // namespace bgp
