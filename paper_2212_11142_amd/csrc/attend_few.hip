@@ -18,10 +18,11 @@ constexpr int kKeys = 32;      // keys of a wavefront's step
 constexpr int kRows = 32;      // rows of a tile
 constexpr float kSlack = 8.f;  // as in the general form
 constexpr int kFewBlocks = 160;
+constexpr int kFewChunk = 2048;    // keys of a block, at most
 constexpr int kMaxValues = 4096;   // of the table for a group
 
-constexpr int few_tiles(int dp) {
-  const int tiles = 16 * kKeys * dp * 2, sums = 4 * kRows * (dp + 4) * 4;
+constexpr int few_tiles(int dp, int stages) {
+  const int tiles = stages * 8 * kKeys * dp * 2, sums = 4 * kRows * (dp + 4) * 4;
   return tiles > sums ? tiles : sums;
 }
 
@@ -35,16 +36,16 @@ FewPlan plan(int docs, int kv_heads, int group, int max_q, int max_k) {
   p.row_tiles = (int)((r + kRows - 1) / kRows);
   p.rows = (int)(r < kRows ? r : kRows);
   const int64_t units = (int64_t)docs * kv_heads * p.row_tiles;
-  // about 8 blocks per compute unit; where those would have less than 512 keys each, one per
+  // about 16 blocks per compute unit; where those would have less than 512 keys each, one per
   // compute unit, of 128 keys at least
   auto up = [](int64_t x) { return (x + 127) / 128 * 128; };
-  int64_t c = up((int64_t)max_k * units / (8 * kSeqCus));
+  int64_t c = up((int64_t)max_k * units / (16 * kSeqCus));
   if (c < 512) {
     c = up((int64_t)max_k * units / kSeqCus);
     if (c > 512) c = 512;
     if (c < 128) c = 128;
   }
-  if (c > 4096) c = 4096;
+  if (c > kFewChunk) c = kFewChunk;
   p.chunk = (int)c;
   p.chunks = (int)((max_k + c - 1) / c);
   if (p.chunks < 1) p.chunks = 1;
@@ -80,8 +81,11 @@ __device__ inline void write_quad(const AttnArgs &a, int row, int head, int d, f
         l == 0.f ? -__builtin_inff() : (m + __builtin_amdgcn_logf(l)) * kLn2;
 }
 
-template <class T, int DP, bool CAP, int BIAS, bool REST>
-__global__ __launch_bounds__(kThreads, 1) void few_kernel(const AttnArgs a, const FewPlan p,
+// STAGES: tiles of K and of V that a wavefront has room for. Two where a compute unit has
+// one block (the next tile arrives while this one is used); one where it has more: two blocks
+// then fit, which overlap their starts and ends too.
+template <class T, int DP, bool CAP, int BIAS, bool REST, int STAGES>
+__global__ __launch_bounds__(kThreads, STAGES == 1 ? 2 : 1) void few_kernel(const AttnArgs a, const FewPlan p,
                                                           void *part) {
   constexpr int KS = DP / 16, DT = DP / 32;
   constexpr int kTile = kKeys * DP * 2;
@@ -91,7 +95,7 @@ __global__ __launch_bounds__(kThreads, 1) void few_kernel(const AttnArgs a, cons
   __shared__ float ml[4][kRows][2];
   __shared__ int any_dirty;
   // tiles (then the wavefronts' sums), the group's rows of the table, buckets by distance
-  float *values = reinterpret_cast<float *>(lds + few_tiles(DP));
+  float *values = reinterpret_cast<float *>(lds + few_tiles(DP, STAGES));
 
   int id = blockIdx.x;
   const int kvh = id % a.kv_heads;
@@ -127,7 +131,7 @@ __global__ __launch_bounds__(kThreads, 1) void few_kernel(const AttnArgs a, cons
   TileCopy<DP, kKeys, 1> kc, vc;
   kc.init(0, lane, (int)a.k_row, a.bytes);
   vc.init(0, lane, (int)a.v_row, a.bytes);
-  char *mine = lds + wave * 4 * kTile;              // K, V of two steps
+  char *mine = lds + wave * STAGES * 2 * kTile;     // K, V of each stage
   // (past the last key: nothing but zeros is copied, so that the waits below count evenly)
   auto start_k = [&](int key, int buf) {
     kc.start(row_buffer(kbase, key, key < key_hi ? min(lk - key, kKeys) : 0, a.k_row, a.bytes),
@@ -142,10 +146,11 @@ __global__ __launch_bounds__(kThreads, 1) void few_kernel(const AttnArgs a, cons
                    a.bytes, lane, qf);
   int key = key_lo + wave * kKeys;
   if (key < key_hi) {
-    start_k(key, 0);
-    start_v(key, 0);
-    start_k(key + 4 * kKeys, 1);
-    start_v(key + 4 * kKeys, 1);
+#pragma unroll
+    for (int s = 0; s < STAGES; ++s) {
+      start_k(key + s * 4 * kKeys, s);
+      start_v(key + s * 4 * kKeys, s);
+    }
   }
 
   int reach = 0, span = 1, nb = 0;
@@ -175,16 +180,16 @@ __global__ __launch_bounds__(kThreads, 1) void few_kernel(const AttnArgs a, cons
   if (threadIdx.x == 0) any_dirty = 0;
   __syncthreads();
 
-  for (int buf = 0; key < key_hi; key += 4 * kKeys, buf ^= 1) {
-    // two steps' tiles are under way; each is asked for again as soon as it has been read
-    wait_copies<3 * kCopies>();
+  for (int buf = 0; key < key_hi; key += 4 * kKeys, buf ^= STAGES - 1) {
+    // a tile's room is filled again as soon as it has been read
+    wait_copies<(2 * STAGES - 1) * kCopies>();
     const uint32_t kb = rd.at(lds_address(mine) + buf * 2 * kTile, rd.row);
     const uint32_t vb = rd.at(lds_address(mine) + (buf * 2 + 1) * kTile, rd.col);
     f32x16 s = {};
 #pragma unroll
     for (int k = 0; k < KS; ++k) s = T::mfma(row_operand<DP>(kb, 0, k), qf[k], s);
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-    start_k(key + 8 * kKeys, buf);
+    start_k(key + STAGES * 4 * kKeys, buf);
 #pragma unroll
     for (int e = 0; e < 16; ++e) s[e] = __builtin_fmaf(score_x<CAP>(s[e], sc), sc.a, sc.b);
     if (BIAS == kBiasSlope) {
@@ -236,7 +241,7 @@ __global__ __launch_bounds__(kThreads, 1) void few_kernel(const AttnArgs a, cons
     for (int k = 0; k < 2; ++k)
 #pragma unroll
       for (int w = 0; w < 4; ++w) pr[k][w] = T::pack(s[8 * k + 2 * w], s[8 * k + 2 * w + 1]);
-    wait_copies<3 * kCopies>();
+    wait_copies<(2 * STAGES - 1) * kCopies>();
     bool clean = true;
     if (masked && lim_lo < lk) {                    // as in the general form
       uint32_t bad = 0;
@@ -264,7 +269,7 @@ __global__ __launch_bounds__(kThreads, 1) void few_kernel(const AttnArgs a, cons
       }
     }
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-    start_v(key + 8 * kKeys, buf);
+    start_v(key + STAGES * 4 * kKeys, buf);
   }
   l = sum_halves(l);
 
@@ -383,18 +388,17 @@ __global__ __launch_bounds__(kThreads) void few_join(const AttnArgs a, const Few
   write_quad<T, REST>(a, q0 + r % lq, kvh * a.group + r / lq, 4 * quad, x, top, ll);
 }
 
-template <class T, int DP, bool CAP, int BIAS, bool REST>
-hipError_t launch_form(const AttnArgs &a, void *part, hipStream_t s) {
+template <class T, int DP, bool CAP, int BIAS, bool REST, int STAGES>
+hipError_t launch_form(const AttnArgs &a, const FewPlan &p, void *part, hipStream_t s) {
   static LdsLimit limit;
-  const FewPlan p = plan(a.docs, a.kv_heads, a.group, a.max_q, a.max_k);
-  int lds = few_tiles(DP);
+  int lds = few_tiles(DP, STAGES);
   if (BIAS == kBiasTable)
     lds += a.group * bucket_count(a.buckets) * 4 + 2 * a.buckets.start[a.buckets.per_side - 1] + 4;
-  hipError_t e = limit.set(reinterpret_cast<const void *>(&few_kernel<T, DP, CAP, BIAS, REST>),
-                           few_tiles(DP) + kMaxValues * 4 + 2 * kMaxReach + 4);
+  hipError_t e = limit.set(reinterpret_cast<const void *>(&few_kernel<T, DP, CAP, BIAS, REST, STAGES>),
+                           few_tiles(DP, STAGES) + kMaxValues * 4 + 2 * kMaxReach + 4);
   if (e != hipSuccess) return e;
   const int64_t units = (int64_t)a.docs * a.kv_heads * p.row_tiles;
-  few_kernel<T, DP, CAP, BIAS, REST>
+  few_kernel<T, DP, CAP, BIAS, REST, STAGES>
       <<<dim3((uint32_t)(units * p.chunks)), kThreads, lds, s>>>(a, p, part);
   if (p.chunks > 1)
     few_join<T, DP, REST><<<dim3((uint32_t)(units * p.rows)), kThreads, 0, s>>>(a, p, part);
@@ -403,8 +407,13 @@ hipError_t launch_form(const AttnArgs &a, void *part, hipStream_t s) {
 
 template <class T, int DP, bool CAP, int BIAS>
 hipError_t launch(const AttnArgs &a, void *part, hipStream_t s) {
-  if (a.rest) return launch_form<T, DP, CAP, BIAS, true>(a, part, s);
-  return launch_form<T, DP, CAP, BIAS, false>(a, part, s);
+  const FewPlan p = plan(a.docs, a.kv_heads, a.group, a.max_q, a.max_k);
+  const bool one = (int64_t)a.docs * a.kv_heads * p.row_tiles * p.chunks > kSeqCus;
+  if (a.rest)
+    return one ? launch_form<T, DP, CAP, BIAS, true, 1>(a, p, part, s)
+               : launch_form<T, DP, CAP, BIAS, true, 2>(a, p, part, s);
+  return one ? launch_form<T, DP, CAP, BIAS, false, 1>(a, p, part, s)
+             : launch_form<T, DP, CAP, BIAS, false, 2>(a, p, part, s);
 }
 
 template <class T, int DP>

@@ -36,13 +36,6 @@ __device__ inline void copy_words(u32x4 buf, int voff, uint32_t lds) {
                : "memory");
 }
 
-// Sum over the wavefront's four rows of 16 lanes, on all of them.
-__device__ inline float sum_rows(float x) {
-  const uint32_t u = __builtin_bit_cast(uint32_t, x);
-  const u32x2 a = __builtin_amdgcn_permlane16_swap(u, u, false, false);
-  return sum_halves(word_float(a[0]) + word_float(a[1]));
-}
-
 // Adds the four wavefronts' results; true on the one (the first) that has the sum then.
 template <int DT>
 __device__ __forceinline__ bool add_waves(f32x16 *acc, char *lds) {

@@ -86,22 +86,42 @@ __device__ inline float key_value(uint64_t k) {
 }
 __device__ inline int64_t key_index(uint64_t k) { return 0xffffffffu - (uint32_t)k; }
 
-// Running sums at the maximum m (raw units; kLowest before the first entry).
+// Running sums at the maximum m (raw units; kLowest before the first entry). A term's
+// exponent is d = fl(x c2 - r), one instruction, with r = fl(m c2) in m c2's place; what r is
+// off by is taken out of the sums' logarithm. Where m is so large that this would be many
+// units, d = (x - m) c2.
 struct Sums {
   float m, a, b;
 };
+__device__ inline bool near_zero(float r) { return __builtin_fabsf(r) <= 1e6f; }
+// the reference less m c2
+__device__ inline float ref_error(float m, float c2) {
+  const float r = m * c2;
+  return near_zero(r) ? -__builtin_fmaf(m, c2, -r) : 0.f;
+}
 __device__ inline void raise(Sums &s, float m, float c2) {
-  const float d = fmaxf((s.m - m) * c2, -1e4f);   // (finite: the sums may be 0)
+  const float d = fmaxf(__builtin_fmaf(s.m - m, c2, ref_error(s.m, c2) - ref_error(m, c2)),
+                        -1e4f);   // (finite: the sums may be 0)
   const float f = fast_exp2(d);
   s.b = (s.b + s.a * d) * f;
   s.a *= f;
   s.m = m;
 }
-__device__ inline void add(Sums &s, float x, float c2) {
-  const float d = (x - s.m) * c2;
+__device__ inline void add(Sums &s, float d) {
   const float e = fast_exp2(d);
   s.a += e;
-  s.b = __builtin_fmaf(e, fmaxf(d, -200.f), s.b);   // (a ruled out entry: 0 times -200)
+  s.b = __builtin_fmaf(e, max2(d, -200.f), s.b);   // (a ruled out entry: 0 times -200)
+}
+template <int M, int N>
+__device__ inline void add_all(Sums &s, const float (&x)[M][N], float c2) {
+  const float r = s.m * c2;
+  if (near_zero(r)) {
+#pragma unroll
+    for (int i = 0; i < M * N; ++i) add(s, __builtin_fmaf(x[i / N][i % N], c2, -r));
+  } else {
+#pragma unroll
+    for (int i = 0; i < M * N; ++i) add(s, (x[i / N][i % N] - s.m) * c2);
+  }
 }
 __device__ inline Sums joined(Sums x, Sums y, float c2) {
   const float m = fmaxf(x.m, y.m);
@@ -118,6 +138,10 @@ __device__ inline uint64_t max64(uint64_t a, uint64_t b) { return a > b ? a : b;
 struct RowOut {
   float lse, logp, entropy;
 };
+// log of the sum of e^(scale (x - m))
+__device__ inline float log_sum(const Sums &s, float c2) {
+  return __builtin_fmaf(kLn2, ref_error(s.m, c2), logf(s.a));
+}
 // x_t: the given entry (only read if there is one)
 __device__ inline RowOut finish(const Sums &s, float scale, bool has, float xt) {
   RowOut r;
@@ -125,16 +149,16 @@ __device__ inline RowOut finish(const Sums &s, float scale, bool has, float xt) 
     const float inf = __builtin_inff();
     return RowOut{-inf, has ? -inf : 0.f, 0.f};
   }
-  const float la = logf(s.a);
+  const float c2 = scale * kLog2e, la = log_sum(s, c2);
   r.lse = __builtin_fmaf(scale, s.m, la);
   r.logp = has ? __builtin_fmaf(scale, xt - s.m, -la) : 0.f;
-  r.entropy = la - kLn2 * (s.b / s.a);
+  r.entropy = logf(s.a) - kLn2 * (s.b / s.a);
   return r;
 }
 __device__ inline float alt_logp(const Sums &s, float scale, uint64_t key) {
   if (key == 0) return __builtin_nanf("");
   if (s.a == 0.f) return -__builtin_inff();
-  return __builtin_fmaf(scale, key_value(key) - s.m, -logf(s.a));
+  return __builtin_fmaf(scale, key_value(key) - s.m, -log_sum(s, scale * kLog2e));
 }
 
 // ------------------------------------------------------------------ short rows
@@ -153,20 +177,12 @@ __global__ __launch_bounds__(kThreads) void logprob_wave(const LogprobArgs a) {
   for (int v = 0; v < VL; ++v) {
     load_some<DT>(p, v * 64 + lane, a.width, -__builtin_inff(), x[v]);
 #pragma unroll
-    for (int i = 0; i < kVec; ++i) m = fmaxf(m, x[v][i]);
+    for (int i = 0; i < kVec; i += 2) m = max3(m, x[v][i], x[v][i + 1]);
   }
-#pragma unroll
-  for (int o = 32; o; o >>= 1) m = fmaxf(m, __shfl_xor(m, o));
-  Sums s{m, 0.f, 0.f};
-#pragma unroll
-  for (int v = 0; v < VL; ++v)
-#pragma unroll
-    for (int i = 0; i < kVec; ++i) add(s, x[v][i], c2);
-#pragma unroll
-  for (int o = 32; o; o >>= 1) {
-    s.a += __shfl_xor(s.a, o);
-    s.b += __shfl_xor(s.b, o);
-  }
+  Sums s{wave_max(m), 0.f, 0.f};
+  add_all(s, x, c2);
+  s.a = wave_sum(s.a);
+  s.b = wave_sum(s.b);
   const int64_t t = a.target ? a.target[row] : -1;
   const bool has = t >= 0 && t < a.width;
   if (lane == 0) {
@@ -294,8 +310,8 @@ __device__ inline void by_passes(TopShared &sh, const char *p, int64_t n, int k,
 // A thread's share of a block's range [0, n) at p (index `first` of the row on): its sums, and
 // with KEYS the key of its largest entry.
 template <int DT, bool KEYS>
-__device__ inline Sums range_pass(const char *p, int64_t first, int64_t n, float c2,
-                                  uint64_t *key) {
+__device__ __forceinline__ Sums range_pass(const char *p, int64_t first, int64_t n, float c2,
+                                           uint64_t *key) {
   constexpr int kVec = Elem<DT>::kVec, kUnroll = 4;
   const int64_t nv = (n + kVec - 1) / kVec;
   const float inf = __builtin_inff();
@@ -313,19 +329,20 @@ __device__ inline Sums range_pass(const char *p, int64_t first, int64_t n, float
     }
 #pragma unroll
     for (int u = 0; u < kUnroll; ++u) {
-      top[u] = x[u][0];
+      top[u] = max3(x[u][0], x[u][1], x[u][2]);
 #pragma unroll
-      for (int i = 1; i < kVec; ++i) top[u] = fmaxf(top[u], x[u][i]);
-      if (top[u] > best) {
-        best = top[u];
-        if (KEYS) best_v = v0 + u * kThreads;
+      for (int i = 3; i < kVec; i += 2) top[u] = max3(top[u], x[u][i], x[u][i + 1 < kVec ? i + 1 : i]);
+      if (KEYS) {
+        if (top[u] > best) {
+          best = top[u];
+          best_v = v0 + u * kThreads;
+        }
+      } else {
+        best = max2(best, top[u]);
       }
     }
-    raise(s, fmaxf(s.m, best), c2);
-#pragma unroll
-    for (int u = 0; u < kUnroll; ++u)
-#pragma unroll
-      for (int i = 0; i < kVec; ++i) add(s, x[u][i], c2);
+    raise(s, max2(s.m, best), c2);
+    add_all(s, x, c2);
   };
   int64_t v = threadIdx.x;
   for (; (v + (kUnroll - 1) * kThreads + 1) * kVec <= n; v += kUnroll * kThreads)
@@ -345,11 +362,9 @@ __device__ inline Sums range_pass(const char *p, int64_t first, int64_t n, float
 
 // The block's sums, the same on every thread.
 __device__ inline Sums block_sums(Sums s, float c2, float (*red)[3]) {
-#pragma unroll
-  for (int o = 32; o; o >>= 1) {
-    Sums y{__shfl_xor(s.m, o), __shfl_xor(s.a, o), __shfl_xor(s.b, o)};
-    s = joined(s, y, c2);
-  }
+  raise(s, wave_max(s.m), c2);
+  s.a = wave_sum(s.a);
+  s.b = wave_sum(s.b);
   const int wave = threadIdx.x >> 6;
   if ((threadIdx.x & 63) == 0) {
     red[wave][0] = s.m;

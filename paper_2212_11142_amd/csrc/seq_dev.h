@@ -80,6 +80,12 @@ __device__ inline float max3(float a, float b, float c) {
   return r;
 }
 
+__device__ inline float max2(float a, float b) {
+  float r;
+  asm("v_max_f32 %0, %1, %2" : "=v"(r) : "v"(a), "v"(b));
+  return r;
+}
+
 // Sum and maximum over a lane and the one 32 away.
 __device__ inline float sum_halves(float x) {
   const uint32_t u = __builtin_bit_cast(uint32_t, x);
@@ -90,6 +96,36 @@ __device__ inline float max_halves(float x) {
   const uint32_t u = __builtin_bit_cast(uint32_t, x);
   const u32x2 r = __builtin_amdgcn_permlane32_swap(u, u, false, false);
   return fmaxf(word_float(r[0]), word_float(r[1]));
+}
+
+// Sum and maximum over the wavefront, on every lane, without LDS: neighbours, pairs, halves
+// of 8 and rows of 16 mirrored, then rows and halves swapped.
+template <int CTRL>
+__device__ inline float moved(float x) {
+  const int u = __builtin_bit_cast(int, x);
+  return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(u, u, CTRL, 0xf, 0xf, false));
+}
+// over the four rows of 16 lanes
+__device__ inline float sum_rows(float x) {
+  const uint32_t u = __builtin_bit_cast(uint32_t, x);
+  const u32x2 r = __builtin_amdgcn_permlane16_swap(u, u, false, false);
+  return sum_halves(word_float(r[0]) + word_float(r[1]));
+}
+__device__ inline float wave_sum(float x) {
+  x += moved<0xb1>(x);    // quad_perm 1 0 3 2
+  x += moved<0x4e>(x);    // quad_perm 2 3 0 1
+  x += moved<0x141>(x);   // row_half_mirror
+  x += moved<0x140>(x);   // row_mirror
+  return sum_rows(x);
+}
+__device__ inline float wave_max(float x) {
+  x = fmaxf(x, moved<0xb1>(x));
+  x = fmaxf(x, moved<0x4e>(x));
+  x = fmaxf(x, moved<0x141>(x));
+  x = fmaxf(x, moved<0x140>(x));
+  const uint32_t u = __builtin_bit_cast(uint32_t, x);
+  const u32x2 r = __builtin_amdgcn_permlane16_swap(u, u, false, false);
+  return max_halves(fmaxf(word_float(r[0]), word_float(r[1])));
 }
 
 // ------------------------------------------------------------------ LDS tiles

@@ -83,12 +83,16 @@ class Documents:
         self.k_full = self.k_disjoint and sum(k_len) == self.k_rows
         self.n = n
         self.max_q, self.max_k = max(q_len, default=0), max(k_len, default=0)
-        rows = [qb, [a + b for a, b in zip(qb, q_len)], kb, [a + b for a, b in zip(kb, k_len)]]
-        if prefix is not None:
-            rows.append([int(x) for x in prefix])
-        self._dev = torch.tensor(rows, dtype=torch.int32).reshape(len(rows), n).cuda()
-        self.q_begin, self.q_end, self.k_begin, self.k_end = self._dev[:4]
-        self.prefix = self._dev[4] if prefix is not None else None
+        rows = [qb, [a + b for a, b in zip(qb, q_len)], kb, [a + b for a, b in zip(kb, k_len)],
+                [0] * n if prefix is None else [int(x) for x in prefix]]
+        # the calls get the documents with the longest first: their blocks start first, and
+        # the short ones fill the device's end
+        order = sorted(range(n), key=lambda d: -q_len[d] * k_len[d])
+        both = torch.tensor([rows, [[r[d] for d in order] for r in rows]], dtype=torch.int32)
+        both = both.reshape(2, 5, n).cuda()
+        self.q_begin, self.q_end, self.k_begin, self.k_end, pre = both[0]
+        self.prefix = None if prefix is None else pre
+        self.sorted = both[1]
 
     @classmethod
     def on_device(cls, q_begin, q_end, k_begin, k_end, q_rows, k_rows, max_q, max_k, prefix=None):
@@ -105,6 +109,7 @@ class Documents:
                 raise ValueError("ranges must be contiguous int32 CUDA vectors of one length")
         self.q_begin, self.q_end, self.k_begin, self.k_end = ts[:4]
         self.prefix = prefix
+        self.sorted = ts + [None] * (5 - len(ts))    # (in the order given)
         self.n = int(q_begin.shape[0])
         self.q_rows, self.k_rows = int(q_rows), int(k_rows)
         self.max_q, self.max_k = int(max_q), int(max_k)
@@ -166,9 +171,9 @@ class Attention:
         s.dtype, s.heads, s.kv_heads, s.dim = _dtype_code(dtype), heads, kv_heads, dim
         s.n_docs, s.q_rows, s.k_rows = docs.n, docs.q_rows, docs.k_rows
         s.max_q, s.max_k = min(docs.max_q, docs.q_rows), min(docs.max_k, docs.k_rows)
-        s.q_begin, s.q_end = docs.q_begin.data_ptr(), docs.q_end.data_ptr()
-        s.k_begin, s.k_end = docs.k_begin.data_ptr(), docs.k_end.data_ptr()
-        s.prefix = docs.prefix.data_ptr() if docs.prefix is not None else None
+        qb, qe, kb, ke, pre = docs.sorted
+        s.q_begin, s.q_end, s.k_begin, s.k_end = (t.data_ptr() for t in (qb, qe, kb, ke))
+        s.prefix = pre.data_ptr() if docs.prefix is not None else None
         s.causal = 1 if causal else 0
         s.scale = 1.0 / math.sqrt(dim) if scale is None else float(scale)
         s.cap = float(cap)
