@@ -22,11 +22,9 @@ constexpr int kRowBlocks = 512;    // blocks of the row pass, at most
 constexpr float kP16 = 12.f;       // fp16: log2 of the factor of P
 constexpr int kSkew = 16 * 64;      // floats of a wavefront's skewed values
 
-// Rows of a step (the tiles that go through LDS while a block's own stay).
-template <int DP>
-struct GradTiles {
-  static constexpr int kStep = DP == 128 ? 32 : 64;
-};
+// Queries of a step of dK and dV: as many as leave room for three blocks of head size 64, or
+// two of 128, in LDS.
+constexpr int kv_step(int dp, bool narrow) { return narrow || dp == 128 ? 32 : 64; }
 
 // Starts the copy of one word per lane into LDS.
 __device__ inline void copy_words(u32x4 buf, int voff, uint32_t lds) {
@@ -193,7 +191,7 @@ template <class T, int DP, bool CAP, int BIAS, bool NARROW>
 __device__ __forceinline__ void grad_kv(const AttnGradArgs &ga, int row_blocks, int id, char *lds,
                                         float *red) {
   constexpr int KS = DP / 16, DT = DP / 32;
-  constexpr int kBQ = NARROW ? 32 : GradTiles<DP>::kStep;    // queries of a step
+  constexpr int kBQ = kv_step(DP, NARROW);     // queries of a step
   constexpr int kTile = kBQ * DP * 2;
   constexpr int kBK = NARROW ? 32 : 128;       // keys of a block
   constexpr int kParts = NARROW ? 4 : 1;       // wavefronts (or the block) with own steps
@@ -249,7 +247,9 @@ __device__ __forceinline__ void grad_kv(const AttnGradArgs &ga, int row_blocks, 
     if (sixty4 < kBQ / 32)
       copy_words(row_buffer(reinterpret_cast<const char *>(ga.rows) +
                                 ((int64_t)head * a.q_rows + q0) * 8, i, rows, 8, 8),
-                 (sixty4 * 64 + lane) * 4, lds_address(rows_lds) + buf * kBQ * 8 + sixty4 * 256);
+                 // (32 log-sums, then their 32 D)
+                 (sixty4 * 64 + 2 * (lane & 31) + h) * 4,
+                 lds_address(rows_lds) + buf * kBQ * 8 + sixty4 * 256);
   };
   {
     TileCopy<DP, kBK, 4> vc;
@@ -306,7 +306,7 @@ __device__ __forceinline__ void grad_kv(const AttnGradArgs &ga, int row_blocks, 
       const uint32_t tile = lds_address(tiles) + buf * 2 * kTile;
       const uint32_t qr = rd.at(tile, rd.row), qc0 = rd.at(tile, rd.col);
       const uint32_t vr = rd.at(lds_address(vt), rd.row);
-      const char *rows = rows_lds + (buf * kBQ + sub + 4 * h) * 8;
+      const char *rows = rows_lds + (buf * kBQ + sub) * 8 + 16 * h;
       f32x16 s = {}, dp = {};
 #pragma unroll
       for (int k = 0; k < KS; ++k) s = T::mfma(row_operand<DP>(qr, sub, k), kf[k], s);
@@ -316,13 +316,12 @@ __device__ __forceinline__ void grad_kv(const AttnGradArgs &ga, int row_blocks, 
       const bool masked = i0 < i_whole || i0 + 32 > lq;
 #pragma unroll
       for (int g = 0; g < 4; ++g) {   // (dP - D) dZ/dS first: the capped products then are done
-        const f32x4 x0 = *reinterpret_cast<const f32x4 *>(rows + 64 * g);
-        const f32x4 x1 = *reinterpret_cast<const f32x4 *>(rows + 64 * g + 16);
+        const f32x4 delta = *reinterpret_cast<const f32x4 *>(rows + 128 + 32 * g);
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
           const int e = 4 * g + r;
           s[e] = score_x<CAP>(s[e], sc);
-          dp[e] -= r < 2 ? x0[2 * r + 1] : x1[2 * r - 3];
+          dp[e] -= delta[r];
           if (CAP) dp[e] *= cap_slope(s[e]);
         }
       }
@@ -354,15 +353,14 @@ __device__ __forceinline__ void grad_kv(const AttnGradArgs &ga, int row_blocks, 
           if (row_of(e) < lo || row_of(e) >= hi) s[e] = -__builtin_inff();
         }
       }
-      asm volatile("" ::: "memory");   // reads the rows again rather than keep 32 registers
+      asm volatile("" ::: "memory");
 #pragma unroll
       for (int g = 0; g < 4; ++g) {
-        const f32x4 x0 = *reinterpret_cast<const f32x4 *>(rows + 64 * g);
-        const f32x4 x1 = *reinterpret_cast<const f32x4 *>(rows + 64 * g + 16);
+        const f32x4 lse = *reinterpret_cast<const f32x4 *>(rows + 32 * g);
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
           const int e = 4 * g + r;
-          s[e] = fast_exp2(__builtin_fmaf(s[e], f.a, off - (r < 2 ? x0[2 * r] : x1[2 * r - 4])));
+          s[e] = fast_exp2(__builtin_fmaf(s[e], f.a, off - lse[r]));
           dp[e] *= ps.kHalf ? s[e] * ds_scale : s[e];
         }
       }
@@ -393,7 +391,7 @@ __device__ __forceinline__ void grad_kv(const AttnGradArgs &ga, int row_blocks, 
   store_row<T, DT>(ga.dv + (int64_t)(t.b0 + key) * ga.dv_row + kvh * ga.dv_head, ok, a.bytes, dv,
                    exp2f(-p0), lane);
   store_row<T, DT>(ga.dk + (int64_t)(t.b0 + key) * ga.dk_row + kvh * ga.dk_head, ok, a.bytes, dk,
-                   a.scale * ldexpf(1.f, -ps.ds0), lane);
+                   a.scale * (CAP ? kCapSlope : 1.f) * ldexpf(1.f, -ps.ds0), lane);
 }
 
 // ------------------------------------------------------------------ dQ, table
@@ -409,7 +407,7 @@ template <class T, int DP, bool CAP, int BIAS, bool NARROW>
 __device__ __forceinline__ void grad_q(const AttnGradArgs &ga, int row_blocks, int id, char *lds,
                                        float *red) {
   constexpr int KS = DP / 16, DT = DP / 32;
-  constexpr int kBN = NARROW ? 32 : GradTiles<DP>::kStep;    // keys of a step
+  constexpr int kBN = 32;                      // keys of a step
   constexpr int kTile = kBN * DP * 2;
   constexpr int kBM = NARROW ? 32 : 128;
   constexpr int kParts = NARROW ? 4 : 1;
@@ -509,17 +507,15 @@ __device__ __forceinline__ void grad_q(const AttnGradArgs &ga, int row_blocks, i
     } else if (tile + 1 < n_tiles) {
       start(tile + 1, buf ^ 1);
     }
-#pragma unroll 1
-    for (int sub = 0; sub < kBN; sub += 32) {
-      const int key0 = tile * kBN + sub;
-      if (key0 >= lim_hi) break;
+    const int key0 = tile * kBN;
+    if (key0 < lim_hi) {
       const uint32_t tile_at = lds_address(kv_tiles) + buf * 2 * kTile;
       const uint32_t kr = rd.at(tile_at, rd.row), kcol = rd.at(tile_at, rd.col);
       f32x16 s = {}, dp = {};
 #pragma unroll
-      for (int k = 0; k < KS; ++k) s = T::mfma(row_operand<DP>(kr, sub, k), qf[k], s);
+      for (int k = 0; k < KS; ++k) s = T::mfma(row_operand<DP>(kr, 0, k), qf[k], s);
 #pragma unroll
-      for (int k = 0; k < KS; ++k) dp = T::mfma(row_operand<DP>(kr + kTile, sub, k), df[k], dp);
+      for (int k = 0; k < KS; ++k) dp = T::mfma(row_operand<DP>(kr + kTile, 0, k), df[k], dp);
       f32x16 z;   // x of the capped products
       if (CAP) {
 #pragma unroll
@@ -581,7 +577,7 @@ __device__ __forceinline__ void grad_q(const AttnGradArgs &ga, int row_blocks, i
       for (int k = 0; k < 2; ++k)
 #pragma unroll
         for (int c = 0; c < DT; ++c)
-          acc[c] = T::mfma(col_operand<DP>(kcol, sub + 16 * k, c), dr[k], acc[c]);
+          acc[c] = T::mfma(col_operand<DP>(kcol, 16 * k, c), dr[k], acc[c]);
     }
     if (!NARROW) copies_barrier();
   }
@@ -592,7 +588,7 @@ __device__ __forceinline__ void grad_q(const AttnGradArgs &ga, int row_blocks, i
   }
   if (writes)
     store_row<T, DT>(ga.dq + (int64_t)(t.b0 + row) * ga.dq_row + head * ga.dq_head, ok, a.bytes,
-                     acc, a.scale * ldexpf(1.f, -ps.ds0), lane);
+                     acc, a.scale * (CAP ? kCapSlope : 1.f) * ldexpf(1.f, -ps.ds0), lane);
 
   if (BIAS == kBiasTable) {
 #pragma unroll
@@ -667,10 +663,10 @@ int64_t tile_bound(int64_t rows, int64_t docs, int64_t longest, int tile) {
 
 // LDS of a block; lut: bytes of a head's table of biases, 0 without, and of the map to it.
 constexpr int pair_bytes(int dp, bool narrow, int lut, int map) {
-  const int step = narrow || dp == 128 ? 32 : 64, parts = narrow ? 4 : 1;
-  const int tiles = parts * 4 * step * dp * 2;
-  const int kv = tiles + (narrow ? 32 : 128) * dp * 2 + parts * (2 * step * 8 + lut) + map;
-  const int q = tiles + (lut ? 4 * kSkew * 4 + 5 * lut + map : 0);
+  const int step = kv_step(dp, narrow), parts = narrow ? 4 : 1;
+  const int kv = parts * 4 * step * dp * 2 + (narrow ? 32 : 128) * dp * 2 +
+                 parts * (2 * step * 8 + lut) + map;
+  const int q = parts * 4 * 32 * dp * 2 + (lut ? 4 * kSkew * 4 + 5 * lut + map : 0);
   return kv > q ? kv : q;
 }
 

@@ -17,7 +17,7 @@ namespace bgp {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kList = 2048;        // candidates for the alternatives
+constexpr int kList = 1024;        // candidates for the alternatives (8 blocks fit LDS)
 constexpr int kOwners = 512;       // groups of entries that may hold candidates
 constexpr int kWaveWidth = 1024;   // widest row of the one-wavefront form
 constexpr float kLowest = -3.4028234663852886e38f;
@@ -72,6 +72,35 @@ __device__ inline void load_some(const char *p, int64_t v, int64_t n, float fill
     for (int i = 0; i < kVec; ++i) x[i] = v * kVec + i < n ? load_one<DT>(p, v * kVec + i) : fill;
   }
 }
+
+// A row (or a block's range of one) from p on as aligned vectors: entry i is at place i +
+// skip, the first vector lacks its first `skip` places. (Vectors across 16-byte boundaries
+// cost about a seventh of the rate.)
+template <int DT>
+struct Aligned {
+  const char *p;
+  int skip;
+  int64_t end;      // places
+  __device__ Aligned(const char *row, int64_t n) {
+    skip = (int)((uintptr_t)row % 16) / Elem<DT>::kSize;
+    p = row - skip * Elem<DT>::kSize;
+    end = n + skip;
+  }
+  __device__ int64_t vectors() const { return (end + Elem<DT>::kVec - 1) / Elem<DT>::kVec; }
+  __device__ bool whole(int64_t v) const {
+    return v * Elem<DT>::kVec >= skip && (v + 1) * Elem<DT>::kVec <= end;
+  }
+  __device__ void load(int64_t v, float fill, float *x) const {
+    constexpr int kVec = Elem<DT>::kVec;
+    if (whole(v)) {
+      load_vec<DT>(p + v * 16, x);
+    } else {
+#pragma unroll
+      for (int i = 0; i < kVec; ++i)
+        x[i] = v * kVec + i >= skip && v * kVec + i < end ? load_one<DT>(p, v * kVec + i) : fill;
+    }
+  }
+};
 
 // Sort key of an entry: larger for a larger value, then for a lower index; 0 for a NaN.
 __device__ inline uint64_t key_of(float x, int64_t index) {
@@ -161,6 +190,25 @@ __device__ inline float alt_logp(const Sums &s, float scale, uint64_t key) {
   return __builtin_fmaf(scale, key_value(key) - s.m, -log_sum(s, scale * kLog2e));
 }
 
+// A row's target and its logit, asked for before the sums.
+struct Target {
+  bool has;
+  float x;
+};
+template <int DT>
+__device__ inline Target target_of(const LogprobArgs &a, int64_t row, const char *p) {
+  const int64_t t = a.target ? a.target[row] : -1;
+  const bool has = t >= 0 && t < a.width;
+  return Target{has, has ? load_one<DT>(p, t) : 0.f};
+}
+
+__device__ inline void write_row(const LogprobArgs &a, int64_t row, const Sums &s, const Target &t) {
+  const RowOut r = finish(s, a.scale, t.has, t.x);
+  if (a.logp) a.logp[row] = r.logp;
+  if (a.entropy) a.entropy[row] = r.entropy;
+  if (a.lse) a.lse[row] = r.lse;
+}
+
 // ------------------------------------------------------------------ short rows
 // One wavefront per row, the row in registers (VL vectors a lane).
 template <int DT, int VL>
@@ -171,6 +219,7 @@ __global__ __launch_bounds__(kThreads) void logprob_wave(const LogprobArgs a) {
   if (row >= a.rows) return;
   const char *p = static_cast<const char *>(a.x) + row * a.row * Elem<DT>::kSize;
   const float c2 = a.scale * kLog2e;
+  const Target given = target_of<DT>(a, row, p);
   float x[VL][kVec];
   float m = kLowest;
 #pragma unroll
@@ -183,14 +232,7 @@ __global__ __launch_bounds__(kThreads) void logprob_wave(const LogprobArgs a) {
   add_all(s, x, c2);
   s.a = wave_sum(s.a);
   s.b = wave_sum(s.b);
-  const int64_t t = a.target ? a.target[row] : -1;
-  const bool has = t >= 0 && t < a.width;
-  if (lane == 0) {
-    const RowOut r = finish(s, a.scale, has, has ? load_one<DT>(p, t) : 0.f);
-    if (a.logp) a.logp[row] = r.logp;
-    if (a.entropy) a.entropy[row] = r.entropy;
-    if (a.lse) a.lse[row] = r.lse;
-  }
+  if (lane == 0) write_row(a, row, s, given);
   uint64_t last = ~0ull;
   for (int k = 0; k < a.top; ++k) {     // the best entry below the last one
     uint64_t best = 0;
@@ -313,7 +355,8 @@ template <int DT, bool KEYS>
 __device__ __forceinline__ Sums range_pass(const char *p, int64_t first, int64_t n, float c2,
                                            uint64_t *key) {
   constexpr int kVec = Elem<DT>::kVec, kUnroll = 4;
-  const int64_t nv = (n + kVec - 1) / kVec;
+  const Aligned<DT> row(p, n);
+  const int64_t nv = row.vectors();
   const float inf = __builtin_inff();
   Sums s{kLowest, 0.f, 0.f};
   float best = -inf;                    // largest entry of this thread,
@@ -324,8 +367,8 @@ __device__ __forceinline__ Sums range_pass(const char *p, int64_t first, int64_t
 #pragma unroll
     for (int u = 0; u < kUnroll; ++u) {
       const int64_t v = v0 + u * kThreads;
-      if (kWhole) load_vec<DT>(p + v * 16, x[u]);
-      else load_some<DT>(p, v, n, -inf, x[u]);
+      if (kWhole) load_vec<DT>(row.p + v * 16, x[u]);
+      else row.load(v, -inf, x[u]);
     }
 #pragma unroll
     for (int u = 0; u < kUnroll; ++u) {
@@ -345,16 +388,20 @@ __device__ __forceinline__ Sums range_pass(const char *p, int64_t first, int64_t
     add_all(s, x, c2);
   };
   int64_t v = threadIdx.x;
-  for (; (v + (kUnroll - 1) * kThreads + 1) * kVec <= n; v += kUnroll * kThreads)
-    batch(v, std::true_type{});
+  if (!row.whole(v) && v < nv) {
+    batch(v, std::false_type{});
+    v += kUnroll * kThreads;
+  }
+  for (; row.whole(v + (kUnroll - 1) * kThreads); v += kUnroll * kThreads) batch(v, std::true_type{});
   for (; v < nv; v += kUnroll * kThreads) batch(v, std::false_type{});
   if (KEYS) {
     *key = 0;
     if (best_v < nv) {
       float x[kVec];
-      load_some<DT>(p, best_v, n, __builtin_nanf(""), x);
+      row.load(best_v, __builtin_nanf(""), x);
 #pragma unroll
-      for (int i = 0; i < kVec; ++i) *key = max64(*key, key_of(x[i], first + best_v * kVec + i));
+      for (int i = 0; i < kVec; ++i)
+        *key = max64(*key, key_of(x[i], first + best_v * kVec + i - row.skip));
     }
   }
   return s;
@@ -378,16 +425,6 @@ __device__ inline Sums block_sums(Sums s, float c2, float (*red)[3]) {
   return s;
 }
 
-template <int DT>
-__device__ inline void write_row(const LogprobArgs &a, int64_t row, const Sums &s, const char *p) {
-  const int64_t t = a.target ? a.target[row] : -1;
-  const bool has = t >= 0 && t < a.width;
-  const RowOut r = finish(s, a.scale, has, has ? load_one<DT>(p, t) : 0.f);
-  if (a.logp) a.logp[row] = r.logp;
-  if (a.entropy) a.entropy[row] = r.entropy;
-  if (a.lse) a.lse[row] = r.lse;
-}
-
 template <int DT, bool KEYS>
 __global__ __launch_bounds__(kThreads) void logprob_row(const LogprobArgs a) {
   constexpr int kVec = Elem<DT>::kVec;
@@ -395,23 +432,24 @@ __global__ __launch_bounds__(kThreads) void logprob_row(const LogprobArgs a) {
   const int64_t row = blockIdx.x;
   const char *p = static_cast<const char *>(a.x) + row * a.row * Elem<DT>::kSize;
   const float c2 = a.scale * kLog2e;
+  const Target given = target_of<DT>(a, row, p);
   uint64_t mine = 0;
   const Sums s = block_sums(range_pass<DT, KEYS>(p, 0, a.width, c2, &mine), c2, red);
-  if (threadIdx.x == 0) write_row<DT>(a, row, s, p);
+  if (threadIdx.x == 0) write_row(a, row, s, given);
   if (!KEYS) return;
   __shared__ TopShared sh;
   const uint64_t bound = bound_from_below(sh, mine, a.top);
   if (mine && mine >= bound) sh.owners[atomicAdd(&sh.n_owners, 1)] = threadIdx.x;
   __syncthreads();
   // a wavefront looks through one such thread's vectors at a time
-  const int64_t nv = (a.width + kVec - 1) / kVec;
+  const Aligned<DT> all(p, a.width);
   for (int o = threadIdx.x >> 6; o < sh.n_owners; o += 4)
-    for (int64_t w = sh.owners[o] + (int64_t)(threadIdx.x & 63) * kThreads; w < nv;
+    for (int64_t w = sh.owners[o] + (int64_t)(threadIdx.x & 63) * kThreads; w < all.vectors();
          w += 64 * kThreads) {
       float x[kVec];
-      load_some<DT>(p, w, a.width, __builtin_nanf(""), x);
+      all.load(w, __builtin_nanf(""), x);
 #pragma unroll
-      for (int i = 0; i < kVec; ++i) offer(sh, key_of(x[i], w * kVec + i), bound);
+      for (int i = 0; i < kVec; ++i) offer(sh, key_of(x[i], w * kVec + i - all.skip), bound);
     }
   __syncthreads();
   auto out = [&](int r, uint64_t k) {
@@ -485,6 +523,7 @@ __global__ __launch_bounds__(kThreads) void logprob_join(const LogprobArgs a, Sp
   const PartSpace sc = part_space(ws, a.rows, sp.parts, KEYS);
   const char *p = static_cast<const char *>(a.x) + row * a.row * Elem<DT>::kSize;
   const float c2 = a.scale * kLog2e;
+  const Target given = target_of<DT>(a, row, p);
   uint64_t mine = 0;
   const uint64_t *kr = sc.keys + row * sp.parts * 64;
   const int n = sp.parts * 64;
@@ -498,7 +537,7 @@ __global__ __launch_bounds__(kThreads) void logprob_join(const LogprobArgs a, Sp
     s = joined(s, Sums{q[0], q[1], q[2]}, c2);
   }
   s = block_sums(s, c2, red);
-  if (threadIdx.x == 0) write_row<DT>(a, row, s, p);
+  if (threadIdx.x == 0) write_row(a, row, s, given);
   if (!KEYS) return;
   __shared__ TopShared sh;
   const uint64_t bound = bound_from_below(sh, mine, a.top);
@@ -516,15 +555,17 @@ __global__ __launch_bounds__(kThreads) void logprob_join(const LogprobArgs a, Sp
   };
   if (sh.n_owners <= kOwners) {
     // 4 vectors side by side every 256 of the group's block
-    const int turns = (int)((sp.chunk / kVec + kThreads - 1) / kThreads), items = sh.n_owners * turns * 4;
+    const int turns = (int)((sp.chunk / kVec + 1 + kThreads - 1) / kThreads);
+    const int items = sh.n_owners * turns * 4;
     for (int i = threadIdx.x; i < items; i += kThreads) {
       const int g = sh.owners[i / (turns * 4)];
       const int64_t from = (g / 64) * sp.chunk, v = (int64_t)(i / 4 % turns) * kThreads + g % 64 * 4 + i % 4;
       const int64_t len = from + sp.chunk < a.width ? sp.chunk : a.width - from;
+      const Aligned<DT> range(p + from * Elem<DT>::kSize, len);
       float x[kVec];
-      load_some<DT>(p + from * Elem<DT>::kSize, v, len, __builtin_nanf(""), x);
+      range.load(v, __builtin_nanf(""), x);
 #pragma unroll
-      for (int e = 0; e < kVec; ++e) offer(sh, key_of(x[e], from + v * kVec + e), bound);
+      for (int e = 0; e < kVec; ++e) offer(sh, key_of(x[e], from + v * kVec + e - range.skip), bound);
     }
     __syncthreads();
     if (sh.n_list <= kList) {
@@ -566,8 +607,9 @@ __global__ __launch_bounds__(kThreads) void logprob_grad(const LogprobArgs a, in
   constexpr int kVec = Elem<DT>::kVec;
   // `threads` of the block's 256 share a row
   const int64_t unit = (int64_t)blockIdx.x * (kThreads / threads) + threadIdx.x / threads;
-  const int64_t row = unit / per_row;
-  if (row >= a.rows) return;
+  // the last rows first: the caches hold them still from the forward pass
+  const int64_t row = a.rows - 1 - unit / per_row;
+  if (row < 0) return;
   const int64_t first = unit % per_row * threads + threadIdx.x % threads;
   const int64_t step = (int64_t)per_row * threads;
   const char *p = static_cast<const char *>(a.x) + row * a.row * Elem<DT>::kSize;
@@ -580,10 +622,11 @@ __global__ __launch_bounds__(kThreads) void logprob_grad(const LogprobArgs a, in
   const float eh = (!none && a.g_entropy) ? a.g_entropy[row] * a.scale : 0.f;
   const float H = (!none && a.g_entropy) ? a.entropy[row] : 0.f;
   const float w = __builtin_fmaf(eh, H, g);
-  const int64_t nv = (a.width + kVec - 1) / kVec;
-  for (int64_t v = first; v < nv; v += step) {
+  const Aligned<DT> in(p, a.width);
+  q -= in.skip * Elem<DT>::kSize;
+  for (int64_t v = first; v < in.vectors(); v += step) {
     float x[kVec];
-    load_some<DT>(p, v, a.width, -__builtin_inff(), x);
+    in.load(v, -__builtin_inff(), x);
 #pragma unroll
     for (int i = 0; i < kVec; ++i) {
       const float lp = __builtin_fmaf(x[i], a.scale, -lse);
@@ -591,15 +634,15 @@ __global__ __launch_bounds__(kThreads) void logprob_grad(const LogprobArgs a, in
       // -p (g + h (log p + H)), 0 for a ruled out entry
       float y = -pr * __builtin_fmaf(eh, fmaxf(lp, -1e30f), w);
       if (none) y = 0.f;
-      if (v * kVec + i == t) y += g;
+      if (v * kVec + i - in.skip == t) y += g;
       x[i] = y;
     }
-    if ((v + 1) * kVec <= a.width) {
+    if (in.whole(v)) {
       store_vec<DT>(q + v * 16, x);
     } else {
 #pragma unroll
       for (int i = 0; i < kVec; ++i)
-        if (v * kVec + i < a.width) store_one<DT>(q, v * kVec + i, x[i]);
+        if (v * kVec + i >= in.skip && v * kVec + i < in.end) store_one<DT>(q, v * kVec + i, x[i]);
     }
   }
 }

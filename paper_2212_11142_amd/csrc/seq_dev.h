@@ -381,8 +381,10 @@ template <bool CAP>
 __device__ inline float score_x(float s, const ScoreScale &k) {
   return CAP ? __builtin_amdgcn_rcpf(-(1.f + fast_exp2(s * k.c))) : s;
 }
-// Derivative of the capped product, 1 - tanh^2 = 1 - (1 + 2 x)^2 = -4 x (1 + x).
-__device__ inline float cap_slope(float x) { return -4.f * x * (1.f + x); }
+// Derivative of the capped product, 1 - tanh^2 = 1 - (1 + 2 x)^2 = kCapSlope (x + x^2); the
+// constant is left to the results.
+constexpr float kCapSlope = -4.f;
+__device__ inline float cap_slope(float x) { return __builtin_fmaf(x, x, x); }
 
 enum BiasKind { kBiasNone = 0, kBiasSlope = 1, kBiasTable = 2 };
 
