@@ -187,6 +187,9 @@ struct GradScale {
 //
 // NARROW: a block has 32 keys, its wavefronts go over every fourth step of the queries with
 // LDS buffers of their own, and their sums are added at the end.
+//
+// Where few key heads and documents make few blocks of many steps, `shares` blocks take a
+// part of a tile's steps each and leave fp32 sums, which grad_shares adds in order.
 template <class T, int DP, bool CAP, int BIAS, bool NARROW>
 __device__ __forceinline__ void grad_kv(const AttnGradArgs &ga, int row_blocks, int id, char *lds,
                                         float *red) {
@@ -210,6 +213,8 @@ __device__ __forceinline__ void grad_kv(const AttnGradArgs &ga, int row_blocks, 
     lut += part * n;
   }
 
+  const int share = id % ga.shares;
+  id /= ga.shares;
   const int kvh = id % a.kv_heads;
   const DocTile t = find_tile<kBK>(a.kb, a.ke, a.docs, a.k_rows, id / a.kv_heads);
   if (t.doc < 0) return;
@@ -223,12 +228,15 @@ __device__ __forceinline__ void grad_kv(const AttnGradArgs &ga, int row_blocks, 
   const int key_lo = NARROW ? j0 : j0 + 32 * wave, key = key_lo + (lane & 31);
   // queries that see key j: those from first(j) on
   auto first = [&](int j) { return (a.causal && j >= prefix) ? max(j - shift, 0) : 0; };
+  auto limit = [&](int i) { return a.causal ? min(lk, max(i + shift + 1, prefix)) : lk; };
   const int i_start = first(j0) / kBQ * kBQ;
   const int i_wave = key_lo < lk ? first(key_lo) : lq;                 // any key of the wavefront
   const int i_whole = key_lo + 31 < lk ? first(key_lo + 31) : lq;      // all of its keys
   const int mine = key < lk ? first(key) : lq;
   const int steps = max((lq - i_start + kBQ - 1) / kBQ, 0);
-  const int total = steps * a.group;
+  // this block's part of the group's heads' steps
+  const int from = (int)((int64_t)steps * a.group * share / ga.shares);
+  const int total = (int)((int64_t)steps * a.group * (share + 1) / ga.shares);
 
   TileReader<DP> rd;
   rd.init(lane);
@@ -258,7 +266,7 @@ __device__ __forceinline__ void grad_kv(const AttnGradArgs &ga, int row_blocks, 
                         a.v_row, a.bytes),
              lds_address(vt));
   }
-  if (part < total) start(part, 0);
+  if (from + part < total) start(from + part, 0);
 
   u32x4 kf[KS];
   load_operand<DP>(a.k + (int64_t)t.b0 * a.k_row + kvh * a.k_head, a.k_row, key, lk, a.bytes, lane, kf);
@@ -277,7 +285,7 @@ __device__ __forceinline__ void grad_kv(const AttnGradArgs &ga, int row_blocks, 
 
   copies_barrier();
   int head_now = -1;
-  for (int n = part, buf = 0; n < total; n += kParts, buf ^= 1) {
+  for (int n = from + part, buf = 0; n < total; n += kParts, buf ^= 1) {
     if (BIAS != kBiasNone && n / steps != head_now) {   // the next head
       head_now = n / steps;
       const int head = kvh * a.group + head_now;
@@ -351,6 +359,8 @@ __device__ __forceinline__ void grad_kv(const AttnGradArgs &ga, int row_blocks, 
 #pragma unroll
         for (int e = 0; e < 16; ++e) {
           if (row_of(e) < lo || row_of(e) >= hi) s[e] = -__builtin_inff();
+          // a query that sees one key: dP - D is 0 but for the order of the sums
+          if (limit(i0 + 4 * h + row_of(e)) == 1) dp[e] = 0.f;
         }
       }
       asm volatile("" ::: "memory");
@@ -388,10 +398,56 @@ __device__ __forceinline__ void grad_kv(const AttnGradArgs &ga, int row_blocks, 
     if (!add_waves<DT>(dk, lds)) return;
   }
   const bool ok = key < lk;
+  const float fv = exp2f(-p0), fk = a.scale * (CAP ? kCapSlope : 1.f) * ldexpf(1.f, -ps.ds0);
+  if (ga.shares > 1) {
+    float *x = ga.kv_part + (((int64_t)share * a.k_rows + t.b0 + key) * a.kv_heads + kvh) * 2 * DP;
+    if (ok) {
+#pragma unroll
+      for (int c = 0; c < DT; ++c)
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+          f32x4 k4, v4;
+#pragma unroll
+          for (int r = 0; r < 4; ++r) {
+            k4[r] = dk[c][4 * g + r] * fk;
+            v4[r] = dv[c][4 * g + r] * fv;
+          }
+          *reinterpret_cast<f32x4 *>(x + 32 * c + 8 * g + 4 * h) = k4;
+          *reinterpret_cast<f32x4 *>(x + DP + 32 * c + 8 * g + 4 * h) = v4;
+        }
+    }
+    return;
+  }
   store_row<T, DT>(ga.dv + (int64_t)(t.b0 + key) * ga.dv_row + kvh * ga.dv_head, ok, a.bytes, dv,
-                   exp2f(-p0), lane);
+                   fv, lane);
   store_row<T, DT>(ga.dk + (int64_t)(t.b0 + key) * ga.dk_row + kvh * ga.dk_head, ok, a.bytes, dk,
-                   a.scale * (CAP ? kCapSlope : 1.f) * ldexpf(1.f, -ps.ds0), lane);
+                   fk, lane);
+}
+
+// dK and dV from the shares' sums: a block per tile and key head.
+template <class T, int DP>
+__global__ __launch_bounds__(kThreads) void grad_shares(const AttnGradArgs ga) {
+  const AttnArgs &a = ga.f;
+  constexpr int kPieces = DP / 8;
+  const int kvh = blockIdx.x % a.kv_heads;
+  const DocTile t = find_tile<128>(a.kb, a.ke, a.docs, a.k_rows, blockIdx.x / a.kv_heads);
+  if (t.doc < 0) return;
+  for (int i = threadIdx.x; i < 128 * 2 * kPieces; i += kThreads) {
+    const int row = t.tile * 128 + i / (2 * kPieces), piece = i % kPieces;
+    const bool v = i / kPieces % 2;
+    if (row >= t.b1 - t.b0 || piece * 16 >= a.bytes) continue;
+    f32x4 lo = {}, hi = {};
+    for (int s = 0; s < ga.shares; ++s) {
+      const float *x = ga.kv_part + (((int64_t)s * a.k_rows + t.b0 + row) * a.kv_heads + kvh) * 2 * DP +
+                       (v ? DP : 0) + piece * 8;
+      lo += *reinterpret_cast<const f32x4 *>(x);
+      hi += *reinterpret_cast<const f32x4 *>(x + 4);
+    }
+    char *to = v ? ga.dv + (int64_t)(t.b0 + row) * ga.dv_row + kvh * ga.dv_head
+                 : ga.dk + (int64_t)(t.b0 + row) * ga.dk_row + kvh * ga.dk_head;
+    *reinterpret_cast<u32x4 *>(to + piece * 16) =
+        u32x4{T::pack(lo[0], lo[1]), T::pack(lo[2], lo[3]), T::pack(hi[0], hi[1]), T::pack(hi[2], hi[3])};
+  }
 }
 
 // ------------------------------------------------------------------ dQ, table
@@ -468,7 +524,9 @@ __device__ __forceinline__ void grad_q(const AttnGradArgs &ga, int row_blocks, i
   load_operand<DP>(ga.dout + (int64_t)t.b0 * ga.do_row + head * ga.do_head, ga.do_row, row, lq,
                    a.bytes, lane, df);
   const int64_t at = (int64_t)head * a.q_rows + t.b0 + row;
-  const float lse = ok ? ga.rows[2 * at] : 0.f, delta = ok ? ga.rows[2 * at + 1] : 0.f;
+  // (a query that sees one key: dP - D is 0 but for the order of the sums)
+  const float lse = ok && lim > 1 ? ga.rows[2 * at] : __builtin_inff();
+  const float delta = ok ? ga.rows[2 * at + 1] : 0.f;
   GradScale<T> ps;
   ps.init(ga, row_blocks, red);
   const ScoreScale sc = score_scale<CAP>(a.scale, a.cap);
@@ -685,6 +743,22 @@ int tile_rows(const AttnArgs &f) {
   return wide <= kNarrowBlocks && pair_bytes(f, true) <= kLdsBytes - 1024 ? 32 : 128;
 }
 
+// Blocks that share a tile's steps. With slots for 2 blocks on each compute unit, a key tile's
+// 4 and a query tile's 3 products per step, r is what the longest block takes of the time that
+// the whole would with all of them busy (half of it under a causal mask, but not the longest
+// block's). Where that is more than 1.25, the tile is split so that no part is more than 2/3.
+// (15,169 rows, 12 heads over 3 key heads of 64: 417 -> 290 us with 3 shares; 4096 rows, 16 key
+// heads, r = 1.14: 283 us without, 297 with 2.)
+int share_count(const AttnArgs &f) {
+  if (tile_rows(f) == 32 || f.q_rows == 0 || f.k_rows == 0) return 1;
+  const double mean = (double)f.k_rows / f.docs;
+  const double r = (f.causal ? 2. : 1.) * 4. / 7. * 2 * kSeqCus * 128 * f.max_q /
+                   ((double)f.q_rows * mean * f.kv_heads);
+  if (r <= 1.25) return 1;
+  const int s = (int)(1.5 * r) + 1;
+  return s < 8 ? s : 8;
+}
+
 template <class T, int DP, bool CAP, int BIAS, bool NARROW>
 hipError_t launch_form(const AttnGradArgs &a, int row_blocks, hipStream_t s) {
   static LdsLimit limit;
@@ -693,12 +767,14 @@ hipError_t launch_form(const AttnGradArgs &a, int row_blocks, hipStream_t s) {
   hipError_t e = limit.set(reinterpret_cast<const void *>(&grad_pairs<T, DP, CAP, BIAS, NARROW>),
                            kLdsBytes - 1024);   // (the rest for what is static)
   if (e != hipSuccess) return e;
-  const int64_t kb = tile_bound(a.f.k_rows, a.f.docs, a.f.max_k, kTile) * a.f.kv_heads;
+  const int64_t kv_tiles = tile_bound(a.f.k_rows, a.f.docs, a.f.max_k, kTile) * a.f.kv_heads;
+  const int64_t kb = kv_tiles * a.shares;
   const int64_t units = tile_bound(a.f.q_rows, a.f.docs, a.f.max_q, kTile);
   const int64_t blocks = kb + units * a.f.heads;
   if (blocks > 0)
     grad_pairs<T, DP, CAP, BIAS, NARROW>
         <<<dim3((uint32_t)blocks), kThreads, lds, s>>>(a, row_blocks, (int)kb);
+  if (a.shares > 1) grad_shares<T, DP><<<dim3((uint32_t)kv_tiles), kThreads, 0, s>>>(a);
   if (BIAS == kBiasTable) {
     const int nb = bucket_count(a.f.buckets);
     grad_table<T><<<dim3((uint32_t)(a.f.heads * nb)), 256, 0, s>>>(a, (int)units, nb);
@@ -733,6 +809,8 @@ size_t attend_grad_bytes(const AttnArgs &f) {
   if (f.fp16) n += 2 * kRowBlocks;
   const int nb = bucket_count(f.buckets);
   n += up(tile_bound(f.q_rows, f.docs, f.max_q, tile_rows(f)) * f.heads * nb);
+  const int shares = share_count(f);
+  if (shares > 1) n += shares * (int64_t)f.k_rows * f.kv_heads * 2 * (f.bytes <= 128 ? 64 : 128);
   return (size_t)n * 4;
 }
 
@@ -742,6 +820,9 @@ hipError_t launch_attend_grad(const AttnGradArgs &args, void *ws, hipStream_t s)
   a.rows = static_cast<float *>(ws);
   a.bound = a.rows + up(2 * (int64_t)a.f.q_rows * a.f.heads);
   a.tpart = a.bound + (a.f.fp16 ? 2 * kRowBlocks : 0);
+  a.kv_part = a.tpart + up(tile_bound(a.f.q_rows, a.f.docs, a.f.max_q, tile_rows(a.f)) * a.f.heads *
+                           bucket_count(a.f.buckets));
+  a.shares = share_count(a.f);
   int64_t need = (int64_t)a.f.q_rows * a.f.heads;
   if (a.f.fp16 && (int64_t)a.f.k_rows * a.f.kv_heads > need) need = (int64_t)a.f.k_rows * a.f.kv_heads;
   int64_t blocks = (need + kThreads / 16 - 1) / (kThreads / 16);

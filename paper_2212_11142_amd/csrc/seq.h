@@ -55,6 +55,8 @@ struct AttnGradArgs {
   float *rows;                         // [heads][q_rows][2] log-sum, dout . out
   float *bound;                        // fp16: block maxima and the power of two dS is kept at
   float *tpart;                        // [tiles][heads][buckets] partial table gradients
+  float *kv_part;                      // [shares][k_rows][kv_heads][dK, dV], with shares
+  int32_t shares;                      // blocks of a key tile
 };
 
 hipError_t launch_attend(const AttnArgs &a, hipStream_t s);
