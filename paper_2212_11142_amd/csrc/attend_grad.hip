@@ -743,20 +743,17 @@ int tile_rows(const AttnArgs &f) {
   return wide <= kNarrowBlocks && pair_bytes(f, true) <= kLdsBytes - 1024 ? 32 : 128;
 }
 
-// Blocks that share a tile's steps. With slots for 2 blocks on each compute unit, a key tile's
-// 4 and a query tile's 3 products per step, r is what the longest block takes of the time that
-// the whole would with all of them busy (half of it under a causal mask, but not the longest
-// block's). Where that is more than 1.25, the tile is split so that no part is more than 2/3.
-// (15,169 rows, 12 heads over 3 key heads of 64: 417 -> 290 us with 3 shares; 4096 rows, 16 key
-// heads, r = 1.14: 283 us without, 297 with 2.)
+// Blocks that share a key tile's steps: as many as it takes to have a block of keys for each
+// of the 2 places on a compute unit. More would only add to the sums that are written and
+// read again. Steps with 1 / 2 / 3 / 4 / 8 shares: 8862 rows in 16 documents, 4 key heads of
+// 64 (308 tiles): 256 / 257 / 266 / 265 / 281 us; 4096 rows, 4 key heads of 128 (128 tiles):
+// - / 533 / 461 / 430 / 461 us; 1 key head (32 tiles): - / 839 / 616 / 505 / 375 us.
 int share_count(const AttnArgs &f) {
-  if (tile_rows(f) == 32 || f.q_rows == 0 || f.k_rows == 0) return 1;
-  const double mean = (double)f.k_rows / f.docs;
-  const double r = (f.causal ? 2. : 1.) * 4. / 7. * 2 * kSeqCus * 128 * f.max_q /
-                   ((double)f.q_rows * mean * f.kv_heads);
-  if (r <= 1.25) return 1;
-  const int s = (int)(1.5 * r) + 1;
-  return s < 8 ? s : 8;
+  if (tile_rows(f) == 32 || f.q_rows == 0) return 1;
+  const int64_t blocks = ((int64_t)f.k_rows + 127) / 128 * f.kv_heads;
+  if (blocks == 0) return 1;
+  const int64_t s = (2 * kSeqCus + blocks - 1) / blocks;
+  return (int)(s < 8 ? s : 8);
 }
 
 template <class T, int DP, bool CAP, int BIAS, bool NARROW>
