@@ -247,6 +247,62 @@ def test_attend_shared_keys_broadcast():
     c.check()
 
 
+# ------------------------------------------------------------------ larger calls
+# Enough heads that the blocks of 128 queries (or keys) fill the device: the forms that small
+# calls do not take.
+@pytest.mark.parametrize("dtype,dim", [("bf16", 64), ("fp16", 72), ("bf16", 128)])
+@pytest.mark.parametrize("cap,bias", [(0.0, "none"), (3.0, "slope"), (0.0, "one"), (20.0, "two")])
+@pytest.mark.parametrize("mask", ["full", "causal", "prefix"])
+def test_attend_large(dtype, dim, cap, bias, mask):
+    lens = [(200, 200), (129, 257), (1, 1), (65, 40), (300, 300)]
+    Case(dtype, lens, 48, 6, dim, causal=mask != "full", cap=cap, bias=bias, size=2.0,
+         prefix=[90, 257, 0, 3, 131] if mask == "prefix" else None).check()
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("value", [math.nan, math.inf, -math.inf])
+def test_attend_large_anything_in_masked_places(dtype, value):
+    import torch
+    c = Case(dtype, [(300, 300), (70, 150)], 96, 2, 72, causal=True, k_begin=[0, 400], k_rows=700)
+    for a, b in ((300, 400), (550, 700)):
+        c.k[a:b] = value
+        c.v[a:b] = value
+    c.check()
+    c.v[180, 0, 5] = value               # a key of the first document, seen from row 180 on
+    ref = c.oracle()
+    with np.errstate(invalid="ignore"):
+        ref["out_abs"][:, :, 5] = np.where(np.isfinite(ref["out"][:, :, 5]), ref["out_abs"][:, :, 5], 0)
+    c.check(ref=ref)
+    c.k[180, 0, :] = math.nan
+    b = c.run()
+    assert b.out[:180].isfinite().all() and b.out[180:300, :48].isnan().all()
+    assert b.out[180:300, 48:].isfinite().all()
+
+
+@pytest.mark.parametrize("dtype,heads,kv,dim,cap,bias,mask", [
+    ("bf16", 32, 2, 64, 0.0, "slope", "causal"),     # key tiles shared by 8 blocks
+    ("fp16", 32, 4, 128, 5.0, "two", "prefix"),
+    ("bf16", 32, 32, 64, 0.0, "two", "full"),        # one block per key tile and head
+    ("bf16", 32, 32, 128, 0.0, "none", "causal"),
+    ("fp16", 32, 16, 80, 10.0, "one", "causal")])
+def test_grad_large(dtype, heads, kv, dim, cap, bias, mask):
+    lens = [(620, 620), (300, 90), (90, 300), (1, 1), (33, 33)]
+    Case(dtype, lens, heads, kv, dim, causal=mask != "full", cap=cap, bias=bias, grad=True,
+         prefix=[200, 0, 260, 0, 40] if mask == "prefix" else None).check()
+
+
+def test_grad_of_one_key_is_zero():
+    """A softmax over one key does not depend on its score."""
+    for heads, lens in ((2, [(1, 1), (5, 1)]), (64, [(1, 1), (300, 1), (130, 1), (260, 260)])):
+        c = Case("bf16", lens, heads, heads, 64, causal=heads > 2, bias="one", grad=True)
+        b = c.run()
+        n = sum(a for a, k in lens if k == 1)
+        assert (b.dq[:n] == 0).all()
+        m = sum(k for _, k in lens if k == 1)
+        assert (b.dk[:m] == 0).all() and not (b.dv[:m] == 0).all()
+        c.check(b)
+
+
 # ------------------------------------------------------------------ few rows, long caches
 @pytest.mark.parametrize("dtype", TYPES)
 @pytest.mark.parametrize("lq", [1, 2, 5])
