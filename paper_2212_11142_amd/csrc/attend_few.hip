@@ -17,12 +17,13 @@ constexpr int kThreads = 256;
 constexpr int kKeys = 32;      // keys of a wavefront's step
 constexpr int kRows = 32;      // rows of a tile
 constexpr float kSlack = 8.f;  // as in the general form
-constexpr int kFewBlocks = 160;
-constexpr int kFewChunk = 2048;    // keys of a block, at most
+// Keys of a block, at most: 64 caches of 32,768 at most, 4 key heads of 128, with 512 / 1024 /
+// 2048 / unlimited: 445 / 429 / 445 / 442 us; the same, all full: 808 / 767 / 781 / 781.
+constexpr int kFewChunk = 1024;
 constexpr int kMaxValues = 4096;   // of the table for a group
 
-constexpr int few_tiles(int dp, int stages) {
-  const int tiles = stages * 8 * kKeys * dp * 2, sums = 4 * kRows * (dp + 4) * 4;
+constexpr int few_tiles(int dp) {
+  const int tiles = 8 * kKeys * dp * 2, sums = 4 * kRows * (dp + 4) * 4;
   return tiles > sums ? tiles : sums;
 }
 
@@ -36,16 +37,23 @@ FewPlan plan(int docs, int kv_heads, int group, int max_q, int max_k) {
   p.row_tiles = (int)((r + kRows - 1) / kRows);
   p.rows = (int)(r < kRows ? r : kRows);
   const int64_t units = (int64_t)docs * kv_heads * p.row_tiles;
-  // about 16 blocks per compute unit; where those would have less than 512 keys each, one per
-  // compute unit, of 128 keys at least
   auto up = [](int64_t x) { return (x + 127) / 128 * 128; };
-  int64_t c = up((int64_t)max_k * units / (16 * kSeqCus));
-  if (c < 512) {
-    c = up((int64_t)max_k * units / kSeqCus);
-    if (c > 512) c = 512;
+  // Few rows: about 16 blocks per compute unit; where those would have less than 512 keys each,
+  // one per compute unit, of 128 keys at least. Full tiles, whose sums are the larger: one per
+  // compute unit.
+  int64_t c = up(max_k * units / (16 * kSeqCus));
+  if (r > kRows || c < 512) {
+    c = up(max_k * units / kSeqCus);
+    if (r <= kRows && c > 512) c = 512;
     if (c < 128) c = 128;
   }
-  if (c > kFewChunk) c = kFewChunk;
+  if (r <= kRows && c > kFewChunk) c = kFewChunk;
+  // What the split saves, max_k - c keys of a block, has to pay for the second kernel and the
+  // sums between them. Without / with: 192 rows of 16 heads of 128 9.3 / 14.6 us, 1024 rows
+  // 19.6 / 50; 64 rows over 4096 keys, 8 heads of 128, 36 / 14; one row, 500 keys 9.1 / 9.1;
+  // 64 rows of their own 1000 keys 24.8 / 28.7.
+  if (max_k - c <= 384 + units * p.rows / 4) c = max_k > 0 ? up(max_k) : 128;
+  if (c > 1 << 30) c = 1 << 30;
   p.chunk = (int)c;
   p.chunks = (int)((max_k + c - 1) / c);
   if (p.chunks < 1) p.chunks = 1;
@@ -81,11 +89,12 @@ __device__ inline void write_quad(const AttnArgs &a, int row, int head, int d, f
         l == 0.f ? -__builtin_inff() : (m + __builtin_amdgcn_logf(l)) * kLn2;
 }
 
-// STAGES: tiles of K and of V that a wavefront has room for. Two where a compute unit has
-// one block (the next tile arrives while this one is used); one where it has more: two blocks
-// then fit, which overlap their starts and ends too.
-template <class T, int DP, bool CAP, int BIAS, bool REST, int STAGES>
-__global__ __launch_bounds__(kThreads, STAGES == 1 ? 2 : 1) void few_kernel(const AttnArgs a, const FewPlan p,
+// A wavefront has room for one tile of K and one of V, asked for again as soon as they have
+// been read: the eight wavefronts that a compute unit then holds keep more loads in flight than
+// four with two tiles each (64 caches of 2048 keys, 4 key heads of 128: 48 against 58 us; one
+// of 4095: 9.5 against 10.2).
+template <class T, int DP, bool CAP, int BIAS, bool REST>
+__global__ __launch_bounds__(kThreads, 2) void few_kernel(const AttnArgs a, const FewPlan p,
                                                           void *part) {
   constexpr int KS = DP / 16, DT = DP / 32;
   constexpr int kTile = kKeys * DP * 2;
@@ -95,7 +104,7 @@ __global__ __launch_bounds__(kThreads, STAGES == 1 ? 2 : 1) void few_kernel(cons
   __shared__ float ml[4][kRows][2];
   __shared__ int any_dirty;
   // tiles (then the wavefronts' sums), the group's rows of the table, buckets by distance
-  float *values = reinterpret_cast<float *>(lds + few_tiles(DP, STAGES));
+  float *values = reinterpret_cast<float *>(lds + few_tiles(DP));
 
   int id = blockIdx.x;
   const int kvh = id % a.kv_heads;
@@ -112,9 +121,12 @@ __global__ __launch_bounds__(kThreads, STAGES == 1 ? 2 : 1) void few_kernel(cons
   const int prefix = (a.causal && a.prefix) ? a.prefix[doc] : 0;
   const int shift = lk - lq;
   auto limit = [&](int i) { return a.causal ? min(lk, max(i + shift + 1, prefix)) : lk; };
-  const int lim_lo = limit(0), lim_hi = limit(lq - 1);
-  const int n_chunks = max((lim_hi + p.chunk - 1) / p.chunk, 1);
+  const int n_chunks = max((limit(lq - 1) + p.chunk - 1) / p.chunk, 1);
   if (chunk >= n_chunks || n_chunks > p.chunks) return;
+  // a tile within one head has a range of the queries
+  const int r_lo = rt * kRows, r_hi = r_lo + rows - 1;
+  const bool one_head = r_lo / lq == r_hi / lq;
+  const int lim_lo = limit(one_head ? r_lo % lq : 0), lim_hi = limit(one_head ? r_hi % lq : lq - 1);
   const int key_lo = chunk * p.chunk, key_hi = min(key_lo + p.chunk, lim_hi);
 
   const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6), h = lane >> 5;
@@ -131,26 +143,23 @@ __global__ __launch_bounds__(kThreads, STAGES == 1 ? 2 : 1) void few_kernel(cons
   TileCopy<DP, kKeys, 1> kc, vc;
   kc.init(0, lane, (int)a.k_row, a.bytes);
   vc.init(0, lane, (int)a.v_row, a.bytes);
-  char *mine = lds + wave * STAGES * 2 * kTile;     // K, V of each stage
+  char *mine = lds + wave * 2 * kTile;
   // (past the last key: nothing but zeros is copied, so that the waits below count evenly)
-  auto start_k = [&](int key, int buf) {
+  auto start_k = [&](int key) {
     kc.start(row_buffer(kbase, key, key < key_hi ? min(lk - key, kKeys) : 0, a.k_row, a.bytes),
-             lds_address(mine) + buf * 2 * kTile);
+             lds_address(mine));
   };
-  auto start_v = [&](int key, int buf) {
+  auto start_v = [&](int key) {
     vc.start(row_buffer(vbase, key, key < key_hi ? min(lk - key, kKeys) : 0, a.v_row, a.bytes),
-             lds_address(mine) + (buf * 2 + 1) * kTile);
+             lds_address(mine) + kTile);
   };
   u32x4 qf[KS];   // (asked for before the tiles: their arrival is waited for in order)
   load_operand<DP>(a.q + (int64_t)(q0 + i) * a.q_row + head * a.q_head, 0, live ? 0 : 1, 1,
                    a.bytes, lane, qf);
   int key = key_lo + wave * kKeys;
   if (key < key_hi) {
-#pragma unroll
-    for (int s = 0; s < STAGES; ++s) {
-      start_k(key + s * 4 * kKeys, s);
-      start_v(key + s * 4 * kKeys, s);
-    }
+    start_k(key);
+    start_v(key);
   }
 
   int reach = 0, span = 1, nb = 0;
@@ -180,16 +189,15 @@ __global__ __launch_bounds__(kThreads, STAGES == 1 ? 2 : 1) void few_kernel(cons
   if (threadIdx.x == 0) any_dirty = 0;
   __syncthreads();
 
-  for (int buf = 0; key < key_hi; key += 4 * kKeys, buf ^= STAGES - 1) {
-    // a tile's room is filled again as soon as it has been read
-    wait_copies<(2 * STAGES - 1) * kCopies>();
-    const uint32_t kb = rd.at(lds_address(mine) + buf * 2 * kTile, rd.row);
-    const uint32_t vb = rd.at(lds_address(mine) + (buf * 2 + 1) * kTile, rd.col);
+  const uint32_t kb = rd.at(lds_address(mine), rd.row);
+  const uint32_t vb = rd.at(lds_address(mine) + kTile, rd.col);
+  for (; key < key_hi; key += 4 * kKeys) {
+    wait_copies<kCopies>();       // K has arrived
     f32x16 s = {};
 #pragma unroll
     for (int k = 0; k < KS; ++k) s = T::mfma(row_operand<DP>(kb, 0, k), qf[k], s);
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-    start_k(key + STAGES * 4 * kKeys, buf);
+    start_k(key + 4 * kKeys);
 #pragma unroll
     for (int e = 0; e < 16; ++e) s[e] = __builtin_fmaf(score_x<CAP>(s[e], sc), sc.a, sc.b);
     if (BIAS == kBiasSlope) {
@@ -241,7 +249,7 @@ __global__ __launch_bounds__(kThreads, STAGES == 1 ? 2 : 1) void few_kernel(cons
     for (int k = 0; k < 2; ++k)
 #pragma unroll
       for (int w = 0; w < 4; ++w) pr[k][w] = T::pack(s[8 * k + 2 * w], s[8 * k + 2 * w + 1]);
-    wait_copies<(2 * STAGES - 1) * kCopies>();
+    wait_copies<kCopies>();       // V has
     bool clean = true;
     if (masked && lim_lo < lk) {                    // as in the general form
       uint32_t bad = 0;
@@ -269,7 +277,7 @@ __global__ __launch_bounds__(kThreads, STAGES == 1 ? 2 : 1) void few_kernel(cons
       }
     }
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-    start_v(key + STAGES * 4 * kKeys, buf);
+    start_v(key + 4 * kKeys);
   }
   l = sum_halves(l);
 
@@ -388,17 +396,17 @@ __global__ __launch_bounds__(kThreads) void few_join(const AttnArgs a, const Few
   write_quad<T, REST>(a, q0 + r % lq, kvh * a.group + r / lq, 4 * quad, x, top, ll);
 }
 
-template <class T, int DP, bool CAP, int BIAS, bool REST, int STAGES>
+template <class T, int DP, bool CAP, int BIAS, bool REST>
 hipError_t launch_form(const AttnArgs &a, const FewPlan &p, void *part, hipStream_t s) {
   static LdsLimit limit;
-  int lds = few_tiles(DP, STAGES);
+  int lds = few_tiles(DP);
   if (BIAS == kBiasTable)
     lds += a.group * bucket_count(a.buckets) * 4 + 2 * a.buckets.start[a.buckets.per_side - 1] + 4;
-  hipError_t e = limit.set(reinterpret_cast<const void *>(&few_kernel<T, DP, CAP, BIAS, REST, STAGES>),
-                           few_tiles(DP, STAGES) + kMaxValues * 4 + 2 * kMaxReach + 4);
+  hipError_t e = limit.set(reinterpret_cast<const void *>(&few_kernel<T, DP, CAP, BIAS, REST>),
+                           few_tiles(DP) + kMaxValues * 4 + 2 * kMaxReach + 4);
   if (e != hipSuccess) return e;
   const int64_t units = (int64_t)a.docs * a.kv_heads * p.row_tiles;
-  few_kernel<T, DP, CAP, BIAS, REST, STAGES>
+  few_kernel<T, DP, CAP, BIAS, REST>
       <<<dim3((uint32_t)(units * p.chunks)), kThreads, lds, s>>>(a, p, part);
   if (p.chunks > 1)
     few_join<T, DP, REST><<<dim3((uint32_t)(units * p.rows)), kThreads, 0, s>>>(a, p, part);
@@ -408,12 +416,8 @@ hipError_t launch_form(const AttnArgs &a, const FewPlan &p, void *part, hipStrea
 template <class T, int DP, bool CAP, int BIAS>
 hipError_t launch(const AttnArgs &a, void *part, hipStream_t s) {
   const FewPlan p = plan(a.docs, a.kv_heads, a.group, a.max_q, a.max_k);
-  const bool one = (int64_t)a.docs * a.kv_heads * p.row_tiles * p.chunks > kSeqCus;
-  if (a.rest)
-    return one ? launch_form<T, DP, CAP, BIAS, true, 1>(a, p, part, s)
-               : launch_form<T, DP, CAP, BIAS, true, 2>(a, p, part, s);
-  return one ? launch_form<T, DP, CAP, BIAS, false, 1>(a, p, part, s)
-             : launch_form<T, DP, CAP, BIAS, false, 2>(a, p, part, s);
+  if (a.rest) return launch_form<T, DP, CAP, BIAS, true>(a, p, part, s);
+  return launch_form<T, DP, CAP, BIAS, false>(a, p, part, s);
 }
 
 template <class T, int DP>
@@ -432,7 +436,12 @@ hipError_t by_bias(const AttnArgs &a, void *part, hipStream_t s) {
 }  // namespace
 
 // Small calls too: while the general form's blocks of 128 queries leave compute units idle,
-// 32 rows per block with the keys split over its wavefronts finish sooner.
+// 32 rows per block with the keys split over its wavefronts finish sooner. This form / the
+// general one at n of its blocks: 16 heads of 128, causal, n = 64 11.8 / 18.0 us, 128 19.6 /
+// 28.0, 160 30.0 / 33.3, 224 42.4 / 43.3, 256 65.7 / 64.0, 512 130 / 109; 16 heads of 64,
+// n = 224 21.3 / 30.0; documents of 200 rows, 8 heads of 64, n = 192 11.0 / 11.3, 256 12.4 / 11.6.
+constexpr int kFewBlocks = 224;
+
 bool attend_use_few(const AttnArgs &a) {
   if ((int64_t)a.group * bucket_count(a.buckets) > kMaxValues) return false;
   if ((int64_t)a.group * a.max_q <= kRows) return true;

@@ -355,6 +355,32 @@ def test_attend_cache_past_32_bit_offsets():
     assert torch.equal(got["out"], c.run().out)
 
 
+def test_large_calls_in_a_cache_past_32_bit_offsets():
+    """The forms for many query rows, and the gradient, over the last rows of such a cache."""
+    import types
+
+    import torch
+    from paper_2212_11142_amd import seq
+    H, D, n, rows = 192, 128, 130, (1 << 24) + 4096
+    c = Case("bf16", [(n, n)], H, 2, D, grad=True)
+    k = torch.zeros((rows, 2, D), dtype=torch.bfloat16, device="cuda")
+    v = torch.zeros_like(k)
+    assert k.numel() > 2 ** 31
+    k[-n:], v[-n:] = c.k, c.v
+    docs = seq.Documents([n], [n], k_begin=[rows - n], k_rows=rows)
+    att = seq.Attention(docs, H, 2, D, torch.bfloat16)
+    bufs = seq.AttendBuffers(att, grad=True)
+    bufs.dk.fill_(7.0)
+    bufs.dv.fill_(7.0)
+    seq.attend_into(att, c.q, k, v, bufs)
+    seq.attend_grad_into(att, c.q, k, v, c.dout, bufs)
+    torch.cuda.synchronize()
+    c.check(types.SimpleNamespace(out=bufs.out, lse=bufs.lse, dq=bufs.dq, dk=bufs.dk[-n:],
+                                  dv=bufs.dv[-n:]))
+    for d in (bufs.dk, bufs.dv):     # rows of no document keep their contents
+        assert bool((d[:-n] == 7.0).all())
+
+
 # ------------------------------------------------------------------ gradients
 @pytest.mark.parametrize("dtype", TYPES)
 @pytest.mark.parametrize("dim", [16, 64, 80, 128])
