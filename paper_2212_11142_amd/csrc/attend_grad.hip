@@ -729,8 +729,11 @@ constexpr int pair_bytes(int dp, bool narrow, int lut, int map) {
 }
 
 // The narrow form's tiles where the wide one's blocks would leave compute units idle, if
-// the table leaves room in LDS.
-constexpr int kNarrowBlocks = 256;
+// the table leaves room in LDS. Narrow / wide at n wide blocks: 3 documents of 333, 6 heads of
+// 80, n = 24 50 / 93 us; 8 documents of 250, 8 heads of 64, n = 256 51 / 61; one of 2560, n = 320
+// 114 / 151; 12 of 250, n = 384 74 / 64; 16 heads of 128, 1536 rows, n = 384 155 / 156; 2048
+// rows, n = 512 228 / 184.
+constexpr int kNarrowBlocks = 320;
 int pair_bytes(const AttnArgs &f, bool narrow) {
   const int dp = f.bytes <= 128 ? 64 : 128;
   if (f.buckets.per_side == 0) return pair_bytes(dp, narrow, 0, 0);
