@@ -19,7 +19,14 @@ namespace {
 constexpr int kThreads = 256;
 constexpr int kList = 1024;        // candidates for the alternatives (8 blocks fit LDS)
 constexpr int kOwners = 512;       // groups of entries that may hold candidates
-constexpr int kWaveWidth = 1024;   // widest row of the one-wavefront form
+// Alternatives up to which 64 groups' bound is tight enough. With 64 / 256 groups: 40
+// alternatives of one row of 10,000 10.9 / 12.7 us, of 200 rows of 131,072 38.6 / 35.0; 50: 11.2 /
+// 13.0 and 48.2 / 37.5.
+constexpr int kSixtyFour = 40;
+// Widest row of the one-wavefront form (64 entries a lane). 16,384 rows, this form / a block per
+// row: 1100 wide bf16 14.3 / 54.6 us, with 5 alternatives 24.1 / 115; 4096 wide bf16 26.4 / 43.0,
+// 38.1 / 95.9; 4096 wide fp32 42.3 / 41.1, 45.4 / 70.5.
+constexpr int kWaveWidth = 4096;
 constexpr float kLowest = -3.4028234663852886e38f;
 
 enum { kBf16 = GP_BF16, kFp16 = GP_FP16, kFp32 = GP_FP32 };
@@ -184,10 +191,12 @@ __device__ inline RowOut finish(const Sums &s, float scale, bool has, float xt) 
   r.entropy = logf(s.a) - kLn2 * (s.b / s.a);
   return r;
 }
-__device__ inline float alt_logp(const Sums &s, float scale, uint64_t key) {
-  if (key == 0) return __builtin_nanf("");
+__device__ inline float alt_logp(const Sums &s, float scale, float x) {
   if (s.a == 0.f) return -__builtin_inff();
-  return __builtin_fmaf(scale, key_value(key) - s.m, -log_sum(s, scale * kLog2e));
+  return __builtin_fmaf(scale, x - s.m, -log_sum(s, scale * kLog2e));
+}
+__device__ inline float alt_logp(const Sums &s, float scale, uint64_t key) {
+  return key ? alt_logp(s, scale, key_value(key)) : __builtin_nanf("");
 }
 
 // A row's target and its logit, asked for before the sums.
@@ -210,7 +219,9 @@ __device__ inline void write_row(const LogprobArgs &a, int64_t row, const Sums &
 }
 
 // ------------------------------------------------------------------ short rows
-// One wavefront per row, the row in registers (VL vectors a lane).
+// One wavefront per row, the row in registers (VL vectors a lane). The alternatives one by
+// one: the maximum of the lanes' maxima, the first vector and lane that hold it (so the lowest
+// index), which strike the entry out.
 template <int DT, int VL>
 __global__ __launch_bounds__(kThreads) void logprob_wave(const LogprobArgs a) {
   constexpr int kVec = Elem<DT>::kVec;
@@ -220,37 +231,62 @@ __global__ __launch_bounds__(kThreads) void logprob_wave(const LogprobArgs a) {
   const char *p = static_cast<const char *>(a.x) + row * a.row * Elem<DT>::kSize;
   const float c2 = a.scale * kLog2e;
   const Target given = target_of<DT>(a, row, p);
-  float x[VL][kVec];
+  float x[VL][kVec], top[VL];     // (top: of a vector)
   float m = kLowest;
+  auto top_of = [&](const float *y) {
+    float t = max3(y[0], y[1], y[2]);
+#pragma unroll
+    for (int i = 3; i < kVec; i += 2) t = max3(t, y[i], y[i + 1 < kVec ? i + 1 : i]);
+    return t;
+  };
+#pragma unroll
+  for (int v = 0; v < VL; ++v) load_some<DT>(p, v * 64 + lane, a.width, -__builtin_inff(), x[v]);
 #pragma unroll
   for (int v = 0; v < VL; ++v) {
-    load_some<DT>(p, v * 64 + lane, a.width, -__builtin_inff(), x[v]);
-#pragma unroll
-    for (int i = 0; i < kVec; i += 2) m = max3(m, x[v][i], x[v][i + 1]);
+    top[v] = top_of(x[v]);
+    m = max2(m, top[v]);
   }
   Sums s{wave_max(m), 0.f, 0.f};
   add_all(s, x, c2);
   s.a = wave_sum(s.a);
   s.b = wave_sum(s.b);
   if (lane == 0) write_row(a, row, s, given);
-  uint64_t last = ~0ull;
-  for (int k = 0; k < a.top; ++k) {     // the best entry below the last one
-    uint64_t best = 0;
+  bool more = true;
+  for (int k0 = 0; k0 < a.top; k0 += 64) {    // lane k of 64 keeps alternative k0 + k
+    float value = 0.f;
+    int at = -1;
+    for (int k = 0; k < min(a.top - k0, 64) && more; ++k) {
+      float best = top[0];
 #pragma unroll
-    for (int v = 0; v < VL; ++v)
+      for (int v = 1; v < VL; ++v) best = max2(best, top[v]);
+      best = wave_max(best);
+      more = false;
 #pragma unroll
-      for (int i = 0; i < kVec; ++i) {
-        const int64_t at = ((int64_t)v * 64 + lane) * kVec + i;
-        const uint64_t key = at < a.width ? key_of(x[v][i], at) : 0;
-        if (key < last) best = max64(best, key);
+      for (int v = 0; v < VL; ++v) {
+        const uint64_t same = more ? 0 : __ballot(top[v] == best);
+        if (same) {
+          const int owner = __builtin_ctzll(same);
+          int i0 = 0;
+#pragma unroll
+          for (int i = kVec - 1; i >= 0; --i) i0 = x[v][i] == best ? i : i0;
+          const int index = (v * 64 + owner) * kVec + __builtin_amdgcn_readlane(i0, owner);
+#pragma unroll
+          for (int i = 0; i < kVec; ++i)
+            if (lane == owner && i == i0) x[v][i] = __builtin_nanf("");
+          if (lane == owner) top[v] = top_of(x[v]);
+          // (past the row's end there are entries of -inf, after all of its own)
+          more = index < a.width;
+          if (lane == k && more) {
+            value = best;
+            at = index;
+          }
+        }
       }
-#pragma unroll
-    for (int o = 32; o; o >>= 1) best = max64(best, shfl_xor64(best, o));
-    if (lane == 0) {
-      a.top_logp[row * a.top + k] = alt_logp(s, a.scale, best);
-      a.top_id[row * a.top + k] = best ? key_index(best) : -1;
     }
-    last = best;
+    if (k0 + lane < a.top) {
+      a.top_logp[row * a.top + k0 + lane] = at < 0 ? __builtin_nanf("") : alt_logp(s, a.scale, value);
+      a.top_id[row * a.top + k0 + lane] = at;
+    }
   }
 }
 
@@ -270,7 +306,7 @@ __device__ inline uint64_t bound_from_below(TopShared &sh, uint64_t mine, int k)
     sh.n_owners = sh.n_list = 0;
     sh.best[0] = 0;
   }
-  if (k <= 32) {
+  if (k <= kSixtyFour) {
     uint64_t g = max64(mine, shfl_xor64(mine, 1));
     g = max64(g, shfl_xor64(g, 2));
     if (threadIdx.x % 4 == 0) sh.group[threadIdx.x / 4] = g;
@@ -427,7 +463,7 @@ __device__ inline Sums block_sums(Sums s, float c2, float (*red)[3]) {
 
 template <int DT, bool KEYS>
 __global__ __launch_bounds__(kThreads) void logprob_row(const LogprobArgs a) {
-  constexpr int kVec = Elem<DT>::kVec;
+  constexpr int kVec = Elem<DT>::kVec, kAhead = 2;
   __shared__ float red[4][3];
   const int64_t row = blockIdx.x;
   const char *p = static_cast<const char *>(a.x) + row * a.row * Elem<DT>::kSize;
@@ -441,16 +477,24 @@ __global__ __launch_bounds__(kThreads) void logprob_row(const LogprobArgs a) {
   const uint64_t bound = bound_from_below(sh, mine, a.top);
   if (mine && mine >= bound) sh.owners[atomicAdd(&sh.n_owners, 1)] = threadIdx.x;
   __syncthreads();
-  // a wavefront looks through one such thread's vectors at a time
+  // all of the block look through those threads' vectors
   const Aligned<DT> all(p, a.width);
-  for (int o = threadIdx.x >> 6; o < sh.n_owners; o += 4)
-    for (int64_t w = sh.owners[o] + (int64_t)(threadIdx.x & 63) * kThreads; w < all.vectors();
-         w += 64 * kThreads) {
-      float x[kVec];
-      all.load(w, __builtin_nanf(""), x);
+  const int turns = (int)((all.vectors() + kThreads - 1) / kThreads);
+  const int items = sh.n_owners * turns;
+  for (int n0 = threadIdx.x; n0 < items; n0 += kAhead * kThreads) {
+    float x[kAhead][kVec];
+    int64_t w[kAhead];
 #pragma unroll
-      for (int i = 0; i < kVec; ++i) offer(sh, key_of(x[i], w * kVec + i - all.skip), bound);
+    for (int u = 0; u < kAhead; ++u) {
+      const int n = n0 + u * kThreads;
+      w[u] = n < items ? sh.owners[n / turns] + (int64_t)(n % turns) * kThreads : all.vectors();
+      all.load(w[u], __builtin_nanf(""), x[u]);
     }
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u)
+#pragma unroll
+      for (int i = 0; i < kVec; ++i) offer(sh, key_of(x[u][i], w[u] * kVec + i - all.skip), bound);
+  }
   __syncthreads();
   auto out = [&](int r, uint64_t k) {
     a.top_logp[row * a.top + r] = alt_logp(s, a.scale, k);
@@ -466,12 +510,21 @@ struct SplitPlan {
   int parts;       // blocks of a row
   int64_t chunk;   // entries of a block
 };
+// One block per row where that fills the device, or where the rows are too short to pay for the
+// second kernel; fewer parts of more rows save less. Split / not, bf16, 5 alternatives: 1 row of
+// 40,000 11.1 / 11.4 us, of 60,000 11.2 / 13.2, of 131,072 11.7 / 17.4; 40 rows of 60,000 13.3 /
+// 13.6; 100 of 60,000 14.9 / 13.7, of 80,000 16.3 / 15.8, of 131,072 18.2 / 18.3; 200 of 60,000
+// 18.3 / 14.0, of 131,072 23.4 / 24.4; 300 of 20,000 14.5 / 11.9.
+constexpr int kSplitWidth = 49152;
 SplitPlan split_plan(int32_t rows, int32_t width) {
   SplitPlan p{1, width};
-  // one block per row where that fills the device, or the rows are short
-  if (rows >= 2 * kSeqCus || width <= 8192) return p;
+  if (rows >= kSeqCus || width <= kSplitWidth + 256 * (int64_t)rows) return p;
   int64_t parts = (4 * (int64_t)kSeqCus + rows - 1) / rows;
-  const int64_t most = width / 2048;            // (a vector or two per thread)
+  // A part has at least 4096 entries (2 vectors of 2-byte entries per thread): shorter ones save
+  // less than their keys cost the joining block, longer ones leave too few loads in flight. With
+  // at least 2048, 4096, 8192: 8 rows of 131,072 bf16, 20 alternatives, 16.0, 14.0, 13.4 us;
+  // 3 rows of 11,419, 33 alternatives, 18.0, 16.6, 20.3; 21 rows of 53,830 without, 9.6, 9.7, 9.6.
+  const int64_t most = width / 4096;
   if (parts > most) parts = most;
   if (parts < 2) return p;
   p.chunk = ((width + parts - 1) / parts + 63) / 64 * 64;
@@ -655,6 +708,8 @@ hipError_t forward(const LogprobArgs &a, void *ws, hipStream_t s) {
     const int vl = (a.width + 64 * kVec - 1) / (64 * kVec);
     if (vl <= 1) logprob_wave<DT, 1><<<grid, kThreads, 0, s>>>(a);
     else if (vl <= 2) logprob_wave<DT, 2><<<grid, kThreads, 0, s>>>(a);
+    else if (vl <= 4) logprob_wave<DT, 4><<<grid, kThreads, 0, s>>>(a);
+    else if (vl <= 8) logprob_wave<DT, 8><<<grid, kThreads, 0, s>>>(a);
     else logprob_wave<DT, kWaveWidth / (64 * kVec)><<<grid, kThreads, 0, s>>>(a);
     return hipGetLastError();
   }
@@ -680,9 +735,11 @@ template <int DT>
 hipError_t gradient(const LogprobArgs &a, hipStream_t s) {
   constexpr int kVec = Elem<DT>::kVec;
   const int64_t nv = (a.width + kVec - 1) / kVec;
-  // a wavefront per row up to 512 vectors, a block per row above; more blocks per row (each
-  // thread 4 vectors at least) while the rows do not fill the device
-  const int threads = nv <= 512 ? 64 : kThreads;
+  // A wavefront per row below 512 vectors, a block per row from there on; more blocks per row (each
+  // thread 4 vectors at least) while the rows do not fill the device. 16,384 rows, a wavefront / a
+  // block each: 512 bf16 10.4 / 19.3 us, 2048 bf16 23.5 / 30.1, 4096 bf16 46.5 / 44.3, 2048 fp32
+  // 45.8 / 42.8. Several blocks / one per row: 8 of 131,072 4.9 / 30, 300 of 65,536 16.4 / 25.3.
+  const int threads = nv < 512 ? 64 : kThreads;
   int64_t per_row = 1;
   if (threads == kThreads) {
     const int64_t want = (8 * (int64_t)kSeqCus + a.rows - 1) / a.rows, most = nv / (4 * kThreads);
