@@ -22,14 +22,18 @@ constexpr int kThreads = 256;
 // probabilities, fp16's) range, and the rescaling of the output is skipped almost always.
 constexpr float kSlack = 8.f;
 
-template <class T, int DP, bool CAP, int BIAS, bool REST>
-__global__ __launch_bounds__(kThreads, 2) void attend_kernel(const AttnArgs a) {
+// PARTS = 2: two groups of 4 wavefronts take every second tile each, with LDS buffers of their
+// own, and the first adds up their sums at the end.
+template <class T, int DP, bool CAP, int BIAS, bool REST, int PARTS>
+__global__ __launch_bounds__(kThreads * PARTS, 2) void attend_kernel(const AttnArgs a) {
   constexpr int KS = DP / 16;   // k-steps of the score product
   constexpr int DT = DP / 32;   // column blocks of V
   constexpr int kTile = kBN * DP * 2;
   extern __shared__ __align__(1024) char lds[];
-  char *kt = lds, *vt = lds + 2 * kTile;
-  float *lut = reinterpret_cast<float *>(lds + 4 * kTile);
+  const int lane = threadIdx.x & 63, h = lane >> 5;
+  const int wave = uniform(threadIdx.x >> 6) % 4, part = uniform(threadIdx.x >> 8);
+  char *kt = lds + part * 4 * kTile, *vt = kt + 2 * kTile;
+  float *lut = reinterpret_cast<float *>(lds + PARTS * 4 * kTile);
 
   // kv heads fastest: the blocks of one XCD (every 8th) then share few heads' keys; the
   // last tiles of a document, which see the most keys under a causal mask, come first
@@ -46,7 +50,6 @@ __global__ __launch_bounds__(kThreads, 2) void attend_kernel(const AttnArgs a) {
   const int tiles = (lq + kBM - 1) / kBM;
   const int i0 = (tiles - 1 - t.tile) * kBM;
 
-  const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6), h = lane >> 5;
   const int row_lo = i0 + 32 * wave;             // first query of the wavefront
   const int row = row_lo + (lane & 31);
   const int shift = lk - lq;                     // position of query 0
@@ -71,7 +74,7 @@ __global__ __launch_bounds__(kThreads, 2) void attend_kernel(const AttnArgs a) {
     vc.start(row_buffer(vbase, (int64_t)tile * kBN, n, a.v_row, a.bytes),
              lds_address(vt) + buf * kTile);
   };
-  if (n_tiles > 0) start(0, 0);
+  if (part < n_tiles) start(part, 0);
 
   u32x4 qf[KS];
   load_operand<DP>(a.q + (int64_t)t.b0 * a.q_row + head * a.q_head, a.q_row, row, lq, a.bytes, lane,
@@ -81,8 +84,8 @@ __global__ __launch_bounds__(kThreads, 2) void attend_kernel(const AttnArgs a) {
   if (BIAS == kBiasTable) {
     reach = a.buckets.start[a.buckets.per_side - 1];
     uint8_t *map = reinterpret_cast<uint8_t *>(lut + lut_size(reach));
-    fill_map(map, a.buckets, threadIdx.x, kThreads);   // (each thread reads what it wrote)
-    fill_lut<T>(lut, map, a.buckets, a.table, head, threadIdx.x, kThreads);
+    fill_map(map, a.buckets, threadIdx.x, kThreads * PARTS);   // (each thread reads what it wrote)
+    fill_lut<T>(lut, map, a.buckets, a.table, head, threadIdx.x, kThreads * PARTS);
   }
   if (BIAS == kBiasSlope) slope2 = a.slopes[head] * kLog2e;
   float steps[16];
@@ -95,11 +98,11 @@ __global__ __launch_bounds__(kThreads, 2) void attend_kernel(const AttnArgs a) {
   float m = -__builtin_inff(), l = 0.f;   // l: this lane's half of the row's sum
   bool dirty = false;
 
-  // one tile; `masked`: some row's limit may fall into it
-  auto step = [&](int tile, auto masked_tile) {
+  // one tile per part; `masked`: some row's limit may fall into it
+  auto step = [&](int turn, auto masked_tile) {
     constexpr bool masked = decltype(masked_tile)::value;
-    const int buf = tile & 1, key0 = tile * kBN;
-    if (tile + 1 < n_tiles) start(tile + 1, buf ^ 1);
+    const int tile = turn * PARTS + part, buf = turn & 1, key0 = tile * kBN;
+    if (tile + PARTS < n_tiles) start(tile + PARTS, buf ^ 1);
     if (key0 < lim_hi) {
       const uint32_t kb = rd.at(lds_address(kt) + buf * kTile, rd.row);
       const uint32_t vb = rd.at(lds_address(vt) + buf * kTile, rd.col);
@@ -196,11 +199,42 @@ __global__ __launch_bounds__(kThreads, 2) void attend_kernel(const AttnArgs a) {
   };
 
   copies_barrier();
-  const int whole = min(max(lim_lo, 0) / kBN, n_tiles);   // tiles that every row sees
-  for (int tile = 0; tile < whole; ++tile) step(tile, std::false_type{});
-  for (int tile = whole; tile < n_tiles; ++tile) step(tile, std::true_type{});
+  const int turns = (n_tiles + PARTS - 1) / PARTS;
+  const int whole = min(max(lim_lo, 0) / kBN, n_tiles) / PARTS;   // of tiles that every row sees
+  for (int turn = 0; turn < whole; ++turn) step(turn, std::false_type{});
+  for (int turn = whole; turn < turns; ++turn) step(turn, std::true_type{});
 
   l = sum_halves(l);
+  if (PARTS == 2) {   // [wave][column block, quad][lane] of the other part's output; m, l; flags
+    f32x4 *o = reinterpret_cast<f32x4 *>(lds) + wave * DT * 4 * 64 + lane;
+    f32x2 *ml = reinterpret_cast<f32x2 *>(lds + 4 * DT * 4 * 64 * 16) + wave * 64 + lane;
+    int *flag = reinterpret_cast<int *>(lds + 4 * DT * 4 * 64 * 16 + 4 * 64 * 8) + wave;
+    if (part == 1) {
+#pragma unroll
+      for (int c = 0; c < DT; ++c)
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          o[(4 * c + e) * 64] = f32x4{acc[c][4 * e], acc[c][4 * e + 1], acc[c][4 * e + 2], acc[c][4 * e + 3]};
+      *ml = f32x2{m, l};
+      if (lane == 0) *flag = dirty;
+    }
+    __syncthreads();
+    if (part == 1) return;
+    const f32x2 other = *ml;
+    const float mn = fmaxf(m, other[0]), base = mn == -__builtin_inff() ? 0.f : mn;
+    const float f0 = fast_exp2(m - base), f1 = fast_exp2(other[0] - base);
+    m = mn;
+    l = l * f0 + other[1] * f1;
+    dirty |= *flag != 0;
+#pragma unroll
+    for (int c = 0; c < DT; ++c)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const f32x4 x = o[(4 * c + e) * 64];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) acc[c][4 * e + i] = acc[c][4 * e + i] * f0 + x[i] * f1;
+      }
+  }
   const bool ok = row < lq;
   const float inv = l > 0.f ? 1.f / l : (l == 0.f ? 0.f : l);   // a NaN sum stays one
   store_row<T, DT>(a.o + (int64_t)(t.b0 + row) * a.o_row + head * a.o_head, ok, a.bytes, acc, inv,
@@ -213,7 +247,7 @@ __global__ __launch_bounds__(kThreads, 2) void attend_kernel(const AttnArgs a) {
         l == 0.f ? -__builtin_inff() : (m + __builtin_amdgcn_logf(l)) * kLn2;
   if (dirty) {
     __threadfence_block();
-    const int first = max(lim_lo, 0) / kBN * kBN;   // of the first tile with a masked place
+    const int first = whole * PARTS * kBN;   // from here on tiles were looked through
     for (int r = row_lo; r < min(row_lo + 32, lq); ++r)
       for (int d = lane; 2 * d < a.bytes; d += 64) {
         const float x = nonfinite_sum<T>(vbase, a.v_row, first, limit(r), d);
@@ -223,24 +257,43 @@ __global__ __launch_bounds__(kThreads, 2) void attend_kernel(const AttnArgs a) {
   }
 }
 
-template <class T, int DP, bool CAP, int BIAS, bool REST>
-hipError_t launch_form(const AttnArgs &a, hipStream_t s) {
+template <class T, int DP, bool CAP, int BIAS, bool REST, int PARTS>
+hipError_t launch_parts(const AttnArgs &a, int64_t blocks, hipStream_t s) {
   static LdsLimit limit;
-  int lds = 4 * kBN * DP * 2;
+  constexpr int kTiles = PARTS * 4 * kBN * DP * 2;
+  int lds = kTiles;
   if (BIAS == kBiasTable) {
     const int reach = a.buckets.start[a.buckets.per_side - 1];
     lds += lut_size(reach) * 4 + map_bytes(reach);
   }
-  hipError_t e = limit.set(reinterpret_cast<const void *>(&attend_kernel<T, DP, CAP, BIAS, REST>),
-                           4 * kBN * DP * 2 + lut_size(kMaxReach) * 4 + map_bytes(kMaxReach));
+  hipError_t e = limit.set(reinterpret_cast<const void *>(&attend_kernel<T, DP, CAP, BIAS, REST, PARTS>),
+                           kTiles + lut_size(kMaxReach) * 4 + map_bytes(kMaxReach));
   if (e != hipSuccess) return e;
+  attend_kernel<T, DP, CAP, BIAS, REST, PARTS>
+      <<<dim3((uint32_t)blocks), kThreads * PARTS, lds, s>>>(a);
+  return hipGetLastError();
+}
+
+// Two groups of wavefronts per block while there is one block per compute unit; up to two, if
+// most are of one document (under a causal mask its last blocks alone set the time then). Two
+// groups / one, causal, at n blocks: 2048 rows, 16 heads of 128, n = 256 50.0 / 64.3 us; 3600 rows,
+// n = 464 68.8 / 88.6; 4 documents of 1000, 8 heads of 64, n = 256 17.7 / 23.3; 4096 rows, 16 heads
+// of 64, n = 512 54.9 / 68.8; 9 documents of 400, 8 heads of 128, n = 288 28.0 / 21.2; 12 of 500,
+// 8 heads of 64 and slopes, n = 384 21.5 / 18.5.
+bool use_parts(const AttnArgs &a, int64_t blocks) {
+  const int64_t longest = (int64_t)((a.max_q + kBM - 1) / kBM) * a.heads;
+  return blocks <= kSeqCus || (blocks <= 2 * kSeqCus && 2 * longest > blocks);
+}
+
+template <class T, int DP, bool CAP, int BIAS, bool REST>
+hipError_t launch_form(const AttnArgs &a, hipStream_t s) {
   // an upper bound of the documents' tiles; the blocks past the last one end at once
   const int64_t tiles = (int64_t)a.q_rows / kBM + a.docs;
   const int64_t by_max = (int64_t)a.docs * ((a.max_q + kBM - 1) / kBM);
   const int64_t blocks = (tiles < by_max ? tiles : by_max) * a.heads;
   if (blocks == 0) return hipSuccess;
-  attend_kernel<T, DP, CAP, BIAS, REST><<<dim3((uint32_t)blocks), kThreads, lds, s>>>(a);
-  return hipGetLastError();
+  if (use_parts(a, blocks)) return launch_parts<T, DP, CAP, BIAS, REST, 2>(a, blocks, s);
+  return launch_parts<T, DP, CAP, BIAS, REST, 1>(a, blocks, s);
 }
 
 template <class T, int DP, bool CAP, int BIAS>

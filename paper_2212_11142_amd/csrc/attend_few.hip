@@ -437,10 +437,10 @@ hipError_t by_bias(const AttnArgs &a, void *part, hipStream_t s) {
 
 // Small calls too: while the general form's blocks of 128 queries leave compute units idle,
 // 32 rows per block with the keys split over its wavefronts finish sooner. This form / the
-// general one at n of its blocks: 16 heads of 128, causal, n = 64 11.8 / 18.0 us, 128 19.6 /
-// 28.0, 160 30.0 / 33.3, 224 42.4 / 43.3, 256 65.7 / 64.0, 512 130 / 109; 16 heads of 64,
-// n = 224 21.3 / 30.0; documents of 200 rows, 8 heads of 64, n = 192 11.0 / 11.3, 256 12.4 / 11.6.
-constexpr int kFewBlocks = 224;
+// general one at n of its blocks, causal: 16 heads of 128, n = 64 11.8 / 18.0 us, 128 22.4 / 27.9,
+// 192 37.3 / 32.2; 8 heads of 64, n = 64 9.9 / 15.4, 160 22.1 / 29.1; 16 of 64, n = 192 18.5 /
+// 21.3; documents of 200 rows, 8 heads of 64, n = 128 9.6 / 11.4, 192 10.9 / 9.5.
+constexpr int kFewBlocks = 160;
 
 bool attend_use_few(const AttnArgs &a) {
   if ((int64_t)a.group * bucket_count(a.buckets) > kMaxValues) return false;

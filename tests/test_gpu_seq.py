@@ -279,6 +279,35 @@ def test_attend_large_anything_in_masked_places(dtype, value):
     assert b.out[180:300, 48:].isfinite().all()
 
 
+@pytest.mark.parametrize("dtype,dim", [("fp16", 64), ("bf16", 120), ("fp16", 128)])
+@pytest.mark.parametrize("cap,bias", [(0.0, "none"), (3.0, "slope"), (20.0, "one"), (0.0, "two")])
+@pytest.mark.parametrize("mask", ["full", "causal", "prefix"])
+def test_attend_a_block_per_compute_unit(dtype, dim, cap, bias, mask):
+    """Fewer blocks, whose key tiles two groups of wavefronts share; also as in training."""
+    lens = [(200, 200), (129, 257), (1, 1), (65, 40), (300, 300)]
+    for grad in (False, True):
+        Case(dtype, lens, 20, 5, dim, causal=mask != "full", cap=cap, bias=bias, size=2.0, grad=grad,
+             prefix=[90, 257, 0, 3, 131] if mask == "prefix" else None).check()
+
+
+@pytest.mark.parametrize("heads", [44, 192])     # two groups of wavefronts, and one
+@pytest.mark.parametrize("value", [math.nan, math.inf])
+def test_attend_values_that_some_rows_see(heads, value):
+    """A value and a key that no number is, in one head from one row on, in every tile's place."""
+    for at in (0, 63, 64, 130, 299):
+        c = Case("bf16", [(300, 300), (70, 150)], heads, 2, 64, causal=True, k_begin=[0, 400], k_rows=700)
+        c.v[at, 0, 5] = value
+        ref = c.oracle()
+        with np.errstate(invalid="ignore"):
+            ref["out_abs"][:, :, 5] = np.where(np.isfinite(ref["out"][:, :, 5]), ref["out_abs"][:, :, 5], 0)
+        c.check(ref=ref)
+        c.k[at, 0, :] = math.nan
+        b = c.run()
+        half = heads // 2
+        assert b.out[:at].isfinite().all() and b.out[at:300, :half].isnan().all()
+        assert b.out[at:, half:].isfinite().all() and b.out[300:].isfinite().all()
+
+
 @pytest.mark.parametrize("dtype,heads,kv,dim,cap,bias,mask", [
     ("bf16", 32, 2, 64, 0.0, "slope", "causal"),     # key tiles shared by 8 blocks
     ("fp16", 32, 4, 128, 5.0, "two", "prefix"),
