@@ -424,19 +424,22 @@ __device__ __forceinline__ void grad_kv(const AttnGradArgs &ga, int row_blocks, 
                    fk, lane);
 }
 
-// dK and dV from the shares' sums: a block per tile and key head.
+// dK and dV from the shares' sums, in their order: a block per 32 keys and key head, all shares'
+// loads under way at once.
+constexpr int kShareRows = 32;
 template <class T, int DP>
 __global__ __launch_bounds__(kThreads) void grad_shares(const AttnGradArgs ga) {
   const AttnArgs &a = ga.f;
   constexpr int kPieces = DP / 8;
   const int kvh = blockIdx.x % a.kv_heads;
-  const DocTile t = find_tile<128>(a.kb, a.ke, a.docs, a.k_rows, blockIdx.x / a.kv_heads);
+  const DocTile t = find_tile<kShareRows>(a.kb, a.ke, a.docs, a.k_rows, blockIdx.x / a.kv_heads);
   if (t.doc < 0) return;
-  for (int i = threadIdx.x; i < 128 * 2 * kPieces; i += kThreads) {
-    const int row = t.tile * 128 + i / (2 * kPieces), piece = i % kPieces;
+  for (int i = threadIdx.x; i < kShareRows * 2 * kPieces; i += kThreads) {
+    const int row = t.tile * kShareRows + i / (2 * kPieces), piece = i % kPieces;
     const bool v = i / kPieces % 2;
     if (row >= t.b1 - t.b0 || piece * 16 >= a.bytes) continue;
     f32x4 lo = {}, hi = {};
+#pragma unroll 4
     for (int s = 0; s < ga.shares; ++s) {
       const float *x = ga.kv_part + (((int64_t)s * a.k_rows + t.b0 + row) * a.kv_heads + kvh) * 2 * DP +
                        (v ? DP : 0) + piece * 8;
@@ -729,11 +732,11 @@ constexpr int pair_bytes(int dp, bool narrow, int lut, int map) {
 }
 
 // The narrow form's tiles where the wide one's blocks would leave compute units idle, if
-// the table leaves room in LDS. Narrow / wide at n wide blocks: 3 documents of 333, 6 heads of
-// 80, n = 24 50 / 93 us; 8 documents of 250, 8 heads of 64, n = 256 51 / 61; one of 2560, n = 320
-// 114 / 151; 12 of 250, n = 384 74 / 64; 16 heads of 128, 1536 rows, n = 384 155 / 156; 2048
-// rows, n = 512 228 / 184.
-constexpr int kNarrowBlocks = 320;
+// the table leaves room in LDS. Narrow / wide at n wide blocks, with a table: documents of 120
+// rows, 8 heads of 64, n = 32 21.9 / 25.2 us, 128 30.4 / 26.8; 250 rows, 16 heads of 64 with 4 of
+// keys, n = 160 45 / 60, 320 77 / 68; 500 rows, 8 heads of 128 with 2 of keys, n = 160 84 / 85,
+// 320 137 / 96; 3 of 333, 6 heads of 80, n = 24 50 / 93.
+constexpr int kNarrowBlocks = 160;
 int pair_bytes(const AttnArgs &f, bool narrow) {
   const int dp = f.bytes <= 128 ? 64 : 128;
   if (f.buckets.per_side == 0) return pair_bytes(dp, narrow, 0, 0);
@@ -746,16 +749,23 @@ int tile_rows(const AttnArgs &f) {
   return wide <= kNarrowBlocks && pair_bytes(f, true) <= kLdsBytes - 1024 ? 32 : 128;
 }
 
-// Blocks that share a key tile's steps: as many as it takes to have a block of keys for each
-// of the 2 places on a compute unit. More would only add to the sums that are written and
-// read again. Steps with 1 / 2 / 3 / 4 / 8 shares: 8862 rows in 16 documents, 4 key heads of
-// 64 (308 tiles): 256 / 257 / 266 / 265 / 281 us; 4096 rows, 4 key heads of 128 (128 tiles):
-// - / 533 / 461 / 430 / 461 us; 1 key head (32 tiles): - / 839 / 616 / 505 / 375 us.
+// Blocks that share a key tile's steps, so that the longest of them does not outlast the rest:
+// about 384 blocks of keys in all (more with several query heads per key head, whose blocks are
+// that much longer), none with less than 512 queries. Steps with 1 / 2 / 3 / 4 / 8 shares, D = 64,
+// 4 heads per key head: 16 documents of 1024 at most (277 tiles) 258 / 230 / 231 / - / - us; 3 of
+// 2000, 12 heads (141 tiles) - / 219 / 192 / 203 / 208; one of 4096, 12 heads (96 tiles) - / - / - /
+// 234 / 259; D = 128, 2 key heads, 2 documents of 2500 (80 tiles) - / - / - / 244 / 290; one head
+// per key head, one of 4096, 8 heads (256 tiles) 210 / 235 / 249 / - / -; 24 documents of 120 rows,
+// 8 heads (184 tiles) 35 / - / 54 / - / -.
+constexpr int kShareQueries = 512, kShareBlocks = 384;
 int share_count(const AttnArgs &f) {
   if (tile_rows(f) == 32 || f.q_rows == 0) return 1;
   const int64_t blocks = ((int64_t)f.k_rows + 127) / 128 * f.kv_heads;
   if (blocks == 0) return 1;
-  const int64_t s = (2 * kSeqCus + blocks - 1) / blocks;
+  int64_t s = (kShareBlocks + (f.group > 1 ? blocks - 1 : 0)) / blocks;
+  const int64_t most = (int64_t)f.group * f.max_q / kShareQueries;
+  if (s > most) s = most;
+  if (s < 1) s = 1;
   return (int)(s < 8 ? s : 8);
 }
 
@@ -767,14 +777,16 @@ hipError_t launch_form(const AttnGradArgs &a, int row_blocks, hipStream_t s) {
   hipError_t e = limit.set(reinterpret_cast<const void *>(&grad_pairs<T, DP, CAP, BIAS, NARROW>),
                            kLdsBytes - 1024);   // (the rest for what is static)
   if (e != hipSuccess) return e;
-  const int64_t kv_tiles = tile_bound(a.f.k_rows, a.f.docs, a.f.max_k, kTile) * a.f.kv_heads;
-  const int64_t kb = kv_tiles * a.shares;
+  const int64_t kb = tile_bound(a.f.k_rows, a.f.docs, a.f.max_k, kTile) * a.f.kv_heads * a.shares;
   const int64_t units = tile_bound(a.f.q_rows, a.f.docs, a.f.max_q, kTile);
   const int64_t blocks = kb + units * a.f.heads;
   if (blocks > 0)
     grad_pairs<T, DP, CAP, BIAS, NARROW>
         <<<dim3((uint32_t)blocks), kThreads, lds, s>>>(a, row_blocks, (int)kb);
-  if (a.shares > 1) grad_shares<T, DP><<<dim3((uint32_t)kv_tiles), kThreads, 0, s>>>(a);
+  if (a.shares > 1) {
+    const int64_t n = tile_bound(a.f.k_rows, a.f.docs, a.f.max_k, kShareRows) * a.f.kv_heads;
+    grad_shares<T, DP><<<dim3((uint32_t)n), kThreads, 0, s>>>(a);
+  }
   if (BIAS == kBiasTable) {
     const int nb = bucket_count(a.f.buckets);
     grad_table<T><<<dim3((uint32_t)(a.f.heads * nb)), 256, 0, s>>>(a, (int)units, nb);
