@@ -45,6 +45,9 @@ gp_status check_attention(const gp_attention *t) {
   // grids are 32-bit
   const int64_t tiles = (int64_t)t->q_rows / 128 + (int64_t)t->k_rows / 128 + 2 * (int64_t)t->n_docs;
   if (tiles * t->heads > (int64_t)INT32_MAX) return seq_fail(GP_E_UNSUPPORTED, "too many tiles");
+  const int64_t few = t->max_q < 32 ? t->max_q : 32;    // (a block per row joins the few-row form)
+  if ((int64_t)t->n_docs * t->heads * few > (int64_t)INT32_MAX)
+    return seq_fail(GP_E_UNSUPPORTED, "too many rows");
   return GP_OK;
 }
 

@@ -81,6 +81,20 @@ def test_workspaces_refused(lib):
     assert _call(lib, s, grad=True, ws=255, nbytes=g) == WORKSPACE
 
 
+def test_grids_of_loose_bounds(lib):
+    """max_q and max_k may be far above the documents' lengths: the grids stay within 32 bits."""
+    big = 1 << 30
+    n = lib.gp_attend_workspace_bytes(C.byref(_desc(q_rows=4096, k_rows=big, max_q=1, max_k=big,
+                                                    n_docs=4096)), 0)
+    assert 0 < n < C.c_size_t(-1).value
+    s = _desc()
+    blocks = (1 << 24) + 4096 * s.kv_heads
+    group = s.heads // s.kv_heads
+    assert n <= blocks * min(32, group) * (128 + 2) * 4 + 4096
+    s = _desc(q_rows=32, k_rows=1, max_q=32, max_k=1, n_docs=1 << 24, heads=32, kv_heads=32)
+    assert _call(lib, s) == UNSUPPORTED
+
+
 def test_workspace_grows_with_the_work(lib):
     f = lambda **kw: lib.gp_attend_workspace_bytes(C.byref(_desc(q_rows=1 << 16, k_rows=1 << 16,
                                                                  max_q=1 << 10, max_k=1 << 10, **kw)), 1)
