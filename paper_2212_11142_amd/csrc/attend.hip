@@ -7,6 +7,14 @@
 // second product V^T P^T, so that only K and V go through LDS, and each once per block.
 // lim(i) = min(Lk, max(position + 1, prefix)) covers the causal, prefix and document masks
 // with one comparison per score, made only in tiles where some row's limit falls.
+//
+// Bound by the matrix units and by the scores' own instructions (an exponential, two fused
+// multiply-adds, the maximum, the sum and half a conversion each) in turn. Measured: 16,384 rows,
+// causal, 16 heads of 128, fp16, 1242 us, 0.89 PFLOP/s (a library product of 8192^3 has 1.11; the
+// matrix units are busy for half of the cycles, the vector units for 65%); 1,048,576 rows over
+// 512 keys, 8 heads of 64, bf16, 1469 us, 0.75 PFLOP/s (vector units 80%: at this head size half
+// the products per score); 13 documents of up to 1021 rows, cap and table, 57 us. More queries per
+// wavefront or keys per tile would not fit the registers.
 #include <type_traits>
 
 #include "seq_dev.h"
