@@ -28,7 +28,8 @@ constexpr float kP16 = 12.f;       // fp16: log2 of the factor of P
 constexpr int kSkew = 16 * 64;      // floats of a wavefront's skewed values
 
 // Queries of a step of dK and dV: as many as leave room for three blocks of head size 64, or
-// two of 128, in LDS.
+// two of 128, in LDS. With 64 / 32 at head size 64: 16 documents of up to 1024 236 / 247 us, one of
+// 8192, 16 heads with 2 of keys, 961 / 996; one of 4096, 16 heads, a table, 264 / 255.
 constexpr int kv_step(int dp, bool narrow) { return narrow || dp == 128 ? 32 : 64; }
 
 // Starts the copy of one word per lane into LDS.
@@ -764,14 +765,24 @@ int tile_rows(const AttnArgs &f) {
 // 2000, 12 heads (141 tiles) - / 219 / 192 / 203 / 208; one of 4096, 12 heads (96 tiles) - / - / - /
 // 234 / 259; D = 128, 2 key heads, 2 documents of 2500 (80 tiles) - / - / - / 244 / 290; one head
 // per key head, one of 4096, 8 heads (256 tiles) 210 / 235 / 249 / - / -; 24 documents of 120 rows,
-// 8 heads (184 tiles) 35 / - / 54 / - / -.
-constexpr int kShareQueries = 512, kShareBlocks = 384;
+// 8 heads (184 tiles) 35 / - / 54 / - / -. Narrow blocks: about 192, with the more queries each the
+// more there are. None / n shares: one of 1500 rows, 8 heads of 64 with 1 of keys (47 tiles) 144 /
+// 74 (n = 4); of 120 (4 tiles) 34.5 / 28.4 (3); 1000 rows, 8 heads of 128 with 2 of keys (64 tiles)
+// 97 / 75 (3); 4 documents of 250 (64 tiles), which this leaves whole, 47 / 53 (2).
+constexpr int kShareQueries = 512, kShareBlocks = 384, kNarrowShares = 192;
 int share_count(const AttnArgs &f) {
-  if (tile_rows(f) == 32 || f.q_rows == 0) return 1;
-  const int64_t blocks = ((int64_t)f.k_rows + 127) / 128 * f.kv_heads;
-  if (blocks == 0) return 1;
-  int64_t s = (kShareBlocks + (f.group > 1 ? blocks - 1 : 0)) / blocks;
-  const int64_t most = (int64_t)f.group * f.max_q / kShareQueries;
+  const int tile = tile_rows(f);
+  const int64_t blocks = ((int64_t)f.k_rows + tile - 1) / tile * f.kv_heads;
+  if (blocks == 0 || f.q_rows == 0) return 1;
+  const int64_t queries = (int64_t)f.group * f.max_q;
+  int64_t s, most;
+  if (tile == 32) {
+    s = kNarrowShares / blocks;
+    most = queries / (256 + 6 * blocks);
+  } else {
+    s = (kShareBlocks + (f.group > 1 ? blocks - 1 : 0)) / blocks;
+    most = queries / kShareQueries;
+  }
   if (s > most) s = most;
   if (s < 1) s = 1;
   return (int)(s < 8 ? s : 8);

@@ -320,6 +320,15 @@ def test_grad_large(dtype, heads, kv, dim, cap, bias, mask):
          prefix=[200, 0, 260, 0, 40] if mask == "prefix" else None).check()
 
 
+@pytest.mark.parametrize("dtype,heads,kv,dim", [("bf16", 8, 1, 64), ("fp16", 16, 2, 72), ("bf16", 6, 1, 128)])
+@pytest.mark.parametrize("cap,bias,mask", [(0.0, "two", "full"), (4.0, "slope", "causal"), (0.0, "one", "prefix")])
+def test_grad_small_with_many_heads_per_key_head(dtype, heads, kv, dim, cap, bias, mask):
+    """Small calls whose key tiles are shared, with documents shorter than the shares."""
+    lens = [(260, 260), (40, 90), (1, 1), (3, 0), (97, 33)]
+    Case(dtype, lens, heads, kv, dim, causal=mask != "full", cap=cap, bias=bias, grad=True,
+         prefix=[31, 90, 0, 0, 12] if mask == "prefix" else None).check()
+
+
 def test_grad_of_one_key_is_zero():
     """A softmax over one key does not depend on its score."""
     for heads, lens in ((2, [(1, 1), (5, 1)]), (64, [(1, 1), (300, 1), (130, 1), (260, 260)])):
