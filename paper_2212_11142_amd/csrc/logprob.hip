@@ -19,10 +19,11 @@ namespace {
 constexpr int kThreads = 256;
 constexpr int kList = 1024;        // candidates for the alternatives (8 blocks fit LDS)
 constexpr int kOwners = 512;       // groups of entries that may hold candidates
-// Alternatives up to which 64 groups' bound is tight enough. With 64 / 256 groups: 40
-// alternatives of one row of 10,000 10.9 / 12.7 us, of 200 rows of 131,072 38.6 / 35.0; 50: 11.2 /
-// 13.0 and 48.2 / 37.5.
-constexpr int kSixtyFour = 40;
+// Alternatives up to which 64 groups' bound is taken instead of 256 groups'. Even a row of equal
+// entries then lists 32 (k - 1) + 1 candidates at most in a block per row (8 (k - 1) + 1 with 256).
+// With 64 / 256 groups: 40 alternatives of one row of 10,000 10.9 / 12.7 us, of 200 rows of
+// 131,072 38.6 / 30.7.
+constexpr int kSixtyFour = 32;
 // Widest row of the one-wavefront form (64 entries a lane). 16,384 rows, this form / a block per
 // row: 1100 wide bf16 14.3 / 54.6 us, with 5 alternatives 24.1 / 115; 4096 wide bf16 26.4 / 43.0,
 // 38.1 / 95.9; 4096 wide fp32 42.3 / 41.1, 45.4 / 70.5.
@@ -536,18 +537,23 @@ SplitPlan split_plan(int32_t rows, int32_t width) {
   return p;
 }
 
-// Every block leaves its range's sums and the keys of its 64 groups of 4 threads; a second
-// kernel joins them, one block per row. Bound by latency: 8 rows of 131,072, bf16, 20 alternatives,
+// Groups of threads that a block leaves the best keys of.
+__host__ __device__ inline int key_groups(int top) {
+  return top == 0 ? 0 : (top <= kSixtyFour ? 64 : kThreads);
+}
+
+// Every block leaves its range's sums and the keys of its groups of threads; a second kernel
+// joins them, one block per row. Bound by latency: 8 rows of 131,072, bf16, 20 alternatives,
 // 5.0 us and 9.9 for the join, whose choice of the alternatives is a chain of four passes over
 // LDS and of two over the candidates' memory.
 struct PartSpace {
-  uint64_t *keys;    // [rows][parts][64]
+  uint64_t *keys;    // [rows][parts][groups]
   float *sums;       // [rows][parts][4]
 };
-__host__ __device__ inline PartSpace part_space(void *ws, int64_t rows, int parts, bool keys) {
+__host__ __device__ inline PartSpace part_space(void *ws, int64_t rows, int parts, int top) {
   PartSpace s;
   s.keys = static_cast<uint64_t *>(ws);
-  s.sums = reinterpret_cast<float *>(s.keys + (keys ? rows * parts * 64 : 0));
+  s.sums = reinterpret_cast<float *>(s.keys + rows * parts * key_groups(top));
   return s;
 }
 
@@ -557,16 +563,20 @@ __global__ __launch_bounds__(kThreads) void logprob_part(const LogprobArgs a, Sp
   __shared__ float red[4][3];
   const int64_t row = blockIdx.x / sp.parts;
   const int part = blockIdx.x % sp.parts;
-  const PartSpace sc = part_space(ws, a.rows, sp.parts, KEYS);
+  const PartSpace sc = part_space(ws, a.rows, sp.parts, a.top);
   const char *p = static_cast<const char *>(a.x) + row * a.row * Elem<DT>::kSize;
   const float c2 = a.scale * kLog2e;
   const int64_t lo = part * sp.chunk, hi = lo + sp.chunk < a.width ? lo + sp.chunk : a.width;
   uint64_t mine = 0;
   Sums s = range_pass<DT, KEYS>(p + lo * Elem<DT>::kSize, lo, hi - lo, c2, &mine);
   if (KEYS) {
-    mine = max64(mine, shfl_xor64(mine, 1));
-    mine = max64(mine, shfl_xor64(mine, 2));
-    if (threadIdx.x % 4 == 0) sc.keys[(int64_t)blockIdx.x * 64 + threadIdx.x / 4] = mine;
+    if (a.top <= kSixtyFour) {
+      mine = max64(mine, shfl_xor64(mine, 1));
+      mine = max64(mine, shfl_xor64(mine, 2));
+      if (threadIdx.x % 4 == 0) sc.keys[(int64_t)blockIdx.x * 64 + threadIdx.x / 4] = mine;
+    } else {
+      sc.keys[(int64_t)blockIdx.x * kThreads + threadIdx.x] = mine;
+    }
   }
   s = block_sums(s, c2, red);
   if (threadIdx.x == 0)
@@ -579,13 +589,13 @@ __global__ __launch_bounds__(kThreads) void logprob_join(const LogprobArgs a, Sp
   constexpr int kVec = Elem<DT>::kVec;
   __shared__ float red[4][3];
   const int64_t row = blockIdx.x;
-  const PartSpace sc = part_space(ws, a.rows, sp.parts, KEYS);
+  const PartSpace sc = part_space(ws, a.rows, sp.parts, a.top);
   const char *p = static_cast<const char *>(a.x) + row * a.row * Elem<DT>::kSize;
   const float c2 = a.scale * kLog2e;
   const Target given = target_of<DT>(a, row, p);
   uint64_t mine = 0;
-  const uint64_t *kr = sc.keys + row * sp.parts * 64;
-  const int n = sp.parts * 64;
+  const int groups = key_groups(a.top), n = sp.parts * groups;
+  const uint64_t *kr = sc.keys + row * n;
   if (KEYS) {
 #pragma unroll 4
     for (int i = threadIdx.x; i < n; i += kThreads) mine = max64(mine, kr[i]);
@@ -599,7 +609,7 @@ __global__ __launch_bounds__(kThreads) void logprob_join(const LogprobArgs a, Sp
   if (threadIdx.x == 0) write_row(a, row, s, given);
   if (!KEYS) return;
   __shared__ TopShared sh;
-  const uint64_t bound = bound_from_below(sh, mine, a.top);
+  uint64_t bound = bound_from_below(sh, mine, a.top);
   for (int i = threadIdx.x; i < n; i += kThreads) {
     const uint64_t k = kr[i];
     if (k && k >= bound) {
@@ -612,13 +622,43 @@ __global__ __launch_bounds__(kThreads) void logprob_join(const LogprobArgs a, Sp
     a.top_logp[row * a.top + r] = alt_logp(s, a.scale, k);
     a.top_id[row * a.top + r] = k ? key_index(k) : -1;
   };
-  if (sh.n_owners <= kOwners) {
-    // 4 vectors side by side every 256 of the group's block
+  int owners = sh.n_owners;
+  if (owners <= kOwners) {
+    if (owners > 2 * a.top) {
+      // Many groups, as where many entries are equal: the k-th of their keys is a bound too, and
+      // k groups have keys above it. (A row of 131,072 equal entries without: 720 us, 20 passes.)
+      for (int i = threadIdx.x; i < owners; i += kThreads) sh.list[i] = kr[sh.owners[i]];
+      __syncthreads();
+      int keep[kOwners / kThreads];
+#pragma unroll
+      for (int u = 0; u < kOwners / kThreads; ++u) {
+        const int i = threadIdx.x + u * kThreads;
+        keep[u] = -1;
+        if (i < owners) {
+          const uint64_t own = sh.list[i];
+          int rank = 0;
+          for (int j = 0; j < owners; ++j) rank += sh.list[j] > own ? 1 : 0;
+          if (rank < a.top) keep[u] = sh.owners[i];
+          if (rank == a.top - 1) sh.best[1] = own;
+        }
+      }
+      if (threadIdx.x == 0) sh.n_owners = 0;
+      __syncthreads();
+      bound = sh.best[1];
+#pragma unroll
+      for (int u = 0; u < kOwners / kThreads; ++u)
+        if (keep[u] >= 0) sh.owners[atomicAdd(&sh.n_owners, 1)] = keep[u];
+      __syncthreads();
+      owners = a.top;
+    }
+    // `per` vectors side by side every 256 of the group's block
+    const int per = kThreads / groups;
     const int turns = (int)((sp.chunk / kVec + 1 + kThreads - 1) / kThreads);
-    const int items = sh.n_owners * turns * 4;
+    const int items = owners * turns * per;
     for (int i = threadIdx.x; i < items; i += kThreads) {
-      const int g = sh.owners[i / (turns * 4)];
-      const int64_t from = (g / 64) * sp.chunk, v = (int64_t)(i / 4 % turns) * kThreads + g % 64 * 4 + i % 4;
+      const int g = sh.owners[i / (turns * per)];
+      const int64_t from = (g / groups) * sp.chunk;
+      const int64_t v = (int64_t)(i / per % turns) * kThreads + g % groups * per + i % per;
       const int64_t len = from + sp.chunk < a.width ? sp.chunk : a.width - from;
       const Aligned<DT> range(p + from * Elem<DT>::kSize, len);
       float x[kVec];
@@ -766,7 +806,7 @@ size_t logprob_bytes(int32_t rows, int32_t width, int32_t top) {
   if (width <= kWaveWidth) return 0;
   const SplitPlan sp = split_plan(rows, width);
   if (sp.parts == 1) return 0;
-  return (size_t)rows * sp.parts * ((top > 0 ? 64 * 8 : 0) + 16);
+  return (size_t)rows * sp.parts * (key_groups(top) * 8 + 16);
 }
 
 hipError_t launch_logprob(const LogprobArgs &a, void *ws, hipStream_t s) {

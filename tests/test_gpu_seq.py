@@ -715,6 +715,25 @@ def test_logprob_ties_and_crowded_threads(rows):
     assert torch.equal(b["top_id"].cpu(), torch.arange(50).expand(2, 50))
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("rows,width", [(3, 100003), (5, 60001), (260, 9000), (7, 3000)])
+def test_logprob_alternatives_of_few_values(rows, width, dtype):
+    """Rows of two, three and many equal values, in every form: the lowest indices first."""
+    import torch
+    from paper_2212_11142_amd import seq
+    g = torch.Generator().manual_seed(5)
+    x = torch.randn((rows, width), generator=g).clamp(-1, 1).round()
+    x[0] = 0.0
+    x[1] = (torch.rand(width, generator=g) < 1e-3).float()
+    x[2, width // 2:] = 3.0
+    x = x.to(_torch_dtype(dtype)).cuda()
+    t = torch.zeros(rows, dtype=torch.int64, device="cuda")
+    order = torch.sort(x.float().cpu(), dim=1, descending=True, stable=True)[1]
+    for top in (1, 20, 32, 33, 128):
+        b = seq.logprob(x, t, top=top)
+        assert torch.equal(b["top_id"].cpu(), order[:, :top]), top
+
+
 @pytest.mark.parametrize("width", [40, 5000, 70000])
 def test_logprob_values_at_the_ends(width):
     """Ruled out entries, rows of nothing else, the type's lowest value, infinities, NaN,
