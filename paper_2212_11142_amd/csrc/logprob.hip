@@ -126,9 +126,11 @@ __device__ inline int64_t key_index(uint64_t k) { return 0xffffffffu - (uint32_t
 // Running sums at the maximum m (raw units; kLowest before the first entry). A term's
 // exponent is d = fl(x c2 - r), one instruction, with r = fl(m c2) in m c2's place; what r is
 // off by is taken out of the sums' logarithm. Where m is so large that this would be many
-// units, d = (x - m) c2.
+// units, and in short rows (`exact`, where reading hides the instruction: a row of one entry
+// then gives exact zeros), d = (x - m) c2.
 struct Sums {
   float m, a, b;
+  bool exact = false;
 };
 __device__ inline bool near_zero(float r) { return __builtin_fabsf(r) <= 1e6f; }
 // the reference less m c2
@@ -152,7 +154,7 @@ __device__ inline void add(Sums &s, float d) {
 template <int M, int N>
 __device__ inline void add_all(Sums &s, const float (&x)[M][N], float c2) {
   const float r = s.m * c2;
-  if (near_zero(r)) {
+  if (!s.exact && near_zero(r)) {
 #pragma unroll
     for (int i = 0; i < M * N; ++i) add(s, __builtin_fmaf(x[i / N][i % N], c2, -r));
   } else {
@@ -175,9 +177,11 @@ __device__ inline uint64_t max64(uint64_t a, uint64_t b) { return a > b ? a : b;
 struct RowOut {
   float lse, logp, entropy;
 };
+// (rounding aside, neither is below 0; a NaN stays one)
+__device__ inline float not_below_0(float x) { return x < 0.f ? 0.f : x; }
 // log of the sum of e^(scale (x - m))
 __device__ inline float log_sum(const Sums &s, float c2) {
-  return __builtin_fmaf(kLn2, ref_error(s.m, c2), logf(s.a));
+  return not_below_0(s.exact ? logf(s.a) : __builtin_fmaf(kLn2, ref_error(s.m, c2), logf(s.a)));
 }
 // x_t: the given entry (only read if there is one)
 __device__ inline RowOut finish(const Sums &s, float scale, bool has, float xt) {
@@ -189,7 +193,7 @@ __device__ inline RowOut finish(const Sums &s, float scale, bool has, float xt) 
   const float c2 = scale * kLog2e, la = log_sum(s, c2);
   r.lse = __builtin_fmaf(scale, s.m, la);
   r.logp = has ? __builtin_fmaf(scale, xt - s.m, -la) : 0.f;
-  r.entropy = logf(s.a) - kLn2 * (s.b / s.a);
+  r.entropy = not_below_0(logf(s.a) - kLn2 * (s.b / s.a));
   return r;
 }
 __device__ inline float alt_logp(const Sums &s, float scale, float x) {
@@ -248,7 +252,7 @@ __global__ __launch_bounds__(kThreads) void logprob_wave(const LogprobArgs a) {
     top[v] = top_of(x[v]);
     m = max2(m, top[v]);
   }
-  Sums s{wave_max(m), 0.f, 0.f};
+  Sums s{wave_max(m), 0.f, 0.f, true};
   add_all(s, x, c2);
   s.a = wave_sum(s.a);
   s.b = wave_sum(s.b);

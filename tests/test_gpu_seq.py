@@ -715,6 +715,25 @@ def test_logprob_ties_and_crowded_threads(rows):
     assert torch.equal(b["top_id"].cpu(), torch.arange(50).expand(2, 50))
 
 
+@pytest.mark.parametrize("width", [1, 2, 700, 4096])
+def test_logprob_rows_of_one_entry(width):
+    """Everything but one entry ruled out: log probability, entropy and gradient are 0."""
+    import torch
+    from paper_2212_11142_amd import seq
+    g = torch.Generator().manual_seed(3)
+    x = torch.full((300, width), -math.inf)
+    t = torch.randint(0, width, (300,), generator=g)
+    x[torch.arange(300), t] = torch.randn(300, generator=g) * 5
+    x, t = x.cuda(), t.cuda()
+    bufs = seq.LogprobBuffers(300, width, torch.float32, grad=True)
+    seq.logprob_into(x, t, bufs)
+    one = torch.ones(300, device="cuda")
+    seq.logprob_grad_into(x, t, one, one, bufs)
+    torch.cuda.synchronize()
+    assert bool((bufs.logp == 0).all()) and bool((bufs.entropy == 0).all())
+    assert bool((bufs.dlogits == 0).all())
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "fp32"])
 @pytest.mark.parametrize("rows,width", [(3, 100003), (5, 60001), (260, 9000), (7, 3000)])
 def test_logprob_alternatives_of_few_values(rows, width, dtype):
