@@ -32,6 +32,20 @@ constexpr float kLowest = -3.4028234663852886e38f;
 
 enum { kBf16 = GP_BF16, kFp16 = GP_FP16, kFp32 = GP_FP32 };
 
+// Largest number of three and of two (a NaN is passed over). fmaxf would first multiply each
+// operand that was loaded by 1, against signalling NaN. The compiler does not wait before inline
+// assembly for the results of transcendental instructions: none may be an operand here.
+__device__ inline float top3(float a, float b, float c) {
+  float r;
+  asm("v_max3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));
+  return r;
+}
+__device__ inline float top2(float a, float b) {
+  float r;
+  asm("v_max_f32 %0, %1, %2" : "=v"(r) : "v"(a), "v"(b));
+  return r;
+}
+
 template <int DT>
 struct Elem {
   static constexpr int kVec = 8, kSize = 2;
@@ -149,7 +163,7 @@ __device__ inline void raise(Sums &s, float m, float c2) {
 __device__ inline void add(Sums &s, float d) {
   const float e = fast_exp2(d);
   s.a += e;
-  s.b = __builtin_fmaf(e, max2(d, -200.f), s.b);   // (a ruled out entry: 0 times -200)
+  s.b = __builtin_fmaf(e, top2(d, -200.f), s.b);   // (a ruled out entry: 0 times -200)
 }
 template <int M, int N>
 __device__ inline void add_all(Sums &s, const float (&x)[M][N], float c2) {
@@ -240,9 +254,9 @@ __global__ __launch_bounds__(kThreads) void logprob_wave(const LogprobArgs a) {
   float x[VL][kVec], top[VL];     // (top: of a vector)
   float m = kLowest;
   auto top_of = [&](const float *y) {
-    float t = max3(y[0], y[1], y[2]);
+    float t = top3(y[0], y[1], y[2]);
 #pragma unroll
-    for (int i = 3; i < kVec; i += 2) t = max3(t, y[i], y[i + 1 < kVec ? i + 1 : i]);
+    for (int i = 3; i < kVec; i += 2) t = top3(t, y[i], y[i + 1 < kVec ? i + 1 : i]);
     return t;
   };
 #pragma unroll
@@ -250,7 +264,7 @@ __global__ __launch_bounds__(kThreads) void logprob_wave(const LogprobArgs a) {
 #pragma unroll
   for (int v = 0; v < VL; ++v) {
     top[v] = top_of(x[v]);
-    m = max2(m, top[v]);
+    m = top2(m, top[v]);
   }
   Sums s{wave_max(m), 0.f, 0.f, true};
   add_all(s, x, c2);
@@ -264,7 +278,7 @@ __global__ __launch_bounds__(kThreads) void logprob_wave(const LogprobArgs a) {
     for (int k = 0; k < min(a.top - k0, 64) && more; ++k) {
       float best = top[0];
 #pragma unroll
-      for (int v = 1; v < VL; ++v) best = max2(best, top[v]);
+      for (int v = 1; v < VL; ++v) best = top2(best, top[v]);
       best = wave_max(best);
       more = false;
 #pragma unroll
@@ -417,19 +431,19 @@ __device__ __forceinline__ Sums range_pass(const char *p, int64_t first, int64_t
     }
 #pragma unroll
     for (int u = 0; u < kUnroll; ++u) {
-      top[u] = max3(x[u][0], x[u][1], x[u][2]);
+      top[u] = top3(x[u][0], x[u][1], x[u][2]);
 #pragma unroll
-      for (int i = 3; i < kVec; i += 2) top[u] = max3(top[u], x[u][i], x[u][i + 1 < kVec ? i + 1 : i]);
+      for (int i = 3; i < kVec; i += 2) top[u] = top3(top[u], x[u][i], x[u][i + 1 < kVec ? i + 1 : i]);
       if (KEYS) {
         if (top[u] > best) {
           best = top[u];
           best_v = v0 + u * kThreads;
         }
       } else {
-        best = max2(best, top[u]);
+        best = top2(best, top[u]);
       }
     }
-    raise(s, max2(s.m, best), c2);
+    raise(s, top2(s.m, best), c2);
     add_all(s, x, c2);
   };
   int64_t v = threadIdx.x;

@@ -73,18 +73,12 @@ __device__ inline int uniform(int x) { return __builtin_amdgcn_readfirstlane(x);
 // (a parameter, not an element of a vector: __builtin_bit_cast takes those from the front)
 __device__ inline float word_float(uint32_t x) { return __builtin_bit_cast(float, x); }
 
-// (the compiler would first multiply each operand that comes out of a matrix instruction by
-// 1, against signalling NaN)
+// Largest of three, NaN if one of them is: one instruction, and one that the compiler knows, so
+// that it waits for the matrix and the transcendental instructions whose results these are.
+// (fmaxf, which passes over a NaN, would first multiply each such operand by 1, against signalling
+// NaN.)
 __device__ inline float max3(float a, float b, float c) {
-  float r;
-  asm("v_max3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));
-  return r;
-}
-
-__device__ inline float max2(float a, float b) {
-  float r;
-  asm("v_max_f32 %0, %1, %2" : "=v"(r) : "v"(a), "v"(b));
-  return r;
+  return __builtin_elementwise_maximum(__builtin_elementwise_maximum(a, b), c);
 }
 
 // Sum and maximum over a lane and the one 32 away.

@@ -1,0 +1,21 @@
+"""What the sequence kernels' sources have to keep to, checked without a GPU."""
+import os
+import re
+
+import pytest
+
+CSRC = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))),
+                    "paper_2212_11142_amd", "csrc")
+
+
+@pytest.mark.parametrize("name", ["attend.hip", "attend_few.hip", "attend_grad.hip", "seq_dev.h"])
+def test_no_vector_arithmetic_in_inline_assembly(name):
+    """The results of a matrix or a transcendental instruction may be read a number of cycles
+    later only. The compiler counts them for the instructions that it knows; inline assembly is
+    read as soon as it stands there, so that the attention kernels have none that computes."""
+    text = open(os.path.join(CSRC, name)).read()
+    blocks = re.findall(r"\basm\s*(?:volatile)?\s*\(((?:[^()]|\([^()]*\))*)\)", text)
+    assert blocks or name != "seq_dev.h"
+    for b in blocks:
+        code = "".join(re.findall(r'"((?:[^"\\]|\\.)*)"', b.split(":")[0]))
+        assert not re.search(r"(?<![A-Za-z0-9_])v_[a-z]", code), (name, code)
