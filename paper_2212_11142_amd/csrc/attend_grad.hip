@@ -35,7 +35,7 @@ constexpr int kv_step(int dp, bool narrow) { return narrow || dp == 128 ? 32 : 6
 // Starts the copy of one word per lane into LDS.
 __device__ inline void copy_words(u32x4 buf, int voff, uint32_t lds) {
   const uint32_t m = uniform((int)lds);
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dword %1, %2, 0 offen lds"
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tbuffer_load_dword %1, %2, 0 offen lds"
                ::"s"(m), "v"(voff), "s"(buf)
                : "memory");
 }

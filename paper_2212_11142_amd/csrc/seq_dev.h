@@ -149,7 +149,9 @@ __device__ inline u32x4 row_buffer(const char *base, int64_t r0, int rows, int64
 
 // Starts the copy of ROWS rows of a buffer into an LDS tile by WAVES wavefronts (`wave`
 // is this one's number): each instruction moves 64 pieces of 16 bytes, and what is out of
-// range arrives as zeros. Completion: wait_copies().
+// range arrives as zeros. Completion: wait_copies(). (s_nop: a scalar register that a vector
+// instruction wrote, v_readfirstlane say, must be 5 cycles old when such an instruction reads it;
+// the compiler counts none of them before inline assembly.)
 template <int DP, int ROWS, int WAVES>
 struct TileCopy {
   static constexpr int kPieces = DP / 8;               // pieces of a row
@@ -168,12 +170,29 @@ struct TileCopy {
     lds0 = wave * 1024;
   }
   __device__ void start(u32x4 buf, uint32_t lds) const {
-#pragma unroll
-    for (int i = 0; i < kCount; ++i) {
-      const uint32_t m = uniform((int)(lds + lds0 + i * WAVES * 1024));
-      asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds"
-                   ::"s"(m), "v"(voff[i]), "s"(buf)
+    constexpr int kStep = WAVES * 1024;
+    const uint32_t m = uniform((int)(lds + lds0));
+    if constexpr (kCount == 1) {
+      asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds"
+                   ::"s"(m), "v"(voff[0]), "s"(buf)
                    : "memory");
+    } else if constexpr (kCount == 2) {
+      asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tbuffer_load_dwordx4 %2, %4, 0 offen lds\n\t"
+                   "s_mov_b32 m0, %1\n\ts_nop 0\n\tbuffer_load_dwordx4 %3, %4, 0 offen lds"
+                   ::"s"(m), "s"(m + kStep), "v"(voff[0]), "v"(voff[1]), "s"(buf)
+                   : "memory");
+    } else {
+      static_assert(kCount % 4 == 0);
+#pragma unroll
+      for (int i = 0; i < kCount; i += 4)
+        asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tbuffer_load_dwordx4 %4, %8, 0 offen lds\n\t"
+                     "s_mov_b32 m0, %1\n\ts_nop 0\n\tbuffer_load_dwordx4 %5, %8, 0 offen lds\n\t"
+                     "s_mov_b32 m0, %2\n\ts_nop 0\n\tbuffer_load_dwordx4 %6, %8, 0 offen lds\n\t"
+                     "s_mov_b32 m0, %3\n\ts_nop 0\n\tbuffer_load_dwordx4 %7, %8, 0 offen lds"
+                     ::"s"(m + i * kStep), "s"(m + (i + 1) * kStep), "s"(m + (i + 2) * kStep),
+                     "s"(m + (i + 3) * kStep), "v"(voff[i]), "v"(voff[i + 1]), "v"(voff[i + 2]),
+                     "v"(voff[i + 3]), "s"(buf)
+                     : "memory");
     }
   }
 };
