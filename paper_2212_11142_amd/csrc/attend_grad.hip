@@ -13,8 +13,8 @@
 // 8862 rows in 16 documents, 16 heads of 64 with 4 of keys, prefix masks, cap and table: 163 us,
 // bound by the scores' instructions (cap and bias double them) and by the last blocks' tail.
 //
-// fp16: P is kept times 2^12 and dS times a power of two from a bound of |dS|,
-// 2 max|dO_i| max|v_j|, so that neither leaves fp16's normal range; exact to undo.
+// fp16: P is kept times 2^12 and dS times a power of two from a bound of |dS| in the document and
+// head, 2 max|dO_i| max|v_j|, so that neither leaves fp16's normal range; exact to undo.
 #include <type_traits>
 
 #include "seq_dev.h"
@@ -23,7 +23,6 @@ namespace bgp {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kRowBlocks = 512;    // blocks of the row pass, at most
 constexpr float kP16 = 12.f;       // fp16: log2 of the factor of P
 constexpr int kSkew = 16 * 64;      // floats of a wavefront's skewed values
 
@@ -69,11 +68,15 @@ __device__ __forceinline__ bool add_waves(f32x16 *acc, char *lds) {
 }
 
 // ------------------------------------------------------------------ rows
-// rows[head][row] = {log-sum in units of log 2, D = dO . (O + what its rounding took)}; for
-// fp16 also block maxima of |dO_i|^2 (bound[0..]) and of |v_j|^2 (bound[kRowBlocks..]). 16
-// lanes per row. D is a difference's other half in dS, so it takes O at full precision: the
-// rounding of O alone would double the error of dQ and dK. Bound by reading the three: 8192 rows
-// of 16 heads of 128, 101 MB, 18.3 us, 5.5 TB/s.
+// rows[head][row] = {log-sum in units of log 2, D = dO . (O + what its rounding took)} of the
+// documents' rows. For fp16 also the largest |dO_i|^2 and |v_j|^2 of each 16 rows of a document,
+// at the first of them (bound: [heads][q_rows], then [kv_heads][k_rows]): what lies outside the
+// documents, and rows that saw nothing, take no part. A wavefront per 16 rows and head, 16 lanes
+// per row. D is a difference's other half in dS, so it takes O at full precision: the rounding of O
+// alone would double the error of dQ and dK. Bound by reading the three: 8192 rows of 16 heads of
+// 128, 101 MB, 18.1 us, 5.6 TB/s.
+constexpr int kRowTile = 16;
+constexpr int kRowBlocks = 16384;  // blocks of the row pass, at most
 template <class T>
 __device__ inline float dot8(u32x4 a, u32x4 b) {
   float x = 0.f;
@@ -86,74 +89,90 @@ __device__ inline float dot8(u32x4 a, u32x4 b) {
 }
 
 template <class T>
-__global__ __launch_bounds__(kThreads) void grad_rows(const AttnGradArgs a) {
-  __shared__ float red[2][4];
-  const int l16 = threadIdx.x & 15;
-  const int64_t step = (int64_t)gridDim.x * (kThreads / 16);
+__global__ __launch_bounds__(kThreads) void grad_rows(const AttnGradArgs a, int64_t q_units,
+                                                      int64_t units) {
+  constexpr int kTurns = kRowTile / 4;   // 4 rows at a time
+  const int lane = threadIdx.x & 63, l16 = lane & 15;
   const bool in = l16 * 16 < a.f.bytes;
-  float top = 0.f, vtop = 0.f;
-  const int64_t n = (int64_t)a.f.q_rows * a.f.heads;
-  for (int64_t r = blockIdx.x * (kThreads / 16) + threadIdx.x / 16; r < n; r += step) {
-    const int64_t row = r / a.f.heads;
-    const int head = (int)(r % a.f.heads);
-    float d = 0.f, nrm = 0.f;
-    if (in) {
-      const u32x4 g = *reinterpret_cast<const u32x4 *>(a.dout + row * a.do_row + head * a.do_head + l16 * 16);
-      const u32x4 o = *reinterpret_cast<const u32x4 *>(a.f.o + row * a.f.o_row + head * a.f.o_head + l16 * 16);
-      const u32x4 e = *reinterpret_cast<const u32x4 *>(a.f.rest + row * a.f.rest_row + head * a.f.rest_head + l16 * 16);
-      d = dot8<T>(g, o) + dot8<T>(g, e);
-      if (a.f.fp16) nrm = dot8<T>(g, g);
-    }
+  const u32x4 zero = {};
+  for (int64_t u = (int64_t)blockIdx.x * 4 + uniform(threadIdx.x >> 6); u < units;
+       u += (int64_t)gridDim.x * 4) {
+    const bool keys = u >= q_units;
+    const int heads = keys ? a.f.kv_heads : a.f.heads;
+    const int64_t n = keys ? u - q_units : u;
+    const int head = (int)(n % heads), tile = (int)(n / heads);
+    const DocTile t = keys ? find_tile<kRowTile>(a.f.kb, a.f.ke, a.f.docs, a.f.k_rows, tile)
+                           : find_tile<kRowTile>(a.f.qb, a.f.qe, a.f.docs, a.f.q_rows, tile);
+    if (t.doc < 0) continue;
+    const int first = t.b0 + t.tile * kRowTile, rows = min(t.b1 - first, kRowTile);
+    float top = 0.f;
+    if (keys) {
+      u32x4 v[kTurns];
 #pragma unroll
-    for (int o = 8; o; o >>= 1) {
-      d += __shfl_xor(d, o);
-      if (a.f.fp16) nrm += __shfl_xor(nrm, o);
-    }
-    if (l16 == 0) {
-      const int64_t at = (int64_t)head * a.f.q_rows + row;
-      const float lse = a.f.lse[at];
-      // (a row that saw nothing: +inf, so that its P is 0)
-      a.rows[2 * at] = lse == -__builtin_inff() ? __builtin_inff() : lse * kLog2e;
-      a.rows[2 * at + 1] = d;
-    }
-    top = fmaxf(top, nrm);
-  }
-  if (!a.f.fp16) return;
-  const int64_t nv = (int64_t)a.f.k_rows * a.f.kv_heads;
-  for (int64_t r = blockIdx.x * (kThreads / 16) + threadIdx.x / 16; r < nv; r += step) {
-    float nrm = 0.f;
-    if (in) {
-      const u32x4 v = *reinterpret_cast<const u32x4 *>(a.f.v + (r / a.f.kv_heads) * a.f.v_row +
-                                                       (r % a.f.kv_heads) * a.f.v_head + l16 * 16);
-      nrm = dot8<T>(v, v);
-    }
+      for (int i = 0; i < kTurns; ++i) {
+        const int r = 4 * i + (lane >> 4);
+        v[i] = zero;
+        if (r < rows && in)
+          v[i] = *reinterpret_cast<const u32x4 *>(a.f.v + (int64_t)(first + r) * a.f.v_row +
+                                                  head * a.f.v_head + l16 * 16);
+      }
 #pragma unroll
-    for (int o = 8; o; o >>= 1) nrm += __shfl_xor(nrm, o);
-    vtop = fmaxf(vtop, nrm);   // (NaN is passed over)
-  }
+      for (int i = 0; i < kTurns; ++i) {
+        top = fmaxf(top, row_sum(dot8<T>(v[i], v[i])));
+      }
+    } else {
+      u32x4 g[kTurns], o[kTurns], e[kTurns];
+      float lse[kTurns];
 #pragma unroll
-  for (int o = 32; o; o >>= 1) {
-    top = fmaxf(top, __shfl_xor(top, o));
-    vtop = fmaxf(vtop, __shfl_xor(vtop, o));
-  }
-  if ((threadIdx.x & 63) == 0) {
-    red[0][threadIdx.x >> 6] = top;
-    red[1][threadIdx.x >> 6] = vtop;
-  }
-  __syncthreads();
-  if (threadIdx.x < 2) {
-    const float *x = red[threadIdx.x];
-    a.bound[threadIdx.x * kRowBlocks + blockIdx.x] = fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3]));
+      for (int i = 0; i < kTurns; ++i) {
+        const int r = 4 * i + (lane >> 4);
+        const int64_t row = first + r;
+        lse[i] = r < rows ? a.f.lse[(int64_t)head * a.f.q_rows + row] : -__builtin_inff();
+        g[i] = o[i] = e[i] = zero;
+        if (r < rows && in) {
+          g[i] = *reinterpret_cast<const u32x4 *>(a.dout + row * a.do_row + head * a.do_head + l16 * 16);
+          o[i] = *reinterpret_cast<const u32x4 *>(a.f.o + row * a.f.o_row + head * a.f.o_head + l16 * 16);
+          e[i] = *reinterpret_cast<const u32x4 *>(a.f.rest + row * a.f.rest_row +
+                                                  head * a.f.rest_head + l16 * 16);
+        }
+      }
+#pragma unroll
+      for (int i = 0; i < kTurns; ++i) {
+        const int r = 4 * i + (lane >> 4);
+        const int64_t at = (int64_t)head * a.f.q_rows + first + r;
+        const float d = row_sum(dot8<T>(g[i], o[i]) + dot8<T>(g[i], e[i]));
+        if (l16 == 0 && r < rows) {
+          // (a row that saw nothing: +inf, so that its P is 0)
+          a.rows[2 * at] = lse[i] == -__builtin_inff() ? __builtin_inff() : lse[i] * kLog2e;
+          a.rows[2 * at + 1] = d;
+        }
+        if (a.f.fp16 && lse[i] != -__builtin_inff()) top = fmaxf(top, row_sum(dot8<T>(g[i], g[i])));
+      }
+    }
+    if (a.f.fp16) {
+      top = fmaxf(top, __shfl_xor(top, 16));
+      top = fmaxf(top, __shfl_xor(top, 32));
+      if (lane == 0)
+        a.bound[keys ? (int64_t)a.f.heads * a.f.q_rows + (int64_t)head * a.f.k_rows + first
+                     : (int64_t)head * a.f.q_rows + first] = top;
+    }
   }
 }
 
-// Exponent e of the factor 2^e that dS is kept at: |dS| <= 2 max|dO_i| max|v_j| < 2^15 / 2^e.
-__device__ inline int ds_exponent(const float *bound, int blocks, float *red) {
+// Exponent e of the factor 2^e that dS is kept at, for a document's `heads` heads from `head` on
+// of key head kvh: |dS| <= 2 max|dO_i| max|v_j| < 2^15 / 2^e over its rows q0.. (lq of them) and
+// keys k0.. (lk).
+__device__ inline int ds_exponent(const AttnGradArgs &a, int head, int heads, int kvh, int q0, int lq,
+                                  int k0, int lk, float *red) {
   float x = 0.f, y = 0.f;
-  for (int i = threadIdx.x; i < blocks; i += kThreads) {
-    x = fmaxf(x, bound[i]);
-    y = fmaxf(y, bound[kRowBlocks + i]);
-  }
+  const float *bq = a.bound + (int64_t)head * a.f.q_rows + q0;
+  const float *bv = a.bound + (int64_t)a.f.heads * a.f.q_rows + (int64_t)kvh * a.f.k_rows + k0;
+  for (int h = 0; h < heads; ++h)
+#pragma unroll 4
+    for (int i = threadIdx.x * kRowTile; i < lq; i += kThreads * kRowTile)
+      x = fmaxf(x, bq[(int64_t)h * a.f.q_rows + i]);
+#pragma unroll 4
+  for (int i = threadIdx.x * kRowTile; i < lk; i += kThreads * kRowTile) y = fmaxf(y, bv[i]);
 #pragma unroll
   for (int o = 32; o; o >>= 1) {
     x = fmaxf(x, __shfl_xor(x, o));
@@ -181,8 +200,9 @@ struct GradScale {
   float ds_scale;
   int ds0;
 
-  __device__ void init(const AttnGradArgs &g, int row_blocks, float *red) {
-    ds0 = kHalf ? ds_exponent(g.bound, row_blocks, red) : 0;
+  __device__ void init(const AttnGradArgs &g, int head, int heads, int kvh, int q0, int lq, int k0,
+                       int lk, float *red) {
+    ds0 = kHalf ? ds_exponent(g, head, heads, kvh, q0, lq, k0, lk, red) : 0;
     ds_scale = kHalf ? ldexpf(1.f, ds0) : 1.f;
   }
 };
@@ -198,7 +218,7 @@ struct GradScale {
 // Where few key heads and documents make few blocks of many steps, `shares` blocks take a
 // part of a tile's steps each and leave fp32 sums, which grad_shares adds in order.
 template <class T, int DP, bool CAP, int BIAS, bool NARROW>
-__device__ __forceinline__ void grad_kv(const AttnGradArgs &ga, int row_blocks, int id, char *lds,
+__device__ __forceinline__ void grad_kv(const AttnGradArgs &ga, int id, char *lds,
                                         float *red) {
   constexpr int KS = DP / 16, DT = DP / 32;
   constexpr int kBQ = kv_step(DP, NARROW);     // queries of a step
@@ -278,7 +298,7 @@ __device__ __forceinline__ void grad_kv(const AttnGradArgs &ga, int row_blocks, 
   u32x4 kf[KS];
   load_operand<DP>(a.k + (int64_t)t.b0 * a.k_row + kvh * a.k_head, a.k_row, key, lk, a.bytes, lane, kf);
   GradScale<T> ps;
-  ps.init(ga, row_blocks, red);
+  ps.init(ga, kvh * a.group, a.group, kvh, q0, lq, t.b0, lk, red);
   const ScoreScale sc = score_scale<CAP>(a.scale, a.cap);
   const float p0 = ps.kHalf ? kP16 : 0.f, ds_scale = ps.ds_scale * exp2f(-p0);
   const int reach = BIAS == kBiasTable ? a.buckets.start[a.buckets.per_side - 1] : 0;
@@ -470,7 +490,7 @@ __global__ __launch_bounds__(kThreads) void grad_shares(const AttnGradArgs ga) {
 //
 // NARROW: a block has 32 queries, its wavefronts go over every fourth step of the keys.
 template <class T, int DP, bool CAP, int BIAS, bool NARROW>
-__device__ __forceinline__ void grad_q(const AttnGradArgs &ga, int row_blocks, int id, char *lds,
+__device__ __forceinline__ void grad_q(const AttnGradArgs &ga, int id, char *lds,
                                        float *red) {
   constexpr int KS = DP / 16, DT = DP / 32;
   constexpr int kBN = 32;                      // keys of a step
@@ -538,7 +558,7 @@ __device__ __forceinline__ void grad_q(const AttnGradArgs &ga, int row_blocks, i
   const float lse = ok && lim > 1 ? ga.rows[2 * at] : __builtin_inff();
   const float delta = ok ? ga.rows[2 * at + 1] : 0.f;
   GradScale<T> ps;
-  ps.init(ga, row_blocks, red);
+  ps.init(ga, head, 1, kvh, t.b0, lq, k0, lk, red);
   const ScoreScale sc = score_scale<CAP>(a.scale, a.cap);
   int reach = 0;
   float slope2 = 0.f;
@@ -698,14 +718,14 @@ __device__ __forceinline__ void grad_q(const AttnGradArgs &ga, int row_blocks, i
 // Both in one launch, the longer-running blocks of dK and dV first. (In two
 // launches each kind's last blocks would leave the device idle.)
 template <class T, int DP, bool CAP, int BIAS, bool NARROW>
-__global__ __launch_bounds__(kThreads, NARROW && DP == 128 ? 1 : 2) void grad_pairs(const AttnGradArgs ga, int row_blocks,
+__global__ __launch_bounds__(kThreads, NARROW && DP == 128 ? 1 : 2) void grad_pairs(const AttnGradArgs ga,
                                                           int kv_blocks) {
   extern __shared__ __align__(1024) char lds[];
   __shared__ float red[8];
   if ((int)blockIdx.x < kv_blocks)
-    grad_kv<T, DP, CAP, BIAS, NARROW>(ga, row_blocks, blockIdx.x, lds, red);
+    grad_kv<T, DP, CAP, BIAS, NARROW>(ga, blockIdx.x, lds, red);
   else
-    grad_q<T, DP, CAP, BIAS, NARROW>(ga, row_blocks, blockIdx.x - kv_blocks, lds, red);
+    grad_q<T, DP, CAP, BIAS, NARROW>(ga, blockIdx.x - kv_blocks, lds, red);
 }
 
 // dtable[head][b]: the tiles' partial sums, strided over the threads, then joined in a tree. 4 us,
@@ -724,6 +744,10 @@ __global__ __launch_bounds__(256) void grad_table(const AttnGradArgs a, int unit
     __syncthreads();
   }
   if (threadIdx.x == 0) T::store(a.dtable, (int64_t)head * nb + b, red[0]);
+}
+
+int64_t bound_floats(const AttnArgs &f) {
+  return f.fp16 ? (int64_t)f.q_rows * f.heads + (int64_t)f.k_rows * f.kv_heads : 0;
 }
 
 int64_t tile_bound(int64_t rows, int64_t docs, int64_t longest, int tile) {
@@ -789,7 +813,7 @@ int share_count(const AttnArgs &f) {
 }
 
 template <class T, int DP, bool CAP, int BIAS, bool NARROW>
-hipError_t launch_form(const AttnGradArgs &a, int row_blocks, hipStream_t s) {
+hipError_t launch_form(const AttnGradArgs &a, hipStream_t s) {
   static LdsLimit limit;
   constexpr int kTile = NARROW ? 32 : 128;
   const int lds = pair_bytes(a.f, NARROW);
@@ -801,7 +825,7 @@ hipError_t launch_form(const AttnGradArgs &a, int row_blocks, hipStream_t s) {
   const int64_t blocks = kb + units * a.f.heads;
   if (blocks > 0)
     grad_pairs<T, DP, CAP, BIAS, NARROW>
-        <<<dim3((uint32_t)blocks), kThreads, lds, s>>>(a, row_blocks, (int)kb);
+        <<<dim3((uint32_t)blocks), kThreads, lds, s>>>(a, (int)kb);
   if (a.shares > 1) {
     const int64_t n = tile_bound(a.f.k_rows, a.f.docs, a.f.max_k, kShareRows) * a.f.kv_heads;
     grad_shares<T, DP><<<dim3((uint32_t)n), kThreads, 0, s>>>(a);
@@ -814,22 +838,22 @@ hipError_t launch_form(const AttnGradArgs &a, int row_blocks, hipStream_t s) {
 }
 
 template <class T, int DP, bool CAP, int BIAS>
-hipError_t launch(const AttnGradArgs &a, int row_blocks, hipStream_t s) {
-  if (tile_rows(a.f) == 32) return launch_form<T, DP, CAP, BIAS, true>(a, row_blocks, s);
-  return launch_form<T, DP, CAP, BIAS, false>(a, row_blocks, s);
+hipError_t launch(const AttnGradArgs &a, hipStream_t s) {
+  if (tile_rows(a.f) == 32) return launch_form<T, DP, CAP, BIAS, true>(a, s);
+  return launch_form<T, DP, CAP, BIAS, false>(a, s);
 }
 
 template <class T, int DP>
-hipError_t by_bias(const AttnGradArgs &a, int row_blocks, hipStream_t s) {
+hipError_t by_bias(const AttnGradArgs &a, hipStream_t s) {
   const int bias = a.f.table ? kBiasTable : (a.f.slopes ? kBiasSlope : kBiasNone);
   if (a.f.cap > 0.f) {
-    if (bias == kBiasTable) return launch<T, DP, true, kBiasTable>(a, row_blocks, s);
-    if (bias == kBiasSlope) return launch<T, DP, true, kBiasSlope>(a, row_blocks, s);
-    return launch<T, DP, true, kBiasNone>(a, row_blocks, s);
+    if (bias == kBiasTable) return launch<T, DP, true, kBiasTable>(a, s);
+    if (bias == kBiasSlope) return launch<T, DP, true, kBiasSlope>(a, s);
+    return launch<T, DP, true, kBiasNone>(a, s);
   }
-  if (bias == kBiasTable) return launch<T, DP, false, kBiasTable>(a, row_blocks, s);
-  if (bias == kBiasSlope) return launch<T, DP, false, kBiasSlope>(a, row_blocks, s);
-  return launch<T, DP, false, kBiasNone>(a, row_blocks, s);
+  if (bias == kBiasTable) return launch<T, DP, false, kBiasTable>(a, s);
+  if (bias == kBiasSlope) return launch<T, DP, false, kBiasSlope>(a, s);
+  return launch<T, DP, false, kBiasNone>(a, s);
 }
 
 }  // namespace
@@ -837,7 +861,7 @@ hipError_t by_bias(const AttnGradArgs &a, int row_blocks, hipStream_t s) {
 size_t attend_grad_bytes(const AttnArgs &f) {
   auto up = [](int64_t n) { return (n + 63) / 64 * 64; };
   int64_t n = up(2 * (int64_t)f.q_rows * f.heads);
-  if (f.fp16) n += 2 * kRowBlocks;
+  n += up(bound_floats(f));
   const int nb = bucket_count(f.buckets);
   n += up(tile_bound(f.q_rows, f.docs, f.max_q, tile_rows(f)) * f.heads * nb);
   const int shares = share_count(f);
@@ -850,26 +874,23 @@ hipError_t launch_attend_grad(const AttnGradArgs &args, void *ws, hipStream_t s)
   auto up = [](int64_t n) { return (n + 63) / 64 * 64; };
   a.rows = static_cast<float *>(ws);
   a.bound = a.rows + up(2 * (int64_t)a.f.q_rows * a.f.heads);
-  a.tpart = a.bound + (a.f.fp16 ? 2 * kRowBlocks : 0);
+  a.tpart = a.bound + up(bound_floats(a.f));
   a.kv_part = a.tpart + up(tile_bound(a.f.q_rows, a.f.docs, a.f.max_q, tile_rows(a.f)) * a.f.heads *
                            bucket_count(a.f.buckets));
   a.shares = share_count(a.f);
-  int64_t need = (int64_t)a.f.q_rows * a.f.heads;
-  if (a.f.fp16 && (int64_t)a.f.k_rows * a.f.kv_heads > need) need = (int64_t)a.f.k_rows * a.f.kv_heads;
-  int64_t blocks = (need + kThreads / 16 - 1) / (kThreads / 16);
-  if (!a.f.fp16) {
-    if (blocks > 8192) blocks = 8192;
-  } else if (blocks > kRowBlocks) {
-    blocks = kRowBlocks;
+  const int64_t q_units = tile_bound(a.f.q_rows, a.f.docs, a.f.max_q, kRowTile) * a.f.heads;
+  int64_t units = q_units;
+  if (a.f.fp16) units += tile_bound(a.f.k_rows, a.f.docs, a.f.max_k, kRowTile) * a.f.kv_heads;
+  int64_t blocks = (units + 3) / 4;
+  if (blocks > kRowBlocks) blocks = kRowBlocks;
+  if (blocks > 0) {
+    if (a.f.fp16) grad_rows<Fp16><<<dim3((uint32_t)blocks), kThreads, 0, s>>>(a, q_units, units);
+    else grad_rows<Bf16><<<dim3((uint32_t)blocks), kThreads, 0, s>>>(a, q_units, units);
   }
-  if (blocks < 1) blocks = 1;
-  if (a.f.fp16) grad_rows<Fp16><<<dim3((uint32_t)blocks), kThreads, 0, s>>>(a);
-  else grad_rows<Bf16><<<dim3((uint32_t)blocks), kThreads, 0, s>>>(a);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  const int rb = (int)blocks;
-  if (a.f.bytes <= 128) return a.f.fp16 ? by_bias<Fp16, 64>(a, rb, s) : by_bias<Bf16, 64>(a, rb, s);
-  return a.f.fp16 ? by_bias<Fp16, 128>(a, rb, s) : by_bias<Bf16, 128>(a, rb, s);
+  if (a.f.bytes <= 128) return a.f.fp16 ? by_bias<Fp16, 64>(a, s) : by_bias<Bf16, 64>(a, s);
+  return a.f.fp16 ? by_bias<Fp16, 128>(a, s) : by_bias<Bf16, 128>(a, s);
 }
 
 }  // namespace bgp

@@ -53,7 +53,7 @@ struct AttnGradArgs {
   int64_t do_row, do_head, dq_row, dq_head, dk_row, dk_head, dv_row, dv_head;
   // workspace
   float *rows;                         // [heads][q_rows][2] log-sum, dout . out
-  float *bound;                        // fp16: block maxima and the power of two dS is kept at
+  float *bound;                        // fp16: largest |dout|^2 and |v|^2 of every 16 rows
   float *tpart;                        // [tiles][heads][buckets] partial table gradients
   float *kv_part;                      // [shares][k_rows][kv_heads][dK, dV], with shares
   int32_t shares;                      // blocks of a key tile

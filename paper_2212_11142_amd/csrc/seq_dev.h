@@ -106,13 +106,15 @@ __device__ inline float sum_rows(float x) {
   const u32x2 r = __builtin_amdgcn_permlane16_swap(u, u, false, false);
   return sum_halves(word_float(r[0]) + word_float(r[1]));
 }
-__device__ inline float wave_sum(float x) {
+// over a row of 16 lanes
+__device__ inline float row_sum(float x) {
   x += moved<0xb1>(x);    // quad_perm 1 0 3 2
   x += moved<0x4e>(x);    // quad_perm 2 3 0 1
   x += moved<0x141>(x);   // row_half_mirror
   x += moved<0x140>(x);   // row_mirror
-  return sum_rows(x);
+  return x;
 }
+__device__ inline float wave_sum(float x) { return sum_rows(row_sum(x)); }
 __device__ inline float wave_max(float x) {
   x = fmaxf(x, moved<0xb1>(x));
   x = fmaxf(x, moved<0x4e>(x));
