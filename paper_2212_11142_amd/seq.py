@@ -14,7 +14,7 @@ import math
 from typing import Optional, Sequence
 
 from . import gp
-from .gp import GPError, _check, _ptr, _torch
+from .gp import GPError, _check, _torch
 
 MAX_REACH = 1024     # the last bucket starts at this distance at most
 _INVALID = (1 << (8 * C.sizeof(C.c_size_t))) - 1
@@ -265,14 +265,14 @@ class _Slot:
         return self.ref
 
 
-def _table(table, att: Attention):
+def _table(table, att: Attention, name="table"):
     if (table is None) != (att.buckets is None):
-        raise ValueError("a table goes with a description that has buckets")
+        raise ValueError(f"a {name} goes with a description that has buckets")
     if table is None:
         return None
     if table.shape != att.table_shape or table.dtype is not att.dtype or not table.is_cuda or \
             not table.is_contiguous():
-        raise ValueError(f"table must be a contiguous {att.dtype} CUDA tensor {att.table_shape}")
+        raise ValueError(f"{name} must be a contiguous {att.dtype} CUDA tensor {att.table_shape}")
     return table.data_ptr()
 
 
@@ -304,8 +304,8 @@ def attend_grad_into(att: Attention, q, k, v, dout, bufs: AttendBuffers, table=N
     st = att.lib.gp_attend_grad(
         att.ref, t["q"](q), t["k"](k), t["v"](v), _table(table, att), t["out"](bufs.out),
         t["rest"](bufs.rest), bufs.lse.data_ptr(), t["dout"](dout), t["dq"](bufs.dq),
-        t["dk"](bufs.dk), t["dv"](bufs.dv), _ptr(bufs.dtable), bufs.grad_workspace.data_ptr(),
-        bufs.grad_workspace_bytes, _stream(q))
+        t["dk"](bufs.dk), t["dv"](bufs.dv), _table(bufs.dtable, att, "dtable"),
+        bufs.grad_workspace.data_ptr(), bufs.grad_workspace_bytes, _stream(q))
     if st:
         _check(st)
 
