@@ -300,6 +300,8 @@ def attend_grad_into(att: Attention, q, k, v, dout, bufs: AttendBuffers, table=N
     the out and lse that attend_into left in bufs for the same inputs."""
     if bufs.dq is None:
         raise ValueError("the buffers were made without grad")
+    if not att.docs.k_disjoint:
+        raise ValueError("gradients need documents whose key rows do not overlap")
     t = att.slots
     st = att.lib.gp_attend_grad(
         att.ref, t["q"](q), t["k"](k), t["v"](v), _table(table, att), t["out"](bufs.out),

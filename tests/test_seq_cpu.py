@@ -116,3 +116,14 @@ def test_table_gradient_of_another_layout_refused():
         with pytest.raises(ValueError):
             seq.attend_grad_into(att, q, k, v, q, buffers(att, dtable=dtable), table=table)
     assert not att.lib.calls
+
+
+def test_gradient_of_overlapping_keys_refused():
+    """Two documents' blocks would write the same rows of dk and dv, whoever made the buffers."""
+    att = attention(documents(k_disjoint=False, docs=2))
+    att.lib = Library()
+    q, k, v = inputs(att)
+    seq.attend_into(att, q, k, v, buffers(att))
+    with pytest.raises(ValueError):
+        seq.attend_grad_into(att, q, k, v, q, buffers(att))
+    assert att.lib.calls == ["gp_attend"]
