@@ -175,7 +175,7 @@ __global__ __launch_bounds__(kThreads, 2) void few_kernel(const AttnArgs a, cons
   uint8_t *map = nullptr;
   if (BIAS == kBiasTable) {   // buckets by distance -span..span
     reach = a.buckets.start[a.buckets.per_side - 1];
-    span = max(reach, 1);     // (the sides differ from distance 1 on)
+    span = ahead_reach(reach);
     nb = bucket_count(a.buckets);
     map = reinterpret_cast<uint8_t *>(values + a.group * nb);
     far = T::load(a.table, (int64_t)head * nb + a.buckets.per_side - 1) * kLog2e;

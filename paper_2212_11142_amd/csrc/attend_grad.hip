@@ -371,7 +371,7 @@ __device__ __forceinline__ void grad_kv(const AttnGradArgs &ga, int id, char *ld
       }
       if (BIAS == kBiasTable) {
         const int far_hi = key_lo + 31 - (i0 + shift), far_lo = key_lo - (i0 + 31 + shift);
-        if (far_hi <= -reach || far_lo >= reach) {
+        if (far_hi <= -reach || far_lo >= ahead_reach(reach)) {
           f.b += far_hi <= -reach ? lut[0] : lut[lut_size(reach) - 1];
         } else {
           const float *p = lut + (key - shift - i0 - 4 * h + reach + kLutPad);
@@ -627,7 +627,7 @@ __device__ __forceinline__ void grad_q(const AttnGradArgs &ga, int id, char *lds
         const int d_hi = key0 + 31 - (row_lo + shift), d_lo = key0 - (row_lo + 31 + shift);
         if (d_hi <= -reach) {
           far_l += sum;
-        } else if (d_lo >= reach) {
+        } else if (d_lo >= ahead_reach(reach)) {
           far_r += sum;
         } else {
           // 16 keys at a time: value (key k, query q) at [k][k - q + 31]; what lies outside

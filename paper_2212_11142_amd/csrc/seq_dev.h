@@ -409,6 +409,10 @@ enum BiasKind { kBiasNone = 0, kBiasSlope = 1, kBiasTable = 2 };
 constexpr int kLutPad = 64;
 __host__ __device__ inline int lut_size(int reach) { return 2 * (reach + kLutPad) + 1; }
 
+// Distance from which on keys ahead of a query share a bucket: the sides differ from distance 1 on,
+// with one class a side (reach 0) too.
+__device__ inline int ahead_reach(int reach) { return max(reach, 1); }
+
 // Bucket of the distance delta = key - query position. (The starts past the last one are
 // never reached, so that the comparisons go in eights.)
 __device__ inline int bucket_of(const BucketMap &m, int delta) {
@@ -470,7 +474,7 @@ __device__ inline Affine add_bias(f32x16 &x, const ScoreScale &k, int key0, int 
   }
   if (BIAS == kBiasTable) {
     if (key0 + 31 - pos_lo <= -reach) return Affine{k.a, k.b + lut[0]};
-    if (key0 - (pos_lo + 31) >= reach) return Affine{k.a, k.b + lut[lut_size(reach) - 1]};
+    if (key0 - (pos_lo + 31) >= ahead_reach(reach)) return Affine{k.a, k.b + lut[lut_size(reach) - 1]};
     const float *p = lut + (key0 + 4 * h - pos + reach + kLutPad);
 #pragma unroll
     for (int e = 0; e < 16; ++e) x[e] = __builtin_fmaf(x[e], k.a, p[row_of(e)]);

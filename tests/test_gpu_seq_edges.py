@@ -105,3 +105,14 @@ def test_grad_of_a_document_is_its_own(heads, kv):
     torch.cuda.synchronize()
     for n, rows in (("dq", 450), ("dk", 155), ("dv", 155)):
         assert torch.equal(getattr(got, n)[:rows], getattr(want, n)[:rows]), n
+
+
+# ------------------------------------------------------------------ one class per side
+@pytest.mark.parametrize("heads,kv", [(4, 2), (48, 24)])
+@pytest.mark.parametrize("lens", [[(160, 193)], [(64, 65), (150, 151)], [(200, 233), (3, 36)]])
+@pytest.mark.parametrize("causal", [False, True])
+def test_two_sided_table_of_one_class(heads, kv, lens, causal):
+    """One class per side: distance 0 belongs to the side behind, wherever the pair lies in a
+    tile."""
+    for grad in (False, True):
+        Case("bf16", lens, heads, kv, 64, causal=causal, bias="two", start=(0,), grad=grad).check()
