@@ -32,7 +32,7 @@ constexpr float kSlack = 8.f;
 
 // PARTS = 2: two groups of 4 wavefronts take every second tile each, with LDS buffers of their
 // own, and the first adds up their sums at the end.
-template <class T, int DP, bool CAP, int BIAS, bool REST, int PARTS>
+template <class T, int DP, int CAP, int BIAS, bool REST, int PARTS>
 __global__ __launch_bounds__(kThreads * PARTS, 2) void attend_kernel(const AttnArgs a) {
   constexpr int KS = DP / 16;   // k-steps of the score product
   constexpr int DT = DP / 32;   // column blocks of V
@@ -265,7 +265,7 @@ __global__ __launch_bounds__(kThreads * PARTS, 2) void attend_kernel(const AttnA
   }
 }
 
-template <class T, int DP, bool CAP, int BIAS, bool REST, int PARTS>
+template <class T, int DP, int CAP, int BIAS, bool REST, int PARTS>
 hipError_t launch_parts(const AttnArgs &a, int64_t blocks, hipStream_t s) {
   static LdsLimit limit;
   constexpr int kTiles = PARTS * 4 * kBN * DP * 2;
@@ -293,7 +293,7 @@ bool use_parts(const AttnArgs &a, int64_t blocks) {
   return blocks <= kSeqCus || (blocks <= 2 * kSeqCus && 2 * longest > blocks);
 }
 
-template <class T, int DP, bool CAP, int BIAS, bool REST>
+template <class T, int DP, int CAP, int BIAS, bool REST>
 hipError_t launch_form(const AttnArgs &a, hipStream_t s) {
   // an upper bound of the documents' tiles; the blocks past the last one end at once
   const int64_t tiles = (int64_t)a.q_rows / kBM + a.docs;
@@ -304,30 +304,33 @@ hipError_t launch_form(const AttnArgs &a, hipStream_t s) {
   return launch_parts<T, DP, CAP, BIAS, REST, 1>(a, blocks, s);
 }
 
-template <class T, int DP, bool CAP, int BIAS>
+template <class T, int DP, int CAP, int BIAS>
 hipError_t launch(const AttnArgs &a, hipStream_t s) {
   if (a.rest) return launch_form<T, DP, CAP, BIAS, true>(a, s);
   return launch_form<T, DP, CAP, BIAS, false>(a, s);
 }
 
-template <class T, int DP>
+template <class T, int DP, int CAP>
 hipError_t by_bias(const AttnArgs &a, hipStream_t s) {
-  const int bias = a.table ? kBiasTable : (a.slopes ? kBiasSlope : kBiasNone);
-  if (a.cap > 0.f) {
-    if (bias == kBiasTable) return launch<T, DP, true, kBiasTable>(a, s);
-    if (bias == kBiasSlope) return launch<T, DP, true, kBiasSlope>(a, s);
-    return launch<T, DP, true, kBiasNone>(a, s);
+  if (a.table) return launch<T, DP, CAP, kBiasTable>(a, s);
+  if (a.slopes) return launch<T, DP, CAP, kBiasSlope>(a, s);
+  return launch<T, DP, CAP, kBiasNone>(a, s);
+}
+
+template <class T, int DP>
+hipError_t by_cap(const AttnArgs &a, hipStream_t s) {
+  switch (cap_kind(a.cap)) {
+    case kCapNone: return by_bias<T, DP, kCapNone>(a, s);
+    case kCapNear: return by_bias<T, DP, kCapNear>(a, s);
+    default: return by_bias<T, DP, kCapFar>(a, s);
   }
-  if (bias == kBiasTable) return launch<T, DP, false, kBiasTable>(a, s);
-  if (bias == kBiasSlope) return launch<T, DP, false, kBiasSlope>(a, s);
-  return launch<T, DP, false, kBiasNone>(a, s);
 }
 
 }  // namespace
 
 hipError_t launch_attend(const AttnArgs &a, hipStream_t s) {
-  if (a.bytes <= 128) return a.fp16 ? by_bias<Fp16, 64>(a, s) : by_bias<Bf16, 64>(a, s);
-  return a.fp16 ? by_bias<Fp16, 128>(a, s) : by_bias<Bf16, 128>(a, s);
+  if (a.bytes <= 128) return a.fp16 ? by_cap<Fp16, 64>(a, s) : by_cap<Bf16, 64>(a, s);
+  return a.fp16 ? by_cap<Fp16, 128>(a, s) : by_cap<Bf16, 128>(a, s);
 }
 
 }  // namespace bgp

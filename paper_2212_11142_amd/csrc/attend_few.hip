@@ -101,7 +101,7 @@ __device__ inline void write_quad(const AttnArgs &a, int row, int head, int d, f
 // been read: the eight wavefronts that a compute unit then holds keep more loads in flight than
 // four with two tiles each (64 caches of 2048 keys, 4 key heads of 128: 48 against 58 us; one
 // of 4095: 9.5 against 10.2).
-template <class T, int DP, bool CAP, int BIAS, bool REST>
+template <class T, int DP, int CAP, int BIAS, bool REST>
 __global__ __launch_bounds__(kThreads, 2) void few_kernel(const AttnArgs a, const FewPlan p,
                                                           void *part) {
   constexpr int KS = DP / 16, DT = DP / 32;
@@ -405,7 +405,7 @@ __global__ __launch_bounds__(kThreads) void few_join(const AttnArgs a, const Few
   write_quad<T, REST>(a, q0 + r % lq, kvh * a.group + r / lq, 4 * quad, x, top, ll);
 }
 
-template <class T, int DP, bool CAP, int BIAS, bool REST>
+template <class T, int DP, int CAP, int BIAS, bool REST>
 hipError_t launch_form(const AttnArgs &a, const FewPlan &p, void *part, hipStream_t s) {
   static LdsLimit limit;
   int lds = few_tiles(DP);
@@ -422,24 +422,27 @@ hipError_t launch_form(const AttnArgs &a, const FewPlan &p, void *part, hipStrea
   return hipGetLastError();
 }
 
-template <class T, int DP, bool CAP, int BIAS>
+template <class T, int DP, int CAP, int BIAS>
 hipError_t launch(const AttnArgs &a, void *part, hipStream_t s) {
   const FewPlan p = plan(a.docs, a.kv_heads, a.group, a.max_q, a.max_k);
   if (a.rest) return launch_form<T, DP, CAP, BIAS, true>(a, p, part, s);
   return launch_form<T, DP, CAP, BIAS, false>(a, p, part, s);
 }
 
-template <class T, int DP>
+template <class T, int DP, int CAP>
 hipError_t by_bias(const AttnArgs &a, void *part, hipStream_t s) {
-  const int bias = a.table ? kBiasTable : (a.slopes ? kBiasSlope : kBiasNone);
-  if (a.cap > 0.f) {
-    if (bias == kBiasTable) return launch<T, DP, true, kBiasTable>(a, part, s);
-    if (bias == kBiasSlope) return launch<T, DP, true, kBiasSlope>(a, part, s);
-    return launch<T, DP, true, kBiasNone>(a, part, s);
+  if (a.table) return launch<T, DP, CAP, kBiasTable>(a, part, s);
+  if (a.slopes) return launch<T, DP, CAP, kBiasSlope>(a, part, s);
+  return launch<T, DP, CAP, kBiasNone>(a, part, s);
+}
+
+template <class T, int DP>
+hipError_t by_cap(const AttnArgs &a, void *part, hipStream_t s) {
+  switch (cap_kind(a.cap)) {
+    case kCapNone: return by_bias<T, DP, kCapNone>(a, part, s);
+    case kCapNear: return by_bias<T, DP, kCapNear>(a, part, s);
+    default: return by_bias<T, DP, kCapFar>(a, part, s);
   }
-  if (bias == kBiasTable) return launch<T, DP, false, kBiasTable>(a, part, s);
-  if (bias == kBiasSlope) return launch<T, DP, false, kBiasSlope>(a, part, s);
-  return launch<T, DP, false, kBiasNone>(a, part, s);
 }
 
 }  // namespace
@@ -468,8 +471,8 @@ size_t attend_few_bytes(const AttnArgs &a) {
 
 hipError_t launch_attend_few(const AttnArgs &a, void *part, hipStream_t s) {
   if (a.bytes <= 128)
-    return a.fp16 ? by_bias<Fp16, 64>(a, part, s) : by_bias<Bf16, 64>(a, part, s);
-  return a.fp16 ? by_bias<Fp16, 128>(a, part, s) : by_bias<Bf16, 128>(a, part, s);
+    return a.fp16 ? by_cap<Fp16, 64>(a, part, s) : by_cap<Bf16, 64>(a, part, s);
+  return a.fp16 ? by_cap<Fp16, 128>(a, part, s) : by_cap<Bf16, 128>(a, part, s);
 }
 
 }  // namespace bgp

@@ -217,7 +217,7 @@ struct GradScale {
 //
 // Where few key heads and documents make few blocks of many steps, `shares` blocks take a
 // part of a tile's steps each and leave fp32 sums, which grad_shares adds in order.
-template <class T, int DP, bool CAP, int BIAS, bool NARROW>
+template <class T, int DP, int CAP, int BIAS, bool NARROW>
 __device__ __forceinline__ void grad_kv(const AttnGradArgs &ga, int id, char *lds,
                                         float *red) {
   constexpr int KS = DP / 16, DT = DP / 32;
@@ -357,7 +357,7 @@ __device__ __forceinline__ void grad_kv(const AttnGradArgs &ga, int id, char *ld
           const int e = 4 * g + r;
           s[e] = score_x<CAP>(s[e], sc);
           dp[e] -= delta[r];
-          if (CAP) dp[e] *= cap_slope(s[e]);
+          if (CAP) dp[e] *= cap_slope<CAP>(s[e], sc);
         }
       }
       // the distance falls with the query: add_bias's elements in the other direction
@@ -425,7 +425,7 @@ __device__ __forceinline__ void grad_kv(const AttnGradArgs &ga, int id, char *ld
     if (!add_waves<DT>(dk, lds)) return;
   }
   const bool ok = key < lk;
-  const float fv = exp2f(-p0), fk = a.scale * (CAP ? kCapSlope : 1.f) * ldexpf(1.f, -ps.ds0);
+  const float fv = exp2f(-p0), fk = a.scale * cap_factor<CAP>() * ldexpf(1.f, -ps.ds0);
   if (ga.shares > 1) {
     float *x = ga.kv_part + (((int64_t)share * a.k_rows + t.b0 + key) * a.kv_heads + kvh) * 2 * DP;
     if (ok) {
@@ -489,7 +489,7 @@ __global__ __launch_bounds__(kThreads) void grad_shares(const AttnGradArgs ga) {
 // took 3.5 times as long).
 //
 // NARROW: a block has 32 queries, its wavefronts go over every fourth step of the keys.
-template <class T, int DP, bool CAP, int BIAS, bool NARROW>
+template <class T, int DP, int CAP, int BIAS, bool NARROW>
 __device__ __forceinline__ void grad_q(const AttnGradArgs &ga, int id, char *lds,
                                        float *red) {
   constexpr int KS = DP / 16, DT = DP / 32;
@@ -652,7 +652,7 @@ __device__ __forceinline__ void grad_q(const AttnGradArgs &ga, int id, char *lds
       }
 #pragma unroll
       for (int e = 0; e < 16; ++e) {
-        if (CAP) dp[e] *= cap_slope(z[e]);
+        if (CAP) dp[e] *= cap_slope<CAP>(z[e], sc);
         if (ps.kHalf) dp[e] *= ps.ds_scale;
       }
       u32x4 dr[2];
@@ -676,7 +676,7 @@ __device__ __forceinline__ void grad_q(const AttnGradArgs &ga, int id, char *lds
   }
   if (writes)
     store_row<T, DT>(ga.dq + (int64_t)(t.b0 + row) * ga.dq_row + head * ga.dq_head, ok, a.bytes,
-                     acc, a.scale * (CAP ? kCapSlope : 1.f) * ldexpf(1.f, -ps.ds0), lane);
+                     acc, a.scale * cap_factor<CAP>() * ldexpf(1.f, -ps.ds0), lane);
 
   if (BIAS == kBiasTable) {
 #pragma unroll
@@ -717,7 +717,7 @@ __device__ __forceinline__ void grad_q(const AttnGradArgs &ga, int id, char *lds
 
 // Both in one launch, the longer-running blocks of dK and dV first. (In two
 // launches each kind's last blocks would leave the device idle.)
-template <class T, int DP, bool CAP, int BIAS, bool NARROW>
+template <class T, int DP, int CAP, int BIAS, bool NARROW>
 __global__ __launch_bounds__(kThreads, NARROW && DP == 128 ? 1 : 2) void grad_pairs(const AttnGradArgs ga,
                                                           int kv_blocks) {
   extern __shared__ __align__(1024) char lds[];
@@ -812,7 +812,7 @@ int share_count(const AttnArgs &f) {
   return (int)(s < 8 ? s : 8);
 }
 
-template <class T, int DP, bool CAP, int BIAS, bool NARROW>
+template <class T, int DP, int CAP, int BIAS, bool NARROW>
 hipError_t launch_form(const AttnGradArgs &a, hipStream_t s) {
   static LdsLimit limit;
   constexpr int kTile = NARROW ? 32 : 128;
@@ -837,23 +837,26 @@ hipError_t launch_form(const AttnGradArgs &a, hipStream_t s) {
   return hipGetLastError();
 }
 
-template <class T, int DP, bool CAP, int BIAS>
+template <class T, int DP, int CAP, int BIAS>
 hipError_t launch(const AttnGradArgs &a, hipStream_t s) {
   if (tile_rows(a.f) == 32) return launch_form<T, DP, CAP, BIAS, true>(a, s);
   return launch_form<T, DP, CAP, BIAS, false>(a, s);
 }
 
-template <class T, int DP>
+template <class T, int DP, int CAP>
 hipError_t by_bias(const AttnGradArgs &a, hipStream_t s) {
-  const int bias = a.f.table ? kBiasTable : (a.f.slopes ? kBiasSlope : kBiasNone);
-  if (a.f.cap > 0.f) {
-    if (bias == kBiasTable) return launch<T, DP, true, kBiasTable>(a, s);
-    if (bias == kBiasSlope) return launch<T, DP, true, kBiasSlope>(a, s);
-    return launch<T, DP, true, kBiasNone>(a, s);
+  if (a.f.table) return launch<T, DP, CAP, kBiasTable>(a, s);
+  if (a.f.slopes) return launch<T, DP, CAP, kBiasSlope>(a, s);
+  return launch<T, DP, CAP, kBiasNone>(a, s);
+}
+
+template <class T, int DP>
+hipError_t by_cap(const AttnGradArgs &a, hipStream_t s) {
+  switch (cap_kind(a.f.cap)) {
+    case kCapNone: return by_bias<T, DP, kCapNone>(a, s);
+    case kCapNear: return by_bias<T, DP, kCapNear>(a, s);
+    default: return by_bias<T, DP, kCapFar>(a, s);
   }
-  if (bias == kBiasTable) return launch<T, DP, false, kBiasTable>(a, s);
-  if (bias == kBiasSlope) return launch<T, DP, false, kBiasSlope>(a, s);
-  return launch<T, DP, false, kBiasNone>(a, s);
 }
 
 }  // namespace
@@ -889,8 +892,8 @@ hipError_t launch_attend_grad(const AttnGradArgs &args, void *ws, hipStream_t s)
   }
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  if (a.f.bytes <= 128) return a.f.fp16 ? by_bias<Fp16, 64>(a, s) : by_bias<Bf16, 64>(a, s);
-  return a.f.fp16 ? by_bias<Fp16, 128>(a, s) : by_bias<Bf16, 128>(a, s);
+  if (a.f.bytes <= 128) return a.f.fp16 ? by_cap<Fp16, 64>(a, s) : by_cap<Bf16, 64>(a, s);
+  return a.f.fp16 ? by_cap<Fp16, 128>(a, s) : by_cap<Bf16, 128>(a, s);
 }
 
 }  // namespace bgp

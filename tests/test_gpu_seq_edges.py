@@ -116,3 +116,32 @@ def test_two_sided_table_of_one_class(heads, kv, lens, causal):
     tile."""
     for grad in (False, True):
         Case("bf16", lens, heads, kv, 64, causal=causal, bias="two", start=(0,), grad=grad).check()
+
+
+# ------------------------------------------------------------------ caps
+@pytest.mark.parametrize("heads,kv", [(4, 2), (48, 24)])
+@pytest.mark.parametrize("cap", [1e-3, 0.5, 60.0, 70.0, 1e3, 1e4, 1e6, 1e30, 3e38])
+def test_caps_of_every_size(heads, kv, cap):
+    """A cap far above the scores leaves them as they are, one far below leaves their signs."""
+    for dtype, dim, size in (("fp16", 64, 2.0), ("bf16", 128, 30.0)):
+        Case(dtype, [(140, 140), (33, 70)], heads, kv, dim, cap=cap, bias="two", size=size,
+             grad=True).check()
+
+
+@pytest.mark.parametrize("cap", [64.0, 65.0, 5e3])
+def test_caps_about_the_scores(cap):
+    """Scores on both sides of the cap."""
+    for heads in (2, 96):
+        c = Case("bf16", [(130, 130)], heads, 2, 64, cap=cap, grad=True)
+        c.q *= cap / 8.0
+        c.q[5:9] *= 2.0 ** -20
+        c.check()
+
+
+@pytest.mark.parametrize("cap", [1e-37, 1e-39, 1e-44])
+def test_caps_near_zero(cap):
+    """Scores of nothing: every visible key has the same weight, for queries of 0 too."""
+    for heads in (2, 96):
+        c = Case("bf16", [(130, 130)], heads, 2, 64, cap=cap)
+        c.q[3:60] = 0.0
+        c.check()
