@@ -569,6 +569,13 @@ gp_status gp_logprob(int32_t dtype, const void *x, int64_t stride, int32_t rows,
                      float *entropy, float *lse, float *top_logp, int64_t *top_id,
                      void *workspace, size_t ws_bytes, void *stream);
 
+/* The same, and norm (device float[rows][2] or NULL): a row's largest logit m and log sum
+ * e^(scale (x - m)) (-inf if nothing is left), for the gradient. */
+gp_status gp_logprob_norm(int32_t dtype, const void *x, int64_t stride, int32_t rows,
+                          int32_t width, float scale, const int64_t *target, int32_t top,
+                          float *logp, float *entropy, float *lse, float *norm, float *top_logp,
+                          int64_t *top_id, void *workspace, size_t ws_bytes, void *stream);
+
 /* dx = scale (g_logp (1[target] - p) - g_entropy p (log p + entropy)), of x's type, row
  * stride dx_stride. lse and entropy are gp_logprob's; g_logp (with target) and g_entropy
  * (with entropy) device float[rows] or NULL. A row without a target takes nothing from
@@ -577,6 +584,15 @@ gp_status gp_logprob_grad(int32_t dtype, const void *x, int64_t stride, int32_t 
                           int32_t width, float scale, const int64_t *target, const float *lse,
                           const float *entropy, const float *g_logp, const float *g_entropy,
                           void *dx, int64_t dx_stride, void *stream);
+
+/* The same from gp_logprob_norm's norm in lse's place. One rounded lse costs every p of a row a
+ * relative error of up to 2^-24 |lse|, and a log-sum beyond fp32 the row; from norm the gradient is
+ * as exact whatever a row's logits have in common. */
+gp_status gp_logprob_norm_grad(int32_t dtype, const void *x, int64_t stride, int32_t rows,
+                               int32_t width, float scale, const int64_t *target,
+                               const float *norm, const float *entropy, const float *g_logp,
+                               const float *g_entropy, void *dx, int64_t dx_stride,
+                               void *stream);
 
 /* ---------------------------------------------------------------- inspection */
 

@@ -189,7 +189,7 @@ __device__ inline uint64_t shfl_xor64(uint64_t v, int o) {
 __device__ inline uint64_t max64(uint64_t a, uint64_t b) { return a > b ? a : b; }
 
 struct RowOut {
-  float lse, logp, entropy;
+  float lse, logp, entropy, log_sum;   // (log_sum: of e^(scale (x - m)))
 };
 // (rounding aside, neither is below 0; a NaN stays one)
 __device__ inline float not_below_0(float x) { return x < 0.f ? 0.f : x; }
@@ -202,12 +202,13 @@ __device__ inline RowOut finish(const Sums &s, float scale, bool has, float xt) 
   RowOut r;
   if (s.a == 0.f) {      // nothing but ruled out entries
     const float inf = __builtin_inff();
-    return RowOut{-inf, has ? -inf : 0.f, 0.f};
+    return RowOut{-inf, has ? -inf : 0.f, 0.f, -inf};
   }
   const float c2 = scale * kLog2e, la = log_sum(s, c2);
   r.lse = __builtin_fmaf(scale, s.m, la);
   r.logp = has ? __builtin_fmaf(scale, xt - s.m, -la) : 0.f;
   r.entropy = not_below_0(logf(s.a) - kLn2 * (s.b / s.a));
+  r.log_sum = la;
   return r;
 }
 __device__ inline float alt_logp(const Sums &s, float scale, float x) {
@@ -235,6 +236,10 @@ __device__ inline void write_row(const LogprobArgs &a, int64_t row, const Sums &
   if (a.logp) a.logp[row] = r.logp;
   if (a.entropy) a.entropy[row] = r.entropy;
   if (a.lse) a.lse[row] = r.lse;
+  if (a.norm) {
+    a.norm[2 * row] = s.m;
+    a.norm[2 * row + 1] = r.log_sum;
+  }
 }
 
 // ------------------------------------------------------------------ short rows
@@ -733,7 +738,9 @@ __global__ __launch_bounds__(kThreads) void logprob_grad(const LogprobArgs a, in
   const int64_t step = (int64_t)per_row * threads;
   const char *p = static_cast<const char *>(a.x) + row * a.row * Elem<DT>::kSize;
   char *q = static_cast<char *>(a.dx) + row * a.dx_row * Elem<DT>::kSize;
-  const float lse = a.lse[row];
+  // log p = c x - lse; with the maximum and the log-sum apart c (x - m) - log_sum, whose error does
+  // not grow with what the row's logits have in common
+  const float m = a.norm ? a.norm[2 * row] : 0.f, lse = a.norm ? a.norm[2 * row + 1] : a.lse[row];
   const bool none = lse == -__builtin_inff();
   const int64_t t = a.target ? a.target[row] : -1;
   const bool has = !none && t >= 0 && t < a.width && a.g_logp;
@@ -748,7 +755,7 @@ __global__ __launch_bounds__(kThreads) void logprob_grad(const LogprobArgs a, in
     in.load(v, -__builtin_inff(), x);
 #pragma unroll
     for (int i = 0; i < kVec; ++i) {
-      const float lp = __builtin_fmaf(x[i], a.scale, -lse);
+      const float lp = __builtin_fmaf(x[i] - m, a.scale, -lse);
       const float pr = fast_exp2(lp * kLog2e);
       // -p (g + h (log p + H)), 0 for a ruled out entry
       float y = -pr * __builtin_fmaf(eh, fmaxf(lp, -1e30f), w);

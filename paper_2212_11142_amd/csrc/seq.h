@@ -75,6 +75,7 @@ struct LogprobArgs {
   float scale;
   const int64_t *target;
   float *logp, *entropy, *lse, *top_logp;
+  float *norm;                         // [rows][2] the maximum m, log sum e^(scale (x - m))
   int64_t *top_id;
   const float *g_logp, *g_entropy;     // gradient
   void *dx;

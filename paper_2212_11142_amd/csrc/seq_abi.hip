@@ -135,6 +135,28 @@ gp_status check_logits(int32_t dtype, const void *x, int64_t stride, int32_t row
   return GP_OK;
 }
 
+// From lse or from norm.
+gp_status logprob_grad(int32_t dtype, const void *x, int64_t stride, int32_t rows, int32_t width,
+                       float scale, const int64_t *target, const float *lse, const float *norm,
+                       const float *entropy, const float *g_logp, const float *g_entropy, void *dx,
+                       int64_t dx_stride, void *stream) {
+  gp_status st = check_logits(dtype, x, stride, rows, width, scale, "x");
+  if (st == GP_OK) st = check_logits(dtype, dx, dx_stride, rows, width, scale, "dx");
+  if (st != GP_OK) return st;
+  if (g_logp && !target) return bad("g_logp needs target");
+  if (g_entropy && !entropy) return bad("g_entropy needs entropy");
+  if (rows > 1 && dx_stride < width) return bad("rows of dx overlap");
+  if (rows == 0) return GP_OK;
+  LogprobArgs a;
+  std::memset(&a, 0, sizeof a);
+  a.x = x, a.row = stride, a.rows = rows, a.width = width, a.dtype = dtype, a.scale = scale;
+  a.target = target, a.lse = const_cast<float *>(lse), a.norm = const_cast<float *>(norm);
+  a.entropy = const_cast<float *>(entropy);
+  a.g_logp = g_logp, a.g_entropy = g_entropy, a.dx = dx, a.dx_row = dx_stride;
+  return hip_status(launch_logprob_grad(a, static_cast<hipStream_t>(stream)),
+                    "log probability gradient");
+}
+
 template <class F>
 gp_status guarded(F f) {
   try {
@@ -231,10 +253,10 @@ size_t gp_logprob_workspace_bytes(int32_t rows, int32_t width, int32_t top) {
   return logprob_bytes(rows, width, top);
 }
 
-gp_status gp_logprob(int32_t dtype, const void *x, int64_t stride, int32_t rows, int32_t width,
-                     float scale, const int64_t *target, int32_t top, float *logp, float *entropy,
-                     float *lse, float *top_logp, int64_t *top_id, void *workspace, size_t ws_bytes,
-                     void *stream) {
+gp_status gp_logprob_norm(int32_t dtype, const void *x, int64_t stride, int32_t rows, int32_t width,
+                          float scale, const int64_t *target, int32_t top, float *logp,
+                          float *entropy, float *lse, float *norm, float *top_logp,
+                          int64_t *top_id, void *workspace, size_t ws_bytes, void *stream) {
   return guarded([&]() -> gp_status {
     gp_status st = check_logits(dtype, x, stride, rows, width, scale, "x");
     if (st != GP_OK) return st;
@@ -249,10 +271,18 @@ gp_status gp_logprob(int32_t dtype, const void *x, int64_t stride, int32_t rows,
     std::memset(&a, 0, sizeof a);
     a.x = x, a.row = stride, a.rows = rows, a.width = width, a.top = top, a.dtype = dtype;
     a.scale = scale, a.target = target, a.logp = logp, a.entropy = entropy, a.lse = lse;
-    a.top_logp = top_logp, a.top_id = top_id;
+    a.norm = norm, a.top_logp = top_logp, a.top_id = top_id;
     return hip_status(launch_logprob(a, workspace, static_cast<hipStream_t>(stream)),
                       "log probabilities");
   });
+}
+
+gp_status gp_logprob(int32_t dtype, const void *x, int64_t stride, int32_t rows, int32_t width,
+                     float scale, const int64_t *target, int32_t top, float *logp, float *entropy,
+                     float *lse, float *top_logp, int64_t *top_id, void *workspace, size_t ws_bytes,
+                     void *stream) {
+  return gp_logprob_norm(dtype, x, stride, rows, width, scale, target, top, logp, entropy, lse,
+                         nullptr, top_logp, top_id, workspace, ws_bytes, stream);
 }
 
 gp_status gp_logprob_grad(int32_t dtype, const void *x, int64_t stride, int32_t rows, int32_t width,
@@ -260,21 +290,20 @@ gp_status gp_logprob_grad(int32_t dtype, const void *x, int64_t stride, int32_t 
                           const float *entropy, const float *g_logp, const float *g_entropy,
                           void *dx, int64_t dx_stride, void *stream) {
   return guarded([&]() -> gp_status {
-    gp_status st = check_logits(dtype, x, stride, rows, width, scale, "x");
-    if (st == GP_OK) st = check_logits(dtype, dx, dx_stride, rows, width, scale, "dx");
-    if (st != GP_OK) return st;
     if (rows > 0 && !lse) return bad("lse is NULL");
-    if (g_logp && !target) return bad("g_logp needs target");
-    if (g_entropy && !entropy) return bad("g_entropy needs entropy");
-    if (rows > 1 && dx_stride < width) return bad("rows of dx overlap");
-    if (rows == 0) return GP_OK;
-    LogprobArgs a;
-    std::memset(&a, 0, sizeof a);
-    a.x = x, a.row = stride, a.rows = rows, a.width = width, a.dtype = dtype, a.scale = scale;
-    a.target = target, a.lse = const_cast<float *>(lse), a.entropy = const_cast<float *>(entropy);
-    a.g_logp = g_logp, a.g_entropy = g_entropy, a.dx = dx, a.dx_row = dx_stride;
-    return hip_status(launch_logprob_grad(a, static_cast<hipStream_t>(stream)),
-                      "log probability gradient");
+    return logprob_grad(dtype, x, stride, rows, width, scale, target, lse, nullptr, entropy, g_logp,
+                        g_entropy, dx, dx_stride, stream);
+  });
+}
+
+gp_status gp_logprob_norm_grad(int32_t dtype, const void *x, int64_t stride, int32_t rows,
+                               int32_t width, float scale, const int64_t *target, const float *norm,
+                               const float *entropy, const float *g_logp, const float *g_entropy,
+                               void *dx, int64_t dx_stride, void *stream) {
+  return guarded([&]() -> gp_status {
+    if (rows > 0 && !norm) return bad("norm is NULL");
+    return logprob_grad(dtype, x, stride, rows, width, scale, target, nullptr, norm, entropy, g_logp,
+                        g_entropy, dx, dx_stride, stream);
   });
 }
 

@@ -129,8 +129,12 @@ _SIGS = [
     ("gp_logprob_workspace_bytes", C.c_size_t, [C.c_int32, C.c_int32, C.c_int32]),
     ("gp_logprob", C.c_int, [C.c_int32, _VP, C.c_int64, C.c_int32, C.c_int32, C.c_float, _VP,
                              C.c_int32, _VP, _VP, _VP, _VP, _VP, _VP, C.c_size_t, _VP]),
+    ("gp_logprob_norm", C.c_int, [C.c_int32, _VP, C.c_int64, C.c_int32, C.c_int32, C.c_float, _VP,
+                                  C.c_int32, _VP, _VP, _VP, _VP, _VP, _VP, _VP, C.c_size_t, _VP]),
     ("gp_logprob_grad", C.c_int, [C.c_int32, _VP, C.c_int64, C.c_int32, C.c_int32, C.c_float,
                                   _VP, _VP, _VP, _VP, _VP, _VP, C.c_int64, _VP]),
+    ("gp_logprob_norm_grad", C.c_int, [C.c_int32, _VP, C.c_int64, C.c_int32, C.c_int32, C.c_float,
+                                       _VP, _VP, _VP, _VP, _VP, _VP, C.c_int64, _VP]),
     ("gp_debug_workspace_bytes", C.c_size_t, [C.POINTER(_Space), _VP, C.c_int64]),
     ("gp_debug_encode", C.c_int, [C.POINTER(_Space), C.POINTER(_VP), C.c_int64, _VP, _VP, _VP,
                                   C.c_size_t, _VP]),

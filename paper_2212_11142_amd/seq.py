@@ -316,7 +316,7 @@ def attend_grad_into(att: Attention, q, k, v, dout, bufs: AttendBuffers, table=N
 class LogprobBuffers:
     """Outputs and workspace of logprob calls on [rows, width] logits: logp, entropy, lse
     [rows], with top the best alternatives top_logp and top_id [rows, top], and with grad
-    dlogits."""
+    dlogits and norm [rows, 2] (maxima and log-sums apart, which the gradient reads)."""
 
     def __init__(self, rows: int, width: int, dtype, top: int = 0, grad: bool = False):
         torch = _torch()
@@ -328,6 +328,7 @@ class LogprobBuffers:
                        if top else None)
         self.dlogits = (torch.empty((self.rows, self.width), dtype=dtype, device="cuda")
                         if grad else None)
+        self.norm = torch.empty((self.rows, 2), **f32) if grad else None
         self.code = _dtype_code(dtype)
         self.shape = (self.rows, self.width)
         self.lib = gp.load()
@@ -353,7 +354,7 @@ def _row_vector(x, bufs, dtype, name):
 
 
 def logprob_into(logits, targets, bufs: LogprobBuffers, scale: float = 1.0):
-    """gp_logprob of logits [rows, width] (the rows' stride is free): log p(targets)
+    """gp_logprob_norm of logits [rows, width] (the rows' stride is free): log p(targets)
     (int64 [rows]; outside 0..width-1: no target, 0), entropy and lse of
     softmax(scale * logits), and the bufs.top best entries, into bufs."""
     x, stride = _logits(logits, bufs)
@@ -361,9 +362,11 @@ def logprob_into(logits, targets, bufs: LogprobBuffers, scale: float = 1.0):
     if t is None:
         raise ValueError("targets are required")
     ws, top = bufs.workspace, bufs.top
-    st = bufs.lib.gp_logprob(
+    st = bufs.lib.gp_logprob_norm(
         bufs.code, x, stride, bufs.rows, bufs.width, scale, t, top, bufs.logp.data_ptr(),
-        bufs.entropy.data_ptr(), bufs.lse.data_ptr(), bufs.top_logp.data_ptr() if top else None,
+        bufs.entropy.data_ptr(), bufs.lse.data_ptr(),
+        None if bufs.norm is None else bufs.norm.data_ptr(),
+        bufs.top_logp.data_ptr() if top else None,
         bufs.top_id.data_ptr() if top else None, None if ws is None else ws.data_ptr(),
         bufs.workspace_bytes, _stream(logits))
     if st:
@@ -382,16 +385,16 @@ def logprob(logits, targets, top: int = 0, scale: float = 1.0) -> dict:
 
 def logprob_grad_into(logits, targets, g_logp, g_entropy, bufs: LogprobBuffers,
                       scale: float = 1.0):
-    """gp_logprob_grad into bufs.dlogits, from the gradients (float32 [rows], or None) of
+    """gp_logprob_norm_grad into bufs.dlogits, from the gradients (float32 [rows], or None) of
     logp and entropy and what logprob_into left in bufs for the same inputs."""
     torch = _torch()
     if bufs.dlogits is None:
         raise ValueError("the buffers were made without grad")
     x, stride = _logits(logits, bufs)
     dx, dstride = _logits(bufs.dlogits, bufs, "dlogits")
-    st = bufs.lib.gp_logprob_grad(
+    st = bufs.lib.gp_logprob_norm_grad(
         bufs.code, x, stride, bufs.rows, bufs.width, scale,
-        _row_vector(targets, bufs, torch.int64, "targets"), bufs.lse.data_ptr(),
+        _row_vector(targets, bufs, torch.int64, "targets"), bufs.norm.data_ptr(),
         bufs.entropy.data_ptr(), _row_vector(g_logp, bufs, torch.float32, "g_logp"),
         _row_vector(g_entropy, bufs, torch.float32, "g_entropy"), dx, dstride, _stream(logits))
     if st:

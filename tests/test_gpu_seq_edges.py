@@ -145,3 +145,85 @@ def test_caps_near_zero(cap):
         c = Case("bf16", [(130, 130)], heads, 2, 64, cap=cap)
         c.q[3:60] = 0.0
         c.check()
+
+
+# ------------------------------------------------------------------ offsets of logits
+@pytest.mark.parametrize("rows,width", [(70, 300), (5, 3000), (300, 5000), (6, 70000)])
+@pytest.mark.parametrize("offset", [0.0, 2.0 ** 10, 2.0 ** 20, -2.0 ** 20])
+def test_logprob_grad_of_rows_with_an_offset(rows, width, offset):
+    """What a row's logits have in common cancels: the gradient has the same error with it as
+    without. Logits are multiples of 2^-3 within 16 (exact with the offsets). p = e^d, d a
+    few fp32 roundings of |d| < 64 and of the sum's logarithm off, e of test_gpu_seq.py and
+    2^-18 together; the result is rounded."""
+    import torch
+    from oracle import gp_seq as gs
+    from paper_2212_11142_amd import seq
+    g = torch.Generator().manual_seed(width)
+    x = (torch.randn((rows, width), generator=g) * 2.5).clamp(-16, 16).mul(8).round() / 8
+    t = torch.randint(0, width, (rows,), generator=g)
+    gl, ge = torch.randn(rows, generator=g), torch.randn(rows, generator=g)
+    b = seq.LogprobBuffers(rows, width, torch.float32, grad=True)
+    y, tc = (x + offset).cuda(), t.cuda()
+    assert torch.equal(y.double().cpu() - offset, x.double())
+    seq.logprob_into(y, tc, b)
+    seq.logprob_grad_into(y, tc, gl.cuda(), ge.cuda(), b)
+    torch.cuda.synchronize()
+    f = lambda a: a.double().numpy()
+    r = gs.logprob(f(x), t.numpy(), g_logp=f(gl), g_entropy=f(ge))
+    lp = f(x) - r["lse"][:, None]
+    e = (width / 256 + 64) * 2.0 ** -24 + 2.0 ** -18
+    w = np.abs(f(gl))[:, None] + np.abs(f(ge))[:, None] * (1 + np.abs(lp) + r["entropy"][:, None])
+    near(b.dlogits, r["dlogits"], 2.0 ** -24 * np.abs(r["dlogits"]) + 2 * e * w * np.exp(lp), "dlogits")
+
+
+def test_logprob_grad_of_rows_at_the_types_ends():
+    """Rows whose log-sum is beyond fp32 (the lowest value in every place, at a scale above 1)
+    still have the gradient of equal entries."""
+    import torch
+    from paper_2212_11142_amd import seq
+    for width in (40, 5000):
+        x = torch.full((3, width), torch.finfo(torch.float32).min, device="cuda")
+        x[1] = torch.finfo(torch.float32).max
+        x[2, 1:] = -math.inf
+        x[2, 0] = torch.finfo(torch.float32).max
+        t = torch.tensor([1, 1, 0], device="cuda")
+        b = seq.LogprobBuffers(3, width, torch.float32, grad=True)
+        one = torch.ones(3, device="cuda")
+        seq.logprob_into(x, t, b, scale=2.0)
+        seq.logprob_grad_into(x, t, one, one, b, scale=2.0)
+        want = torch.full((3, width), -2.0 / width, dtype=torch.float64)
+        want[:2, 1] += 2.0
+        want[2] = 0.0
+        assert torch.allclose(b.dlogits.double().cpu(), want, rtol=1e-4, atol=1e-9)
+        assert torch.allclose(b.logp[:2].cpu(), torch.full((2,), -math.log(width)), rtol=1e-5)
+
+
+def test_logprob_grad_from_log_sums_alone():
+    """gp_logprob and gp_logprob_grad, whose only memory of the forward pass is lse and
+    entropy: p's relative error grows with |lse|."""
+    import ctypes as C
+
+    import torch
+    from paper_2212_11142_amd import gp, seq
+    lib = gp.load()
+    rows, width = 9, 700
+    x = torch.randn((rows, width), generator=torch.Generator().manual_seed(0)).cuda()
+    t = torch.arange(rows, device="cuda")
+    gl, ge = torch.randn(rows, device="cuda"), torch.randn(rows, device="cuda")
+    b = seq.LogprobBuffers(rows, width, torch.float32, grad=True)
+    seq.logprob_into(x, t, b)
+    seq.logprob_grad_into(x, t, gl, ge, b)
+    logp, entropy, lse = (torch.empty(rows, device="cuda") for _ in range(3))
+    dx = torch.empty_like(x)
+    p = lambda a: C.c_void_p(a.data_ptr())
+    s = C.c_void_p(torch.cuda.current_stream().cuda_stream)
+    assert lib.gp_logprob(2, p(x), width, rows, width, 1.0, p(t), 0, p(logp), p(entropy), p(lse), None,
+                          None, None, 0, s) == 0
+    assert lib.gp_logprob_grad(2, p(x), width, rows, width, 1.0, p(t), p(lse), p(entropy), p(gl),
+                               p(ge), p(dx), width, s) == 0
+    torch.cuda.synchronize()
+    for a, w in ((logp, b.logp), (entropy, b.entropy), (lse, b.lse)):
+        assert torch.equal(a, w)
+    w = gl.abs()[:, None] + ge.abs()[:, None] * 16
+    bound = torch.exp(x - lse[:, None]) * w * 2.0 ** -24 * 4 * (1 + lse.abs()[:, None]) + 2.0 ** -23 * dx.abs()
+    assert bool(((dx - b.dlogits).abs() <= bound).all())

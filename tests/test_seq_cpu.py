@@ -127,3 +127,17 @@ def test_gradient_of_overlapping_keys_refused():
     with pytest.raises(ValueError):
         seq.attend_grad_into(att, q, k, v, q, buffers(att))
     assert att.lib.calls == ["gp_attend"]
+
+
+def test_norms_are_required():
+    lib = gp.load()
+    def call(**kw):
+        a = dict(norm=256, t=256, e=256, gl=256, ge=256, dx=256, ds=10, rows=2)
+        a.update(kw)
+        return lib.gp_logprob_norm_grad(2, 256, 10, a["rows"], 10, 1.0, a["t"], a["norm"], a["e"],
+                                        a["gl"], a["ge"], a["dx"], a["ds"], None)
+    for kw in (dict(norm=None), dict(t=None), dict(e=None), dict(dx=None), dict(ds=9), dict(rows=-1)):
+        assert call(**kw) == 1, kw
+    assert call(rows=0, norm=None) == 0
+    assert lib.gp_logprob_norm(3, 256, 10, 2, 10, 1.0, 256, 0, 256, None, None, 256, None, None, None, 0,
+                               None) == 1
