@@ -25,11 +25,6 @@ namespace {
 constexpr int kBM = 128;   // queries of a block
 constexpr int kBN = 64;    // keys of a tile
 constexpr int kThreads = 256;
-// The running maximum is raised, and the sums rescaled, only when a row's scores pass it by
-// more than 2^8: the sums then hold values up to 2^8, far from fp32's (and, for the rounded
-// probabilities, fp16's) range, and the rescaling of the output is skipped almost always.
-constexpr float kSlack = 8.f;
-
 // PARTS = 2: two groups of 4 wavefronts take every second tile each, with LDS buffers of their
 // own, and the first adds up their sums at the end.
 template <class T, int DP, int CAP, int BIAS, bool REST, int PARTS>
@@ -62,6 +57,7 @@ __global__ __launch_bounds__(kThreads * PARTS, 2) void attend_kernel(const AttnA
   const int row = row_lo + (lane & 31);
   const int shift = lk - lq;                     // position of query 0
   auto limit = [&](int i) { return a.causal ? min(lk, max(i + shift + 1, prefix)) : lk; };
+  const float slack = Probs<T>::slack(lk), p_shift = Probs<T>::shift(lk);
   const int lim = limit(row);
   const int lim_lo = limit(row_lo);                             // keys all rows see
   const int lim_hi = row_lo < lq ? limit(min(row_lo + 31, lq - 1)) : 0;  // keys any row sees
@@ -143,8 +139,8 @@ __global__ __launch_bounds__(kThreads * PARTS, 2) void attend_kernel(const AttnA
         top = fmaxf(top, __builtin_fmaf(t, f[b].a, f[b].b));
       }
       top = max_halves(top);
-      if (__any(top > m + kSlack)) {
-        const float mn = top > m + kSlack ? top : m;
+      if (__any(top > m + slack)) {
+        const float mn = top > m + slack ? top : m;
         const float r = mn == -__builtin_inff() ? 1.f : fast_exp2(m - mn);
         m = mn;
         l *= r;
@@ -153,7 +149,7 @@ __global__ __launch_bounds__(kThreads * PARTS, 2) void attend_kernel(const AttnA
 #pragma unroll
           for (int e = 0; e < 16; ++e) acc[c][e] *= r;
       }
-      const float ms = m == -__builtin_inff() ? 0.f : m;
+      const float ms = (m == -__builtin_inff() ? 0.f : m) - p_shift;
       u32x4 p[kBN / 16];
 #pragma unroll
       for (int b = 0; b < 2; ++b) {
@@ -252,7 +248,7 @@ __global__ __launch_bounds__(kThreads * PARTS, 2) void attend_kernel(const AttnA
                            a.bytes, acc, inv, lane);
   if (ok && h == 0)
     a.lse[(int64_t)head * a.q_rows + t.b0 + row] =
-        l == 0.f ? -__builtin_inff() : (m + __builtin_amdgcn_logf(l)) * kLn2;
+        l == 0.f ? -__builtin_inff() : (m - p_shift + __builtin_amdgcn_logf(l)) * kLn2;
   if (dirty) {
     __threadfence_block();
     const int first = whole * PARTS * kBN;   // from here on tiles were looked through

@@ -21,7 +21,6 @@ namespace {
 constexpr int kThreads = 256;
 constexpr int kKeys = 32;      // keys of a wavefront's step
 constexpr int kRows = 32;      // rows of a tile
-constexpr float kSlack = 8.f;  // as in the general form
 // Keys of a block, at most: 64 caches of 32,768 at most, 4 key heads of 128, with 512 / 1024 /
 // 2048 / unlimited: 445 / 429 / 445 / 442 us; the same, all full: 808 / 767 / 781 / 781.
 constexpr int kFewChunk = 1024;
@@ -78,10 +77,10 @@ __host__ __device__ inline Part part_of(void *base, const FewPlan &p, int64_t un
   return Part{f, f + (units * p.chunks * p.rows * 2 + 63) / 64 * 64};
 }
 
-// Writes 4 columns of a finished row (sum l at the maximum m, in log 2 units).
+// Writes 4 columns of a finished row (sum l, times 2^p_shift, at the maximum m, in log 2 units).
 template <class T, bool REST>
 __device__ inline void write_quad(const AttnArgs &a, int row, int head, int d, f32x4 x, float m,
-                                  float l) {
+                                  float l, float p_shift) {
   const float inv = l > 0.f ? 1.f / l : (l == 0.f ? 0.f : l);   // a NaN sum stays one
   x *= inv;
   if (2 * d < a.bytes) {
@@ -94,7 +93,7 @@ __device__ inline void write_quad(const AttnArgs &a, int row, int head, int d, f
   }
   if (d == 0)
     a.lse[(int64_t)head * a.q_rows + row] =
-        l == 0.f ? -__builtin_inff() : (m + __builtin_amdgcn_logf(l)) * kLn2;
+        l == 0.f ? -__builtin_inff() : (m - p_shift + __builtin_amdgcn_logf(l)) * kLn2;
 }
 
 // A wavefront has room for one tile of K and one of V, asked for again as soon as they have
@@ -129,6 +128,7 @@ __global__ __launch_bounds__(kThreads, 2) void few_kernel(const AttnArgs a, cons
   const int prefix = (a.causal && a.prefix) ? a.prefix[doc] : 0;
   const int shift = lk - lq;
   auto limit = [&](int i) { return a.causal ? min(lk, max(i + shift + 1, prefix)) : lk; };
+  const float slack = Probs<T>::slack(lk), p_shift = Probs<T>::shift(lk);
   const int n_chunks = max((limit(lq - 1) + p.chunk - 1) / p.chunk, 1);
   if (chunk >= n_chunks || n_chunks > p.chunks) return;
   // a tile within one head has a range of the queries
@@ -236,8 +236,8 @@ __global__ __launch_bounds__(kThreads, 2) void few_kernel(const AttnArgs a, cons
 #pragma unroll
     for (int e = 1; e < 16; ++e) top = fmaxf(top, s[e]);
     top = max_halves(top);
-    if (__any(top > m + kSlack)) {
-      const float mn = top > m + kSlack ? top : m;
+    if (__any(top > m + slack)) {
+      const float mn = top > m + slack ? top : m;
       const float f = mn == -__builtin_inff() ? 1.f : fast_exp2(m - mn);
       m = mn;
       l *= f;
@@ -246,7 +246,7 @@ __global__ __launch_bounds__(kThreads, 2) void few_kernel(const AttnArgs a, cons
 #pragma unroll
         for (int e = 0; e < 16; ++e) acc[c][e] *= f;
     }
-    const float ms = m == -__builtin_inff() ? 0.f : m;
+    const float ms = (m == -__builtin_inff() ? 0.f : m) - p_shift;
     u32x4 pr[2];
 #pragma unroll
     for (int e = 0; e < 16; ++e) {
@@ -332,7 +332,7 @@ __global__ __launch_bounds__(kThreads, 2) void few_kernel(const AttnArgs a, cons
           x[e] += nonfinite_sum<T>(vbase, a.v_row, first, min(limit(qi), key_hi), d + e);
     }
     if (n_chunks == 1) {
-      write_quad<T, REST>(a, q0 + qi, qh, d, x, mm, ll);
+      write_quad<T, REST>(a, q0 + qi, qh, d, x, mm, ll, p_shift);
     } else {
       const int64_t at = (unit * p.chunks + chunk) * p.rows + q;
       *reinterpret_cast<f32x4 *>(pt.o + at * DP + d) = x;
@@ -402,7 +402,8 @@ __global__ __launch_bounds__(kThreads) void few_join(const AttnArgs a, const Few
     ll += f * sml[s][1];
     x += f * so[s][quad];
   }
-  write_quad<T, REST>(a, q0 + r % lq, kvh * a.group + r / lq, 4 * quad, x, top, ll);
+  write_quad<T, REST>(a, q0 + r % lq, kvh * a.group + r / lq, 4 * quad, x, top, ll,
+                      Probs<T>::shift(lk));
 }
 
 template <class T, int DP, int CAP, int BIAS, bool REST>

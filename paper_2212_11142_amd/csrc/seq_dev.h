@@ -67,6 +67,28 @@ struct Fp16 {
   }
 };
 
+// The forward pass's probabilities are e^(score - m) times 2^shift, m the running maximum. It is
+// raised, and the sums rescaled, only when a row's scores pass it by more than `slack` (in log 2):
+// so the rescaling is skipped almost always, and what enters the second product reaches
+// 2^(slack + shift). bf16 has fp32's range for that. fp16 ends at 2^16 and, below its normal
+// numbers, rounds to multiples of 2^-24: with 2^15 for the largest a probability is off by its 11
+// bits' rounding or by 2^-(25 + shift) of the maximum. Up to 4096 keys, 2^-32 each, that is 2^-20 of
+// the largest |v| at most; more keys, each of which may have little, get 2^-39 (2^-19 at 2^20 keys)
+// by raising the maximum more often. Slack 8 / 4 / 1: 1,048,576 rows over 512 keys 1481 / 1509 / 1562
+// us (before 2^shift too), 13 documents of up to 1021 62 / 63.4 / 65.2, one of 16,384 1194 / 1195 /
+// 1196.
+constexpr int kManyKeys = 4096;
+template <class T>
+struct Probs {
+  static __device__ float slack(int) { return 8.f; }
+  static __device__ float shift(int) { return 0.f; }
+};
+template <>
+struct Probs<Fp16> {
+  static __device__ float slack(int lk) { return lk > kManyKeys ? 1.f : 8.f; }
+  static __device__ float shift(int lk) { return 15.f - slack(lk); }
+};
+
 __device__ inline float fast_exp2(float x) { return __builtin_amdgcn_exp2f(x); }
 __device__ inline int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
 

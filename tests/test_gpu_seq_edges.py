@@ -227,3 +227,31 @@ def test_logprob_grad_from_log_sums_alone():
     w = gl.abs()[:, None] + ge.abs()[:, None] * 16
     bound = torch.exp(x - lse[:, None]) * w * 2.0 ** -24 * 4 * (1 + lse.abs()[:, None]) + 2.0 ** -23 * dx.abs()
     assert bool(((dx - b.dlogits).abs() <= bound).all())
+
+
+# ------------------------------------------------------------------ small probabilities
+@pytest.mark.parametrize("heads,rows,keys", [(192, 130, 1 << 16), (24, 120, 1 << 16), (192, 130, 4096),
+                                             (1, 1, 1024), (1, 5, 700)])
+@pytest.mark.parametrize("grad", [False, True])
+def test_small_probabilities_of_many_keys(heads, rows, keys, grad):
+    """fp16: one key has nearly all of the weight and the value 0; the others, e^-18 each,
+    make the output. A probability is kept to half of fp16's smallest step, 2^-25, at 2^7 times
+    the row's (running) maximum, 2^14 in documents of more than 4096 keys: each is off by 2^-32
+    (2^-39) of the largest beside its relative rounding u and e."""
+    import torch
+    from paper_2212_11142_amd import seq
+    d = 64
+    q = torch.zeros((rows, heads, d), dtype=torch.float16, device="cuda")
+    k = torch.zeros((keys, 1, d), dtype=torch.float16, device="cuda")
+    v = torch.full((keys, 1, d), 64.0, dtype=torch.float16, device="cuda")
+    q[:, :, 0], k[0, 0, 0], v[0] = 8.0, 18.0, 0.0
+    att = seq.Attention(seq.Documents([rows], [keys]), heads, 1, d, torch.float16, causal=False)
+    b = seq.AttendBuffers(att, grad=grad)
+    seq.attend_into(att, q, k, v, b)
+    torch.cuda.synchronize()
+    tail = (keys - 1) * math.exp(-18.0)
+    want = 64.0 * tail / (1.0 + tail)
+    u, e = 2.0 ** -11, 2.0 ** -19 * 19
+    bound = 1.1 * ((2 * u + e) * want + 64.0 * keys * 2.0 ** (-39 if keys > 4096 else -32) + 2.0 ** -25)
+    err = (b.out.double() - want).abs().max().item()
+    assert err <= bound, (err, bound, want)
