@@ -289,12 +289,16 @@ bool use_parts(const AttnArgs &a, int64_t blocks) {
   return blocks <= kSeqCus || (blocks <= 2 * kSeqCus && 2 * longest > blocks);
 }
 
+// An upper bound of the documents' tiles; the blocks past the last one end at once.
+int64_t block_count(const AttnArgs &a) {
+  const int64_t tiles = (int64_t)a.q_rows / kBM + a.docs;
+  const int64_t by_max = (int64_t)a.docs * (((int64_t)a.max_q + kBM - 1) / kBM);
+  return (tiles < by_max ? tiles : by_max) * a.heads;
+}
+
 template <class T, int DP, int CAP, int BIAS, bool REST>
 hipError_t launch_form(const AttnArgs &a, hipStream_t s) {
-  // an upper bound of the documents' tiles; the blocks past the last one end at once
-  const int64_t tiles = (int64_t)a.q_rows / kBM + a.docs;
-  const int64_t by_max = (int64_t)a.docs * ((a.max_q + kBM - 1) / kBM);
-  const int64_t blocks = (tiles < by_max ? tiles : by_max) * a.heads;
+  const int64_t blocks = block_count(a);
   if (blocks == 0) return hipSuccess;
   if (use_parts(a, blocks)) return launch_parts<T, DP, CAP, BIAS, REST, 2>(a, blocks, s);
   return launch_parts<T, DP, CAP, BIAS, REST, 1>(a, blocks, s);
@@ -323,6 +327,8 @@ hipError_t by_cap(const AttnArgs &a, hipStream_t s) {
 }
 
 }  // namespace
+
+bool attend_fits(const AttnArgs &a) { return block_count(a) <= kMaxBlocks; }
 
 hipError_t launch_attend(const AttnArgs &a, hipStream_t s) {
   if (a.bytes <= 128) return a.fp16 ? by_cap<Fp16, 64>(a, s) : by_cap<Bf16, 64>(a, s);

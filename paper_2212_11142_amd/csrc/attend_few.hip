@@ -56,10 +56,13 @@ FewPlan plan(int docs, int kv_heads, int group, int max_q, int max_k) {
   // sums between them. Without / with: 192 rows of 16 heads of 128 9.3 / 14.6 us, 1024 rows
   // 19.6 / 50; 64 rows over 4096 keys, 8 heads of 128, 36 / 14; one row, 500 keys 9.1 / 9.1;
   // 64 rows of their own 1000 keys 24.8 / 28.7.
-  if (max_k - c <= 384 + units * p.rows / 4) c = max_k > 0 ? up(max_k) : 128;
+  // (max_k may be a loose bound, and the second kernel has a block per row: both grids fit, or
+  // there is no second kernel)
+  if (max_k - c <= 384 + units * p.rows / 4 || units * p.rows > kMaxBlocks)
+    c = max_k > 0 ? up(max_k) : 128;
   if (c > 1 << 30) c = 1 << 30;
-  // (max_k may be a loose bound: 2^24 blocks are enough, and a grid is 32-bit)
-  const int64_t least = up(max_k * units / (1 << 24));
+  const int64_t most = units > 0 && units < kMaxBlocks ? kMaxBlocks / units : 1;   // ranges
+  const int64_t least = up((max_k + most - 1) / most);
   if (c < least) c = least;
   p.chunk = (int)c;
   p.chunks = (int)((max_k + c - 1) / c);
@@ -460,6 +463,11 @@ bool attend_use_few(const AttnArgs &a) {
   if ((int64_t)a.group * a.max_q <= kRows) return true;
   const int64_t x = (int64_t)a.q_rows / 128 + a.docs, y = (int64_t)a.docs * ((a.max_q + 127) / 128);
   return (x < y ? x : y) * a.heads <= kFewBlocks;
+}
+
+bool attend_few_fits(const AttnArgs &a) {
+  const FewPlan p = plan(a.docs, a.kv_heads, a.group, a.max_q, a.max_k);
+  return (int64_t)a.docs * a.kv_heads * p.row_tiles * p.chunks <= kMaxBlocks;
 }
 
 size_t attend_few_bytes(const AttnArgs &a) {

@@ -812,6 +812,18 @@ int share_count(const AttnArgs &f) {
   return (int)(s < 8 ? s : 8);
 }
 
+// Blocks of the passes over the keys and over the queries.
+struct PairGrid {
+  int64_t kv, units, all;
+};
+PairGrid pair_grid(const AttnArgs &f, int tile, int shares) {
+  PairGrid g;
+  g.kv = tile_bound(f.k_rows, f.docs, f.max_k, tile) * f.kv_heads * shares;
+  g.units = tile_bound(f.q_rows, f.docs, f.max_q, tile);
+  g.all = g.kv + g.units * f.heads;
+  return g;
+}
+
 template <class T, int DP, int CAP, int BIAS, bool NARROW>
 hipError_t launch_form(const AttnGradArgs &a, hipStream_t s) {
   static LdsLimit limit;
@@ -820,19 +832,17 @@ hipError_t launch_form(const AttnGradArgs &a, hipStream_t s) {
   hipError_t e = limit.set(reinterpret_cast<const void *>(&grad_pairs<T, DP, CAP, BIAS, NARROW>),
                            kLdsBytes - 1024);   // (the rest for what is static)
   if (e != hipSuccess) return e;
-  const int64_t kb = tile_bound(a.f.k_rows, a.f.docs, a.f.max_k, kTile) * a.f.kv_heads * a.shares;
-  const int64_t units = tile_bound(a.f.q_rows, a.f.docs, a.f.max_q, kTile);
-  const int64_t blocks = kb + units * a.f.heads;
-  if (blocks > 0)
+  const PairGrid g = pair_grid(a.f, kTile, a.shares);
+  if (g.all > 0)
     grad_pairs<T, DP, CAP, BIAS, NARROW>
-        <<<dim3((uint32_t)blocks), kThreads, lds, s>>>(a, (int)kb);
+        <<<dim3((uint32_t)g.all), kThreads, lds, s>>>(a, (int)g.kv);
   if (a.shares > 1) {
     const int64_t n = tile_bound(a.f.k_rows, a.f.docs, a.f.max_k, kShareRows) * a.f.kv_heads;
     grad_shares<T, DP><<<dim3((uint32_t)n), kThreads, 0, s>>>(a);
   }
   if (BIAS == kBiasTable) {
     const int nb = bucket_count(a.f.buckets);
-    grad_table<T><<<dim3((uint32_t)(a.f.heads * nb)), 256, 0, s>>>(a, (int)units, nb);
+    grad_table<T><<<dim3((uint32_t)(a.f.heads * nb)), 256, 0, s>>>(a, (int)g.units, nb);
   }
   return hipGetLastError();
 }
@@ -870,6 +880,12 @@ size_t attend_grad_bytes(const AttnArgs &f) {
   const int shares = share_count(f);
   if (shares > 1) n += shares * (int64_t)f.k_rows * f.kv_heads * 2 * (f.bytes <= 128 ? 64 : 128);
   return (size_t)n * 4;
+}
+
+bool attend_grad_fits(const AttnArgs &f) {
+  const int shares = share_count(f);
+  const int64_t sums = shares > 1 ? tile_bound(f.k_rows, f.docs, f.max_k, kShareRows) * f.kv_heads : 0;
+  return pair_grid(f, tile_rows(f), shares).all <= kMaxBlocks && sums <= kMaxBlocks;
 }
 
 hipError_t launch_attend_grad(const AttnGradArgs &args, void *ws, hipStream_t s) {

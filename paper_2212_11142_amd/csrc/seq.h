@@ -18,6 +18,8 @@ constexpr int kMaxBuckets = 64;       // buckets of one side
 constexpr int kMaxReach = 1024;       // first distance of the last bucket
 constexpr int kMaxTop = 128;          // alternatives of a row
 constexpr int kLdsBytes = 160 * 1024; // of a compute unit
+// Blocks of 256 threads of a launch, at most: it has fewer than 2^32 threads.
+constexpr int64_t kMaxBlocks = (1 << 24) - 1;
 
 // First distance of each bucket of a side (start[0] = 0, ascending; INT32_MAX past the last).
 struct BucketMap {
@@ -59,13 +61,17 @@ struct AttnGradArgs {
   int32_t shares;                      // blocks of a key tile
 };
 
+// attend_fits and the like: whether a description's grids are within a launch's limits
+bool attend_fits(const AttnArgs &a);
 hipError_t launch_attend(const AttnArgs &a, hipStream_t s);
 // few query rows: key ranges split over blocks; part: attend_few_bytes() of workspace
 size_t attend_few_bytes(const AttnArgs &a);
 bool attend_use_few(const AttnArgs &a);
+bool attend_few_fits(const AttnArgs &a);
 hipError_t launch_attend_few(const AttnArgs &a, void *part, hipStream_t s);
 
 size_t attend_grad_bytes(const AttnArgs &f);
+bool attend_grad_fits(const AttnArgs &f);
 hipError_t launch_attend_grad(const AttnGradArgs &a, void *ws, hipStream_t s);
 
 struct LogprobArgs {

@@ -42,12 +42,6 @@ gp_status check_attention(const gp_attention *t) {
     if (t->bucket_start[t->per_side - 1] > kMaxReach)
       return seq_fail(GP_E_UNSUPPORTED, "the last bucket must start at 1024 or less");
   }
-  // grids are 32-bit
-  const int64_t tiles = (int64_t)t->q_rows / 128 + (int64_t)t->k_rows / 128 + 2 * (int64_t)t->n_docs;
-  if (tiles * t->heads > (int64_t)INT32_MAX) return seq_fail(GP_E_UNSUPPORTED, "too many tiles");
-  const int64_t few = t->max_q < 32 ? t->max_q : 32;    // (a block per row joins the few-row form)
-  if ((int64_t)t->n_docs * t->heads * few > (int64_t)INT32_MAX)
-    return seq_fail(GP_E_UNSUPPORTED, "too many rows");
   return GP_OK;
 }
 
@@ -109,6 +103,13 @@ gp_status check_workspace(const void *ws, size_t bytes, size_t need) {
     return seq_fail(GP_E_WORKSPACE, "workspace too small: need " + std::to_string(need) +
                                         " bytes, have " + std::to_string(bytes));
   return GP_OK;
+}
+
+gp_status check_grids(const AttnArgs &a, bool grad) {
+  const bool ok = grad ? attend_grad_fits(a)
+                       : a.docs == 0 || a.max_q == 0 ||
+                             (attend_use_few(a) ? attend_few_fits(a) : attend_fits(a));
+  return ok ? GP_OK : seq_fail(GP_E_UNSUPPORTED, "too many tiles: a launch has at most 2^24 - 1 blocks");
 }
 
 size_t attend_bytes(const AttnArgs &a) {
@@ -175,9 +176,12 @@ extern "C" {
 size_t gp_attend_workspace_bytes(const gp_attention *t, int32_t with_grad) {
   size_t n = SIZE_MAX;
   guarded([&] {
-    const gp_status st = check_attention(t);
+    gp_status st = check_attention(t);
     if (st != GP_OK) return st;
-    n = with_grad ? attend_grad_bytes(make_args(t)) : attend_bytes(make_args(t));
+    const AttnArgs a = make_args(t);
+    st = check_grids(a, with_grad);
+    if (st != GP_OK) return st;
+    n = with_grad ? attend_grad_bytes(a) : attend_bytes(a);
     return GP_OK;
   });
   return n;
@@ -200,7 +204,8 @@ gp_status gp_attend(const gp_attention *t, const gp_heads *q, const gp_heads *k,
     hipStream_t s = static_cast<hipStream_t>(stream);
     AttnArgs a = make_args(t);
     set_tensors(a, q, k, v, out, rest, table, lse);
-    st = check_workspace(workspace, ws_bytes, attend_bytes(a));
+    st = check_grids(a, false);
+    if (st == GP_OK) st = check_workspace(workspace, ws_bytes, attend_bytes(a));
     if (st != GP_OK) return st;
     if (attend_use_few(a))
       return hip_status(launch_attend_few(a, workspace, s), "attention");
@@ -232,7 +237,8 @@ gp_status gp_attend_grad(const gp_attention *t, const gp_heads *q, const gp_head
     std::memset(&g, 0, sizeof g);
     g.f = make_args(t);
     set_tensors(g.f, q, k, v, out, rest, table, const_cast<float *>(lse));
-    st = check_workspace(workspace, ws_bytes, attend_grad_bytes(g.f));
+    st = check_grids(g.f, true);
+    if (st == GP_OK) st = check_workspace(workspace, ws_bytes, attend_grad_bytes(g.f));
     if (st != GP_OK) return st;
     g.dout = static_cast<const char *>(dout->data);
     g.dq = static_cast<char *>(dq->data);

@@ -141,3 +141,49 @@ def test_norms_are_required():
     assert call(rows=0, norm=None) == 0
     assert lib.gp_logprob_norm(3, 256, 10, 2, 10, 1.0, 256, 0, 256, None, None, 256, None, None, None, 0,
                                None) == 1
+
+
+# ------------------------------------------------------------------ limits of a launch
+BIG = 1 << 30
+
+
+def description(**kw):
+    s = gp._Attention()
+    base = dict(dtype=0, heads=4, kv_heads=2, dim=64, n_docs=1, q_rows=8, k_rows=8, max_q=8, max_k=8,
+                q_begin=16, q_end=16, k_begin=16, k_end=16, causal=1, scale=0.125, cap=0.0)
+    base.update(kw)
+    for k, v in base.items():
+        setattr(s, k, v)
+    return s
+
+
+def workspace(grad=0, **kw):
+    return gp.load().gp_attend_workspace_bytes(C.byref(description(**kw)), grad)
+
+
+REFUSED = C.c_size_t(-1).value
+
+
+@pytest.mark.parametrize("docs", [1, 3, 4096, 5000, (1 << 22) - 3])
+def test_ranges_of_few_rows_fit_a_launch(docs):
+    """A launch has fewer than 2^32 threads, 2^24 - 1 blocks of 256: as many ranges of keys as
+    that leaves, from the workspace, which holds 64 + 2 floats of each row of each range."""
+    n = workspace(q_rows=docs, k_rows=BIG, max_q=1, max_k=BIG, n_docs=docs)
+    rows = 2                                           # the query heads of a key head
+    assert n != REFUSED
+    ranges = n // (rows * 66 * 4)                      # (of all documents and key heads)
+    assert ranges * 256 < 1 << 32
+    assert n == 0 or ranges >= 2 * docs
+
+
+def test_grids_beyond_a_launch_refused():
+    assert workspace(q_rows=BIG, max_q=BIG, n_docs=1) == REFUSED             # 2^23 tiles of 4 heads
+    assert workspace(q_rows=1 << 29, max_q=1 << 29, n_docs=1, heads=2) != REFUSED
+    many = dict(q_rows=1 << 27, k_rows=1 << 27, max_q=1 << 27, max_k=1 << 27, heads=8, kv_heads=8)
+    assert workspace(**many) != REFUSED
+    assert workspace(grad=1, **many) == REFUSED                              # keys' and queries' blocks
+    # many documents of which few can have rows
+    assert workspace(q_rows=1 << 16, k_rows=1 << 16, max_q=100, max_k=100, n_docs=1 << 20) != REFUSED
+    few = dict(q_rows=1 << 23, max_q=1, n_docs=1 << 23, heads=2)
+    assert workspace(kv_heads=1, **few) != REFUSED
+    assert workspace(kv_heads=2, **few) == REFUSED
