@@ -834,16 +834,48 @@ size_t logprob_bytes(int32_t rows, int32_t width, int32_t top) {
   return (size_t)rows * sp.parts * (key_groups(top) * 8 + 16);
 }
 
+// A launch has fewer than 2^32 threads, up to 256 for each row: more rows take several launches.
+// (Rows that several blocks share are fewer.)
+constexpr int32_t kLaunchRows = 1 << 23;
+
+LogprobArgs rows_from(const LogprobArgs &a, int32_t r) {
+  LogprobArgs b = a;
+  const int64_t size = a.dtype == kFp32 ? 4 : 2;
+  b.rows = a.rows - r < kLaunchRows ? a.rows - r : kLaunchRows;
+  b.x = static_cast<const char *>(a.x) + r * a.row * size;
+  if (a.target) b.target = a.target + r;
+  if (a.logp) b.logp = a.logp + r;
+  if (a.entropy) b.entropy = a.entropy + r;
+  if (a.lse) b.lse = a.lse + r;
+  if (a.norm) b.norm = a.norm + 2 * (int64_t)r;
+  if (a.top_logp) b.top_logp = a.top_logp + r * (int64_t)a.top;
+  if (a.top_id) b.top_id = a.top_id + r * (int64_t)a.top;
+  if (a.g_logp) b.g_logp = a.g_logp + r;
+  if (a.g_entropy) b.g_entropy = a.g_entropy + r;
+  if (a.dx) b.dx = static_cast<char *>(a.dx) + r * a.dx_row * size;
+  return b;
+}
+
 hipError_t launch_logprob(const LogprobArgs &a, void *ws, hipStream_t s) {
-  if (a.dtype == kBf16) return forward<kBf16>(a, ws, s);
-  if (a.dtype == kFp16) return forward<kFp16>(a, ws, s);
-  return forward<kFp32>(a, ws, s);
+  hipError_t e = hipSuccess;
+  for (int64_t r = 0; r < a.rows && e == hipSuccess; r += kLaunchRows) {
+    const LogprobArgs b = rows_from(a, (int32_t)r);
+    e = a.dtype == kBf16   ? forward<kBf16>(b, ws, s)
+        : a.dtype == kFp16 ? forward<kFp16>(b, ws, s)
+                           : forward<kFp32>(b, ws, s);
+  }
+  return e;
 }
 
 hipError_t launch_logprob_grad(const LogprobArgs &a, hipStream_t s) {
-  if (a.dtype == kBf16) return gradient<kBf16>(a, s);
-  if (a.dtype == kFp16) return gradient<kFp16>(a, s);
-  return gradient<kFp32>(a, s);
+  hipError_t e = hipSuccess;
+  for (int64_t r = 0; r < a.rows && e == hipSuccess; r += kLaunchRows) {
+    const LogprobArgs b = rows_from(a, (int32_t)r);
+    e = a.dtype == kBf16   ? gradient<kBf16>(b, s)
+        : a.dtype == kFp16 ? gradient<kFp16>(b, s)
+                           : gradient<kFp32>(b, s);
+  }
+  return e;
 }
 
 }  // namespace bgp

@@ -255,3 +255,28 @@ def test_small_probabilities_of_many_keys(heads, rows, keys, grad):
     bound = 1.1 * ((2 * u + e) * want + 64.0 * keys * 2.0 ** (-39 if keys > 4096 else -32) + 2.0 ** -25)
     err = (b.out.double() - want).abs().max().item()
     assert err <= bound, (err, bound, want)
+
+
+# ------------------------------------------------------------------ very many rows
+@pytest.mark.parametrize("rows,width,grad", [((1 << 26) + 5, 3, True), ((1 << 24) + 3, 4100, False)])
+def test_logprob_of_more_rows_than_a_launch_takes(rows, width, grad):
+    """A launch has fewer than 2^32 threads: these rows take several. (One stored row, read
+    by all.)"""
+    import torch
+    from paper_2212_11142_amd import seq
+    x = torch.randn((1, width), generator=torch.Generator().manual_seed(0)).bfloat16().cuda()
+    few = seq.LogprobBuffers(2, width, torch.bfloat16, grad=grad)
+    many = seq.LogprobBuffers(rows, width, torch.bfloat16, grad=grad)
+    for t in (many.logp, many.entropy, many.lse):
+        t.fill_(7.0)
+    for b in (few, many):
+        n = b.rows
+        t = torch.arange(n, device="cuda") % 2
+        seq.logprob_into(x.expand(n, -1), t, b)
+        if grad:
+            one = torch.ones(n, device="cuda")
+            seq.logprob_grad_into(x.expand(n, -1), t, one, None, b)
+    names = ("logp", "entropy", "lse") + (("dlogits",) if grad else ())
+    for n in names:
+        a, w = getattr(many, n), getattr(few, n)
+        assert bool((a[0::2] == w[0]).all()) and bool((a[1::2] == w[1]).all()), n
