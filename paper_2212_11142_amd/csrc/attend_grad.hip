@@ -838,7 +838,8 @@ hipError_t launch_form(const AttnGradArgs &a, hipStream_t s) {
         <<<dim3((uint32_t)g.all), kThreads, lds, s>>>(a, (int)g.kv);
   if (a.shares > 1) {
     const int64_t n = tile_bound(a.f.k_rows, a.f.docs, a.f.max_k, kShareRows) * a.f.kv_heads;
-    grad_shares<T, DP><<<dim3((uint32_t)n), kThreads, 0, s>>>(a);
+    if (n > 0)   // (a cache of which no document has a row yet)
+      grad_shares<T, DP><<<dim3((uint32_t)n), kThreads, 0, s>>>(a);
   }
   if (BIAS == kBiasTable) {
     const int nb = bucket_count(a.f.buckets);

@@ -280,3 +280,23 @@ def test_logprob_of_more_rows_than_a_launch_takes(rows, width, grad):
     for n in names:
         a, w = getattr(many, n), getattr(few, n)
         assert bool((a[0::2] == w[0]).all()) and bool((a[1::2] == w[1]).all()), n
+
+
+# ------------------------------------------------------------------ nothing to read
+@pytest.mark.parametrize("bias", [False, True])
+def test_grad_of_documents_without_keys(bias):
+    """Many queries over a cache in which their documents have no keys yet."""
+    import torch
+    from paper_2212_11142_amd import seq
+    docs = seq.Documents([1000, 700], [0, 0], k_rows=640)
+    buckets = seq.Buckets([0, 3]) if bias else None
+    att = seq.Attention(docs, 4, 2, 64, torch.bfloat16, buckets=buckets)
+    q, k = (torch.ones((n, h, 64), dtype=torch.bfloat16, device="cuda") for n, h in ((1700, 4), (640, 2)))
+    table = torch.ones((4, 2), dtype=torch.bfloat16, device="cuda") if bias else None
+    b = seq.AttendBuffers(att, grad=True)
+    seq.attend_into(att, q, k, k, b, table=table)
+    seq.attend_grad_into(att, q, k, k, q, b, table=table)
+    torch.cuda.synchronize()
+    for x in (b.out, b.dq, b.dk, b.dv) + ((b.dtable,) if bias else ()):
+        assert bool((x == 0).all())
+    assert bool(b.lse.isneginf().all())
