@@ -91,7 +91,7 @@ class Documents:
         spans = sorted((b, b + x) for b, x in zip(kb, k_len) if x > 0)
         self.k_disjoint = all(a[1] <= b[0] for a, b in zip(spans, spans[1:]))
         self.k_full = self.k_disjoint and sum(k_len) == self.k_rows
-        self.n = n
+        self.n, self.moving = n, False
         self.max_q, self.max_k = max(q_len, default=0), max(k_len, default=0)
         rows = [qb, [a + b for a, b in zip(qb, q_len)], kb, [a + b for a, b in zip(kb, k_len)],
                 [0] * n if prefix is None else [int(x) for x in prefix]]
@@ -105,11 +105,14 @@ class Documents:
         self.sorted = both[1]
 
     @classmethod
-    def on_device(cls, q_begin, q_end, k_begin, k_end, q_rows, k_rows, max_q, max_k, prefix=None):
+    def on_device(cls, q_begin, q_end, k_begin, k_end, q_rows, k_rows, max_q, max_k, prefix=None,
+                  q_full=False, k_full=False):
         """From int32 CUDA tensors that already hold the ranges (a cache whose lengths grow
         on the device, e.g. within a captured graph). max_q and max_k bound the lengths.
-        Nothing is read back, so gradients of rows outside the documents are zeroed by the
-        buffers, and disjoint key ranges are the caller's promise."""
+        Nothing is read back: disjoint key ranges are the caller's promise, and as the ranges
+        may have moved since the last call, every call first clears its outputs. q_full and
+        k_full promise that every query (key) row is always some document's, so that there
+        is nothing to clear."""
         torch = _torch()
         self = cls.__new__(cls)
         ts = [q_begin, q_end, k_begin, k_end] + ([prefix] if prefix is not None else [])
@@ -123,8 +126,8 @@ class Documents:
         self.n = int(q_begin.shape[0])
         self.q_rows, self.k_rows = int(q_rows), int(k_rows)
         self.max_q, self.max_k = int(max_q), int(max_k)
-        self.q_full = self.k_full = False
-        self.k_disjoint = True
+        self.q_full, self.k_full = bool(q_full), bool(k_full)
+        self.k_disjoint = self.moving = True
         return self
 
 
@@ -214,7 +217,8 @@ class Attention:
 class AttendBuffers:
     """Outputs and workspaces of attention calls with a description: out, lse
     [heads, q_rows], and with grad dq, dk, dv and (with buckets) dtable, and rest (what
-    rounding took from out, which the gradient reads). Rows outside every document are 0."""
+    rounding took from out, which the gradient reads). Rows outside every document are 0
+    (lse -inf)."""
 
     def __init__(self, att: Attention, grad: bool = False):
         torch = _torch()
@@ -281,10 +285,13 @@ def attend_into(att: Attention, q, k, v, bufs: AttendBuffers, table=None):
     [q_rows, heads, dim], k and v [k_rows, kv_heads, dim]; strides of rows and heads are
     free (multiples of 8)."""
     t, ws, rest = att.slots, bufs.workspace, bufs.rest
-    st = att.lib.gp_attend(att.ref, t["q"](q), t["k"](k), t["v"](v), _table(table, att),
-                           t["out"](bufs.out), None if rest is None else t["rest"](rest),
-                           bufs.lse.data_ptr(), None if ws is None else ws.data_ptr(),
-                           bufs.workspace_bytes, _stream(q))
+    args = (att.ref, t["q"](q), t["k"](k), t["v"](v), _table(table, att), t["out"](bufs.out),
+            None if rest is None else t["rest"](rest), bufs.lse.data_ptr(),
+            None if ws is None else ws.data_ptr(), bufs.workspace_bytes, _stream(q))
+    if att.docs.moving and not att.docs.q_full:
+        bufs.out.zero_()
+        bufs.lse.fill_(-math.inf)
+    st = att.lib.gp_attend(*args)
     if st:
         _check(st)
 
@@ -303,11 +310,16 @@ def attend_grad_into(att: Attention, q, k, v, dout, bufs: AttendBuffers, table=N
     if not att.docs.k_disjoint:
         raise ValueError("gradients need documents whose key rows do not overlap")
     t = att.slots
-    st = att.lib.gp_attend_grad(
-        att.ref, t["q"](q), t["k"](k), t["v"](v), _table(table, att), t["out"](bufs.out),
-        t["rest"](bufs.rest), bufs.lse.data_ptr(), t["dout"](dout), t["dq"](bufs.dq),
-        t["dk"](bufs.dk), t["dv"](bufs.dv), _table(bufs.dtable, att, "dtable"),
-        bufs.grad_workspace.data_ptr(), bufs.grad_workspace_bytes, _stream(q))
+    args = (att.ref, t["q"](q), t["k"](k), t["v"](v), _table(table, att), t["out"](bufs.out),
+            t["rest"](bufs.rest), bufs.lse.data_ptr(), t["dout"](dout), t["dq"](bufs.dq),
+            t["dk"](bufs.dk), t["dv"](bufs.dv), _table(bufs.dtable, att, "dtable"),
+            bufs.grad_workspace.data_ptr(), bufs.grad_workspace_bytes, _stream(q))
+    if att.docs.moving:
+        for x, full in ((bufs.dq, att.docs.q_full), (bufs.dk, att.docs.k_full),
+                        (bufs.dv, att.docs.k_full)):
+            if not full:
+                x.zero_()
+    st = att.lib.gp_attend_grad(*args)
     if st:
         _check(st)
 

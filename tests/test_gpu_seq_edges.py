@@ -282,6 +282,59 @@ def test_logprob_of_more_rows_than_a_launch_takes(rows, width, grad):
         assert bool((a[0::2] == w[0]).all()) and bool((a[1::2] == w[1]).all()), n
 
 
+# ------------------------------------------------------------------ ranges that move
+@pytest.mark.parametrize("heads,kv", [(4, 2), (96, 2)])
+def test_rows_that_leave_the_documents_become_zero(heads, kv):
+    """Ranges on the device shrink between calls: the outputs of the rows that no document has
+    now are 0 (lse -inf), not the earlier call's."""
+    import torch
+    from paper_2212_11142_amd import seq
+    i32 = dict(dtype=torch.int32, device="cuda")
+    qb, qe = torch.tensor([0, 150], **i32), torch.tensor([150, 300], **i32)
+    kb, ke = torch.tensor([0, 150], **i32), torch.tensor([150, 300], **i32)
+    docs = seq.Documents.on_device(qb, qe, kb, ke, 300, 300, 150, 150)
+    att = seq.Attention(docs, heads, kv, 64, torch.bfloat16)
+    g = torch.Generator().manual_seed(0)
+    q, do = (torch.randn((300, heads, 64), generator=g).bfloat16().cuda() for _ in range(2))
+    k, v = (torch.randn((300, kv, 64), generator=g).bfloat16().cuda() for _ in range(2))
+
+    def call(b):
+        seq.attend_into(att, q, k, v, b)
+        seq.attend_grad_into(att, q, k, v, do, b)
+        torch.cuda.synchronize()
+
+    b = seq.AttendBuffers(att, grad=True)
+    call(b)
+    assert bool((b.dq[100:150] != 0).any())
+    qe[0], ke[0] = 100, 120
+    call(b)
+    fresh = seq.AttendBuffers(att, grad=True)
+    call(fresh)
+    for n in ("out", "dq"):
+        assert bool((getattr(b, n)[100:150] == 0).all()), n
+    for n in ("dk", "dv"):
+        assert bool((getattr(b, n)[120:150] == 0).all()), n
+    assert bool(b.lse[:, 100:150].isneginf().all())
+    for n in ("out", "lse", "dq", "dk", "dv"):
+        assert torch.equal(getattr(b, n), getattr(fresh, n)), n
+
+
+def test_ranges_that_cover_every_row():
+    """The promise that documents have every query row leaves the outputs' clearing out."""
+    import torch
+    from paper_2212_11142_amd import seq
+    i32 = dict(dtype=torch.int32, device="cuda")
+    at = torch.arange(3, **i32)
+    ke = torch.tensor([40, 90, 130], **i32)
+    docs = seq.Documents.on_device(at, at + 1, at * 200, at * 200 + ke, 3, 600, 1, 200, q_full=True)
+    att = seq.Attention(docs, 4, 2, 64, torch.bfloat16)
+    q, k, v = (torch.randn(s, device="cuda").bfloat16() for s in ((3, 4, 64), (600, 2, 64), (600, 2, 64)))
+    got = seq.attend(att, q, k, v)
+    want = seq.attend(seq.Attention(seq.Documents([1] * 3, [40, 90, 130], k_begin=[0, 200, 400], k_rows=600),
+                                    4, 2, 64, torch.bfloat16), q, k, v)
+    assert torch.equal(got["out"], want["out"]) and torch.equal(got["lse"], want["lse"])
+
+
 # ------------------------------------------------------------------ nothing to read
 @pytest.mark.parametrize("bias", [False, True])
 def test_grad_of_documents_without_keys(bias):

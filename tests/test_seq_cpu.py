@@ -60,8 +60,7 @@ def documents(q_rows=8, k_rows=8, docs=1, max_q=None, max_k=None, **kw):
     d.prefix, d.n, d.q_rows, d.k_rows = None, docs, q_rows, k_rows
     d.max_q, d.max_k = max_q or q_rows, max_k or k_rows
     d.q_full = d.k_full = d.k_disjoint = True
-    d.on_dev = False
-    d.device = 0
+    d.moving = False
     for k, v in kw.items():
         setattr(d, k, v)
     return d
