@@ -5,12 +5,14 @@ and the log probabilities of an output row with theirs.
 As in ``gp``, this module only marshals arguments. A layout of documents and an `Attention`
 description are made once per batch shape, buffers once per use; the `*_into` calls are
 asynchronous on the current stream, and the plain calls allocate their outputs. A
-description's tensors and a call's buffers belong to one stream at a time.
+description's tensors and a call's buffers belong to one stream at a time; threads may share a
+description, each with buffers of its own.
 """
 from __future__ import annotations
 
 import ctypes as C
 import math
+import threading
 from typing import Optional, Sequence
 
 from . import gp
@@ -200,10 +202,7 @@ class Attention:
         self.lib = gp.load()
         self.workspace_bytes(False)          # raises if the description is invalid
         self.table_shape = None if buckets is None else (self.heads, buckets.count)
-        self.slots = {n: _Slot(n, docs.q_rows, self.heads, self)
-                      for n in ("q", "out", "rest", "dout", "dq")}
-        self.slots.update({n: _Slot(n, docs.k_rows, self.kv_heads, self)
-                           for n in ("k", "v", "dk", "dv")})
+        self.slots = _Slots(self)
 
     def workspace_bytes(self, with_grad: bool) -> int:
         lib = gp.load()
@@ -269,6 +268,16 @@ class _Slot:
         return self.ref
 
 
+class _Slots(threading.local):
+    """A description's slots, a set per thread: a call releases the interpreter while the
+    library reads them."""
+
+    def __init__(self, att):
+        d = att.docs
+        self.of = {n: _Slot(n, d.q_rows, att.heads, att) for n in ("q", "out", "rest", "dout", "dq")}
+        self.of.update({n: _Slot(n, d.k_rows, att.kv_heads, att) for n in ("k", "v", "dk", "dv")})
+
+
 def _table(table, att: Attention, name="table"):
     if (table is None) != (att.buckets is None):
         raise ValueError(f"a {name} goes with a description that has buckets")
@@ -284,7 +293,7 @@ def attend_into(att: Attention, q, k, v, bufs: AttendBuffers, table=None):
     """gp_attend into bufs.out and bufs.lse (asynchronous on the current stream). q
     [q_rows, heads, dim], k and v [k_rows, kv_heads, dim]; strides of rows and heads are
     free (multiples of 8)."""
-    t, ws, rest = att.slots, bufs.workspace, bufs.rest
+    t, ws, rest = att.slots.of, bufs.workspace, bufs.rest
     args = (att.ref, t["q"](q), t["k"](k), t["v"](v), _table(table, att), t["out"](bufs.out),
             None if rest is None else t["rest"](rest), bufs.lse.data_ptr(),
             None if ws is None else ws.data_ptr(), bufs.workspace_bytes, _stream(q))
@@ -309,7 +318,7 @@ def attend_grad_into(att: Attention, q, k, v, dout, bufs: AttendBuffers, table=N
         raise ValueError("the buffers were made without grad")
     if not att.docs.k_disjoint:
         raise ValueError("gradients need documents whose key rows do not overlap")
-    t = att.slots
+    t = att.slots.of
     args = (att.ref, t["q"](q), t["k"](k), t["v"](v), _table(table, att), t["out"](bufs.out),
             t["rest"](bufs.rest), bufs.lse.data_ptr(), t["dout"](dout), t["dq"](bufs.dq),
             t["dk"](bufs.dk), t["dv"](bufs.dv), _table(bufs.dtable, att, "dtable"),

@@ -186,3 +186,34 @@ def test_grids_beyond_a_launch_refused():
     few = dict(q_rows=1 << 23, max_q=1, n_docs=1 << 23, heads=2)
     assert workspace(kv_heads=1, **few) != REFUSED
     assert workspace(kv_heads=2, **few) == REFUSED
+
+
+# ------------------------------------------------------------------ threads
+def test_threads_share_a_description():
+    """A call releases the interpreter: another thread's call with the same description and
+    buffers of its own must not change the arguments of this one."""
+    import threading
+    att = attention()
+    entered, done, found = threading.Event(), threading.Event(), {}
+
+    def seen(name, args):
+        me = threading.current_thread().name
+        if me == "first":
+            entered.set()
+            assert done.wait(20)
+        found[me] = [a._obj.data for a in (args[1], args[2], args[3], args[5])]
+
+    att.lib = Library(seen)
+
+    def call(at):
+        seq.attend_into(att, *inputs(att, at=at), buffers(att, at=2 * at))
+
+    first = threading.Thread(target=call, args=(1 << 20,), name="first")
+    first.start()
+    assert entered.wait(20)
+    second = threading.Thread(target=call, args=(1 << 28,), name="second")
+    second.start()
+    second.join(20)
+    done.set()
+    first.join(20)
+    assert found == {"first": [1 << 20] * 3 + [1 << 21], "second": [1 << 28] * 3 + [1 << 29]}
