@@ -40,11 +40,29 @@ def _stream(x):
     return raw(x.get_device())
 
 
-def _workspace(nbytes):
-    """A workspace and its size."""
+def _current_device():
+    torch = _torch()
+    raw = getattr(torch._C, "_cuda_getDevice", None)
+    return torch.cuda.current_device() if raw is None else raw()
+
+
+def _call(device, f, args):
+    """f(*args) with `device` current: a launch is the current device's."""
+    if _current_device() == device:
+        st = f(*args)
+    else:
+        with _torch().cuda.device(device):
+            st = f(*args)
+    if st:
+        _check(st)
+
+
+def _workspace(nbytes, device):
+    """A workspace and its size. (torch's allocator returns 512-byte aligned blocks.)"""
     if not nbytes:
         return None, 0
-    ws = gp._workspace(nbytes)
+    torch = _torch()
+    ws = torch.empty(max(int(nbytes), 256), dtype=torch.uint8, device=torch.device("cuda", device))
     return ws, ws.numel()
 
 
@@ -105,6 +123,7 @@ class Documents:
         self.q_begin, self.q_end, self.k_begin, self.k_end, pre = both[0]
         self.prefix = None if prefix is None else pre
         self.sorted = both[1]
+        self.device = both.get_device()
 
     @classmethod
     def on_device(cls, q_begin, q_end, k_begin, k_end, q_rows, k_rows, max_q, max_k, prefix=None,
@@ -120,8 +139,10 @@ class Documents:
         ts = [q_begin, q_end, k_begin, k_end] + ([prefix] if prefix is not None else [])
         for t in ts:
             if t.dtype != torch.int32 or not t.is_cuda or not t.is_contiguous() or \
-                    t.dim() != 1 or t.shape[0] != q_begin.shape[0]:
-                raise ValueError("ranges must be contiguous int32 CUDA vectors of one length")
+                    t.dim() != 1 or t.shape[0] != q_begin.shape[0] or t.device != q_begin.device:
+                raise ValueError("ranges must be contiguous int32 vectors of one length on one "
+                                 "CUDA device")
+        self.device = q_begin.get_device()
         self.q_begin, self.q_end, self.k_begin, self.k_end = ts[:4]
         self.prefix = prefix
         self.sorted = ts + [None] * (5 - len(ts))    # (in the order given)
@@ -167,7 +188,7 @@ def log_buckets(per_side: int, max_distance: int, two_sided: bool = False) -> Bu
 
 # ------------------------------------------------------------------ attention
 class Attention:
-    """What is attended to and how: documents, heads (a multiple of kv_heads), head size,
+    """What is attended to and how, on the documents' device: documents, heads (a multiple of kv_heads), head size,
     dtype (torch.bfloat16 or torch.float16), causal or full mask (a prefix is the
     documents'), scale (1 / sqrt(dim) if None), cap of the scores by a tanh (0: none), and a
     bias by distance: slopes (float32 CUDA [heads], -slope |distance|) or Buckets (the table
@@ -179,9 +200,12 @@ class Attention:
         torch = _torch()
         self.docs, self.heads, self.kv_heads, self.dim = docs, int(heads), int(kv_heads), int(dim)
         self.dtype, self.buckets, self.slopes = dtype, buckets, slopes
-        if slopes is not None and (slopes.dtype != torch.float32 or not slopes.is_cuda or
+        self.device = docs.device
+        if slopes is not None and (slopes.dtype != torch.float32 or
+                                   slopes.get_device() != self.device or
                                    not slopes.is_contiguous() or tuple(slopes.shape) != (heads,)):
-            raise ValueError("slopes must be a contiguous float32 CUDA vector of `heads`")
+            raise ValueError("slopes must be a contiguous float32 vector of `heads` on the "
+                             "documents' device")
         s = gp._Attention()
         s.dtype, s.heads, s.kv_heads, s.dim = _dtype_code(dtype), heads, kv_heads, dim
         s.n_docs, s.q_rows, s.k_rows = docs.n, docs.q_rows, docs.k_rows
@@ -202,7 +226,8 @@ class Attention:
         self.lib = gp.load()
         self.workspace_bytes(False)          # raises if the description is invalid
         self.table_shape = None if buckets is None else (self.heads, buckets.count)
-        self.slots = _Slots(self)
+        self.slots = _Slots((docs.q_rows, self.heads, self.dim),
+                            (docs.k_rows, self.kv_heads, self.dim), dtype, self.device)
 
     def workspace_bytes(self, with_grad: bool) -> int:
         lib = gp.load()
@@ -222,15 +247,16 @@ class AttendBuffers:
     def __init__(self, att: Attention, grad: bool = False):
         torch = _torch()
         d = att.docs
-        f16 = dict(dtype=att.dtype, device="cuda")
+        dev = torch.device("cuda", att.device)
+        f16 = dict(dtype=att.dtype, device=dev)
 
         def rows(full, n, heads):
             make = torch.empty if full else torch.zeros
             return make((n, heads, att.dim), **f16)
 
         self.out = rows(d.q_full, d.q_rows, att.heads)
-        self.lse = torch.full((att.heads, d.q_rows), -math.inf, dtype=torch.float32, device="cuda")
-        self.workspace, self.workspace_bytes = _workspace(att.workspace_bytes(False))
+        self.lse = torch.full((att.heads, d.q_rows), -math.inf, dtype=torch.float32, device=dev)
+        self.workspace, self.workspace_bytes = _workspace(att.workspace_bytes(False), att.device)
         self.dq = self.dk = self.dv = self.dtable = self.rest = self.grad_workspace = None
         if grad:
             if not d.k_disjoint:
@@ -241,25 +267,25 @@ class AttendBuffers:
             self.dv = rows(d.k_full, d.k_rows, att.kv_heads)
             if att.buckets is not None:
                 self.dtable = torch.empty((att.heads, att.buckets.count), **f16)
-            self.grad_workspace = gp._workspace(att.workspace_bytes(True))
-            self.grad_workspace_bytes = self.grad_workspace.numel()
+            self.grad_workspace, self.grad_workspace_bytes = _workspace(
+                max(att.workspace_bytes(True), 1), att.device)
 
 
 class _Slot:
     """One tensor argument of a description's calls: its shape, and the gp_heads struct that
     is filled for each call."""
 
-    __slots__ = ("name", "shape", "dtype", "dim", "struct", "ref")
+    __slots__ = ("name", "shape", "dtype", "device", "struct", "ref")
 
-    def __init__(self, name, rows, heads, att):
-        self.name, self.shape, self.dtype = name, (rows, heads, att.dim), att.dtype
+    def __init__(self, name, shape, dtype, device):
+        self.name, self.shape, self.dtype, self.device = name, shape, dtype, device
         self.struct = gp._Heads()
         self.ref = C.byref(self.struct)
 
     def __call__(self, x):
-        if x.shape != self.shape or x.dtype is not self.dtype or not x.is_cuda:
-            raise ValueError(f"{self.name} must be a {self.dtype} CUDA tensor of shape {self.shape}, "
-                             f"not {x.dtype} {tuple(x.shape)} on {x.device}")
+        if x.shape != self.shape or x.dtype is not self.dtype or x.get_device() != self.device:
+            raise ValueError(f"{self.name} must be a {self.dtype} tensor of shape {self.shape} on "
+                             f"cuda:{self.device}, not {x.dtype} {tuple(x.shape)} on {x.device}")
         s = self.struct
         s.row, s.head, one = x.stride()
         if one != 1:
@@ -272,10 +298,9 @@ class _Slots(threading.local):
     """A description's slots, a set per thread: a call releases the interpreter while the
     library reads them."""
 
-    def __init__(self, att):
-        d = att.docs
-        self.of = {n: _Slot(n, d.q_rows, att.heads, att) for n in ("q", "out", "rest", "dout", "dq")}
-        self.of.update({n: _Slot(n, d.k_rows, att.kv_heads, att) for n in ("k", "v", "dk", "dv")})
+    def __init__(self, q_shape, k_shape, dtype, device):
+        self.of = {n: _Slot(n, q_shape, dtype, device) for n in ("q", "out", "rest", "dout", "dq")}
+        self.of.update({n: _Slot(n, k_shape, dtype, device) for n in ("k", "v", "dk", "dv")})
 
 
 def _table(table, att: Attention, name="table"):
@@ -283,9 +308,10 @@ def _table(table, att: Attention, name="table"):
         raise ValueError(f"a {name} goes with a description that has buckets")
     if table is None:
         return None
-    if table.shape != att.table_shape or table.dtype is not att.dtype or not table.is_cuda or \
-            not table.is_contiguous():
-        raise ValueError(f"{name} must be a contiguous {att.dtype} CUDA tensor {att.table_shape}")
+    if table.shape != att.table_shape or table.dtype is not att.dtype or \
+            table.get_device() != att.device or not table.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous {att.dtype} tensor {att.table_shape} on "
+                         f"cuda:{att.device}")
     return table.data_ptr()
 
 
@@ -300,9 +326,7 @@ def attend_into(att: Attention, q, k, v, bufs: AttendBuffers, table=None):
     if att.docs.moving and not att.docs.q_full:
         bufs.out.zero_()
         bufs.lse.fill_(-math.inf)
-    st = att.lib.gp_attend(*args)
-    if st:
-        _check(st)
+    _call(att.device, att.lib.gp_attend, args)
 
 
 def attend(att: Attention, q, k, v, table=None) -> dict:
@@ -328,38 +352,40 @@ def attend_grad_into(att: Attention, q, k, v, dout, bufs: AttendBuffers, table=N
                         (bufs.dv, att.docs.k_full)):
             if not full:
                 x.zero_()
-    st = att.lib.gp_attend_grad(*args)
-    if st:
-        _check(st)
+    _call(att.device, att.lib.gp_attend_grad, args)
 
 
 # ------------------------------------------------------------------ log probabilities
 class LogprobBuffers:
-    """Outputs and workspace of logprob calls on [rows, width] logits: logp, entropy, lse
+    """Outputs and workspace, on a device (the current one if None), of logprob calls on
+    [rows, width] logits: logp, entropy, lse
     [rows], with top the best alternatives top_logp and top_id [rows, top], and with grad
     dlogits and norm [rows, 2] (maxima and log-sums apart, which the gradient reads)."""
 
-    def __init__(self, rows: int, width: int, dtype, top: int = 0, grad: bool = False):
+    def __init__(self, rows: int, width: int, dtype, top: int = 0, grad: bool = False,
+                 device: Optional[int] = None):
         torch = _torch()
         self.rows, self.width, self.top, self.dtype = int(rows), int(width), int(top), dtype
-        f32 = dict(dtype=torch.float32, device="cuda")
+        self.device = torch.cuda.current_device() if device is None else int(device)
+        dev = torch.device("cuda", self.device)
+        f32 = dict(dtype=torch.float32, device=dev)
         self.logp, self.entropy, self.lse = (torch.empty(self.rows, **f32) for _ in range(3))
         self.top_logp = torch.empty((self.rows, self.top), **f32) if top else None
-        self.top_id = (torch.empty((self.rows, self.top), dtype=torch.int64, device="cuda")
+        self.top_id = (torch.empty((self.rows, self.top), dtype=torch.int64, device=dev)
                        if top else None)
-        self.dlogits = (torch.empty((self.rows, self.width), dtype=dtype, device="cuda")
+        self.dlogits = (torch.empty((self.rows, self.width), dtype=dtype, device=dev)
                         if grad else None)
         self.norm = torch.empty((self.rows, 2), **f32) if grad else None
         self.code = _dtype_code(dtype)
         self.shape = (self.rows, self.width)
         self.lib = gp.load()
         self.workspace, self.workspace_bytes = _workspace(
-            self.lib.gp_logprob_workspace_bytes(self.rows, self.width, self.top))
+            self.lib.gp_logprob_workspace_bytes(self.rows, self.width, self.top), self.device)
 
 
 def _logits(x, bufs, name="logits"):
-    if x.shape != bufs.shape or x.dtype is not bufs.dtype or not x.is_cuda:
-        raise ValueError(f"{name} must be a {bufs.dtype} CUDA tensor {bufs.shape}")
+    if x.shape != bufs.shape or x.dtype is not bufs.dtype or x.get_device() != bufs.device:
+        raise ValueError(f"{name} must be a {bufs.dtype} tensor {bufs.shape} on cuda:{bufs.device}")
     row, one = x.stride()
     if one != 1 and bufs.width > 1:
         raise ValueError(f"{name}'s rows must be contiguous")
@@ -369,8 +395,10 @@ def _logits(x, bufs, name="logits"):
 def _row_vector(x, bufs, dtype, name):
     if x is None:
         return None
-    if x.shape != (bufs.rows,) or x.dtype is not dtype or not x.is_cuda or not x.is_contiguous():
-        raise ValueError(f"{name} must be a contiguous {dtype} CUDA vector of {bufs.rows}")
+    if x.shape != (bufs.rows,) or x.dtype is not dtype or x.get_device() != bufs.device or \
+            not x.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous {dtype} vector of {bufs.rows} on "
+                         f"cuda:{bufs.device}")
     return x.data_ptr()
 
 
@@ -383,19 +411,17 @@ def logprob_into(logits, targets, bufs: LogprobBuffers, scale: float = 1.0):
     if t is None:
         raise ValueError("targets are required")
     ws, top = bufs.workspace, bufs.top
-    st = bufs.lib.gp_logprob_norm(
+    _call(bufs.device, bufs.lib.gp_logprob_norm, (
         bufs.code, x, stride, bufs.rows, bufs.width, scale, t, top, bufs.logp.data_ptr(),
         bufs.entropy.data_ptr(), bufs.lse.data_ptr(),
         None if bufs.norm is None else bufs.norm.data_ptr(),
-        bufs.top_logp.data_ptr() if top else None,
-        bufs.top_id.data_ptr() if top else None, None if ws is None else ws.data_ptr(),
-        bufs.workspace_bytes, _stream(logits))
-    if st:
-        _check(st)
+        bufs.top_logp.data_ptr() if top else None, bufs.top_id.data_ptr() if top else None,
+        None if ws is None else ws.data_ptr(), bufs.workspace_bytes, _stream(logits)))
 
 
 def logprob(logits, targets, top: int = 0, scale: float = 1.0) -> dict:
-    bufs = LogprobBuffers(logits.shape[0], logits.shape[1], logits.dtype, top)
+    bufs = LogprobBuffers(logits.shape[0], logits.shape[1], logits.dtype, top,
+                          device=logits.get_device() if logits.is_cuda else None)
     logprob_into(logits, targets, bufs, scale)
     out = {"logp": bufs.logp, "entropy": bufs.entropy, "lse": bufs.lse}
     if top:
@@ -413,10 +439,8 @@ def logprob_grad_into(logits, targets, g_logp, g_entropy, bufs: LogprobBuffers,
         raise ValueError("the buffers were made without grad")
     x, stride = _logits(logits, bufs)
     dx, dstride = _logits(bufs.dlogits, bufs, "dlogits")
-    st = bufs.lib.gp_logprob_norm_grad(
+    _call(bufs.device, bufs.lib.gp_logprob_norm_grad, (
         bufs.code, x, stride, bufs.rows, bufs.width, scale,
         _row_vector(targets, bufs, torch.int64, "targets"), bufs.norm.data_ptr(),
         bufs.entropy.data_ptr(), _row_vector(g_logp, bufs, torch.float32, "g_logp"),
-        _row_vector(g_entropy, bufs, torch.float32, "g_entropy"), dx, dstride, _stream(logits))
-    if st:
-        _check(st)
+        _row_vector(g_entropy, bufs, torch.float32, "g_entropy"), dx, dstride, _stream(logits)))

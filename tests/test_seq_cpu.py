@@ -12,12 +12,15 @@ BF = torch.bfloat16
 
 
 class Tensor:
-    """What the binding asks of a CUDA tensor."""
-    is_cuda = True
+    """What the binding asks of a CUDA tensor (index -1: of the host's)."""
+    is_cuda = property(lambda self: self.index >= 0)
 
     def __init__(self, shape, dtype=BF, at=1 << 20, device=0):
         self.shape, self.dtype, self.at, self.index = torch.Size(shape), dtype, at, device
-        self.device = torch.device("cuda", device)
+
+    @property
+    def device(self):
+        return torch.device("cuda", self.index) if self.index >= 0 else torch.device("cpu")
 
     def stride(self):
         s = [1]
@@ -60,7 +63,7 @@ def documents(q_rows=8, k_rows=8, docs=1, max_q=None, max_k=None, **kw):
     d.prefix, d.n, d.q_rows, d.k_rows = None, docs, q_rows, k_rows
     d.max_q, d.max_k = max_q or q_rows, max_k or k_rows
     d.q_full = d.k_full = d.k_disjoint = True
-    d.moving = False
+    d.moving, d.device = False, 0
     for k, v in kw.items():
         setattr(d, k, v)
     return d
@@ -94,6 +97,7 @@ def inputs(att, at=1 << 20, **kw):
 @pytest.fixture(autouse=True)
 def _no_stream(monkeypatch):
     monkeypatch.setattr(seq, "_stream", lambda x: None)
+    monkeypatch.setattr(seq, "_current_device", lambda: 0, raising=False)
 
 
 def test_stand_ins_pass():
@@ -217,3 +221,98 @@ def test_threads_share_a_description():
     done.set()
     first.join(20)
     assert found == {"first": [1 << 20] * 3 + [1 << 21], "second": [1 << 28] * 3 + [1 << 29]}
+
+
+# ------------------------------------------------------------------ devices
+def test_tensors_of_another_device_refused():
+    """An address of another device, or of the host, in a launch of the documents' device."""
+    att = attention(buckets=seq.Buckets([0, 3]))
+    att.lib = Library()
+    for device in (1, -1):
+        good, table = inputs(att), Tensor((2, 2))
+        for n in range(3):
+            x = list(good)
+            x[n] = inputs(att, device=device)[n]
+            with pytest.raises(ValueError):
+                seq.attend_into(att, *x, buffers(att), table=table)
+            with pytest.raises(ValueError):
+                seq.attend_grad_into(att, *x, good[0], buffers(att), table=table)
+        away = Tensor((2, 2), device=device)
+        with pytest.raises(ValueError):
+            seq.attend_into(att, *good, buffers(att), table=away)
+        with pytest.raises(ValueError):
+            seq.attend_grad_into(att, *good, inputs(att, device=device)[0], buffers(att), table=table)
+        for k in ("out", "rest"):
+            b = buffers(att)
+            getattr(b, k).index = device
+            with pytest.raises(ValueError):
+                seq.attend_into(att, *good, b, table=table)
+        for k in ("out", "rest", "dq", "dk", "dv", "dtable"):
+            b = buffers(att)
+            getattr(b, k).index = device
+            with pytest.raises(ValueError):
+                seq.attend_grad_into(att, *good, good[0], b, table=table)
+        with pytest.raises(ValueError):
+            attention(slopes=Tensor((2,), torch.float32, device=device))
+    assert not att.lib.calls
+
+
+def logprob_buffers(rows, width, lib, device=0):
+    f = lambda *s, dtype=torch.float32: Tensor(s, dtype, device=device)
+    return types.SimpleNamespace(rows=rows, width=width, top=0, dtype=torch.float32, shape=(rows, width),
+                                 code=2, device=device, lib=lib, logp=f(rows), entropy=f(rows), lse=f(rows),
+                                 norm=f(rows, 2), top_logp=None, top_id=None, dlogits=f(rows, width),
+                                 workspace=None, workspace_bytes=0)
+
+
+def test_rows_of_another_device_refused():
+    lib = Library()
+    b = logprob_buffers(4, 10, lib)
+    x, t, g = Tensor((4, 10), torch.float32), Tensor((4,), torch.int64), Tensor((4,), torch.float32)
+    seq.logprob_into(x, t, b)
+    seq.logprob_grad_into(x, t, g, g, b)
+    assert len(lib.calls) == 2
+    for n in range(4):
+        a = [Tensor((4, 10), torch.float32), Tensor((4,), torch.int64), Tensor((4,), torch.float32),
+             Tensor((4,), torch.float32)]
+        a[n].index = 1
+        if n < 2:
+            with pytest.raises(ValueError):
+                seq.logprob_into(*a[:2], b)
+        with pytest.raises(ValueError):
+            seq.logprob_grad_into(*a, b)
+    assert len(lib.calls) == 2
+
+
+def test_launches_are_the_tensors_devices(monkeypatch):
+    """With another device current, the call makes theirs current."""
+    class Device:
+        now = [0]
+
+        def __init__(self, index):
+            self.index = index
+
+        def __enter__(self):
+            self.now.append(self.index)
+
+        def __exit__(self, *a):
+            self.now.pop()
+
+    monkeypatch.setattr(torch.cuda, "device", Device)
+    monkeypatch.setattr(seq, "_current_device", lambda: Device.now[-1], raising=False)
+    at = []
+    lib = Library(lambda name, args: at.append(Device.now[-1]))
+    for device in (0, 1):
+        att = attention(documents(device=device))
+        att.lib = lib
+        b = buffers(att)
+        for k in ("out", "rest", "dq", "dk", "dv"):
+            getattr(b, k).index = device
+        x = inputs(att, device=device)
+        seq.attend_into(att, *x, b)
+        seq.attend_grad_into(att, *x, x[0], b)
+        r, t = Tensor((4, 10), torch.float32, device=device), Tensor((4,), torch.int64, device=device)
+        lb = logprob_buffers(4, 10, lib, device)
+        seq.logprob_into(r, t, lb)
+        seq.logprob_grad_into(r, t, None, None, lb)
+    assert at == [0] * 4 + [1] * 4 and Device.now == [0]
