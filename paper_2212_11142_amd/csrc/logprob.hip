@@ -459,14 +459,19 @@ __device__ __forceinline__ Sums range_pass(const char *p, int64_t first, int64_t
   for (; row.whole(v + (kUnroll - 1) * kThreads); v += kUnroll * kThreads) batch(v, std::true_type{});
   for (; v < nv; v += kUnroll * kThreads) batch(v, std::false_type{});
   if (KEYS) {
-    *key = 0;
-    if (best_v < nv) {
+    auto key_at = [&](int64_t w) {
       float x[kVec];
-      row.load(best_v, __builtin_nanf(""), x);
+      row.load(w, __builtin_nanf(""), x);
+      uint64_t k = 0;
 #pragma unroll
-      for (int i = 0; i < kVec; ++i)
-        *key = max64(*key, key_of(x[i], first + best_v * kVec + i - row.skip));
-    }
+      for (int i = 0; i < kVec; ++i) k = max64(k, key_of(x[i], first + w * kVec + i - row.skip));
+      return k;
+    };
+    *key = best_v < nv ? key_at(best_v) : 0;
+    // where a vector of NaN came first, and nothing above -inf after it: the first with a number
+    if (__builtin_expect(*key == 0, 0))
+#pragma unroll 1
+      for (int64_t w = best_v + kThreads; w < nv && *key == 0; w += kThreads) *key = key_at(w);
   }
   return s;
 }

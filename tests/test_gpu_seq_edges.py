@@ -353,3 +353,28 @@ def test_grad_of_documents_without_keys(bias):
     for x in (b.out, b.dq, b.dk, b.dv) + ((b.dtable,) if bias else ()):
         assert bool((x == 0).all())
     assert bool(b.lse.isneginf().all())
+
+
+# ------------------------------------------------------------------ alternatives beside NaN
+@pytest.mark.parametrize("rows", [3, 600])
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("width", [9000, 80000])
+def test_ruled_out_entries_among_nan_are_alternatives(rows, dtype, width):
+    """A NaN is no alternative, an entry ruled out is one (the last): where nothing else is
+    left those are found, in the places behind a thread's vectors of NaN too."""
+    import torch
+    from paper_2212_11142_amd import seq
+    x = torch.full((rows, width), math.nan)
+    x[0, 2048:2056] = -math.inf
+    x[1, 5000:5003] = -math.inf
+    x[1, 8991] = 1.0
+    x[2] = -math.inf
+    x = x.to(_torch_dtype(dtype)).cuda()
+    t = torch.zeros(rows, dtype=torch.int64, device="cuda")
+    for top in (6, 40):
+        ids = seq.logprob(x, t, top=top)["top_id"].cpu()
+        none = lambda n: torch.full((n,), -1, dtype=torch.int64)
+        assert torch.equal(ids[0], torch.cat([torch.arange(2048, 2056), none(40)])[:top])
+        assert torch.equal(ids[1], torch.cat([torch.tensor([8991, 5000, 5001, 5002]), none(40)])[:top])
+        assert torch.equal(ids[2], torch.arange(top))
+        assert bool((ids[3:] == -1).all())
