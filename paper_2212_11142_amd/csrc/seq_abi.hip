@@ -105,7 +105,12 @@ gp_status check_workspace(const void *ws, size_t bytes, size_t need) {
   return GP_OK;
 }
 
-gp_status check_grids(const AttnArgs &a, bool grad) {
+// The description, and whether its grids are within a launch's limits. (Before anything else of a
+// call, so that a call with nothing but a description returns the description's own status.)
+gp_status check_description(const gp_attention *t, bool grad) {
+  const gp_status st = check_attention(t);
+  if (st != GP_OK) return st;
+  const AttnArgs a = make_args(t);
   const bool ok = grad ? attend_grad_fits(a)
                        : a.docs == 0 || a.max_q == 0 ||
                              (attend_use_few(a) ? attend_few_fits(a) : attend_fits(a));
@@ -176,11 +181,9 @@ extern "C" {
 size_t gp_attend_workspace_bytes(const gp_attention *t, int32_t with_grad) {
   size_t n = SIZE_MAX;
   guarded([&] {
-    gp_status st = check_attention(t);
+    const gp_status st = check_description(t, with_grad);
     if (st != GP_OK) return st;
     const AttnArgs a = make_args(t);
-    st = check_grids(a, with_grad);
-    if (st != GP_OK) return st;
     n = with_grad ? attend_grad_bytes(a) : attend_bytes(a);
     return GP_OK;
   });
@@ -191,7 +194,7 @@ gp_status gp_attend(const gp_attention *t, const gp_heads *q, const gp_heads *k,
                     const void *table, const gp_heads *out, const gp_heads *rest, float *lse,
                     void *workspace, size_t ws_bytes, void *stream) {
   return guarded([&]() -> gp_status {
-    gp_status st = check_attention(t);
+    gp_status st = check_description(t, false);
     if (st == GP_OK) st = check_heads(q, "q", t->q_rows);
     if (st == GP_OK) st = check_heads(k, "k", t->k_rows);
     if (st == GP_OK) st = check_heads(v, "v", t->k_rows);
@@ -204,8 +207,7 @@ gp_status gp_attend(const gp_attention *t, const gp_heads *q, const gp_heads *k,
     hipStream_t s = static_cast<hipStream_t>(stream);
     AttnArgs a = make_args(t);
     set_tensors(a, q, k, v, out, rest, table, lse);
-    st = check_grids(a, false);
-    if (st == GP_OK) st = check_workspace(workspace, ws_bytes, attend_bytes(a));
+    st = check_workspace(workspace, ws_bytes, attend_bytes(a));
     if (st != GP_OK) return st;
     if (attend_use_few(a))
       return hip_status(launch_attend_few(a, workspace, s), "attention");
@@ -219,7 +221,7 @@ gp_status gp_attend_grad(const gp_attention *t, const gp_heads *q, const gp_head
                          const gp_heads *dk, const gp_heads *dv, void *dtable, void *workspace,
                          size_t ws_bytes, void *stream) {
   return guarded([&]() -> gp_status {
-    gp_status st = check_attention(t);
+    gp_status st = check_description(t, true);
     if (st == GP_OK) st = check_heads(q, "q", t->q_rows);
     if (st == GP_OK) st = check_heads(k, "k", t->k_rows);
     if (st == GP_OK) st = check_heads(v, "v", t->k_rows);
@@ -237,8 +239,7 @@ gp_status gp_attend_grad(const gp_attention *t, const gp_heads *q, const gp_head
     std::memset(&g, 0, sizeof g);
     g.f = make_args(t);
     set_tensors(g.f, q, k, v, out, rest, table, const_cast<float *>(lse));
-    st = check_grids(g.f, true);
-    if (st == GP_OK) st = check_workspace(workspace, ws_bytes, attend_grad_bytes(g.f));
+    st = check_workspace(workspace, ws_bytes, attend_grad_bytes(g.f));
     if (st != GP_OK) return st;
     g.dout = static_cast<const char *>(dout->data);
     g.dq = static_cast<char *>(dq->data);

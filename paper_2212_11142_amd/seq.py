@@ -16,7 +16,7 @@ import threading
 from typing import Optional, Sequence
 
 from . import gp
-from .gp import GPError, _check, _torch
+from .gp import _check, _torch
 
 MAX_REACH = 1024     # the last bucket starts at this distance at most
 _INVALID = (1 << (8 * C.sizeof(C.c_size_t))) - 1
@@ -232,9 +232,10 @@ class Attention:
     def workspace_bytes(self, with_grad: bool) -> int:
         lib = gp.load()
         n = lib.gp_attend_workspace_bytes(self.ref, int(with_grad))
-        if n == _INVALID:
-            msg = lib.gp_last_error().decode()
-            raise GPError(4 if "must be a multiple of 8 in" in msg or "at most" in msg else 1, msg)
+        if n == _INVALID:   # (the size has no room for the status: a call without tensors has it)
+            none = [None]
+            _check(lib.gp_attend_grad(self.ref, *none * 13, 0, None) if with_grad else
+                   lib.gp_attend(self.ref, *none * 8, 0, None))
         return n
 
 

@@ -316,3 +316,27 @@ def test_launches_are_the_tensors_devices(monkeypatch):
         seq.logprob_into(r, t, lb)
         seq.logprob_grad_into(r, t, None, None, lb)
     assert at == [0] * 4 + [1] * 4 and Device.now == [0]
+
+
+# ------------------------------------------------------------------ statuses
+@pytest.mark.parametrize("kw,status", [
+    (dict(heads=3, kv_heads=2), 1), (dict(dim=60), 4), (dict(dim=136), 4), (dict(dtype=torch.float32), 4),
+    (dict(heads=1 << 17), 4), (dict(scale=0.0), 1), (dict(cap=-1.0), 1),
+    (dict(buckets=seq.Buckets([1, 2])), 1), (dict(buckets=seq.Buckets([0, 2000])), 4),
+    (dict(buckets=seq.Buckets(list(range(65)))), 4),
+    (dict(docs=documents(q_rows=(1 << 30) + 1)), 1), (dict(docs=documents(k_rows=(1 << 30) + 1)), 1),
+    (dict(docs=documents(q_rows=1 << 30), heads=4), 4)])
+def test_descriptions_raise_the_librarys_status(kw, status):
+    a = dict(heads=2, kv_heads=1, dim=64)
+    a.update(kw)
+    with pytest.raises(gp.GPError) as e:
+        attention(**a)
+    assert e.value.status == status, str(e.value)
+
+
+def test_gradient_workspaces_raise_the_librarys_status():
+    rows = 1 << 27
+    att = attention(documents(q_rows=rows, k_rows=rows), heads=8, kv_heads=8)
+    with pytest.raises(gp.GPError) as e:
+        att.workspace_bytes(True)
+    assert e.value.status == 4, str(e.value)
