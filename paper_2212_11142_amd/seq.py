@@ -172,7 +172,8 @@ def log_buckets(per_side: int, max_distance: int, two_sided: bool = False) -> Bu
     """per_side classes a side: the first half one distance each, then steps of equal ratio
     up to max_distance; the last class takes all that is farther. The t-th class past the
     exact ones starts at the smallest a with (a / exact)^n >= (max_distance / exact)^t
-    (n of them), compared in integers."""
+    (n of them), compared in integers, or where that is no farther than the class before, at
+    the next distance (classes denser than distances end past max_distance)."""
     exact = max(per_side // 2, 1)
     n = per_side - exact
     if per_side < 1 or (n > 0 and max_distance <= exact):

@@ -340,3 +340,35 @@ def test_gradient_workspaces_raise_the_librarys_status():
     with pytest.raises(gp.GPError) as e:
         att.workspace_bytes(True)
     assert e.value.status == 4, str(e.value)
+
+
+# ------------------------------------------------------------------ buckets
+def test_log_buckets_known():
+    b = seq.log_buckets(16, 128)
+    assert b.start == [0, 1, 2, 3, 4, 5, 6, 7, 8, 12, 16, 23, 32, 46, 64, 91] and b.count == 16
+    assert seq.log_buckets(16, 128, two_sided=True).count == 32
+    assert seq.log_buckets(1, 5).start == [0] and seq.log_buckets(2, 2).start == [0, 1]
+    assert seq.log_buckets(8, 5).start == [0, 1, 2, 3, 4, 5, 6, 7]      # denser than the distances
+    for a in ((0, 5), (2, 1), (16, 8), (-3, 4)):
+        with pytest.raises(ValueError):
+            seq.log_buckets(*a)
+
+
+@pytest.mark.parametrize("per_side,reach", [(16, 128), (32, 128), (7, 50), (64, 1024), (10, 1000), (3, 9)])
+def test_log_buckets_are_logarithmic(per_side, reach):
+    """Distance d past the exact ones is in the class exact + floor(n log(d / exact) /
+    log(reach / exact)), the last one at most: by 60-digit logarithms, beyond doubt where those
+    are not within 1e-40 of a class's edge."""
+    from decimal import Decimal, getcontext
+    getcontext().prec = 60
+    start = seq.log_buckets(per_side, reach).start
+    exact = per_side // 2
+    n = per_side - exact
+    unit = (Decimal(reach) / exact).ln()
+    for d in range(2 * reach):
+        got = max(c for c in range(per_side) if start[c] <= d)
+        if d < exact:
+            assert got == d
+            continue
+        x = n * (Decimal(d) / exact).ln() / unit + Decimal(10) ** -40
+        assert got == min(exact + int(x), per_side - 1), d
