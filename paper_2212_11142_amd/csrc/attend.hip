@@ -241,11 +241,9 @@ __global__ __launch_bounds__(kThreads * PARTS, 2) void attend_kernel(const AttnA
   }
   const bool ok = row < lq;
   const float inv = l > 0.f ? 1.f / l : (l == 0.f ? 0.f : l);   // a NaN sum stays one
-  store_row<T, DT>(a.o + (int64_t)(t.b0 + row) * a.o_row + head * a.o_head, ok, a.bytes, acc, inv,
-                   lane);
-  if (REST)
-    store_row<T, DT, true>(a.rest + (int64_t)(t.b0 + row) * a.rest_row + head * a.rest_head, ok,
-                           a.bytes, acc, inv, lane);
+  store_row<T, DT, REST>(
+      a.o + (int64_t)(t.b0 + row) * a.o_row + head * a.o_head, ok, a.bytes, acc, inv, lane,
+      REST ? a.rest + (int64_t)(t.b0 + row) * a.rest_row + head * a.rest_head : nullptr);
   if (ok && h == 0)
     a.lse[(int64_t)head * a.q_rows + t.b0 + row] =
         l == 0.f ? -__builtin_inff() : (m - p_shift + __builtin_amdgcn_logf(l)) * kLn2;

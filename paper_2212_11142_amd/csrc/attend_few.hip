@@ -87,7 +87,7 @@ __device__ inline void write_quad(const AttnArgs &a, int row, int head, int d, f
   const float inv = l > 0.f ? 1.f / l : (l == 0.f ? 0.f : l);   // a NaN sum stays one
   x *= inv;
   if (2 * d < a.bytes) {
-    const u32x2 w = {T::pack(x[0], x[1]), T::pack(x[2], x[3])};
+    const u32x2 w = {as_stored(T::pack(x[0], x[1])), as_stored(T::pack(x[2], x[3]))};
     *reinterpret_cast<u32x2 *>(a.o + (int64_t)row * a.o_row + head * a.o_head + 2 * d) = w;
     if (REST)
       *reinterpret_cast<u32x2 *>(a.rest + (int64_t)row * a.rest_row + head * a.rest_head + 2 * d) =

@@ -295,33 +295,45 @@ __device__ inline void load_operand(const char *base, int64_t stride, int row, i
   }
 }
 
+// The two packed values as they are stored: what is computed from them then is computed from the
+// numbers in memory. (The compiler may round a value once more for another use, from the product
+// that it comes from instead of from that product's fp32 rounding: one step off at ties.)
+__device__ inline uint32_t as_stored(uint32_t w) {
+  asm("" : "+v"(w));
+  return w;
+}
+
 // Writes a transposed result (D^T: element d = 32 c + 8 g + 4 (lane / 32) + r of the row at
-// p, both lane halves of a row) as 16-byte pieces, times f; with REST what the rounding to T
-// took from each value, instead.
+// p, both lane halves of a row) as 16-byte pieces, times f; with REST also what the rounding to T
+// took from each value, at `rest`.
 template <class T, int DT, bool REST = false>
-__device__ inline void store_row(char *p, bool ok, int bytes, const f32x16 *acc, float f, int lane) {
+__device__ inline void store_row(char *p, bool ok, int bytes, const f32x16 *acc, float f, int lane,
+                                 char *rest = nullptr) {
   const int h = lane >> 5;
 #pragma unroll
   for (int c = 0; c < DT; ++c)
 #pragma unroll
     for (int g = 0; g < 4; g += 2) {
-      uint32_t w[4];
+      uint32_t w[4], e[4];
 #pragma unroll
-      for (int i = 0; i < 2; ++i) {
-#pragma unroll
-        for (int k = 0; k < 2; ++k) {
-          const int e = 4 * (g + i) + 2 * k;
-          const float x = acc[c][e] * f, y = acc[c][e + 1] * f;
-          const uint32_t r = T::pack(x, y);
-          w[2 * i + k] = REST ? T::pack(x - T::lo(r), y - T::hi(r)) : r;
+      for (int i = 0; i < 4; ++i) {
+        const int k = 4 * (g + i / 2) + 2 * (i % 2);
+        const float x = acc[c][k] * f, y = acc[c][k + 1] * f;
+        w[i] = T::pack(x, y);
+        if (REST) {
+          w[i] = as_stored(w[i]);
+          e[i] = T::pack(x - T::lo(w[i]), y - T::hi(w[i]));
         }
       }
       // lower half: all of piece g, upper half: all of piece g + 1
-      const u32x2 x = __builtin_amdgcn_permlane32_swap(w[0], w[2], false, false);
-      const u32x2 y = __builtin_amdgcn_permlane32_swap(w[1], w[3], false, false);
-      const u32x4 v = {x[0], y[0], x[1], y[1]};
-      const int off = (32 * c + 8 * (g + h)) * 2;
-      if (ok && off < bytes) *reinterpret_cast<u32x4 *>(p + off) = v;
+      auto store = [&](char *to, const uint32_t *v) {
+        const u32x2 x = __builtin_amdgcn_permlane32_swap(v[0], v[2], false, false);
+        const u32x2 y = __builtin_amdgcn_permlane32_swap(v[1], v[3], false, false);
+        const int off = (32 * c + 8 * (g + h)) * 2;
+        if (ok && off < bytes) *reinterpret_cast<u32x4 *>(to + off) = u32x4{x[0], y[0], x[1], y[1]};
+      };
+      store(p, w);
+      if (REST) store(rest, e);
     }
 }
 

@@ -378,3 +378,18 @@ def test_ruled_out_entries_among_nan_are_alternatives(rows, dtype, width):
         assert torch.equal(ids[1], torch.cat([torch.tensor([8991, 5000, 5001, 5002]), none(40)])[:top])
         assert torch.equal(ids[2], torch.arange(top))
         assert bool((ids[3:] == -1).all())
+
+
+# ------------------------------------------------------------------ what rounding took
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("heads,kv,dim", [(96, 4, 64), (40, 4, 128), (12, 4, 64)])   # one and two groups, few rows
+def test_out_and_rest_are_out_before_rounding(dtype, heads, kv, dim):
+    """rest is the rest of the out that was stored, where it lies halfway between two numbers
+    too: their sum has the probabilities' error (two terms of u each) and rest's own rounding."""
+    import torch  # noqa: F401
+    c = Case(dtype, [(200, 300), (130, 130)], heads, kv, dim, grad=True, seed=heads)
+    b, ref = c.run(), c.oracle()
+    got = b.out.double() + b.rest.double()
+    u, e = c.u, 2.0 ** -19 * (1 + ref["score"])
+    grid = 2.0 ** -25 if dtype == "fp16" else 0.0
+    near(got, ref["out"], u * u * np.abs(ref["out"]) + (u * u + e) * ref["out_abs"] + grid, "out + rest")
