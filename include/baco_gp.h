@@ -491,7 +491,9 @@ void gp_forest_free(gp_forest *forest);
  * key head are the sums over its query heads. Products take the 16-bit inputs exactly and
  * add in fp32; probabilities and score gradients are rounded to the inputs' type where they
  * enter the second products (fp16: at a power-of-two factor; a probability is then off by 2^-32
- * of the row's largest, 2^-39 in documents of more than 4096 keys, beside its rounding); score
+ * of the row's largest, 2^-39 in documents of more than 4096 keys, beside its rounding). Where
+ * gradients follow, the forward probabilities have two such terms, and so have the score
+ * gradients of documents of up to 128 rows and keys. Score
  * arithmetic, sums, lse and the table's gradient are fp32 until the results are rounded. */
 typedef enum { GP_BF16 = 0, GP_FP16 = 1, GP_FP32 = 2 } gp_dtype;
 

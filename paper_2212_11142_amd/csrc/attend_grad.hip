@@ -207,6 +207,25 @@ struct GradScale {
   }
 };
 
+// dS is rounded to T as an operand. Over few rows those roundings do not average out, and with two
+// keys, whose dS are each other's opposites, dQ and dK would be off by up to 2.3 times what rounding
+// the results costs (1.4 to 1.5 times over many): in short documents a second term holds what the
+// first one's rounding took. Without / with: 24 documents of 120 rows, 8 heads of 64, 36.2 / 37.0
+// us; 200 of 100, 16 heads of 128 with 4 of keys, 385 / 391; one of 8192, which has one term but
+// the instructions beside it, 1328 / 1342.
+constexpr int kTwoTerms = 128;
+__device__ inline bool short_document(int lq, int lk) { return max(lq, lk) <= kTwoTerms; }
+template <class T>
+__device__ inline u32x4 rest_of(const f32x16 &x, int k, u32x4 rounded) {
+  u32x4 r;
+#pragma unroll
+  for (int w = 0; w < 4; ++w) {
+    const uint32_t s = as_stored(rounded[w]);
+    r[w] = T::pack(x[8 * k + 2 * w] - T::lo(s), x[8 * k + 2 * w + 1] - T::hi(s));
+  }
+  return r;
+}
+
 // ------------------------------------------------------------------ dK, dV
 // A lane's key is fixed, its elements are the queries 8 g + 4 h + r of 32: products are
 // Q K^T (queries x keys), their results the operands of dV^T = dO^T P and dK^T = Q^T dZ.
@@ -250,6 +269,7 @@ __device__ __forceinline__ void grad_kv(const AttnGradArgs &ga, int id, char *ld
   const int lq = max(min(a.qe[t.doc], a.q_rows) - q0, 0);
   const int prefix = (a.causal && a.prefix) ? a.prefix[t.doc] : 0;
   const int shift = lk - lq;
+  const bool two_terms = short_document(lq, lk);
   const int j0 = t.tile * kBK;
 
   const int key_lo = NARROW ? j0 : j0 + 32 * wave, key = key_lo + (lane & 31);
@@ -416,6 +436,15 @@ __device__ __forceinline__ void grad_kv(const AttnGradArgs &ga, int id, char *ld
           dv[c] = T::mfma(col_operand<DP>(qc0 + kTile, sub + 16 * k, c), pr[k], dv[c]);
           dk[c] = T::mfma(col_operand<DP>(qc0, sub + 16 * k, c), dr[k], dk[c]);
         }
+      if (__builtin_expect(two_terms, 0)) {
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+          const u32x4 rest = rest_of<T>(dp, k, dr[k]);
+#pragma unroll
+          for (int c = 0; c < DT; ++c)
+            dk[c] = T::mfma(col_operand<DP>(qc0, sub + 16 * k, c), rest, dk[c]);
+        }
+      }
     }
     if (!NARROW) copies_barrier();
   }
@@ -526,6 +555,7 @@ __device__ __forceinline__ void grad_q(const AttnGradArgs &ga, int id, char *lds
 
   const int row_lo = NARROW ? i0 : i0 + 32 * wave, row = row_lo + (lane & 31);
   const int shift = lk - lq;
+  const bool two_terms = short_document(lq, lk);
   auto limit = [&](int i) { return a.causal ? min(lk, max(i + shift + 1, prefix)) : lk; };
   const bool ok = row < lq;
   const int lim = ok ? limit(row) : 0;
@@ -666,6 +696,14 @@ __device__ __forceinline__ void grad_q(const AttnGradArgs &ga, int id, char *lds
 #pragma unroll
         for (int c = 0; c < DT; ++c)
           acc[c] = T::mfma(col_operand<DP>(kcol, 16 * k, c), dr[k], acc[c]);
+      if (__builtin_expect(two_terms, 0)) {
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+          const u32x4 rest = rest_of<T>(dp, k, dr[k]);
+#pragma unroll
+          for (int c = 0; c < DT; ++c) acc[c] = T::mfma(col_operand<DP>(kcol, 16 * k, c), rest, acc[c]);
+        }
+      }
     }
     if (!NARROW) copies_barrier();
   }

@@ -393,3 +393,21 @@ def test_out_and_rest_are_out_before_rounding(dtype, heads, kv, dim):
     u, e = c.u, 2.0 ** -19 * (1 + ref["score"])
     grid = 2.0 ** -25 if dtype == "fp16" else 0.0
     near(got, ref["out"], u * u * np.abs(ref["out"]) + (u * u + e) * ref["out_abs"] + grid, "out + rest")
+
+
+# ------------------------------------------------------------------ short documents
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("heads,kv,dim", [(4, 2, 72), (48, 12, 64), (64, 64, 128)])    # narrow and wide blocks
+@pytest.mark.parametrize("cap,bias", [(0.0, "none"), (30.0, "two"), (0.0, "slope")])
+def test_grad_of_short_documents(dtype, heads, kv, dim, cap, bias):
+    """Documents of up to 128 rows: dS enters its products in two terms, of u^2 each, so that dq
+    and dk have no more than the results' own rounding, and the sums' errors."""
+    lens = [(2, 2), (3, 2), (2, 128), (17, 17), (128, 128), (100, 5)]
+    c = Case(dtype, lens, heads, kv, dim, causal=True, cap=cap, bias=bias, grad=True)
+    b, ref = c.run(), c.oracle()
+    u, e = c.u, 2.0 ** -19 * (1 + ref["score"])
+    grid = 2.0 ** -25 if dtype == "fp16" else 0.0
+    for n in ("dq", "dk"):
+        near(getattr(b, n), ref[n], u * np.abs(ref[n]) + (u * u + e) * (ref[n + "_abs"] + ref[n + "_dif"])
+             + grid, n)
+    c.check(b, ref)
