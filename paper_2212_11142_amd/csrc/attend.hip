@@ -10,11 +10,13 @@
 //
 // Bound by the matrix units and by the scores' own instructions (an exponential, two fused
 // multiply-adds, the maximum, the sum and half a conversion each) in turn. Measured: 16,384 rows,
-// causal, 16 heads of 128, fp16, 1242 us, 0.89 PFLOP/s (a library product of 8192^3 has 1.11; the
+// causal, 16 heads of 128, fp16, 1201 us, 0.92 PFLOP/s (a library product of 8192^3 has 1.11; the
 // matrix units are busy for half of the cycles, the vector units for 65%); 1,048,576 rows over
-// 512 keys, 8 heads of 64, bf16, 1469 us, 0.75 PFLOP/s (vector units 80%: at this head size half
-// the products per score); 13 documents of up to 1021 rows, cap and table, 57 us. More queries per
-// wavefront or keys per tile would not fit the registers.
+// 512 keys, 8 heads of 64, bf16, 1456 us, 0.76 PFLOP/s (vector units 79%: at this head size half
+// the products per score); 13 documents of up to 1021 rows, 16 heads of 128, cap and table, 57 us,
+// where two blocks per compute unit leave both idle (vector units 50%, matrix units 22%; wavefronts
+// wait for 42% of their cycles). More queries per wavefront or keys per tile would not fit the
+// registers.
 #include <type_traits>
 
 #include "seq_dev.h"

@@ -9,10 +9,10 @@
 // block costs more than the launch it saves: what blocks hand over must pass the L2 of each
 // XCD, 15.4 against 7.6 + 4.4 us for 4095 keys and 4 key heads of 128.)
 //
-// Measured, 16 heads of 128 with 4 of keys: 64 caches of up to 32,768 keys, 2.2 GB, 427 us, 5.2
+// Measured, 16 heads of 128 with 4 of keys: 64 caches of up to 32,768 keys, 2.2 GB, 421 us, 5.3
 // TB/s (reading alone reaches 6.3), 7 of them the join; 64 full ones, 4.3 GB, 767 us, 5.6 TB/s;
-// one of 4095 keys, 8.4 MB, 7.6 us and 4.0 for the join, bound by the latency of a wavefront's two
-// steps and of the second launch.
+// one of 4095 keys, 8.4 MB, 7.7 us and 3.9 for the join, bound by the latency of a wavefront's one
+// step (a block has 128 keys) and of the second launch.
 #include "seq_dev.h"
 
 namespace bgp {

@@ -8,10 +8,13 @@
 // goes over the keys for 128 queries of a head and keeps dQ and the head's table gradient.
 // That costs 7 products of the pairs where one kind with atomic sums of dQ would take 5.
 //
-// Bound as the forward kernel is: 8192 rows, causal, 16 heads of 128, slopes: grad_pairs 930-990
-// us for 0.96 TFLOP of its 7 products, 1.0 PFLOP/s (matrix units busy for half of the cycles);
-// 8862 rows in 16 documents, 16 heads of 64 with 4 of keys, prefix masks, cap and table: 163 us,
-// bound by the scores' instructions (cap and bias double them) and by the last blocks' tail.
+// Large calls are bound as the forward kernel is: 8192 rows, causal, 16 heads of 128, slopes:
+// grad_pairs 950-1030 us for 0.96 TFLOP of its 7 products, 0.93 to 1.0 PFLOP/s (matrix units busy
+// for half of the cycles). 8862 rows in 16 documents, 16 heads of 64 with 4 of keys, prefix masks,
+// cap and table: 162 us, where neither unit is the bound (vector 53% of the cycles, matrix 16%):
+// two wavefronts per SIMD go through a chain of product, scores and product, 32 queries or keys at
+// a time. 3 documents of up to 333, 6 heads of 80 with 2 of keys: 35 us, narrow blocks of about
+// eight such steps, each head's biases built anew (wavefronts wait for 54% of their cycles).
 //
 // fp16: P is kept times 2^12 and dS times a power of two from a bound of |dS| in the document and
 // head, 2 max|dO_i| max|v_j|, so that neither leaves fp16's normal range; exact to undo.

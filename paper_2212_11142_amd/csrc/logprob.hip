@@ -245,8 +245,8 @@ __device__ inline void write_row(const LogprobArgs &a, int64_t row, const Sums &
 // ------------------------------------------------------------------ short rows
 // One wavefront per row, the row in registers (VL vectors a lane). The alternatives one by
 // one: the maximum of the lanes' maxima, the first vector and lane that hold it (so the lowest
-// index), which strike the entry out. Bound by reading: 65,536 rows of 512, fp32, 134 MB, 21.8 us,
-// 6.2 TB/s; alternatives cost 1.7 us each at 16,384 rows of 500, 1.8 of 2048.
+// index), which strike the entry out. Bound by reading: 65,536 rows of 512, fp32, 134 MB, 22.1 us,
+// 6.1 TB/s; alternatives cost 1.7 us each at 16,384 rows of 500, 1.8 of 2048.
 template <int DT, int VL>
 __global__ __launch_bounds__(kThreads) void logprob_wave(const LogprobArgs a) {
   constexpr int kVec = Elem<DT>::kVec;
@@ -411,7 +411,7 @@ __device__ inline void by_passes(TopShared &sh, const char *p, int64_t n, int k,
 
 // ------------------------------------------------------------------ long rows
 // A block per row. Bound by reading and by the sums' instructions (an exponential, three others and
-// the maximum per entry), 72% of the cycles: 8191 rows of 32,001, bf16, 524 MB, 122 us, 4.3 TB/s;
+// the maximum per entry), 70 to 79% of the cycles: 8191 rows of 32,001, bf16, 524 MB, 122 us, 4.3 TB/s;
 // 2048 rows of 49,999, fp16, with 5 alternatives, 205 MB, 51 us, 4.0 TB/s.
 // A thread's share of a block's range [0, n) at p (index `first` of the row on): its sums, and
 // with KEYS the key of its largest entry.
@@ -707,8 +707,8 @@ __global__ __launch_bounds__(kThreads) void logprob_join(const LogprobArgs a, Sp
 // ------------------------------------------------------------------ gradient
 // dx_v = c [ g (1[v = t] - p_v) - h p_v (log p_v + H) ]: one pass, each block a range of a
 // row (or, for short rows, each wavefront a row). Bound by reading x and writing dx: 65,536 rows of
-// 512, fp32, 268 MB, 41.2 us, 6.5 TB/s (part of x still in the caches); 8191 rows of 32,001, bf16,
-// 1.05 GB, 200 us, 5.2 TB/s (a copy reaches 5.15).
+// 512, fp32, 268 MB, 42.0 us, 6.4 TB/s (part of x still in the caches); 8191 rows of 32,001, bf16,
+// 1.05 GB, 201 us, 5.2 TB/s (a copy reaches 5.15).
 template <int DT>
 __device__ inline void store_vec(char *p, const float *y) {
   if (DT == kFp32) {
