@@ -500,7 +500,8 @@ void gp_forest_free(gp_forest *forest);
 typedef enum { GP_BF16 = 0, GP_FP16 = 1, GP_FP32 = 2 } gp_dtype;
 
 /* Rows x heads x dim values in device memory: element (r, h, c) at data + r row + h head
- * + c (strides in elements, multiples of 8; data 16-byte aligned; row <= 2^23). */
+ * + c (strides in elements, multiples of 8; data 16-byte aligned; row <= 2^23). Rows and heads of
+ * what is written must not overlap. */
 typedef struct {
   void *data;
   int64_t row;

@@ -57,6 +57,19 @@ gp_status check_heads(const gp_heads *x, const char *name, int32_t rows) {
   return GP_OK;
 }
 
+// A tensor that is written: no two of its rows and heads may share memory.
+gp_status check_output(const gp_heads *x, const char *name, int32_t rows, int32_t heads, int32_t dim) {
+  const gp_status st = check_heads(x, name, rows);
+  if (st != GP_OK) return st;
+  bool apart = (rows < 2 || x->row >= dim) && (heads < 2 || x->head >= dim);
+  // head b is apart from head 0 if no row of it is within dim of one: the nearest two multiples
+  for (int64_t b = 1; apart && rows > 1 && b < heads; ++b) {
+    const int64_t at = b * x->head, r = at / x->row;
+    apart = (r >= rows || at - r * x->row >= dim) && (r + 1 >= rows || (r + 1) * x->row - at >= dim);
+  }
+  return apart ? GP_OK : bad(std::string(name) + "'s rows or heads overlap");
+}
+
 AttnArgs make_args(const gp_attention *t) {
   AttnArgs a;
   std::memset(&a, 0, sizeof a);
@@ -198,8 +211,8 @@ gp_status gp_attend(const gp_attention *t, const gp_heads *q, const gp_heads *k,
     if (st == GP_OK) st = check_heads(q, "q", t->q_rows);
     if (st == GP_OK) st = check_heads(k, "k", t->k_rows);
     if (st == GP_OK) st = check_heads(v, "v", t->k_rows);
-    if (st == GP_OK) st = check_heads(out, "out", t->q_rows);
-    if (st == GP_OK && rest) st = check_heads(rest, "rest", t->q_rows);
+    if (st == GP_OK) st = check_output(out, "out", t->q_rows, t->heads, t->dim);
+    if (st == GP_OK && rest) st = check_output(rest, "rest", t->q_rows, t->heads, t->dim);
     if (st != GP_OK) return st;
     if ((t->per_side > 0) != (table != nullptr)) return bad("a table goes with per_side > 0");
     if (!lse && t->q_rows > 0) return bad("lse is NULL");
@@ -228,9 +241,9 @@ gp_status gp_attend_grad(const gp_attention *t, const gp_heads *q, const gp_head
     if (st == GP_OK) st = check_heads(out, "out", t->q_rows);
     if (st == GP_OK) st = check_heads(rest, "rest", t->q_rows);
     if (st == GP_OK) st = check_heads(dout, "dout", t->q_rows);
-    if (st == GP_OK) st = check_heads(dq, "dq", t->q_rows);
-    if (st == GP_OK) st = check_heads(dk, "dk", t->k_rows);
-    if (st == GP_OK) st = check_heads(dv, "dv", t->k_rows);
+    if (st == GP_OK) st = check_output(dq, "dq", t->q_rows, t->heads, t->dim);
+    if (st == GP_OK) st = check_output(dk, "dk", t->k_rows, t->kv_heads, t->dim);
+    if (st == GP_OK) st = check_output(dv, "dv", t->k_rows, t->kv_heads, t->dim);
     if (st != GP_OK) return st;
     if ((t->per_side > 0) != (table != nullptr)) return bad("a table goes with per_side > 0");
     if ((table != nullptr) != (dtable != nullptr)) return bad("dtable goes with a table");

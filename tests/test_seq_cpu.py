@@ -372,3 +372,40 @@ def test_log_buckets_are_logarithmic(per_side, reach):
             continue
         x = n * (Decimal(d) / exact).ln() / unit + Decimal(10) ** -40
         assert got == min(exact + int(x), per_side - 1), d
+
+
+# ------------------------------------------------------------------ overlapping outputs
+def _attend_status(out, grad=None, rows=8, heads=4, ws=None, nbytes=0, **kw):
+    """Status of gp_attend (or of gp_attend_grad with `grad` in the named place) whose tensors are
+    otherwise in order; 5 (no workspace) means that they all passed."""
+    lib, dim = gp.load(), 64
+    base = dict(q_rows=rows, max_q=rows, k_rows=1 << 20, max_k=1 << 20, heads=heads, kv_heads=2)
+    base.update(kw)
+    s = description(**base)
+    ok, key = gp._Heads(256, heads * dim, dim), gp._Heads(256, 2 * dim, dim)
+    p = lambda x: C.byref(x)
+    if grad is None:
+        return lib.gp_attend(p(s), p(ok), p(key), p(key), None, p(out), None, 256, ws, nbytes, None)
+    t = dict(dq=ok, dk=key, dv=key)
+    t[grad] = out
+    return lib.gp_attend_grad(p(s), p(ok), p(key), p(key), None, p(ok), p(ok), 256, p(ok), p(t["dq"]),
+                              p(t["dk"]), p(t["dv"]), None, None, 0, None)
+
+
+def test_overlapping_outputs_refused():
+    """Rows or heads of an output that share memory would be written by several blocks."""
+    heads = lambda row, head: gp._Heads(256, row, head)
+    good = [heads(256, 64), heads(64, 512), heads(64, 4096), heads(512, 128), heads(256, 64),
+            heads(192, 1536 + 64), heads(128, 1024), heads(128, 64 * 17)]
+    for x in good:                               # (heads interleaved with rows among them)
+        assert _attend_status(x) == 5, (x.row, x.head)
+    for x in (heads(0, 64), heads(256, 0), heads(256, 56), heads(56, 512), heads(64, 64), heads(128, 64),
+              heads(192, 64), heads(64, 448), heads(128, 64 * 3 + 8)):
+        assert _attend_status(x) == 1, (x.row, x.head)
+        assert _attend_status(x, "dq") == 1
+    for n in ("dk", "dv"):
+        assert _attend_status(heads(128, 64), n) == 5
+        assert _attend_status(heads(64, 64), n) == 1 and _attend_status(heads(0, 64), n) == 1
+    # one row, or one head: its stride is not used
+    assert _attend_status(heads(0, 64), rows=1) == 5
+    assert _attend_status(heads(64, 0), rows=8, heads=1, kv_heads=1) == 5
