@@ -189,11 +189,11 @@ def log_buckets(per_side: int, max_distance: int, two_sided: bool = False) -> Bu
 
 # ------------------------------------------------------------------ attention
 class Attention:
-    """What is attended to and how, on the documents' device: documents, heads (a multiple of kv_heads), head size,
-    dtype (torch.bfloat16 or torch.float16), causal or full mask (a prefix is the
-    documents'), scale (1 / sqrt(dim) if None), cap of the scores by a tanh (0: none), and a
-    bias by distance: slopes (float32 CUDA [heads], -slope |distance|) or Buckets (the table
-    [heads, buckets.count] of dtype goes with each call)."""
+    """What is attended to and how, on the documents' device: documents, heads (a multiple of
+    kv_heads), head size, dtype (torch.bfloat16 or torch.float16), causal or full mask (a
+    prefix is the documents'), scale (1 / sqrt(dim) if None), cap of the scores by a tanh (0:
+    none), and a bias by distance: slopes (float32 CUDA [heads], -slope |distance|) or Buckets
+    (the table [heads, buckets.count] of dtype goes with each call)."""
 
     def __init__(self, docs: Documents, heads: int, kv_heads: int, dim: int, dtype,
                  causal: bool = True, scale: Optional[float] = None, cap: float = 0.0,
@@ -244,7 +244,7 @@ class AttendBuffers:
     """Outputs and workspaces of attention calls with a description: out, lse
     [heads, q_rows], and with grad dq, dk, dv and (with buckets) dtable, and rest (what
     rounding took from out, which the gradient reads). Rows outside every document are 0
-    (lse -inf)."""
+    (lse -inf); a call clears them where its documents may have others than the last call's."""
 
     def __init__(self, att: Attention, grad: bool = False):
         torch = _torch()
@@ -260,6 +260,7 @@ class AttendBuffers:
         self.lse = torch.full((att.heads, d.q_rows), -math.inf, dtype=torch.float32, device=dev)
         self.workspace, self.workspace_bytes = _workspace(att.workspace_bytes(False), att.device)
         self.dq = self.dk = self.dv = self.dtable = self.rest = self.grad_workspace = None
+        self.docs = self.grad_docs = d       # whose rows out and lse, and the gradients, hold
         if grad:
             if not d.k_disjoint:
                 raise ValueError("gradients need documents whose key rows do not overlap")
@@ -325,9 +326,12 @@ def attend_into(att: Attention, q, k, v, bufs: AttendBuffers, table=None):
     args = (att.ref, t["q"](q), t["k"](k), t["v"](v), _table(table, att), t["out"](bufs.out),
             None if rest is None else t["rest"](rest), bufs.lse.data_ptr(),
             None if ws is None else ws.data_ptr(), bufs.workspace_bytes, _stream(q))
-    if att.docs.moving and not att.docs.q_full:
-        bufs.out.zero_()
-        bufs.lse.fill_(-math.inf)
+    d = att.docs
+    if d.moving or bufs.docs is not d:
+        if not d.q_full:
+            bufs.out.zero_()
+            bufs.lse.fill_(-math.inf)
+        bufs.docs = d
     _call(att.device, att.lib.gp_attend, args)
 
 
@@ -349,20 +353,21 @@ def attend_grad_into(att: Attention, q, k, v, dout, bufs: AttendBuffers, table=N
             t["rest"](bufs.rest), bufs.lse.data_ptr(), t["dout"](dout), t["dq"](bufs.dq),
             t["dk"](bufs.dk), t["dv"](bufs.dv), _table(bufs.dtable, att, "dtable"),
             bufs.grad_workspace.data_ptr(), bufs.grad_workspace_bytes, _stream(q))
-    if att.docs.moving:
-        for x, full in ((bufs.dq, att.docs.q_full), (bufs.dk, att.docs.k_full),
-                        (bufs.dv, att.docs.k_full)):
+    d = att.docs
+    if d.moving or bufs.grad_docs is not d:
+        for x, full in ((bufs.dq, d.q_full), (bufs.dk, d.k_full), (bufs.dv, d.k_full)):
             if not full:
                 x.zero_()
+        bufs.grad_docs = d
     _call(att.device, att.lib.gp_attend_grad, args)
 
 
 # ------------------------------------------------------------------ log probabilities
 class LogprobBuffers:
     """Outputs and workspace, on a device (the current one if None), of logprob calls on
-    [rows, width] logits: logp, entropy, lse
-    [rows], with top the best alternatives top_logp and top_id [rows, top], and with grad
-    dlogits and norm [rows, 2] (maxima and log-sums apart, which the gradient reads)."""
+    [rows, width] logits: logp, entropy, lse [rows], with top the best alternatives top_logp
+    and top_id [rows, top], and with grad dlogits and norm [rows, 2] (maxima and log-sums
+    apart, which the gradient reads)."""
 
     def __init__(self, rows: int, width: int, dtype, top: int = 0, grad: bool = False,
                  device: Optional[int] = None):

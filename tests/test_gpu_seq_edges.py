@@ -411,3 +411,39 @@ def test_grad_of_short_documents(dtype, heads, kv, dim, cap, bias):
         near(getattr(b, n), ref[n], u * np.abs(ref[n]) + (u * u + e) * (ref[n + "_abs"] + ref[n + "_dif"])
              + grid, n)
     c.check(b, ref)
+
+
+# ------------------------------------------------------------------ buffers of another layout
+@pytest.mark.parametrize("full_first", [False, True])
+def test_buffers_used_with_other_documents(full_first):
+    """Buffers of one layout used with another of the same sizes: the rows of no document are 0
+    there too, not the other layout's results or what the memory held."""
+    import torch
+    from paper_2212_11142_amd import seq
+    g = torch.Generator().manual_seed(0)
+    q, do = (torch.randn((300, 4, 64), generator=g).bfloat16().cuda() for _ in range(2))
+    k, v = (torch.randn((300, 2, 64), generator=g).bfloat16().cuda() for _ in range(2))
+    a = (seq.Documents([150, 150]) if full_first else
+         seq.Documents([150, 140], q_rows=300, k_begin=[0, 160], k_rows=300))
+    b = seq.Documents([90, 60], [90, 60], q_rows=300, k_begin=[20, 200], k_rows=300)
+    att = [seq.Attention(d, 4, 2, 64, torch.bfloat16) for d in (a, b)]
+    bufs = seq.AttendBuffers(att[0], grad=True)
+    for t in (bufs.out, bufs.lse, bufs.dq, bufs.dk, bufs.dv):
+        if full_first:
+            t.fill_(7.0)
+    big = max(x.workspace_bytes(True) for x in att)
+    bufs.grad_workspace = torch.empty(big, dtype=torch.uint8, device="cuda")
+    bufs.grad_workspace_bytes = big
+    small = max(x.workspace_bytes(False) for x in att)
+    if small:
+        bufs.workspace = torch.empty(small, dtype=torch.uint8, device="cuda")
+        bufs.workspace_bytes = small
+    for x in (att[0], att[1], att[0], att[1]):
+        seq.attend_into(x, q, k, v, bufs)
+        seq.attend_grad_into(x, q, k, v, do, bufs)
+        own = seq.AttendBuffers(x, grad=True)
+        seq.attend_into(x, q, k, v, own)
+        seq.attend_grad_into(x, q, k, v, do, own)
+        torch.cuda.synchronize()
+        for n in ("out", "lse", "dq", "dk", "dv"):
+            assert torch.equal(getattr(bufs, n), getattr(own, n)), n

@@ -75,8 +75,8 @@ def attention(docs=None, heads=2, kv_heads=1, dim=64, dtype=BF, **kw):
 
 def buffers(att, at=1 << 24, **kw):
     d, n = att.docs, att.dim
-    b = types.SimpleNamespace(workspace=None, workspace_bytes=0, grad_workspace=Tensor([1 << 20], torch.uint8),
-                              grad_workspace_bytes=1 << 20)
+    b = types.SimpleNamespace(docs=d, grad_docs=d, workspace=None, workspace_bytes=0,
+                              grad_workspace=Tensor([1 << 20], torch.uint8), grad_workspace_bytes=1 << 20)
     for k, rows, heads in (("out", d.q_rows, att.heads), ("rest", d.q_rows, att.heads),
                            ("dq", d.q_rows, att.heads), ("dk", d.k_rows, att.kv_heads),
                            ("dv", d.k_rows, att.kv_heads)):
