@@ -496,7 +496,7 @@ void gp_forest_free(gp_forest *forest);
  * gradients follow, the forward probabilities have two such terms, and so have the score
  * gradients of documents of up to 128 rows and keys. Score arithmetic, sums, lse and the table's
  * gradient are fp32 until the results are rounded; a cap of up to 64 costs a score up to cap
- * 2^-23, a larger one 2^-21 of it. */
+ * 2^-22, a larger one, or one of documents of up to 8 keys, 2^-21 of it. */
 typedef enum { GP_BF16 = 0, GP_FP16 = 1, GP_FP32 = 2 } gp_dtype;
 
 /* Rows x heads x dim values in device memory: element (r, h, c) at data + r row + h head

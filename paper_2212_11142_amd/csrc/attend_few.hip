@@ -442,7 +442,7 @@ hipError_t by_bias(const AttnArgs &a, void *part, hipStream_t s) {
 
 template <class T, int DP>
 hipError_t by_cap(const AttnArgs &a, void *part, hipStream_t s) {
-  switch (cap_kind(a.cap)) {
+  switch (cap_kind(a)) {
     case kCapNone: return by_bias<T, DP, kCapNone>(a, part, s);
     case kCapNear: return by_bias<T, DP, kCapNear>(a, part, s);
     default: return by_bias<T, DP, kCapFar>(a, part, s);

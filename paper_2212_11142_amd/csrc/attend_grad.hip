@@ -904,7 +904,7 @@ hipError_t by_bias(const AttnGradArgs &a, hipStream_t s) {
 
 template <class T, int DP>
 hipError_t by_cap(const AttnGradArgs &a, hipStream_t s) {
-  switch (cap_kind(a.f.cap)) {
+  switch (cap_kind(a.f)) {
     case kCapNone: return by_bias<T, DP, kCapNone>(a, s);
     case kCapNear: return by_bias<T, DP, kCapNear>(a, s);
     default: return by_bias<T, DP, kCapFar>(a, s);

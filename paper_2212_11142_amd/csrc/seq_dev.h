@@ -413,16 +413,21 @@ __device__ inline DocTile find_tile(const int32_t *b, const int32_t *e, int docs
 // A score in units of log 2 is a x + b + bias. Without a cap x is the product itself. With one there
 // are two forms of cap tanh(z / cap), z = scale times the product:
 //   near: cap + 2 cap x, x = -1 / (1 + e^(2 z / cap)); exact at both ends, where the exponential is 0
-//         or infinite, but off by up to cap 2^-23 in all between: 7.6e-6 at a cap of 64, 1e-3 at 1e4;
+//         or infinite, but off by up to cap 2^-22 in all between: 1.5e-5 at a cap of 64, 2e-3 at 1e4;
 //   far:  x is the capped product itself, for |z| < cap / 4 as z times an even polynomial of z / cap
 //         (the series of tanh; the first term left out is 9e-9 of it), else as cap (1 - 2 / (1 +
 //         e^(2 z / cap))): off by 2^-21 of itself, for every cap. It takes longer: near / far,
 //         13 documents of up to 1021 rows, 16 heads of 128, 57 / 68 us; training on 16 documents,
 //         16 heads of 64, 229 / 265; 64 caches of up to 32,768 421 / 423.
 enum CapKind { kCapNone = 0, kCapNear = 1, kCapFar = 2 };
+// Documents of up to 8 keys, whose log-sums are little more than one score, take the far form for
+// every cap (a log-sum of one key at a cap of 50 was off by 1.2e-6 of itself, of 8 keys by 6e-7; up
+// to 32 keys the far form would cost 1000 documents 6 to 9%).
 constexpr float kNearCap = 64.f;   // the largest cap of the near form
-inline CapKind cap_kind(float cap) {
-  return !(cap > 0.f) ? kCapNone : (cap <= kNearCap ? kCapNear : kCapFar);
+constexpr int kNearKeys = 8;       // documents of the near form have more
+inline CapKind cap_kind(const AttnArgs &a) {
+  if (!(a.cap > 0.f)) return kCapNone;
+  return a.cap <= kNearCap && a.max_k > kNearKeys ? kCapNear : kCapFar;
 }
 struct ScoreScale {
   float c;   // near: the product's factor in the exponential; far: scale

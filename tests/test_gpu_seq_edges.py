@@ -147,6 +147,21 @@ def test_caps_near_zero(cap):
         c.check()
 
 
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("cap", [20.0, 50.0, 64.0])
+@pytest.mark.parametrize("heads,kv", [(4, 2), (96, 32)])
+def test_caps_of_few_keys(dtype, cap, heads, kv):
+    """Documents of up to 8 keys, where a log-sum is little more than one score: capped scores
+    are off by 2^-21 of themselves, the sum and its logarithm by as much of 1 + lse."""
+    c = Case(dtype, [(1, 1)] * 9 + [(2, 2), (5, 3), (8, 8), (17, 4)], heads, kv, 64, cap=cap, size=0.3,
+             bias="one", grad=True)
+    c.table *= 0.0
+    b, ref = c.run(), c.oracle()
+    lse = np.where(np.isfinite(ref["lse"]), np.abs(ref["lse"]), 0.0)
+    near(b.lse, ref["lse"], 2.0 ** -21 * (1 + ref["score"]) + 2.0 ** -22 * lse, "lse")
+    c.check(b, ref)
+
+
 # ------------------------------------------------------------------ offsets of logits
 @pytest.mark.parametrize("rows,width", [(70, 300), (5, 3000), (300, 5000), (6, 70000)])
 @pytest.mark.parametrize("offset", [0.0, 2.0 ** 10, 2.0 ** 20, -2.0 ** 20])
