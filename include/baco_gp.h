@@ -601,6 +601,143 @@ gp_status gp_logprob_norm_grad(int32_t dtype, const void *x, int64_t stride, int
                                const float *g_entropy, void *dx, int64_t dx_stride,
                                void *stream);
 
+/* ---------------------------------------------------------------- layers of a sequence surrogate */
+
+/* The layers of such a model around its attention: norms of its rows, rotary positions of query and
+ * key heads, the gated feed-forward block, and the optimiser's step over its weights. All calls
+ * are asynchronous on `stream`, which is the current device's, and deterministic: sums have a fixed
+ * order. An output may be an input's own memory (same pointer and strides) only where it is said. */
+
+/* Norm of rows: h = x + residual, rounded to dtype as it is stored in sum (h = x without a
+ * residual); m the mean of h (0 with centre == 0: the root-mean-square form),
+ *   s = 1 / sqrt(mean((h - m)^2) + eps),  xh = (h - m) s,  out = xh weight + bias,
+ * in fp32, out rounded once. */
+typedef struct {
+  int32_t dtype;         /* gp_dtype of the rows */
+  int32_t weight_dtype;  /* of weight, bias and their gradients: dtype or GP_FP32 */
+  int32_t width;         /* entries of a row, 1..2^24 */
+  int32_t centre;
+  float eps;             /* finite, > 0 */
+} gp_norm_spec;
+
+/* x, residual (NULL: none), out, sum (with a residual): device, rows of `width` entries, strides in
+ * entries; weight and bias: device [width] or NULL (1 and 0). stats: device float[rows][2] or NULL,
+ * receives m and s for the gradient. out, or sum, may be x or residual. */
+gp_status gp_norm(const gp_norm_spec *norm, int32_t rows, const void *x, int64_t x_stride,
+                  const void *residual, int64_t residual_stride, const void *weight, const void *bias,
+                  void *out, int64_t out_stride, void *sum, int64_t sum_stride, float *stats,
+                  void *stream);
+
+/* Gradients from dout = dloss/dout and dsum (NULL: none) = dloss/dsum: with g = dout weight,
+ *   dx = s (g - mean(g) - xh mean(g xh)) + dsum  (without centring no mean(g)),
+ * which is the gradient of the residual too; dweight = sum over rows of dout xh, dbias = that of
+ * dout (device [width] of weight_dtype, either may be NULL; 0 with no rows). h: gp_norm's sum (its x
+ * without a residual), stats and weight gp_norm's. dx may be h, dout or dsum. */
+size_t gp_norm_grad_workspace_bytes(const gp_norm_spec *norm, int32_t rows);
+gp_status gp_norm_grad(const gp_norm_spec *norm, int32_t rows, const void *h, int64_t h_stride,
+                       const float *stats, const void *weight, const void *dout, int64_t dout_stride,
+                       const void *dsum, int64_t dsum_stride, void *dx, int64_t dx_stride, void *dweight,
+                       void *dbias, void *workspace, size_t ws_bytes, void *stream);
+
+/* Rotary positions: pair i of the first `rotated` values of a head, (i, i + rotated / 2) or, with
+ * interleaved, (2 i, 2 i + 1), turns by the angle 2 pi pos turns[i]:
+ *   (a, b) -> magnitude (a cos - b sin, a sin + b cos);
+ * the values behind are copied. Angles are reduced in fp64, the rest is fp32, rounded once. */
+typedef struct {
+  int32_t dtype;         /* gp_dtype of the heads */
+  int32_t dim;           /* head size: a multiple of 8, 8..128 */
+  int32_t rotated;       /* even, 2..dim */
+  int32_t interleaved;
+  float magnitude;       /* finite; 1: lengths stay as they are */
+  const double *turns;   /* device double[rotated / 2]: turns per position */
+} gp_rotary;
+
+/* Rotates rows x heads (gp_heads as for attention, of any gp_dtype) by positions (device
+ * int32[rows], of any sign); with inverse by the opposite angles, which is the gradient's way. out
+ * may be x. */
+gp_status gp_rotate(const gp_rotary *rotary, int32_t rows, const int32_t *positions, int32_t heads,
+                    const gp_heads *x, const gp_heads *out, int32_t inverse, void *stream);
+
+/* New rows of runs with caches, in one launch: out = rotated q; row slots[r] (device int64[rows]) of
+ * k_cache receives the rotated k of row r, that of v_cache its v as it is. A row whose slot is outside
+ * 0..cache_rows-1 is not kept. Slots within the caches must differ: of rows with the same slot, any
+ * one's values are kept, for each value anew. out may be q; the caches must not be inputs. */
+gp_status gp_rotate_append(const gp_rotary *rotary, int32_t rows, const int32_t *positions,
+                           const int64_t *slots, int32_t heads, const gp_heads *q, const gp_heads *out,
+                           int32_t kv_heads, const gp_heads *k, const gp_heads *v, int64_t cache_rows,
+                           const gp_heads *k_cache, const gp_heads *v_cache, void *stream);
+
+/* Gated feed-forward block: out = act(x Wg^T) * (x Wu^T) of rows x [rows][width], w_gate and w_up
+ * [hidden][width]; act(z) = z / (1 + e^-z) or z Phi(z). Products add in fp32, out is rounded once. */
+typedef enum { GP_SILU = 0, GP_GELU = 1 } gp_activation;
+
+/* Element (r, c) of a matrix at data + r row + c (row stride in elements, a multiple of 8, up to
+ * 2^21; data 16-byte aligned). Rows of what is written must not overlap. */
+typedef struct {
+  void *data;
+  int64_t row;
+} gp_matrix;
+
+typedef struct {
+  int32_t dtype;         /* GP_BF16 or GP_FP16 */
+  int32_t width, hidden; /* multiples of 8, up to 2^21 */
+  int32_t activation;    /* gp_activation */
+} gp_gated_spec;
+
+/* out must not be an input. */
+gp_status gp_gated(const gp_gated_spec *gated, int32_t rows, const gp_matrix *x, const gp_matrix *w_gate,
+                   const gp_matrix *w_up, const gp_matrix *out, void *stream);
+
+/* Gradients from dout [rows][hidden]: dx, dw_gate, dw_up (0 with no rows), none of them an input.
+ * Both projections are formed again; their gradients are rounded to dtype once, as operands of the
+ * products that follow. */
+size_t gp_gated_grad_workspace_bytes(const gp_gated_spec *gated, int32_t rows);
+gp_status gp_gated_grad(const gp_gated_spec *gated, int32_t rows, const gp_matrix *x,
+                        const gp_matrix *w_gate, const gp_matrix *w_up, const gp_matrix *dout,
+                        const gp_matrix *dx, const gp_matrix *dw_gate, const gp_matrix *dw_up,
+                        void *workspace, size_t ws_bytes, void *stream);
+
+/* A step of AdamW over many tensors: with g = factor grad and step t,
+ *   m = b1 m + (1 - b1) g,  v = b2 v + (1 - b2) g^2,
+ *   w = w - lr decay w - lr (m / (1 - b1^t)) / (sqrt(v / (1 - b2^t)) + eps),
+ * in fp32. w is the master copy where a tensor has one; param is rounded from it.
+ *
+ * States of 8 bits: each 256 values of a tensor share scales, powers of two, m = e4m3 code x
+ * scales[0], v = e5m2 code x scales[1] (OCP formats). A scale is 2^(k - 7) for m and 2^(k - 14) for
+ * v, k the exponent of the largest magnitude, but 2^-126 at least, and 1 where all are 0. A value
+ * between two codes takes the upper one if its place between them, in 65536ths, and a random 16-bit
+ * number reach 65536 together; an m below its smallest normal code goes to the nearest (upward
+ * halfway), a v above 0 never to 0. The random numbers: with E = 256 (blocks of the tensors before)
+ * + the value's number in its tensor, word E % 4 of Philox4x32-10 with counter (E / 4 low, E / 4
+ * high, t low, 0) and key (seed low, seed high); its low half for m, its high half for v. The step
+ * itself takes the m and v that were not rounded yet. A block with a state that is not finite
+ * becomes NaN (by its scale). */
+typedef struct {
+  int32_t dtype;         /* gp_dtype of the weights */
+  int32_t grad_dtype;    /* of the gradients: dtype or GP_FP32 */
+  int32_t state_bits;    /* 8 or 32 */
+  double beta1, beta2;   /* 0..1, below 1 */
+  double lr, eps, decay; /* eps > 0 */
+  int64_t step;          /* t, >= 1 */
+  const float *lr_device;     /* device float[1], in lr's place; NULL: lr */
+  const int64_t *step_device; /* device int64[1], in step's place (>= 1); NULL: step */
+  const float *factor;        /* device float[1], of the gradients; NULL: 1 */
+  uint64_t seed;
+} gp_adamw_spec;
+
+typedef struct {
+  void *param, *master;  /* device [count]; master fp32, with 16-bit weights, or NULL */
+  void *m, *v;           /* device [count], fp32 or codes */
+  float *scales;         /* device float[ceil(count / 256)][2], with 8 bits */
+  int64_t count;
+} gp_adamw_tensor;
+
+/* tensors: host [count], grads: host array of device pointers, a gradient of its tensor's size each
+ * (both are read before the call returns). A tensor without a gradient (NULL) is left as it is.
+ * Tensors must not overlap. */
+gp_status gp_adamw(const gp_adamw_spec *adamw, int32_t count, const gp_adamw_tensor *tensors,
+                   const void *const *grads, void *stream);
+
 /* ---------------------------------------------------------------- inspection */
 
 /* Bytes of workspace needed by the debug calls below for `count` configurations. */

@@ -60,6 +60,34 @@ class _Heads(C.Structure):
     _fields_ = [("data", C.c_void_p), ("row", C.c_int64), ("head", C.c_int64)]
 
 
+class _Matrix(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("row", C.c_int64)]
+
+
+class _Norm(C.Structure):
+    _fields_ = [(k, C.c_int32) for k in ("dtype", "weight_dtype", "width", "centre")] + [("eps", C.c_float)]
+
+
+class _Rotary(C.Structure):
+    _fields_ = [(k, C.c_int32) for k in ("dtype", "dim", "rotated", "interleaved")] + \
+               [("magnitude", C.c_float), ("turns", C.c_void_p)]
+
+
+class _Gated(C.Structure):
+    _fields_ = [(k, C.c_int32) for k in ("dtype", "width", "hidden", "activation")]
+
+
+class _AdamW(C.Structure):
+    _fields_ = ([(k, C.c_int32) for k in ("dtype", "grad_dtype", "state_bits")]
+                + [(k, C.c_double) for k in ("beta1", "beta2", "lr", "eps", "decay")]
+                + [("step", C.c_int64)] + [(k, C.c_void_p) for k in ("lr_device", "step_device", "factor")]
+                + [("seed", C.c_uint64)])
+
+
+class _AdamWTensor(C.Structure):
+    _fields_ = [(k, C.c_void_p) for k in ("param", "master", "m", "v", "scales")] + [("count", C.c_int64)]
+
+
 class _Attention(C.Structure):
     _fields_ = ([(k, C.c_int32) for k in ("dtype", "heads", "kv_heads", "dim", "n_docs", "q_rows",
                                           "k_rows", "max_q", "max_k")]
@@ -135,6 +163,22 @@ _SIGS = [
                                   _VP, _VP, _VP, _VP, _VP, _VP, C.c_int64, _VP]),
     ("gp_logprob_norm_grad", C.c_int, [C.c_int32, _VP, C.c_int64, C.c_int32, C.c_int32, C.c_float,
                                        _VP, _VP, _VP, _VP, _VP, _VP, C.c_int64, _VP]),
+    ("gp_norm", C.c_int, [C.POINTER(_Norm), C.c_int32, _VP, C.c_int64, _VP, C.c_int64, _VP, _VP, _VP,
+                          C.c_int64, _VP, C.c_int64, _VP, _VP]),
+    ("gp_norm_grad_workspace_bytes", C.c_size_t, [C.POINTER(_Norm), C.c_int32]),
+    ("gp_norm_grad", C.c_int, [C.POINTER(_Norm), C.c_int32, _VP, C.c_int64, _VP, _VP, _VP, C.c_int64,
+                               _VP, C.c_int64, _VP, C.c_int64, _VP, _VP, _VP, C.c_size_t, _VP]),
+    ("gp_rotate", C.c_int, [C.POINTER(_Rotary), C.c_int32, _VP, C.c_int32, C.POINTER(_Heads),
+                            C.POINTER(_Heads), C.c_int32, _VP]),
+    ("gp_rotate_append", C.c_int, [C.POINTER(_Rotary), C.c_int32, _VP, _VP, C.c_int32,
+                                   C.POINTER(_Heads), C.POINTER(_Heads), C.c_int32, C.POINTER(_Heads),
+                                   C.POINTER(_Heads), C.c_int64, C.POINTER(_Heads), C.POINTER(_Heads),
+                                   _VP]),
+    ("gp_gated", C.c_int, [C.POINTER(_Gated), C.c_int32] + [C.POINTER(_Matrix)] * 4 + [_VP]),
+    ("gp_gated_grad_workspace_bytes", C.c_size_t, [C.POINTER(_Gated), C.c_int32]),
+    ("gp_gated_grad", C.c_int, [C.POINTER(_Gated), C.c_int32] + [C.POINTER(_Matrix)] * 7
+     + [_VP, C.c_size_t, _VP]),
+    ("gp_adamw", C.c_int, [C.POINTER(_AdamW), C.c_int32, C.POINTER(_AdamWTensor), C.POINTER(_VP), _VP]),
     ("gp_debug_workspace_bytes", C.c_size_t, [C.POINTER(_Space), _VP, C.c_int64]),
     ("gp_debug_encode", C.c_int, [C.POINTER(_Space), C.POINTER(_VP), C.c_int64, _VP, _VP, _VP,
                                   C.c_size_t, _VP]),
