@@ -19,38 +19,46 @@ namespace {
 constexpr int kStep = 64;              // of the summed axis
 constexpr int kStepBytes = 2 * kStep;
 
-// R rows of an operand, copied by WAVES wavefronts.
+// Copies 64 pieces of 16 bytes of a buffer, a lane's at `offset`, to 1024 bytes of LDS. (s_nop: as for
+// a tile's copies, a scalar register of the descriptor must be 5 cycles old.)
+__device__ inline void copy_pieces(u32x4 buf, int offset, uint32_t lds) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds"
+               ::"s"(uniform((int)lds)), "v"(offset), "s"(buf)
+               : "memory");
+}
+
+// R rows of an operand, copied by WAVES wavefronts. copy(i, ..): the i-th of a wavefront's kCopies
+// instructions for a step that starts at k0; nothing is read if `on` is false.
 template <bool COL, int R, int WAVES>
 struct Side;
 
 template <int R, int WAVES>
 struct Side<false, R, WAVES> {
-  static constexpr int kBytes = R * kStepBytes;
-  TileCopy<64, R, WAVES> copy;
+  typedef TileCopy<64, R, WAVES> Copy;
+  static constexpr int kBytes = R * kStepBytes, kCopies = Copy::kCount, kReads = 1;
+  Copy of;
   TileReader<64> reader;
   const char *base;
   int64_t stride;
-  int rows, wave, lane;
+  int rows, piece;
 
   // rows row0.. of a matrix of `all` rows
-  __device__ void init(const char *p, int64_t row0, int64_t all, int64_t row_stride, int w, int l) {
-    base = p + row0 * row_stride;
-    stride = row_stride;
+  __device__ void move(const char *p, int64_t row0, int64_t all) {
+    base = p + row0 * stride;
     rows = (int)max((int64_t)0, min((int64_t)R, all - row0));
-    wave = w, lane = l;
-    copy.init(wave, lane, (int)stride, kStepBytes);
-    reader.init(lane);
   }
-  // k0.. of k
-  __device__ void start(int64_t k0, int64_t k, uint32_t lds) const {
-    const int64_t left = 2 * (k - k0);
-    if (left >= kStepBytes) {
-      copy.start(row_buffer(base + 2 * k0, 0, rows, stride, kStepBytes), lds);
-    } else {
-      TileCopy<64, R, WAVES> tail;
-      tail.init(wave, lane, (int)stride, (int)left);
-      tail.start(row_buffer(base + 2 * k0, 0, rows, stride, (int)left), lds);
-    }
+  __device__ void init(const char *p, int64_t row0, int64_t all, int64_t row_stride, int wave, int lane) {
+    stride = row_stride;
+    move(p, row0, all);
+    of.init(wave, lane, (int)stride, kStepBytes);
+    reader.init(lane);
+    // the piece of a row that this lane copies: the same in all its rows, which are WAVES * 8 apart
+    piece = ((lane % 8) ^ swizzle<64>(wave * 8 + lane / 8)) * 16;
+  }
+  __device__ void copy(int i, bool on, int64_t k0, int64_t k, uint32_t lds) const {
+    const int left = (int)min((int64_t)kStepBytes, 2 * (k - k0));
+    copy_pieces(row_buffer(base + 2 * k0, 0, on ? rows : 0, stride, left),
+                piece < left ? of.voff[i] : 0x7ffffff0, lds + of.lds0 + i * (WAVES * 1024));
   }
   __device__ uint32_t at(uint32_t lds) const { return TileReader<64>::at(lds, reader.row); }
   // rows 32 i.., k = 16 s ..
@@ -59,8 +67,10 @@ struct Side<false, R, WAVES> {
 
 template <int R, int WAVES>
 struct Side<true, R, WAVES> {
+  typedef TileCopy<128, kStep, WAVES> Copy;
   static constexpr int kBytes = R * kStepBytes, kParts = R / 128, kPart = kStep * 256;
-  TileCopy<128, kStep, WAVES> copy[kParts];
+  static constexpr int kCopies = kParts * Copy::kCount, kReads = 2;
+  Copy of[kParts];
   const char *base;
   int64_t stride;
   int bytes;
@@ -72,20 +82,18 @@ struct Side<true, R, WAVES> {
     stride = row_stride;
     bytes = (int)max((int64_t)0, min((int64_t)R, all - row0)) * 2;
 #pragma unroll
-    for (int i = 0; i < kParts; ++i) copy[i].init(wave, lane, (int)stride, bytes - 256 * i);
+    for (int i = 0; i < kParts; ++i) of[i].init(wave, lane, (int)stride, bytes - 256 * i);
     // the transposing reads of lane half h: the step's rows 16 s + 8 h + 0..3 and + 4..7, so that k
     // runs as in a ROW operand (a row's swizzle differs by one piece between the two)
     const int q = 8 * (lane >> 5) + ((lane & 15) >> 2);
     const int piece = 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1);
     col = q * 256 + (piece ^ swizzle<128>(q)) * 16 + (lane & 1) * 8;
   }
-  __device__ void start(int64_t k0, int64_t k, uint32_t lds) const {
-    const int rows = (int)min((int64_t)kStep, k - k0);
-#pragma unroll
-    for (int i = 0; i < kParts; ++i) {
-      const int b = min(256, bytes - 256 * i);
-      copy[i].start(row_buffer(base + 256 * i, k0, b > 0 ? rows : 0, stride, b), lds + i * kPart);
-    }
+  __device__ void copy(int i, bool on, int64_t k0, int64_t k, uint32_t lds) const {
+    const int rows = (int)min((int64_t)kStep, k - k0), q = i / Copy::kCount, n = i % Copy::kCount;
+    const int b = min(256, bytes - 256 * q);
+    copy_pieces(row_buffer(base + 256 * q, k0, on && b > 0 ? rows : 0, stride, b), of[q].voff[n],
+                lds + q * kPart + of[q].lds0 + n * (WAVES * 1024));
   }
   __device__ uint32_t at(uint32_t lds) const { return TileReader<128>::at(lds, col); }
   static __device__ u32x4 operand(uint32_t x, int i, int s) {
@@ -98,16 +106,57 @@ struct Side<true, R, WAVES> {
   }
 };
 
-// Runs steps first .. end - 1: start(step, stage) copies, compute(stage) multiplies.
-template <class Start, class Compute>
-__device__ inline void run_steps(int first, int end, Start start, Compute compute) {
-  if (first < end) start(first, 0);
-  for (int i = first; i < end; ++i) {
-    const int stage = (i - first) & 1;
-    copies_barrier();                  // this step's copies are there, the other stage has been read
-    if (i + 1 < end) start(i + 1, stage ^ 1);
-    compute(stage);
+// Runs `count` steps, each 4 times 16 of the summed axis: after begin(step), called for one step after
+// the other and for two past the last, copy(stage, i) is the i-th of a wavefront's COPIES copies,
+// read(stage, s, i, operands) fetches the i-th of a quarter's READS operands, multiply(operands, i) is
+// the i-th of its MFMAS products, and end(step, stage) follows a step's products.
+//
+// A quarter's operands are read while the one before is multiplied. The block meets in front of a step's
+// last quarter, whose operands are in registers then: behind that barrier the next step's copies are
+// there, and this step's place in LDS is free for the one after, whose copies go out one by one between
+// the products of two quarters: a wavefront that asks for all at once waits for the units that take
+// them, and its products with it (dx of 16,384 x 1,024 from 8,192: 229 us, 255 with the copies in one
+// go; 239 where the lines were asked for two steps ahead, too). At the end of a step the second half of
+// its place in LDS is unused until the block meets.
+template <class Operands, int COPIES, int MFMAS, int READS, class Begin, class Copy, class Read, class Multiply,
+          class End>
+__device__ inline void run_steps(int64_t count, Begin begin, Copy copy, Read read, Multiply multiply, End end) {
+  if (count <= 0) return;
+  constexpr int kHalf = COPIES / 2;
+  begin(0);
+#pragma unroll
+  for (int i = 0; i < COPIES; ++i) copy(0, i);
+  begin(1);
+#pragma unroll
+  for (int i = 0; i < kHalf; ++i) copy(1, i);
+  asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" ::"n"(kHalf) : "memory");
+  Operands f, g;
+  // multiplies `now` while the next quarter's operands are read, and copies `from`.. to stage `to`
+  auto quarter = [&](const Operands &now, Operands &next, int stage, int s, int to, int from) {
+#pragma unroll
+    for (int i = 0; i < MFMAS; ++i) {
+      multiply(now, i);
+#pragma unroll
+      for (int r = i * READS / MFMAS; r < (i + 1) * READS / MFMAS; ++r) read(stage, s, r, next);
+      if (from >= 0 && (i + 1) * kHalf / MFMAS > i * kHalf / MFMAS)
+        copy(to, from + i * kHalf / MFMAS);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+  };
+#pragma unroll
+  for (int r = 0; r < READS; ++r) read(0, 0, r, f);
+  for (int64_t i = 0; i < count; ++i) {
+    const int stage = (int)i & 1;
+    quarter(f, g, stage, 1, stage ^ 1, kHalf);
+    quarter(g, f, stage, 2, 0, -1);
+    quarter(f, g, stage, 3, 0, -1);
+    begin(i + 2);
+    copies_barrier();
+    quarter(g, f, stage ^ 1, 0, stage, 0);
+    end(i, stage);
   }
+  // (what was asked for past the end: a block's place in LDS ends with it)
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
 }
 
 // Tile of a block: neighbours in m share an XCD's cache for the n side, eight m tiles to a group.
@@ -123,6 +172,64 @@ __device__ inline Tile tile_of(unsigned block, unsigned blocks, int nm, int nn) 
   const unsigned size = min(kGroup, nm - group * kGroup);
   return {(int)(group * kGroup + in % size), (int)(in / size)};
 }
+
+// ------------------------------------------------------------------ results
+// A wavefront's 32 rows of 32 C columns on their way between registers, as the matrix units have
+// them (4 consecutive values of a row a lane), and memory (rows of 64 C bytes, 16 bytes a lane),
+// through its own place in LDS. (Stored from the registers at once, an instruction's 1024 bytes
+// go to 32 rows instead of 16 / C.)
+template <int C>
+struct Exchange {
+  static constexpr int kBytes = 32 * 64 * C, kPieces = 4 * C, kRows = 64 / kPieces, kCount = 32 / kRows;
+  uint32_t lds;
+  int lane;
+
+  __device__ uint32_t at(int row, int piece) const {
+    return lds + row * (64 * C) + (piece ^ (row & (kPieces - 1))) * 16;
+  }
+  // of a lane: values 32 c + 8 g + 4 (lane / 32) + 0..3 of row lane % 32
+  __device__ void put(int c, int g, u32x2 v) const {
+    typedef __attribute__((address_space(3))) u32x2 lds_u32x2;
+    *(lds_u32x2 *)(uintptr_t)(at(lane & 31, 4 * c + g) + 8 * (lane >> 5)) = v;
+  }
+  __device__ u32x2 get(int c, int g) const {
+    typedef __attribute__((address_space(3))) const u32x2 lds_u32x2;
+    return *(lds_u32x2 *)(uintptr_t)(at(lane & 31, 4 * c + g) + 8 * (lane >> 5));
+  }
+  // of a lane: piece lane % kPieces of row kRows i + lane / kPieces
+  __device__ void put_row(int i, u32x4 v) const {
+    typedef __attribute__((address_space(3))) u32x4 lds_u32x4;
+    *(lds_u32x4 *)(uintptr_t)at(kRows * i + lane / kPieces, lane % kPieces) = v;
+  }
+  __device__ u32x4 get_row(int i) const {
+    typedef __attribute__((address_space(3))) const u32x4 lds_u32x4;
+    return *(lds_u32x4 *)(uintptr_t)at(kRows * i + lane / kPieces, lane % kPieces);
+  }
+  // Whether a lane's piece of rows kRows i .. is within `rows` and `bytes`, and its offset.
+  __device__ bool within(int i, int64_t rows, int64_t bytes) const {
+    return kRows * i + lane / kPieces < rows && lane % kPieces * 16 < bytes;
+  }
+  __device__ int64_t offset(int i, int64_t stride) const {
+    return (kRows * i + lane / kPieces) * stride + lane % kPieces * 16;
+  }
+  // Writes what lies in LDS to the rows at p.
+  __device__ void store(char *p, int64_t stride, int64_t rows, int64_t bytes) const {
+    u32x4 v[kCount];
+#pragma unroll
+    for (int i = 0; i < kCount; ++i) v[i] = get_row(i);
+#pragma unroll
+    for (int i = 0; i < kCount; ++i)
+      if (within(i, rows, bytes)) *reinterpret_cast<u32x4 *>(p + offset(i, stride)) = v[i];
+  }
+  template <class T>
+  __device__ void put_all(const f32x16 *v) const {
+#pragma unroll
+    for (int c = 0; c < C; ++c)
+#pragma unroll
+      for (int g = 0; g < 4; ++g)
+        put(c, g, u32x2{T::pack(v[c][4 * g], v[c][4 * g + 1]), T::pack(v[c][4 * g + 2], v[c][4 * g + 3])});
+  }
+};
 
 // ------------------------------------------------------------------ activations
 constexpr int kSilu = 0, kGelu = 1;   // GP_SILU, GP_GELU
@@ -156,91 +263,151 @@ __device__ inline void activation(float z, float &a, float &d) {
 }
 
 // ------------------------------------------------------------------ both projections
-// BM rows of x and BN / 2 hidden values per block, WM x WN wavefronts, each of 32 hidden values.
+// BM rows of x and BN / 2 hidden values per block, WM x WN wavefronts, each of 32 C hidden values.
 template <class T, int BM, int BN, int WM, int WN, int ACT, bool GRAD>
 __global__ __launch_bounds__(64 * WM * WN, 2) void gated_kernel(GatedGradArgs g, char *dg, char *du,
                                                              int nm, int nn) {
-  constexpr int W = WM * WN, TM = BM / 32 / WM;
-  static_assert(BN / 2 == 32 * WN);
+  constexpr int W = WM * WN, TM = BM / 32 / WM, C = BN / 64 / WN;
   extern __shared__ char stages[];
   constexpr int kHalf = BN / 2 * kStepBytes, kStage = (BM + BN) * kStepBytes;
+  typedef Exchange<C> Swap;
+  // (the copies' second half is x's)
+  static_assert(BM * kStepBytes >= W * Swap::kBytes);
+  static_assert(2 * Side<false, BN / 2, W>::kCopies == Side<false, BM, W>::kCopies);
   const GatedArgs &a = g.f;
   const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6);
   const int wm = wave / WN, wn = wave % WN;
-  const Tile t = tile_of(blockIdx.x, gridDim.x, nm, nn);
-  const int64_t m0 = (int64_t)t.m * BM, n0 = (int64_t)t.n * (BN / 2);
-  Side<false, BN / 2, W> gate, up;
-  Side<false, BM, W> x;
-  gate.init(a.w_gate, n0, a.hidden, a.gate_row, wave, lane);
-  up.init(a.w_up, n0, a.hidden, a.up_row, wave, lane);
-  x.init(a.x, m0, a.rows, a.x_row, wave, lane);
+  const unsigned all = (unsigned)nm * nn;
+  Tile t = tile_of(blockIdx.x, all, nm, nn);                // whose products are summed
+  Tile next = t;                                            // whose operands are copied
+  typedef Side<false, BN / 2, W> Half;
+  typedef Side<false, BM, W> Whole;
+  Half gate, up;
+  Whole x;
+  gate.init(a.w_gate, (int64_t)t.n * (BN / 2), a.hidden, a.gate_row, wave, lane);
+  up.init(a.w_up, (int64_t)t.n * (BN / 2), a.hidden, a.up_row, wave, lane);
+  x.init(a.x, (int64_t)t.m * BM, a.rows, a.x_row, wave, lane);
   const uint32_t lds = lds_address(stages);
-  f32x16 acc[2][TM];
+  f32x16 acc[TM][2][C];
+  auto clear = [&] {
 #pragma unroll
-  for (int i = 0; i < 2; ++i)
+    for (int j = 0; j < TM; ++j)
 #pragma unroll
-    for (int j = 0; j < TM; ++j) acc[i][j] = f32x16{0.f};
-  run_steps(
-      0, (a.width + kStep - 1) / kStep,
-      [&](int step, int stage) {
-        const int64_t k0 = (int64_t)step * kStep;
-        const uint32_t to = lds + stage * kStage;
-        gate.start(k0, a.width, to);
-        up.start(k0, a.width, to + kHalf);
-        x.start(k0, a.width, to + 2 * kHalf);
-      },
-      [&](int stage) {
-        const uint32_t at = lds + stage * kStage;
-        const uint32_t pg = gate.at(at + wn * (32 * kStepBytes)), pu = pg + kHalf;
-        const uint32_t px = x.at(at + 2 * kHalf + wm * (BM / WM * kStepBytes));
-#pragma unroll
-        for (int s = 0; s < kStep / 16; ++s) {
-          const u32x4 og = gate.operand(pg, 0, s), ou = up.operand(pu, 0, s);
-#pragma unroll
-          for (int j = 0; j < TM; ++j) {
-            const u32x4 ox = x.operand(px, j, s);
-            acc[0][j] = T::mfma(og, ox, acc[0][j]);
-            acc[1][j] = T::mfma(ou, ox, acc[1][j]);
+      for (int i = 0; i < 2 * C; ++i) acc[j][i / C][i % C] = f32x16{0.f};
+  };
+  clear();
+  struct Operands {
+    u32x4 w[2][C], x[TM];
+  };
+  const int steps = (a.width + kStep - 1) / kStep;
+  // a tile's steps follow those of the block's tile before without a pause. Each row of tiles starts at
+  // another step: rows a power of two apart meet in few of the L2's channels
+  unsigned index = blockIdx.x;           // of next
+  int step = -1, left = steps;           // of next's, the one whose operands are copied; those left of t's
+  int64_t k0 = 0;
+  bool on = true;
+  run_steps<Operands, 2 * Half::kCopies + Whole::kCopies, 2 * C * TM, TM + 2 * C>(
+      (int64_t)steps * ((all - blockIdx.x + gridDim.x - 1) / gridDim.x),
+      [&](int64_t) {
+        if (++step == steps) {
+          step = 0;
+          index += gridDim.x;
+          on = index < all;
+          if (on) {
+            next = tile_of(index, all, nm, nn);
+            gate.move(a.w_gate, (int64_t)next.n * (BN / 2), a.hidden);
+            up.move(a.w_up, (int64_t)next.n * (BN / 2), a.hidden);
+            x.move(a.x, (int64_t)next.m * BM, a.rows);
           }
         }
-      });
-  const int64_t n = n0 + 32 * wn;
-  const int bytes = (int)min((int64_t)64, 2 * (a.hidden - n));
+        const int at = step + next.m % steps;
+        k0 = (int64_t)(at >= steps ? at - steps : at) * kStep;
+      },
+      [&](int stage, int i) {
+        const uint32_t to = lds + stage * kStage;
+        constexpr int H = Half::kCopies;
+        if (i < H) gate.copy(i, on, k0, a.width, to);
+        else if (i < 2 * H) up.copy(i - H, on, k0, a.width, to + kHalf);
+        else x.copy(i - 2 * H, on, k0, a.width, to + 2 * kHalf);
+      },
+      [&](int stage, int s, int i, Operands &o) {
+        const uint32_t at = lds + stage * kStage;
+        if (i < 2 * C)
+          o.w[i / C][i % C] = gate.operand(gate.at(at + wn * (32 * C * kStepBytes)) + i / C * kHalf, i % C, s);
+        else
+          o.x[i - 2 * C] = x.operand(x.at(at + 2 * kHalf + wm * (BM / WM * kStepBytes)), i - 2 * C, s);
+      },
+      [&](const Operands &o, int i) {
+        const int j = i / (2 * C), q = i % (2 * C) / C, c = i % C;
+        acc[j][q][c] = T::mfma(o.w[q][c], o.x[j], acc[j][q][c]);
+      },
+      [&](int64_t, int stage) {
+        if (--left) return;
+        left = steps;
+        // (x's part of the stage: its copies go out last, after the block has met)
+        const Swap swap = {lds + stage * kStage + 2 * kHalf + wave * Swap::kBytes, lane};
+        const int64_t n = (int64_t)t.n * (BN / 2) + 32 * C * wn, bytes = 2 * (a.hidden - n);
+        const int64_t row0 = (int64_t)t.m * BM + wm * (BM / WM);
+        t = next;
 #pragma unroll
-  for (int j = 0; j < TM; ++j) {
-    const int64_t row = m0 + wm * (BM / WM) + 32 * j + (lane & 31);
-    const bool ok = row < a.rows;
-    f32x16 u = acc[0][j], v = acc[1][j];
-    if constexpr (GRAD) {
-      const char *dy = g.dout + row * g.dout_row + 2 * n;
+        for (int j = 0; j < TM; ++j) {
+          const int64_t row = row0 + 32 * j, rows = a.rows - row;
+          f32x16 *u = acc[j][0], *v = acc[j][1];
+          if constexpr (GRAD) {
+            u32x4 dy[Swap::kCount];
 #pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        const int off = (8 * q + 4 * (lane >> 5)) * 2;
-        u32x2 w = {0, 0};
-        if (ok && off < bytes) w = *reinterpret_cast<const u32x2 *>(dy + off);
-        const uint32_t w0 = w[0], w1 = w[1];
-        const float y[4] = {T::lo(w0), T::hi(w0), T::lo(w1), T::hi(w1)};
+            for (int i = 0; i < Swap::kCount; ++i) {
+              dy[i] = u32x4{0, 0, 0, 0};
+              if (swap.within(i, rows, bytes))
+                dy[i] = *reinterpret_cast<const u32x4 *>(g.dout + row * g.dout_row + 2 * n +
+                                                         swap.offset(i, g.dout_row));
+            }
 #pragma unroll
-        for (int r = 0; r < 4; ++r) {
-          float f, d;
-          activation<ACT>(u[4 * q + r], f, d);
-          u[4 * q + r] = y[r] * v[4 * q + r] * d;
-          v[4 * q + r] = y[r] * f;
+            for (int i = 0; i < Swap::kCount; ++i) swap.put_row(i, dy[i]);
+            __builtin_amdgcn_wave_barrier();
+#pragma unroll
+            for (int c = 0; c < C; ++c)
+#pragma unroll
+              for (int q = 0; q < 4; ++q) {
+                if (q % 2 == 0) __builtin_amdgcn_sched_barrier(0);
+                const u32x2 w = swap.get(c, q);
+                const uint32_t w0 = w[0], w1 = w[1];
+                const float y[4] = {T::lo(w0), T::hi(w0), T::lo(w1), T::hi(w1)};
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                  float f, d;
+                  activation<ACT>(u[c][4 * q + r], f, d);
+                  u[c][4 * q + r] = y[r] * v[c][4 * q + r] * d;
+                  v[c][4 * q + r] = y[r] * f;
+                }
+              }
+            const int64_t stride = (int64_t)a.hidden * 2, to = row * stride + 2 * n;
+            __builtin_amdgcn_wave_barrier();
+            swap.template put_all<T>(u);
+            __builtin_amdgcn_wave_barrier();
+            swap.store(dg + to, stride, rows, bytes);
+            __builtin_amdgcn_wave_barrier();
+            swap.template put_all<T>(v);
+            __builtin_amdgcn_wave_barrier();
+            swap.store(du + to, stride, rows, bytes);
+          } else {
+#pragma unroll
+            for (int c = 0; c < C; ++c)
+#pragma unroll
+              for (int i = 0; i < 16; ++i) {
+                float f, d;
+                activation<ACT>(u[c][i], f, d);
+                u[c][i] = f * v[c][i];
+              }
+            swap.template put_all<T>(u);
+            __builtin_amdgcn_wave_barrier();
+            swap.store(a.out + row * a.out_row + 2 * n, a.out_row, rows, bytes);
+          }
+          __builtin_amdgcn_sched_barrier(0);             // (one at a time: registers)
         }
-      }
-      const int64_t to = row * ((int64_t)a.hidden * 2) + 2 * n;
-      store_row<T, 1>(dg + to, ok, bytes, &u, 1.f, lane);
-      store_row<T, 1>(du + to, ok, bytes, &v, 1.f, lane);
-    } else {
-#pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        float f, d;
-        activation<ACT>(u[i], f, d);
-        u[i] = f * v[i];
-      }
-      store_row<T, 1>(a.out + row * a.out_row + 2 * n, ok, bytes, &u, 1.f, lane);
-    }
-  }
+        clear();
+        asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+      });
 }
 
 // ------------------------------------------------------------------ the gradient's products
@@ -272,67 +439,78 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void product_kernel(ProductArgs p)
   const int per = (int)((p.k + kStep - 1) / kStep), all = per * SEGMENTS;
   const int first = (int)((int64_t)all * split / p.splits);
   const int end = (int)((int64_t)all * (split + 1) / p.splits);
+  const int skew = !B_COL && end > first ? t.m % (end - first) : 0;
   ASide a;
   BSide b;
-  int segment = SEGMENTS == 2 ? (first >= per) : output;
+  int segment = SEGMENTS == 2 ? (first + skew >= per) : output;
   a.init(p.a[segment], n0, p.n, p.a_row[segment], wave, lane);
   b.init(p.b[segment], m0, p.m, p.b_row[segment], wave, lane);
   const uint32_t lds = lds_address(stages);
-  f32x16 acc[TN][TM];
+  f32x16 acc[TM][TN];
 #pragma unroll
-  for (int i = 0; i < TN; ++i)
+  for (int j = 0; j < TM; ++j)
 #pragma unroll
-    for (int j = 0; j < TM; ++j) acc[i][j] = f32x16{0.f};
-  run_steps(
-      first, end,
-      [&](int step, int stage) {
-        if (SEGMENTS == 2 && step >= per) {
-          if (!segment) {
-            segment = 1;
-            a.init(p.a[1], n0, p.n, p.a_row[1], wave, lane);
-            b.init(p.b[1], m0, p.m, p.b_row[1], wave, lane);
+    for (int i = 0; i < TN; ++i) acc[j][i] = f32x16{0.f};
+  struct Operands {
+    u32x4 a[TN], b[TM];
+  };
+  bool on = true;                        // copies of a step that there is, from k0 on
+  int64_t k0 = 0;
+  run_steps<Operands, ASide::kCopies + BSide::kCopies, TM * TN, TN + TM>(
+      end - first,
+      [&](int64_t i) {
+        int step = first + (int)i;
+        on = step < end;
+        step += skew;
+        step = step >= end ? step - (end - first) : step;
+        if (SEGMENTS == 2) {
+          const int now = step >= per;
+          if (now != segment && on) {
+            segment = now;
+            a.init(p.a[now], n0, p.n, p.a_row[now], wave, lane);
+            b.init(p.b[now], m0, p.m, p.b_row[now], wave, lane);
           }
-          step -= per;
+          step -= now * per;
         }
-        const int64_t k0 = (int64_t)step * kStep;
-        a.start(k0, p.k, lds + stage * kStage);
-        b.start(k0, p.k, lds + stage * kStage + kA);
+        k0 = on ? (int64_t)step * kStep : 0;
       },
-      [&](int stage) {
-        const uint32_t pa = a.at(lds + stage * kStage), pb = b.at(lds + stage * kStage + kA);
-#pragma unroll
-        for (int s = 0; s < kStep / 16; ++s) {
-          u32x4 oa[TN];
-#pragma unroll
-          for (int i = 0; i < TN; ++i) oa[i] = a.operand(pa, wn * TN + i, s);
-#pragma unroll
-          for (int j = 0; j < TM; ++j) {
-            const u32x4 ob = b.operand(pb, wm * TM + j, s);
-#pragma unroll
-            for (int i = 0; i < TN; ++i) acc[i][j] = T::mfma(oa[i], ob, acc[i][j]);
-          }
-        }
-      });
+      [&](int stage, int i) {
+        if (i < ASide::kCopies) a.copy(i, on, k0, p.k, lds + stage * kStage);
+        else b.copy(i - ASide::kCopies, on, k0, p.k, lds + stage * kStage + kA);
+      },
+      [&](int stage, int s, int i, Operands &o) {
+        if (i < TN) o.a[i] = a.operand(a.at(lds + stage * kStage), wn * TN + i, s);
+        else o.b[i - TN] = b.operand(b.at(lds + stage * kStage + kA), wm * TM + i - TN, s);
+      },
+      [&](const Operands &o, int i) {
+        acc[i / TN][i % TN] = T::mfma(o.a[i % TN], o.b[i / TN], acc[i / TN][i % TN]);
+      },
+      [](int64_t, int) {});
+  typedef Exchange<TN> Swap;
+  static_assert(2 * kStage >= W * Swap::kBytes);
+  const Swap swap = {lds + wave * Swap::kBytes, lane};
+  const int64_t n = n0 + wn * (BN / WN);
+  __syncthreads();                       // (all of the block's operands have been read)
 #pragma unroll
   for (int j = 0; j < TM; ++j) {
-    const int64_t row = m0 + wm * (BM / WM) + 32 * j + (lane & 31);
-    const bool ok = row < p.m;
+    const int64_t row = m0 + wm * (BM / WM) + 32 * j;
+    if (p.splits == 1) {
+      swap.template put_all<T>(acc[j]);
+      __builtin_amdgcn_wave_barrier();
+      swap.store(p.out[output] + row * p.out_row[output] + 2 * n, p.out_row[output], p.m - row,
+                 2 * (p.n - n));
+      __builtin_amdgcn_wave_barrier();
+    } else if (row + (lane & 31) < p.m) {
+      float *to = p.part + (((int64_t)output * p.splits + split) * p.m + row + (lane & 31)) * p.n + n;
 #pragma unroll
-    for (int i = 0; i < TN; ++i) {
-      const int64_t n = n0 + wn * (BN / WN) + 32 * i;
-      if (p.splits == 1) {
-        store_row<T, 1>(p.out[output] + row * p.out_row[output] + 2 * n, ok,
-                        (int)min((int64_t)64, 2 * (p.n - n)), &acc[i][j], 1.f, lane);
-      } else {
-        float *to = p.part + (((int64_t)output * p.splits + split) * p.m + row) * p.n + n;
+      for (int i = 0; i < TN; ++i)
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
-          const int off = 8 * q + 4 * (lane >> 5);
-          if (ok && n + off < p.n)
+          const int off = 32 * i + 8 * q + 4 * (lane >> 5);
+          if (n + off < p.n)
             *reinterpret_cast<f32x4 *>(to + off) =
-                f32x4{acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]};
+                f32x4{acc[j][i][4 * q], acc[j][i][4 * q + 1], acc[j][i][4 * q + 2], acc[j][i][4 * q + 3]};
         }
-      }
     }
   }
 }
@@ -364,20 +542,20 @@ bool use_big(int64_t m, int64_t n, int outputs) {
 
 template <class T, int BM, int BN, int WM, int WN, int ACT, bool GRAD>
 hipError_t launch_projections(const GatedGradArgs &g, char *dg, char *du, hipStream_t s) {
-  constexpr int kLds = 2 * (BM + BN) * kStepBytes;
+  constexpr int kLds = 2 * (BM + BN) * kStepBytes, kResident = kLdsBytes / kLds * kSeqCus;
   static LdsLimit limit;
   const void *f = reinterpret_cast<const void *>(gated_kernel<T, BM, BN, WM, WN, ACT, GRAD>);
   const hipError_t e = limit.set(f, kLds);
   if (e != hipSuccess) return e;
   const int nm = (int)tiles(g.f.rows, BM), nn = (int)tiles(g.f.hidden, BN / 2);
   gated_kernel<T, BM, BN, WM, WN, ACT, GRAD>
-      <<<(unsigned)(nm * nn), 64 * WM * WN, kLds, s>>>(g, dg, du, nm, nn);
+      <<<(unsigned)std::min(nm * nn, kResident), 64 * WM * WN, kLds, s>>>(g, dg, du, nm, nn);
   return hipGetLastError();
 }
 template <class T, int ACT, bool GRAD>
 hipError_t projections(const GatedGradArgs &g, char *dg, char *du, hipStream_t s) {
   if (use_big(g.f.rows, 2 * (int64_t)g.f.hidden, 1))
-    return launch_projections<T, 256, 256, 2, 4, ACT, GRAD>(g, dg, du, s);
+    return launch_projections<T, 256, 256, 4, 2, ACT, GRAD>(g, dg, du, s);
   return launch_projections<T, 128, 128, 2, 2, ACT, GRAD>(g, dg, du, s);
 }
 template <bool GRAD>
