@@ -425,7 +425,7 @@ struct ProductArgs {
 };
 
 template <class T, int BM, int BN, int WM, int WN, bool B_COL, int SEGMENTS>
-__global__ __launch_bounds__(64 * WM * WN, 2) void product_kernel(ProductArgs p) {
+__device__ inline void product_tile(const ProductArgs &p, unsigned block) {
   constexpr int W = WM * WN, TM = BM / 32 / WM, TN = BN / 32 / WN;
   extern __shared__ char stages[];
   constexpr int kStage = (BM + BN) * kStepBytes, kA = BN * kStepBytes;
@@ -433,12 +433,13 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void product_kernel(ProductArgs p)
   typedef Side<B_COL, BM, W> BSide;
   const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6);
   const int wm = wave / WN, wn = wave % WN;
-  const int output = blockIdx.y, split = blockIdx.z;
-  const Tile t = tile_of(blockIdx.x, gridDim.x, p.nm, p.nn);
+  const unsigned all = (unsigned)p.nm * p.nn;
+  const int part = (int)(block / all), output = part / p.splits, split = part % p.splits;
+  const Tile t = tile_of(block - part * all, all, p.nm, p.nn);
   const int64_t m0 = (int64_t)t.m * BM, n0 = (int64_t)t.n * BN;
-  const int per = (int)((p.k + kStep - 1) / kStep), all = per * SEGMENTS;
-  const int first = (int)((int64_t)all * split / p.splits);
-  const int end = (int)((int64_t)all * (split + 1) / p.splits);
+  const int per = (int)((p.k + kStep - 1) / kStep), steps = per * SEGMENTS;
+  const int first = (int)((int64_t)steps * split / p.splits);
+  const int end = (int)((int64_t)steps * (split + 1) / p.splits);
   const int skew = !B_COL && end > first ? t.m % (end - first) : 0;
   ASide a;
   BSide b;
@@ -515,20 +516,33 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void product_kernel(ProductArgs p)
   }
 }
 
-// out = the sum of the splits' parts, 8 values a thread.
+// All three products in one launch, so that one kind's tiles fill up the places that the other's leave:
+// first the `head` blocks of the kind with the longer tiles.
+template <class T, int BM, int BN, int WM, int WN>
+__global__ __launch_bounds__(64 * WM * WN, 2) void products_kernel(ProductArgs x, ProductArgs w, int head,
+                                                                bool x_first) {
+  const bool front = (int)blockIdx.x < head;
+  const unsigned block = front ? blockIdx.x : blockIdx.x - head;
+  if (front == x_first) product_tile<T, BM, BN, WM, WN, false, 2>(x, block);
+  else product_tile<T, BM, BN, WM, WN, true, 1>(w, block);
+}
+
+// out = the sum of the splits' parts, 8 values a thread: dx, dWg and dWu in turn (blockIdx.y).
 template <class T>
-__global__ __launch_bounds__(256) void product_add(ProductArgs p) {
+__global__ __launch_bounds__(256) void product_add(ProductArgs x, ProductArgs w) {
+  const ProductArgs &p = blockIdx.y ? w : x;
+  const int output = blockIdx.y ? blockIdx.y - 1 : 0;
   const int64_t i = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 8, size = p.m * p.n;
-  if (i >= size) return;
-  const float *from = p.part + (int64_t)blockIdx.y * p.splits * size + i;
-  f32x4 x = *reinterpret_cast<const f32x4 *>(from), y = *reinterpret_cast<const f32x4 *>(from + 4);
+  if (i >= size || p.splits == 1) return;
+  const float *from = p.part + (int64_t)output * p.splits * size + i;
+  f32x4 u = *reinterpret_cast<const f32x4 *>(from), v = *reinterpret_cast<const f32x4 *>(from + 4);
   for (int s = 1; s < p.splits; ++s) {
     const f32x4 *q = reinterpret_cast<const f32x4 *>(from + s * size);
-    x += q[0], y += q[1];
+    u += q[0], v += q[1];
   }
   const int64_t row = i / p.n;
-  *reinterpret_cast<u32x4 *>(p.out[blockIdx.y] + row * p.out_row[blockIdx.y] + 2 * (i - row * p.n)) =
-      u32x4{T::pack(x[0], x[1]), T::pack(x[2], x[3]), T::pack(y[0], y[1]), T::pack(y[2], y[3])};
+  *reinterpret_cast<u32x4 *>(p.out[output] + row * p.out_row[output] + 2 * (i - row * p.n)) =
+      u32x4{T::pack(u[0], u[1]), T::pack(u[2], u[3]), T::pack(v[0], v[1]), T::pack(v[2], v[3])};
 }
 
 // ------------------------------------------------------------------ launches
@@ -536,9 +550,7 @@ int64_t tiles(int64_t n, int size) { return (n + size - 1) / size; }
 size_t align256(size_t n) { return (n + 255) & ~(size_t)255; }
 
 // Tiles of 256 x 256 where they fill the device, else of 128 x 128.
-bool use_big(int64_t m, int64_t n, int outputs) {
-  return tiles(m, 256) * tiles(n, 256) * outputs >= kSeqCus;
-}
+bool use_big(int64_t rows, int64_t hidden) { return tiles(rows, 256) * tiles(hidden, 128) >= kSeqCus; }
 
 template <class T, int BM, int BN, int WM, int WN, int ACT, bool GRAD>
 hipError_t launch_projections(const GatedGradArgs &g, char *dg, char *du, hipStream_t s) {
@@ -554,7 +566,7 @@ hipError_t launch_projections(const GatedGradArgs &g, char *dg, char *du, hipStr
 }
 template <class T, int ACT, bool GRAD>
 hipError_t projections(const GatedGradArgs &g, char *dg, char *du, hipStream_t s) {
-  if (use_big(g.f.rows, 2 * (int64_t)g.f.hidden, 1))
+  if (use_big(g.f.rows, g.f.hidden))
     return launch_projections<T, 256, 256, 4, 2, ACT, GRAD>(g, dg, du, s);
   return launch_projections<T, 128, 128, 2, 2, ACT, GRAD>(g, dg, du, s);
 }
@@ -567,62 +579,77 @@ hipError_t by_type(const GatedGradArgs &g, char *dg, char *du, hipStream_t s) {
                           : projections<Bf16, kGelu, GRAD>(g, dg, du, s);
 }
 
-// Parts of the summed axis (`steps` of it): so many that the tiles fill the device, each of 8
-// steps at least.
-int splits_of(int64_t m, int64_t n, int outputs, int64_t steps) {
-  const bool big = use_big(m, n, outputs);
+// The products' tiles, and the parts of their summed axes.
+struct Plan {
+  bool big;
+  int sx, sw;                          // parts of dx's and of dW's summed axis
+  int64_t nx, nw, lx, lw;              // blocks, and a block's steps
+};
+constexpr int kLeast = 8;              // steps of a part at least
+Plan plan_of(int64_t rows, int64_t width, int64_t hidden, bool big) {
   const int size = big ? 256 : 128;
-  const int64_t have = tiles(m, size) * tiles(n, size) * outputs, want = big ? kSeqCus : 2 * kSeqCus;
-  return (int)std::max<int64_t>(1, std::min<int64_t>(want / std::max<int64_t>(have, 1), steps / 8));
+  const int64_t tx = tiles(rows, size) * tiles(width, size), tw = 2 * tiles(hidden, size) * tiles(width, size);
+  const int64_t lx = 2 * tiles(hidden, kStep), lw = tiles(rows, kStep);
+  // a resident block's share of all steps: longer summed axes are split
+  const int64_t share = std::max<int64_t>(kLeast, tiles(tx * lx + tw * lw, big ? kSeqCus : 2 * kSeqCus));
+  Plan p;
+  p.big = big;
+  p.sx = (int)std::max<int64_t>(1, lx / share), p.sw = (int)std::max<int64_t>(1, lw / share);
+  p.nx = tx * p.sx, p.nw = tw * p.sw;
+  p.lx = tiles(lx, p.sx), p.lw = tiles(lw, p.sw);
+  return p;
 }
-int splits_dx(int64_t rows, int64_t width, int64_t hidden) {
-  return splits_of(rows, width, 1, 2 * tiles(hidden, kStep));
+// By the time of a step of either size, measured with full tiles: 1.8 us of 256 x 256, one block a compute
+// unit; 1.2 of 128 x 128, two.
+Plan plan_of(int64_t rows, int64_t width, int64_t hidden) {
+  const Plan a = plan_of(rows, width, hidden, true), b = plan_of(rows, width, hidden, false);
+  auto time = [](const Plan &p, double step, int places) {
+    return step * std::max<double>((double)std::max(p.lx, p.lw), (double)(p.nx * p.lx + p.nw * p.lw) / places);
+  };
+  return time(a, 1.8, kSeqCus) <= time(b, 1.2, 2 * kSeqCus) ? a : b;
 }
-int splits_dw(int64_t rows, int64_t width, int64_t hidden) {
-  return splits_of(hidden, width, 2, tiles(rows, kStep));
+size_t part_bytes(const Plan &p, int64_t rows, int64_t width, int64_t hidden, bool x) {
+  if (x) return p.sx > 1 ? align256((size_t)p.sx * rows * width * 4) : 0;
+  return p.sw > 1 ? align256((size_t)2 * p.sw * hidden * width * 4) : 0;
 }
 
-template <class T, int BM, int BN, int WM, int WN, bool B_COL, int SEGMENTS>
-hipError_t launch_product(ProductArgs p, hipStream_t s) {
-  constexpr int kLds = 2 * (BM + BN) * kStepBytes, kOutputs = SEGMENTS == 2 ? 1 : 2;
+template <class T, int BM, int BN, int WM, int WN>
+hipError_t launch_products(ProductArgs x, ProductArgs w, const Plan &plan, hipStream_t s) {
+  constexpr int kLds = 2 * (BM + BN) * kStepBytes;
   static LdsLimit limit;
-  const void *f = reinterpret_cast<const void *>(product_kernel<T, BM, BN, WM, WN, B_COL, SEGMENTS>);
+  const void *f = reinterpret_cast<const void *>(products_kernel<T, BM, BN, WM, WN>);
   hipError_t e = limit.set(f, kLds);
   if (e != hipSuccess) return e;
-  p.nm = (int)tiles(p.m, BM), p.nn = (int)tiles(p.n, BN);
-  product_kernel<T, BM, BN, WM, WN, B_COL, SEGMENTS>
-      <<<dim3((unsigned)(p.nm * p.nn), kOutputs, p.splits), 64 * WM * WN, kLds, s>>>(p);
+  for (ProductArgs *p : {&x, &w}) p->nm = (int)tiles(p->m, BM), p->nn = (int)tiles(p->n, BN);
+  const bool x_first = plan.lx > plan.lw;
+  products_kernel<T, BM, BN, WM, WN><<<(unsigned)(plan.nx + plan.nw), 64 * WM * WN, kLds, s>>>(
+      x, w, (int)(x_first ? plan.nx : plan.nw), x_first);
   e = hipGetLastError();
-  if (e != hipSuccess || p.splits == 1) return e;
-  product_add<T><<<dim3((unsigned)tiles(p.m * p.n, 256 * 8), kOutputs), 256, 0, s>>>(p);
+  if (e != hipSuccess || (x.splits == 1 && w.splits == 1)) return e;
+  const int64_t most = std::max(x.splits > 1 ? x.m * x.n : 0, w.splits > 1 ? w.m * w.n : 0);
+  product_add<T><<<dim3((unsigned)tiles(most, 256 * 8), 3), 256, 0, s>>>(x, w);
   return hipGetLastError();
-}
-template <class T, bool B_COL, int SEGMENTS>
-hipError_t product(const ProductArgs &p, hipStream_t s) {
-  if (use_big(p.m, p.n, SEGMENTS == 2 ? 1 : 2))
-    return launch_product<T, 256, 256, 2, 4, B_COL, SEGMENTS>(p, s);
-  return launch_product<T, 128, 128, 2, 2, B_COL, SEGMENTS>(p, s);
 }
 
 template <class T>
 hipError_t gradient(const GatedGradArgs &g, char *ws, hipStream_t s) {
   const GatedArgs &f = g.f;
+  const Plan plan = plan_of(f.rows, f.width, f.hidden);
   const size_t hidden_bytes = align256((size_t)f.rows * f.hidden * 2);
   char *dg = ws, *du = ws + hidden_bytes;
-  float *part = reinterpret_cast<float *>(ws + 2 * hidden_bytes);
+  float *px = reinterpret_cast<float *>(ws + 2 * hidden_bytes);
+  float *pw = reinterpret_cast<float *>(ws + 2 * hidden_bytes + part_bytes(plan, f.rows, f.width, f.hidden, true));
   const int64_t row = (int64_t)f.hidden * 2;
-  hipError_t e;
   if (f.rows > 0) {
-    if ((e = by_type<true>(g, dg, du, s)) != hipSuccess) return e;
-    ProductArgs x = {{f.w_gate, f.w_up}, {dg, du}, {f.gate_row, f.up_row}, {row, row}, {g.dx, nullptr},
-                     {g.dx_row, 0}, part, f.rows, f.width, f.hidden, 0, 0,
-                     splits_dx(f.rows, f.width, f.hidden)};
-    if ((e = product<T, false, 2>(x, s)) != hipSuccess) return e;
+    const hipError_t e = by_type<true>(g, dg, du, s);
+    if (e != hipSuccess) return e;
   }
-  ProductArgs w = {{f.x, f.x}, {dg, du}, {f.x_row, f.x_row}, {row, row}, {g.dw_gate, g.dw_up},
-                   {g.dgate_row, g.dup_row}, part, f.hidden, f.width, f.rows, 0, 0,
-                   splits_dw(f.rows, f.width, f.hidden)};
-  return product<T, true, 1>(w, s);
+  const ProductArgs x = {{f.w_gate, f.w_up}, {dg, du}, {f.gate_row, f.up_row}, {row, row}, {g.dx, nullptr},
+                         {g.dx_row, 0}, px, f.rows, f.width, f.hidden, 0, 0, plan.sx};
+  const ProductArgs w = {{f.x, f.x}, {dg, du}, {f.x_row, f.x_row}, {row, row}, {g.dw_gate, g.dw_up},
+                         {g.dgate_row, g.dup_row}, pw, f.hidden, f.width, f.rows, 0, 0, plan.sw};
+  return plan.big ? launch_products<T, 256, 256, 2, 4>(x, w, plan, s)
+                  : launch_products<T, 128, 128, 2, 2>(x, w, plan, s);
 }
 
 }  // namespace
@@ -635,21 +662,20 @@ hipError_t launch_gated(const GatedArgs &a, hipStream_t s) {
 }
 
 bool gated_fits(int64_t rows, int64_t width, int64_t hidden, bool grad) {
-  // (the smallest tiles; at most 512 threads a block)
+  // (at most 512 threads a block)
   constexpr int64_t kMost = kMaxBlocks / 2;
   bool ok = tiles(rows, 128) * tiles(hidden, 64) <= kMost;
-  if (grad)
-    ok = ok && tiles(rows, 128) * tiles(width, 128) <= kMost &&
-         tiles(hidden, 128) * tiles(width, 128) * 2 <= kMost &&
-         tiles(std::max(rows, hidden) * width, 256 * 8) <= kMost;
+  if (grad && ok) {
+    const Plan a = plan_of(rows, width, hidden);
+    ok = a.nx + a.nw <= kMost && tiles(std::max(rows, hidden) * width, 256 * 8) <= kMost;
+  }
   return ok;
 }
 
 size_t gated_grad_bytes(int32_t rows, int32_t width, int32_t hidden) {
-  const int sx = splits_dx(rows, width, hidden), sw = splits_dw(rows, width, hidden);
-  const size_t px = sx > 1 ? (size_t)sx * rows * width * 4 : 0;
-  const size_t pw = sw > 1 ? (size_t)2 * sw * hidden * width * 4 : 0;
-  return 2 * align256((size_t)rows * hidden * 2) + align256(std::max(px, pw));
+  const Plan p = plan_of(rows, width, hidden);
+  return 2 * align256((size_t)rows * hidden * 2) + part_bytes(p, rows, width, hidden, true) +
+         part_bytes(p, rows, width, hidden, false);
 }
 
 hipError_t launch_gated_grad(const GatedGradArgs &g, void *ws, hipStream_t s) {
