@@ -410,6 +410,87 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void gated_kernel(GatedGradArgs g,
       });
 }
 
+// ------------------------------------------------------------------ few rows
+// Both projections of up to 16 N rows a block: what counts is that the weights stream in. A block has 16
+// hidden values; its wavefronts split the summed axis, each with four times 32 of it on its way at once,
+// straight into the matrix units' registers, and are added up in LDS in order.
+constexpr int kFewWaves = 8;
+
+template <class T>
+__device__ inline f32x4 mfma16(u32x4 a, u32x4 b, f32x4 c);
+template <>
+__device__ inline f32x4 mfma16<Bf16>(u32x4 a, u32x4 b, f32x4 c) {
+  return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b),
+                                                 c, 0, 0, 0);
+}
+template <>
+__device__ inline f32x4 mfma16<Fp16>(u32x4 a, u32x4 b, f32x4 c) {
+  return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c,
+                                                0, 0, 0);
+}
+
+template <class T, int N, int ACT>
+__global__ __launch_bounds__(64 * kFewWaves) void gated_few(GatedArgs a) {
+  constexpr int kUnroll = 4;
+  // A lane has row lane % 16 of an operand, values 8 (lane / 16) .. of 32, and of a result row
+  // (hidden value) 4 (lane / 16) + 0..3 and column (row of x) lane % 16.
+  __shared__ f32x4 sums[kFewWaves][2 * N][64];
+  const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6);
+  const int64_t n0 = (int64_t)blockIdx.x * 16, m0 = (int64_t)blockIdx.y * (16 * N);
+  const int r = lane & 15, off = (lane >> 4) * 16;
+  const int chunks = (a.width + 31) / 32, per = (chunks + kFewWaves - 1) / kFewWaves;
+  const int first = wave * per, end = min(first + per, chunks);
+  const int64_t n = min(n0 + r, (int64_t)a.hidden - 1);   // (results past the last are not stored)
+  const char *src[2 + N];
+  src[0] = a.w_gate + n * a.gate_row + off;
+  src[1] = a.w_up + n * a.up_row + off;
+#pragma unroll
+  for (int j = 0; j < N; ++j) src[2 + j] = a.x + min(m0 + 16 * j + r, (int64_t)a.rows - 1) * a.x_row + off;
+  f32x4 acc[2][N];
+#pragma unroll
+  for (int j = 0; j < N; ++j) acc[0][j] = acc[1][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+  for (int c = first; c < end; c += kUnroll) {
+    u32x4 v[kUnroll][2 + N];
+#pragma unroll
+    for (int u = 0; u < kUnroll; ++u) {
+      const bool in = c + u < end && (c + u) * 64 + off < 2 * a.width;
+#pragma unroll
+      for (int i = 0; i < 2 + N; ++i) {
+        v[u][i] = u32x4{0, 0, 0, 0};
+        if (in) v[u][i] = *reinterpret_cast<const u32x4 *>(src[i] + (int64_t)(c + u) * 64);
+      }
+    }
+#pragma unroll
+    for (int u = 0; u < kUnroll; ++u)
+#pragma unroll
+      for (int j = 0; j < N; ++j) {
+        acc[0][j] = mfma16<T>(v[u][0], v[u][2 + j], acc[0][j]);
+        acc[1][j] = mfma16<T>(v[u][1], v[u][2 + j], acc[1][j]);
+      }
+  }
+#pragma unroll
+  for (int i = 0; i < 2; ++i)
+#pragma unroll
+    for (int j = 0; j < N; ++j) sums[wave][i * N + j][lane] = acc[i][j];
+  __syncthreads();
+  // a wavefront joins 16 rows of x
+  for (int j = wave; j < N; j += kFewWaves) {
+    f32x4 g = sums[0][j][lane], u = sums[0][N + j][lane];
+#pragma unroll
+    for (int w = 1; w < kFewWaves; ++w) g += sums[w][j][lane], u += sums[w][N + j][lane];
+    float f[4], d;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      activation<ACT>(g[i], f[i], d);
+      f[i] *= u[i];
+    }
+    const int64_t row = m0 + 16 * j + r, to = n0 + 4 * (lane >> 4);
+    if (row < a.rows && to < a.hidden)
+      *reinterpret_cast<u32x2 *>(a.out + row * a.out_row + 2 * to) =
+          u32x2{T::pack(f[0], f[1]), T::pack(f[2], f[3])};
+  }
+}
+
 // ------------------------------------------------------------------ the gradient's products
 // out[m][n] = sum over k of B(m, k) A(n, k), A in COL form.
 // SEGMENTS 2: one output, the summed axis in two segments of k each with operands of their own
@@ -564,8 +645,25 @@ hipError_t launch_projections(const GatedGradArgs &g, char *dg, char *du, hipStr
       <<<(unsigned)std::min(nm * nn, kResident), 64 * WM * WN, kLds, s>>>(g, dg, du, nm, nn);
   return hipGetLastError();
 }
+// Whether the weights stream past the rows: up to 32 rows, and more where a block for each 16 hidden values and
+// 64 rows has a compute unit of its own. Measured, us, this form and tiles: 16 rows of 1,024 x 4,096 6.1 and
+// 13.1, 64 rows 9.2 and 13.2, 96 rows (512 blocks) 13.9 and 13.3; 256 rows of 4,096 x 1,024 24.8 and 42.1, of
+// 256 x 1,024 4.6 and 6.0; of 2,048 x 8,192 32 rows 18.5 and 25.2, 64 rows (512 blocks) 26.8 and 25.4.
+bool use_few(int64_t rows, int64_t hidden) {
+  return rows <= 32 || tiles(hidden, 16) * tiles(rows, 64) <= kSeqCus;
+}
+template <class T, int N, int ACT>
+hipError_t launch_few(const GatedArgs &a, hipStream_t s) {
+  gated_few<T, N, ACT><<<dim3((unsigned)tiles(a.hidden, 16), (unsigned)tiles(a.rows, 16 * N)), 64 * kFewWaves, 0, s>>>(a);
+  return hipGetLastError();
+}
 template <class T, int ACT, bool GRAD>
 hipError_t projections(const GatedGradArgs &g, char *dg, char *du, hipStream_t s) {
+  if (!GRAD && use_few(g.f.rows, g.f.hidden)) {
+    if (g.f.rows <= 16) return launch_few<T, 1, ACT>(g.f, s);
+    if (g.f.rows <= 32) return launch_few<T, 2, ACT>(g.f, s);
+    return launch_few<T, 4, ACT>(g.f, s);
+  }
   if (use_big(g.f.rows, g.f.hidden))
     return launch_projections<T, 256, 256, 4, 2, ACT, GRAD>(g, dg, du, s);
   return launch_projections<T, 128, 128, 2, 2, ACT, GRAD>(g, dg, du, s);
