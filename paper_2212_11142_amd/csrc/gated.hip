@@ -109,7 +109,8 @@ struct Side<true, R, WAVES> {
 // Runs `count` steps, each 4 times 16 of the summed axis: after begin(step), called for one step after
 // the other and for two past the last, copy(stage, i) is the i-th of a wavefront's COPIES copies,
 // read(stage, s, i, operands) fetches the i-th of a quarter's READS operands, multiply(operands, i) is
-// the i-th of its MFMAS products, and end(step, stage) follows a step's products.
+// the i-th of its MFMAS products, and end(step, stage) follows a step's products and says whether it did
+// anything.
 //
 // A quarter's operands are read while the one before is multiplied. The block meets in front of a step's
 // last quarter, whose operands are in registers then: behind that barrier the next step's copies are
@@ -153,7 +154,10 @@ __device__ inline void run_steps(int64_t count, Begin begin, Copy copy, Read rea
     begin(i + 2);
     copies_barrier();
     quarter(g, f, stage ^ 1, 0, stage, 0);
-    end(i, stage);
+    // (operands read already do not stay in registers beside what end() does)
+    if (end(i, stage))
+#pragma unroll
+      for (int r = 0; r < READS; ++r) read(stage ^ 1, 0, r, f);
   }
   // (what was asked for past the end: a block's place in LDS ends with it)
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
@@ -342,7 +346,7 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void gated_kernel(GatedGradArgs g,
         acc[j][q][c] = T::mfma(o.w[q][c], o.x[j], acc[j][q][c]);
       },
       [&](int64_t, int stage) {
-        if (--left) return;
+        if (--left) return false;
         left = steps;
         // (x's part of the stage: its copies go out last, after the block has met)
         const Swap swap = {lds + stage * kStage + 2 * kHalf + wave * Swap::kBytes, lane};
@@ -369,7 +373,7 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void gated_kernel(GatedGradArgs g,
             for (int c = 0; c < C; ++c)
 #pragma unroll
               for (int q = 0; q < 4; ++q) {
-                if (q % 2 == 0) __builtin_amdgcn_sched_barrier(0);
+                __builtin_amdgcn_sched_barrier(0);       // (a few at a time: registers)
                 const u32x2 w = swap.get(c, q);
                 const uint32_t w0 = w[0], w1 = w[1];
                 const float y[4] = {T::lo(w0), T::hi(w0), T::lo(w1), T::hi(w1)};
@@ -407,6 +411,7 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void gated_kernel(GatedGradArgs g,
         }
         clear();
         asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+        return true;
       });
 }
 
@@ -567,7 +572,7 @@ __device__ inline void product_tile(const ProductArgs &p, unsigned block) {
       [&](const Operands &o, int i) {
         acc[i / TN][i % TN] = T::mfma(o.a[i % TN], o.b[i / TN], acc[i / TN][i % TN]);
       },
-      [](int64_t, int) {});
+      [](int64_t, int) { return false; });
   typedef Exchange<TN> Swap;
   static_assert(2 * kStage >= W * Swap::kBytes);
   const Swap swap = {lds + wave * Swap::kBytes, lane};
