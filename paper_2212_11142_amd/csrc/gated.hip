@@ -306,7 +306,7 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void gated_kernel(GatedGradArgs g,
   const int steps = (a.width + kStep - 1) / kStep;
   // a tile's steps follow those of the block's tile before without a pause. Each row of tiles starts at
   // another step: rows a power of two apart meet in few of the L2's channels
-  unsigned index = blockIdx.x;           // of next
+  unsigned index = blockIdx.x, current = blockIdx.x;       // of next and of t (two tiles apart, with one step a tile)
   int step = -1, left = steps;           // of next's, the one whose operands are copied; those left of t's
   int64_t k0 = 0;
   bool on = true;
@@ -352,7 +352,8 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void gated_kernel(GatedGradArgs g,
         const Swap swap = {lds + stage * kStage + 2 * kHalf + wave * Swap::kBytes, lane};
         const int64_t n = (int64_t)t.n * (BN / 2) + 32 * C * wn, bytes = 2 * (a.hidden - n);
         const int64_t row0 = (int64_t)t.m * BM + wm * (BM / WM);
-        t = next;
+        current += gridDim.x;
+        if (current < all) t = tile_of(current, all, nm, nn);
 #pragma unroll
         for (int j = 0; j < TM; ++j) {
           const int64_t row = row0 + 32 * j, rows = a.rows - row;

@@ -338,7 +338,8 @@ gp_status gp_adamw(const gp_adamw_spec *t, int32_t count, const gp_adamw_tensor 
     if (t->state_bits != 8 && t->state_bits != 32) return unsupported("states have 8 or 32 bits");
     if (!(t->beta1 >= 0. && t->beta1 < 1. && t->beta2 >= 0. && t->beta2 < 1.))
       return bad("beta1 and beta2 must be in 0..1, below 1");
-    if (!(t->eps > 0.) || !std::isfinite(t->eps)) return bad("eps must be finite and > 0");
+    // (in fp32, as the kernels take it)
+    if (!((float)t->eps > 0.f) || !std::isfinite((float)t->eps)) return bad("eps must be finite and > 0 in fp32");
     if (!std::isfinite(t->decay)) return bad("decay must be finite");
     if (!t->lr_device && !std::isfinite(t->lr)) return bad("lr must be finite");
     if (!t->step_device && t->step < 1) return bad("step must be >= 1");

@@ -306,29 +306,40 @@ def test_gated_strides(rows, width, hidden, dtype, kind):
     run_gated(rows, width, hidden, dtype, kind, pad=8)
 
 
-def test_gated_large_tiles():
-    """Sizes of the larger tiles, with ragged edges in every direction; the sums' errors together, against
-    what rounding the results alone takes (1.5 of it: one more rounding of the operands)."""
-    rows, width, hidden = 2100, 2120, 2200
-    for dtype in (BF, FP):
-        g = gen(1)
-        x = rand(g, rows, width, dtype=dtype)
-        wg, wu = (rand(g, hidden, width, dtype=dtype, scale=width ** -0.5) for _ in range(2))
-        dout = rand(g, rows, hidden, dtype=dtype)
-        t = layers.Gated(width, hidden, dtype)
-        b = layers.GatedBuffers(t, rows, grad=True)
-        layers.gated_into(t, x, wg, wu, b)
-        layers.gated_grad_into(t, x, wg, wu, dout, b)
-        X, A, B, D = (v.double() for v in (x, wg, wu, dout))
-        G, U = X @ A.t(), X @ B.t()
-        p = torch.sigmoid(G)
-        dg, du = D * U * p * (1 + G * (1 - p)), D * G * p
-        for got, want, k in ((b.out, G * p * U, 1.0), (b.dx, dg @ A + du @ B, 1.5), (b.dw_gate, dg.t() @ X, 1.5),
-                             (b.dw_up, du.t() @ X, 1.5)):
-            alone = (want.to(dtype).double() - want).norm()
-            assert (got.double() - want).norm() <= 1.02 * k * alone
-            # each value: a hundred standard deviations of a sum's errors would not reach this
-            assert (got.double() - want).abs().max() <= 8 * HALF[dtype] * want.abs().max()
+@pytest.mark.parametrize("rows,width,hidden,kind", [
+    (2100, 2120, 2200, "silu"),            # larger tiles, ragged in every direction
+    (8100, 1016, 1032, "gelu"),            # ... the weights' gradients in parts
+    (520, 2056, 8200, "silu"),             # ... dx in parts
+    (4090, 72, 1904, "gelu"),              # smaller tiles, more than are resident at once
+    (20000, 56, 1032, "silu"),             # a tile a step, several tiles a block
+    (30000, 120, 776, "gelu"),             # ... two steps
+    (17000, 200, 2056, "silu"),            # ... four
+    (1000, 520, 1368, "silu")])            # ... every sum in parts
+@pytest.mark.parametrize("dtype", [BF, FP])
+def test_gated_tiles(dtype, rows, width, hidden, kind):
+    """The sums' errors together, against what rounding the results alone takes: the forward pass adds
+    fp32's, the gradient one more rounding of its operands, independent of the results': sqrt(2) of it, taken
+    as 1.5."""
+    g = gen(1)
+    x = rand(g, rows, width, dtype=dtype)
+    wg, wu = (rand(g, hidden, width, dtype=dtype, scale=width ** -0.5) for _ in range(2))
+    dout = rand(g, rows, hidden, dtype=dtype)
+    t = layers.Gated(width, hidden, dtype, activation=kind)
+    b = layers.GatedBuffers(t, rows, grad=True)
+    layers.gated_into(t, x, wg, wu, b)
+    layers.gated_grad_into(t, x, wg, wu, dout, b)
+    X, A, B, D = (v.double() for v in (x, wg, wu, dout))
+    G, U = X @ A.t(), X @ B.t()
+    p = torch.sigmoid(G) if kind == "silu" else torch.special.ndtr(G)
+    d = p * (1 + G * (1 - p)) if kind == "silu" else p + G * torch.exp(-G * G / 2) / (2 * np.pi) ** 0.5
+    dg, du = D * U * d, D * G * p
+    for got, want, k in ((b.out, G * p * U, 1.0), (b.dx, dg @ A + du @ B, 1.5), (b.dw_gate, dg.t() @ X, 1.5),
+                         (b.dw_up, du.t() @ X, 1.5)):
+        alone = (want.to(dtype).double() - want).norm()
+        assert (got.double() - want).norm() <= 1.02 * k * alone
+        # each value: the operands' roundings are off by half a step of each of some hundred or thousand
+        # terms, independently: 8 half steps of the largest sum are over 20 standard deviations
+        assert (got.double() - want).abs().max() <= 8 * HALF[dtype] * want.abs().max()
 
 
 def test_gated_of_no_rows():

@@ -201,7 +201,7 @@ def call_adamw(lib, spec, count=1, grad=256, tensors=True, **kw):
 @pytest.mark.parametrize("kw,status", [
     (dict(dtype=3), INVALID), (dict(grad_dtype=1), UNSUPPORTED), (dict(dtype=2), UNSUPPORTED),
     (dict(state_bits=16), UNSUPPORTED), (dict(beta1=1.0), INVALID), (dict(beta2=-0.1), INVALID), (dict(beta1=NAN), INVALID),
-    (dict(eps=0.0), INVALID), (dict(eps=NAN), INVALID), (dict(decay=INF), INVALID), (dict(lr=NAN), INVALID),
+    (dict(eps=0.0), INVALID), (dict(eps=NAN), INVALID), (dict(eps=1e-60), INVALID), (dict(eps=1e60), INVALID), (dict(decay=INF), INVALID), (dict(lr=NAN), INVALID),
     (dict(step=0), INVALID), (dict(lr_device=258), INVALID), (dict(step_device=260), INVALID), (dict(factor=257), INVALID)])
 def test_adamw_descriptions_refused(lib, kw, status):
     assert call_adamw(lib, adamw(**kw)) == status
