@@ -238,10 +238,10 @@ struct Exchange {
 // ------------------------------------------------------------------ activations
 constexpr int kSilu = 0, kGelu = 1;   // GP_SILU, GP_GELU
 
-// act(z) and its derivative. gelu's normal distribution function is 1/2 erfc(-z / sqrt(2)), and
-// erfc(x) = e^(-x^2) t q(t), t = 1 / (1 + 0.375 x), for x >= 0, q a least-maximum fit of degree 6
-// with a relative error of 6.4e-7: the tail keeps its digits, and the derivative has the same
-// exponential.
+// act(z) and its derivative. gelu: z Phi(z), where
+// Phi(-|z|) = 1/2 erfc(|z| / sqrt(2)) = e^(-z^2 / 2) t q(t) / 2, t = 1 / (1 + 0.375 |z| / sqrt(2)), q a least-maximum
+// fit of degree 6 to e^(x^2) erfc(x) / t with a relative error of 6.4e-7: the tail keeps its digits, and the
+// derivative has the same exponential.
 template <int ACT>
 __device__ inline void activation(float z, float &a, float &d) {
   if (ACT == kSilu) {
@@ -249,17 +249,16 @@ __device__ inline void activation(float z, float &a, float &d) {
     a = z * p;
     d = p + a * (1.f - p);
   } else {
-    const float x = fabsf(z) * 0.70710678f;
-    const float t = __builtin_amdgcn_rcpf(fmaf(0.375f, x, 1.f));
-    float q = -0.13509515f;
-    q = fmaf(q, t, 0.38793566f);
-    q = fmaf(q, t, -0.12959506f);
-    q = fmaf(q, t, 0.28306065f);
-    q = fmaf(q, t, 0.16666456f);
-    q = fmaf(q, t, 0.21568926f);
-    q = fmaf(q, t, 0.21133943f);
+    const float t = __builtin_amdgcn_rcpf(fmaf(0.26516504f, fabsf(z), 1.f));
+    float q = -0.5f * 0.13509515f;
+    q = fmaf(q, t, 0.5f * 0.38793566f);
+    q = fmaf(q, t, -0.5f * 0.12959506f);
+    q = fmaf(q, t, 0.5f * 0.28306065f);
+    q = fmaf(q, t, 0.5f * 0.16666456f);
+    q = fmaf(q, t, 0.5f * 0.21568926f);
+    q = fmaf(q, t, 0.5f * 0.21133943f);
     const float e = fast_exp2(z * z * (-0.5f * kLog2e));
-    const float tail = 0.5f * e * t * q;
+    const float tail = e * (t * q);
     const float p = z < 0.f ? tail : 1.f - tail;
     a = z * p;
     d = fmaf(z * e, 0.39894228f, p);

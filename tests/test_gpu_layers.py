@@ -376,6 +376,21 @@ def test_activation_values(kind):
          + SMALL[FP], FP, "derivative")
 
 
+@pytest.mark.parametrize("kind", ["silu", "gelu"])
+@pytest.mark.parametrize("rows", [1, 200])
+def test_gated_values_that_are_not_finite(kind, rows):
+    """act(inf) = inf, act(NaN) = NaN, and what is finite beside them stays as it is."""
+    x = torch.zeros((rows, 8), dtype=BF, device="cuda")
+    w = torch.zeros((2, 8, 8), dtype=BF, device="cuda")
+    x[:, 0] = 1.0
+    w[0, :, 0] = torch.tensor([float("inf"), float("nan"), 3e38, -3e38, 2.0, -2.0, 0.0, -0.0])
+    w[1, :, 0] = 1.0
+    y = layers.gated(layers.Gated(8, 8, BF, activation=kind), x, w[0], w[1])[rows - 1]
+    assert y[0] == float("inf") and y[1].isnan() and y[2] == w[0, 2, 0] and y[3] == 0
+    want = ol.activation(np.array([2.0, -2.0, 0.0, 0.0]), kind)[0]
+    np.testing.assert_allclose(host(y[4:]), want, rtol=HALF[BF], atol=0)
+
+
 # ------------------------------------------------------------------ AdamW
 def weights(g, shapes, dtype, master):
     w = [rand(g, *s, scale=0.1) for s in shapes]
