@@ -11,15 +11,30 @@
 // random: an m below its smallest normal code goes to the nearest (a code taken by chance could be
 // thousands of times the value, over a root of v just as small), and a v above 0 stays above 0.
 //
-// Bound by memory: every value is read and written once. A wavefront has a block of 256 values,
-// four a lane; the tensors' table travels in the launch's arguments.
+// Bound by memory: every value is read and written once. A wavefront has 256 values, four a lane, or
+// with 8-bit states two blocks of 256, eight a lane (four a lane, 4 bytes of codes each: 233 us instead of
+// 228 for 63.5 M weights with master copies); the tensors' table travels in the launch's arguments.
 #include "layer_dev.h"
 
 namespace bgp {
 namespace {
 
-constexpr int kShare = 256;            // values that share a scale: a wavefront's
+constexpr int kShare = 256;            // values that share a scale
 constexpr int kWaves = 4;
+// Values of a lane.
+template <int BITS>
+constexpr int kLane = BITS == 8 ? 8 : 4;
+
+// Largest value of a lane's half wavefront.
+__device__ inline float half_max(float x) {
+  x = fmaxf(x, moved<0xb1>(x));
+  x = fmaxf(x, moved<0x4e>(x));
+  x = fmaxf(x, moved<0x141>(x));
+  x = fmaxf(x, moved<0x140>(x));
+  const uint32_t u = __builtin_bit_cast(uint32_t, x);
+  const u32x2 r = __builtin_amdgcn_permlane16_swap(u, u, false, false);
+  return fmaxf(word_float(r[0]), word_float(r[1]));
+}
 
 // What a step's number and rate give: the averages' corrections.
 __host__ __device__ inline AdamStep step_of(const AdamArgs &a, double t, double lr) {
@@ -82,57 +97,59 @@ __device__ inline float value_of(uint32_t code) {
   return (float)code * kStep;
 }
 
-template <class T>
-__device__ inline void load4(const void *p, int64_t i, bool whole, int left, float *v) {
-  if (whole) {
-    if constexpr (Piece<T>::kSize == 4) {
-      Piece<T>::unpack(*reinterpret_cast<const u32x4_any *>(static_cast<const float *>(p) + i), v);
-    } else {
-      typedef u32x2 __attribute__((aligned(2))) pair;
-      const u32x2 w = *reinterpret_cast<const pair *>(static_cast<const uint16_t *>(p) + i);
-      const uint32_t a = w[0], b = w[1];
-      v[0] = T::lo(a), v[1] = T::hi(a), v[2] = T::lo(b), v[3] = T::hi(b);
-    }
-  } else {
+// The N values (4 or 8) from i on, of which `left` are the tensor's.
+template <class T, int N>
+__device__ inline void load_values(const void *p, int64_t i, int left, float *v) {
+  const char *q = static_cast<const char *>(p) + i * Piece<T>::kSize;
+  if (left < N) {
 #pragma unroll
-    for (int k = 0; k < 4; ++k) v[k] = k < left ? T::load(p, i + k) : 0.f;
+    for (int k = 0; k < N; ++k) v[k] = k < left ? T::load(q, k) : 0.f;
+  } else if constexpr (Piece<T>::kV <= N) {
+#pragma unroll
+    for (int k = 0; k < N; k += Piece<T>::kV)
+      Piece<T>::unpack(*reinterpret_cast<const u32x4_any *>(q + k * Piece<T>::kSize), v + k);
+  } else {
+    typedef u32x2 __attribute__((aligned(2))) pair;
+    const u32x2 w = *reinterpret_cast<const pair *>(q);
+    const uint32_t a = w[0], b = w[1];
+    v[0] = T::lo(a), v[1] = T::hi(a), v[2] = T::lo(b), v[3] = T::hi(b);
   }
 }
-template <class T>
-__device__ inline void store4(void *p, int64_t i, bool whole, int left, const float *v) {
-  if (whole) {
-    if constexpr (Piece<T>::kSize == 4) {
-      *reinterpret_cast<u32x4_any *>(static_cast<float *>(p) + i) = Piece<T>::pack(v);
-    } else {
-      typedef u32x2 __attribute__((aligned(2))) pair;
-      *reinterpret_cast<pair *>(static_cast<uint16_t *>(p) + i) =
-          u32x2{T::pack(v[0], v[1]), T::pack(v[2], v[3])};
-    }
-  } else {
+template <class T, int N>
+__device__ inline void store_values(void *p, int64_t i, int left, const float *v) {
+  char *q = static_cast<char *>(p) + i * Piece<T>::kSize;
+  if (left < N) {
 #pragma unroll
-    for (int k = 0; k < 4; ++k)
-      if (k < left) T::store(p, i + k, v[k]);
+    for (int k = 0; k < N; ++k)
+      if (k < left) T::store(q, k, v[k]);
+  } else if constexpr (Piece<T>::kV <= N) {
+#pragma unroll
+    for (int k = 0; k < N; k += Piece<T>::kV)
+      *reinterpret_cast<u32x4_any *>(q + k * Piece<T>::kSize) = Piece<T>::pack(v + k);
+  } else {
+    typedef u32x2 __attribute__((aligned(2))) pair;
+    *reinterpret_cast<pair *>(q) = u32x2{T::pack(v[0], v[1]), T::pack(v[2], v[3])};
   }
 }
-__device__ inline uint32_t load_codes(const void *p, int64_t i, bool whole, int left) {
-  typedef uint32_t __attribute__((aligned(1))) word;
+// Eight codes.
+typedef u32x2 __attribute__((aligned(1))) codes_any;
+__device__ inline u32x2 load_codes(const void *p, int64_t i, int left) {
   const uint8_t *q = static_cast<const uint8_t *>(p) + i;
-  if (whole) return *reinterpret_cast<const word *>(q);
-  uint32_t w = 0;
+  if (left == 8) return *reinterpret_cast<const codes_any *>(q);
+  u32x2 w = {0, 0};
 #pragma unroll
-  for (int k = 0; k < 4; ++k)
-    if (k < left) w |= (uint32_t)q[k] << (8 * k);
+  for (int k = 0; k < 8; ++k)
+    if (k < left) w[k / 4] |= (uint32_t)q[k] << (8 * (k % 4));
   return w;
 }
-__device__ inline void store_codes(void *p, int64_t i, bool whole, int left, uint32_t w) {
-  typedef uint32_t __attribute__((aligned(1))) word;
+__device__ inline void store_codes(void *p, int64_t i, int left, u32x2 w) {
   uint8_t *q = static_cast<uint8_t *>(p) + i;
-  if (whole) {
-    *reinterpret_cast<word *>(q) = w;
+  if (left == 8) {
+    *reinterpret_cast<codes_any *>(q) = w;
   } else {
 #pragma unroll
-    for (int k = 0; k < 4; ++k)
-      if (k < left) q[k] = (uint8_t)(w >> (8 * k));
+    for (int k = 0; k < 8; ++k)
+      if (k < left) q[k] = (uint8_t)(w[k / 4] >> (8 * (k % 4)));
   }
 }
 
@@ -152,10 +169,11 @@ __global__ __launch_bounds__(64 * kWaves) void adamw_kernel(AdamArgs a, int64_t 
   const float b1 = (float)a.beta1, c1 = (float)(1.0 - a.beta1);
   const float b2 = (float)a.beta2, c2 = (float)(1.0 - a.beta2), eps = (float)a.eps;
   const uint32_t step = (uint32_t)(a.step_dev ? *a.step_dev : a.step);
+  constexpr int N = kLane<BITS>;
   const int lane = threadIdx.x % 64;
   int64_t b = (int64_t)blockIdx.x * kWaves + uniform(threadIdx.x / 64);
   for (; b < blocks; b += (int64_t)gridDim.x * kWaves) {
-    // the tensor that has the block: the last one that starts at it or before
+    // the tensor that has the wavefront's values: the last one that starts at them or before
     int lo = 0, hi = a.n;
     while (hi - lo > 1) {
       const int mid = (lo + hi) / 2;
@@ -163,23 +181,23 @@ __global__ __launch_bounds__(64 * kWaves) void adamw_kernel(AdamArgs a, int64_t 
       else hi = mid;
     }
     const AdamTensor t = a.t[uniform(lo)];
-    const int64_t own = b - t.begin;
-    const int64_t i = own * kShare + 4 * lane;
-    const int left = (int)max((int64_t)0, min((int64_t)4, t.count - i));
-    const bool whole = left == 4;
-    float g[4], w[4], m[4], v[4];
-    load4<G>(t.grad, i, whole, left, g);
-    if (t.master) load4<Fp32>(t.master, i, whole, left, w);
-    else load4<T>(t.param, i, whole, left, w);
+    const int64_t i = (b - t.begin) * (64 * N) + N * lane;
+    const int left = (int)max((int64_t)0, min((int64_t)N, t.count - i));
+    float g[N], w[N], m[N], v[N];
+    load_values<G, N>(t.grad, i, left, g);
+    if (t.master) load_values<Fp32, N>(t.master, i, left, w);
+    else load_values<T, N>(t.param, i, left, w);
+    const int64_t share = i / kShare;    // (8 bits: of half a wavefront)
+    const bool any = share * kShare < t.count;
     if constexpr (BITS == 32) {
-      load4<Fp32>(t.m, i, whole, left, m);
-      load4<Fp32>(t.v, i, whole, left, v);
+      load_values<Fp32, N>(t.m, i, left, m);
+      load_values<Fp32, N>(t.v, i, left, v);
     } else {
-      const uint32_t cm = load_codes(t.m, i, whole, left), cv = load_codes(t.v, i, whole, left);
-      const float sm = t.scales[2 * own], sv = t.scales[2 * own + 1];
+      const u32x2 cm = load_codes(t.m, i, left), cv = load_codes(t.v, i, left);
+      const float sm = any ? t.scales[2 * share] : 1.f, sv = any ? t.scales[2 * share + 1] : 1.f;
 #pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        const uint32_t x = cm >> (8 * k) & 0xff, y = cv >> (8 * k) & 0xff;
+      for (int k = 0; k < N; ++k) {
+        const uint32_t x = cm[k / 4] >> (8 * (k % 4)) & 0xff, y = cv[k / 4] >> (8 * (k % 4)) & 0xff;
         m[k] = value_of<3, -6>(x & 0x7f) * sm;
         m[k] = x & 0x80 ? -m[k] : m[k];
         v[k] = value_of<2, -14>(y & 0x7f) * sv;
@@ -187,7 +205,7 @@ __global__ __launch_bounds__(64 * kWaves) void adamw_kernel(AdamArgs a, int64_t 
     }
     float big_m = 0.f, big_v = 0.f;
 #pragma unroll
-    for (int k = 0; k < 4; ++k) {
+    for (int k = 0; k < N; ++k) {
       g[k] = g[k] * factor;
       m[k] = m[k] * b1 + g[k] * c1;
       v[k] = v[k] * b2 + g[k] * g[k] * c2;
@@ -195,49 +213,59 @@ __global__ __launch_bounds__(64 * kWaves) void adamw_kernel(AdamArgs a, int64_t 
       big_v = fmaxf(big_v, v[k]);
       w[k] = w[k] - w[k] * s.decay - m[k] * s.lr_m / (sqrtf(v[k]) * s.root + eps);
     }
-    if (t.master) store4<Fp32>(t.master, i, whole, left, w);
-    store4<T>(t.param, i, whole, left, w);
+    if (t.master) store_values<Fp32, N>(t.master, i, left, w);
+    store_values<T, N>(t.param, i, left, w);
     if constexpr (BITS == 32) {
-      store4<Fp32>(t.m, i, whole, left, m);
-      store4<Fp32>(t.v, i, whole, left, v);
+      store_values<Fp32, N>(t.m, i, left, m);
+      store_values<Fp32, N>(t.v, i, left, v);
     } else {
       float sm, im, sv, iv;
       bool fm = true, fv = true;       // (fmaxf passes over a NaN)
 #pragma unroll
-      for (int k = 0; k < 4; ++k) fm &= fabsf(m[k]) < INFINITY, fv &= v[k] < INFINITY;
-      scale_of(wave_max(big_m), __all(fm), 7, sm, im);
-      scale_of(wave_max(big_v), __all(fv), 14, sv, iv);
-      const u32x4 r = philox((t.first * kShare + (uint64_t)i) / 4, step, a.key0, a.key1);
-      uint32_t cm = 0, cv = 0;
+      for (int k = 0; k < N; ++k) fm &= fabsf(m[k]) < INFINITY, fv &= v[k] < INFINITY;
+      const uint64_t half = 0xffffffffull << (lane & 32);
+      scale_of(half_max(big_m), (~__ballot(fm) & half) == 0, 7, sm, im);
+      scale_of(half_max(big_v), (~__ballot(fv) & half) == 0, 14, sv, iv);
+      const uint64_t quad = (t.first * kShare + (uint64_t)i) / 4;
+      u32x2 cm = {0, 0}, cv = {0, 0};
 #pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        const uint32_t word = r[k];
-        uint32_t x = code_of<3, -6>(fabsf(m[k]) * im, word & 0xffff, 32768);
-        if (m[k] < 0.f) x |= 0x80;
-        uint32_t y = code_of<2, -14>(v[k] * iv, word >> 16, word >> 16);
-        if (v[k] > 0.f && y == 0) y = 1;
-        cm |= (x & 0xff) << (8 * k);
-        cv |= (y & 0xff) << (8 * k);
+      for (int k = 0; k < N; k += 4) {
+        const u32x4 r = philox(quad + k / 4, step, a.key0, a.key1);
+#pragma unroll
+        for (int n = 0; n < 4; ++n) {
+          const uint32_t word = r[n];
+          uint32_t x = code_of<3, -6>(fabsf(m[k + n]) * im, word & 0xffff, 32768);
+          if (m[k + n] < 0.f) x |= 0x80;
+          uint32_t y = code_of<2, -14>(v[k + n] * iv, word >> 16, word >> 16);
+          if (v[k + n] > 0.f && y == 0) y = 1;
+          cm[k / 4] |= (x & 0xff) << (8 * n);
+          cv[k / 4] |= (y & 0xff) << (8 * n);
+        }
       }
-      store_codes(t.m, i, whole, left, cm);
-      store_codes(t.v, i, whole, left, cv);
-      if (lane == 0) t.scales[2 * own] = sm, t.scales[2 * own + 1] = sv;
+      store_codes(t.m, i, left, cm);
+      store_codes(t.v, i, left, cv);
+      if (any && lane % 32 == 0) t.scales[2 * share] = sm, t.scales[2 * share + 1] = sv;
     }
   }
 }
 
-template <class T, class G>
-void launch(AdamArgs a, int bits, hipStream_t s) {
+template <class T, class G, int BITS>
+void launch(AdamArgs a, hipStream_t s) {
   if (!a.step_dev && !a.lr_dev) a.s = step_of(a, (double)a.step, a.lr);
-  int64_t blocks = 0;
+  constexpr int kPer = 64 * kLane<BITS>;
+  int64_t blocks = 0;                  // wavefronts' values
   for (int i = 0; i < a.n; ++i) {
     a.t[i].begin = blocks;
-    blocks += (a.t[i].count + kShare - 1) / kShare;
+    blocks += (a.t[i].count + kPer - 1) / kPer;
   }
   if (blocks == 0) return;
   const unsigned grid = (unsigned)std::min<int64_t>((blocks + kWaves - 1) / kWaves, 8 * kSeqCus);
-  if (bits == 8) adamw_kernel<T, G, 8><<<grid, 64 * kWaves, 0, s>>>(a, blocks);
-  else adamw_kernel<T, G, 32><<<grid, 64 * kWaves, 0, s>>>(a, blocks);
+  adamw_kernel<T, G, BITS><<<grid, 64 * kWaves, 0, s>>>(a, blocks);
+}
+template <class T, class G>
+void launch(const AdamArgs &a, int bits, hipStream_t s) {
+  if (bits == 8) launch<T, G, 8>(a, s);
+  else launch<T, G, 32>(a, s);
 }
 
 template <class T>

@@ -78,8 +78,8 @@ struct AdamTensor {
   const void *grad;
   float *scales;
   int64_t count;
-  int64_t begin;                       // its first block of 256 values, of those of the launch
-  uint64_t first;                      // ... and counted through all tensors of a call
+  int64_t begin;                       // its first wavefront's values, of those of the launch
+  uint64_t first;                      // its first block of 256 values, counted through all tensors of a call
 };
 struct AdamStep {
   float lr_m, root, decay;             // lr / (1 - b1^t), 1 / sqrt(1 - b2^t), lr decay
