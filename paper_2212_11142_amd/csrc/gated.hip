@@ -635,8 +635,10 @@ __global__ __launch_bounds__(256) void product_add(ProductArgs x, ProductArgs w)
 int64_t tiles(int64_t n, int size) { return (n + size - 1) / size; }
 size_t align256(size_t n) { return (n + 255) & ~(size_t)255; }
 
-// Tiles of 256 x 256 where they fill the device, else of 128 x 128.
-bool use_big(int64_t rows, int64_t hidden) { return tiles(rows, 256) * tiles(hidden, 128) >= kSeqCus; }
+// Tiles of 256 x 256 where those of 128 x 128 are more than are resident at once. Measured, us, large and small:
+// 2,048 x 1,024 x 2,048 (512 small tiles) 27.7 and 21.5, 4,096 x 1,024 x 1,024 (512) 28.4 and 27.0, 1,408 hidden
+// values (704) 29.2 and 37.9, 2,048 (1,024) 33.9 and 41.4; 8,192 x 256 x 1,024 (1,024) 15.1 and 17.1.
+bool use_big(int64_t rows, int64_t hidden) { return tiles(rows, 128) * tiles(hidden, 64) > 2 * kSeqCus; }
 
 template <class T, int BM, int BN, int WM, int WN, int ACT, bool GRAD>
 hipError_t launch_projections(const GatedGradArgs &g, char *dg, char *du, hipStream_t s) {
@@ -688,7 +690,9 @@ struct Plan {
   int sx, sw;                          // parts of dx's and of dW's summed axis
   int64_t nx, nw, lx, lw;              // blocks, and a block's steps
 };
-constexpr int kLeast = 8;              // steps of a part at least
+// Steps of a part at least: 1,021 x 520 x 1,368 with 8 19.6 us and 5.2 for adding the parts, with 16 23.6 and 4.1,
+// with 4 19.8 and 5.5.
+constexpr int kLeast = 8;
 Plan plan_of(int64_t rows, int64_t width, int64_t hidden, bool big) {
   const int size = big ? 256 : 128;
   const int64_t tx = tiles(rows, size) * tiles(width, size), tw = 2 * tiles(hidden, size) * tiles(width, size);

@@ -310,9 +310,10 @@ def test_gated_strides(rows, width, hidden, dtype, kind):
     (2100, 2120, 2200, "silu"),            # larger tiles, ragged in every direction
     (8100, 1016, 1032, "gelu"),            # ... the weights' gradients in parts
     (520, 2056, 8200, "silu"),             # ... dx in parts
-    (4090, 72, 1904, "gelu"),              # smaller tiles, more than are resident at once
+    (4090, 72, 1904, "gelu"),              # two steps a tile
+    (3900, 328, 1000, "silu"),             # smaller tiles, as many as are resident at once
     (20000, 56, 1032, "silu"),             # a tile a step, several tiles a block
-    (30000, 120, 776, "gelu"),             # ... two steps
+    (30000, 120, 776, "gelu"),             # ... two steps, several tiles a block
     (17000, 200, 2056, "silu"),            # ... four
     (1000, 520, 1368, "silu")])            # ... every sum in parts
 @pytest.mark.parametrize("dtype", [BF, FP])
