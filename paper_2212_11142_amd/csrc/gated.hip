@@ -266,10 +266,13 @@ __device__ inline void activation(float z, float &a, float &d) {
 }
 
 // ------------------------------------------------------------------ both projections
-// BM rows of x and BN / 2 hidden values per block, WM x WN wavefronts, each of 32 C hidden values.
-template <class T, int BM, int BN, int WM, int WN, int ACT, bool GRAD>
-__global__ __launch_bounds__(64 * WM * WN, 2) void gated_kernel(GatedGradArgs g, char *dg, char *du,
-                                                             int nm, int nn) {
+// BM rows of x and BN / 2 hidden values per block, WM x WN wavefronts, each of 32 C hidden values. With
+// GROUPS 2 a block has two such groups of wavefronts, each with half of the summed axis and places in LDS of
+// its own, and one tile: where tiles are few, what counts is how long a step takes, not how many run at once.
+// The groups hand each other half of their sums in the end.
+template <class T, int BM, int BN, int WM, int WN, int GROUPS, int ACT, bool GRAD>
+__global__ __launch_bounds__(64 * WM * WN * GROUPS, 2) void gated_kernel(GatedGradArgs g, char *dg, char *du,
+                                                                      int nm, int nn) {
   constexpr int W = WM * WN, TM = BM / 32 / WM, C = BN / 64 / WN;
   extern __shared__ char stages[];
   constexpr int kHalf = BN / 2 * kStepBytes, kStage = (BM + BN) * kStepBytes;
@@ -278,7 +281,8 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void gated_kernel(GatedGradArgs g,
   static_assert(BM * kStepBytes >= W * Swap::kBytes);
   static_assert(2 * Side<false, BN / 2, W>::kCopies == Side<false, BM, W>::kCopies);
   const GatedArgs &a = g.f;
-  const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6);
+  const int lane = threadIdx.x & 63, waves = uniform(threadIdx.x >> 6);
+  const int group = GROUPS > 1 ? waves / W : 0, wave = GROUPS > 1 ? waves % W : waves;
   const int wm = wave / WN, wn = wave % WN;
   const unsigned all = (unsigned)nm * nn;
   Tile t = tile_of(blockIdx.x, all, nm, nn);                // whose products are summed
@@ -290,7 +294,7 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void gated_kernel(GatedGradArgs g,
   gate.init(a.w_gate, (int64_t)t.n * (BN / 2), a.hidden, a.gate_row, wave, lane);
   up.init(a.w_up, (int64_t)t.n * (BN / 2), a.hidden, a.up_row, wave, lane);
   x.init(a.x, (int64_t)t.m * BM, a.rows, a.x_row, wave, lane);
-  const uint32_t lds = lds_address(stages);
+  const uint32_t lds = lds_address(stages) + group * (2 * kStage);
   f32x16 acc[TM][2][C];
   auto clear = [&] {
 #pragma unroll
@@ -302,17 +306,78 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void gated_kernel(GatedGradArgs g,
   struct Operands {
     u32x4 w[2][C], x[TM];
   };
-  const int steps = (a.width + kStep - 1) / kStep;
+  // what becomes of 32 rows of tile `of`
+  auto finish = [&](int j, const Tile &of, const Swap &swap) {
+    const int64_t n = (int64_t)of.n * (BN / 2) + 32 * C * wn, bytes = 2 * (a.hidden - n);
+    const int64_t row = (int64_t)of.m * BM + wm * (BM / WM) + 32 * j, rows = a.rows - row;
+    f32x16 *u = acc[j][0], *v = acc[j][1];
+    if constexpr (GRAD) {
+      u32x4 dy[Swap::kCount];
+#pragma unroll
+      for (int i = 0; i < Swap::kCount; ++i) {
+        dy[i] = u32x4{0, 0, 0, 0};
+        if (swap.within(i, rows, bytes))
+          dy[i] = *reinterpret_cast<const u32x4 *>(g.dout + row * g.dout_row + 2 * n +
+                                                   swap.offset(i, g.dout_row));
+      }
+#pragma unroll
+      for (int i = 0; i < Swap::kCount; ++i) swap.put_row(i, dy[i]);
+      __builtin_amdgcn_wave_barrier();
+#pragma unroll
+      for (int c = 0; c < C; ++c)
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          __builtin_amdgcn_sched_barrier(0);       // (a few at a time: registers)
+          const u32x2 w = swap.get(c, q);
+          const uint32_t w0 = w[0], w1 = w[1];
+          const float y[4] = {T::lo(w0), T::hi(w0), T::lo(w1), T::hi(w1)};
+#pragma unroll
+          for (int r = 0; r < 4; ++r) {
+            float f, d;
+            activation<ACT>(u[c][4 * q + r], f, d);
+            u[c][4 * q + r] = y[r] * v[c][4 * q + r] * d;
+            v[c][4 * q + r] = y[r] * f;
+          }
+        }
+      const int64_t stride = (int64_t)a.hidden * 2, to = row * stride + 2 * n;
+      __builtin_amdgcn_wave_barrier();
+      swap.template put_all<T>(u);
+      __builtin_amdgcn_wave_barrier();
+      swap.store(dg + to, stride, rows, bytes);
+      __builtin_amdgcn_wave_barrier();
+      swap.template put_all<T>(v);
+      __builtin_amdgcn_wave_barrier();
+      swap.store(du + to, stride, rows, bytes);
+    } else {
+#pragma unroll
+      for (int c = 0; c < C; ++c)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          float f, d;
+          activation<ACT>(u[c][i], f, d);
+          u[c][i] = f * v[c][i];
+        }
+      swap.template put_all<T>(u);
+      __builtin_amdgcn_wave_barrier();
+      swap.store(a.out + row * a.out_row + 2 * n, a.out_row, rows, bytes);
+    }
+  };
   // a tile's steps follow those of the block's tile before without a pause. Each row of tiles starts at
-  // another step: rows a power of two apart meet in few of the L2's channels
+  // another step: rows a power of two apart meet in few of the L2's channels (263 us without, 259 with it)
+  const int total = (a.width + kStep - 1) / kStep, steps = (total + GROUPS - 1) / GROUPS;
+  const int first = group * steps;                         // a group's steps
+  const int mine = GROUPS > 1 ? max(1, min(steps, total - first)) : steps;
   unsigned index = blockIdx.x, current = blockIdx.x;       // of next and of t (two tiles apart, with one step a tile)
   int step = -1, left = steps;           // of next's, the one whose operands are copied; those left of t's
   int64_t k0 = 0;
   bool on = true;
   run_steps<Operands, 2 * Half::kCopies + Whole::kCopies, 2 * C * TM, TM + 2 * C>(
-      (int64_t)steps * ((all - blockIdx.x + gridDim.x - 1) / gridDim.x),
+      GROUPS > 1 ? steps : (int64_t)steps * ((all - blockIdx.x + gridDim.x - 1) / gridDim.x),
       [&](int64_t) {
-        if (++step == steps) {
+        ++step;
+        if (GROUPS > 1) {
+          on = step < steps && first + step < total;
+        } else if (step == steps) {
           step = 0;
           index += gridDim.x;
           on = index < all;
@@ -323,8 +388,8 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void gated_kernel(GatedGradArgs g,
             x.move(a.x, (int64_t)next.m * BM, a.rows);
           }
         }
-        const int at = step + next.m % steps;
-        k0 = (int64_t)(at >= steps ? at - steps : at) * kStep;
+        const int at = step + next.m % mine;
+        k0 = on ? (int64_t)(first + (at >= mine ? at - mine : at)) * kStep : 0;
       },
       [&](int stage, int i) {
         const uint32_t to = lds + stage * kStage;
@@ -345,74 +410,56 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void gated_kernel(GatedGradArgs g,
         acc[j][q][c] = T::mfma(o.w[q][c], o.x[j], acc[j][q][c]);
       },
       [&](int64_t, int stage) {
-        if (--left) return false;
+        if (GROUPS > 1 || --left) return false;
         left = steps;
         // (x's part of the stage: its copies go out last, after the block has met)
         const Swap swap = {lds + stage * kStage + 2 * kHalf + wave * Swap::kBytes, lane};
-        const int64_t n = (int64_t)t.n * (BN / 2) + 32 * C * wn, bytes = 2 * (a.hidden - n);
-        const int64_t row0 = (int64_t)t.m * BM + wm * (BM / WM);
-        current += gridDim.x;
-        if (current < all) t = tile_of(current, all, nm, nn);
 #pragma unroll
         for (int j = 0; j < TM; ++j) {
-          const int64_t row = row0 + 32 * j, rows = a.rows - row;
-          f32x16 *u = acc[j][0], *v = acc[j][1];
-          if constexpr (GRAD) {
-            u32x4 dy[Swap::kCount];
-#pragma unroll
-            for (int i = 0; i < Swap::kCount; ++i) {
-              dy[i] = u32x4{0, 0, 0, 0};
-              if (swap.within(i, rows, bytes))
-                dy[i] = *reinterpret_cast<const u32x4 *>(g.dout + row * g.dout_row + 2 * n +
-                                                         swap.offset(i, g.dout_row));
-            }
-#pragma unroll
-            for (int i = 0; i < Swap::kCount; ++i) swap.put_row(i, dy[i]);
-            __builtin_amdgcn_wave_barrier();
-#pragma unroll
-            for (int c = 0; c < C; ++c)
-#pragma unroll
-              for (int q = 0; q < 4; ++q) {
-                __builtin_amdgcn_sched_barrier(0);       // (a few at a time: registers)
-                const u32x2 w = swap.get(c, q);
-                const uint32_t w0 = w[0], w1 = w[1];
-                const float y[4] = {T::lo(w0), T::hi(w0), T::lo(w1), T::hi(w1)};
-#pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                  float f, d;
-                  activation<ACT>(u[c][4 * q + r], f, d);
-                  u[c][4 * q + r] = y[r] * v[c][4 * q + r] * d;
-                  v[c][4 * q + r] = y[r] * f;
-                }
-              }
-            const int64_t stride = (int64_t)a.hidden * 2, to = row * stride + 2 * n;
-            __builtin_amdgcn_wave_barrier();
-            swap.template put_all<T>(u);
-            __builtin_amdgcn_wave_barrier();
-            swap.store(dg + to, stride, rows, bytes);
-            __builtin_amdgcn_wave_barrier();
-            swap.template put_all<T>(v);
-            __builtin_amdgcn_wave_barrier();
-            swap.store(du + to, stride, rows, bytes);
-          } else {
-#pragma unroll
-            for (int c = 0; c < C; ++c)
-#pragma unroll
-              for (int i = 0; i < 16; ++i) {
-                float f, d;
-                activation<ACT>(u[c][i], f, d);
-                u[c][i] = f * v[c][i];
-              }
-            swap.template put_all<T>(u);
-            __builtin_amdgcn_wave_barrier();
-            swap.store(a.out + row * a.out_row + 2 * n, a.out_row, rows, bytes);
-          }
+          finish(j, t, swap);
           __builtin_amdgcn_sched_barrier(0);             // (one at a time: registers)
         }
+        current += gridDim.x;
+        if (current < all) t = tile_of(current, all, nm, nn);
         clear();
         asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
         return true;
       });
+  if constexpr (GROUPS > 1) {
+    static_assert(GROUPS == 2 && TM == 2 && C == 1);
+    constexpr int kSums = W * 8 * 1024;  // half a group's: 8 pieces of 16 bytes a lane
+    static_assert(2 * kSums + 2 * W * Swap::kBytes <= 4 * kStage);
+    typedef __attribute__((address_space(3))) f32x4 lds_f32x4;
+    const uint32_t at = lds_address(stages) + (wave * 8 * 64 + lane) * 16;
+    auto give = [&](const f32x16 (&v)[2][C], uint32_t to) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const f32x16 &x = v[i / 4][0];
+        const int k = 4 * (i % 4);
+        *(lds_f32x4 *)(uintptr_t)(to + i * 1024) = f32x4{x[k], x[k + 1], x[k + 2], x[k + 3]};
+      }
+    };
+    auto take = [&](f32x16 (&v)[2][C], uint32_t from) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const f32x4 y = *(lds_f32x4 *)(uintptr_t)(from + i * 1024);
+#pragma unroll
+        for (int r = 0; r < 4; ++r) v[i / 4][0][4 * (i % 4) + r] += y[r];
+      }
+    };
+    const Swap swap = {lds_address(stages) + 2 * kSums + (group * W + wave) * Swap::kBytes, lane};
+    __syncthreads();                     // (all copies have landed, all operands have been read)
+    if (group) give(acc[0], at + kSums);
+    else give(acc[1], at);
+    __syncthreads();
+    if (group) {
+      take(acc[1], at);
+      finish(1, t, swap);
+    } else {
+      take(acc[0], at + kSums);
+      finish(0, t, swap);
+    }
+  }
 }
 
 // ------------------------------------------------------------------ few rows
@@ -640,22 +687,29 @@ size_t align256(size_t n) { return (n + 255) & ~(size_t)255; }
 // values (704) 29.2 and 37.9, 2,048 (1,024) 33.9 and 41.4; 8,192 x 256 x 1,024 (1,024) 15.1 and 17.1.
 bool use_big(int64_t rows, int64_t hidden) { return tiles(rows, 128) * tiles(hidden, 64) > 2 * kSeqCus; }
 
-template <class T, int BM, int BN, int WM, int WN, int ACT, bool GRAD>
+// Two groups of wavefronts a tile where each tile has a compute unit of its own, and sums long enough to pay
+// for the exchange (1024 x 1024: from 1024 wide 10.3 us, 12.7 with one group; 256 wide 6.1 both; 64 wide 5.2 and 4.3).
+bool use_groups(int64_t rows, int64_t width, int64_t hidden) {
+  return width > 4 * kStep && tiles(rows, 128) * tiles(hidden, 64) <= kSeqCus;
+}
+
+template <class T, int BM, int BN, int WM, int WN, int GROUPS, int ACT, bool GRAD>
 hipError_t launch_projections(const GatedGradArgs &g, char *dg, char *du, hipStream_t s) {
-  constexpr int kLds = 2 * (BM + BN) * kStepBytes, kResident = kLdsBytes / kLds * kSeqCus;
+  constexpr int kLds = 2 * GROUPS * (BM + BN) * kStepBytes, kResident = kLdsBytes / kLds * kSeqCus;
   static LdsLimit limit;
-  const void *f = reinterpret_cast<const void *>(gated_kernel<T, BM, BN, WM, WN, ACT, GRAD>);
+  const void *f = reinterpret_cast<const void *>(gated_kernel<T, BM, BN, WM, WN, GROUPS, ACT, GRAD>);
   const hipError_t e = limit.set(f, kLds);
   if (e != hipSuccess) return e;
   const int nm = (int)tiles(g.f.rows, BM), nn = (int)tiles(g.f.hidden, BN / 2);
-  gated_kernel<T, BM, BN, WM, WN, ACT, GRAD>
-      <<<(unsigned)std::min(nm * nn, kResident), 64 * WM * WN, kLds, s>>>(g, dg, du, nm, nn);
+  gated_kernel<T, BM, BN, WM, WN, GROUPS, ACT, GRAD>
+      <<<(unsigned)(GROUPS > 1 ? nm * nn : std::min(nm * nn, kResident)), 64 * WM * WN * GROUPS, kLds, s>>>(
+          g, dg, du, nm, nn);
   return hipGetLastError();
 }
 // Whether the weights stream past the rows: up to 32 rows, and more where a block for each 16 hidden values and
-// 64 rows has a compute unit of its own. Measured, us, this form and tiles: 16 rows of 1,024 x 4,096 6.1 and
-// 13.1, 64 rows 9.2 and 13.2, 96 rows (512 blocks) 13.9 and 13.3; 256 rows of 4,096 x 1,024 24.8 and 42.1, of
-// 256 x 1,024 4.6 and 6.0; of 2,048 x 8,192 32 rows 18.5 and 25.2, 64 rows (512 blocks) 26.8 and 25.4.
+// 64 rows has a compute unit of its own. Measured, us, this form and tiles: 16 rows of 1,024 x 4,096 5.0 and
+// 10.0, 64 rows 8.2 and 10.1, 96 rows (512 blocks) 13.1 and 10.2; 256 rows of 4,096 x 1,024 24.3 and 28.3, of
+// 256 x 1,024 4.2 and 5.9; of 2,048 x 8,192 32 rows 18.1 and 21.1, 64 rows (512 blocks) 26.7 and 21.3.
 bool use_few(int64_t rows, int64_t hidden) {
   return rows <= 32 || tiles(hidden, 16) * tiles(rows, 64) <= kSeqCus;
 }
@@ -672,8 +726,10 @@ hipError_t projections(const GatedGradArgs &g, char *dg, char *du, hipStream_t s
     return launch_few<T, 4, ACT>(g.f, s);
   }
   if (use_big(g.f.rows, g.f.hidden))
-    return launch_projections<T, 256, 256, 4, 2, ACT, GRAD>(g, dg, du, s);
-  return launch_projections<T, 128, 128, 2, 2, ACT, GRAD>(g, dg, du, s);
+    return launch_projections<T, 256, 256, 4, 2, 1, ACT, GRAD>(g, dg, du, s);
+  if (use_groups(g.f.rows, g.f.width, g.f.hidden))
+    return launch_projections<T, 128, 128, 2, 2, 2, ACT, GRAD>(g, dg, du, s);
+  return launch_projections<T, 128, 128, 2, 2, 1, ACT, GRAD>(g, dg, du, s);
 }
 template <bool GRAD>
 hipError_t by_type(const GatedGradArgs &g, char *dg, char *du, hipStream_t s) {

@@ -315,7 +315,10 @@ def test_gated_strides(rows, width, hidden, dtype, kind):
     (20000, 56, 1032, "silu"),             # a tile a step, several tiles a block
     (30000, 120, 776, "gelu"),             # ... two steps, several tiles a block
     (17000, 200, 2056, "silu"),            # ... four
-    (1000, 520, 1368, "silu")])            # ... every sum in parts
+    (1000, 520, 1368, "silu"),             # ... every sum in parts
+    (1000, 264, 1032, "gelu"),             # two groups of wavefronts a tile: 3 and 2 steps
+    (1990, 344, 968, "silu"),              # ... 3 and 3, ragged
+    (300, 1080, 4104, "gelu")])            # ... 9 and 8, ragged
 @pytest.mark.parametrize("dtype", [BF, FP])
 def test_gated_tiles(dtype, rows, width, hidden, kind):
     """The sums' errors together, against what rounding the results alone takes: the forward pass adds
