@@ -187,6 +187,7 @@ gp_status gp_norm(const gp_norm_spec *t, int32_t rows, const void *x, int64_t x_
     }
     if (st != GP_OK) return st;
     if (!residual && sum) return bad("a sum needs a residual");
+    if (!aligned(stats, 4)) return bad("stats is not aligned to its type");
     if (rows == 0) return GP_OK;
     if (residual && out == sum) return bad("out and sum are the same");
     NormArgs a;
@@ -227,6 +228,7 @@ gp_status gp_norm_grad(const gp_norm_spec *t, int32_t rows, const void *h, int64
     if (st == GP_OK) st = check_weight(dbias, t, "dbias");
     if (st != GP_OK) return st;
     if (!stats && rows > 0) return bad("stats is NULL");
+    if (!aligned(stats, 4)) return bad("stats is not aligned to its type");
     NormGradArgs a = norm_grad_args(t, rows, dweight, dbias);
     st = check_workspace(workspace, ws_bytes, norm_grad_bytes(a));
     if (st != GP_OK) return st;

@@ -399,7 +399,8 @@ _shape, _dtype = operator.attrgetter("shape"), operator.attrgetter("dtype")
 class AdamW:
     """AdamW's states for a list of weights of one dtype, on their device: m and v of 32 bits, or of
     8 (e4m3 and e5m2 codes, with scales [blocks, 2] of each 256 values). masters: fp32 copies of
-    16-bit weights, which the step is made on. grad_dtype: the gradients' (None: the weights').
+    16-bit weights, which the step is made on. grad_dtype: the gradients' (None: the weights'). A
+    weight may be given once only: none of them may share memory.
 
     The states lie one tensor after another in m_all and v_all [blocks, 256] (and scales_all
     [blocks, 2]), each from a block of its own on; m, v and scales are views of them. They start at
@@ -458,8 +459,9 @@ class AdamW:
         """The weights' addresses, as they are now: a weight's storage may have been replaced."""
         torch = _torch()
         at = list(map(torch.Tensor.data_ptr, self._weights))
-        if at == self._at:
+        if at == self._at and all(map(torch.Tensor.is_contiguous, self._weights)):
             return
+        self._at = None
         n = len(self.params)
         for i, t in enumerate(self.tensors):
             p = self.params[i]
@@ -475,6 +477,9 @@ class AdamW:
                                      f"weight's shape on cuda:{self.device}")
                 t.master = at[n + i] or None
             t.param = at[i] or None
+        ends = sorted((a, a + w.numel() * w.element_size()) for a, w in zip(at, self._weights) if a)
+        if any(end > begin for (_, end), (begin, _) in zip(ends, ends[1:])):
+            raise ValueError("weights (and master copies) must not share memory")
         self._at = at
 
     def _gradients(self, grads):

@@ -71,6 +71,10 @@ def test_norm_calls_refused(lib):
     assert call_norm(lib, s, rows=0, x=None, out=None) == 0
 
 
+def test_norm_statistics_at_odd_addresses_refused(lib):
+    assert call_norm(lib, norm(), stats=258) == INVALID and call_norm_grad(lib, norm(), stats=258) == INVALID
+
+
 def test_norm_workspaces(lib):
     """As many sums as blocks that are resident at once, however many rows; wide rows' means beside."""
     f = lambda rows, **kw: lib.gp_norm_grad_workspace_bytes(C.byref(norm(**kw)), rows)     # noqa: E731

@@ -208,6 +208,46 @@ def test_adamw_descriptions():
             layers.AdamW(*args, **kw)
 
 
+def adamw_of(params, masters=None):
+    """A state's marshalling alone, of host tensors."""
+    o = layers.AdamW.__new__(layers.AdamW)
+    o.params, o.masters, o.dtype, o.device = params, masters, params[0].dtype, -1
+    o.shapes = [p.shape for p in params]
+    o.tensors = (gp._AdamWTensor * len(params))()
+    o._weights, o._at = params + (masters or []), None
+    return o
+
+
+def test_adamw_weights_share_no_memory():
+    x = torch.zeros(64)
+    a, b = x[:32], x[32:]
+    adamw_of([b, a, torch.zeros(0), torch.zeros(0)])._update()
+    for params in ([a, b, a], [x, a], [a, x[31:40]]):
+        with pytest.raises(ValueError, match="share"):
+            adamw_of(params)._update()
+    h, w = torch.zeros(32, dtype=BF), torch.zeros(32)
+    adamw_of([h], [w])._update()
+    with pytest.raises(ValueError, match="share"):
+        adamw_of([h, torch.zeros(32, dtype=BF)], [w, w])._update()
+    with pytest.raises(ValueError, match="share"):
+        adamw_of([w.view(BF)[:32]], [w])._update()
+
+
+def test_adamw_weights_whose_layout_changes():
+    """At the same address, too; and after a refusal the next call looks again."""
+    p = torch.nn.Parameter(torch.zeros(4, 4))
+    o = adamw_of([p])
+    o._update()
+    o._update()
+    p.data = p.data.t()
+    for _ in range(2):
+        with pytest.raises(ValueError, match="contiguous"):
+            o._update()
+    p.data = torch.zeros(4, 4)
+    o._update()
+    assert o.tensors[0].param == p.data_ptr()
+
+
 # ------------------------------------------------------------------ sources
 @pytest.mark.parametrize("name", ["gated.hip", "norm.hip", "rotate.hip", "adamw.hip", "layer_dev.h"])
 def test_no_vector_arithmetic_in_inline_assembly(name):
