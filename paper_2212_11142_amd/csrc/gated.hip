@@ -235,6 +235,37 @@ struct Exchange {
   }
 };
 
+// Two groups of W wavefronts have sums of the same tile, x, of different parts of the summed axis: each gives
+// the other half of its own, through LDS, and keeps in x[0] the whole of x[0] (group 0) or x[1] (group 1).
+template <int W>
+constexpr int kHandOver = 2 * W * 8 * 1024;    // 8 pieces of 16 bytes a lane, both ways
+template <int W>
+__device__ inline void hand_over(uint32_t lds, int group, int wave, int lane, f32x16 (&x)[2][2]) {
+  typedef __attribute__((address_space(3))) f32x4 lds_f32x4;
+  const uint32_t at = lds + (wave * 8 * 64 + lane) * 16, half = W * 8 * 1024;
+  const uint32_t to = at + (group ? half : 0), from = at + (group ? 0 : half);
+  __syncthreads();                       // (all copies have landed, all operands have been read)
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    f32x16 a = x[0][i / 4], b = x[1][i / 4];
+    f32x4 y;
+#pragma unroll
+    for (int r = 4 * (i % 4); r < 4 * (i % 4) + 4; ++r) {
+      y[r % 4] = group ? +a[r] : +b[r];
+      a[r] = group ? +b[r] : +a[r];
+    }
+    x[0][i / 4] = a;
+    *(lds_f32x4 *)(uintptr_t)(to + i * 1024) = y;
+  }
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const f32x4 y = *(lds_f32x4 *)(uintptr_t)(from + i * 1024);
+#pragma unroll
+    for (int r = 0; r < 4; ++r) x[0][i / 4][4 * (i % 4) + r] += y[r];
+  }
+}
+
 // ------------------------------------------------------------------ activations
 constexpr int kSilu = 0, kGelu = 1;   // GP_SILU, GP_GELU
 
@@ -306,10 +337,10 @@ __global__ __launch_bounds__(64 * WM * WN * GROUPS, 2) void gated_kernel(GatedGr
   struct Operands {
     u32x4 w[2][C], x[TM];
   };
-  // what becomes of 32 rows of tile `of`
-  auto finish = [&](int j, const Tile &of, const Swap &swap) {
+  // what becomes of sums j: rows 32 at .. of a wavefront's of tile `of`
+  auto finish = [&](int j, int at, const Tile &of, const Swap &swap) {
     const int64_t n = (int64_t)of.n * (BN / 2) + 32 * C * wn, bytes = 2 * (a.hidden - n);
-    const int64_t row = (int64_t)of.m * BM + wm * (BM / WM) + 32 * j, rows = a.rows - row;
+    const int64_t row = (int64_t)of.m * BM + wm * (BM / WM) + 32 * at, rows = a.rows - row;
     f32x16 *u = acc[j][0], *v = acc[j][1];
     if constexpr (GRAD) {
       u32x4 dy[Swap::kCount];
@@ -416,7 +447,7 @@ __global__ __launch_bounds__(64 * WM * WN * GROUPS, 2) void gated_kernel(GatedGr
         const Swap swap = {lds + stage * kStage + 2 * kHalf + wave * Swap::kBytes, lane};
 #pragma unroll
         for (int j = 0; j < TM; ++j) {
-          finish(j, t, swap);
+          finish(j, j, t, swap);
           __builtin_amdgcn_sched_barrier(0);             // (one at a time: registers)
         }
         current += gridDim.x;
@@ -427,38 +458,10 @@ __global__ __launch_bounds__(64 * WM * WN * GROUPS, 2) void gated_kernel(GatedGr
       });
   if constexpr (GROUPS > 1) {
     static_assert(GROUPS == 2 && TM == 2 && C == 1);
-    constexpr int kSums = W * 8 * 1024;  // half a group's: 8 pieces of 16 bytes a lane
-    static_assert(2 * kSums + 2 * W * Swap::kBytes <= 4 * kStage);
-    typedef __attribute__((address_space(3))) f32x4 lds_f32x4;
-    const uint32_t at = lds_address(stages) + (wave * 8 * 64 + lane) * 16;
-    auto give = [&](const f32x16 (&v)[2][C], uint32_t to) {
-#pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const f32x16 &x = v[i / 4][0];
-        const int k = 4 * (i % 4);
-        *(lds_f32x4 *)(uintptr_t)(to + i * 1024) = f32x4{x[k], x[k + 1], x[k + 2], x[k + 3]};
-      }
-    };
-    auto take = [&](f32x16 (&v)[2][C], uint32_t from) {
-#pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const f32x4 y = *(lds_f32x4 *)(uintptr_t)(from + i * 1024);
-#pragma unroll
-        for (int r = 0; r < 4; ++r) v[i / 4][0][4 * (i % 4) + r] += y[r];
-      }
-    };
-    const Swap swap = {lds_address(stages) + 2 * kSums + (group * W + wave) * Swap::kBytes, lane};
-    __syncthreads();                     // (all copies have landed, all operands have been read)
-    if (group) give(acc[0], at + kSums);
-    else give(acc[1], at);
-    __syncthreads();
-    if (group) {
-      take(acc[1], at);
-      finish(1, t, swap);
-    } else {
-      take(acc[0], at + kSums);
-      finish(0, t, swap);
-    }
+    static_assert(kHandOver<W> + 2 * W * Swap::kBytes <= 4 * kStage);
+    const Swap swap = {lds_address(stages) + kHandOver<W> + (group * W + wave) * Swap::kBytes, lane};
+    hand_over<W>(lds_address(stages), group, wave, lane, reinterpret_cast<f32x16 (&)[2][2]>(acc));
+    finish(0, group, t, swap);
   }
 }
 
@@ -557,29 +560,32 @@ struct ProductArgs {
   int nm, nn, splits;
 };
 
-template <class T, int BM, int BN, int WM, int WN, bool B_COL, int SEGMENTS>
+template <class T, int BM, int BN, int WM, int WN, int GROUPS, bool B_COL, int SEGMENTS>
 __device__ inline void product_tile(const ProductArgs &p, unsigned block) {
   constexpr int W = WM * WN, TM = BM / 32 / WM, TN = BN / 32 / WN;
   extern __shared__ char stages[];
   constexpr int kStage = (BM + BN) * kStepBytes, kA = BN * kStepBytes;
   typedef Side<true, BN, W> ASide;
   typedef Side<B_COL, BM, W> BSide;
-  const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6);
+  const int lane = threadIdx.x & 63, waves = uniform(threadIdx.x >> 6);
+  const int group = GROUPS > 1 ? waves / W : 0, wave = GROUPS > 1 ? waves % W : waves;
   const int wm = wave / WN, wn = wave % WN;
   const unsigned all = (unsigned)p.nm * p.nn;
   const int part = (int)(block / all), output = part / p.splits, split = part % p.splits;
   const Tile t = tile_of(block - part * all, all, p.nm, p.nn);
   const int64_t m0 = (int64_t)t.m * BM, n0 = (int64_t)t.n * BN;
   const int per = (int)((p.k + kStep - 1) / kStep), steps = per * SEGMENTS;
-  const int first = (int)((int64_t)steps * split / p.splits);
-  const int end = (int)((int64_t)steps * (split + 1) / p.splits);
+  // a block's steps, or a group's: the first one's as many as the second's or one more
+  const int begin = (int)((int64_t)steps * split / p.splits);
+  const int behind = (int)((int64_t)steps * (split + 1) / p.splits), half = (behind - begin + 1) / 2;
+  const int first = begin + group * half, end = GROUPS > 1 && group == 0 ? begin + half : behind;
   const int skew = !B_COL && end > first ? t.m % (end - first) : 0;
   ASide a;
   BSide b;
   int segment = SEGMENTS == 2 ? (first + skew >= per) : output;
   a.init(p.a[segment], n0, p.n, p.a_row[segment], wave, lane);
   b.init(p.b[segment], m0, p.m, p.b_row[segment], wave, lane);
-  const uint32_t lds = lds_address(stages);
+  const uint32_t lds = lds_address(stages) + group * (2 * kStage);
   f32x16 acc[TM][TN];
 #pragma unroll
   for (int j = 0; j < TM; ++j)
@@ -591,7 +597,7 @@ __device__ inline void product_tile(const ProductArgs &p, unsigned block) {
   bool on = true;                        // copies of a step that there is, from k0 on
   int64_t k0 = 0;
   run_steps<Operands, ASide::kCopies + BSide::kCopies, TM * TN, TN + TM>(
-      end - first,
+      GROUPS > 1 ? half : end - first,
       [&](int64_t i) {
         int step = first + (int)i;
         on = step < end;
@@ -621,13 +627,9 @@ __device__ inline void product_tile(const ProductArgs &p, unsigned block) {
       },
       [](int64_t, int) { return false; });
   typedef Exchange<TN> Swap;
-  static_assert(2 * kStage >= W * Swap::kBytes);
-  const Swap swap = {lds + wave * Swap::kBytes, lane};
   const int64_t n = n0 + wn * (BN / WN);
-  __syncthreads();                       // (all of the block's operands have been read)
-#pragma unroll
-  for (int j = 0; j < TM; ++j) {
-    const int64_t row = m0 + wm * (BM / WM) + 32 * j;
+  auto finish = [&](int j, int at, const Swap &swap) {
+    const int64_t row = m0 + wm * (BM / WM) + 32 * at;
     if (p.splits == 1) {
       swap.template put_all<T>(acc[j]);
       __builtin_amdgcn_wave_barrier();
@@ -646,18 +648,30 @@ __device__ inline void product_tile(const ProductArgs &p, unsigned block) {
                 f32x4{acc[j][i][4 * q], acc[j][i][4 * q + 1], acc[j][i][4 * q + 2], acc[j][i][4 * q + 3]};
         }
     }
+  };
+  if constexpr (GROUPS == 1) {
+    static_assert(2 * kStage >= W * Swap::kBytes);
+    const Swap swap = {lds + wave * Swap::kBytes, lane};
+    __syncthreads();                     // (all of the block's operands have been read)
+#pragma unroll
+    for (int j = 0; j < TM; ++j) finish(j, j, swap);
+  } else {
+    static_assert(GROUPS == 2 && kHandOver<W> + 2 * W * Swap::kBytes <= 4 * kStage);
+    const Swap swap = {lds_address(stages) + kHandOver<W> + (group * W + wave) * Swap::kBytes, lane};
+    hand_over<W>(lds_address(stages), group, wave, lane, acc);
+    finish(0, group, swap);
   }
 }
 
 // All three products in one launch, so that one kind's tiles fill up the places that the other's leave:
 // first the `head` blocks of the kind with the longer tiles.
-template <class T, int BM, int BN, int WM, int WN>
-__global__ __launch_bounds__(64 * WM * WN, 2) void products_kernel(ProductArgs x, ProductArgs w, int head,
+template <class T, int BM, int BN, int WM, int WN, int GROUPS>
+__global__ __launch_bounds__(64 * WM * WN * GROUPS, 2) void products_kernel(ProductArgs x, ProductArgs w, int head,
                                                                 bool x_first) {
   const bool front = (int)blockIdx.x < head;
   const unsigned block = front ? blockIdx.x : blockIdx.x - head;
-  if (front == x_first) product_tile<T, BM, BN, WM, WN, false, 2>(x, block);
-  else product_tile<T, BM, BN, WM, WN, true, 1>(w, block);
+  if (front == x_first) product_tile<T, BM, BN, WM, WN, GROUPS, false, 2>(x, block);
+  else product_tile<T, BM, BN, WM, WN, GROUPS, true, 1>(w, block);
 }
 
 // out = the sum of the splits' parts, 8 values a thread: dx, dWg and dWu in turn (blockIdx.y).
@@ -742,50 +756,55 @@ hipError_t by_type(const GatedGradArgs &g, char *dg, char *du, hipStream_t s) {
 
 // The products' tiles, and the parts of their summed axes.
 struct Plan {
-  bool big;
+  bool big, groups;
   int sx, sw;                          // parts of dx's and of dW's summed axis
   int64_t nx, nw, lx, lw;              // blocks, and a block's steps
 };
-// Steps of a part at least: 1,021 x 520 x 1,368 with 8 19.6 us and 5.2 for adding the parts, with 16 23.6 and 4.1,
-// with 4 19.8 and 5.5.
+// Steps of a part at least: 1,021 x 520 x 1,368 with one group of wavefronts a tile and 8 19.6 us and 5.2 for adding
+// the parts, with 16 23.6 and 4.1, with 4 19.8 and 5.5; with two groups and 8 19.2 and 4.0, with 16 21.2 and 4.0.
 constexpr int kLeast = 8;
-Plan plan_of(int64_t rows, int64_t width, int64_t hidden, bool big) {
+Plan plan_of(int64_t rows, int64_t width, int64_t hidden, bool big, bool groups) {
   const int size = big ? 256 : 128;
   const int64_t tx = tiles(rows, size) * tiles(width, size), tw = 2 * tiles(hidden, size) * tiles(width, size);
   const int64_t lx = 2 * tiles(hidden, kStep), lw = tiles(rows, kStep);
   // a resident block's share of all steps: longer summed axes are split
-  const int64_t share = std::max<int64_t>(kLeast, tiles(tx * lx + tw * lw, big ? kSeqCus : 2 * kSeqCus));
+  const int64_t places = big || groups ? kSeqCus : 2 * kSeqCus;
+  const int64_t share = std::max<int64_t>(kLeast, tiles(tx * lx + tw * lw, places));
   Plan p;
-  p.big = big;
+  p.big = big, p.groups = groups;
   p.sx = (int)std::max<int64_t>(1, lx / share), p.sw = (int)std::max<int64_t>(1, lw / share);
   p.nx = tx * p.sx, p.nw = tw * p.sw;
   p.lx = tiles(lx, p.sx), p.lw = tiles(lw, p.sw);
   return p;
 }
 // By the time of a step of either size, measured with full tiles: 1.8 us of 256 x 256, one block a compute
-// unit; 1.2 of 128 x 128, two.
+// unit; 1.2 of 128 x 128, two. Two groups of wavefronts a tile where each block has a compute unit of its own and
+// more steps than a few: the gradient of 1,021 x 2,048 x 512 36 us, 49 with one group; 1,024 x 1,024 x 1,024 35 and
+// 41; 1,021 x 520 x 1,368 35.5 and 37.3; 128 x 64 x 64, of two steps, 12.1 and 11.3.
 Plan plan_of(int64_t rows, int64_t width, int64_t hidden) {
-  const Plan a = plan_of(rows, width, hidden, true), b = plan_of(rows, width, hidden, false);
+  const Plan a = plan_of(rows, width, hidden, true, false), b = plan_of(rows, width, hidden, false, false);
   auto time = [](const Plan &p, double step, int places) {
     return step * std::max<double>((double)std::max(p.lx, p.lw), (double)(p.nx * p.lx + p.nw * p.lw) / places);
   };
-  return time(a, 1.8, kSeqCus) <= time(b, 1.2, 2 * kSeqCus) ? a : b;
+  if (time(a, 1.8, kSeqCus) <= time(b, 1.2, 2 * kSeqCus)) return a;
+  const Plan c = plan_of(rows, width, hidden, false, true);
+  return c.nx + c.nw <= kSeqCus && std::max(c.lx, c.lw) > 4 ? c : b;
 }
 size_t part_bytes(const Plan &p, int64_t rows, int64_t width, int64_t hidden, bool x) {
   if (x) return p.sx > 1 ? align256((size_t)p.sx * rows * width * 4) : 0;
   return p.sw > 1 ? align256((size_t)2 * p.sw * hidden * width * 4) : 0;
 }
 
-template <class T, int BM, int BN, int WM, int WN>
+template <class T, int BM, int BN, int WM, int WN, int GROUPS>
 hipError_t launch_products(ProductArgs x, ProductArgs w, const Plan &plan, hipStream_t s) {
-  constexpr int kLds = 2 * (BM + BN) * kStepBytes;
+  constexpr int kLds = 2 * GROUPS * (BM + BN) * kStepBytes;
   static LdsLimit limit;
-  const void *f = reinterpret_cast<const void *>(products_kernel<T, BM, BN, WM, WN>);
+  const void *f = reinterpret_cast<const void *>(products_kernel<T, BM, BN, WM, WN, GROUPS>);
   hipError_t e = limit.set(f, kLds);
   if (e != hipSuccess) return e;
   for (ProductArgs *p : {&x, &w}) p->nm = (int)tiles(p->m, BM), p->nn = (int)tiles(p->n, BN);
   const bool x_first = plan.lx > plan.lw;
-  products_kernel<T, BM, BN, WM, WN><<<(unsigned)(plan.nx + plan.nw), 64 * WM * WN, kLds, s>>>(
+  products_kernel<T, BM, BN, WM, WN, GROUPS><<<(unsigned)(plan.nx + plan.nw), 64 * WM * WN * GROUPS, kLds, s>>>(
       x, w, (int)(x_first ? plan.nx : plan.nw), x_first);
   e = hipGetLastError();
   if (e != hipSuccess || (x.splits == 1 && w.splits == 1)) return e;
@@ -811,8 +830,9 @@ hipError_t gradient(const GatedGradArgs &g, char *ws, hipStream_t s) {
                          {g.dx_row, 0}, px, f.rows, f.width, f.hidden, 0, 0, plan.sx};
   const ProductArgs w = {{f.x, f.x}, {dg, du}, {f.x_row, f.x_row}, {row, row}, {g.dw_gate, g.dw_up},
                          {g.dgate_row, g.dup_row}, pw, f.hidden, f.width, f.rows, 0, 0, plan.sw};
-  return plan.big ? launch_products<T, 256, 256, 2, 4>(x, w, plan, s)
-                  : launch_products<T, 128, 128, 2, 2>(x, w, plan, s);
+  if (plan.big) return launch_products<T, 256, 256, 2, 4, 1>(x, w, plan, s);
+  return plan.groups ? launch_products<T, 128, 128, 2, 2, 2>(x, w, plan, s)
+                     : launch_products<T, 128, 128, 2, 2, 1>(x, w, plan, s);
 }
 
 }  // namespace
