@@ -706,12 +706,11 @@ gp_status gp_gated_grad(const gp_gated_spec *gated, int32_t rows, const gp_matri
  * scales[0], v = e5m2 code x scales[1] (OCP formats). A scale is 2^(k - 7) for m and 2^(k - 14) for
  * v, k the exponent of the largest magnitude, but 2^-126 at least, and 1 where all are 0. A value
  * between two codes takes the upper one if its place between them, in 65536ths, and a random 16-bit
- * number reach 65536 together; an m below its smallest normal code goes to the nearest (upward
- * halfway), a v above 0 never to 0. The random numbers: with E = 256 (blocks of the tensors before)
- * + the value's number in its tensor, word E % 4 of Philox4x32-10 with counter (E / 4 low, E / 4
- * high, t low, 0) and key (seed low, seed high); its low half for m, its high half for v. The step
- * itself takes the m and v that were not rounded yet. A block with a state that is not finite
- * becomes NaN (by its scale). */
+ * number reach 65536 together; an m below an eighth of its lowest code is 0, a v above 0 never.
+ * The random numbers: with E = 256 (blocks of the tensors before) + the value's number in its
+ * tensor, word E % 4 of Philox4x32-10 with counter (E / 4 low, E / 4 high, t low, 0) and key (seed
+ * low, seed high); its low half for m, its high half for v. The step itself takes the m and v that
+ * were not rounded yet. A block with a state that is not finite becomes NaN (by its scale). */
 typedef struct {
   int32_t dtype;         /* gp_dtype of the weights */
   int32_t grad_dtype;    /* of the gradients: dtype or GP_FP32 */

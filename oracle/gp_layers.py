@@ -200,20 +200,20 @@ def _scales(x, top):
 
 def encode(m, v, first, step, seed):
     """Codes and scales [blocks, 2] of fp32 states, by the definition: neighbours on the grid, the
-    place between them in 65536ths."""
+    place between them in 65536ths; an m below an eighth of the lowest code is 0."""
     m, v = np.asarray(m, np.float64), np.asarray(v, np.float64)
     sm, sv = _scales(m, 7), _scales(v, 14)
     rm, rv = state_random(first, len(m), step, seed)
     out = []
-    for x, scale, values, r, lowest in ((np.abs(m), sm, M_GRID, rm, 2.0 ** -6), (v, sv, V_GRID, rv, None)):
+    for x, scale, values, r, least in ((np.abs(m), sm, M_GRID, rm, M_GRID[1] / 8), (v, sv, V_GRID, rv, None)):
         x = x / np.repeat(scale, SHARE)[:len(x)]
         lo = np.searchsorted(values, x, side="right") - 1
         hi = np.minimum(lo + 1, len(values) - 1)
         place = np.where(hi > lo, (x - values[lo]) / np.where(hi > lo, values[hi] - values[lo], 1), 0.0)
-        if lowest is not None:
-            r = np.where(x < lowest, 32768, r)
+        if least is not None:
+            r = np.where(x < least, 0, r)
         code = np.where(place * 65536 + r >= 65536, hi, lo)
-        out.append(np.where((x > 0) & (code == 0), 1, code) if lowest is None else code)
+        out.append(np.where((x > 0) & (code == 0), 1, code) if least is None else code)
     cm = np.where(m < 0, out[0] | 0x80, out[0])
     return cm.astype(np.uint8), out[1].astype(np.uint8), np.stack([sm, sv], 1)
 

@@ -7,9 +7,11 @@
 // States in 8 bits: 256 values share a power of two, so that scaling rounds nothing. m is e4m3 and
 // v e5m2 (v has no sign, but twice its exponent range), rounded to one of the two neighbours at
 // random with the probabilities that keep their mean: rounded to the nearest, an average that moves
-// by a thousandth of the way a step would never leave its code. Where that would do harm it is not
-// random: an m below its smallest normal code goes to the nearest (a code taken by chance could be
-// thousands of times the value, over a root of v just as small), and a v above 0 stays above 0.
+// by a thousandth of the way a step would never leave its code, and one below the smallest normal
+// codes, whose gradient has ended, would never reach 0 while v goes on falling beneath it. Where
+// chance would do harm there is none: a v above 0 stays above 0, so that an m of its lowest code
+// (2^-16 of the largest's) stands over a root of 2^-15 of the largest's at least, and an m below an
+// eighth of its lowest code is 0.
 //
 // Bound by memory: every value is read and written once. A wavefront has 256 values, four a lane, or
 // with 8-bit states two blocks of 256, eight a lane (four a lane, 4 bytes of codes each: 233 us instead of
@@ -21,6 +23,7 @@ namespace {
 
 constexpr int kShare = 256;            // values that share a scale
 constexpr int kWaves = 4;
+constexpr float kLeast = 1.f / 4096;   // scaled m that are rounded at random: an eighth of the lowest code on
 // Values of a lane.
 template <int BITS>
 constexpr int kLane = BITS == 8 ? 8 : 4;
@@ -77,17 +80,16 @@ __device__ inline void scale_of(float big, bool finite, int top, float &scale, f
 }
 
 // The code of |x| on a grid of KEEP bits behind the leading one whose smallest normal number is
-// 2^LOWEST: the upper neighbour if the place between the two, in 65536ths, and r reach 65536;
-// below 2^LOWEST by `below` in r's place.
+// 2^LOWEST: the upper neighbour if the place between the two, in 65536ths, and r reach 65536.
 template <int KEEP, int LOWEST>
-__device__ inline uint32_t code_of(float x, uint32_t r, uint32_t below) {
+__device__ inline uint32_t code_of(float x, uint32_t r) {
   constexpr int kLift = 23 - KEEP;
   if (x >= word_float((uint32_t)(LOWEST + 127) << 23))
     return ((__builtin_bit_cast(uint32_t, x) + (r << (kLift - 16))) >> kLift) -
            ((uint32_t)(LOWEST + 126) << KEEP);
   constexpr float kInv = (float)(1 << (KEEP - LOWEST));
   const float t = x * kInv, whole = floorf(t);           // (all of it exact)
-  return (uint32_t)whole + (t - whole >= (float)(65536 - below) * (1.f / 65536.f));
+  return (uint32_t)whole + (t - whole >= (float)(65536 - r) * (1.f / 65536.f));
 }
 // The value of a code.
 template <int KEEP, int LOWEST>
@@ -234,9 +236,10 @@ __global__ __launch_bounds__(64 * kWaves) void adamw_kernel(AdamArgs a, int64_t 
 #pragma unroll
         for (int n = 0; n < 4; ++n) {
           const uint32_t word = r[n];
-          uint32_t x = code_of<3, -6>(fabsf(m[k + n]) * im, word & 0xffff, 32768);
+          const float scaled = fabsf(m[k + n]) * im;
+          uint32_t x = code_of<3, -6>(scaled, scaled < kLeast ? 0 : word & 0xffff);
           if (m[k + n] < 0.f) x |= 0x80;
-          uint32_t y = code_of<2, -14>(v[k + n] * iv, word >> 16, word >> 16);
+          uint32_t y = code_of<2, -14>(v[k + n] * iv, word >> 16);
           if (v[k + n] > 0.f && y == 0) y = 1;
           cm[k / 4] |= (x & 0xff) << (8 * n);
           cv[k / 4] |= (y & 0xff) << (8 * n);
