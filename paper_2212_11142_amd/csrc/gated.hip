@@ -772,7 +772,8 @@ Plan plan_of(int64_t rows, int64_t width, int64_t hidden, bool big, bool groups)
   const int64_t share = std::max<int64_t>(kLeast, tiles(tx * lx + tw * lw, places));
   Plan p;
   p.big = big, p.groups = groups;
-  p.sx = (int)std::max<int64_t>(1, lx / share), p.sw = (int)std::max<int64_t>(1, lw / share);
+  // (of no rows there is no dx to split: its parts would be added up by a launch without blocks)
+  p.sx = tx > 0 ? (int)std::max<int64_t>(1, lx / share) : 1, p.sw = (int)std::max<int64_t>(1, lw / share);
   p.nx = tx * p.sx, p.nw = tw * p.sw;
   p.lx = tiles(lx, p.sx), p.lw = tiles(lw, p.sw);
   return p;
