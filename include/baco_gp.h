@@ -690,7 +690,8 @@ gp_status gp_gated(const gp_gated_spec *gated, int32_t rows, const gp_matrix *x,
 
 /* Gradients from dout [rows][hidden]: dx, dw_gate, dw_up (0 with no rows), none of them an input.
  * Both projections are formed again; their gradients are rounded to dtype once, as operands of the
- * products that follow. */
+ * products that follow (fp16: times a power of two for each 64 rows x 64 hidden values, so that
+ * what is finite does not leave fp16's range, and 2^-21 of the largest there keeps its digits). */
 size_t gp_gated_grad_workspace_bytes(const gp_gated_spec *gated, int32_t rows);
 gp_status gp_gated_grad(const gp_gated_spec *gated, int32_t rows, const gp_matrix *x,
                         const gp_matrix *w_gate, const gp_matrix *w_up, const gp_matrix *dout,

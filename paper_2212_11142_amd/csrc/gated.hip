@@ -4,7 +4,7 @@
 // as tiled products on the matrix units with fp32 sums. The forward pass has both projections of
 // a tile of hidden values in one block, whose epilogue multiplies them; the gradient forms g and u
 // again in the same way (nothing is kept from the forward pass), its epilogue writes dg and du,
-// rounded once as operands of the three products that follow.
+// rounded once as operands of the three products that follow; in fp16 times a power of two.
 //
 // Tiles. Every product is taken transposed: the result's contiguous axis is the A operand's, so
 // that a lane holds 4 consecutive values of a result's row. A step has 64 of the summed axis; an
@@ -296,13 +296,51 @@ __device__ inline void activation(float z, float &a, float &d) {
   }
 }
 
+// ------------------------------------------------------------------ powers of two
+// dg and du can be far outside of fp16's range where the gradients that come of them are not: each block of
+// 64 rows and 64 hidden values has a power 2^e of its own, with which its largest finite magnitude is
+// in 2^7 .. 2^15, so that what is 2^-21 of it still has all digits. The products' sums are kept at the power of
+// the present step's block, and moved to the next one's where it is another: e goes in steps of 8, so that this is
+// rare. (e of 40 at most: a larger one would save what is below 2^-65, and could bring sums of 2^87 to
+// infinity.) Blocks of zeros have none. 16,384 rows of 1,024 x 4,096, gradient: 811 us, 772 without powers, 890 where
+// every block has another than the next.
+template <class T>
+constexpr bool kPowers = false;
+template <>
+constexpr bool kPowers<Fp16> = true;
+constexpr int kNoPower = 127, kMaxPower = 40, kPowerBlock = 64;
+
+__device__ inline int power_of(float most) {
+  const int k = (int)(__builtin_bit_cast(uint32_t, most) >> 23) - 127;
+  return most > 0.f ? min((14 - k) >> 3 << 3, kMaxPower) : kNoPower;
+}
+__device__ inline float two_to(int e) { return e == kNoPower ? 1.f : word_float((uint32_t)(e + 127) << 23); }
+
+// Largest finite magnitude of N sums, over the wavefront: with 0 times itself added, what is not finite is NaN,
+// which fmaxf passes over.
+template <int N>
+__device__ inline float most_of(const f32x16 *x) {
+  float m = 0.f;
+#pragma unroll
+  for (int i = 0; i < N; ++i)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) m = fmaxf(m, fmaf(fabsf(x[i][r]), 0.f, fabsf(x[i][r])));
+  return wave_max(m);
+}
+
 // ------------------------------------------------------------------ both projections
+// What the gradient's products read: dg and du [rows][hidden], and their blocks' exponents [2][rows / 64][hidden / 64]
+// (fp16).
+struct HiddenGrads {
+  char *dg, *du;
+  int32_t *powers;
+};
 // BM rows of x and BN / 2 hidden values per block, WM x WN wavefronts, each of 32 C hidden values. With
 // GROUPS 2 a block has two such groups of wavefronts, each with half of the summed axis and places in LDS of
 // its own, and one tile: where tiles are few, what counts is how long a step takes, not how many run at once.
 // The groups hand each other half of their sums in the end.
 template <class T, int BM, int BN, int WM, int WN, int GROUPS, int ACT, bool GRAD>
-__global__ __launch_bounds__(64 * WM * WN * GROUPS, 2) void gated_kernel(GatedGradArgs g, char *dg, char *du,
+__global__ __launch_bounds__(64 * WM * WN * GROUPS, 2) void gated_kernel(GatedGradArgs g, HiddenGrads to,
                                                                       int nm, int nn) {
   constexpr int W = WM * WN, TM = BM / 32 / WM, C = BN / 64 / WN;
   extern __shared__ char stages[];
@@ -337,8 +375,8 @@ __global__ __launch_bounds__(64 * WM * WN * GROUPS, 2) void gated_kernel(GatedGr
   struct Operands {
     u32x4 w[2][C], x[TM];
   };
-  // what becomes of sums j: rows 32 at .. of a wavefront's of tile `of`
-  auto finish = [&](int j, int at, const Tile &of, const Swap &swap) {
+  // The gradient: sums j become dg and du of rows 32 at .. of a wavefront's of tile `of` ...
+  auto form = [&](int j, int at, const Tile &of, const Swap &swap) {
     const int64_t n = (int64_t)of.n * (BN / 2) + 32 * C * wn, bytes = 2 * (a.hidden - n);
     const int64_t row = (int64_t)of.m * BM + wm * (BM / WM) + 32 * at, rows = a.rows - row;
     f32x16 *u = acc[j][0], *v = acc[j][1];
@@ -370,15 +408,28 @@ __global__ __launch_bounds__(64 * WM * WN * GROUPS, 2) void gated_kernel(GatedGr
             v[c][4 * q + r] = y[r] * f;
           }
         }
-      const int64_t stride = (int64_t)a.hidden * 2, to = row * stride + 2 * n;
       __builtin_amdgcn_wave_barrier();
+    }
+  };
+  // ... which are scaled and stored; else the forward pass's results.
+  float scale_g = 1.f, scale_u = 1.f;
+  auto finish = [&](int j, int at, const Tile &of, const Swap &swap) {
+    const int64_t n = (int64_t)of.n * (BN / 2) + 32 * C * wn, bytes = 2 * (a.hidden - n);
+    const int64_t row = (int64_t)of.m * BM + wm * (BM / WM) + 32 * at, rows = a.rows - row;
+    f32x16 *u = acc[j][0], *v = acc[j][1];
+    if constexpr (GRAD) {
+      if constexpr (kPowers<T>)
+#pragma unroll
+        for (int c = 0; c < C; ++c) u[c] *= scale_g, v[c] *= scale_u;
+      const int64_t stride = (int64_t)a.hidden * 2, offset = row * stride + 2 * n;
       swap.template put_all<T>(u);
       __builtin_amdgcn_wave_barrier();
-      swap.store(dg + to, stride, rows, bytes);
+      swap.store(to.dg + offset, stride, rows, bytes);
       __builtin_amdgcn_wave_barrier();
       swap.template put_all<T>(v);
       __builtin_amdgcn_wave_barrier();
-      swap.store(du + to, stride, rows, bytes);
+      swap.store(to.du + offset, stride, rows, bytes);
+      __builtin_amdgcn_wave_barrier();
     } else {
 #pragma unroll
       for (int c = 0; c < C; ++c)
@@ -391,6 +442,41 @@ __global__ __launch_bounds__(64 * WM * WN * GROUPS, 2) void gated_kernel(GatedGr
       swap.template put_all<T>(u);
       __builtin_amdgcn_wave_barrier();
       swap.store(a.out + row * a.out_row + 2 * n, a.out_row, rows, bytes);
+    }
+  };
+  // The powers of the dg and du that a wavefront has formed in sums 0 .. SUMS - 1; a block of 64 x 64 is one
+  // wavefront's, or of all that have its rows.
+  constexpr int SUMS = GROUPS > 1 ? 1 : TM;
+  auto find_powers = [&](const Tile &of) {
+    if constexpr (GRAD && kPowers<T>) {
+      static_assert(BM / WM == kPowerBlock && (C == 2 || (C == 1 && WN == 2)));
+      float big[2] = {0.f, 0.f};
+#pragma unroll
+      for (int j = 0; j < SUMS; ++j)
+#pragma unroll
+        for (int q = 0; q < 2; ++q) {
+          big[q] = fmaxf(big[q], most_of<C>(acc[j][q]));
+          __builtin_amdgcn_sched_barrier(0);
+        }
+      if constexpr (C == 1) {
+        // (behind the stages, whose addresses are multiples of their rows' swizzles)
+        typedef __attribute__((address_space(3))) float lds_float;
+        lds_float *most = (lds_float *)(uintptr_t)(lds_address(stages) + 2 * GROUPS * kStage);
+        if (lane < 2) most[2 * (group * W + wave) + lane] = big[lane];
+        asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+#pragma unroll
+        for (int q = 0; q < 2; ++q)
+#pragma unroll
+          for (int i = 0; i < GROUPS * WN; ++i)
+            big[q] = fmaxf(big[q], most[2 * (i / WN * W + wm * WN + i % WN) + q]);
+      }
+      const int eg = uniform(power_of(big[0])), eu = uniform(power_of(big[1]));
+      scale_g = two_to(eg), scale_u = two_to(eu);
+      const int64_t nr = (a.rows + kPowerBlock - 1) / kPowerBlock, nh = (a.hidden + kPowerBlock - 1) / kPowerBlock;
+      const int64_t r = (int64_t)of.m * (BM / kPowerBlock) + wm;
+      const int64_t h = ((int64_t)of.n * (BN / 2) + 32 * C * wn) / kPowerBlock;
+      if (lane < 2 && group == 0 && (C == 2 || wn == 0) && r < nr && h < nh)
+        to.powers[(lane * nr + r) * nh + h] = lane ? eu : eg;
     }
   };
   // a tile's steps follow those of the block's tile before without a pause. Each row of tiles starts at
@@ -444,11 +530,22 @@ __global__ __launch_bounds__(64 * WM * WN * GROUPS, 2) void gated_kernel(GatedGr
         if (GROUPS > 1 || --left) return false;
         left = steps;
         // (x's part of the stage: its copies go out last, after the block has met)
-        const Swap swap = {lds + stage * kStage + 2 * kHalf + wave * Swap::kBytes, lane};
+        int here = lane;
+        if (GRAD) asm volatile("" : "+v"(here));         // (addresses are made here, not kept through the steps)
+        const Swap swap = {lds + stage * kStage + 2 * kHalf + wave * Swap::kBytes, here};
+        if constexpr (GRAD && kPowers<T>) {
+#pragma unroll
+          for (int j = 0; j < TM; ++j) {
+            form(j, j, t, swap);
+            __builtin_amdgcn_sched_barrier(0);           // (one at a time: registers)
+          }
+          find_powers(t);
+        }
 #pragma unroll
         for (int j = 0; j < TM; ++j) {
+          if constexpr (!kPowers<T>) form(j, j, t, swap);
           finish(j, j, t, swap);
-          __builtin_amdgcn_sched_barrier(0);             // (one at a time: registers)
+          __builtin_amdgcn_sched_barrier(0);
         }
         current += gridDim.x;
         if (current < all) t = tile_of(current, all, nm, nn);
@@ -461,6 +558,8 @@ __global__ __launch_bounds__(64 * WM * WN * GROUPS, 2) void gated_kernel(GatedGr
     static_assert(kHandOver<W> + 2 * W * Swap::kBytes <= 4 * kStage);
     const Swap swap = {lds_address(stages) + kHandOver<W> + (group * W + wave) * Swap::kBytes, lane};
     hand_over<W>(lds_address(stages), group, wave, lane, reinterpret_cast<f32x16 (&)[2][2]>(acc));
+    form(0, group, t, swap);
+    find_powers(t);
     finish(0, group, t, swap);
   }
 }
@@ -556,6 +655,10 @@ struct ProductArgs {
   char *out[2];
   int64_t out_row[2];
   float *part;                         // [output][split][m][n] fp32, with splits
+  // fp16: exponents of B's blocks, one for 64 of m and a step: of the segment or output with power_all,
+  // power_m and power_k apart
+  const int32_t *powers;
+  int64_t power_all, power_m, power_k;
   int64_t m, n, k;
   int nm, nn, splits;
 };
@@ -594,6 +697,37 @@ __device__ inline void product_tile(const ProductArgs &p, unsigned block) {
   struct Operands {
     u32x4 a[TN], b[TM];
   };
+  // The power that a wavefront's sums are kept at, for each 64 of its m, and that of the next step. (Through the
+  // constant address space: scalar loads, which no copy has to be waited for.)
+  constexpr int POWERS = kPowers<T> ? BM / WM / kPowerBlock : 0;
+  typedef __attribute__((address_space(4))) const int32_t const_int;
+  int power[POWERS + 1] = {}, coming[POWERS + 1] = {};
+  auto fetch = [&](int i) {
+    if (POWERS == 0 || first + i >= end) return;
+    int step = first + i + skew;
+    step = step >= end ? step - (end - first) : step;
+    const int of = SEGMENTS == 2 ? step >= per : output;
+    step -= SEGMENTS == 2 ? of * per : 0;
+#pragma unroll
+    for (int q = 0; q < POWERS; ++q) {
+      const int64_t block = min((m0 + wm * (BM / WM)) / kPowerBlock + q, (p.m - 1) / kPowerBlock);
+      coming[q] = ((const_int *)(uintptr_t)p.powers)[of * p.power_all + block * p.power_m + step * p.power_k];
+    }
+  };
+  // sums j .. of a 64 of m times 2^e
+  auto lift = [&](int q, int e) {
+    constexpr int kSums = kPowerBlock / 32;
+#pragma unroll
+    for (int j = q * kSums; j < (q + 1) * kSums; ++j)
+#pragma unroll
+      for (int i = 0; i < TN; ++i)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) acc[j][i][r] = __builtin_amdgcn_ldexpf(acc[j][i][r], e);
+  };
+  fetch(0);
+#pragma unroll
+  for (int q = 0; q < POWERS; ++q) power[q] = coming[q] == kNoPower ? 0 : coming[q];
+  fetch(1);
   bool on = true;                        // copies of a step that there is, from k0 on
   int64_t k0 = 0;
   run_steps<Operands, ASide::kCopies + BSide::kCopies, TM * TN, TN + TM>(
@@ -625,7 +759,18 @@ __device__ inline void product_tile(const ProductArgs &p, unsigned block) {
       [&](const Operands &o, int i) {
         acc[i / TN][i % TN] = T::mfma(o.a[i % TN], o.b[i / TN], acc[i / TN][i % TN]);
       },
-      [](int64_t, int) { return false; });
+      [&](int64_t i, int) {
+#pragma unroll
+        for (int q = 0; q < POWERS; ++q)
+          if (coming[q] != power[q] && coming[q] != kNoPower) {
+            lift(q, coming[q] - power[q]);
+            power[q] = coming[q];
+          }
+        fetch((int)i + 2);
+        return false;
+      });
+#pragma unroll
+  for (int q = 0; q < POWERS; ++q) lift(q, -power[q]);
   typedef Exchange<TN> Swap;
   const int64_t n = n0 + wn * (BN / WN);
   auto finish = [&](int j, int at, const Swap &swap) {
@@ -708,8 +853,9 @@ bool use_groups(int64_t rows, int64_t width, int64_t hidden) {
 }
 
 template <class T, int BM, int BN, int WM, int WN, int GROUPS, int ACT, bool GRAD>
-hipError_t launch_projections(const GatedGradArgs &g, char *dg, char *du, hipStream_t s) {
-  constexpr int kLds = 2 * GROUPS * (BM + BN) * kStepBytes, kResident = kLdsBytes / kLds * kSeqCus;
+hipError_t launch_projections(const GatedGradArgs &g, const HiddenGrads &to, hipStream_t s) {
+  constexpr int kMost = GRAD && kPowers<T> ? 2 * GROUPS * WM * WN * 4 : 0;
+  constexpr int kLds = 2 * GROUPS * (BM + BN) * kStepBytes + kMost, kResident = kLdsBytes / kLds * kSeqCus;
   static LdsLimit limit;
   const void *f = reinterpret_cast<const void *>(gated_kernel<T, BM, BN, WM, WN, GROUPS, ACT, GRAD>);
   const hipError_t e = limit.set(f, kLds);
@@ -717,7 +863,7 @@ hipError_t launch_projections(const GatedGradArgs &g, char *dg, char *du, hipStr
   const int nm = (int)tiles(g.f.rows, BM), nn = (int)tiles(g.f.hidden, BN / 2);
   gated_kernel<T, BM, BN, WM, WN, GROUPS, ACT, GRAD>
       <<<(unsigned)(GROUPS > 1 ? nm * nn : std::min(nm * nn, kResident)), 64 * WM * WN * GROUPS, kLds, s>>>(
-          g, dg, du, nm, nn);
+          g, to, nm, nn);
   return hipGetLastError();
 }
 // Whether the weights stream past the rows: up to 32 rows, and more where a block for each 16 hidden values and
@@ -733,25 +879,23 @@ hipError_t launch_few(const GatedArgs &a, hipStream_t s) {
   return hipGetLastError();
 }
 template <class T, int ACT, bool GRAD>
-hipError_t projections(const GatedGradArgs &g, char *dg, char *du, hipStream_t s) {
+hipError_t projections(const GatedGradArgs &g, const HiddenGrads &to, hipStream_t s) {
   if (!GRAD && use_few(g.f.rows, g.f.hidden)) {
     if (g.f.rows <= 16) return launch_few<T, 1, ACT>(g.f, s);
     if (g.f.rows <= 32) return launch_few<T, 2, ACT>(g.f, s);
     return launch_few<T, 4, ACT>(g.f, s);
   }
   if (use_big(g.f.rows, g.f.hidden))
-    return launch_projections<T, 256, 256, 4, 2, 1, ACT, GRAD>(g, dg, du, s);
+    return launch_projections<T, 256, 256, 4, 2, 1, ACT, GRAD>(g, to, s);
   if (use_groups(g.f.rows, g.f.width, g.f.hidden))
-    return launch_projections<T, 128, 128, 2, 2, 2, ACT, GRAD>(g, dg, du, s);
-  return launch_projections<T, 128, 128, 2, 2, 1, ACT, GRAD>(g, dg, du, s);
+    return launch_projections<T, 128, 128, 2, 2, 2, ACT, GRAD>(g, to, s);
+  return launch_projections<T, 128, 128, 2, 2, 1, ACT, GRAD>(g, to, s);
 }
 template <bool GRAD>
-hipError_t by_type(const GatedGradArgs &g, char *dg, char *du, hipStream_t s) {
+hipError_t by_type(const GatedGradArgs &g, const HiddenGrads &to, hipStream_t s) {
   if (g.f.fp16)
-    return g.f.act == kSilu ? projections<Fp16, kSilu, GRAD>(g, dg, du, s)
-                            : projections<Fp16, kGelu, GRAD>(g, dg, du, s);
-  return g.f.act == kSilu ? projections<Bf16, kSilu, GRAD>(g, dg, du, s)
-                          : projections<Bf16, kGelu, GRAD>(g, dg, du, s);
+    return g.f.act == kSilu ? projections<Fp16, kSilu, GRAD>(g, to, s) : projections<Fp16, kGelu, GRAD>(g, to, s);
+  return g.f.act == kSilu ? projections<Bf16, kSilu, GRAD>(g, to, s) : projections<Bf16, kGelu, GRAD>(g, to, s);
 }
 
 // The products' tiles, and the parts of their summed axes.
@@ -796,6 +940,10 @@ size_t part_bytes(const Plan &p, int64_t rows, int64_t width, int64_t hidden, bo
   return p.sw > 1 ? align256((size_t)2 * p.sw * hidden * width * 4) : 0;
 }
 
+size_t power_bytes(int64_t rows, int64_t hidden) {
+  return align256((size_t)2 * tiles(rows, kPowerBlock) * tiles(hidden, kPowerBlock) * 4);
+}
+
 template <class T, int BM, int BN, int WM, int WN, int GROUPS>
 hipError_t launch_products(ProductArgs x, ProductArgs w, const Plan &plan, hipStream_t s) {
   constexpr int kLds = 2 * GROUPS * (BM + BN) * kStepBytes;
@@ -820,17 +968,21 @@ hipError_t gradient(const GatedGradArgs &g, char *ws, hipStream_t s) {
   const Plan plan = plan_of(f.rows, f.width, f.hidden);
   const size_t hidden_bytes = align256((size_t)f.rows * f.hidden * 2);
   char *dg = ws, *du = ws + hidden_bytes;
-  float *px = reinterpret_cast<float *>(ws + 2 * hidden_bytes);
-  float *pw = reinterpret_cast<float *>(ws + 2 * hidden_bytes + part_bytes(plan, f.rows, f.width, f.hidden, true));
+  ws += 2 * hidden_bytes;
+  int32_t *powers = reinterpret_cast<int32_t *>(ws);
+  ws += f.fp16 ? power_bytes(f.rows, f.hidden) : 0;
+  float *px = reinterpret_cast<float *>(ws);
+  float *pw = reinterpret_cast<float *>(ws + part_bytes(plan, f.rows, f.width, f.hidden, true));
   const int64_t row = (int64_t)f.hidden * 2;
+  const int64_t nr = tiles(f.rows, kPowerBlock), nh = tiles(f.hidden, kPowerBlock);
   if (f.rows > 0) {
-    const hipError_t e = by_type<true>(g, dg, du, s);
+    const hipError_t e = by_type<true>(g, {dg, du, powers}, s);
     if (e != hipSuccess) return e;
   }
   const ProductArgs x = {{f.w_gate, f.w_up}, {dg, du}, {f.gate_row, f.up_row}, {row, row}, {g.dx, nullptr},
-                         {g.dx_row, 0}, px, f.rows, f.width, f.hidden, 0, 0, plan.sx};
+                         {g.dx_row, 0}, px, powers, nr * nh, nh, 1, f.rows, f.width, f.hidden, 0, 0, plan.sx};
   const ProductArgs w = {{f.x, f.x}, {dg, du}, {f.x_row, f.x_row}, {row, row}, {g.dw_gate, g.dw_up},
-                         {g.dgate_row, g.dup_row}, pw, f.hidden, f.width, f.rows, 0, 0, plan.sw};
+                         {g.dgate_row, g.dup_row}, pw, powers, nr * nh, 1, nh, f.hidden, f.width, f.rows, 0, 0, plan.sw};
   if (plan.big) return launch_products<T, 256, 256, 2, 4, 1>(x, w, plan, s);
   return plan.groups ? launch_products<T, 128, 128, 2, 2, 2>(x, w, plan, s)
                      : launch_products<T, 128, 128, 2, 2, 1>(x, w, plan, s);
@@ -842,7 +994,7 @@ hipError_t launch_gated(const GatedArgs &a, hipStream_t s) {
   if (a.rows == 0) return hipSuccess;
   GatedGradArgs g = {};
   g.f = a;
-  return by_type<false>(g, nullptr, nullptr, s);
+  return by_type<false>(g, HiddenGrads{}, s);
 }
 
 bool gated_fits(int64_t rows, int64_t width, int64_t hidden, bool grad) {
@@ -856,9 +1008,10 @@ bool gated_fits(int64_t rows, int64_t width, int64_t hidden, bool grad) {
   return ok;
 }
 
-size_t gated_grad_bytes(int32_t rows, int32_t width, int32_t hidden) {
+size_t gated_grad_bytes(int32_t rows, int32_t width, int32_t hidden, bool fp16) {
   const Plan p = plan_of(rows, width, hidden);
-  return 2 * align256((size_t)rows * hidden * 2) + part_bytes(p, rows, width, hidden, true) +
+  return 2 * align256((size_t)rows * hidden * 2) + (fp16 ? power_bytes(rows, hidden) : 0) +
+         part_bytes(p, rows, width, hidden, true) +
          part_bytes(p, rows, width, hidden, false);
 }
 

@@ -69,7 +69,7 @@ struct GatedGradArgs {
 };
 // whether the products' grids are within a launch's limits
 bool gated_fits(int64_t rows, int64_t width, int64_t hidden, bool grad);
-size_t gated_grad_bytes(int32_t rows, int32_t width, int32_t hidden);
+size_t gated_grad_bytes(int32_t rows, int32_t width, int32_t hidden, bool fp16);
 hipError_t launch_gated_grad(const GatedGradArgs &a, void *ws, hipStream_t s);
 
 constexpr int kAdamTensors = 48;       // tensors of a launch: what its arguments hold

@@ -296,7 +296,7 @@ size_t gp_gated_grad_workspace_bytes(const gp_gated_spec *t, int32_t rows) {
   size_t n = SIZE_MAX;
   guarded([&] {
     const gp_status st = check_gated(t, rows, true);
-    if (st == GP_OK) n = gated_grad_bytes(rows, t->width, t->hidden);
+    if (st == GP_OK) n = gated_grad_bytes(rows, t->width, t->hidden, t->dtype == GP_FP16);
     return st;
   });
   return n;
@@ -316,7 +316,8 @@ gp_status gp_gated_grad(const gp_gated_spec *t, int32_t rows, const gp_matrix *x
     if (st == GP_OK) st = check_matrix(dw_gate, t->hidden, t->width, true, "dw_gate");
     if (st == GP_OK) st = check_matrix(dw_up, t->hidden, t->width, true, "dw_up");
     if (st != GP_OK) return st;
-    st = check_workspace(workspace, ws_bytes, gated_grad_bytes(rows, t->width, t->hidden));
+    st = check_workspace(workspace, ws_bytes,
+                         gated_grad_bytes(rows, t->width, t->hidden, t->dtype == GP_FP16));
     if (st != GP_OK) return st;
     GatedGradArgs g;
     std::memset(&g, 0, sizeof g);
