@@ -34,20 +34,24 @@ LOW, HIGH = -4.0, 4.0                       # range of the bins (standardised ou
 
 
 # ------------------------------------------------------------------ the operators in autograd
+# (A context keeps a call's buffers without its outputs: those belong to the graph, whose node belongs to them and
+# has the context, a cycle that would keep each step's buffers. What the gradient reads of them is saved.)
 class Attend(torch.autograd.Function):
     @staticmethod
     def forward(ctx, att, q, k, v, table):
         bufs = seq.AttendBuffers(att, grad=True)
         seq.attend_into(att, q, k, v, bufs, table=table)
+        out, bufs.out = bufs.out, None
         ctx.att, ctx.bufs = att, bufs
-        ctx.save_for_backward(q, k, v, table)
-        return bufs.out
+        ctx.save_for_backward(q, k, v, table, out)
+        return out
 
     @staticmethod
     def backward(ctx, dout):
-        q, k, v, table = ctx.saved_tensors
         b = ctx.bufs
+        q, k, v, table, b.out = ctx.saved_tensors
         seq.attend_grad_into(ctx.att, q, k, v, dout.contiguous(), b, table=table)
+        b.out = None
         return None, b.dq, b.dk, b.dv, b.dtable
 
 
@@ -58,16 +62,18 @@ class Logprob(torch.autograd.Function):
     def forward(ctx, logits, targets):
         bufs = seq.LogprobBuffers(*logits.shape, logits.dtype, grad=True)
         seq.logprob_into(logits, targets, bufs)
+        logp, entropy, bufs.logp, bufs.entropy = bufs.logp, bufs.entropy, None, None
         ctx.bufs = bufs
-        ctx.save_for_backward(logits, targets)
-        return bufs.logp, bufs.entropy
+        ctx.save_for_backward(logits, targets, entropy)
+        return logp, entropy
 
     @staticmethod
     def backward(ctx, g_logp, g_entropy):
-        logits, targets = ctx.saved_tensors
-        seq.logprob_grad_into(logits, targets, g_logp.contiguous(), g_entropy.contiguous(),
-                              ctx.bufs)
-        return ctx.bufs.dlogits, None
+        b = ctx.bufs
+        logits, targets, b.entropy = ctx.saved_tensors
+        seq.logprob_grad_into(logits, targets, g_logp.contiguous(), g_entropy.contiguous(), b)
+        b.entropy = None
+        return b.dlogits, None
 
 
 class Norm(torch.autograd.Function):
@@ -77,9 +83,10 @@ class Norm(torch.autograd.Function):
     def forward(ctx, norm, x, residual, weight, bias):
         bufs = layers.NormBuffers(norm, x.shape[0], residual=residual is not None, grad=True)
         layers.norm_into(norm, x, bufs, weight=weight, bias=bias, residual=residual)
+        out, total, bufs.out, bufs.sum = bufs.out, bufs.sum, None, None
         ctx.norm, ctx.bufs = norm, bufs
-        ctx.save_for_backward(x if residual is None else bufs.sum, weight)
-        return bufs.out if residual is None else (bufs.out, bufs.sum)
+        ctx.save_for_backward(x if residual is None else total, weight)
+        return out if residual is None else (out, total)
 
     @staticmethod
     def backward(ctx, dout, dsum=None):
@@ -87,7 +94,7 @@ class Norm(torch.autograd.Function):
         b = ctx.bufs
         layers.norm_grad_into(ctx.norm, h, dout.contiguous(), b, weight=weight,
                               dsum=None if dsum is None else dsum.contiguous())
-        return None, b.dx, b.dx if b.sum is not None else None, b.dweight, b.dbias
+        return None, b.dx, b.dx if ctx.needs_input_grad[2] else None, b.dweight, b.dbias
 
 
 class Rotate(torch.autograd.Function):
