@@ -456,13 +456,17 @@ class AdamW:
         self._update()
 
     def _update(self):
-        """The weights' addresses, as they are now: a weight's storage may have been replaced."""
+        """The weights' addresses, as they are now: a weight's storage may have been replaced, also by
+        another view of the same memory or by what the allocator has put in its place."""
         torch = _torch()
-        at = list(map(torch.Tensor.data_ptr, self._weights))
-        if at == self._at and all(map(torch.Tensor.is_contiguous, self._weights)):
+        weights, n = self._weights, len(self.params)
+        copies = len(weights) - n
+        at = list(map(torch.Tensor.data_ptr, weights))
+        if at == self._at and all(map(torch.Tensor.is_contiguous, weights)) and \
+                list(map(_shape, weights)) == (self.shapes * 2 if copies else self.shapes) and \
+                list(map(_dtype, weights)) == [self.dtype] * n + [torch.float32] * copies:
             return
         self._at = None
-        n = len(self.params)
         for i, t in enumerate(self.tensors):
             p = self.params[i]
             if p.dtype is not self.dtype or p.get_device() != self.device or not p.is_contiguous() or \
