@@ -404,7 +404,11 @@ class AdamW:
 
     The states lie one tensor after another in m_all and v_all [blocks, 256] (and scales_all
     [blocks, 2]), each from a block of its own on; m, v and scales are views of them. They start at
-    0; a checkpoint keeps the *_all tensors and the caller's step."""
+    0; a checkpoint keeps the *_all tensors and the caller's step, and is copied into them: the library
+    has their addresses."""
+
+    m_all, v_all, scales_all, m, v, scales = (
+        property(operator.attrgetter("_" + name)) for name in ("m_all", "v_all", "scales_all", "m", "v", "scales"))
 
     def __init__(self, params, masters=None, state_bits: int = 32, grad_dtype=None):
         torch = _torch()
@@ -428,20 +432,20 @@ class AdamW:
         for n in counts:
             first.append(first[-1] + -(-n // SHARE))
         kinds = (torch.float8_e4m3fn, torch.float8_e5m2) if state_bits == 8 else (torch.float32,) * 2
-        self.m_all, self.v_all = (
+        self._m_all, self._v_all = (
             torch.zeros((first[-1], SHARE * k.itemsize), dtype=torch.uint8, device=dev).view(k)
             for k in kinds)
 
         def views(x):
             flat = x.view(-1)
-            return [flat[SHARE * a:SHARE * a + n].view(p.shape)
-                    for a, n, p in zip(first, counts, self.params)]
+            return tuple(flat[SHARE * a:SHARE * a + n].view(p.shape)
+                         for a, n, p in zip(first, counts, self.params))
 
-        self.m, self.v = views(self.m_all), views(self.v_all)
-        self.scales_all = self.scales = None
+        self._m, self._v = views(self.m_all), views(self.v_all)
+        self._scales_all = self._scales = None
         if state_bits == 8:
-            self.scales_all = torch.ones((first[-1], 2), dtype=torch.float32, device=dev)
-            self.scales = [self.scales_all[a:b] for a, b in zip(first, first[1:])]
+            self._scales_all = torch.ones((first[-1], 2), dtype=torch.float32, device=dev)
+            self._scales = tuple(self.scales_all[a:b] for a, b in zip(first, first[1:]))
         s = gp._AdamW()
         s.dtype, s.grad_dtype, s.state_bits = _dtype_code(self.dtype), _dtype_code(self.grad_dtype), state_bits
         self.struct, self.ref = s, C.byref(s)

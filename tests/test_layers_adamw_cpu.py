@@ -48,3 +48,11 @@ def test_master_copies_that_change_at_the_same_address(change):
             o._update()
     w.data = keep
     o._update()
+
+
+@pytest.mark.parametrize("name", ["m", "v", "scales", "m_all", "v_all", "scales_all"])
+def test_states_are_copied_into(name):
+    """The library has their addresses: a tensor put in their place would not be used."""
+    o = layers.AdamW.__new__(layers.AdamW)
+    with pytest.raises(AttributeError):
+        setattr(o, name, torch.zeros(3))
