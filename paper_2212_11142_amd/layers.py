@@ -5,7 +5,8 @@ each with its gradient, and a step of AdamW over many tensors.
 As in ``seq``, this module only marshals arguments. A description is made once, buffers once per
 use; the `*_into` calls are asynchronous on the current stream, and the plain calls allocate their
 outputs. A call's buffers belong to one stream at a time; threads may share a description, each with
-buffers of its own.
+buffers of its own. No call records a graph: gradients have calls of their own, for a
+torch.autograd.Function, and the plain calls refuse tensors that ask for one outside of it.
 """
 from __future__ import annotations
 
@@ -42,6 +43,13 @@ def _vector(x, shape, dtype, device, name):
         raise ValueError(f"{name} must be a contiguous {dtype} tensor of shape {tuple(shape)} on "
                          f"cuda:{device}")
     return x.data_ptr()
+
+
+def _no_graph(*tensors):
+    """For calls whose results have no graph: they would lose a gradient without a word."""
+    if _torch().is_grad_enabled() and any(x is not None and x.requires_grad for x in tensors):
+        raise ValueError("a tensor requires a gradient, and the result would have no graph: call within a "
+                         "torch.autograd.Function, or under torch.no_grad()")
 
 
 def _workspace_size(n):
@@ -126,6 +134,7 @@ def norm_into(norm: Norm, x, bufs: NormBuffers, weight=None, bias=None, residual
 
 
 def norm(norm: Norm, x, weight=None, bias=None, residual=None) -> dict:
+    _no_graph(x, weight, bias, residual)
     bufs = NormBuffers(norm, x.shape[0], residual=residual is not None,
                        device=x.get_device() if x.is_cuda else None)
     norm_into(norm, x, bufs, weight, bias, residual)
@@ -273,6 +282,7 @@ def rotate_into(rotary: Rotary, positions, x, out, inverse: bool = False):
 
 
 def rotate(rotary: Rotary, positions, x, inverse: bool = False):
+    _no_graph(x)
     out = _torch().empty(x.shape, dtype=x.dtype, device=x.device)
     rotate_into(rotary, positions, x, out, inverse)
     return out
@@ -370,6 +380,7 @@ def gated_into(gated: Gated, x, w_gate, w_up, bufs: GatedBuffers):
 
 
 def gated(gated: Gated, x, w_gate, w_up):
+    _no_graph(x, w_gate, w_up)
     bufs = GatedBuffers(gated, x.shape[0], device=x.get_device() if x.is_cuda else None)
     gated_into(gated, x, w_gate, w_up, bufs)
     return bufs.out
