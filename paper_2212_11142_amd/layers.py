@@ -499,7 +499,19 @@ class AdamW:
         ends = sorted((a, a + w.numel() * w.element_size()) for a, w in zip(at, self._weights) if a)
         if any(end > begin for (_, end), (begin, _) in zip(ends, ends[1:])):
             raise ValueError("weights (and master copies) must not share memory")
+        self._uncounted = any(map(torch.Tensor.is_inference, weights))
         self._at = at
+
+    def _count(self, grads):
+        """Raises the version counters of the weights that were changed: autograd refuses to use what it
+        saved of them before."""
+        changed = self._weights
+        if any(g is None for g in grads):
+            grads = list(grads) * (1 if self.masters is None else 2)
+            changed = [w for w, g in zip(changed, grads) if g is not None]
+        if self._uncounted:
+            changed = [w for w in changed if not w.is_inference()]
+        _torch().autograd.graph.increment_version(changed)
 
     def _gradients(self, grads):
         """Their addresses, 0 for none. (map over a method: a loop of checks would cost 17 us for 28
@@ -555,3 +567,4 @@ def adamw_into(opt: AdamW, grads, lr, step, betas=(0.9, 0.999), eps: float = 1e-
     if factor is not None:
         s.factor = _scalar(factor, torch.float32, dev, "factor")
     _call(dev, opt.lib.gp_adamw, (C.byref(s), len(grads), opt.tensors, at, _stream(opt.params[0])))
+    opt._count(grads)
