@@ -126,7 +126,7 @@ def gated_grad(x, w_gate, w_up, dout, kind):
 def gated_bounds(x, w_gate, w_up, dout, kind, half):
     """What fp32, and in the gradient one rounding of dg and du to a type of half step `half`, may take
     from out, dx, dw_gate and dw_up. A sum of n products is off by n F32 of their sizes; the activations
-    by 2e-6 + 2 F32 z^2 of themselves (a fit to 6.4e-7, an exponential whose argument is rounded,
+    by 2e-6 + 2 F32 z^2 of themselves (a fit to 6.6e-7, an exponential whose argument is rounded,
     a reciprocal, and products); the derivative as much of 1 + |z|."""
     x, wg, wu, dout = (np.asarray(v, np.float64) for v in (x, w_gate, w_up, dout))
     n = x.shape[1]

@@ -271,8 +271,8 @@ constexpr int kSilu = 0, kGelu = 1;   // GP_SILU, GP_GELU
 
 // act(z) and its derivative. gelu: z Phi(z), where
 // Phi(-|z|) = 1/2 erfc(|z| / sqrt(2)) = e^(-z^2 / 2) t q(t) / 2, t = 1 / (1 + 0.375 |z| / sqrt(2)), q a least-maximum
-// fit of degree 6 to e^(x^2) erfc(x) / t with a relative error of 6.4e-7: the tail keeps its digits, and the
-// derivative has the same exponential.
+// fit of degree 6 to e^(x^2) erfc(x) / t with a relative error of 6.6e-7 up to |z| = 14.5 (at 0, with these fp32 constants;
+// beyond, e^(-z^2 / 2) is 0): the tail keeps its digits, and the derivative has the same exponential.
 template <int ACT>
 __device__ inline void activation(float z, float &a, float &d) {
   if (ACT == kSilu) {
