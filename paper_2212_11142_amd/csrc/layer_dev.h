@@ -76,10 +76,7 @@ __device__ inline void store_piece(void *row, int e, int width, const float *v) 
   }
 }
 
-// Values of a type that the launch gives.
-__device__ inline float load_any(int dtype, const void *p, int64_t i) {
-  return dtype == GP_BF16 ? Bf16::load(p, i) : dtype == GP_FP16 ? Fp16::load(p, i) : Fp32::load(p, i);
-}
+// A value of a type that the launch gives.
 __device__ inline void store_any(int dtype, void *p, int64_t i, float v) {
   if (dtype == GP_BF16) Bf16::store(p, i, v);
   else if (dtype == GP_FP16) Fp16::store(p, i, v);
