@@ -11,6 +11,7 @@
 // operand's tile in LDS has either its rows running along the summed axis (ROW) or the summed
 // axis' rows running along its own (COL), which the transposing reads turn. Copies go to LDS
 // directly, the next step's while this one's products run.
+#include "gated_tiles.h"
 #include "layer_dev.h"
 
 namespace bgp {
@@ -161,20 +162,6 @@ __device__ inline void run_steps(int64_t count, Begin begin, Copy copy, Read rea
   }
   // (what was asked for past the end: a block's place in LDS ends with it)
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-}
-
-// Tile of a block: neighbours in m share an XCD's cache for the n side, eight m tiles to a group.
-struct Tile {
-  int m, n;
-};
-__device__ inline Tile tile_of(unsigned block, unsigned blocks, int nm, int nn) {
-  // blocks go round the 8 XCDs: each gets a run of tiles
-  const unsigned per = blocks / 8, more = blocks % 8, x = block % 8;
-  const unsigned i = x * per + min(x, more) + block / 8;
-  constexpr unsigned kGroup = 8;
-  const unsigned group = i / (kGroup * nn), in = i - group * kGroup * nn;
-  const unsigned size = min(kGroup, nm - group * kGroup);
-  return {(int)(group * kGroup + in % size), (int)(in / size)};
 }
 
 // ------------------------------------------------------------------ results
