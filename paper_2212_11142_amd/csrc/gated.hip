@@ -891,8 +891,8 @@ struct Plan {
   int sx, sw;                          // parts of dx's and of dW's summed axis
   int64_t nx, nw, lx, lw;              // blocks, and a block's steps
 };
-// Steps of a part at least: 1,021 x 520 x 1,368 with one group of wavefronts a tile and 8 19.6 us and 5.2 for adding
-// the parts, with 16 23.6 and 4.1, with 4 19.8 and 5.5; with two groups and 8 19.2 and 4.0, with 16 21.2 and 4.0.
+// Steps of a part at least: 1,021 x 520 x 1,368 in fp16 with one group of wavefronts a tile and 8 20.9 us and 5.2 for
+// adding the parts, with 16 25.7 and 4.3, with 4 20.9 and 5.5; with two groups and 8 20.0 and 4.3, with 16 22.5 and 4.1.
 constexpr int kLeast = 8;
 Plan plan_of(int64_t rows, int64_t width, int64_t hidden, bool big, bool groups) {
   const int size = big ? 256 : 128;
@@ -911,8 +911,8 @@ Plan plan_of(int64_t rows, int64_t width, int64_t hidden, bool big, bool groups)
 }
 // By the time of a step of either size, measured with full tiles: 1.8 us of 256 x 256, one block a compute
 // unit; 1.2 of 128 x 128, two. Two groups of wavefronts a tile where each block has a compute unit of its own and
-// more steps than a few: the gradient of 1,021 x 2,048 x 512 36 us, 49 with one group; 1,024 x 1,024 x 1,024 35 and
-// 41; 1,021 x 520 x 1,368 35.5 and 37.3; 128 x 64 x 64, of two steps, 12.1 and 11.3.
+// more steps than a few: the gradient of 1,021 x 2,048 x 512 36 us, 49 with one group; 1,024 x 1,024 x 1,024 33 and
+// 39; 1,021 x 520 x 1,368 34.1 and 35.7 (fp16: 35.6 and 37.6); 128 x 64 x 64, of two steps, 12.1 and 11.3.
 Plan plan_of(int64_t rows, int64_t width, int64_t hidden) {
   const Plan a = plan_of(rows, width, hidden, true, false), b = plan_of(rows, width, hidden, false, false);
   auto time = [](const Plan &p, double step, int places) {
